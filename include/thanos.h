@@ -330,6 +330,123 @@ size_t thanos_dense_product_workspace(int64_t M, int64_t N, int64_t K);
 thanos_status_t thanos_fp32_fma_probe(float* out, int64_t out_elems, int32_t ctas, int32_t iters,
                                       double* flop_out, void* stream);
 
+/*
+ * Recovery of a pruned layer, 1: the projection with low-rank adapters.
+ *
+ * A pruned weight W stays as it is and many tasks' (or requests') adapters (A_i, B_i, s_i) of rank
+ * r run beside it; every token names its adapter or none:
+ *
+ *     V[t] = X[t] A_i^T,   Y[t] = X[t] W^T + s_i V[t] B_i^T      i = index[t]
+ *     V[t] = 0,            Y[t] = X[t] W^T                       index[t] = -1
+ *
+ *  Y        device [n_tok, c] of dtype, leading dimension ldy >= c (elements).
+ *  V        device fp32 [n_tok, r] or NULL: kept for thanos_adapter_backward.
+ *  X        device [n_tok, b] of dtype, leading dimension ldx >= b, ldx % 8 == 0.
+ *  W        device [c, b] of dtype, leading dimension ldw >= b, ldw % 8 == 0.
+ *  A        device [n_adapters, r, b] of dtype, dense.   B  device [n_adapters, c, r], dense.
+ *  index    device int32 [n_tok], -1 or 0 <= index < n_adapters, in any order.  Any other value is
+ *           taken as -1 and reported in the status word (THANOS_ERR_INVALID_ARG).
+ *  scale    device fp32 [n_adapters]: s_i.
+ *  n_adapters may be 0: then A, B, scale, index are not read and V is not written (all may be NULL).
+ *  8 <= b <= 65536, b % 8 == 0; 1 <= c <= 2^20; 0 <= n_tok <= 2^24 (0 is a no-op);
+ *  1 <= r <= 128 (ignored when n_adapters is 0).
+ *  Sums are fp32.  With 16-bit types s_i V[t] is rounded to bf16 before it meets B_i, and Y once.
+ *  workspace: thanos_adapter_workspace_bytes(0, ...) bytes.  Its first int32 is the device status
+ *           word of the call, cleared when the call starts.
+ * The result does not depend on the order of concurrent work: the same inputs give the same bits.
+ * Outputs must not overlap inputs.
+ */
+thanos_status_t thanos_adapter_forward(void* Y, int64_t ldy, float* V, const void* X, int64_t ldx,
+                                       const void* W, int64_t ldw, const void* A, const void* B,
+                                       const int32_t* index, const float* scale,
+                                       thanos_dtype_t dtype, int64_t n_tok, int64_t c, int64_t b,
+                                       int64_t n_adapters, int32_t r, void* workspace,
+                                       size_t ws_bytes, void* stream);
+
+/*
+ * Gradients of thanos_adapter_forward (W and s are constants):
+ *
+ *     U[t] = s_i dY[t] B_i,   dX[t] = dY[t] W + U[t] A_i,
+ *     dA_i = sum over the tokens of adapter i of U[t]^T X[t],
+ *     dB_i = s_i sum over the same tokens of dY[t]^T V[t].
+ *
+ *  dX       device [n_tok, b] of dtype, leading dimension lddx >= b, or NULL (not wanted).
+ *  dA, dB   device fp32, dense, shaped like A and B; both or neither NULL.  accumulate == 0: written
+ *           (0 for an adapter without tokens), else added to.
+ *  dY       device [n_tok, c] of dtype, leading dimension lddy >= c (any).
+ *  V        device fp32 [n_tok, r], from thanos_adapter_forward.  X and V are read only when dA and
+ *           dB are wanted and may be NULL otherwise.
+ *  Everything else as in thanos_adapter_forward; n_tok == 0 still writes zero gradients.
+ *  workspace: thanos_adapter_workspace_bytes(1, ...) bytes, status word as above.
+ * Sums over tokens have a fixed order: the same inputs give the same bits.
+ */
+thanos_status_t thanos_adapter_backward(void* dX, int64_t lddx, float* dA, float* dB,
+                                        int32_t accumulate, const void* dY, int64_t lddy,
+                                        const void* X, int64_t ldx, const float* V, const void* W,
+                                        int64_t ldw, const void* A, const void* B,
+                                        const int32_t* index, const float* scale,
+                                        thanos_dtype_t dtype, int64_t n_tok, int64_t c, int64_t b,
+                                        int64_t n_adapters, int32_t r, void* workspace,
+                                        size_t ws_bytes, void* stream);
+
+/* Workspace of thanos_adapter_forward (backward == 0) or thanos_adapter_backward (!= 0); 0 if the
+ * arguments are not accepted. */
+size_t thanos_adapter_workspace_bytes(int32_t backward, int64_t n_tok, int64_t c, int64_t b,
+                                      int64_t n_adapters, int32_t r, thanos_dtype_t dtype);
+
+/*
+ * Recovery of a pruned layer, 2: the orthogonalised update.
+ *
+ * Newton-Schulz iteration on each of `batch` matrices G [m, n] (the shorter side's products are
+ * formed, whichever it is):
+ *
+ *     X_0 = G / (||G||_F + eps),   S = X_k X_k^T,   X_{k+1} = a X_k + (b S + c S S) X_k
+ *
+ * `steps` times; O = X_steps.  With (a, b, c) = (3.4445, -4.7750, 2.0315) and five steps this moves
+ * the singular values of G to between about 0.7 and 1.2.
+ *
+ *  O        device bf16 [batch, m, n], dense.
+ *  G        device [batch, m, n] of gdtype, dense.
+ *  coef     HOST float[3]: a, b, c.  Finite; they have to keep the iteration bounded: operands of
+ *           the products are held in fp16, scaled for singular values up to about 2.
+ *  1 <= steps <= 32, eps >= 0; 0 <= batch <= 65535 (0 is a no-op), 1 <= m, n <= 65536.
+ *  A zero matrix gives zeros (eps > 0); a matrix with an infinity or NaN gives NaN.
+ *  workspace: thanos_orthogonal_workspace_bytes(batch, m, n) bytes; its first int32 is the device
+ *           status word of the call.
+ * Same inputs, same bits.
+ */
+thanos_status_t thanos_orthogonalise(void* O, const void* G, thanos_dtype_t gdtype, int64_t batch,
+                                     int64_t m, int64_t n, const float* coef, int32_t steps,
+                                     float eps, void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * One optimiser step that keeps a pruned layer pruned.  With g = G where mask is 0 and 0 where it
+ * is 1 (whatever G holds there):
+ *
+ *     M_out = momentum M_in + g
+ *     g'    = nesterov ? g + momentum M_out : M_out         (both 0 where mask is 1)
+ *     W_out = (1 - lr weight_decay) W_in - lr gain O(g')    exact 0 where mask is 1
+ *
+ * with O() as in thanos_orthogonalise.
+ *
+ *  W_in, W_out  device [batch, m, n] of wdtype, dense; may be the same buffer.
+ *  M_in, M_out  device fp32 [batch, m, n], dense; may be the same buffer.
+ *  G        device [batch, m, n] of gdtype, dense.
+ *  mask     device uint8 [batch, m, n] or NULL: non-zero = removed, as thanos_prune_layer writes it.
+ * Everything else as in thanos_orthogonalise.
+ */
+thanos_status_t thanos_orthogonal_step(void* W_out, const void* W_in, thanos_dtype_t wdtype,
+                                       float* M_out, const float* M_in, const void* G,
+                                       thanos_dtype_t gdtype, const uint8_t* mask, int64_t batch,
+                                       int64_t m, int64_t n, float lr, float gain, float momentum,
+                                       int32_t nesterov, float weight_decay, const float* coef,
+                                       int32_t steps, float eps, void* workspace, size_t ws_bytes,
+                                       void* stream);
+
+/* Workspace of thanos_orthogonalise and thanos_orthogonal_step; 0 if the arguments are not
+ * accepted. */
+size_t thanos_orthogonal_workspace_bytes(int64_t batch, int64_t m, int64_t n);
+
 /* Minimum workspace in bytes for a call (see thanos_ws_which_t); 0 for unsupported shapes. */
 size_t thanos_workspace_bytes(int32_t which, int64_t c, int64_t b, int32_t B, thanos_dtype_t dtype);
 

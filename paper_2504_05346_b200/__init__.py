@@ -21,6 +21,11 @@ from .binding import (  # noqa: F401
     fp32_fma_probe,
     prune_layer_outliers,
     prune_layer_structured,
+    adapter_forward,
+    adapter_backward,
+    orthogonalise,
+    orthogonal_step,
+    NEWTON_SCHULZ,
     workspace_bytes,
     launch_count,
     status_string,

@@ -2,6 +2,7 @@
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from dataclasses import dataclass
@@ -113,6 +114,22 @@ def load_library():
     lib.thanos_dense_product.restype = i32
     lib.thanos_dense_product_workspace.argtypes = [i64, i64, i64]
     lib.thanos_dense_product_workspace.restype = sz
+    f32 = ctypes.c_float
+    lib.thanos_adapter_forward.argtypes = [vp, i64, vp, vp, i64, vp, i64, vp, vp, vp, vp, i32, i64,
+                                           i64, i64, i64, i32, vp, sz, vp]
+    lib.thanos_adapter_forward.restype = i32
+    lib.thanos_adapter_backward.argtypes = [vp, i64, vp, vp, i32, vp, i64, vp, i64, vp, vp, i64, vp,
+                                            vp, vp, vp, i32, i64, i64, i64, i64, i32, vp, sz, vp]
+    lib.thanos_adapter_backward.restype = i32
+    lib.thanos_adapter_workspace_bytes.argtypes = [i32, i64, i64, i64, i64, i32, i32]
+    lib.thanos_adapter_workspace_bytes.restype = sz
+    lib.thanos_orthogonalise.argtypes = [vp, vp, i32, i64, i64, i64, vp, i32, f32, vp, sz, vp]
+    lib.thanos_orthogonalise.restype = i32
+    lib.thanos_orthogonal_step.argtypes = [vp, vp, i32, vp, vp, vp, i32, vp, i64, i64, i64, f32, f32,
+                                           f32, i32, f32, vp, i32, f32, vp, sz, vp]
+    lib.thanos_orthogonal_step.restype = i32
+    lib.thanos_orthogonal_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.thanos_orthogonal_workspace_bytes.restype = sz
     lib.thanos_fp32_fma_probe.argtypes = [vp, i64, i32, i32, ctypes.POINTER(ctypes.c_double), vp]
     lib.thanos_fp32_fma_probe.restype = i32
     lib.thanos_workspace_bytes.argtypes = [i32, i64, i64, i32, i32]
@@ -469,3 +486,244 @@ def prune_layer_structured(W: torch.Tensor, factor: torch.Tensor, xnorm: torch.T
     if st.status != 0:
         raise ThanosError(st.status, "thanos_prune_layer_structured (index %d)" % st.err_index)
     return out, colrm, flags, st
+
+
+# ------------------------------------------------------------------ recovery of a pruned layer
+def _alloc_scope(stream):
+    """Buffers made for a call on another stream come from that stream's pool: the caching
+    allocator then neither hands out memory that the current stream still uses nor takes it back
+    before the call is done."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def _rows(t: torch.Tensor, cols: int, name: str) -> int:
+    """Leading dimension of a CUDA matrix with `cols` columns and unit inner stride."""
+    if not t.is_cuda or t.dim() != 2 or t.shape[1] != cols:
+        raise ValueError("%s must be a CUDA matrix with %d columns" % (name, cols))
+    if t.shape[0] > 1:
+        if cols > 1 and t.stride(1) != 1:
+            raise ValueError("%s must have unit inner stride" % name)
+        return t.stride(0)
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError("%s must have unit inner stride" % name)
+    return (cols + 7) // 8 * 8   # one row: its stride is never used
+
+
+def _dense(t: torch.Tensor, shape, dtype, name: str) -> torch.Tensor:
+    if not t.is_cuda or not t.is_contiguous() or tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        raise ValueError("%s must be a contiguous CUDA %s tensor of shape %s"
+                         % (name, dtype, tuple(shape)))
+    return t
+
+
+def _same_device(*ts):
+    for t in ts[1:]:
+        if t is not None and t.device != ts[0].device:
+            raise ValueError("all tensors must be on one device")
+
+
+def _adapters(X, W, A, B, index, scale):
+    """Checked sizes (T, c, b, n, r) and dtype code of an adapted projection."""
+    dt = _dtype_code(X)
+    if W.dim() != 2 or W.dtype != X.dtype:
+        raise ValueError("W must be a matrix of X's dtype")
+    c, b = W.shape
+    T = X.shape[0]
+    if A is None:
+        if not (B is None and index is None and scale is None):
+            raise ValueError("without A there is no B, index or scale either")
+        return T, c, b, 0, 0, dt
+    if A.dim() != 3:
+        raise ValueError("A must have the shape [n_adapters, r, b]")
+    n, r = A.shape[0], A.shape[1]
+    _dense(A, (n, r, b), X.dtype, "A")
+    _dense(B, (n, c, r), X.dtype, "B")
+    _dense(index, (T,), torch.int32, "index")
+    _dense(scale, (n,), torch.float32, "scale")
+    _same_device(X, W, A, B, index, scale)
+    return T, c, b, n, r, dt
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _status(workspace: torch.Tensor, where: str) -> None:
+    st = int(workspace[:4].view(torch.int32).item())
+    if st != 0:
+        raise ThanosError(st, where + " (device)")
+
+
+def adapter_forward(X: torch.Tensor, W: torch.Tensor, A: Optional[torch.Tensor] = None,
+                    B: Optional[torch.Tensor] = None, index: Optional[torch.Tensor] = None,
+                    scale: Optional[torch.Tensor] = None, stream=None,
+                    workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                    V: Optional[torch.Tensor] = None, check: bool = False):
+    """thanos_adapter_forward: Y[t] = X[t] W^T + scale[i] (X[t] A[i]^T) B[i]^T with i = index[t],
+    -1 for a token without adapter.  X [T, b], W [c, b], A [n, r, b], B [n, c, r] share a dtype
+    (float32 or bfloat16); index int32 [T], scale float32 [n].  Returns (Y, V): V float32 [T, r]
+    holds X[t] A[i]^T for adapter_backward (None without adapters).  With check=True the call's
+    device status word is read back (this waits for the call)."""
+    lib = load_library()
+    T, c, b, n, r, dt = _adapters(X, W, A, B, index, scale)
+    ldx, ldw = _rows(X, b, "X"), _rows(W, b, "W")
+    with _on(X):
+        with _alloc_scope(stream):
+            if out is None:
+                out = torch.empty((T, c), dtype=X.dtype, device=X.device)
+            if V is None and n > 0:
+                V = torch.empty((T, r), dtype=torch.float32, device=X.device)
+            if workspace is None:
+                workspace = _ws(lib.thanos_adapter_workspace_bytes(0, T, c, b, n, r, dt), X.device)
+        if out.dtype != X.dtype or out.shape[0] != T:
+            raise ValueError("out must be a [T, c] tensor of X's dtype")
+        ldy = _rows(out, c, "out")
+        if n > 0:
+            _dense(V, (T, r), torch.float32, "V")
+        _same_device(X, W, out, V, workspace)
+        _check(lib.thanos_adapter_forward(out.data_ptr(), ldy, _ptr(V), X.data_ptr(), ldx,
+                                          W.data_ptr(), ldw, _ptr(A), _ptr(B), _ptr(index),
+                                          _ptr(scale), dt, T, c, b, n, r, workspace.data_ptr(),
+                                          workspace.numel(), _stream_ptr(stream)),
+               "thanos_adapter_forward")
+        if check:
+            _status(workspace, "thanos_adapter_forward")
+    return out, V
+
+
+def adapter_backward(dY: torch.Tensor, X: Optional[torch.Tensor], V: Optional[torch.Tensor],
+                     W: torch.Tensor, A: Optional[torch.Tensor] = None,
+                     B: Optional[torch.Tensor] = None, index: Optional[torch.Tensor] = None,
+                     scale: Optional[torch.Tensor] = None, need_dx: bool = True,
+                     dA: Optional[torch.Tensor] = None, dB: Optional[torch.Tensor] = None,
+                     accumulate: bool = False, need_grads: bool = True, stream=None,
+                     workspace: Optional[torch.Tensor] = None, dX: Optional[torch.Tensor] = None,
+                     check: bool = False):
+    """thanos_adapter_backward: (dX, dA, dB) of adapter_forward for the output gradient dY [T, c].
+    V is what adapter_forward returned.  dA, dB are float32, shaped like A and B; with
+    accumulate=True they are added to (pass them in).  need_dx=False / need_grads=False leave a
+    part out (None is returned for it; X and V may then be None without gradients)."""
+    lib = load_library()
+    T, c, b, n, r, dt = _adapters(dY, W, A, B, index, scale)
+    lddy, ldw = _rows(dY, c, "dY"), _rows(W, b, "W")
+    need_grads = need_grads and n > 0
+    ldx = 0
+    if need_grads:
+        if X is None or V is None:
+            raise ValueError("the adapters' gradients need X and V")
+        if X.dtype != dY.dtype or X.shape[0] != T:
+            raise ValueError("X must be a [T, b] tensor of dY's dtype")
+        ldx = _rows(X, b, "X")
+        _dense(V, (T, r), torch.float32, "V")
+    if accumulate and (dA is None or dB is None) and need_grads:
+        raise ValueError("accumulate=True needs dA and dB")
+    with _on(dY):
+        with _alloc_scope(stream):
+            if need_dx and dX is None:
+                dX = torch.empty((T, b), dtype=dY.dtype, device=dY.device)
+            if need_grads and dA is None:
+                dA = torch.empty((n, r, b), dtype=torch.float32, device=dY.device)
+            if need_grads and dB is None:
+                dB = torch.empty((n, c, r), dtype=torch.float32, device=dY.device)
+            if workspace is None:
+                workspace = _ws(lib.thanos_adapter_workspace_bytes(1, T, c, b, n, r, dt), dY.device)
+        lddx = 0
+        if need_dx:
+            if dX.dtype != dY.dtype or dX.shape[0] != T:
+                raise ValueError("dX must be a [T, b] tensor of dY's dtype")
+            lddx = _rows(dX, b, "dX")
+        else:
+            dX = None
+        if need_grads:
+            _dense(dA, (n, r, b), torch.float32, "dA")
+            _dense(dB, (n, c, r), torch.float32, "dB")
+        else:
+            dA = dB = None
+        _same_device(dY, W, X if need_grads else None, V if need_grads else None, dX, dA, dB,
+                     workspace)
+        _check(lib.thanos_adapter_backward(_ptr(dX), lddx, _ptr(dA), _ptr(dB),
+                                           1 if accumulate else 0, dY.data_ptr(), lddy,
+                                           _ptr(X) if need_grads else None, ldx,
+                                           _ptr(V) if need_grads else None, W.data_ptr(), ldw,
+                                           _ptr(A), _ptr(B), _ptr(index), _ptr(scale), dt, T, c, b,
+                                           n, r, workspace.data_ptr(), workspace.numel(),
+                                           _stream_ptr(stream)), "thanos_adapter_backward")
+        if check:
+            _status(workspace, "thanos_adapter_backward")
+    return dX, dA, dB
+
+
+NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)  # quintic with a steep slope at zero, five steps
+
+
+def _matrices(G: torch.Tensor):
+    if G.dim() not in (2, 3):
+        raise ValueError("expected a matrix or a batch of matrices")
+    return (1 if G.dim() == 2 else G.shape[0]), G.shape[-2], G.shape[-1]
+
+
+def orthogonalise(G: torch.Tensor, steps: int = 5, coef=NEWTON_SCHULZ, eps: float = 1e-7,
+                  stream=None, workspace: Optional[torch.Tensor] = None,
+                  out: Optional[torch.Tensor] = None, check: bool = False) -> torch.Tensor:
+    """thanos_orthogonalise: Newton-Schulz iteration on G [m, n] or [batch, m, n] (float32 or
+    bfloat16, contiguous); returns bfloat16 of the same shape."""
+    lib = load_library()
+    k, m, n = _matrices(G)
+    dt = _dtype_code(G)
+    _dense(G, G.shape, G.dtype, "G")
+    with _on(G):
+        with _alloc_scope(stream):
+            if out is None:
+                out = torch.empty(G.shape, dtype=torch.bfloat16, device=G.device)
+            if workspace is None:
+                workspace = _ws(lib.thanos_orthogonal_workspace_bytes(k, m, n), G.device)
+        _dense(out, G.shape, torch.bfloat16, "out")
+        _same_device(G, out, workspace)
+        abc = (ctypes.c_float * 3)(*coef)
+        _check(lib.thanos_orthogonalise(out.data_ptr(), G.data_ptr(), dt, k, m, n, abc, steps,
+                                        float(eps), workspace.data_ptr(), workspace.numel(),
+                                        _stream_ptr(stream)), "thanos_orthogonalise")
+        if check:
+            _status(workspace, "thanos_orthogonalise")
+    return out
+
+
+def orthogonal_step(W: torch.Tensor, M: torch.Tensor, G: torch.Tensor,
+                    mask: Optional[torch.Tensor] = None, lr: float = 2e-4, gain: float = 1.0,
+                    momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0,
+                    steps: int = 5, coef=NEWTON_SCHULZ, eps: float = 1e-7, stream=None,
+                    workspace: Optional[torch.Tensor] = None, W_out: Optional[torch.Tensor] = None,
+                    M_out: Optional[torch.Tensor] = None, check: bool = False):
+    """thanos_orthogonal_step: momentum, orthogonalised update and new weights in one call; weights
+    that `mask` (uint8, non-zero = removed) marks stay exact zeros and take no part.  W, G float32
+    or bfloat16, M float32, all [m, n] or [batch, m, n] and contiguous.  Returns (W_out, M_out);
+    pass W_out=W, M_out=M to update in place."""
+    lib = load_library()
+    k, m, n = _matrices(G)
+    wdt, gdt = _dtype_code(W), _dtype_code(G)
+    _dense(G, G.shape, G.dtype, "G")
+    _dense(W, G.shape, W.dtype, "W")
+    _dense(M, G.shape, torch.float32, "M")
+    if mask is not None:
+        _dense(mask, G.shape, torch.uint8, "mask")
+    with _on(G):
+        with _alloc_scope(stream):
+            if W_out is None:
+                W_out = torch.empty_like(W)
+            if M_out is None:
+                M_out = torch.empty_like(M)
+            if workspace is None:
+                workspace = _ws(lib.thanos_orthogonal_workspace_bytes(k, m, n), G.device)
+        _dense(W_out, G.shape, W.dtype, "W_out")
+        _dense(M_out, G.shape, torch.float32, "M_out")
+        _same_device(G, W, M, mask, W_out, M_out, workspace)
+        abc = (ctypes.c_float * 3)(*coef)
+        _check(lib.thanos_orthogonal_step(W_out.data_ptr(), W.data_ptr(), wdt, M_out.data_ptr(),
+                                          M.data_ptr(), G.data_ptr(), gdt, _ptr(mask), k, m, n,
+                                          float(lr), float(gain), float(momentum),
+                                          1 if nesterov else 0, float(weight_decay), abc, steps,
+                                          float(eps), workspace.data_ptr(), workspace.numel(),
+                                          _stream_ptr(stream)), "thanos_orthogonal_step")
+        if check:
+            _status(workspace, "thanos_orthogonal_step")
+    return W_out, M_out
