@@ -2,8 +2,10 @@
 //   V[t] = X[t] A_i^T,  Y[t] = X[t] W^T + s_i V[t] B_i^T
 //   U[t] = s_i dY[t] B_i,  dX[t] = dY[t] W + U[t] A_i,  dA_i = sum_t U[t]^T X[t],
 //   dB_i = s_i sum_t dY[t]^T V[t]
+#include "proj_gemm.cuh"
 #include "recovery.cuh"
 #include "simt_gemm.cuh"
+#include "tc_common.cuh"
 
 namespace thanos {
 namespace {
@@ -136,6 +138,21 @@ thanos_status_t forward(const AdapterArgs& a, int32_t* status, float* V, cudaStr
 }
 
 template <typename E>
+thanos_status_t simple_grads(const AdapterArgs& a, const float* U, cudaStream_t stream) {
+  const int64_t nr = a.n * a.r;
+  const unsigned gy = (unsigned)(nr < 65535 ? nr : 65535), gz = (unsigned)ceil_div(nr, 65535);
+  grad_kernel<E, false><<<dim3((unsigned)ceil_div(a.b, 256), gy, gz), 256, 0, stream>>>(
+      a.dA, U, static_cast<const E*>(a.X), a.ldx, a.index, a.scale, a.T, (int)a.b, (int)a.n, a.r,
+      a.accumulate);
+  THANOS_CHECK_LAUNCH();
+  grad_kernel<E, true><<<dim3((unsigned)ceil_div(a.c, 256), gy, gz), 256, 0, stream>>>(
+      a.dB, a.Vin, static_cast<const E*>(a.in), a.ldi, a.index, a.scale, a.T, (int)a.c, (int)a.n,
+      a.r, a.accumulate);
+  THANOS_CHECK_LAUNCH();
+  return THANOS_OK;
+}
+
+template <typename E>
 thanos_status_t backward(const AdapterArgs& a, int32_t* status, float* U, cudaStream_t stream) {
   if (a.n > 0) {
     const int64_t warps = a.T * a.r;
@@ -145,48 +162,374 @@ thanos_status_t backward(const AdapterArgs& a, int32_t* status, float* U, cudaSt
     THANOS_CHECK_LAUNCH();
   }
   if (a.out) THANOS_TRY((project<E, true>(a, U, stream)));
-  if (a.dA) {
-    const int64_t nr = a.n * a.r;
-    const unsigned gy = (unsigned)(nr < 65535 ? nr : 65535), gz = (unsigned)ceil_div(nr, 65535);
-    grad_kernel<E, false><<<dim3((unsigned)ceil_div(a.b, 256), gy, gz), 256, 0, stream>>>(
-        a.dA, U, static_cast<const E*>(a.X), a.ldx, a.index, a.scale, a.T, (int)a.b, (int)a.n, a.r,
-        a.accumulate);
-    THANOS_CHECK_LAUNCH();
-    grad_kernel<E, true><<<dim3((unsigned)ceil_div(a.c, 256), gy, gz), 256, 0, stream>>>(
-        a.dB, a.Vin, static_cast<const E*>(a.in), a.ldi, a.index, a.scale, a.T, (int)a.c, (int)a.n,
-        a.r, a.accumulate);
-    THANOS_CHECK_LAUNCH();
+  if (a.dA) THANOS_TRY(simple_grads<E>(a, U, stream));
+  return THANOS_OK;
+}
+
+
+// ---------------------------------------------------------------------------- 16-bit operands
+using bf16 = __nv_bfloat16;
+
+// What the tensor-core kernels need of a call before they start; blocks by number:
+//   [0, n_list)          the distinct adapters of a token tile, by first occurrence
+//   next n_copy          16-byte aligned copies: rows of dY, or the adapters' B with padded ranks
+//   next n_turn          B_i [c, r] -> [r, c] (the skinny product's operand in the backward pass)
+//   the rest             V of a few tokens, a CTA per token and four ranks
+struct FrontParams {
+  int32_t* status;
+  const int32_t* index;
+  int32_t* count;
+  int32_t* list;
+  int T, nt, n, n_list;
+  const bf16* copy_src;
+  bf16* copy_dst;
+  int64_t copy_rows, copy_ls, copy_ld;
+  int copy_cols, n_copy;
+  const bf16* turn_src;
+  bf16* turn_dst;
+  int64_t turn_ld;
+  int c, r, n_turn;
+  const bf16* X;
+  int64_t ldx;
+  const bf16* A;
+  float* V;
+  int b;
+};
+
+constexpr int SHRINK_RANKS = 4;   // ranks of a token that one CTA computes
+
+__device__ __forceinline__ float dot8(const uint4& a, const uint4& b, float s) {
+  const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    s = fmaf(__uint_as_float(x[e] << 16), __uint_as_float(y[e] << 16), s);
+    s = fmaf(__uint_as_float(x[e] & 0xFFFF0000u), __uint_as_float(y[e] & 0xFFFF0000u), s);
   }
+  return s;
+}
+
+__global__ void __launch_bounds__(256) front_kernel(const FrontParams p) {
+  __shared__ float sh[64 * 65];
+  grid_dependency_wait();
+  grid_dependents_launch();
+  const int tid = threadIdx.x;
+  int blk = blockIdx.x;
+  if (blk == 0 && tid == 0) *p.status = 0;
+  if (blk < p.n_list) {
+    int* ids = reinterpret_cast<int*>(sh);
+    int* base = ids + 256;
+    const int t = blk * p.nt + tid;
+    const int i = tid < p.nt && t < p.T ? adapter_of(p.index, t, p.n) : -1;
+    ids[tid] = i;
+    __syncthreads();
+    bool first = i >= 0;
+    for (int u = 0; u < p.nt; ++u)
+      if (u < tid && ids[u] == i) first = false;
+    const unsigned vote = __ballot_sync(0xffffffffu, first);
+    if ((tid & 31) == 0) base[tid >> 5] = __popc(vote);
+    __syncthreads();
+    int at = __popc(vote & ((1u << (tid & 31)) - 1u)), all = 0;
+    for (int w = 0; w < 8; ++w) {
+      if (w < (tid >> 5)) at += base[w];
+      all += base[w];
+    }
+    if (first) p.list[(int64_t)blk * p.nt + at] = i;
+    if (tid == 0) p.count[blk] = all;
+    return;
+  }
+  blk -= p.n_list;
+  if (blk < p.n_copy) {
+    const int64_t total = p.copy_rows * p.copy_cols;
+    for (int64_t e = (int64_t)blk * 256 + tid; e < total; e += (int64_t)p.n_copy * 256) {
+      const int64_t row = e / p.copy_cols;
+      p.copy_dst[row * p.copy_ld + (e - row * p.copy_cols)] =
+          p.copy_src[row * p.copy_ls + (e - row * p.copy_cols)];
+    }
+    return;
+  }
+  blk -= p.n_copy;
+  if (blk < p.n_turn) {
+    // 64 rows of one B_i at a time through shared memory
+    const int tiles = (p.c + 63) / 64;
+    const int64_t units = (int64_t)p.n * tiles;
+    for (int64_t u = blk; u < units; u += p.n_turn) {
+      const int64_t i = u / tiles;
+      const int c0 = (int)(u - i * tiles) * 64;
+      for (int j0 = 0; j0 < p.r; j0 += 64) {
+        const int nj = min(64, p.r - j0);
+        __syncthreads();
+        for (int e = tid; e < 64 * nj; e += 256) {
+          const int row = e / nj, j = e - row * nj;
+          if (c0 + row < p.c)
+            sh[j * 65 + row] = to_float(p.turn_src[(i * p.c + c0 + row) * p.r + j0 + j]);
+        }
+        __syncthreads();
+        for (int e = tid; e < 64 * nj; e += 256) {
+          const int j = e >> 6, row = e & 63;
+          if (c0 + row < p.c)
+            p.turn_dst[(i * p.r + j0 + j) * p.turn_ld + c0 + row] =
+                __float2bfloat16_rn(sh[j * 65 + row]);
+        }
+      }
+    }
+    return;
+  }
+  blk -= p.n_turn;
+  // V[t, j0 .. j0 + 3]: the warps take k in turns of 256, eight elements a lane
+  const int groups = (p.r + SHRINK_RANKS - 1) / SHRINK_RANKS;
+  const int t = blk / groups, j0 = (blk - t * groups) * SHRINK_RANKS;
+  const int i = adapter_of(p.index, t, p.n);
+  float s[SHRINK_RANKS] = {};
+  if (i >= 0) {
+    const bf16* x = p.X + (int64_t)t * p.ldx;
+    const bf16* a = p.A + ((int64_t)i * p.r + j0) * p.b;
+#pragma unroll 2
+    for (int k = tid * 8; k < p.b; k += 2048) {
+      const uint4 xv = *reinterpret_cast<const uint4*>(x + k);
+#pragma unroll
+      for (int j = 0; j < SHRINK_RANKS; ++j)
+        if (j0 + j < p.r)
+          s[j] = dot8(xv, *reinterpret_cast<const uint4*>(a + (int64_t)j * p.b + k), s[j]);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < SHRINK_RANKS; ++j) {
+    for (int o = 16; o > 0; o >>= 1) s[j] += __shfl_xor_sync(0xffffffffu, s[j], o);
+    if ((tid & 31) == 0) sh[j * 8 + (tid >> 5)] = s[j];
+  }
+  __syncthreads();
+  if (tid < SHRINK_RANKS && j0 + tid < p.r) {
+    float v = 0.f;
+    for (int w = 0; w < 8; ++w) v += sh[tid * 8 + w];
+    p.V[(int64_t)t * p.r + j0 + tid] = v;
+  }
+}
+
+thanos_status_t launch_front(const FrontParams& p, int64_t shrink_blocks, cudaStream_t stream) {
+  const int64_t blocks = (int64_t)p.n_list + p.n_copy + p.n_turn + shrink_blocks;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)blocks, 1, 1);
+  cfg.blockDim = dim3(256, 1, 1);
+  cfg.stream = stream;
+  count_launch();
+  THANOS_CUDA(cudaLaunchKernelEx(&cfg, front_kernel, p));
+  return THANOS_OK;
+}
+
+// Few tokens: V by dot products in the first launch; more: one more launch on the tensor cores.
+bool few_tokens(const AdapterArgs& a) { return a.T <= 64; }
+
+struct Layout {
+  int32_t* status;
+  float* R;          // V or U
+  int32_t* count;
+  int32_t* list;
+  bf16* copy;        // padded B (forward) or dY (backward)
+  bf16* turned;      // backward: B_i transposed
+};
+
+bool carve(Arena& ar, Layout& L, bool backward, int64_t T, int64_t c, int64_t n, int r,
+           bool copy_dy) {
+  const int64_t nt = proj_token_tile(T, c), tiles = ceil_div(T, nt);
+  L.status = ar.take<int32_t>(64);
+  L.R = ar.take<float>((size_t)T * r);
+  L.count = ar.take<int32_t>((size_t)tiles);
+  L.list = ar.take<int32_t>((size_t)(tiles * nt));
+  L.copy = nullptr;
+  L.turned = nullptr;
+  if (!backward && r % 8) L.copy = ar.take<bf16>((size_t)n * c * round_up(r, 8));
+  if (backward && copy_dy) L.copy = ar.take<bf16>((size_t)T * round_up(c, 8));
+  if (backward) L.turned = ar.take<bf16>((size_t)n * r * round_up(c, 8));
+  return ar.ok();
+}
+
+thanos_status_t forward16(const AdapterArgs& a, void* workspace, size_t ws_bytes,
+                          cudaStream_t stream) {
+  Arena ar(workspace, ws_bytes);
+  Layout L;
+  if (!carve(ar, L, false, a.T, a.c, a.n, a.r, false)) return THANOS_ERR_WORKSPACE;
+  float* V = a.V ? a.V : L.R;
+  ProjArgs g;
+  g.M = (int)a.c;
+  g.N = (int)a.T;
+  g.K = (int)a.b;
+  g.A = a.W;
+  g.lda = a.ldw;
+  g.B = a.in;
+  g.ldb = a.ldi;
+  g.status = L.status;
+  g.out = a.out;
+  g.ldo = a.ldo;
+  g.nt = proj_token_tile(a.T, a.c);
+  if (a.n == 0) {
+    THANOS_CUDA(cudaMemsetAsync(L.status, 0, 16, stream));
+    return proj_gemm(g, stream);
+  }
+  FrontParams f = {};
+  f.status = L.status;
+  f.index = a.index;
+  f.count = L.count;
+  f.list = L.list;
+  f.T = (int)a.T;
+  f.nt = g.nt;
+  f.n = (int)a.n;
+  f.n_list = (int)ceil_div(a.T, g.nt);
+  f.r = a.r;
+  if (a.r % 8) {
+    f.copy_src = static_cast<const bf16*>(a.B);
+    f.copy_dst = L.copy;
+    f.copy_rows = a.n * a.c;
+    f.copy_cols = a.r;
+    f.copy_ls = a.r;
+    f.copy_ld = (int64_t)round_up(a.r, 8);
+    const int64_t want = ceil_div(f.copy_rows * a.r, 1024);
+    f.n_copy = (int)(want < 4 * NUM_SMS ? want : 4 * NUM_SMS);
+  }
+  int64_t shrink = 0;
+  if (few_tokens(a)) {
+    f.X = static_cast<const bf16*>(a.in);
+    f.ldx = a.ldi;
+    f.A = static_cast<const bf16*>(a.A);
+    f.V = V;
+    f.b = (int)a.b;
+    shrink = a.T * ceil_div(a.r, SHRINK_RANKS);
+  }
+  THANOS_TRY(launch_front(f, shrink, stream));
+  g.V = V;
+  g.index = a.index;
+  g.n_adapters = (int)a.n;
+  g.r = a.r;
+  g.tile_count = L.count;
+  g.tile_list = L.list;
+  if (!few_tokens(a)) {
+    ProjArgs s = g;
+    s.epi = PROJ_SHRINK;
+    s.A = a.A;
+    s.lda = a.b;
+    s.M = (int)(a.n * a.r);
+    THANOS_TRY(proj_gemm(s, stream));
+  }
+  g.scale = a.scale;
+  g.P = a.r % 8 ? static_cast<const void*>(L.copy) : a.B;
+  g.ldp = (int64_t)round_up(a.r, 8);
+  g.p_adapter = a.c * g.ldp;
+  g.early = 1;
+  return proj_gemm(g, stream);
+}
+
+thanos_status_t backward16(const AdapterArgs& a, void* workspace, size_t ws_bytes,
+                           cudaStream_t stream) {
+  const bool copy_dy = a.ldi % 8 != 0;
+  Arena ar(workspace, ws_bytes);
+  Layout L;
+  if (!carve(ar, L, true, a.T, a.c, a.n, a.r, copy_dy)) return THANOS_ERR_WORKSPACE;
+  const int64_t c8 = (int64_t)round_up(a.c, 8);
+  const void* dY = copy_dy ? static_cast<const void*>(L.copy) : a.in;
+  const int64_t lddy = copy_dy ? c8 : a.ldi;
+  ProjArgs g;
+  g.M = (int)a.b;
+  g.N = (int)a.T;
+  g.K = (int)a.c;
+  g.A = a.W;
+  g.lda = a.ldw;
+  g.a_mn = 1;
+  g.B = dY;
+  g.ldb = lddy;
+  g.status = L.status;
+  g.out = a.out;
+  g.ldo = a.ldo;
+  g.nt = proj_token_tile(a.T, a.b);
+  FrontParams f = {};
+  f.status = L.status;
+  f.index = a.index;
+  f.count = L.count;
+  f.list = L.list;
+  f.T = (int)a.T;
+  f.nt = g.nt;
+  f.n = (int)a.n;
+  f.n_list = a.n > 0 ? (int)ceil_div(a.T, g.nt) : 0;
+  f.r = a.r;
+  f.c = (int)a.c;
+  if (copy_dy) {
+    f.copy_src = static_cast<const bf16*>(a.in);
+    f.copy_dst = L.copy;
+    f.copy_rows = a.T;
+    f.copy_cols = (int)a.c;
+    f.copy_ls = a.ldi;
+    f.copy_ld = c8;
+    const int64_t want = ceil_div(a.T * a.c, 1024);
+    f.n_copy = (int)(want < 4 * NUM_SMS ? want : 4 * NUM_SMS);
+  }
+  if (a.n > 0) {
+    f.turn_src = static_cast<const bf16*>(a.B);
+    f.turn_dst = L.turned;
+    f.turn_ld = c8;
+    const int64_t want = a.n * ceil_div(a.c, 64);
+    f.n_turn = (int)(want < 4 * NUM_SMS ? want : 4 * NUM_SMS);
+  }
+  if (f.n_list + f.n_copy + f.n_turn > 0) THANOS_TRY(launch_front(f, 0, stream));
+  else THANOS_CUDA(cudaMemsetAsync(L.status, 0, 16, stream));
+  if (a.n > 0) {
+    g.V = L.R;
+    g.index = a.index;
+    g.n_adapters = (int)a.n;
+    g.r = a.r;
+    g.tile_count = L.count;
+    g.tile_list = L.list;
+    ProjArgs s = g;
+    s.epi = PROJ_SHRINK;
+    s.a_mn = 0;
+    s.A = L.turned;
+    s.lda = c8;
+    s.M = (int)(a.n * a.r);
+    s.scale = a.scale;
+    THANOS_TRY(proj_gemm(s, stream));
+    g.P = a.A;
+    g.ldp = a.b;
+    g.p_adapter = (int64_t)a.r * a.b;
+    g.early = copy_dy ? 0 : 1;
+  }
+  if (a.out) THANOS_TRY(proj_gemm(g, stream));
+  if (a.dA) THANOS_TRY(simple_grads<bf16>(a, L.R, stream));
   return THANOS_OK;
 }
 
 }  // namespace
 
-size_t adapter_workspace_bytes(bool, int64_t T, int64_t, int64_t, int64_t, int r, thanos_dtype_t) {
-  return 256 + round_up((size_t)T * (size_t)r * 4, 256);
+size_t adapter_workspace_bytes(bool backward, int64_t T, int64_t c, int64_t, int64_t n, int r,
+                               thanos_dtype_t dtype) {
+  const int64_t nt = proj_token_tile(T, c), tiles = ceil_div(T, nt);
+  size_t need = 256 + round_up((size_t)T * (size_t)r * 4, 256);
+  if (dtype == THANOS_F32) return need;
+  need += round_up((size_t)tiles * 4, 256) + round_up((size_t)(tiles * nt) * 4, 256);
+  const size_t c8 = round_up((size_t)c, 8);
+  if (!backward && r % 8) need += round_up((size_t)n * c * round_up(r, 8) * 2, 256);
+  // room for a copy of dY whose rows are not 16-byte aligned
+  if (backward) need += round_up((size_t)T * c8 * 2, 256) + round_up((size_t)n * r * c8 * 2, 256);
+  return need;
 }
 
 thanos_status_t adapter_forward_impl(const AdapterArgs& a, void* workspace, size_t ws_bytes,
                                      cudaStream_t stream) {
+  if (a.dtype == THANOS_BF16) return forward16(a, workspace, ws_bytes, stream);
   Arena ar(workspace, ws_bytes);
   int32_t* status = ar.take<int32_t>(64);
   float* V = ar.take<float>((size_t)a.T * a.r);
   if (!ar.ok()) return THANOS_ERR_WORKSPACE;
   if (a.V) V = a.V;
   THANOS_CUDA(cudaMemsetAsync(status, 0, 16, stream));
-  return a.dtype == THANOS_F32 ? forward<float>(a, status, V, stream)
-                               : forward<__nv_bfloat16>(a, status, V, stream);
+  return forward<float>(a, status, V, stream);
 }
 
 thanos_status_t adapter_backward_impl(const AdapterArgs& a, void* workspace, size_t ws_bytes,
                                       cudaStream_t stream) {
+  if (a.dtype == THANOS_BF16) return backward16(a, workspace, ws_bytes, stream);
   Arena ar(workspace, ws_bytes);
   int32_t* status = ar.take<int32_t>(64);
   float* U = ar.take<float>((size_t)a.T * a.r);
   if (!ar.ok()) return THANOS_ERR_WORKSPACE;
   THANOS_CUDA(cudaMemsetAsync(status, 0, 16, stream));
-  return a.dtype == THANOS_F32 ? backward<float>(a, status, U, stream)
-                               : backward<__nv_bfloat16>(a, status, U, stream);
+  return backward<float>(a, status, U, stream);
 }
 
 }  // namespace thanos

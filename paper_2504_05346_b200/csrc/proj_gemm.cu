@@ -1,0 +1,699 @@
+// See proj_gemm.cuh.  One CTA per 128 x nt output tile and slice of k; a cluster of 1, 2, 4 or 8
+// CTAs splits the k range of a tile when there are fewer tiles than SMs and adds the partial
+// sums over distributed shared memory in rank order (same inputs, same bits).
+//
+// Roles of the 256 threads:
+//   warp 0      TMA producer: per 64-wide k step the A tile (128 x 64, 128-byte swizzle; K-major, or
+//               two MN-major boxes of 64 m x 64 k) and the B tile (nt x 64, K-major)
+//   warp 1      tcgen05.mma issuer, 128 x nt x 16 each
+//   warps 2..3  adapter part: for every adapter that occurs in the token tile, k is extended by the
+//               adapter's rank in chunks of 16: the wide factor's rows come by TMA (32-byte swizzle;
+//               MN-major: 128-byte), the factor of the tokens, s_i V[t], is built here in bf16 with
+//               zero rows for tokens of other adapters.  0 times a non-finite weight would reach
+//               those tokens, so the chunk is scanned, non-finite weights become zeros and the
+//               epilogue adds their products to the adapter's own tokens.
+//   warps 4..7  epilogue
+// Every wait is bounded (see tc_common.cuh); on expiry the status word gets THANOS_ERR_TIMEOUT.
+#include "proj_gemm.cuh"
+
+#include "tc_common.cuh"
+
+namespace thanos {
+
+namespace {
+
+using namespace tc;
+
+constexpr int TM = 128;
+constexpr int BK = 64;
+constexpr int A_BYTES = TM * BK * 2;
+constexpr int CHUNK_BYTES = TM * 16 * 2;      // a 16-wide chunk of an adapter's wide factor
+constexpr int CHUNKS = 4;                     // chunks per stage
+constexpr int MAX_STAGES = 10;
+constexpr int NTHREADS = 256;
+constexpr int RING_BYTES = 200 * 1024;
+constexpr size_t SMEM_BYTES = RING_BYTES + 1024 /*align*/ + 512 /*barriers*/;
+static_assert((4 * MAX_STAGES + 4) * 8 <= 512, "barriers");
+
+struct Params {
+  int M, N, K, tiles_m, tiles_n, nt, stages, splits, batch_z;
+  int symmetric, f16, early;
+  int32_t* status;
+  // adapter part
+  void* out;
+  int64_t ldo;
+  float* V;
+  const int32_t* index;
+  const float* scale;
+  int n_adapters, r, chunks;          // chunks of 16 per adapter
+  const int32_t* tile_count;
+  const int32_t* tile_list;
+  const __nv_bfloat16* P;
+  int64_t ldp, p_adapter;
+  // iteration
+  float alpha, beta;
+  __half* S;
+  int64_t lds, s_batch;
+  __half* Pm;
+  const __half* Xh;
+  const __half* Xl;
+  __half* Yh;
+  __half* Yl;
+  int64_t ldx, x_batch;
+  __nv_bfloat16* O;
+  void* W_out;
+  const void* W_in;
+  const uint8_t* mask;
+  int w_bf16, tall;
+  float keep, rate;
+};
+
+__device__ __forceinline__ uint64_t make_desc(uint32_t addr, uint32_t lbo, uint32_t sbo,
+                                              uint32_t layout) {
+  uint64_t d = 0;
+  d |= (uint64_t)((addr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)(lbo >> 4) << 16;
+  d |= (uint64_t)(sbo >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)layout << 61;
+  return d;
+}
+constexpr uint32_t SW128 = 2, SW32 = 6;
+
+__device__ __forceinline__ float ld_cluster(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+
+__device__ __forceinline__ bool bf16_nonfinite(uint32_t h) { return (h & 0x7F80u) == 0x7F80u; }
+// any non-finite bf16 in a 16-byte vector
+__device__ __forceinline__ bool any_nonfinite(const uint4& q) {
+  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+  bool bad = false;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    bad = bad || bf16_nonfinite(w[e]) || bf16_nonfinite(w[e] >> 16);
+  return bad;
+}
+__device__ __forceinline__ uint32_t drop_nonfinite(uint32_t w) {
+  if (bf16_nonfinite(w)) w &= 0xFFFF0000u;
+  if (bf16_nonfinite(w >> 16)) w &= 0x0000FFFFu;
+  return w;
+}
+
+__device__ __forceinline__ int valid_adapter(const Params& p, int t) {
+  const int i = p.index[t];
+  return i >= 0 && i < p.n_adapters ? i : -1;
+}
+
+// The factor of a token's row: fp32 s_i V[t, j] rounded to bf16, as the tensor cores see it.
+__device__ __forceinline__ __nv_bfloat16 token_factor(const Params& p, int t, int i, int j) {
+  const float v = p.V[(int64_t)t * p.r + j];
+  return __float2bfloat16_rn(p.scale ? p.scale[i] * v : v);
+}
+
+template <bool AMN>
+__device__ __noinline__ float poison_terms(const Params& p, int m, int t) {
+  const int i = valid_adapter(p, t);
+  float s = 0.f;
+  if (i < 0) return s;
+  for (int j = 0; j < p.r; ++j) {
+    const __nv_bfloat16 w =
+        p.P[(int64_t)i * p.p_adapter + (AMN ? (int64_t)j * p.ldp + m : (int64_t)m * p.ldp + j)];
+    if (bf16_nonfinite(__bfloat16_as_ushort(w)))
+      s += __bfloat162float(token_factor(p, t, i, j)) * __bfloat162float(w);
+  }
+  return s;
+}
+
+__device__ __forceinline__ uint4 pack8_half(const float (&v)[8]) {
+  uint4 q;
+  uint32_t* w = reinterpret_cast<uint32_t*>(&q);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const __half2 h = __floats2half2_rn(v[2 * e], v[2 * e + 1]);
+    w[e] = *reinterpret_cast<const uint32_t*>(&h);
+  }
+  return q;
+}
+
+// Eight consecutive n of one m.
+template <bool AMN, int EPI>
+__device__ __forceinline__ void emit(const Params& p, int z, int m, int n0, float (&v)[8],
+                                     bool mirror, bool poisoned) {
+  if (m >= p.M || n0 >= p.N) return;
+  if constexpr (EPI == PROJ_OUT) {
+    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (n0 + e >= p.N) break;
+      float x = v[e];
+      if (poisoned) x += poison_terms<AMN>(p, m, n0 + e);
+      out[(int64_t)(n0 + e) * p.ldo + m] = __float2bfloat16_rn(x);
+    }
+  } else if constexpr (EPI == PROJ_SHRINK) {
+    const int i = m / p.r, j = m - i * p.r;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int t = n0 + e;
+      if (t >= p.N) break;
+      const int own = valid_adapter(p, t);
+      if (own == i) p.V[(int64_t)t * p.r + j] = p.scale ? p.scale[i] * v[e] : v[e];
+      else if (own < 0 && i == 0) p.V[(int64_t)t * p.r + j] = 0.f;
+    }
+  } else if constexpr (EPI == PROJ_GRAM || EPI == PROJ_POLY) {
+    const __half* S = p.S + (int64_t)z * p.s_batch;
+    __half* D = (EPI == PROJ_GRAM ? p.S : p.Pm) + (int64_t)z * p.s_batch;
+    float o[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      o[e] = p.alpha * v[e];
+      if (EPI == PROJ_POLY && n0 + e < p.N)
+        o[e] = fmaf(p.beta, __half2float(S[(int64_t)(n0 + e) * p.lds + m]), o[e]);
+      if (n0 + e < p.N) D[(int64_t)(n0 + e) * p.lds + m] = __float2half_rn(o[e]);
+    }
+    if (mirror) {
+      __half* row = D + (int64_t)m * p.lds + n0;
+      if (n0 + 8 <= p.N) {
+        *reinterpret_cast<uint4*>(row) = pack8_half(o);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (n0 + e < p.N) row[e] = __float2half_rn(o[e]);
+      }
+    }
+  } else {
+    float o[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      o[e] = 0.f;
+      if (n0 + e >= p.N) continue;
+      const int64_t at = (int64_t)z * p.x_batch + (int64_t)(n0 + e) * p.ldx + m;
+      const float x = __half2float(p.Xh[at]) + __half2float(p.Xl[at]);
+      o[e] = fmaf(p.beta, x, p.alpha * v[e]);
+      if constexpr (EPI == PROJ_NEXT) {
+        const __half h = __float2half_rn(o[e]);
+        p.Yh[at] = h;
+        p.Yl[at] = __float2half_rn(o[e] - __half2float(h));
+      }
+    }
+    if constexpr (EPI == PROJ_FINAL) {
+      const int64_t base = (int64_t)z * (int64_t)p.M * p.N;
+      const int64_t step = p.tall ? 1 : p.M;
+      const int64_t at0 = base + (p.tall ? (int64_t)m * p.N + n0 : (int64_t)n0 * p.M + m);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (n0 + e >= p.N) break;
+        const int64_t at = at0 + e * step;
+        if (p.O) {
+          p.O[at] = __float2bfloat16_rn(o[e]);
+        } else {
+          const float w0 = p.w_bf16
+                               ? __bfloat162float(static_cast<const __nv_bfloat16*>(p.W_in)[at])
+                               : static_cast<const float*>(p.W_in)[at];
+          float w = fmaf(-p.rate, o[e], p.keep * w0);
+          if (p.mask && p.mask[at] != 0) w = 0.f;
+          if (p.w_bf16) static_cast<__nv_bfloat16*>(p.W_out)[at] = __float2bfloat16_rn(w);
+          else static_cast<float*>(p.W_out)[at] = w;
+        }
+      }
+    }
+  }
+}
+
+template <bool AMN, int EPI>
+__global__ void __launch_bounds__(NTHREADS, 1)
+proj_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
+            const __grid_constant__ CUtensorMap mapP, const Params p) {
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* smem = reinterpret_cast<unsigned char*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + RING_BYTES);
+  // full, empty, factor ready, stage granted to the factor's warps (MAX_STAGES each), accumulator
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 4 * MAX_STAGES + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 4 * MAX_STAGES + 2);
+  int* poison = reinterpret_cast<int*>(bars + 4 * MAX_STAGES + 3);
+
+  const int warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31;
+  const uint32_t smem_base = smem_u32(smem);
+  const uint32_t bar_base = smem_u32(bars);
+  auto full_bar = [&](int s) { return bar_base + 8u * s; };
+  auto empty_bar = [&](int s) { return bar_base + 8u * (MAX_STAGES + s); };
+  auto factor_bar = [&](int s) { return bar_base + 8u * (2 * MAX_STAGES + s); };
+  auto grant_bar = [&](int s) { return bar_base + 8u * (3 * MAX_STAGES + s); };
+  const uint32_t done_bar = bar_base + 8u * (4 * MAX_STAGES);
+
+  const int S = p.splits;
+  const int rank = S > 1 ? (int)cluster_ctarank() : 0;
+  const int tile = (int)(blockIdx.x / S);
+  const int tn = tile / p.tiles_m, tm = tile - tn * p.tiles_m;
+  const int m0 = tm * TM, n0 = tn * p.nt;
+  const int z = blockIdx.y;
+  const int stage_bytes = A_BYTES + p.nt * BK * 2;
+
+  // symmetric results: the lower tiles are the mirror of the upper ones (nt == TM)
+  if (p.symmetric && tn < tm) return;
+  if constexpr (EPI == PROJ_SHRINK) {
+    // rows of adapters that no token of the tile uses are not needed (tile row 0 also writes the
+    // zeros of tokens without adapter)
+    grid_dependency_wait();
+    grid_dependents_launch();
+    if (tm > 0) {
+      const int lo = m0 / p.r, hi = (min(m0 + TM, p.M) - 1) / p.r;
+      const int cnt = p.tile_count[tn];
+      bool hit = false;
+      for (int q = lane; q < cnt; q += 32) {
+        const int i = p.tile_list[(int64_t)tn * p.nt + q];
+        hit = hit || (i >= lo && i <= hi);
+      }
+      if (!__any_sync(0xffffffffu, hit)) return;  // the same answer in every warp of the cluster
+    }
+  }
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < p.stages; ++s) {
+      mbar_init(full_bar(s), 1);
+      mbar_init(empty_bar(s), 1);
+      mbar_init(factor_bar(s), 2);
+      mbar_init(grant_bar(s), 1);
+    }
+    mbar_init(done_bar, 1);
+    *abort_flag = 0;
+    *poison = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
+                     smem_u32(tmem_slot)),
+                 "r"(p.nt)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+
+  if constexpr (EPI != PROJ_SHRINK) {
+    if (!p.early) grid_dependency_wait();
+    grid_dependents_launch();
+  }
+
+  const int nk = (p.K + BK - 1) / BK;
+  const int ks0 = (int)((int64_t)nk * rank / S), ks1 = (int)((int64_t)nk * (rank + 1) / S);
+  const bool ext = EPI == PROJ_OUT && p.n_adapters > 0;
+
+  if (warp == 0) {
+    // ------------------------------------------------------------ TMA producer
+    int s = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int ks = ks0; ks < ks1 && ok; ++ks) {
+      ok = mbar_wait(empty_bar(s), phase ^ 1u, abort_flag);
+      if (ok && lane == 0) {
+        const uint32_t dst = smem_base + (uint32_t)s * stage_bytes;
+        mbar_expect_tx(full_bar(s), stage_bytes);
+        if (AMN) {
+          tma_load_3d(dst, &mapA, full_bar(s), m0, ks * BK, z);
+          tma_load_3d(dst + A_BYTES / 2, &mapA, full_bar(s), m0 + 64, ks * BK, z);
+        } else {
+          tma_load_3d(dst, &mapA, full_bar(s), ks * BK, m0, z);
+        }
+        tma_load_3d(dst + A_BYTES, &mapB, full_bar(s), ks * BK, n0, z);
+      }
+      __syncwarp();
+      if (++s == p.stages) {
+        s = 0;
+        phase ^= 1u;
+      }
+    }
+    if (ext) {
+      grid_dependency_wait();
+      const int total = p.tile_count[tn] * p.chunks;
+      for (int e = rank; e * CHUNKS < total && ok; e += S) {
+        ok = mbar_wait(empty_bar(s), phase ^ 1u, abort_flag);
+        if (ok && lane == 0) {
+          const uint32_t dst = smem_base + (uint32_t)s * stage_bytes;
+          const int nc = min(CHUNKS, total - e * CHUNKS);
+          mbar_arrive(grant_bar(s));
+          mbar_expect_tx(full_bar(s), nc * CHUNK_BYTES);
+          for (int q = 0; q < nc; ++q) {
+            const int ch = e * CHUNKS + q;
+            const int who = p.tile_list[(int64_t)tn * p.nt + ch / p.chunks];
+            const int j = 16 * (ch % p.chunks);
+            if (AMN) {
+              tma_load_3d(dst + q * CHUNK_BYTES, &mapP, full_bar(s), m0, j, who);
+              tma_load_3d(dst + q * CHUNK_BYTES + CHUNK_BYTES / 2, &mapP, full_bar(s), m0 + 64, j,
+                          who);
+            } else {
+              tma_load_3d(dst + q * CHUNK_BYTES, &mapP, full_bar(s), j, m0, who);
+            }
+          }
+        }
+        __syncwarp();
+        if (++s == p.stages) {
+          s = 0;
+          phase ^= 1u;
+        }
+      }
+    }
+    // let copies that are still in flight land before the CTA's shared memory goes away
+    if (!ok) {
+      for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------ MMA issuer
+    uint32_t idesc = 0;
+    idesc |= 1u << 4;  // D fp32
+    if (!p.f16) idesc |= (1u << 7) | (1u << 10);  // both operands bf16 (0: both fp16)
+    if (AMN) idesc |= 1u << 15;
+    idesc |= (uint32_t)(p.nt >> 3) << 17;
+    idesc |= (uint32_t)(TM >> 4) << 24;
+    int s = 0;
+    uint32_t phase = 0, acc = 0;
+    bool ok = true;
+    for (int ks = ks0; ks < ks1 && ok; ++ks) {
+      ok = mbar_wait(full_bar(s), phase, abort_flag);
+      tc_fence_after();
+      if (ok && lane == 0) {
+        const uint32_t sa = smem_base + (uint32_t)s * stage_bytes;
+        const uint32_t sb = sa + A_BYTES;
+#pragma unroll
+        for (int k4 = 0; k4 < BK / 16; ++k4) {
+          const uint64_t ad = AMN ? make_desc(sa + k4 * 2048, A_BYTES / 2, 1024, SW128)
+                                  : make_desc(sa + k4 * 32, 16, 1024, SW128);
+          tc_mma_bf16(tmem_base, ad, make_desc(sb + k4 * 32, 16, 1024, SW128), idesc, acc);
+          acc = 1;
+        }
+        tc_commit(empty_bar(s));
+      }
+      __syncwarp();
+      if (++s == p.stages) {
+        s = 0;
+        phase ^= 1u;
+      }
+    }
+    if (ext && ok) {
+      grid_dependency_wait();
+      const int total = p.tile_count[tn] * p.chunks;
+      int o = 0;
+      for (int e = rank; e * CHUNKS < total && ok; e += S, ++o) {
+        ok = mbar_wait(full_bar(s), phase, abort_flag) &&
+             mbar_wait(factor_bar(s), (uint32_t)(o / p.stages) & 1u, abort_flag);
+        tc_fence_after();
+        if (ok && lane == 0) {
+          const uint32_t sa = smem_base + (uint32_t)s * stage_bytes;
+          const uint32_t sb = sa + A_BYTES;
+          const int nc = min(CHUNKS, total - e * CHUNKS);
+          for (int q = 0; q < nc; ++q) {
+            const uint32_t ca = sa + q * CHUNK_BYTES;
+            const uint64_t ad = AMN ? make_desc(ca, CHUNK_BYTES / 2, 1024, SW128)
+                                    : make_desc(ca, 16, 256, SW32);
+            tc_mma_bf16(tmem_base, ad, make_desc(sb + q * p.nt * 32, 16, 256, SW32), idesc, acc);
+            acc = 1;
+          }
+          tc_commit(empty_bar(s));
+        }
+        __syncwarp();
+        if (++s == p.stages) {
+          s = 0;
+          phase ^= 1u;
+        }
+      }
+    }
+    if (ok && lane == 0) tc_commit(done_bar);
+    __syncwarp();
+  } else if (warp < 4) {
+    // ------------------------------------------------------------ factors of the tokens
+    if (ext) {
+      grid_dependency_wait();
+      const int total = p.tile_count[tn] * p.chunks;
+      const int tid = threadIdx.x - 64;
+      int s = (ks1 - ks0) % p.stages;
+      uint32_t phase = (uint32_t)((ks1 - ks0) / p.stages) & 1u;
+      bool ok = true;
+      int o = 0;
+      for (int e = rank; e * CHUNKS < total && ok; e += S, ++o) {
+        // these warps skip the main k steps, so the parity of the ring's own barriers says nothing
+        // to them before the producer, which has seen every turn, hands the stage over
+        ok = mbar_wait(grant_bar(s), (uint32_t)(o / p.stages) & 1u, abort_flag);
+        if (!ok) break;
+        unsigned char* st = smem + (size_t)s * stage_bytes;
+        const int nc = min(CHUNKS, total - e * CHUNKS);
+        for (int q = 0; q < nc; ++q) {
+          const int ch = e * CHUNKS + q;
+          const int who = p.tile_list[(int64_t)tn * p.nt + ch / p.chunks];
+          const int j0 = 16 * (ch % p.chunks);
+          unsigned char* fac = st + A_BYTES + (size_t)q * p.nt * 32;
+          for (int row = tid; row < p.nt; row += 64) {
+            uint32_t w[8] = {};
+            const int t = n0 + row;
+            if (t < p.N && p.index[t] == who) {
+#pragma unroll
+              for (int j = 0; j < 16; ++j) {
+                const uint32_t h =
+                    j0 + j < p.r ? __bfloat16_as_ushort(token_factor(p, t, who, j0 + j)) : 0u;
+                w[j >> 1] |= h << (16 * (j & 1));
+              }
+            }
+            // 32-byte rows, 32-byte swizzle: the 16-byte halves swap every four rows
+            const int sw = ((row >> 2) & 1) << 4;
+            *reinterpret_cast<uint4*>(fac + row * 32 + (0 ^ sw)) = make_uint4(w[0], w[1], w[2], w[3]);
+            *reinterpret_cast<uint4*>(fac + row * 32 + (16 ^ sw)) = make_uint4(w[4], w[5], w[6], w[7]);
+          }
+        }
+        ok = mbar_wait(full_bar(s), phase, abort_flag);
+        if (!ok) break;
+        for (int q = tid; q < nc * (CHUNK_BYTES / 16); q += 64) {
+          uint4* at = reinterpret_cast<uint4*>(st) + q;
+          uint4 w = *at;
+          if (any_nonfinite(w)) {
+            w.x = drop_nonfinite(w.x);
+            w.y = drop_nonfinite(w.y);
+            w.z = drop_nonfinite(w.z);
+            w.w = drop_nonfinite(w.w);
+            *at = w;
+            *poison = 1;
+          }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(factor_bar(s));
+        if (++s == p.stages) {
+          s = 0;
+          phase ^= 1u;
+        }
+      }
+    }
+  } else {
+    // ------------------------------------------------------------ epilogue, one slice of k
+    const int g = warp & 3;
+    const bool ok = mbar_wait(done_bar, 0, abort_flag);
+    tc_fence_after();
+    if (ext || p.early) grid_dependency_wait();
+    const uint32_t taddr = tmem_base + ((uint32_t)(32 * g) << 16);
+    const int row = 32 * g + lane;
+    if (ext && tm == 0 && rank == 0) {
+      for (int t = n0 + row; t < min(n0 + p.nt, p.N); t += 128)
+        if (p.index[t] != -1 && valid_adapter(p, t) < 0)
+          atomicCAS(p.status, 0, (int)THANOS_ERR_INVALID_ARG);
+    }
+    if (ok) {
+      const bool poisoned = ext && *(volatile int*)poison != 0;
+      for (int cc = 0; cc < p.nt; cc += 32) {
+        uint32_t v[32];
+        tc_ld32(taddr + cc, v);
+        tc_wait_ld();
+        if (S == 1) {
+#pragma unroll
+          for (int c8 = 0; c8 < 4; ++c8) {
+            float f[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(v[8 * c8 + e]);
+            emit<AMN, EPI>(p, z, m0 + row, n0 + cc + 8 * c8, f, tn != tm, poisoned);
+          }
+        } else {
+          // partial sums [n][m] in the ring, whose operands have all been consumed
+          float* part = reinterpret_cast<float*>(smem);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) part[(cc + e) * TM + row] = __uint_as_float(v[e]);
+        }
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(p.nt)
+                 : "memory");
+  }
+  if (threadIdx.x == 0 && *abort_flag) atomicCAS(p.status, 0, (int)THANOS_ERR_TIMEOUT);
+  if (S > 1) {
+    cluster_sync_all();
+    if (warp >= 4) {
+      bool bad = false, poisoned = false;
+      for (int q = 0; q < S; ++q) {
+        bad = bad || ld_cluster_u32(map_to_cta(smem_u32((const void*)abort_flag), q)) != 0;
+        poisoned = poisoned || ld_cluster_u32(map_to_cta(smem_u32(poison), q)) != 0;
+      }
+      const int row = threadIdx.x - 128;
+      for (int c8 = rank; c8 * 8 < p.nt && !bad; c8 += S) {
+        float f[8] = {};
+        for (int q = 0; q < S; ++q) {
+          const uint32_t src = map_to_cta(smem_base, q) + (uint32_t)(c8 * 8 * TM + row) * 4u;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f[e] += ld_cluster(src + e * TM * 4);
+        }
+        emit<AMN, EPI>(p, z, m0 + row, n0 + c8 * 8, f, tn != tm, poisoned);
+      }
+    }
+    cluster_sync_all();  // no CTA leaves while another may still read its partial sums
+  }
+}
+
+bool make_map3(CUtensorMap* map, const void* base, bool f16, int64_t inner, int64_t rows, int64_t ld,
+               int64_t batch, int64_t batch_stride, int box_inner, int box_rows,
+               CUtensorMapSwizzle swizzle) {
+  EncodeTiledFn enc = encode_fn();
+  if (!enc) return false;
+  if (batch_stride <= 0) batch_stride = ld;  // never stepped over when it has one entry
+  cuuint64_t gdim[3] = {(cuuint64_t)inner, (cuuint64_t)rows, (cuuint64_t)batch};
+  cuuint64_t gstr[2] = {(cuuint64_t)ld * 2, (cuuint64_t)batch_stride * 2};
+  cuuint32_t box[3] = {(cuuint32_t)box_inner, (cuuint32_t)box_rows, 1};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return enc(map, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
+             const_cast<void*>(base), gdim, gstr, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <bool AMN, int EPI>
+thanos_status_t launch(const CUtensorMap& mA, const CUtensorMap& mB, const CUtensorMap& mP,
+                       const Params& p, cudaStream_t stream) {
+  static std::atomic<unsigned long long> done{0};
+  THANOS_CUDA(ensure_max_dyn_smem(proj_kernel<AMN, EPI>, (int)SMEM_BYTES, done));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((int64_t)p.tiles_m * p.tiles_n * p.splits), (unsigned)p.batch_z, 1);
+  cfg.blockDim = dim3(NTHREADS, 1, 1);
+  cfg.dynamicSmemBytes = SMEM_BYTES;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)p.splits;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  count_launch();
+  THANOS_CUDA(cudaLaunchKernelEx(&cfg, proj_kernel<AMN, EPI>, mA, mB, mP, p));
+  return THANOS_OK;
+}
+
+}  // namespace
+
+int proj_token_tile(int64_t N, int64_t) {
+  return N <= 32 ? 32 : N <= 64 ? 64 : N <= 128 ? 128 : 256;
+}
+
+thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
+  if (a.M <= 0 || a.N <= 0 || a.batch <= 0) return THANOS_OK;
+  if (a.lda % 8 || a.ldb % 8 || a.a_batch % 8 || a.b_batch % 8 || !aligned16(a.A) || !aligned16(a.B))
+    return THANOS_ERR_ALIGNMENT;
+  const bool symmetric = a.epi == PROJ_GRAM || a.epi == PROJ_POLY;
+  Params p = {};
+  p.M = a.M;
+  p.N = a.N;
+  p.K = a.K;
+  p.nt = symmetric ? TM : a.nt ? a.nt : proj_token_tile(a.N, a.M);
+  p.tiles_m = (a.M + TM - 1) / TM;
+  p.tiles_n = (a.N + p.nt - 1) / p.nt;
+  p.batch_z = a.batch;
+  p.symmetric = symmetric;
+  p.f16 = a.f16;
+  p.early = a.early;
+  p.status = a.status;
+  int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * a.batch;
+  if (symmetric) tiles = (int64_t)p.tiles_m * (p.tiles_m + 1) / 2 * a.batch;
+  const int nk = (a.K + BK - 1) / BK;
+  p.splits = 1;
+  while (p.splits < 8 && tiles * p.splits * 2 <= sm_count() && nk >= 8 * p.splits) p.splits *= 2;
+  if (tiles > (1 << 27) || a.batch > 65535) return THANOS_ERR_SHAPE;
+  const int stage_bytes = A_BYTES + p.nt * BK * 2;
+  p.stages = RING_BYTES / stage_bytes;
+  if (p.stages > MAX_STAGES) p.stages = MAX_STAGES;
+  p.out = a.out;
+  p.ldo = a.ldo;
+  p.V = a.V;
+  p.index = a.index;
+  p.scale = a.scale;
+  p.n_adapters = a.n_adapters;
+  p.r = a.r;
+  p.chunks = (a.r + 15) / 16;
+  p.tile_count = a.tile_count;
+  p.tile_list = a.tile_list;
+  p.P = static_cast<const __nv_bfloat16*>(a.P);
+  p.ldp = a.ldp;
+  p.p_adapter = a.p_adapter;
+  p.alpha = a.alpha;
+  p.beta = a.beta;
+  p.S = a.S;
+  p.lds = a.lds;
+  p.s_batch = a.s_batch;
+  p.Pm = a.Pm;
+  p.Xh = a.Xh;
+  p.Xl = a.Xl;
+  p.Yh = a.Yh;
+  p.Yl = a.Yl;
+  p.ldx = a.ldx;
+  p.x_batch = a.x_batch;
+  p.O = a.O;
+  p.W_out = a.W_out;
+  p.W_in = a.W_in;
+  p.mask = a.mask;
+  p.w_bf16 = a.w_bf16;
+  p.tall = a.tall;
+  p.keep = a.keep;
+  p.rate = a.rate;
+
+  CUtensorMap mA, mB, mP;
+  const CUtensorMapSwizzle sw = CU_TENSOR_MAP_SWIZZLE_128B;
+  const bool okA = a.a_mn ? make_map3(&mA, a.A, a.f16, a.M, a.K, a.lda, a.batch, a.a_batch, 64, BK, sw)
+                          : make_map3(&mA, a.A, a.f16, a.K, a.M, a.lda, a.batch, a.a_batch, BK, TM, sw);
+  if (!okA || !make_map3(&mB, a.B, a.f16, a.K, a.N, a.ldb, a.batch, a.b_batch, BK, p.nt, sw))
+    return THANOS_ERR_CUDA;
+  mP = mA;
+  if (a.epi == PROJ_OUT && a.n_adapters > 0) {
+    if (a.ldp % 8 || a.p_adapter % 8 || !aligned16(a.P)) return THANOS_ERR_ALIGNMENT;
+    const bool ok =
+        a.a_mn ? make_map3(&mP, a.P, false, a.M, a.r, a.ldp, a.n_adapters, a.p_adapter, 64, 16, sw)
+               : make_map3(&mP, a.P, false, a.r, a.M, a.ldp, a.n_adapters, a.p_adapter, 16, TM,
+                           CU_TENSOR_MAP_SWIZZLE_32B);
+    if (!ok) return THANOS_ERR_CUDA;
+  }
+  switch (a.epi) {
+    case PROJ_OUT:
+      return a.a_mn ? launch<true, PROJ_OUT>(mA, mB, mP, p, stream)
+                    : launch<false, PROJ_OUT>(mA, mB, mP, p, stream);
+    case PROJ_SHRINK:
+      return launch<false, PROJ_SHRINK>(mA, mB, mP, p, stream);
+    case PROJ_GRAM:
+      return launch<false, PROJ_GRAM>(mA, mB, mP, p, stream);
+    case PROJ_POLY:
+      return launch<false, PROJ_POLY>(mA, mB, mP, p, stream);
+    case PROJ_NEXT:
+      return launch<true, PROJ_NEXT>(mA, mB, mP, p, stream);
+    default:
+      return launch<true, PROJ_FINAL>(mA, mB, mP, p, stream);
+  }
+}
+
+}  // namespace thanos

@@ -1,0 +1,81 @@
+// 16-bit products on tcgen05 for the recovery operators: the adapted projection, its skinny
+// companion (V = X A^T) and the products of the Newton-Schulz iteration.
+//
+//   D[m, n] = sum_k A(m, k) B(n, k)     A [M, K] K-major, or stored [K, M] (MN-major); B [N, K]
+//
+// with m along the lanes of tensor memory.  Consecutive m are consecutive in memory for every
+// output (y[n, m] for token n and feature m), so a warp's stores are coalesced without a
+// transposition, and few tokens are simply a small n (down to 16 columns of the instruction).
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+
+namespace thanos {
+
+enum ProjEpilogue {
+  PROJ_OUT = 0,     // out[n, m] = bf16(D + adapter part)
+  PROJ_SHRINK = 1,  // m = (adapter, rank): V[n, rank] where the token's adapter is the row's
+  PROJ_GRAM = 2,    // S = alpha D, fp16, symmetric: upper tiles computed, mirror written
+  PROJ_POLY = 3,    // P = beta S + alpha D, fp16, symmetric
+  PROJ_NEXT = 4,    // X' = beta (hi + lo) + alpha D, as two fp16 planes
+  PROJ_FINAL = 5    // the same value, unscaled, into O (bf16) or the new weights
+};
+
+struct ProjArgs {
+  int M = 0, N = 0, K = 0, batch = 1;
+  const void* A = nullptr;
+  int64_t lda = 0, a_batch = 0;
+  int a_mn = 0;                  // A stored [K, M]
+  const void* B = nullptr;
+  int64_t ldb = 0, b_batch = 0;
+  int f16 = 0;                   // operands fp16 instead of bf16
+  int epi = PROJ_OUT;
+  int nt = 0;                    // tile width in n: 32, 64, 128, 256 (0: chosen here)
+  int early = 0;                 // operands do not depend on the previous launch of the stream
+  int32_t* status = nullptr;
+  // PROJ_OUT, PROJ_SHRINK
+  void* out = nullptr;           // bf16 [N, ldo]
+  int64_t ldo = 0;
+  float* V = nullptr;            // [N, r]: PROJ_OUT reads it (forward: V, backward: U); SHRINK writes
+  const int32_t* index = nullptr;
+  const float* scale = nullptr;  // factor of a row of V by its adapter, or null
+  int n_adapters = 0, r = 0;
+  const int32_t* tile_count = nullptr;  // distinct adapters of every token tile of width nt
+  const int32_t* tile_list = nullptr;   // [tiles, nt]
+  const void* P = nullptr;       // PROJ_OUT: the adapters' wide factor, bf16
+  int64_t ldp = 0, p_adapter = 0;       // a_mn == 0: [n][M][ldp]; else [n][r][ldp]
+  // PROJ_GRAM .. PROJ_FINAL
+  float alpha = 1.f, beta = 0.f;
+  __half* S = nullptr;           // GRAM: written, POLY: read
+  int64_t lds = 0, s_batch = 0;
+  __half* Pm = nullptr;          // POLY: written (strides as S)
+  const __half* Xh = nullptr;
+  const __half* Xl = nullptr;
+  __half* Yh = nullptr;
+  __half* Yl = nullptr;
+  int64_t ldx = 0, x_batch = 0;
+  __nv_bfloat16* O = nullptr;
+  void* W_out = nullptr;
+  const void* W_in = nullptr;
+  const uint8_t* mask = nullptr;
+  int w_bf16 = 0, tall = 0;
+  float keep = 1.f, rate = 0.f;
+};
+
+// Width of the token tiles that PROJ_OUT and PROJ_SHRINK use for N tokens and M features.
+int proj_token_tile(int64_t N, int64_t M);
+
+thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream);
+
+// Programmatic launch: the kernel may start while its predecessor in the stream still runs; it
+// waits (griddepcontrol.wait) before it touches anything the predecessor writes.
+__device__ __forceinline__ void grid_dependency_wait() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+__device__ __forceinline__ void grid_dependents_launch() {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
+}  // namespace thanos
