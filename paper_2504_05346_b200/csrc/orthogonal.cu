@@ -14,7 +14,7 @@
 namespace thanos {
 namespace {
 
-constexpr int MAX_PARTS = 256;   // partial sums of squares per matrix
+constexpr int MAX_PARTS = 1024;  // partial sums of squares per matrix
 
 __device__ __forceinline__ float load_any(const void* p, int bf16, int64_t e) {
   return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[e])
@@ -53,62 +53,145 @@ __device__ __forceinline__ float update_of(const StepParams& p, int64_t e, float
   return p.nesterov ? fmaf(p.momentum, mo, load_any(p.G, p.g_bf16, e)) : mo;
 }
 
-// New momentum and the sums of squares of the iteration's input.
+template <int VEC>
+__device__ __forceinline__ void load_vec(const void* p, int bf16, int64_t e, float (&v)[VEC]) {
+  if constexpr (VEC == 1) {
+    v[0] = load_any(p, bf16, e);
+  } else if (bf16) {
+    const uint2 q = *reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(p) + e);
+    v[0] = __uint_as_float(q.x << 16);
+    v[1] = __uint_as_float(q.x & 0xFFFF0000u);
+    v[2] = __uint_as_float(q.y << 16);
+    v[3] = __uint_as_float(q.y & 0xFFFF0000u);
+  } else {
+    const float4 q = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + e);
+    v[0] = q.x;
+    v[1] = q.y;
+    v[2] = q.z;
+    v[3] = q.w;
+  }
+}
+
+// VEC consecutive elements of the iteration's input; FIRST reads the old momentum and writes the
+// new one, else the new one is read.
+template <int VEC, bool FIRST>
+__device__ __forceinline__ void update_vec(const StepParams& p, int64_t at, float (&v)[VEC]) {
+  uint32_t gone = 0;
+  if (p.mask) {
+    if constexpr (VEC == 4) {
+      const uint32_t w = *reinterpret_cast<const uint32_t*>(p.mask + at);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) gone |= ((w >> (8 * e)) & 0xFFu ? 1u : 0u) << e;
+    } else {
+      gone = p.mask[at] != 0;
+    }
+  }
+  float g[VEC];
+  if (FIRST || !p.M_out || p.nesterov) load_vec<VEC>(p.G, p.g_bf16, at, g);
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) {
+    if ((gone >> e) & 1u) g[e] = 0.f;
+    v[e] = g[e];
+  }
+  if (!p.M_out) return;
+  float mo[VEC];
+  if (FIRST) {
+    load_vec<VEC>(p.M_in, 0, at, mo);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) mo[e] = fmaf(p.momentum, mo[e], g[e]);
+    if constexpr (VEC == 4) *reinterpret_cast<float4*>(p.M_out + at) = make_float4(mo[0], mo[1], mo[2], mo[3]);
+    else p.M_out[at] = mo[0];
+  } else {
+    load_vec<VEC>(p.M_out, 0, at, mo);
+  }
+#pragma unroll
+  for (int e = 0; e < VEC; ++e)
+    v[e] = (gone >> e) & 1u ? 0.f : p.nesterov ? fmaf(p.momentum, mo[e], g[e]) : mo[e];
+}
+
+// New momentum and the sums of squares of the iteration's input (fp32 over a thread's share, fp64
+// from there).
+template <int VEC>
 __global__ void __launch_bounds__(256) norm_kernel(const StepParams p) {
   __shared__ double red[8];
   if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.status = 0;
   const int64_t mn = (int64_t)p.m * p.n, base = (int64_t)blockIdx.y * mn;
   double sum = 0.0;
-  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < mn; e += 256ll * p.parts) {
-    float mo = 0.f;
-    if (p.M_out) {
-      const bool gone = p.mask && p.mask[base + e] != 0;
-      const float g = gone ? 0.f : load_any(p.G, p.g_bf16, base + e);
-      mo = fmaf(p.momentum, p.M_in[base + e], g);
-      p.M_out[base + e] = mo;
+  const int64_t step = 256ll * VEC * p.parts;
+  for (int64_t e0 = ((int64_t)blockIdx.x * 256 + threadIdx.x) * VEC; e0 < mn; e0 += 4 * step) {
+    float part = 0.f;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int64_t e = e0 + u * step;
+      if (e >= mn) break;
+      float v[VEC];
+      update_vec<VEC, true>(p, base + e, v);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) part = fmaf(v[i], v[i], part);
     }
-    const float v = update_of(p, base + e, mo);
-    sum += (double)v * (double)v;
+    sum += (double)part;
   }
   sum = block_sum(sum, red);
   if (threadIdx.x == 0) p.part[(int64_t)blockIdx.y * p.parts + blockIdx.x] = sum;
 }
 
+__device__ __forceinline__ void split_half(float x, uint32_t& hi, uint32_t& lo) {
+  const __half h = __float2half_rn(x);
+  hi = __half_as_ushort(h);
+  lo = __half_as_ushort(__float2half_rn(x - __half2float(h)));
+}
+
 // X_0 = unit * update / (norm + eps) as two fp16 planes [s, l], turned when the matrix is tall.
+template <int VEC>
 __global__ void __launch_bounds__(256) split_kernel(const StepParams p) {
   __shared__ double red[8];
   __shared__ float tile[64][65];
-  const double sq = block_sum(threadIdx.x < p.parts ? p.part[(int64_t)blockIdx.y * p.parts + threadIdx.x] : 0.0, red);
+  double sq = 0.0;
+  for (int i = threadIdx.x; i < p.parts; i += 256) sq += p.part[(int64_t)blockIdx.y * p.parts + i];
+  sq = block_sum(sq, red);
   const float f = p.unit / ((float)sqrt(sq) + p.eps);
   const int64_t base = (int64_t)blockIdx.y * (int64_t)p.m * p.n;
   const int tn = (p.n + 63) / 64;
   const int64_t tiles = (int64_t)((p.m + 63) / 64) * tn;
   for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
     const int r0 = (int)(t / tn) * 64, c0 = (int)(t % tn) * 64;
-    for (int e = threadIdx.x; e < 4096; e += 256) {
+#pragma unroll 4
+    for (int e = threadIdx.x * VEC; e < 4096; e += 256 * VEC) {
       const int r = e >> 6, c = e & 63;
       if (r0 + r >= p.m || c0 + c >= p.n) continue;
-      const int64_t at = base + (int64_t)(r0 + r) * p.n + c0 + c;
-      const float x = f * update_of(p, at, p.M_out ? p.M_out[at] : 0.f);
+      float x[VEC];
+      update_vec<VEC, false>(p, base + (int64_t)(r0 + r) * p.n + c0 + c, x);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) x[i] *= f;
       if (p.tall) {
-        tile[c][r] = x;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) tile[c + i][r] = x[i];
       } else {
         const int64_t o = (int64_t)blockIdx.y * p.x_batch + (int64_t)(r0 + r) * p.ldx + c0 + c;
-        const __half h = __float2half_rn(x);
-        p.Xh[o] = h;
-        p.Xl[o] = __float2half_rn(x - __half2float(h));
+        uint32_t hi[VEC], lo[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) split_half(x[i], hi[i], lo[i]);
+        if constexpr (VEC == 4) {
+          *reinterpret_cast<uint2*>(p.Xh + o) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+          *reinterpret_cast<uint2*>(p.Xl + o) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+        } else {
+          p.Xh[o] = __ushort_as_half((unsigned short)hi[0]);
+          p.Xl[o] = __ushort_as_half((unsigned short)lo[0]);
+        }
       }
     }
     if (p.tall) {
       __syncthreads();
-      for (int e = threadIdx.x; e < 4096; e += 256) {
+      for (int e = threadIdx.x * 2; e < 4096; e += 512) {
         const int c = e >> 6, r = e & 63;
         if (r0 + r >= p.m || c0 + c >= p.n) continue;
         const int64_t o = (int64_t)blockIdx.y * p.x_batch + (int64_t)(c0 + c) * p.ldx + r0 + r;
-        const float x = tile[c][r];
-        const __half h = __float2half_rn(x);
-        p.Xh[o] = h;
-        p.Xl[o] = __float2half_rn(x - __half2float(h));
+        uint32_t hi[2], lo[2];
+        split_half(tile[c][r], hi[0], lo[0]);
+        split_half(tile[c][r + 1], hi[1], lo[1]);
+        // a last row without a partner fills the padding of the leading dimension
+        *reinterpret_cast<uint32_t*>(p.Xh + o) = hi[0] | hi[1] << 16;
+        *reinterpret_cast<uint32_t*>(p.Xl + o) = lo[0] | lo[1] << 16;
       }
       __syncthreads();
     }
@@ -426,7 +509,7 @@ float pow2_at_most(double x, int most) {
 }
 
 int norm_parts(int64_t mn) {
-  const int64_t want = ceil_div(mn, 4096);
+  const int64_t want = ceil_div(mn, 8192);
   return (int)(want < MAX_PARTS ? want : MAX_PARTS);
 }
 
@@ -486,11 +569,18 @@ thanos_status_t orthogonal_impl(const OrthogonalArgs& a, void* workspace, size_t
   sp.Xl = X[0][1];
   sp.ldx = ldx;
   sp.x_batch = s * ldx;
-  norm_kernel<<<dim3(sp.parts, (unsigned)k), 256, 0, stream>>>(sp);
-  THANOS_CHECK_LAUNCH();
   const int64_t tiles = ceil_div(a.m, 64) * ceil_div(a.n, 64);
-  split_kernel<<<dim3((unsigned)(tiles < 8 * NUM_SMS ? tiles : 8 * NUM_SMS), (unsigned)k), 256, 0,
-                 stream>>>(sp);
+  const dim3 norm_grid((unsigned)sp.parts, (unsigned)k);
+  const dim3 split_grid((unsigned)(tiles < 8 * NUM_SMS ? tiles : 8 * NUM_SMS), (unsigned)k);
+  if (a.n % 4 == 0) {
+    norm_kernel<4><<<norm_grid, 256, 0, stream>>>(sp);
+    THANOS_CHECK_LAUNCH();
+    split_kernel<4><<<split_grid, 256, 0, stream>>>(sp);
+  } else {
+    norm_kernel<1><<<norm_grid, 256, 0, stream>>>(sp);
+    THANOS_CHECK_LAUNCH();
+    split_kernel<1><<<split_grid, 256, 0, stream>>>(sp);
+  }
   THANOS_CHECK_LAUNCH();
   ProjArgs g;
   g.batch = (int)k;

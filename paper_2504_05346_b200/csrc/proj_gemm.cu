@@ -2,7 +2,7 @@
 // CTAs splits the k range of a tile when there are fewer tiles than SMs and adds the partial
 // sums over distributed shared memory in rank order (same inputs, same bits).
 //
-// Roles of the 256 threads:
+// Roles of the 384 threads:
 //   warp 0      TMA producer: per 64-wide k step the A tile (128 x 64, 128-byte swizzle; K-major, or
 //               two MN-major boxes of 64 m x 64 k) and the B tile (nt x 64, K-major)
 //   warp 1      tcgen05.mma issuer, 128 x nt x 16 each
@@ -12,7 +12,7 @@
 //               zero rows for tokens of other adapters.  0 times a non-finite weight would reach
 //               those tokens, so the chunk is scanned, non-finite weights become zeros and the
 //               epilogue adds their products to the adapter's own tokens.
-//   warps 4..7  epilogue
+//   warps 4..11 epilogue: a quarter of the TMEM lanes and half of the columns each
 // Every wait is bounded (see tc_common.cuh); on expiry the status word gets THANOS_ERR_TIMEOUT.
 #include "proj_gemm.cuh"
 
@@ -30,7 +30,7 @@ constexpr int A_BYTES = TM * BK * 2;
 constexpr int CHUNK_BYTES = TM * 16 * 2;      // a 16-wide chunk of an adapter's wide factor
 constexpr int CHUNKS = 4;                     // chunks per stage
 constexpr int MAX_STAGES = 10;
-constexpr int NTHREADS = 256;
+constexpr int NTHREADS = 384;
 constexpr int RING_BYTES = 200 * 1024;
 constexpr size_t SMEM_BYTES = RING_BYTES + 1024 /*align*/ + 512 /*barriers*/;
 static_assert((4 * MAX_STAGES + 4) * 8 <= 512, "barriers");
@@ -118,6 +118,34 @@ __device__ __forceinline__ __nv_bfloat16 token_factor(const Params& p, int t, in
   return __float2bfloat16_rn(p.scale ? p.scale[i] * v : v);
 }
 
+// The 16 columns j0.. of a token's factor as packed bf16: s_i V[t, j] for the adapter `who`'s own
+// tokens, zeros for all others and beyond the rank.
+__device__ __forceinline__ void factor_row(const Params& p, int t, int who, int j0,
+                                           uint32_t (&w)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) w[e] = 0u;
+  if (t < p.N && p.index[t] == who) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      const uint32_t h =
+          j0 + j < p.r ? __bfloat16_as_ushort(token_factor(p, t, who, j0 + j)) : 0u;
+      w[j >> 1] |= h << (16 * (j & 1));
+    }
+  }
+}
+
+__device__ __forceinline__ void clean_vector(uint4* at, int* poison) {
+  uint4 w = *at;
+  if (any_nonfinite(w)) {
+    w.x = drop_nonfinite(w.x);
+    w.y = drop_nonfinite(w.y);
+    w.z = drop_nonfinite(w.z);
+    w.w = drop_nonfinite(w.w);
+    *at = w;
+    *poison = 1;
+  }
+}
+
 template <bool AMN>
 __device__ __noinline__ float poison_terms(const Params& p, int m, int t) {
   const int i = valid_adapter(p, t);
@@ -143,84 +171,131 @@ __device__ __forceinline__ uint4 pack8_half(const float (&v)[8]) {
   return q;
 }
 
-// Eight consecutive n of one m.
-template <bool AMN, int EPI>
-__device__ __forceinline__ void emit(const Params& p, int z, int m, int n0, float (&v)[8],
+// NC consecutive n of one m (a lane); n0 is a multiple of 8.
+template <bool AMN, int EPI, int NC>
+__device__ __forceinline__ void emit(const Params& p, int z, int m, int n0, float (&v)[NC],
                                      bool mirror, bool poisoned) {
   if (m >= p.M || n0 >= p.N) return;
+  const int nc = p.N - n0;  // columns that exist
   if constexpr (EPI == PROJ_OUT) {
-    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out);
+    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + (int64_t)n0 * p.ldo + m;
+    if (poisoned) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      if (n0 + e >= p.N) break;
-      float x = v[e];
-      if (poisoned) x += poison_terms<AMN>(p, m, n0 + e);
-      out[(int64_t)(n0 + e) * p.ldo + m] = __float2bfloat16_rn(x);
+      for (int e = 0; e < NC; ++e)
+        if (e < nc) v[e] += poison_terms<AMN>(p, m, n0 + e);
     }
+#pragma unroll
+    for (int e = 0; e < NC; ++e)
+      if (e < nc) out[(int64_t)e * p.ldo] = __float2bfloat16_rn(v[e]);
   } else if constexpr (EPI == PROJ_SHRINK) {
     const int i = m / p.r, j = m - i * p.r;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < NC; ++e) {
       const int t = n0 + e;
-      if (t >= p.N) break;
+      if (e >= nc) break;
       const int own = valid_adapter(p, t);
       if (own == i) p.V[(int64_t)t * p.r + j] = p.scale ? p.scale[i] * v[e] : v[e];
       else if (own < 0 && i == 0) p.V[(int64_t)t * p.r + j] = 0.f;
     }
   } else if constexpr (EPI == PROJ_GRAM || EPI == PROJ_POLY) {
-    const __half* S = p.S + (int64_t)z * p.s_batch;
     __half* D = (EPI == PROJ_GRAM ? p.S : p.Pm) + (int64_t)z * p.s_batch;
-    float o[8];
+    if constexpr (EPI == PROJ_POLY) {
+      const __half* S = p.S + (int64_t)z * p.s_batch + (int64_t)n0 * p.lds + m;
+      __half old[NC];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      o[e] = p.alpha * v[e];
-      if (EPI == PROJ_POLY && n0 + e < p.N)
-        o[e] = fmaf(p.beta, __half2float(S[(int64_t)(n0 + e) * p.lds + m]), o[e]);
-      if (n0 + e < p.N) D[(int64_t)(n0 + e) * p.lds + m] = __float2half_rn(o[e]);
+      for (int e = 0; e < NC; ++e) old[e] = e < nc ? S[(int64_t)e * p.lds] : __half(0.f);
+#pragma unroll
+      for (int e = 0; e < NC; ++e) v[e] = fmaf(p.beta, __half2float(old[e]), p.alpha * v[e]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < NC; ++e) v[e] *= p.alpha;
     }
+    __half* col = D + (int64_t)n0 * p.lds + m;
+#pragma unroll
+    for (int e = 0; e < NC; ++e)
+      if (e < nc) col[(int64_t)e * p.lds] = __float2half_rn(v[e]);
     if (mirror) {
       __half* row = D + (int64_t)m * p.lds + n0;
-      if (n0 + 8 <= p.N) {
-        *reinterpret_cast<uint4*>(row) = pack8_half(o);
-      } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (n0 + e < p.N) row[e] = __float2half_rn(o[e]);
+      for (int e8 = 0; e8 < NC; e8 += 8) {
+        if (e8 + 8 <= nc) {
+          float f[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f[e] = v[e8 + e];
+          *reinterpret_cast<uint4*>(row + e8) = pack8_half(f);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (e8 + e < nc) row[e8 + e] = __float2half_rn(v[e8 + e]);
+        }
       }
     }
   } else {
-    float o[8];
+    const int64_t at = (int64_t)z * p.x_batch + (int64_t)n0 * p.ldx + m;
+    __half hi[NC], lo[NC];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      o[e] = 0.f;
-      if (n0 + e >= p.N) continue;
-      const int64_t at = (int64_t)z * p.x_batch + (int64_t)(n0 + e) * p.ldx + m;
-      const float x = __half2float(p.Xh[at]) + __half2float(p.Xl[at]);
-      o[e] = fmaf(p.beta, x, p.alpha * v[e]);
-      if constexpr (EPI == PROJ_NEXT) {
-        const __half h = __float2half_rn(o[e]);
-        p.Yh[at] = h;
-        p.Yl[at] = __float2half_rn(o[e] - __half2float(h));
-      }
+    for (int e = 0; e < NC; ++e) {
+      hi[e] = e < nc ? p.Xh[at + (int64_t)e * p.ldx] : __half(0.f);
+      lo[e] = e < nc ? p.Xl[at + (int64_t)e * p.ldx] : __half(0.f);
     }
-    if constexpr (EPI == PROJ_FINAL) {
+#pragma unroll
+    for (int e = 0; e < NC; ++e)
+      v[e] = fmaf(p.beta, __half2float(hi[e]) + __half2float(lo[e]), p.alpha * v[e]);
+    if constexpr (EPI == PROJ_NEXT) {
+#pragma unroll
+      for (int e = 0; e < NC; ++e) {
+        if (e >= nc) break;
+        const __half h = __float2half_rn(v[e]);
+        p.Yh[at + (int64_t)e * p.ldx] = h;
+        p.Yl[at + (int64_t)e * p.ldx] = __float2half_rn(v[e] - __half2float(h));
+      }
+    } else {
       const int64_t base = (int64_t)z * (int64_t)p.M * p.N;
       const int64_t step = p.tall ? 1 : p.M;
       const int64_t at0 = base + (p.tall ? (int64_t)m * p.N + n0 : (int64_t)n0 * p.M + m);
+      if (p.O) {
+        if (p.tall && p.N % 8 == 0) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if (n0 + e >= p.N) break;
-        const int64_t at = at0 + e * step;
-        if (p.O) {
-          p.O[at] = __float2bfloat16_rn(o[e]);
+          for (int e8 = 0; e8 < NC; e8 += 8) {
+            if (e8 >= nc) break;
+            uint4 q;
+            uint32_t* w = reinterpret_cast<uint32_t*>(&q);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              w[e] = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(v[e8 + 2 * e])) |
+                     ((uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(v[e8 + 2 * e + 1])) << 16);
+            *reinterpret_cast<uint4*>(p.O + at0 + e8) = q;
+          }
         } else {
-          const float w0 = p.w_bf16
-                               ? __bfloat162float(static_cast<const __nv_bfloat16*>(p.W_in)[at])
-                               : static_cast<const float*>(p.W_in)[at];
-          float w = fmaf(-p.rate, o[e], p.keep * w0);
-          if (p.mask && p.mask[at] != 0) w = 0.f;
-          if (p.w_bf16) static_cast<__nv_bfloat16*>(p.W_out)[at] = __float2bfloat16_rn(w);
-          else static_cast<float*>(p.W_out)[at] = w;
+#pragma unroll
+          for (int e = 0; e < NC; ++e)
+            if (e < nc) p.O[at0 + e * step] = __float2bfloat16_rn(v[e]);
+        }
+      } else {
+        // loads first: W_in may be W_out, so the compiler cannot move them over the stores
+        float w[NC];
+#pragma unroll
+        for (int e = 0; e < NC; ++e) {
+          w[e] = 0.f;
+          if (e < nc)
+            w[e] = p.w_bf16 ? __bfloat162float(
+                                  static_cast<const __nv_bfloat16*>(p.W_in)[at0 + e * step])
+                            : static_cast<const float*>(p.W_in)[at0 + e * step];
+        }
+        uint32_t gone = 0;
+        if (p.mask) {
+#pragma unroll
+          for (int e = 0; e < NC; ++e)
+            if (e < nc && p.mask[at0 + e * step] != 0) gone |= 1u << e;
+        }
+#pragma unroll
+        for (int e = 0; e < NC; ++e) {
+          if (e >= nc) break;
+          const float x = (gone >> e) & 1u ? 0.f : fmaf(-p.rate, v[e], p.keep * w[e]);
+          if (p.w_bf16)
+            static_cast<__nv_bfloat16*>(p.W_out)[at0 + e * step] = __float2bfloat16_rn(x);
+          else
+            static_cast<float*>(p.W_out)[at0 + e * step] = x;
         }
       }
     }
@@ -453,16 +528,8 @@ proj_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
           const int j0 = 16 * (ch % p.chunks);
           unsigned char* fac = st + A_BYTES + (size_t)q * p.nt * 32;
           for (int row = tid; row < p.nt; row += 64) {
-            uint32_t w[8] = {};
-            const int t = n0 + row;
-            if (t < p.N && p.index[t] == who) {
-#pragma unroll
-              for (int j = 0; j < 16; ++j) {
-                const uint32_t h =
-                    j0 + j < p.r ? __bfloat16_as_ushort(token_factor(p, t, who, j0 + j)) : 0u;
-                w[j >> 1] |= h << (16 * (j & 1));
-              }
-            }
+            uint32_t w[8];
+            factor_row(p, n0 + row, who, j0, w);
             // 32-byte rows, 32-byte swizzle: the 16-byte halves swap every four rows
             const int sw = ((row >> 2) & 1) << 4;
             *reinterpret_cast<uint4*>(fac + row * 32 + (0 ^ sw)) = make_uint4(w[0], w[1], w[2], w[3]);
@@ -471,18 +538,8 @@ proj_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
         }
         ok = mbar_wait(full_bar(s), phase, abort_flag);
         if (!ok) break;
-        for (int q = tid; q < nc * (CHUNK_BYTES / 16); q += 64) {
-          uint4* at = reinterpret_cast<uint4*>(st) + q;
-          uint4 w = *at;
-          if (any_nonfinite(w)) {
-            w.x = drop_nonfinite(w.x);
-            w.y = drop_nonfinite(w.y);
-            w.z = drop_nonfinite(w.z);
-            w.w = drop_nonfinite(w.w);
-            *at = w;
-            *poison = 1;
-          }
-        }
+        for (int q = tid; q < nc * (CHUNK_BYTES / 16); q += 64)
+          clean_vector(reinterpret_cast<uint4*>(st) + q, poison);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) mbar_arrive(factor_bar(s));
@@ -501,29 +558,26 @@ proj_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
     const uint32_t taddr = tmem_base + ((uint32_t)(32 * g) << 16);
     const int row = 32 * g + lane;
     if (ext && tm == 0 && rank == 0) {
-      for (int t = n0 + row; t < min(n0 + p.nt, p.N); t += 128)
+      for (int t = n0 + (int)threadIdx.x - 128; t < min(n0 + p.nt, p.N); t += 256)
         if (p.index[t] != -1 && valid_adapter(p, t) < 0)
           atomicCAS(p.status, 0, (int)THANOS_ERR_INVALID_ARG);
     }
     if (ok) {
       const bool poisoned = ext && *(volatile int*)poison != 0;
-      for (int cc = 0; cc < p.nt; cc += 32) {
-        uint32_t v[32];
-        tc_ld32(taddr + cc, v);
+      for (int cc = 32 * ((warp - 4) >> 2); cc < p.nt; cc += 64) {
+        uint32_t u[32];
+        tc_ld32(taddr + cc, u);
         tc_wait_ld();
+        float v[32];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(u[e]);
         if (S == 1) {
-#pragma unroll
-          for (int c8 = 0; c8 < 4; ++c8) {
-            float f[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(v[8 * c8 + e]);
-            emit<AMN, EPI>(p, z, m0 + row, n0 + cc + 8 * c8, f, tn != tm, poisoned);
-          }
+          emit<AMN, EPI, 32>(p, z, m0 + row, n0 + cc, v, tn != tm, poisoned);
         } else {
           // partial sums [n][m] in the ring, whose operands have all been consumed
           float* part = reinterpret_cast<float*>(smem);
 #pragma unroll
-          for (int e = 0; e < 32; ++e) part[(cc + e) * TM + row] = __uint_as_float(v[e]);
+          for (int e = 0; e < 32; ++e) part[(cc + e) * TM + row] = v[e];
         }
       }
     }
@@ -544,19 +598,373 @@ proj_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
         bad = bad || ld_cluster_u32(map_to_cta(smem_u32((const void*)abort_flag), q)) != 0;
         poisoned = poisoned || ld_cluster_u32(map_to_cta(smem_u32(poison), q)) != 0;
       }
-      const int row = threadIdx.x - 128;
-      for (int c8 = rank; c8 * 8 < p.nt && !bad; c8 += S) {
+      const int row = (threadIdx.x - 128) & 127, half = (threadIdx.x - 128) >> 7;
+      for (int c8 = rank + S * half; c8 * 8 < p.nt && !bad; c8 += 2 * S) {
         float f[8] = {};
         for (int q = 0; q < S; ++q) {
           const uint32_t src = map_to_cta(smem_base, q) + (uint32_t)(c8 * 8 * TM + row) * 4u;
 #pragma unroll
           for (int e = 0; e < 8; ++e) f[e] += ld_cluster(src + e * TM * 4);
         }
-        emit<AMN, EPI>(p, z, m0 + row, n0 + c8 * 8, f, tn != tm, poisoned);
+        emit<AMN, EPI, 8>(p, z, m0 + row, n0 + c8 * 8, f, tn != tm, poisoned);
       }
     }
     cluster_sync_all();  // no CTA leaves while another may still read its partial sums
   }
+}
+
+// ------------------------------------------------------------------------------- CTA pairs
+// The same product on a persistent cluster of two CTAs with tcgen05.mma.cta_group::2: tiles of 256 x
+// nt, CTA r holds rows 128 r .. +127 in its tensor memory and loads only those and half of the n
+// rows, so an SM moves 32 KB instead of 48 KB through shared memory per 64-wide k step of a 256-wide
+// tile.  Two accumulators: the epilogue of a tile runs beside the next tile's products.
+constexpr int PTM = 256;
+constexpr int PSTAGES = 6;
+constexpr int PSTAGE_BYTES = 2 * A_BYTES;
+constexpr size_t PSMEM_BYTES = (size_t)PSTAGES * PSTAGE_BYTES + 1024 + 512;
+
+__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap* map,
+                                                 uint32_t lead_bar, int x, int y, int z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+      "[%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(lead_bar), "r"(x), "r"(y), "r"(z)
+      : "memory");
+}
+
+struct PairTile {
+  int z, tm, tn;
+};
+// Tiles by groups of eight columns, rows inside: the pairs that run at the same time share the
+// operands of about 8 x 9 tiles, which L2 holds.
+__device__ __forceinline__ PairTile pair_tile(const Params& p, int t) {
+  PairTile r;
+  if (p.symmetric) {
+    const int per = p.tiles_m * (p.tiles_m + 1) / 2;
+    r.z = t / per;
+    int u = t - r.z * per, col = 0;
+    while (u > col) {  // column col of the triangle has col + 1 tiles
+      u -= col + 1;
+      ++col;
+    }
+    r.tm = u;
+    r.tn = col;
+    return r;
+  }
+  const int per = p.tiles_m * p.tiles_n;
+  r.z = t / per;
+  int u = t - r.z * per;
+  const int group = u / (8 * p.tiles_m);
+  u -= group * 8 * p.tiles_m;
+  const int wide = min(8, p.tiles_n - 8 * group);
+  r.tm = u / wide;
+  r.tn = 8 * group + (u - r.tm * wide);
+  return r;
+}
+
+template <bool AMN, int EPI>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1)
+pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
+            const __grid_constant__ CUtensorMap mapP, const Params p, const int n_tiles) {
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* smem = reinterpret_cast<unsigned char*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + (size_t)PSTAGES * PSTAGE_BYTES);
+  // full, empty, factor ready (full and factor used in the first CTA), stage granted, chunk landed;
+  // then accumulator full (2) and empty (2, used in the first CTA)
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 5 * PSTAGES + 4);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 5 * PSTAGES + 5);
+  int* poison = reinterpret_cast<int*>(bars + 5 * PSTAGES + 6);
+
+  const int warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
+  const uint32_t smem_base = smem_u32(smem);
+  const uint32_t bar_base = smem_u32(bars);
+  auto full_bar = [&](int s) { return bar_base + 8u * s; };
+  auto empty_bar = [&](int s) { return bar_base + 8u * (PSTAGES + s); };
+  auto factor_bar = [&](int s) { return bar_base + 8u * (2 * PSTAGES + s); };
+  auto grant_bar = [&](int s) { return bar_base + 8u * (3 * PSTAGES + s); };
+  auto land_bar = [&](int s) { return bar_base + 8u * (4 * PSTAGES + s); };
+  auto tfull_bar = [&](int q) { return bar_base + 8u * (5 * PSTAGES + q); };
+  auto tempty_bar = [&](int q) { return bar_base + 8u * (5 * PSTAGES + 2 + q); };
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < PSTAGES; ++s) {
+      mbar_init(full_bar(s), 1);
+      mbar_init(empty_bar(s), 1);
+      mbar_init(factor_bar(s), 4);  // two warps in each CTA
+      mbar_init(grant_bar(s), 1);
+      mbar_init(land_bar(s), 1);
+    }
+    for (int q = 0; q < 2; ++q) {
+      mbar_init(tfull_bar(q), 1);
+      mbar_init(tempty_bar(q), 16);  // eight epilogue warps in each CTA
+    }
+    *abort_flag = 0;
+    *poison = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
+                     smem_u32(tmem_slot)),
+                 "r"(512)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();  // both CTAs' barriers are initialised before anything signals them
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+
+  if (!p.early) grid_dependency_wait();
+  grid_dependents_launch();
+
+  const int nk = (p.K + BK - 1) / BK;
+  const int half = p.nt / 2;  // n rows that this CTA loads
+  constexpr bool EXT = EPI == PROJ_OUT;
+  const bool ext = EXT && p.n_adapters > 0;
+
+  if (warp == 0) {
+    // ------------------------------------------------------------ TMA producer
+    int s = 0;
+    uint32_t phase = 0;
+    bool ok = true, waited = false;
+    for (int t = pair; t < n_tiles && ok; t += npairs) {
+      const PairTile tl = pair_tile(p, t);
+      const int m0 = tl.tm * PTM + 128 * (int)rank, n0 = tl.tn * p.nt + half * (int)rank;
+      for (int ks = 0; ks < nk && ok; ++ks) {
+        ok = mbar_wait(empty_bar(s), phase ^ 1u, abort_flag);
+        if (ok && lane == 0) {
+          const uint32_t dst = smem_base + (uint32_t)s * PSTAGE_BYTES;
+          const uint32_t lead = map_to_cta(full_bar(s), 0);
+          if (rank == 0) mbar_expect_tx(full_bar(s), 2 * (A_BYTES + half * BK * 2));
+          if (AMN) {
+            tma_load_3d_pair(dst, &mapA, lead, m0, ks * BK, tl.z);
+            tma_load_3d_pair(dst + A_BYTES / 2, &mapA, lead, m0 + 64, ks * BK, tl.z);
+          } else {
+            tma_load_3d_pair(dst, &mapA, lead, ks * BK, m0, tl.z);
+          }
+          tma_load_3d_pair(dst + A_BYTES, &mapB, lead, ks * BK, n0, tl.z);
+        }
+        __syncwarp();
+        if (++s == PSTAGES) {
+          s = 0;
+          phase ^= 1u;
+        }
+      }
+      if (ext && ok) {
+        if (!waited) grid_dependency_wait();
+        waited = true;
+        const int total = p.tile_count[tl.tn] * p.chunks;
+        for (int c0 = 0; c0 < total && ok; c0 += CHUNKS) {
+          ok = mbar_wait(empty_bar(s), phase ^ 1u, abort_flag);
+          if (ok && lane == 0) {
+            const uint32_t dst = smem_base + (uint32_t)s * PSTAGE_BYTES;
+            const int nc = min(CHUNKS, total - c0);
+            // the stage's readiness goes over the factor barrier; its turn on the full barrier is
+            // only kept in step
+            if (rank == 0) mbar_arrive(full_bar(s));
+            mbar_arrive(grant_bar(s));
+            mbar_expect_tx(land_bar(s), nc * CHUNK_BYTES);
+            for (int q = 0; q < nc; ++q) {
+              const int who = p.tile_list[(int64_t)tl.tn * p.nt + (c0 + q) / p.chunks];
+              const int j = 16 * ((c0 + q) % p.chunks);
+              if (AMN) {
+                tma_load_3d(dst + q * CHUNK_BYTES, &mapP, land_bar(s), m0, j, who);
+                tma_load_3d(dst + q * CHUNK_BYTES + CHUNK_BYTES / 2, &mapP, land_bar(s), m0 + 64, j,
+                            who);
+              } else {
+                tma_load_3d(dst + q * CHUNK_BYTES, &mapP, land_bar(s), j, m0, who);
+              }
+            }
+          }
+          __syncwarp();
+          if (++s == PSTAGES) {
+            s = 0;
+            phase ^= 1u;
+          }
+        }
+      }
+    }
+    // let copies that are still in flight land before the CTA's shared memory goes away
+    if (!ok) {
+      for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------ MMA issuer (first CTA only)
+    if (rank == 0) {
+      uint32_t idesc = 0;
+      idesc |= 1u << 4;  // D fp32
+      if (!p.f16) idesc |= (1u << 7) | (1u << 10);
+      if (AMN) idesc |= 1u << 15;
+      idesc |= (uint32_t)(p.nt >> 3) << 17;
+      idesc |= (uint32_t)(PTM >> 4) << 24;
+      int s = 0, q = 0;
+      uint32_t phase = 0, tphase = 0, turn = 0;  // turn: bit s = parity of stage s as adapter stage
+      bool ok = true, waited = false;
+      for (int t = pair; t < n_tiles && ok; t += npairs) {
+        const PairTile tl = pair_tile(p, t);
+        ok = mbar_wait(tempty_bar(q), tphase ^ 1u, abort_flag);
+        tc_fence_after();
+        const uint32_t d = tmem_base + (uint32_t)q * 256;
+        for (int ks = 0; ks < nk && ok; ++ks) {
+          ok = mbar_wait(full_bar(s), phase, abort_flag);
+          tc_fence_after();
+          if (ok && lane == 0) {
+            const uint32_t sa = smem_base + (uint32_t)s * PSTAGE_BYTES;
+            const uint32_t sb = sa + A_BYTES;
+#pragma unroll
+            for (int k4 = 0; k4 < BK / 16; ++k4) {
+              const uint64_t ad = AMN ? make_desc(sa + k4 * 2048, A_BYTES / 2, 1024, SW128)
+                                      : make_desc(sa + k4 * 32, 16, 1024, SW128);
+              tc_mma_bf16_pair(d, ad, make_desc(sb + k4 * 32, 16, 1024, SW128), idesc,
+                               (ks > 0 || k4 > 0) ? 1u : 0u);
+            }
+            tc_commit_pair(empty_bar(s));
+          }
+          __syncwarp();
+          if (++s == PSTAGES) {
+            s = 0;
+            phase ^= 1u;
+          }
+        }
+        if (ext && ok) {
+          if (!waited) grid_dependency_wait();
+          waited = true;
+          const int total = p.tile_count[tl.tn] * p.chunks;
+          for (int c0 = 0; c0 < total && ok; c0 += CHUNKS) {
+            ok = mbar_wait(full_bar(s), phase, abort_flag) &&
+                 mbar_wait(factor_bar(s), (turn >> s) & 1u, abort_flag);
+            turn ^= 1u << s;
+            tc_fence_after();
+            if (ok && lane == 0) {
+              const uint32_t sa = smem_base + (uint32_t)s * PSTAGE_BYTES;
+              const uint32_t sb = sa + A_BYTES;
+              const int nc = min(CHUNKS, total - c0);
+              for (int c = 0; c < nc; ++c) {
+                const uint32_t ca = sa + c * CHUNK_BYTES;
+                const uint64_t ad = AMN ? make_desc(ca, CHUNK_BYTES / 2, 1024, SW128)
+                                        : make_desc(ca, 16, 256, SW32);
+                tc_mma_bf16_pair(d, ad, make_desc(sb + c * 128 * 32, 16, 256, SW32), idesc, 1u);
+              }
+              tc_commit_pair(empty_bar(s));
+            }
+            __syncwarp();
+            if (++s == PSTAGES) {
+              s = 0;
+              phase ^= 1u;
+            }
+          }
+        }
+        if (ok && lane == 0) tc_commit_pair(tfull_bar(q));
+        __syncwarp();
+        if (++q == 2) {
+          q = 0;
+          tphase ^= 1u;
+        }
+      }
+    }
+  } else if (warp < 4) {
+    // ------------------------------------------------------------ factors of the tokens
+    if (ext) {
+      grid_dependency_wait();
+      const int tid = threadIdx.x - 64;
+      int s = 0;
+      uint32_t turn = 0;
+      bool ok = true;
+      for (int t = pair; t < n_tiles && ok; t += npairs) {
+        const PairTile tl = pair_tile(p, t);
+        const int n0 = tl.tn * p.nt + half * (int)rank;
+        const int total = p.tile_count[tl.tn] * p.chunks;
+        s = (s + nk) % PSTAGES;
+        for (int c0 = 0; c0 < total && ok; c0 += CHUNKS) {
+          const uint32_t par = (turn >> s) & 1u;
+          turn ^= 1u << s;
+          ok = mbar_wait(grant_bar(s), par, abort_flag);
+          if (!ok) break;
+          unsigned char* st = smem + (size_t)s * PSTAGE_BYTES;
+          const int nc = min(CHUNKS, total - c0);
+          for (int q = 0; q < nc; ++q) {
+            const int who = p.tile_list[(int64_t)tl.tn * p.nt + (c0 + q) / p.chunks];
+            const int j0 = 16 * ((c0 + q) % p.chunks);
+            unsigned char* fac = st + A_BYTES + (size_t)q * 128 * 32;
+            for (int row = tid; row < half; row += 64) {
+              uint32_t w[8];
+              factor_row(p, n0 + row, who, j0, w);
+              const int sw = ((row >> 2) & 1) << 4;
+              *reinterpret_cast<uint4*>(fac + row * 32 + sw) = make_uint4(w[0], w[1], w[2], w[3]);
+              *reinterpret_cast<uint4*>(fac + row * 32 + (16 ^ sw)) =
+                  make_uint4(w[4], w[5], w[6], w[7]);
+            }
+          }
+          ok = mbar_wait(land_bar(s), par, abort_flag);
+          if (!ok) break;
+          for (int q = tid; q < nc * (CHUNK_BYTES / 16); q += 64)
+            clean_vector(reinterpret_cast<uint4*>(st) + q, poison);
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(map_to_cta(factor_bar(s), 0));
+          if (++s == PSTAGES) s = 0;
+        }
+      }
+    }
+  } else {
+    // ------------------------------------------------------------ epilogue
+    const int g = warp & 3, h = (warp - 4) >> 2;
+    const uint32_t lead_tempty[2] = {map_to_cta(tempty_bar(0), 0), map_to_cta(tempty_bar(1), 0)};
+    if (ext || p.early) grid_dependency_wait();
+    int q = 0;
+    uint32_t tphase = 0;
+    bool ok = true;
+    for (int t = pair; t < n_tiles; t += npairs) {
+      const PairTile tl = pair_tile(p, t);
+      ok = ok && mbar_wait(tfull_bar(q), tphase, abort_flag);
+      tc_fence_after();
+      if (ok) {
+        const int n0 = tl.tn * p.nt;
+        const int m = tl.tm * PTM + 128 * (int)rank + 32 * g + lane;
+        if (ext && tl.tm == 0 && rank == 0) {
+          for (int u = n0 + (int)threadIdx.x - 128; u < min(n0 + p.nt, p.N); u += 256)
+            if (p.index[u] != -1 && valid_adapter(p, u) < 0)
+              atomicCAS(p.status, 0, (int)THANOS_ERR_INVALID_ARG);
+        }
+        const bool poisoned = ext && *(volatile int*)poison != 0;
+        const uint32_t taddr = tmem_base + ((uint32_t)(32 * g) << 16) + (uint32_t)q * 256;
+#pragma unroll 1
+        for (int cc = 32 * h; cc < p.nt; cc += 64) {
+          uint32_t u[32];
+          tc_ld32(taddr + cc, u);
+          tc_wait_ld();
+          float v[32];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(u[e]);
+          emit<AMN, EPI, 32>(p, tl.z, m, n0 + cc, v, tl.tm != tl.tn, poisoned);
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(lead_tempty[q]);
+      if (++q == 2) {
+        q = 0;
+        tphase ^= 1u;
+      }
+    }
+  }
+
+  // Neither CTA may leave (or free tensor memory) while its partner can still read its shared
+  // memory, signal its barriers or write its tensor memory.
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512)
+                 : "memory");
+  }
+  if (threadIdx.x == 0 && *abort_flag) atomicCAS(p.status, 0, (int)THANOS_ERR_TIMEOUT);
 }
 
 bool make_map3(CUtensorMap* map, const void* base, bool f16, int64_t inner, int64_t rows, int64_t ld,
@@ -598,9 +1006,80 @@ thanos_status_t launch(const CUtensorMap& mA, const CUtensorMap& mB, const CUten
   return THANOS_OK;
 }
 
+template <bool AMN, int EPI>
+int max_active_pairs() {
+  static std::atomic<int> cached_by_dev[64];  // 0 = not asked yet, else pairs + 1
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+  const int have = cached_by_dev[dev].load(std::memory_order_relaxed);
+  if (have > 0) return have - 1;
+  if (cudaFuncSetAttribute(pair_kernel<AMN, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                           (int)PSMEM_BYTES) != cudaSuccess) {
+    cudaGetLastError();
+    return 0;
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(2 * sm_count(), 1, 1);
+  cfg.blockDim = dim3(NTHREADS, 1, 1);
+  cfg.dynamicSmemBytes = PSMEM_BYTES;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  int n = 0;
+  if (cudaOccupancyMaxActiveClusters(&n, pair_kernel<AMN, EPI>, &cfg) != cudaSuccess || n <= 0) {
+    cudaGetLastError();
+    n = 0;
+  }
+  cached_by_dev[dev].store(n + 1, std::memory_order_relaxed);
+  return n;
+}
+
+template <bool AMN, int EPI>
+thanos_status_t launch_pair(const CUtensorMap& mA, const CUtensorMap& mB, const CUtensorMap& mP,
+                            const Params& p, cudaStream_t stream) {
+  const int G = max_active_pairs<AMN, EPI>();
+  if (G < 1) return THANOS_ERR_CUDA;
+  const int64_t per = p.symmetric ? (int64_t)p.tiles_m * (p.tiles_m + 1) / 2
+                                  : (int64_t)p.tiles_m * p.tiles_n;
+  const int64_t tiles = per * p.batch_z;
+  if (tiles > (1 << 30)) return THANOS_ERR_SHAPE;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(2 * (tiles < G ? tiles : G)), 1, 1);
+  cfg.blockDim = dim3(NTHREADS, 1, 1);
+  cfg.dynamicSmemBytes = PSMEM_BYTES;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  count_launch();
+  THANOS_CUDA(cudaLaunchKernelEx(&cfg, pair_kernel<AMN, EPI>, mA, mB, mP, p, (int)tiles));
+  return THANOS_OK;
+}
+
+template <bool AMN, int EPI>
+thanos_status_t launch_any(bool pairs, const CUtensorMap& mA, const CUtensorMap& mB,
+                           const CUtensorMap& mP, const Params& p, cudaStream_t stream) {
+  return pairs ? launch_pair<AMN, EPI>(mA, mB, mP, p, stream)
+               : launch<AMN, EPI>(mA, mB, mP, p, stream);
+}
+
+// Whether a product runs on CTA pairs: once its 256 x 256 tiles occupy at least half of the pairs.
+bool use_pairs(int64_t M, int64_t N, int64_t batch, bool symmetric) {
+  const int64_t tm = ceil_div(M, PTM), tn = ceil_div(N, PTM);
+  const int64_t tiles = (symmetric ? tm * (tm + 1) / 2 : tm * tn) * batch;
+  return M > TM && N > TM && tiles * 4 >= sm_count();
+}
+
 }  // namespace
 
-int proj_token_tile(int64_t N, int64_t) {
+int proj_token_tile(int64_t N, int64_t M) {
+  if (use_pairs(M, N, 1, false)) return 256;
   return N <= 32 ? 32 : N <= 64 ? 64 : N <= 128 ? 128 : 256;
 }
 
@@ -613,8 +1092,10 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
   p.M = a.M;
   p.N = a.N;
   p.K = a.K;
-  p.nt = symmetric ? TM : a.nt ? a.nt : proj_token_tile(a.N, a.M);
-  p.tiles_m = (a.M + TM - 1) / TM;
+  const bool pairs = a.epi != PROJ_SHRINK && use_pairs(a.M, a.N, a.batch, symmetric);
+  p.nt = symmetric ? (pairs ? PTM : TM) : a.nt ? a.nt : proj_token_tile(a.N, a.M);
+  if (pairs && a.epi > PROJ_SHRINK) p.nt = PTM;
+  p.tiles_m = (a.M + (pairs ? PTM : TM) - 1) / (pairs ? PTM : TM);
   p.tiles_n = (a.N + p.nt - 1) / p.nt;
   p.batch_z = a.batch;
   p.symmetric = symmetric;
@@ -668,7 +1149,8 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
   const CUtensorMapSwizzle sw = CU_TENSOR_MAP_SWIZZLE_128B;
   const bool okA = a.a_mn ? make_map3(&mA, a.A, a.f16, a.M, a.K, a.lda, a.batch, a.a_batch, 64, BK, sw)
                           : make_map3(&mA, a.A, a.f16, a.K, a.M, a.lda, a.batch, a.a_batch, BK, TM, sw);
-  if (!okA || !make_map3(&mB, a.B, a.f16, a.K, a.N, a.ldb, a.batch, a.b_batch, BK, p.nt, sw))
+  if (!okA || !make_map3(&mB, a.B, a.f16, a.K, a.N, a.ldb, a.batch, a.b_batch, BK,
+                         pairs ? p.nt / 2 : p.nt, sw))
     return THANOS_ERR_CUDA;
   mP = mA;
   if (a.epi == PROJ_OUT && a.n_adapters > 0) {
@@ -681,18 +1163,18 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
   }
   switch (a.epi) {
     case PROJ_OUT:
-      return a.a_mn ? launch<true, PROJ_OUT>(mA, mB, mP, p, stream)
-                    : launch<false, PROJ_OUT>(mA, mB, mP, p, stream);
+      return a.a_mn ? launch_any<true, PROJ_OUT>(pairs, mA, mB, mP, p, stream)
+                    : launch_any<false, PROJ_OUT>(pairs, mA, mB, mP, p, stream);
     case PROJ_SHRINK:
       return launch<false, PROJ_SHRINK>(mA, mB, mP, p, stream);
     case PROJ_GRAM:
-      return launch<false, PROJ_GRAM>(mA, mB, mP, p, stream);
+      return launch_any<false, PROJ_GRAM>(pairs, mA, mB, mP, p, stream);
     case PROJ_POLY:
-      return launch<false, PROJ_POLY>(mA, mB, mP, p, stream);
+      return launch_any<false, PROJ_POLY>(pairs, mA, mB, mP, p, stream);
     case PROJ_NEXT:
-      return launch<true, PROJ_NEXT>(mA, mB, mP, p, stream);
+      return launch_any<true, PROJ_NEXT>(pairs, mA, mB, mP, p, stream);
     default:
-      return launch<true, PROJ_FINAL>(mA, mB, mP, p, stream);
+      return launch_any<true, PROJ_FINAL>(pairs, mA, mB, mP, p, stream);
   }
 }
 
