@@ -2,6 +2,7 @@
 //   V[t] = X[t] A_i^T,  Y[t] = X[t] W^T + s_i V[t] B_i^T
 //   U[t] = s_i dY[t] B_i,  dX[t] = dY[t] W + U[t] A_i,  dA_i = sum_t U[t]^T X[t],
 //   dB_i = s_i sum_t dY[t]^T V[t]
+#include "adapter_grad.cuh"
 #include "proj_gemm.cuh"
 #include "recovery.cuh"
 #include "simt_gemm.cuh"
@@ -176,7 +177,7 @@ using bf16 = __nv_bfloat16;
 //   next n_turn          B_i [c, r] -> [r, c] (the skinny product's operand in the backward pass)
 //   the rest             V of a few tokens, a CTA per token and four ranks
 struct FrontParams {
-  int32_t* status;
+  int32_t* status;             // cleared here unless the sort did (then null)
   const int32_t* index;
   int32_t* count;
   int32_t* list;
@@ -210,11 +211,14 @@ __device__ __forceinline__ float dot8(const uint4& a, const uint4& b, float s) {
 
 __global__ void __launch_bounds__(256) front_kernel(const FrontParams p) {
   __shared__ float sh[64 * 65];
-  grid_dependency_wait();
+  // Launched plainly, or beside the sort of the tokens, which this does not depend on and which
+  // was itself launched plainly: what came before in the stream is done.  Block 0 waits for the sort
+  // so that whoever waits for this launch finds it finished too.
   grid_dependents_launch();
   const int tid = threadIdx.x;
   int blk = blockIdx.x;
-  if (blk == 0 && tid == 0) *p.status = 0;
+  if (blk == 0) grid_dependency_wait();
+  if (blk == 0 && tid == 0 && p.status) *p.status = 0;
   if (blk < p.n_list) {
     int* ids = reinterpret_cast<int*>(sh);
     int* base = ids + 256;
@@ -305,12 +309,20 @@ __global__ void __launch_bounds__(256) front_kernel(const FrontParams p) {
   }
 }
 
-thanos_status_t launch_front(const FrontParams& p, int64_t shrink_blocks, cudaStream_t stream) {
+thanos_status_t launch_front(const FrontParams& p, int64_t shrink_blocks, bool beside_sort,
+                             cudaStream_t stream) {
   const int64_t blocks = (int64_t)p.n_list + p.n_copy + p.n_turn + shrink_blocks;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)blocks, 1, 1);
   cfg.blockDim = dim3(256, 1, 1);
   cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  if (beside_sort) {
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+  }
   count_launch();
   THANOS_CUDA(cudaLaunchKernelEx(&cfg, front_kernel, p));
   return THANOS_OK;
@@ -326,6 +338,9 @@ struct Layout {
   int32_t* list;
   bf16* copy;        // padded B (forward) or dY (backward)
   bf16* turned;      // backward: B_i transposed
+  int32_t* order;    // backward: tokens by adapter
+  int32_t* spare;
+  int32_t* off;
 };
 
 bool carve(Arena& ar, Layout& L, bool backward, int64_t T, int64_t c, int64_t n, int r,
@@ -339,7 +354,12 @@ bool carve(Arena& ar, Layout& L, bool backward, int64_t T, int64_t c, int64_t n,
   L.turned = nullptr;
   if (!backward && r % 8) L.copy = ar.take<bf16>((size_t)n * c * round_up(r, 8));
   if (backward && copy_dy) L.copy = ar.take<bf16>((size_t)T * round_up(c, 8));
-  if (backward) L.turned = ar.take<bf16>((size_t)n * r * round_up(c, 8));
+  if (backward) {
+    L.turned = ar.take<bf16>((size_t)n * r * round_up(c, 8));
+    L.order = ar.take<int32_t>((size_t)T);
+    L.spare = ar.take<int32_t>((size_t)T);
+    L.off = ar.take<int32_t>((size_t)n + 1);
+  }
   return ar.ok();
 }
 
@@ -394,7 +414,7 @@ thanos_status_t forward16(const AdapterArgs& a, void* workspace, size_t ws_bytes
     f.b = (int)a.b;
     shrink = a.T * ceil_div(a.r, SHRINK_RANKS);
   }
-  THANOS_TRY(launch_front(f, shrink, stream));
+  THANOS_TRY(launch_front(f, shrink, false, stream));
   g.V = V;
   g.index = a.index;
   g.n_adapters = (int)a.n;
@@ -467,7 +487,12 @@ thanos_status_t backward16(const AdapterArgs& a, void* workspace, size_t ws_byte
     const int64_t want = a.n * ceil_div(a.c, 64);
     f.n_turn = (int)(want < 4 * NUM_SMS ? want : 4 * NUM_SMS);
   }
-  if (f.n_list + f.n_copy + f.n_turn > 0) THANOS_TRY(launch_front(f, 0, stream));
+  const bool sorts = a.dA != nullptr;
+  if (sorts) {
+    THANOS_TRY(sort_tokens(a.index, a.T, a.n, L.order, L.spare, L.off, L.status, stream));
+    f.status = nullptr;
+  }
+  if (f.n_list + f.n_copy + f.n_turn > 0) THANOS_TRY(launch_front(f, 0, sorts, stream));
   else THANOS_CUDA(cudaMemsetAsync(L.status, 0, 16, stream));
   if (a.n > 0) {
     g.V = L.R;
@@ -490,7 +515,22 @@ thanos_status_t backward16(const AdapterArgs& a, void* workspace, size_t ws_byte
     g.early = copy_dy ? 0 : 1;
   }
   if (a.out) THANOS_TRY(proj_gemm(g, stream));
-  if (a.dA) THANOS_TRY(simple_grads<bf16>(a, L.R, stream));
+  if (a.dA) {
+    AdapterGradSide sa, sb;
+    sa.Z = static_cast<const bf16*>(a.X);
+    sa.ldz = a.ldx;
+    sa.R = L.R;
+    sa.out = a.dA;
+    sa.F = (int)a.b;
+    sb.Z = static_cast<const bf16*>(dY);
+    sb.ldz = lddy;
+    sb.R = a.Vin;
+    sb.scale = a.scale;
+    sb.out = a.dB;
+    sb.F = (int)a.c;
+    sb.by_feature = 1;
+    THANOS_TRY(adapter_grads(sa, sb, L.order, L.off, a.T, a.n, a.r, a.accumulate, L.status, stream));
+  }
   return THANOS_OK;
 }
 
@@ -505,7 +545,9 @@ size_t adapter_workspace_bytes(bool backward, int64_t T, int64_t c, int64_t, int
   const size_t c8 = round_up((size_t)c, 8);
   if (!backward && r % 8) need += round_up((size_t)n * c * round_up(r, 8) * 2, 256);
   // room for a copy of dY whose rows are not 16-byte aligned
-  if (backward) need += round_up((size_t)T * c8 * 2, 256) + round_up((size_t)n * r * c8 * 2, 256);
+  if (backward)
+    need += round_up((size_t)T * c8 * 2, 256) + round_up((size_t)n * r * c8 * 2, 256) +
+            2 * round_up((size_t)T * 4, 256) + round_up(((size_t)n + 1) * 4, 256);
   return need;
 }
 

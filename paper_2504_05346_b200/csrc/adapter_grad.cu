@@ -1,0 +1,455 @@
+// dA_i = sum U[t]^T X[t] and dB_i = s_i sum dY[t]^T V[t] over the tokens of adapter i.
+//
+// A skinny contraction over tokens: 2 r flops per 16-bit value read, so reading X and dY once is the
+// bound (r up to 128: at most 256 flops per 2 bytes, below the tensor cores' balance of about 500).
+// A CTA owns one adapter and 128 features; tokens come in the order of sort_tokens, so a tile never
+// mixes adapters (nothing that is not finite crosses from one to another) and needs no mask.
+//   warps 0..3   gather 64 tokens per stage: rows of Z by cp.async into the MN-major layout of the
+//                tensor cores (64 features x 64 tokens, 128-byte swizzle); the fp32 rows of R are
+//                split into two bf16 planes hi + lo (16 significant bits, so that the result keeps
+//                fp32 quality with exact 16-bit products) side by side in n: [hi | lo]
+//   warp 4       tcgen05.mma issuer, 128 x 2 r x 16
+//   warps 4..7   epilogue: hi + lo columns added, written (or added) to the gradient
+// A cluster of up to eight CTAs splits the adapter's tokens when there are few tiles; the partial
+// sums are added over distributed shared memory in rank order (same inputs, same bits).
+#include "adapter_grad.cuh"
+
+#include "proj_gemm.cuh"
+#include "tc_common.cuh"
+
+namespace thanos {
+
+namespace {
+
+using namespace tc;
+
+// ------------------------------------------------------------------------------------- sorting
+constexpr int SORT_THREADS = 1024;
+
+__global__ void __launch_bounds__(SORT_THREADS)
+sort_kernel(const int32_t* __restrict__ index, int T, int n, int32_t* order, int32_t* spare,
+            int32_t* __restrict__ off, int32_t* __restrict__ status) {
+  __shared__ int base[256];
+  __shared__ int wh[32][256];
+  grid_dependents_launch();
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) *status = 0;
+  __syncthreads();
+  auto key_of = [&](int t) {
+    const int i = index[t];
+    return i >= 0 && i < n ? i : n;
+  };
+  int digits = 1;
+  while (digits < 4 && (n >> (8 * digits)) != 0) ++digits;
+  int32_t* dst = (digits & 1) ? order : spare;
+  int32_t* src = (digits & 1) ? spare : order;
+  for (int d = 0; d < digits; ++d) {
+    if (tid < 256) base[tid] = 0;
+    __syncthreads();
+    for (int p = tid; p < T; p += SORT_THREADS) {
+      const int k = key_of(d == 0 ? p : src[p]);
+      if (d == 0 && k == n && index[p] != -1) atomicCAS(status, 0, (int)THANOS_ERR_INVALID_ARG);
+      atomicAdd(&base[(k >> (8 * d)) & 255], 1);
+    }
+    __syncthreads();
+    if (warp == 0) {  // exclusive scan, eight bins a lane
+      int v[8], sum = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        v[e] = sum;
+        sum += base[8 * lane + e];
+      }
+      int before = sum;
+      for (int o = 1; o < 32; o <<= 1) {
+        const int u = __shfl_up_sync(0xffffffffu, before, o);
+        if (lane >= o) before += u;
+      }
+      before -= sum;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) base[8 * lane + e] = before + v[e];
+    }
+    __syncthreads();
+    for (int p0 = 0; p0 < T; p0 += SORT_THREADS) {
+      for (int e = tid; e < 32 * 256; e += SORT_THREADS) (&wh[0][0])[e] = 0;
+      __syncthreads();
+      const int p = p0 + tid;
+      const int t = p < T ? (d == 0 ? p : src[p]) : 0;
+      const int bin = p < T ? (key_of(t) >> (8 * d)) & 255 : -1;
+      const unsigned same = __match_any_sync(0xffffffffu, bin);
+      const int before = __popc(same & ((1u << lane) - 1u));
+      if (bin >= 0 && before == 0) wh[warp][bin] = __popc(same);
+      __syncthreads();
+      if (tid < 256) {
+        int run = base[tid];
+#pragma unroll
+        for (int w = 0; w < 32; ++w) {
+          const int c = wh[w][tid];
+          wh[w][tid] = run;
+          run += c;
+        }
+        base[tid] = run;
+      }
+      __syncthreads();
+      if (bin >= 0) dst[wh[warp][bin] + before] = t;
+      __syncthreads();
+    }
+    int32_t* x = dst;
+    dst = src;
+    src = x;
+  }
+  // src == order now; first position of every adapter
+  for (int p = tid; p <= T; p += SORT_THREADS) {
+    const int k = p < T ? key_of(src[p]) : n;
+    const int prev = p > 0 ? key_of(src[p - 1]) : -1;
+    for (int i = prev + 1; i <= k; ++i) off[i] = p;
+  }
+}
+
+// ----------------------------------------------------------------------------------- gradients
+constexpr int GF = 128;                  // features per CTA
+constexpr int GK = 64;                   // tokens per stage
+constexpr int GA_BYTES = GF * GK * 2;
+constexpr int G_MAX_STAGES = 6;
+constexpr int G_THREADS = 256;
+
+struct GradParams {
+  AdapterGradSide side[2];
+  int tiles0, tiles;                     // feature tiles of side 0, of both
+  const int32_t* order;
+  const int32_t* off;
+  int32_t* status;
+  int n, r, r16, stages, splits, accumulate, ring_bytes;
+  int tmem_cols;
+};
+
+__device__ __forceinline__ uint64_t grad_desc(uint32_t addr, uint32_t lbo, uint32_t sbo,
+                                              uint32_t layout) {
+  uint64_t d = 0;
+  d |= (uint64_t)((addr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)(lbo >> 4) << 16;
+  d |= (uint64_t)(sbo >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)layout << 61;
+  return d;
+}
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes)
+               : "memory");
+}
+__device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]),
+        "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]),
+        "=r"(v[14]), "=r"(v[15])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ float grad_ld_cluster(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
+
+// The stage whose copies were issued `behind` turns ago is complete for this thread.
+__device__ __forceinline__ void publish(uint32_t bar, int lane) {
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  __syncwarp();
+  if (lane == 0) mbar_arrive(bar);
+}
+
+__global__ void __launch_bounds__(G_THREADS) grad_tc_kernel(const GradParams p) {
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* smem = reinterpret_cast<unsigned char*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + p.ring_bytes);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * G_MAX_STAGES + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 2 * G_MAX_STAGES + 2);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t smem_base = smem_u32(smem), bar_base = smem_u32(bars);
+  auto full_bar = [&](int s) { return bar_base + 8u * s; };
+  auto empty_bar = [&](int s) { return bar_base + 8u * (G_MAX_STAGES + s); };
+  const uint32_t done_bar = bar_base + 8u * (2 * G_MAX_STAGES);
+
+  const int S = p.splits;
+  const int rank = S > 1 ? (int)cluster_ctarank() : 0;
+  const int tile = (int)(blockIdx.x / S);
+  const AdapterGradSide& sd = tile < p.tiles0 ? p.side[0] : p.side[1];
+  const int f0 = (tile < p.tiles0 ? tile : tile - p.tiles0) * GF;
+  const int F = sd.F, r = p.r, r16 = p.r16, N = 2 * r16;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < p.stages; ++s) {
+      mbar_init(full_bar(s), 4);
+      mbar_init(empty_bar(s), 1);
+    }
+    mbar_init(done_bar, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 4) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
+                     smem_u32(tmem_slot)),
+                 "r"(p.tmem_cols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  const int stage_bytes = GA_BYTES + N * GK * 2;
+  // the ring and the barriers run on from adapter to adapter
+  int s = 0, s_pub = 0;
+  uint32_t phase = 0, done_phase = 0;
+  bool ok = true;
+
+  grid_dependency_wait();
+  for (int64_t i = blockIdx.y; i < p.n; i += gridDim.y) {
+    const int lo = p.off[i], len = p.off[i + 1] - lo;
+    if (len == 0) {
+      // an adapter without tokens: zeros, or nothing to add
+      if (!p.accumulate && rank == 0) {
+        for (int e = threadIdx.x; e < GF * r; e += G_THREADS) {
+          const int j = sd.by_feature ? e % r : e / GF, f = f0 + (sd.by_feature ? e / r : e % GF);
+          if (f < F) sd.out[sd.by_feature ? (i * F + f) * r + j : (i * r + j) * F + f] = 0.f;
+        }
+      }
+      continue;
+    }
+    const int nk = (len + GK - 1) / GK;
+    const int ks0 = (int)((int64_t)nk * rank / S), ks1 = (int)((int64_t)nk * (rank + 1) / S);
+
+
+    if (warp < 4) {
+      // ---------------------------------------------------------- gather
+      const int row = threadIdx.x >> 1, sub = threadIdx.x & 1;
+      const int lag = p.stages > 2 ? 2 : 1;
+      int pending = 0;
+      for (int ks = ks0; ks < ks1 && ok; ++ks) {
+        ok = mbar_wait(empty_bar(s), phase ^ 1u, abort_flag);
+        if (!ok) break;
+        const int at = ks * GK + row;
+        const bool live = at < len;
+        const int64_t t = live ? p.order[lo + at] : 0;
+        const uint32_t st = smem_base + (uint32_t)s * stage_bytes;
+        {
+          const int fb = f0 + 64 * sub;
+          const __nv_bfloat16* z = sd.Z + t * sd.ldz;
+          const uint32_t dst = st + sub * (GA_BYTES / 2) + row * 128;
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            const int f = fb + 8 * c;
+            const int left = live ? (F - f) * 2 : 0;
+            const uint32_t bytes = left <= 0 ? 0u : left < 16 ? (uint32_t)left : 16u;
+            cp_async16(dst + ((c ^ (row & 7)) << 4), bytes ? z + f : sd.Z, bytes);
+          }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        // hi and lo planes of R's row; this thread takes half of the 8-wide groups
+        const float* R = sd.R + t * r;
+        for (int g8 = sub; g8 < r16 / 8; g8 += 2) {
+          uint32_t hi[4], lw[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            uint32_t h2[2], l2[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const int j = 8 * g8 + 2 * e + u;
+              const float x = live && j < r ? R[j] : 0.f;
+              const __nv_bfloat16 h = __float2bfloat16_rn(x);
+              h2[u] = __bfloat16_as_ushort(h);
+              // an infinity has no second plane (inf - inf)
+              const float hf = __bfloat162float(h);
+              l2[u] = __bfloat16_as_ushort(__float2bfloat16_rn(isfinite(hf) ? x - hf : 0.f));
+            }
+            hi[e] = h2[0] | h2[1] << 16;
+            lw[e] = l2[0] | l2[1] << 16;
+          }
+          unsigned char* B = smem + (size_t)s * stage_bytes + GA_BYTES;
+          auto put = [&](int nn, const uint32_t(&w)[4]) {
+            // boxes of 32 n x 64 k, 64 bytes per k row, 64-byte swizzle
+            unsigned char* q = B + (nn >> 5) * 4096 + row * 64 +
+                               ((((nn & 31) >> 3) ^ ((row >> 1) & 3)) << 4);
+            *reinterpret_cast<uint4*>(q) = make_uint4(w[0], w[1], w[2], w[3]);
+          };
+          put(8 * g8, hi);
+          put(r16 + 8 * g8, lw);
+        }
+        if (++pending > lag) {
+          if (lag == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
+          else asm volatile("cp.async.wait_group 1;" ::: "memory");
+          publish(full_bar(s_pub), lane);
+          if (++s_pub == p.stages) s_pub = 0;
+          --pending;
+        }
+        if (++s == p.stages) {
+          s = 0;
+          phase ^= 1u;
+        }
+      }
+      asm volatile("cp.async.wait_group 0;" ::: "memory");
+      while (pending-- > 0) {
+        publish(full_bar(s_pub), lane);
+        if (++s_pub == p.stages) s_pub = 0;
+      }
+    } else {
+      if (warp == 4) {
+        // -------------------------------------------------------- MMA issuer
+        uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16);
+        idesc |= (uint32_t)(N >> 3) << 17;
+        idesc |= (uint32_t)(GF >> 4) << 24;
+        for (int ks = ks0; ks < ks1 && ok; ++ks) {
+          ok = mbar_wait(full_bar(s), phase, abort_flag);
+          tc_fence_after();
+          if (ok && lane == 0) {
+            const uint32_t sa = smem_base + (uint32_t)s * stage_bytes, sb = sa + GA_BYTES;
+#pragma unroll
+            for (int k4 = 0; k4 < GK / 16; ++k4)
+              tc_mma_bf16(tmem_base, grad_desc(sa + k4 * 2048, GA_BYTES / 2, 1024, 2),
+                          grad_desc(sb + k4 * 1024, 4096, 512, 4), idesc,
+                          (ks > ks0 || k4 > 0) ? 1u : 0u);
+            tc_commit(empty_bar(s));
+          }
+          __syncwarp();
+          if (++s == p.stages) {
+            s = 0;
+            phase ^= 1u;
+          }
+        }
+        if (ok && lane == 0) tc_commit(done_bar);
+        __syncwarp();
+      }
+      // ---------------------------------------------------------- epilogue, one slice of tokens
+      ok = ok && mbar_wait(done_bar, done_phase, abort_flag);
+      done_phase ^= 1u;
+      tc_fence_after();
+      const int g = warp & 3;
+      const uint32_t taddr = tmem_base + ((uint32_t)(32 * g) << 16);
+      const int row = 32 * g + lane, f = f0 + row;
+      if (ok) {
+        for (int j0 = 0; j0 < r16; j0 += 16) {
+          float v[16];
+          if (ks1 > ks0) {
+            uint32_t h[16], l[16];
+            tc_ld16(taddr + j0, h);
+            tc_ld16(taddr + r16 + j0, l);
+            tc_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[e] = __uint_as_float(h[e]) + __uint_as_float(l[e]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[e] = 0.f;
+          }
+          if (S == 1) {
+            if (f < F) {
+              const float k = sd.scale ? sd.scale[i] : 1.f;
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                if (j0 + e >= r) break;
+                float* o = sd.out + (sd.by_feature ? (i * F + f) * r + j0 + e
+                                                   : (i * r + j0 + e) * (int64_t)F + f);
+                *o = p.accumulate ? *o + k * v[e] : k * v[e];
+              }
+            }
+          } else {
+            float* part = reinterpret_cast<float*>(smem);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) part[(j0 + e) * GF + row] = v[e];
+          }
+        }
+      }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (S > 1) {
+      cluster_sync_all();
+      const float k = sd.scale ? sd.scale[i] : 1.f;
+      const int row = threadIdx.x & 127, f = f0 + row;
+      for (int j = rank + S * (threadIdx.x >> 7); j < r; j += 2 * S) {
+        float v = 0.f;
+        for (int q = 0; q < S; ++q)
+          v += grad_ld_cluster(map_to_cta(smem_base, q) + (uint32_t)(j * GF + row) * 4u);
+        if (f < F) {
+          float* o = sd.out + (sd.by_feature ? (i * F + f) * r + j : (i * r + j) * (int64_t)F + f);
+          *o = p.accumulate ? *o + k * v : k * v;
+        }
+      }
+      cluster_sync_all();  // no CTA goes on while another may still read its partial sums
+    }
+    tc_fence_after();
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 4) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base),
+                 "r"(p.tmem_cols)
+                 : "memory");
+  }
+  if (threadIdx.x == 0 && *abort_flag) atomicCAS(p.status, 0, (int)THANOS_ERR_TIMEOUT);
+}
+
+}  // namespace
+
+thanos_status_t sort_tokens(const int32_t* index, int64_t T, int64_t n, int32_t* order,
+                            int32_t* spare, int32_t* off, int32_t* status, cudaStream_t stream) {
+  sort_kernel<<<1, SORT_THREADS, 0, stream>>>(index, (int)T, (int)n, order, spare, off, status);
+  THANOS_CHECK_LAUNCH();
+  return THANOS_OK;
+}
+
+thanos_status_t adapter_grads(const AdapterGradSide& a, const AdapterGradSide& b,
+                              const int32_t* order, const int32_t* off, int64_t T, int64_t n, int r,
+                              int accumulate, int32_t* status, cudaStream_t stream) {
+  GradParams p = {};
+  p.side[0] = a;
+  p.side[1] = b;
+  p.tiles0 = (int)ceil_div(a.F, GF);
+  p.tiles = p.tiles0 + (int)ceil_div(b.F, GF);
+  p.order = order;
+  p.off = off;
+  p.status = status;
+  p.n = (int)n;
+  p.r = r;
+  p.r16 = (r + 15) / 16 * 16;
+  p.accumulate = accumulate;
+  const int N = 2 * p.r16;
+  p.tmem_cols = 32;
+  while (p.tmem_cols < N) p.tmem_cols *= 2;
+  const int stage_bytes = GA_BYTES + N * GK * 2;
+  // two CTAs share an SM, so that one gathers while the other finishes
+  p.stages = 100 * 1024 / stage_bytes;
+  if (p.stages > G_MAX_STAGES) p.stages = G_MAX_STAGES;
+  p.ring_bytes = p.stages * stage_bytes;
+  if (p.ring_bytes < p.r16 * GF * 4) p.ring_bytes = p.r16 * GF * 4;
+  // token slices: fill two CTAs per SM, but leave a slice some hundred tokens
+  const int64_t units = (int64_t)p.tiles * n;
+  p.splits = 1;
+  while (p.splits < 8 && units * p.splits < 2 * sm_count() && T >= n * p.splits * 512) p.splits *= 2;
+  const size_t smem = (size_t)p.ring_bytes + 1024 + 256;
+  {
+    static std::atomic<unsigned long long> done{0};
+    THANOS_CUDA(ensure_max_dyn_smem(grad_tc_kernel, 113 * 1024, done));
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(p.tiles * p.splits), (unsigned)(n < 65535 ? n : 65535), 1);
+  cfg.blockDim = dim3(G_THREADS, 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)p.splits;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  count_launch();
+  THANOS_CUDA(cudaLaunchKernelEx(&cfg, grad_tc_kernel, p));
+  return THANOS_OK;
+}
+
+}  // namespace thanos

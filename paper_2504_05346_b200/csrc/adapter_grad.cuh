@@ -1,0 +1,28 @@
+// Gradients of the adapters from 16-bit activations (see adapter_grad.cu).
+#pragma once
+
+#include "common.cuh"
+
+namespace thanos {
+
+// Tokens by adapter: order[off[i] .. off[i + 1]) are the tokens of adapter i in ascending order.
+// One CTA; also clears the call's status word and reports an index that names no adapter.
+thanos_status_t sort_tokens(const int32_t* index, int64_t T, int64_t n, int32_t* order,
+                            int32_t* spare, int32_t* off, int32_t* status, cudaStream_t stream);
+
+struct AdapterGradSide {
+  const __nv_bfloat16* Z = nullptr;  // [T, F], leading dimension ldz (multiple of 8)
+  int64_t ldz = 0;
+  const float* R = nullptr;          // [T, r]
+  const float* scale = nullptr;      // factor by adapter, or null
+  float* out = nullptr;              // [n, r, F], or [n, F, r] if by_feature
+  int F = 0;
+  int by_feature = 0;
+};
+
+// out_i = scale_i sum over the adapter's tokens of R[t]^T Z[t], for both sides in one launch.
+thanos_status_t adapter_grads(const AdapterGradSide& a, const AdapterGradSide& b,
+                              const int32_t* order, const int32_t* off, int64_t T, int64_t n, int r,
+                              int accumulate, int32_t* status, cudaStream_t stream);
+
+}  // namespace thanos
