@@ -343,16 +343,17 @@ struct Layout {
   int32_t* off;
 };
 
-bool carve(Arena& ar, Layout& L, bool backward, int64_t T, int64_t c, int64_t n, int r,
+bool carve(Arena& ar, Layout& L, bool backward, int64_t T, int64_t c, int64_t b, int64_t n, int r,
            bool copy_dy) {
-  const int64_t nt = proj_token_tile(T, c), tiles = ceil_div(T, nt);
+  const int64_t nt = proj_pair_tile(T, backward ? b : c), tiles = nt ? ceil_div(T, nt) : 0;
+  L = Layout{};
   L.status = ar.take<int32_t>(64);
   L.R = ar.take<float>((size_t)T * r);
-  L.count = ar.take<int32_t>((size_t)tiles);
-  L.list = ar.take<int32_t>((size_t)(tiles * nt));
-  L.copy = nullptr;
-  L.turned = nullptr;
-  if (!backward && r % 8) L.copy = ar.take<bf16>((size_t)n * c * round_up(r, 8));
+  if (nt) {
+    L.count = ar.take<int32_t>((size_t)tiles);
+    L.list = ar.take<int32_t>((size_t)(tiles * nt));
+  }
+  if (!backward && nt && r % 8) L.copy = ar.take<bf16>((size_t)n * c * round_up(r, 8));
   if (backward && copy_dy) L.copy = ar.take<bf16>((size_t)T * round_up(c, 8));
   if (backward) {
     L.turned = ar.take<bf16>((size_t)n * r * round_up(c, 8));
@@ -367,7 +368,7 @@ thanos_status_t forward16(const AdapterArgs& a, void* workspace, size_t ws_bytes
                           cudaStream_t stream) {
   Arena ar(workspace, ws_bytes);
   Layout L;
-  if (!carve(ar, L, false, a.T, a.c, a.n, a.r, false)) return THANOS_ERR_WORKSPACE;
+  if (!carve(ar, L, false, a.T, a.c, a.b, a.n, a.r, false)) return THANOS_ERR_WORKSPACE;
   float* V = a.V ? a.V : L.R;
   ProjArgs g;
   g.M = (int)a.c;
@@ -380,7 +381,7 @@ thanos_status_t forward16(const AdapterArgs& a, void* workspace, size_t ws_bytes
   g.status = L.status;
   g.out = a.out;
   g.ldo = a.ldo;
-  g.nt = proj_token_tile(a.T, a.c);
+  const int nt = proj_pair_tile(a.T, a.c);
   if (a.n == 0) {
     THANOS_CUDA(cudaMemsetAsync(L.status, 0, 16, stream));
     return proj_gemm(g, stream);
@@ -391,11 +392,12 @@ thanos_status_t forward16(const AdapterArgs& a, void* workspace, size_t ws_bytes
   f.count = L.count;
   f.list = L.list;
   f.T = (int)a.T;
-  f.nt = g.nt;
+  f.nt = nt;
   f.n = (int)a.n;
-  f.n_list = (int)ceil_div(a.T, g.nt);
+  f.n_list = nt ? (int)ceil_div(a.T, nt) : 0;
   f.r = a.r;
-  if (a.r % 8) {
+  const bool pad = nt && a.r % 8;
+  if (pad) {
     f.copy_src = static_cast<const bf16*>(a.B);
     f.copy_dst = L.copy;
     f.copy_rows = a.n * a.c;
@@ -414,7 +416,8 @@ thanos_status_t forward16(const AdapterArgs& a, void* workspace, size_t ws_bytes
     f.b = (int)a.b;
     shrink = a.T * ceil_div(a.r, SHRINK_RANKS);
   }
-  THANOS_TRY(launch_front(f, shrink, false, stream));
+  if (f.n_list + f.n_copy + shrink > 0) THANOS_TRY(launch_front(f, shrink, false, stream));
+  else THANOS_CUDA(cudaMemsetAsync(L.status, 0, 16, stream));
   g.V = V;
   g.index = a.index;
   g.n_adapters = (int)a.n;
@@ -430,8 +433,8 @@ thanos_status_t forward16(const AdapterArgs& a, void* workspace, size_t ws_bytes
     THANOS_TRY(proj_gemm(s, stream));
   }
   g.scale = a.scale;
-  g.P = a.r % 8 ? static_cast<const void*>(L.copy) : a.B;
-  g.ldp = (int64_t)round_up(a.r, 8);
+  g.P = pad ? static_cast<const void*>(L.copy) : a.B;
+  g.ldp = pad ? (int64_t)round_up(a.r, 8) : a.r;
   g.p_adapter = a.c * g.ldp;
   g.early = 1;
   return proj_gemm(g, stream);
@@ -442,7 +445,7 @@ thanos_status_t backward16(const AdapterArgs& a, void* workspace, size_t ws_byte
   const bool copy_dy = a.ldi % 8 != 0;
   Arena ar(workspace, ws_bytes);
   Layout L;
-  if (!carve(ar, L, true, a.T, a.c, a.n, a.r, copy_dy)) return THANOS_ERR_WORKSPACE;
+  if (!carve(ar, L, true, a.T, a.c, a.b, a.n, a.r, copy_dy)) return THANOS_ERR_WORKSPACE;
   const int64_t c8 = (int64_t)round_up(a.c, 8);
   const void* dY = copy_dy ? static_cast<const void*>(L.copy) : a.in;
   const int64_t lddy = copy_dy ? c8 : a.ldi;
@@ -458,16 +461,16 @@ thanos_status_t backward16(const AdapterArgs& a, void* workspace, size_t ws_byte
   g.status = L.status;
   g.out = a.out;
   g.ldo = a.ldo;
-  g.nt = proj_token_tile(a.T, a.b);
+  const int nt = proj_pair_tile(a.T, a.b);
   FrontParams f = {};
   f.status = L.status;
   f.index = a.index;
   f.count = L.count;
   f.list = L.list;
   f.T = (int)a.T;
-  f.nt = g.nt;
+  f.nt = nt;
   f.n = (int)a.n;
-  f.n_list = a.n > 0 ? (int)ceil_div(a.T, g.nt) : 0;
+  f.n_list = a.n > 0 && nt ? (int)ceil_div(a.T, nt) : 0;
   f.r = a.r;
   f.c = (int)a.c;
   if (copy_dy) {
@@ -536,14 +539,14 @@ thanos_status_t backward16(const AdapterArgs& a, void* workspace, size_t ws_byte
 
 }  // namespace
 
-size_t adapter_workspace_bytes(bool backward, int64_t T, int64_t c, int64_t, int64_t n, int r,
+size_t adapter_workspace_bytes(bool backward, int64_t T, int64_t c, int64_t b, int64_t n, int r,
                                thanos_dtype_t dtype) {
-  const int64_t nt = proj_token_tile(T, c), tiles = ceil_div(T, nt);
   size_t need = 256 + round_up((size_t)T * (size_t)r * 4, 256);
   if (dtype == THANOS_F32) return need;
+  const int64_t nt = proj_pair_tile(T, backward ? b : c), tiles = nt ? ceil_div(T, nt) : 0;
   need += round_up((size_t)tiles * 4, 256) + round_up((size_t)(tiles * nt) * 4, 256);
   const size_t c8 = round_up((size_t)c, 8);
-  if (!backward && r % 8) need += round_up((size_t)n * c * round_up(r, 8) * 2, 256);
+  if (!backward && nt && r % 8) need += round_up((size_t)n * c * round_up(r, 8) * 2, 256);
   // room for a copy of dY whose rows are not 16-byte aligned
   if (backward)
     need += round_up((size_t)T * c8 * 2, 256) + round_up((size_t)n * r * c8 * 2, 256) +

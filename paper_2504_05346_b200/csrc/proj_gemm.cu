@@ -1,18 +1,15 @@
-// See proj_gemm.cuh.  One CTA per 128 x nt output tile and slice of k; a cluster of 1, 2, 4 or 8
-// CTAs splits the k range of a tile when there are fewer tiles than SMs and adds the partial
-// sums over distributed shared memory in rank order (same inputs, same bits).
+// See proj_gemm.cuh.  Two kernels share the operand layouts and the epilogues.
 //
-// Roles of the 384 threads:
+// tile_kernel: one CTA per 128 x nt output tile and slice of k.  A cluster of 1, 2, 4 or 8 CTAs
+// splits the k range of a tile when there are fewer tiles than SMs and adds the partial sums over
+// distributed shared memory in rank order (same inputs, same bits).  Roles of its 320 threads:
 //   warp 0      TMA producer: per 64-wide k step the A tile (128 x 64, 128-byte swizzle; K-major, or
 //               two MN-major boxes of 64 m x 64 k) and the B tile (nt x 64, K-major)
 //   warp 1      tcgen05.mma issuer, 128 x nt x 16 each
-//   warps 2..3  adapter part: for every adapter that occurs in the token tile, k is extended by the
-//               adapter's rank in chunks of 16: the wide factor's rows come by TMA (32-byte swizzle;
-//               MN-major: 128-byte), the factor of the tokens, s_i V[t], is built here in bf16 with
-//               zero rows for tokens of other adapters.  0 times a non-finite weight would reach
-//               those tokens, so the chunk is scanned, non-finite weights become zeros and the
-//               epilogue adds their products to the adapter's own tokens.
-//   warps 4..11 epilogue: a quarter of the TMEM lanes and half of the columns each
+//   warps 2..9  first the adapter part of the outputs they will write, in fp32 on the ALUs while the
+//               weights stream in (2 r flops per output, next to 2 K in the product), then the
+//               epilogue: a quarter of the TMEM lanes and half of the columns each
+// pair_kernel: large products, see there.
 // Every wait is bounded (see tc_common.cuh); on expiry the status word gets THANOS_ERR_TIMEOUT.
 #include "proj_gemm.cuh"
 
@@ -27,16 +24,12 @@ using namespace tc;
 constexpr int TM = 128;
 constexpr int BK = 64;
 constexpr int A_BYTES = TM * BK * 2;
-constexpr int CHUNK_BYTES = TM * 16 * 2;      // a 16-wide chunk of an adapter's wide factor
-constexpr int CHUNKS = 4;                     // chunks per stage
 constexpr int MAX_STAGES = 10;
-constexpr int NTHREADS = 384;
-constexpr int RING_BYTES = 200 * 1024;
-constexpr size_t SMEM_BYTES = RING_BYTES + 1024 /*align*/ + 512 /*barriers*/;
-static_assert((4 * MAX_STAGES + 4) * 8 <= 512, "barriers");
+constexpr int TILE_THREADS = 320;
+constexpr int FACTOR_BYTES = 128 * 16 * 4;    // 16 ranks of up to 128 tokens, fp32
 
 struct Params {
-  int M, N, K, tiles_m, tiles_n, nt, stages, splits, batch_z;
+  int M, N, K, tiles_m, tiles_n, nt, stages, splits, batch_z, ring_bytes;
   int symmetric, f16, early;
   int32_t* status;
   // adapter part
@@ -118,20 +111,35 @@ __device__ __forceinline__ __nv_bfloat16 token_factor(const Params& p, int t, in
   return __float2bfloat16_rn(p.scale ? p.scale[i] * v : v);
 }
 
-// The 16 columns j0.. of a token's factor as packed bf16: s_i V[t, j] for the adapter `who`'s own
-// tokens, zeros for all others and beyond the rank.
-__device__ __forceinline__ void factor_row(const Params& p, int t, int who, int j0,
+// The 16 columns j0.. of a token's factor as packed bf16: s_i V[t, j] for the adapter's own tokens,
+// zeros for all others and beyond the rank.
+__device__ __forceinline__ void factor_row(const Params& p, int t, bool own, float sc, int j0,
                                            uint32_t (&w)[8]) {
+  float v[16];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) w[e] = 0u;
-  if (t < p.N && p.index[t] == who) {
+  for (int j = 0; j < 16; ++j) v[j] = 0.f;
+  if (own) {
+    const float* src = p.V + (int64_t)t * p.r + j0;
+    if (p.r % 4 == 0) {
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      const uint32_t h =
-          j0 + j < p.r ? __bfloat16_as_ushort(token_factor(p, t, who, j0 + j)) : 0u;
-      w[j >> 1] |= h << (16 * (j & 1));
+      for (int e = 0; e < 4; ++e)
+        if (j0 + 4 * e < p.r) {
+          const float4 f = *reinterpret_cast<const float4*>(src + 4 * e);
+          v[4 * e] = f.x;
+          v[4 * e + 1] = f.y;
+          v[4 * e + 2] = f.z;
+          v[4 * e + 3] = f.w;
+        }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 16; ++j)
+        if (j0 + j < p.r) v[j] = src[j];
     }
   }
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    w[e] = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(sc * v[2 * e])) |
+           ((uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(sc * v[2 * e + 1])) << 16);
 }
 
 __device__ __forceinline__ void clean_vector(uint4* at, int* poison) {
@@ -302,18 +310,78 @@ __device__ __forceinline__ void emit(const Params& p, int z, int m, int n0, floa
   }
 }
 
+// First column of the q-th group of eight that a thread of tile_kernel writes: without a split 32
+// columns of every 64 (as they come out of tensor memory), else every 2 S-th group.
+__device__ __forceinline__ int tile_column(int S, int rank, int half, int q) {
+  return S == 1 ? 32 * half + 64 * (q >> 2) + 8 * (q & 3) : 8 * (rank + S * (half + 2 * q));
+}
+
+__device__ __forceinline__ void epilogue_sync() {  // the eight epilogue warps of tile_kernel
+  asm volatile("bar.sync 1, 256;" ::: "memory");
+}
+__device__ __forceinline__ float2 unpack2(uint32_t w) {
+  return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+}
+
+// Sixteen ranks of one adapter's row of the wide factor (feature m), packed bf16; zeros beyond r.
+template <bool AMN>
+__device__ __forceinline__ void wide_row(const Params& p, int i, int m, int j0, uint32_t (&w)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) w[e] = 0u;
+  if (i < 0) return;
+  if constexpr (AMN) {
+    const unsigned short* q = reinterpret_cast<const unsigned short*>(p.P) +
+                              (int64_t)i * p.p_adapter + (int64_t)j0 * p.ldp + m;
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+      if (j0 + j < p.r) w[j >> 1] |= (uint32_t)q[(int64_t)j * p.ldp] << (16 * (j & 1));
+  } else {
+    const unsigned short* q = reinterpret_cast<const unsigned short*>(p.P) +
+                              (int64_t)i * p.p_adapter + (int64_t)m * p.ldp + j0;
+    if (p.r % 8 == 0) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (j0 + 8 * h < p.r) {
+          const uint4 v = *reinterpret_cast<const uint4*>(q + 8 * h);
+          w[4 * h] = v.x;
+          w[4 * h + 1] = v.y;
+          w[4 * h + 2] = v.z;
+          w[4 * h + 3] = v.w;
+        }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 16; ++j)
+        if (j0 + j < p.r) w[j >> 1] |= (uint32_t)q[j] << (16 * (j & 1));
+    }
+  }
+}
+
+__device__ __forceinline__ float dot16(const uint32_t (&w)[8], const float* __restrict__ v, float s) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float4 f = reinterpret_cast<const float4*>(v)[e];
+    const float2 a = unpack2(w[2 * e]), b = unpack2(w[2 * e + 1]);
+    s = fmaf(a.x, f.x, s);
+    s = fmaf(a.y, f.y, s);
+    s = fmaf(b.x, f.z, s);
+    s = fmaf(b.y, f.w, s);
+  }
+  return s;
+}
+
 template <bool AMN, int EPI>
-__global__ void __launch_bounds__(NTHREADS, 1)
-proj_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
-            const __grid_constant__ CUtensorMap mapP, const Params p) {
+__global__ void __launch_bounds__(TILE_THREADS, EPI <= PROJ_SHRINK ? 2 : 1)
+tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
+            const Params p) {
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + RING_BYTES);
-  // full, empty, factor ready, stage granted to the factor's warps (MAX_STAGES each), accumulator
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 4 * MAX_STAGES + 1);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 4 * MAX_STAGES + 2);
-  int* poison = reinterpret_cast<int*>(bars + 4 * MAX_STAGES + 3);
+  float* factor = reinterpret_cast<float*>(smem + p.ring_bytes);             // [nt][16]
+  int* ids = reinterpret_cast<int*>(smem + p.ring_bytes + FACTOR_BYTES);     // [nt]
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + p.ring_bytes + FACTOR_BYTES + 512);
+  // full [MAX_STAGES], empty [MAX_STAGES], accumulator ready
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * MAX_STAGES + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 2 * MAX_STAGES + 2);
 
   const int warp = threadIdx.x >> 5;
   const int lane = threadIdx.x & 31;
@@ -321,9 +389,7 @@ proj_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
   const uint32_t bar_base = smem_u32(bars);
   auto full_bar = [&](int s) { return bar_base + 8u * s; };
   auto empty_bar = [&](int s) { return bar_base + 8u * (MAX_STAGES + s); };
-  auto factor_bar = [&](int s) { return bar_base + 8u * (2 * MAX_STAGES + s); };
-  auto grant_bar = [&](int s) { return bar_base + 8u * (3 * MAX_STAGES + s); };
-  const uint32_t done_bar = bar_base + 8u * (4 * MAX_STAGES);
+  const uint32_t done_bar = bar_base + 8u * (2 * MAX_STAGES);
 
   const int S = p.splits;
   const int rank = S > 1 ? (int)cluster_ctarank() : 0;
@@ -342,10 +408,9 @@ proj_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
     grid_dependents_launch();
     if (tm > 0) {
       const int lo = m0 / p.r, hi = (min(m0 + TM, p.M) - 1) / p.r;
-      const int cnt = p.tile_count[tn];
       bool hit = false;
-      for (int q = lane; q < cnt; q += 32) {
-        const int i = p.tile_list[(int64_t)tn * p.nt + q];
+      for (int t = n0 + lane; t < min(n0 + p.nt, p.N); t += 32) {
+        const int i = p.index[t];
         hit = hit || (i >= lo && i <= hi);
       }
       if (!__any_sync(0xffffffffu, hit)) return;  // the same answer in every warp of the cluster
@@ -356,12 +421,9 @@ proj_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
     for (int s = 0; s < p.stages; ++s) {
       mbar_init(full_bar(s), 1);
       mbar_init(empty_bar(s), 1);
-      mbar_init(factor_bar(s), 2);
-      mbar_init(grant_bar(s), 1);
     }
     mbar_init(done_bar, 1);
     *abort_flag = 0;
-    *poison = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
@@ -383,7 +445,8 @@ proj_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
 
   const int nk = (p.K + BK - 1) / BK;
   const int ks0 = (int)((int64_t)nk * rank / S), ks1 = (int)((int64_t)nk * (rank + 1) / S);
-  const bool ext = EPI == PROJ_OUT && p.n_adapters > 0;
+  constexpr int Q = EPI == PROJ_OUT ? 8 : 1;  // groups of eight columns a thread may own (nt <= 128)
+  float own[Q][8];
 
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
@@ -409,36 +472,6 @@ proj_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
         phase ^= 1u;
       }
     }
-    if (ext) {
-      grid_dependency_wait();
-      const int total = p.tile_count[tn] * p.chunks;
-      for (int e = rank; e * CHUNKS < total && ok; e += S) {
-        ok = mbar_wait(empty_bar(s), phase ^ 1u, abort_flag);
-        if (ok && lane == 0) {
-          const uint32_t dst = smem_base + (uint32_t)s * stage_bytes;
-          const int nc = min(CHUNKS, total - e * CHUNKS);
-          mbar_arrive(grant_bar(s));
-          mbar_expect_tx(full_bar(s), nc * CHUNK_BYTES);
-          for (int q = 0; q < nc; ++q) {
-            const int ch = e * CHUNKS + q;
-            const int who = p.tile_list[(int64_t)tn * p.nt + ch / p.chunks];
-            const int j = 16 * (ch % p.chunks);
-            if (AMN) {
-              tma_load_3d(dst + q * CHUNK_BYTES, &mapP, full_bar(s), m0, j, who);
-              tma_load_3d(dst + q * CHUNK_BYTES + CHUNK_BYTES / 2, &mapP, full_bar(s), m0 + 64, j,
-                          who);
-            } else {
-              tma_load_3d(dst + q * CHUNK_BYTES, &mapP, full_bar(s), j, m0, who);
-            }
-          }
-        }
-        __syncwarp();
-        if (++s == p.stages) {
-          s = 0;
-          phase ^= 1u;
-        }
-      }
-    }
     // let copies that are still in flight land before the CTA's shared memory goes away
     if (!ok) {
       for (int i = 0; i < 2000; ++i) __nanosleep(1000);
@@ -452,7 +485,7 @@ proj_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
     idesc |= (uint32_t)(p.nt >> 3) << 17;
     idesc |= (uint32_t)(TM >> 4) << 24;
     int s = 0;
-    uint32_t phase = 0, acc = 0;
+    uint32_t phase = 0;
     bool ok = true;
     for (int ks = ks0; ks < ks1 && ok; ++ks) {
       ok = mbar_wait(full_bar(s), phase, abort_flag);
@@ -464,8 +497,8 @@ proj_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
         for (int k4 = 0; k4 < BK / 16; ++k4) {
           const uint64_t ad = AMN ? make_desc(sa + k4 * 2048, A_BYTES / 2, 1024, SW128)
                                   : make_desc(sa + k4 * 32, 16, 1024, SW128);
-          tc_mma_bf16(tmem_base, ad, make_desc(sb + k4 * 32, 16, 1024, SW128), idesc, acc);
-          acc = 1;
+          tc_mma_bf16(tmem_base, ad, make_desc(sb + k4 * 32, 16, 1024, SW128), idesc,
+                      (ks > ks0 || k4 > 0) ? 1u : 0u);
         }
         tc_commit(empty_bar(s));
       }
@@ -475,96 +508,90 @@ proj_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
         phase ^= 1u;
       }
     }
-    if (ext && ok) {
-      grid_dependency_wait();
-      const int total = p.tile_count[tn] * p.chunks;
-      int o = 0;
-      for (int e = rank; e * CHUNKS < total && ok; e += S, ++o) {
-        ok = mbar_wait(full_bar(s), phase, abort_flag) &&
-             mbar_wait(factor_bar(s), (uint32_t)(o / p.stages) & 1u, abort_flag);
-        tc_fence_after();
-        if (ok && lane == 0) {
-          const uint32_t sa = smem_base + (uint32_t)s * stage_bytes;
-          const uint32_t sb = sa + A_BYTES;
-          const int nc = min(CHUNKS, total - e * CHUNKS);
-          for (int q = 0; q < nc; ++q) {
-            const uint32_t ca = sa + q * CHUNK_BYTES;
-            const uint64_t ad = AMN ? make_desc(ca, CHUNK_BYTES / 2, 1024, SW128)
-                                    : make_desc(ca, 16, 256, SW32);
-            tc_mma_bf16(tmem_base, ad, make_desc(sb + q * p.nt * 32, 16, 256, SW32), idesc, acc);
-            acc = 1;
-          }
-          tc_commit(empty_bar(s));
-        }
-        __syncwarp();
-        if (++s == p.stages) {
-          s = 0;
-          phase ^= 1u;
-        }
-      }
-    }
     if (ok && lane == 0) tc_commit(done_bar);
     __syncwarp();
-  } else if (warp < 4) {
-    // ------------------------------------------------------------ factors of the tokens
-    if (ext) {
-      grid_dependency_wait();
-      const int total = p.tile_count[tn] * p.chunks;
-      const int tid = threadIdx.x - 64;
-      int s = (ks1 - ks0) % p.stages;
-      uint32_t phase = (uint32_t)((ks1 - ks0) / p.stages) & 1u;
-      bool ok = true;
-      int o = 0;
-      for (int e = rank; e * CHUNKS < total && ok; e += S, ++o) {
-        // these warps skip the main k steps, so the parity of the ring's own barriers says nothing
-        // to them before the producer, which has seen every turn, hands the stage over
-        ok = mbar_wait(grant_bar(s), (uint32_t)(o / p.stages) & 1u, abort_flag);
-        if (!ok) break;
-        unsigned char* st = smem + (size_t)s * stage_bytes;
-        const int nc = min(CHUNKS, total - e * CHUNKS);
-        for (int q = 0; q < nc; ++q) {
-          const int ch = e * CHUNKS + q;
-          const int who = p.tile_list[(int64_t)tn * p.nt + ch / p.chunks];
-          const int j0 = 16 * (ch % p.chunks);
-          unsigned char* fac = st + A_BYTES + (size_t)q * p.nt * 32;
-          for (int row = tid; row < p.nt; row += 64) {
-            uint32_t w[8];
-            factor_row(p, n0 + row, who, j0, w);
-            // 32-byte rows, 32-byte swizzle: the 16-byte halves swap every four rows
-            const int sw = ((row >> 2) & 1) << 4;
-            *reinterpret_cast<uint4*>(fac + row * 32 + (0 ^ sw)) = make_uint4(w[0], w[1], w[2], w[3]);
-            *reinterpret_cast<uint4*>(fac + row * 32 + (16 ^ sw)) = make_uint4(w[4], w[5], w[6], w[7]);
-          }
+  } else {
+    const int g = warp & 3, half = (warp - 2) >> 2;
+    const int row = 32 * g + lane;
+    if constexpr (EPI == PROJ_OUT) {
+      // ---------------------------------------------------------- adapter part
+#pragma unroll
+      for (int q = 0; q < Q; ++q)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) own[q][e] = 0.f;
+      if (p.early) grid_dependency_wait();
+      if (p.n_adapters > 0) {
+        const int tid = threadIdx.x - 64, m = m0 + row;
+        bool any = false;
+        if (tid < p.nt) {
+          const int t = n0 + tid;
+          const int i = t < p.N ? valid_adapter(p, t) : -1;
+          ids[tid] = i;
+          any = i >= 0;
+          if (tm == 0 && rank == 0 && t < p.N && i < 0 && p.index[t] != -1)
+            atomicCAS(p.status, 0, (int)THANOS_ERR_INVALID_ARG);
         }
-        ok = mbar_wait(full_bar(s), phase, abort_flag);
-        if (!ok) break;
-        for (int q = tid; q < nc * (CHUNK_BYTES / 16); q += 64)
-          clean_vector(reinterpret_cast<uint4*>(st) + q, poison);
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive(factor_bar(s));
-        if (++s == p.stages) {
-          s = 0;
-          phase ^= 1u;
+        int used;
+        asm volatile(
+            "{\n.reg .pred a, b;\nsetp.ne.u32 a, %1, 0;\n"
+            "barrier.cta.red.or.aligned.pred b, 1, 256, a;\nselp.u32 %0, 1, 0, b;\n}"
+            : "=r"(used)
+            : "r"((int)any)
+            : "memory");
+        for (int j0 = 0; j0 < p.r && used; j0 += 16) {
+          if (j0 > 0) epilogue_sync();
+          for (int e = tid; e < p.nt * 16; e += 256) {
+            const int t = n0 + (e >> 4), j = j0 + (e & 15), i = ids[e >> 4];
+            float v = 0.f;
+            if (i >= 0 && j < p.r) {
+              v = p.V[(int64_t)t * p.r + j];
+              if (p.scale) v *= p.scale[i];
+            }
+            factor[e] = v;
+          }
+          epilogue_sync();
+          if (m < p.M) {
+#pragma unroll
+            for (int q = 0; q < Q; ++q) {
+              const int c = tile_column(S, rank, half, q);
+              if (c >= p.nt || n0 + c >= p.N) continue;
+              const int first = ids[c];
+              bool same = true;
+#pragma unroll
+              for (int e = 1; e < 8; ++e) same = same && ids[c + e] == first;
+              if (same) {  // a run of one request's tokens (or none): its row is read once
+                if (first >= 0) {
+                  uint32_t w[8];
+                  wide_row<AMN>(p, first, m, j0, w);
+#pragma unroll
+                  for (int e = 0; e < 8; ++e) own[q][e] = dot16(w, factor + (c + e) * 16, own[q][e]);
+                }
+              } else {
+#pragma unroll
+                for (int e4 = 0; e4 < 8; e4 += 4) {  // four rows in flight
+                  uint32_t w[4][8];
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) wide_row<AMN>(p, ids[c + e4 + e], m, j0, w[e]);
+#pragma unroll
+                  for (int e = 0; e < 4; ++e)
+                    if (ids[c + e4 + e] >= 0)
+                      own[q][e4 + e] = dot16(w[e], factor + (c + e4 + e) * 16, own[q][e4 + e]);
+                }
+              }
+            }
+          }
         }
       }
     }
-  } else {
     // ------------------------------------------------------------ epilogue, one slice of k
-    const int g = warp & 3;
     const bool ok = mbar_wait(done_bar, 0, abort_flag);
     tc_fence_after();
-    if (ext || p.early) grid_dependency_wait();
     const uint32_t taddr = tmem_base + ((uint32_t)(32 * g) << 16);
-    const int row = 32 * g + lane;
-    if (ext && tm == 0 && rank == 0) {
-      for (int t = n0 + (int)threadIdx.x - 128; t < min(n0 + p.nt, p.N); t += 256)
-        if (p.index[t] != -1 && valid_adapter(p, t) < 0)
-          atomicCAS(p.status, 0, (int)THANOS_ERR_INVALID_ARG);
-    }
     if (ok) {
-      const bool poisoned = ext && *(volatile int*)poison != 0;
-      for (int cc = 32 * ((warp - 4) >> 2); cc < p.nt; cc += 64) {
+#pragma unroll
+      for (int c2 = 0; c2 < 4; ++c2) {
+        const int cc = 32 * half + 64 * c2;
+        if (cc >= p.nt) break;
         uint32_t u[32];
         tc_ld32(taddr + cc, u);
         tc_wait_ld();
@@ -572,7 +599,13 @@ proj_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
 #pragma unroll
         for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(u[e]);
         if (S == 1) {
-          emit<AMN, EPI, 32>(p, z, m0 + row, n0 + cc, v, tn != tm, poisoned);
+          if constexpr (EPI == PROJ_OUT) {
+            if (c2 < Q / 4) {
+#pragma unroll
+              for (int e = 0; e < 32; ++e) v[e] += own[(c2 & 1) * 4 + e / 8][e & 7];
+            }
+          }
+          emit<AMN, EPI, 32>(p, z, m0 + row, n0 + cc, v, tn != tm, false);
         } else {
           // partial sums [n][m] in the ring, whose operands have all been consumed
           float* part = reinterpret_cast<float*>(smem);
@@ -592,21 +625,24 @@ proj_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
   if (threadIdx.x == 0 && *abort_flag) atomicCAS(p.status, 0, (int)THANOS_ERR_TIMEOUT);
   if (S > 1) {
     cluster_sync_all();
-    if (warp >= 4) {
-      bool bad = false, poisoned = false;
-      for (int q = 0; q < S; ++q) {
+    if (warp >= 2) {
+      bool bad = false;
+      for (int q = 0; q < S; ++q)
         bad = bad || ld_cluster_u32(map_to_cta(smem_u32((const void*)abort_flag), q)) != 0;
-        poisoned = poisoned || ld_cluster_u32(map_to_cta(smem_u32(poison), q)) != 0;
-      }
-      const int row = (threadIdx.x - 128) & 127, half = (threadIdx.x - 128) >> 7;
-      for (int c8 = rank + S * half; c8 * 8 < p.nt && !bad; c8 += 2 * S) {
-        float f[8] = {};
+      const int half = (warp - 2) >> 2, row = 32 * (warp & 3) + lane;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int c = tile_column(S, rank, half, k);
+        if (c >= p.nt || bad) continue;
+        float f[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = EPI == PROJ_OUT ? own[k % Q][e] : 0.f;
         for (int q = 0; q < S; ++q) {
-          const uint32_t src = map_to_cta(smem_base, q) + (uint32_t)(c8 * 8 * TM + row) * 4u;
+          const uint32_t src = map_to_cta(smem_base, q) + (uint32_t)(c * TM + row) * 4u;
 #pragma unroll
           for (int e = 0; e < 8; ++e) f[e] += ld_cluster(src + e * TM * 4);
         }
-        emit<AMN, EPI, 8>(p, z, m0 + row, n0 + c8 * 8, f, tn != tm, poisoned);
+        emit<AMN, EPI, 8>(p, z, m0 + row, n0 + c, f, tn != tm, false);
       }
     }
     cluster_sync_all();  // no CTA leaves while another may still read its partial sums
@@ -618,10 +654,22 @@ proj_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
 // nt, CTA r holds rows 128 r .. +127 in its tensor memory and loads only those and half of the n
 // rows, so an SM moves 32 KB instead of 48 KB through shared memory per 64-wide k step of a 256-wide
 // tile.  Two accumulators: the epilogue of a tile runs beside the next tile's products.
+//
+// Adapter part (PROJ_OUT): for every adapter that occurs in the token tile, k is extended by its rank
+// in chunks of 16, four chunks a stage, in a ring of their own that four more warps fill a tile
+// ahead: the wide factor's rows come by TMA (32-byte swizzle; MN-major: 128-byte), the factor of the
+// tokens, s_i V[t], is built in bf16 with zero rows for tokens of other adapters.  0 times a
+// non-finite weight would reach those tokens, so the chunk is scanned, non-finite weights become
+// zeros and the epilogue adds their products to the adapter's own tokens.
 constexpr int PTM = 256;
-constexpr int PSTAGES = 6;
 constexpr int PSTAGE_BYTES = 2 * A_BYTES;
-constexpr size_t PSMEM_BYTES = (size_t)PSTAGES * PSTAGE_BYTES + 1024 + 512;
+constexpr int CHUNK_BYTES = TM * 16 * 2;      // a 16-wide chunk of an adapter's wide factor
+constexpr int CHUNKS = 4;                     // chunks per stage
+constexpr int ESTAGES = 2;
+__host__ __device__ constexpr int pair_stages(int epi) { return epi == PROJ_OUT ? 5 : 7; }
+__host__ __device__ constexpr int pair_threads(int epi) { return epi == PROJ_OUT ? 448 : 320; }
+constexpr size_t PSMEM_BYTES = (size_t)7 * PSTAGE_BYTES + 1024 + 512;
+static_assert(pair_stages(PROJ_OUT) + ESTAGES == 7, "shared memory of the rings");
 
 __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap* map,
                                                  uint32_t lead_bar, int x, int y, int z) {
@@ -663,44 +711,52 @@ __device__ __forceinline__ PairTile pair_tile(const Params& p, int t) {
 }
 
 template <bool AMN, int EPI>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(pair_threads(EPI), 1)
 pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
             const __grid_constant__ CUtensorMap mapP, const Params p, const int n_tiles) {
+  constexpr bool EXT = EPI == PROJ_OUT;
+  constexpr int STAGES = pair_stages(EPI);
+  constexpr int EPI_WARP = EXT ? 6 : 2;       // first of the eight epilogue warps
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + (size_t)PSTAGES * PSTAGE_BYTES);
-  // full, empty, factor ready (full and factor used in the first CTA), stage granted, chunk landed;
-  // then accumulator full (2) and empty (2, used in the first CTA)
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 5 * PSTAGES + 4);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 5 * PSTAGES + 5);
-  int* poison = reinterpret_cast<int*>(bars + 5 * PSTAGES + 6);
+  unsigned char* ering = smem + (size_t)STAGES * PSTAGE_BYTES;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + (size_t)7 * PSTAGE_BYTES);
+  // full (used in the first CTA), empty (STAGES each); accumulator full, accumulator empty (first
+  // CTA); adapter stage: chunks landed, ready (first CTA), empty
+  constexpr int B_TFULL = 2 * STAGES, B_EXT = B_TFULL + 4;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + B_EXT + 3 * ESTAGES);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + B_EXT + 3 * ESTAGES + 1);
+  int* poison = reinterpret_cast<int*>(bars + B_EXT + 3 * ESTAGES + 2);
 
   const int warp = threadIdx.x >> 5;
   const int lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
   const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
   const uint32_t smem_base = smem_u32(smem);
+  const uint32_t ering_base = smem_u32(ering);
   const uint32_t bar_base = smem_u32(bars);
   auto full_bar = [&](int s) { return bar_base + 8u * s; };
-  auto empty_bar = [&](int s) { return bar_base + 8u * (PSTAGES + s); };
-  auto factor_bar = [&](int s) { return bar_base + 8u * (2 * PSTAGES + s); };
-  auto grant_bar = [&](int s) { return bar_base + 8u * (3 * PSTAGES + s); };
-  auto land_bar = [&](int s) { return bar_base + 8u * (4 * PSTAGES + s); };
-  auto tfull_bar = [&](int q) { return bar_base + 8u * (5 * PSTAGES + q); };
-  auto tempty_bar = [&](int q) { return bar_base + 8u * (5 * PSTAGES + 2 + q); };
+  auto empty_bar = [&](int s) { return bar_base + 8u * (STAGES + s); };
+  auto tfull_bar = [&](int q) { return bar_base + 8u * (B_TFULL + q); };
+  auto tempty_bar = [&](int q) { return bar_base + 8u * (B_TFULL + 2 + q); };
+  auto land_bar = [&](int e) { return bar_base + 8u * (B_EXT + e); };
+  auto ready_bar = [&](int e) { return bar_base + 8u * (B_EXT + ESTAGES + e); };
+  auto eempty_bar = [&](int e) { return bar_base + 8u * (B_EXT + 2 * ESTAGES + e); };
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < PSTAGES; ++s) {
+    for (int s = 0; s < STAGES; ++s) {
       mbar_init(full_bar(s), 1);
       mbar_init(empty_bar(s), 1);
-      mbar_init(factor_bar(s), 4);  // two warps in each CTA
-      mbar_init(grant_bar(s), 1);
-      mbar_init(land_bar(s), 1);
     }
     for (int q = 0; q < 2; ++q) {
       mbar_init(tfull_bar(q), 1);
       mbar_init(tempty_bar(q), 16);  // eight epilogue warps in each CTA
+    }
+    for (int e = 0; e < ESTAGES; ++e) {
+      mbar_init(land_bar(e), 1);
+      mbar_init(ready_bar(e), 8);    // four warps in each CTA
+      mbar_init(eempty_bar(e), 1);
     }
     *abort_flag = 0;
     *poison = 0;
@@ -724,14 +780,13 @@ pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
 
   const int nk = (p.K + BK - 1) / BK;
   const int half = p.nt / 2;  // n rows that this CTA loads
-  constexpr bool EXT = EPI == PROJ_OUT;
   const bool ext = EXT && p.n_adapters > 0;
 
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
     int s = 0;
     uint32_t phase = 0;
-    bool ok = true, waited = false;
+    bool ok = true;
     for (int t = pair; t < n_tiles && ok; t += npairs) {
       const PairTile tl = pair_tile(p, t);
       const int m0 = tl.tm * PTM + 128 * (int)rank, n0 = tl.tn * p.nt + half * (int)rank;
@@ -750,42 +805,9 @@ pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
           tma_load_3d_pair(dst + A_BYTES, &mapB, lead, ks * BK, n0, tl.z);
         }
         __syncwarp();
-        if (++s == PSTAGES) {
+        if (++s == STAGES) {
           s = 0;
           phase ^= 1u;
-        }
-      }
-      if (ext && ok) {
-        if (!waited) grid_dependency_wait();
-        waited = true;
-        const int total = p.tile_count[tl.tn] * p.chunks;
-        for (int c0 = 0; c0 < total && ok; c0 += CHUNKS) {
-          ok = mbar_wait(empty_bar(s), phase ^ 1u, abort_flag);
-          if (ok && lane == 0) {
-            const uint32_t dst = smem_base + (uint32_t)s * PSTAGE_BYTES;
-            const int nc = min(CHUNKS, total - c0);
-            // the stage's readiness goes over the factor barrier; its turn on the full barrier is
-            // only kept in step
-            if (rank == 0) mbar_arrive(full_bar(s));
-            mbar_arrive(grant_bar(s));
-            mbar_expect_tx(land_bar(s), nc * CHUNK_BYTES);
-            for (int q = 0; q < nc; ++q) {
-              const int who = p.tile_list[(int64_t)tl.tn * p.nt + (c0 + q) / p.chunks];
-              const int j = 16 * ((c0 + q) % p.chunks);
-              if (AMN) {
-                tma_load_3d(dst + q * CHUNK_BYTES, &mapP, land_bar(s), m0, j, who);
-                tma_load_3d(dst + q * CHUNK_BYTES + CHUNK_BYTES / 2, &mapP, land_bar(s), m0 + 64, j,
-                            who);
-              } else {
-                tma_load_3d(dst + q * CHUNK_BYTES, &mapP, land_bar(s), j, m0, who);
-              }
-            }
-          }
-          __syncwarp();
-          if (++s == PSTAGES) {
-            s = 0;
-            phase ^= 1u;
-          }
         }
       }
     }
@@ -802,8 +824,8 @@ pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
       if (AMN) idesc |= 1u << 15;
       idesc |= (uint32_t)(p.nt >> 3) << 17;
       idesc |= (uint32_t)(PTM >> 4) << 24;
-      int s = 0, q = 0;
-      uint32_t phase = 0, tphase = 0, turn = 0;  // turn: bit s = parity of stage s as adapter stage
+      int s = 0, q = 0, e = 0;
+      uint32_t phase = 0, tphase = 0, ephase = 0;
       bool ok = true, waited = false;
       for (int t = pair; t < n_tiles && ok; t += npairs) {
         const PairTile tl = pair_tile(p, t);
@@ -826,7 +848,7 @@ pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
             tc_commit_pair(empty_bar(s));
           }
           __syncwarp();
-          if (++s == PSTAGES) {
+          if (++s == STAGES) {
             s = 0;
             phase ^= 1u;
           }
@@ -836,12 +858,10 @@ pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
           waited = true;
           const int total = p.tile_count[tl.tn] * p.chunks;
           for (int c0 = 0; c0 < total && ok; c0 += CHUNKS) {
-            ok = mbar_wait(full_bar(s), phase, abort_flag) &&
-                 mbar_wait(factor_bar(s), (turn >> s) & 1u, abort_flag);
-            turn ^= 1u << s;
+            ok = mbar_wait(ready_bar(e), ephase, abort_flag);
             tc_fence_after();
             if (ok && lane == 0) {
-              const uint32_t sa = smem_base + (uint32_t)s * PSTAGE_BYTES;
+              const uint32_t sa = ering_base + (uint32_t)e * PSTAGE_BYTES;
               const uint32_t sb = sa + A_BYTES;
               const int nc = min(CHUNKS, total - c0);
               for (int c = 0; c < nc; ++c) {
@@ -850,12 +870,12 @@ pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
                                         : make_desc(ca, 16, 256, SW32);
                 tc_mma_bf16_pair(d, ad, make_desc(sb + c * 128 * 32, 16, 256, SW32), idesc, 1u);
               }
-              tc_commit_pair(empty_bar(s));
+              tc_commit_pair(eempty_bar(e));
             }
             __syncwarp();
-            if (++s == PSTAGES) {
-              s = 0;
-              phase ^= 1u;
+            if (++e == ESTAGES) {
+              e = 0;
+              ephase ^= 1u;
             }
           }
         }
@@ -867,55 +887,74 @@ pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
         }
       }
     }
-  } else if (warp < 4) {
-    // ------------------------------------------------------------ factors of the tokens
+  } else if (warp < EPI_WARP) {
+    // ------------------------------------------------------------ adapter stages
     if (ext) {
       grid_dependency_wait();
-      const int tid = threadIdx.x - 64;
-      int s = 0;
-      uint32_t turn = 0;
+      const int row = threadIdx.x - 64;  // the token row of this thread, warps 2..5
+      int e = 0;
+      uint32_t ephase = 0;
       bool ok = true;
       for (int t = pair; t < n_tiles && ok; t += npairs) {
         const PairTile tl = pair_tile(p, t);
-        const int n0 = tl.tn * p.nt + half * (int)rank;
+        const int m0 = tl.tm * PTM + 128 * (int)rank;
+        const int tok = tl.tn * p.nt + half * (int)rank + row;
+        const int mine = row < half && tok < p.N ? valid_adapter(p, tok) : -1;
+        const float sc = mine >= 0 && p.scale ? p.scale[mine] : 1.f;
         const int total = p.tile_count[tl.tn] * p.chunks;
-        s = (s + nk) % PSTAGES;
         for (int c0 = 0; c0 < total && ok; c0 += CHUNKS) {
-          const uint32_t par = (turn >> s) & 1u;
-          turn ^= 1u << s;
-          ok = mbar_wait(grant_bar(s), par, abort_flag);
+          ok = mbar_wait(eempty_bar(e), ephase ^ 1u, abort_flag);
           if (!ok) break;
-          unsigned char* st = smem + (size_t)s * PSTAGE_BYTES;
+          unsigned char* st = ering + (size_t)e * PSTAGE_BYTES;
+          const uint32_t dst = ering_base + (uint32_t)e * PSTAGE_BYTES;
           const int nc = min(CHUNKS, total - c0);
-          for (int q = 0; q < nc; ++q) {
-            const int who = p.tile_list[(int64_t)tl.tn * p.nt + (c0 + q) / p.chunks];
-            const int j0 = 16 * ((c0 + q) % p.chunks);
-            unsigned char* fac = st + A_BYTES + (size_t)q * 128 * 32;
-            for (int row = tid; row < half; row += 64) {
-              uint32_t w[8];
-              factor_row(p, n0 + row, who, j0, w);
-              const int sw = ((row >> 2) & 1) << 4;
-              *reinterpret_cast<uint4*>(fac + row * 32 + sw) = make_uint4(w[0], w[1], w[2], w[3]);
-              *reinterpret_cast<uint4*>(fac + row * 32 + (16 ^ sw)) =
-                  make_uint4(w[4], w[5], w[6], w[7]);
+          if (threadIdx.x == 64) {
+            mbar_expect_tx(land_bar(e), nc * CHUNK_BYTES);
+            for (int q = 0; q < nc; ++q) {
+              const int who = p.tile_list[(int64_t)tl.tn * p.nt + (c0 + q) / p.chunks];
+              const int j = 16 * ((c0 + q) % p.chunks);
+              if (AMN) {
+                tma_load_3d(dst + q * CHUNK_BYTES, &mapP, land_bar(e), m0, j, who);
+                tma_load_3d(dst + q * CHUNK_BYTES + CHUNK_BYTES / 2, &mapP, land_bar(e), m0 + 64, j,
+                            who);
+              } else {
+                tma_load_3d(dst + q * CHUNK_BYTES, &mapP, land_bar(e), j, m0, who);
+              }
             }
           }
-          ok = mbar_wait(land_bar(s), par, abort_flag);
+          __syncwarp();
+          for (int q = 0; q < nc; ++q) {
+            const int who = p.tile_list[(int64_t)tl.tn * p.nt + (c0 + q) / p.chunks];
+            uint32_t w[8];
+            factor_row(p, tok, who == mine, sc, 16 * ((c0 + q) % p.chunks), w);
+            // 32-byte rows, 32-byte swizzle: the 16-byte halves swap every four rows
+            unsigned char* fac = st + A_BYTES + (size_t)q * 128 * 32 + row * 32;
+            const int sw = ((row >> 2) & 1) << 4;
+            *reinterpret_cast<uint4*>(fac + sw) = make_uint4(w[0], w[1], w[2], w[3]);
+            *reinterpret_cast<uint4*>(fac + (16 ^ sw)) = make_uint4(w[4], w[5], w[6], w[7]);
+          }
+          ok = mbar_wait(land_bar(e), ephase, abort_flag);
           if (!ok) break;
-          for (int q = tid; q < nc * (CHUNK_BYTES / 16); q += 64)
+          for (int q = row; q < nc * (CHUNK_BYTES / 16); q += 128)
             clean_vector(reinterpret_cast<uint4*>(st) + q, poison);
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(map_to_cta(factor_bar(s), 0));
-          if (++s == PSTAGES) s = 0;
+          if (lane == 0) mbar_arrive_cluster(map_to_cta(ready_bar(e), 0));
+          if (++e == ESTAGES) {
+            e = 0;
+            ephase ^= 1u;
+          }
         }
+      }
+      if (!ok) {  // as above: chunks in flight
+        for (int i = 0; i < 2000; ++i) __nanosleep(1000);
       }
     }
   } else {
     // ------------------------------------------------------------ epilogue
-    const int g = warp & 3, h = (warp - 4) >> 2;
-    const uint32_t lead_tempty[2] = {map_to_cta(tempty_bar(0), 0), map_to_cta(tempty_bar(1), 0)};
-    if (ext || p.early) grid_dependency_wait();
+    const int g = warp & 3, h = (warp - EPI_WARP) >> 2;
+    const uint32_t lead_tempty = map_to_cta(tempty_bar(0), 0);
+    if (p.early) grid_dependency_wait();
     int q = 0;
     uint32_t tphase = 0;
     bool ok = true;
@@ -927,7 +966,7 @@ pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
         const int n0 = tl.tn * p.nt;
         const int m = tl.tm * PTM + 128 * (int)rank + 32 * g + lane;
         if (ext && tl.tm == 0 && rank == 0) {
-          for (int u = n0 + (int)threadIdx.x - 128; u < min(n0 + p.nt, p.N); u += 256)
+          for (int u = n0 + (int)threadIdx.x - 32 * EPI_WARP; u < min(n0 + p.nt, p.N); u += 256)
             if (p.index[u] != -1 && valid_adapter(p, u) < 0)
               atomicCAS(p.status, 0, (int)THANOS_ERR_INVALID_ARG);
         }
@@ -940,13 +979,13 @@ pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
           tc_wait_ld();
           float v[32];
 #pragma unroll
-          for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(u[e]);
+          for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(u[i]);
           emit<AMN, EPI, 32>(p, tl.z, m, n0 + cc, v, tl.tm != tl.tn, poisoned);
         }
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(lead_tempty[q]);
+      if (lane == 0) mbar_arrive_cluster(lead_tempty + 8u * q);
       if (++q == 2) {
         q = 0;
         tphase ^= 1u;
@@ -983,14 +1022,14 @@ bool make_map3(CUtensorMap* map, const void* base, bool f16, int64_t inner, int6
 }
 
 template <bool AMN, int EPI>
-thanos_status_t launch(const CUtensorMap& mA, const CUtensorMap& mB, const CUtensorMap& mP,
-                       const Params& p, cudaStream_t stream) {
+thanos_status_t launch(const CUtensorMap& mA, const CUtensorMap& mB, const Params& p,
+                       cudaStream_t stream) {
   static std::atomic<unsigned long long> done{0};
-  THANOS_CUDA(ensure_max_dyn_smem(proj_kernel<AMN, EPI>, (int)SMEM_BYTES, done));
+  THANOS_CUDA(ensure_max_dyn_smem(tile_kernel<AMN, EPI>, 227 * 1024, done));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((int64_t)p.tiles_m * p.tiles_n * p.splits), (unsigned)p.batch_z, 1);
-  cfg.blockDim = dim3(NTHREADS, 1, 1);
-  cfg.dynamicSmemBytes = SMEM_BYTES;
+  cfg.blockDim = dim3(TILE_THREADS, 1, 1);
+  cfg.dynamicSmemBytes = (size_t)p.ring_bytes + FACTOR_BYTES + 512 /*ids*/ + 256 /*barriers*/ + 1024;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -1002,7 +1041,7 @@ thanos_status_t launch(const CUtensorMap& mA, const CUtensorMap& mB, const CUten
   cfg.attrs = attr;
   cfg.numAttrs = 2;
   count_launch();
-  THANOS_CUDA(cudaLaunchKernelEx(&cfg, proj_kernel<AMN, EPI>, mA, mB, mP, p));
+  THANOS_CUDA(cudaLaunchKernelEx(&cfg, tile_kernel<AMN, EPI>, mA, mB, p));
   return THANOS_OK;
 }
 
@@ -1020,7 +1059,7 @@ int max_active_pairs() {
   }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2 * sm_count(), 1, 1);
-  cfg.blockDim = dim3(NTHREADS, 1, 1);
+  cfg.blockDim = dim3(pair_threads(EPI), 1, 1);
   cfg.dynamicSmemBytes = PSMEM_BYTES;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -1049,7 +1088,7 @@ thanos_status_t launch_pair(const CUtensorMap& mA, const CUtensorMap& mB, const 
   if (tiles > (1 << 30)) return THANOS_ERR_SHAPE;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(2 * (tiles < G ? tiles : G)), 1, 1);
-  cfg.blockDim = dim3(NTHREADS, 1, 1);
+  cfg.blockDim = dim3(pair_threads(EPI), 1, 1);
   cfg.dynamicSmemBytes = PSMEM_BYTES;
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
@@ -1066,7 +1105,7 @@ template <bool AMN, int EPI>
 thanos_status_t launch_any(bool pairs, const CUtensorMap& mA, const CUtensorMap& mB,
                            const CUtensorMap& mP, const Params& p, cudaStream_t stream) {
   return pairs ? launch_pair<AMN, EPI>(mA, mB, mP, p, stream)
-               : launch<AMN, EPI>(mA, mB, mP, p, stream);
+               : launch<AMN, EPI>(mA, mB, p, stream);
 }
 
 // Whether a product runs on CTA pairs: once its 256 x 256 tiles occupy at least half of the pairs.
@@ -1078,10 +1117,7 @@ bool use_pairs(int64_t M, int64_t N, int64_t batch, bool symmetric) {
 
 }  // namespace
 
-int proj_token_tile(int64_t N, int64_t M) {
-  if (use_pairs(M, N, 1, false)) return 256;
-  return N <= 32 ? 32 : N <= 64 ? 64 : N <= 128 ? 128 : 256;
-}
+int proj_pair_tile(int64_t N, int64_t M) { return use_pairs(M, N, 1, false) ? PTM : 0; }
 
 thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
   if (a.M <= 0 || a.N <= 0 || a.batch <= 0) return THANOS_OK;
@@ -1093,8 +1129,7 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
   p.N = a.N;
   p.K = a.K;
   const bool pairs = a.epi != PROJ_SHRINK && use_pairs(a.M, a.N, a.batch, symmetric);
-  p.nt = symmetric ? (pairs ? PTM : TM) : a.nt ? a.nt : proj_token_tile(a.N, a.M);
-  if (pairs && a.epi > PROJ_SHRINK) p.nt = PTM;
+  p.nt = pairs ? PTM : symmetric || a.N > 64 ? TM : a.N > 32 ? 64 : 32;
   p.tiles_m = (a.M + (pairs ? PTM : TM) - 1) / (pairs ? PTM : TM);
   p.tiles_n = (a.N + p.nt - 1) / p.nt;
   p.batch_z = a.batch;
@@ -1106,11 +1141,14 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
   if (symmetric) tiles = (int64_t)p.tiles_m * (p.tiles_m + 1) / 2 * a.batch;
   const int nk = (a.K + BK - 1) / BK;
   p.splits = 1;
-  while (p.splits < 8 && tiles * p.splits * 2 <= sm_count() && nk >= 8 * p.splits) p.splits *= 2;
+  // the projections run two CTAs per SM
+  const int slots = a.epi <= PROJ_SHRINK ? 2 * sm_count() : sm_count();
+  while (p.splits < 8 && tiles * p.splits * 2 <= slots && nk >= 8 * p.splits) p.splits *= 2;
   if (tiles > (1 << 27) || a.batch > 65535) return THANOS_ERR_SHAPE;
   const int stage_bytes = A_BYTES + p.nt * BK * 2;
-  p.stages = RING_BYTES / stage_bytes;
+  p.stages = (a.epi <= PROJ_SHRINK ? 100 : 200) * 1024 / stage_bytes;
   if (p.stages > MAX_STAGES) p.stages = MAX_STAGES;
+  p.ring_bytes = p.stages * stage_bytes;
   p.out = a.out;
   p.ldo = a.ldo;
   p.V = a.V;
@@ -1153,7 +1191,7 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
                          pairs ? p.nt / 2 : p.nt, sw))
     return THANOS_ERR_CUDA;
   mP = mA;
-  if (a.epi == PROJ_OUT && a.n_adapters > 0) {
+  if (pairs && a.epi == PROJ_OUT && a.n_adapters > 0) {
     if (a.ldp % 8 || a.p_adapter % 8 || !aligned16(a.P)) return THANOS_ERR_ALIGNMENT;
     const bool ok =
         a.a_mn ? make_map3(&mP, a.P, false, a.M, a.r, a.ldp, a.n_adapters, a.p_adapter, 64, 16, sw)
@@ -1166,7 +1204,7 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
       return a.a_mn ? launch_any<true, PROJ_OUT>(pairs, mA, mB, mP, p, stream)
                     : launch_any<false, PROJ_OUT>(pairs, mA, mB, mP, p, stream);
     case PROJ_SHRINK:
-      return launch<false, PROJ_SHRINK>(mA, mB, mP, p, stream);
+      return launch<false, PROJ_SHRINK>(mA, mB, p, stream);
     case PROJ_GRAM:
       return launch_any<false, PROJ_GRAM>(pairs, mA, mB, mP, p, stream);
     case PROJ_POLY:

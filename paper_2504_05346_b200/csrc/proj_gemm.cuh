@@ -32,7 +32,6 @@ struct ProjArgs {
   int64_t ldb = 0, b_batch = 0;
   int f16 = 0;                   // operands fp16 instead of bf16
   int epi = PROJ_OUT;
-  int nt = 0;                    // tile width in n: 32, 64, 128, 256 (0: chosen here)
   int early = 0;                 // operands do not depend on the previous launch of the stream
   int32_t* status = nullptr;
   // PROJ_OUT, PROJ_SHRINK
@@ -42,10 +41,12 @@ struct ProjArgs {
   const int32_t* index = nullptr;
   const float* scale = nullptr;  // factor of a row of V by its adapter, or null
   int n_adapters = 0, r = 0;
-  const int32_t* tile_count = nullptr;  // distinct adapters of every token tile of width nt
-  const int32_t* tile_list = nullptr;   // [tiles, nt]
+  // distinct adapters of every token tile of proj_pair_tile() tokens, [tiles] and [tiles, width]
+  const int32_t* tile_count = nullptr;
+  const int32_t* tile_list = nullptr;
   const void* P = nullptr;       // PROJ_OUT: the adapters' wide factor, bf16
-  int64_t ldp = 0, p_adapter = 0;       // a_mn == 0: [n][M][ldp]; else [n][r][ldp]
+  int64_t ldp = 0, p_adapter = 0;       // a_mn == 0: [n][M][ldp]; else [n][r][ldp].  On CTA pairs
+                                        // ldp and p_adapter are multiples of 8
   // PROJ_GRAM .. PROJ_FINAL
   float alpha = 1.f, beta = 0.f;
   __half* S = nullptr;           // GRAM: written, POLY: read
@@ -64,8 +65,9 @@ struct ProjArgs {
   float keep = 1.f, rate = 0.f;
 };
 
-// Width of the token tiles that PROJ_OUT and PROJ_SHRINK use for N tokens and M features.
-int proj_token_tile(int64_t N, int64_t M);
+// Width of the token tiles for which PROJ_OUT needs the lists of distinct adapters; 0 if the product
+// (N tokens, M features) does not run on CTA pairs and needs none.
+int proj_pair_tile(int64_t N, int64_t M);
 
 thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream);
 
