@@ -63,6 +63,7 @@ class PruneStats:
 
 
 _lib = None
+_NO_SCOPE = contextlib.nullcontext()
 
 
 def lib_path() -> str:
@@ -169,8 +170,9 @@ def _dtype_code(t: torch.Tensor) -> int:
 
 
 def _stream_ptr(stream) -> int:
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return int(s.cuda_stream)
+    if stream is not None:
+        return int(stream.cuda_stream)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _check_dev(*ts):
@@ -191,6 +193,8 @@ def _check(code: int, where: str):
 def _on(t: torch.Tensor):
     """Makes the tensor's device current for the duration of a library call (kernels are
     launched on, and per-device state is looked up for, the current device)."""
+    if t.get_device() == torch.cuda.current_device():
+        return _NO_SCOPE
     return torch.cuda.device(t.device)
 
 
@@ -493,39 +497,39 @@ def _alloc_scope(stream):
     """Buffers made for a call on another stream come from that stream's pool: the caching
     allocator then neither hands out memory that the current stream still uses nor takes it back
     before the call is done."""
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+    return _NO_SCOPE if stream is None else torch.cuda.stream(stream)
 
 
-def _rows(t: torch.Tensor, cols: int, name: str) -> int:
-    """Leading dimension of a CUDA matrix with `cols` columns and unit inner stride."""
-    if not t.is_cuda or t.dim() != 2 or t.shape[1] != cols:
-        raise ValueError("%s must be a CUDA matrix with %d columns" % (name, cols))
-    if t.shape[0] > 1:
-        if cols > 1 and t.stride(1) != 1:
-            raise ValueError("%s must have unit inner stride" % name)
-        return t.stride(0)
-    if cols > 1 and t.stride(1) != 1:
+# The checks below run in front of calls that take a dozen microseconds on the device, so they ask
+# each tensor for as little as they can.
+def _rows(t: torch.Tensor, cols: int, device: int, name: str) -> int:
+    """Leading dimension of a matrix on `device` with `cols` columns and unit inner stride."""
+    if t.get_device() != device or t.dim() != 2 or t.shape[1] != cols:
+        raise ValueError("%s must be a matrix of %d columns on CUDA device %d" % (name, cols, device))
+    ld, inner = t.stride()
+    if inner != 1 and cols > 1:
         raise ValueError("%s must have unit inner stride" % name)
-    return (cols + 7) // 8 * 8   # one row: its stride is never used
+    return ld if t.shape[0] > 1 else (cols + 7) // 8 * 8   # one row: its stride is never used
 
 
-def _dense(t: torch.Tensor, shape, dtype, name: str) -> torch.Tensor:
-    if not t.is_cuda or not t.is_contiguous() or tuple(t.shape) != tuple(shape) or t.dtype != dtype:
-        raise ValueError("%s must be a contiguous CUDA %s tensor of shape %s"
-                         % (name, dtype, tuple(shape)))
-    return t
+def _dense(t: torch.Tensor, shape, dtype, device: int, name: str) -> None:
+    if (t.get_device() != device or t.dtype != dtype or t.shape != shape
+            or not t.is_contiguous()):
+        raise ValueError("%s must be a contiguous %s tensor of shape %s on CUDA device %d"
+                         % (name, dtype, tuple(shape), device))
 
 
-def _same_device(*ts):
-    for t in ts[1:]:
-        if t is not None and t.device != ts[0].device:
-            raise ValueError("all tensors must be on one device")
+def _device_of(t: torch.Tensor, name: str) -> int:
+    if not t.is_cuda:
+        raise ValueError("%s must be a CUDA tensor" % name)
+    return t.get_device()
 
 
-def _adapters(X, W, A, B, index, scale):
+def _adapters(X, W, A, B, index, scale, dev):
     """Checked sizes (T, c, b, n, r) and dtype code of an adapted projection."""
+    dtype = X.dtype
     dt = _dtype_code(X)
-    if W.dim() != 2 or W.dtype != X.dtype:
+    if W.dim() != 2 or W.dtype != dtype:
         raise ValueError("W must be a matrix of X's dtype")
     c, b = W.shape
     T = X.shape[0]
@@ -535,13 +539,22 @@ def _adapters(X, W, A, B, index, scale):
         return T, c, b, 0, 0, dt
     if A.dim() != 3:
         raise ValueError("A must have the shape [n_adapters, r, b]")
-    n, r = A.shape[0], A.shape[1]
-    _dense(A, (n, r, b), X.dtype, "A")
-    _dense(B, (n, c, r), X.dtype, "B")
-    _dense(index, (T,), torch.int32, "index")
-    _dense(scale, (n,), torch.float32, "scale")
-    _same_device(X, W, A, B, index, scale)
+    n, r, _ = A.shape
+    _dense(A, (n, r, b), dtype, dev, "A")
+    _dense(B, (n, c, r), dtype, dev, "B")
+    _dense(index, (T,), torch.int32, dev, "index")
+    _dense(scale, (n,), torch.float32, dev, "scale")
     return T, c, b, n, r, dt
+
+
+def _scratch(workspace: Optional[torch.Tensor], nbytes: int, like: torch.Tensor) -> torch.Tensor:
+    """The caller's workspace, or a new one."""
+    if workspace is None:
+        return _ws(nbytes, like.device)
+    if workspace.get_device() != like.get_device() or workspace.dtype != torch.uint8 \
+            or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous uint8 tensor on the call's device")
+    return workspace
 
 
 def _ptr(t):
@@ -565,22 +578,23 @@ def adapter_forward(X: torch.Tensor, W: torch.Tensor, A: Optional[torch.Tensor] 
     holds X[t] A[i]^T for adapter_backward (None without adapters).  With check=True the call's
     device status word is read back (this waits for the call)."""
     lib = load_library()
-    T, c, b, n, r, dt = _adapters(X, W, A, B, index, scale)
-    ldx, ldw = _rows(X, b, "X"), _rows(W, b, "W")
+    dev = _device_of(X, "X")
+    T, c, b, n, r, dt = _adapters(X, W, A, B, index, scale, dev)
+    ldx, ldw = _rows(X, b, dev, "X"), _rows(W, b, dev, "W")
     with _on(X):
         with _alloc_scope(stream):
             if out is None:
                 out = torch.empty((T, c), dtype=X.dtype, device=X.device)
-            if V is None and n > 0:
-                V = torch.empty((T, r), dtype=torch.float32, device=X.device)
-            if workspace is None:
-                workspace = _ws(lib.thanos_adapter_workspace_bytes(0, T, c, b, n, r, dt), X.device)
-        if out.dtype != X.dtype or out.shape[0] != T:
-            raise ValueError("out must be a [T, c] tensor of X's dtype")
-        ldy = _rows(out, c, "out")
-        if n > 0:
-            _dense(V, (T, r), torch.float32, "V")
-        _same_device(X, W, out, V, workspace)
+            elif out.dtype != X.dtype or out.shape[0] != T:
+                raise ValueError("out must be a [T, c] tensor of X's dtype")
+            if n > 0:
+                if V is None:
+                    V = torch.empty((T, r), dtype=torch.float32, device=X.device)
+                else:
+                    _dense(V, (T, r), torch.float32, dev, "V")
+            workspace = _scratch(workspace,
+                                 lib.thanos_adapter_workspace_bytes(0, T, c, b, n, r, dt), X)
+        ldy = _rows(out, c, dev, "out")
         _check(lib.thanos_adapter_forward(out.data_ptr(), ldy, _ptr(V), X.data_ptr(), ldx,
                                           W.data_ptr(), ldw, _ptr(A), _ptr(B), _ptr(index),
                                           _ptr(scale), dt, T, c, b, n, r, workspace.data_ptr(),
@@ -604,8 +618,9 @@ def adapter_backward(dY: torch.Tensor, X: Optional[torch.Tensor], V: Optional[to
     accumulate=True they are added to (pass them in).  need_dx=False / need_grads=False leave a
     part out (None is returned for it; X and V may then be None without gradients)."""
     lib = load_library()
-    T, c, b, n, r, dt = _adapters(dY, W, A, B, index, scale)
-    lddy, ldw = _rows(dY, c, "dY"), _rows(W, b, "W")
+    dev = _device_of(dY, "dY")
+    T, c, b, n, r, dt = _adapters(dY, W, A, B, index, scale, dev)
+    lddy, ldw = _rows(dY, c, dev, "dY"), _rows(W, b, dev, "W")
     need_grads = need_grads and n > 0
     ldx = 0
     if need_grads:
@@ -613,41 +628,40 @@ def adapter_backward(dY: torch.Tensor, X: Optional[torch.Tensor], V: Optional[to
             raise ValueError("the adapters' gradients need X and V")
         if X.dtype != dY.dtype or X.shape[0] != T:
             raise ValueError("X must be a [T, b] tensor of dY's dtype")
-        ldx = _rows(X, b, "X")
-        _dense(V, (T, r), torch.float32, "V")
-    if accumulate and (dA is None or dB is None) and need_grads:
-        raise ValueError("accumulate=True needs dA and dB")
+        ldx = _rows(X, b, dev, "X")
+        _dense(V, (T, r), torch.float32, dev, "V")
+        if accumulate and (dA is None or dB is None):
+            raise ValueError("accumulate=True needs dA and dB")
+    else:
+        X = V = dA = dB = None
     with _on(dY):
-        with _alloc_scope(stream):
-            if need_dx and dX is None:
-                dX = torch.empty((T, b), dtype=dY.dtype, device=dY.device)
-            if need_grads and dA is None:
-                dA = torch.empty((n, r, b), dtype=torch.float32, device=dY.device)
-            if need_grads and dB is None:
-                dB = torch.empty((n, c, r), dtype=torch.float32, device=dY.device)
-            if workspace is None:
-                workspace = _ws(lib.thanos_adapter_workspace_bytes(1, T, c, b, n, r, dt), dY.device)
         lddx = 0
-        if need_dx:
-            if dX.dtype != dY.dtype or dX.shape[0] != T:
+        with _alloc_scope(stream):
+            if not need_dx:
+                dX = None
+            elif dX is None:
+                dX = torch.empty((T, b), dtype=dY.dtype, device=dY.device)
+            elif dX.dtype != dY.dtype or dX.shape[0] != T:
                 raise ValueError("dX must be a [T, b] tensor of dY's dtype")
-            lddx = _rows(dX, b, "dX")
-        else:
-            dX = None
-        if need_grads:
-            _dense(dA, (n, r, b), torch.float32, "dA")
-            _dense(dB, (n, c, r), torch.float32, "dB")
-        else:
-            dA = dB = None
-        _same_device(dY, W, X if need_grads else None, V if need_grads else None, dX, dA, dB,
-                     workspace)
+            if need_grads:
+                if dA is None:
+                    dA = torch.empty((n, r, b), dtype=torch.float32, device=dY.device)
+                else:
+                    _dense(dA, (n, r, b), torch.float32, dev, "dA")
+                if dB is None:
+                    dB = torch.empty((n, c, r), dtype=torch.float32, device=dY.device)
+                else:
+                    _dense(dB, (n, c, r), torch.float32, dev, "dB")
+            workspace = _scratch(workspace,
+                                 lib.thanos_adapter_workspace_bytes(1, T, c, b, n, r, dt), dY)
+        if need_dx:
+            lddx = _rows(dX, b, dev, "dX")
         _check(lib.thanos_adapter_backward(_ptr(dX), lddx, _ptr(dA), _ptr(dB),
-                                           1 if accumulate else 0, dY.data_ptr(), lddy,
-                                           _ptr(X) if need_grads else None, ldx,
-                                           _ptr(V) if need_grads else None, W.data_ptr(), ldw,
-                                           _ptr(A), _ptr(B), _ptr(index), _ptr(scale), dt, T, c, b,
-                                           n, r, workspace.data_ptr(), workspace.numel(),
-                                           _stream_ptr(stream)), "thanos_adapter_backward")
+                                           1 if accumulate else 0, dY.data_ptr(), lddy, _ptr(X), ldx,
+                                           _ptr(V), W.data_ptr(), ldw, _ptr(A), _ptr(B), _ptr(index),
+                                           _ptr(scale), dt, T, c, b, n, r, workspace.data_ptr(),
+                                           workspace.numel(), _stream_ptr(stream)),
+               "thanos_adapter_backward")
         if check:
             _status(workspace, "thanos_adapter_backward")
     return dX, dA, dB
@@ -657,8 +671,8 @@ NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)  # quintic with a steep slope at zero,
 
 
 def _matrices(G: torch.Tensor):
-    if G.dim() not in (2, 3):
-        raise ValueError("expected a matrix or a batch of matrices")
+    if G.dim() not in (2, 3) or not G.is_contiguous():
+        raise ValueError("expected a contiguous matrix or batch of matrices")
     return (1 if G.dim() == 2 else G.shape[0]), G.shape[-2], G.shape[-1]
 
 
@@ -668,17 +682,16 @@ def orthogonalise(G: torch.Tensor, steps: int = 5, coef=NEWTON_SCHULZ, eps: floa
     """thanos_orthogonalise: Newton-Schulz iteration on G [m, n] or [batch, m, n] (float32 or
     bfloat16, contiguous); returns bfloat16 of the same shape."""
     lib = load_library()
+    dev = _device_of(G, "G")
     k, m, n = _matrices(G)
     dt = _dtype_code(G)
-    _dense(G, G.shape, G.dtype, "G")
     with _on(G):
         with _alloc_scope(stream):
             if out is None:
                 out = torch.empty(G.shape, dtype=torch.bfloat16, device=G.device)
-            if workspace is None:
-                workspace = _ws(lib.thanos_orthogonal_workspace_bytes(k, m, n), G.device)
-        _dense(out, G.shape, torch.bfloat16, "out")
-        _same_device(G, out, workspace)
+            else:
+                _dense(out, G.shape, torch.bfloat16, dev, "out")
+            workspace = _scratch(workspace, lib.thanos_orthogonal_workspace_bytes(k, m, n), G)
         abc = (ctypes.c_float * 3)(*coef)
         _check(lib.thanos_orthogonalise(out.data_ptr(), G.data_ptr(), dt, k, m, n, abc, steps,
                                         float(eps), workspace.data_ptr(), workspace.numel(),
@@ -699,24 +712,24 @@ def orthogonal_step(W: torch.Tensor, M: torch.Tensor, G: torch.Tensor,
     or bfloat16, M float32, all [m, n] or [batch, m, n] and contiguous.  Returns (W_out, M_out);
     pass W_out=W, M_out=M to update in place."""
     lib = load_library()
+    dev = _device_of(G, "G")
     k, m, n = _matrices(G)
     wdt, gdt = _dtype_code(W), _dtype_code(G)
-    _dense(G, G.shape, G.dtype, "G")
-    _dense(W, G.shape, W.dtype, "W")
-    _dense(M, G.shape, torch.float32, "M")
+    _dense(W, G.shape, W.dtype, dev, "W")
+    _dense(M, G.shape, torch.float32, dev, "M")
     if mask is not None:
-        _dense(mask, G.shape, torch.uint8, "mask")
+        _dense(mask, G.shape, torch.uint8, dev, "mask")
     with _on(G):
         with _alloc_scope(stream):
             if W_out is None:
                 W_out = torch.empty_like(W)
+            else:
+                _dense(W_out, G.shape, W.dtype, dev, "W_out")
             if M_out is None:
                 M_out = torch.empty_like(M)
-            if workspace is None:
-                workspace = _ws(lib.thanos_orthogonal_workspace_bytes(k, m, n), G.device)
-        _dense(W_out, G.shape, W.dtype, "W_out")
-        _dense(M_out, G.shape, torch.float32, "M_out")
-        _same_device(G, W, M, mask, W_out, M_out, workspace)
+            else:
+                _dense(M_out, G.shape, torch.float32, dev, "M_out")
+            workspace = _scratch(workspace, lib.thanos_orthogonal_workspace_bytes(k, m, n), G)
         abc = (ctypes.c_float * 3)(*coef)
         _check(lib.thanos_orthogonal_step(W_out.data_ptr(), W.data_ptr(), wdt, M_out.data_ptr(),
                                           M.data_ptr(), G.data_ptr(), gdt, _ptr(mask), k, m, n,

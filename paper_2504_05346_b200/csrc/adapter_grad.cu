@@ -300,25 +300,26 @@ __global__ void __launch_bounds__(G_THREADS) grad_tc_kernel(const GradParams p) 
         uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16);
         idesc |= (uint32_t)(N >> 3) << 17;
         idesc |= (uint32_t)(GF >> 4) << 24;
-        for (int ks = ks0; ks < ks1 && ok; ++ks) {
-          ok = mbar_wait(full_bar(s), phase, abort_flag);
-          tc_fence_after();
-          if (ok && lane == 0) {
-            const uint32_t sa = smem_base + (uint32_t)s * stage_bytes, sb = sa + GA_BYTES;
+        if (elect_one()) {  // the same lane every time: it alone follows the ring
+          for (int ks = ks0; ks < ks1 && ok; ++ks) {
+            ok = mbar_wait(full_bar(s), phase, abort_flag);
+            tc_fence_after();
+            if (ok) {
+              const uint32_t sa = smem_base + (uint32_t)s * stage_bytes, sb = sa + GA_BYTES;
 #pragma unroll
-            for (int k4 = 0; k4 < GK / 16; ++k4)
-              tc_mma_bf16(tmem_base, grad_desc(sa + k4 * 2048, GA_BYTES / 2, 1024, 2),
-                          grad_desc(sb + k4 * 1024, 4096, 512, 4), idesc,
-                          (ks > ks0 || k4 > 0) ? 1u : 0u);
-            tc_commit(empty_bar(s));
+              for (int k4 = 0; k4 < GK / 16; ++k4)
+                tc_mma_bf16(tmem_base, grad_desc(sa + k4 * 2048, GA_BYTES / 2, 1024, 2),
+                            grad_desc(sb + k4 * 1024, 4096, 512, 4), idesc,
+                            (ks > ks0 || k4 > 0) ? 1u : 0u);
+              tc_commit(empty_bar(s));
+            }
+            if (++s == p.stages) {
+              s = 0;
+              phase ^= 1u;
+            }
           }
-          __syncwarp();
-          if (++s == p.stages) {
-            s = 0;
-            phase ^= 1u;
-          }
+          if (ok) tc_commit(done_bar);
         }
-        if (ok && lane == 0) tc_commit(done_bar);
         __syncwarp();
       }
       // ---------------------------------------------------------- epilogue, one slice of tokens

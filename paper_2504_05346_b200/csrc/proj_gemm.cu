@@ -29,7 +29,7 @@ constexpr int TILE_THREADS = 320;
 constexpr int FACTOR_BYTES = 128 * 16 * 4;    // 16 ranks of up to 128 tokens, fp32
 
 struct Params {
-  int M, N, K, tiles_m, tiles_n, nt, stages, splits, batch_z, ring_bytes;
+  int M, N, K, tiles_m, tiles_n, nt, stages, splits, batch_z, ring_bytes, tmem_cols;
   int symmetric, f16, early;
   int32_t* status;
   // adapter part
@@ -73,15 +73,51 @@ __device__ __forceinline__ uint64_t make_desc(uint32_t addr, uint32_t lbo, uint3
 }
 constexpr uint32_t SW128 = 2, SW32 = 6;
 
+// The four products of a 64-wide k step whose operands start at the descriptors ad, bd.  Only the
+// start address (16-byte units, in the low bits) moves between them.
+template <bool AMN, bool PAIR>
+__device__ __forceinline__ void mma_step(uint32_t d, uint64_t ad, uint64_t bd, uint32_t idesc,
+                                         uint32_t first) {
+#pragma unroll
+  for (int k4 = 0; k4 < BK / 16; ++k4) {
+    const uint64_t a = ad + (uint64_t)(k4 * (AMN ? 2048 : 32) >> 4);
+    const uint64_t b = bd + (uint64_t)(k4 * 32 >> 4);
+    if (PAIR) tc_mma_bf16_pair(d, a, b, idesc, k4 == 0 ? first : 1u);
+    else tc_mma_bf16(d, a, b, idesc, k4 == 0 ? first : 1u);
+  }
+}
+
 __device__ __forceinline__ float ld_cluster(uint32_t addr) {
   float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr));
   return v;
 }
 __device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t addr) {
   uint32_t v;
   asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
   return v;
+}
+
+__device__ __forceinline__ void tc_ld8(uint32_t taddr, float (&v)[8]) {
+  uint32_t u[8];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]),
+        "=r"(u[7])
+      : "r"(taddr)
+      : "memory");
+  tc_wait_ld();
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(u[e]);
+}
+__device__ __forceinline__ void tc_st8(uint32_t taddr, const float (&v)[8]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr),
+      "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])),
+      "r"(__float_as_uint(v[3])), "r"(__float_as_uint(v[4])), "r"(__float_as_uint(v[5])),
+      "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7]))
+      : "memory");
+  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
 
 __device__ __forceinline__ bool bf16_nonfinite(uint32_t h) { return (h & 0x7F80u) == 0x7F80u; }
@@ -310,14 +346,27 @@ __device__ __forceinline__ void emit(const Params& p, int z, int m, int n0, floa
   }
 }
 
-// First column of the q-th group of eight that a thread of tile_kernel writes: without a split 32
-// columns of every 64 (as they come out of tensor memory), else every 2 S-th group.
+// First column of the q-th group of eight that a thread of tile_kernel writes: every second group,
+// or every 2 S-th with a split.
 __device__ __forceinline__ int tile_column(int S, int rank, int half, int q) {
-  return S == 1 ? 32 * half + 64 * (q >> 2) + 8 * (q & 3) : 8 * (rank + S * (half + 2 * q));
+  return 8 * (rank + S * (half + 2 * q));
 }
 
+__device__ __forceinline__ void prefetch_l2(const void* p) {
+  asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
+}
 __device__ __forceinline__ void epilogue_sync() {  // the eight epilogue warps of tile_kernel
   asm volatile("bar.sync 1, 256;" ::: "memory");
+}
+__device__ __forceinline__ bool epilogue_any(bool mine) {  // whether any of the 256 says yes
+  int r;
+  asm volatile(
+      "{\n.reg .pred a, b;\nsetp.ne.u32 a, %1, 0;\n"
+      "barrier.cta.red.or.aligned.pred b, 1, 256, a;\nselp.u32 %0, 1, 0, b;\n}"
+      : "=r"(r)
+      : "r"((int)mine)
+      : "memory");
+  return r != 0;
 }
 __device__ __forceinline__ float2 unpack2(uint32_t w) {
   return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
@@ -399,8 +448,10 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
   const int z = blockIdx.y;
   const int stage_bytes = A_BYTES + p.nt * BK * 2;
 
-  // symmetric results: the lower tiles are the mirror of the upper ones (nt == TM)
-  if (p.symmetric && tn < tm) return;
+  // symmetric results: tiles left of the diagonal blocks are the mirror of those right of them
+  // (nt divides TM)
+  if (p.symmetric && n0 < m0) return;
+  const bool mirror = n0 >= m0 + TM;
   if constexpr (EPI == PROJ_SHRINK) {
     // rows of adapters that no token of the tile uses are not needed (tile row 0 also writes the
     // zeros of tokens without adapter)
@@ -429,7 +480,7 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
                      smem_u32(tmem_slot)),
-                 "r"(p.nt)
+                 "r"(p.tmem_cols)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -445,17 +496,15 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
 
   const int nk = (p.K + BK - 1) / BK;
   const int ks0 = (int)((int64_t)nk * rank / S), ks1 = (int)((int64_t)nk * (rank + 1) / S);
-  constexpr int Q = EPI == PROJ_OUT ? 8 : 1;  // groups of eight columns a thread may own (nt <= 128)
-  float own[Q][8];
-
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
+    if (elect_one()) {
     int s = 0;
     uint32_t phase = 0;
     bool ok = true;
     for (int ks = ks0; ks < ks1 && ok; ++ks) {
       ok = mbar_wait(empty_bar(s), phase ^ 1u, abort_flag);
-      if (ok && lane == 0) {
+      if (ok) {
         const uint32_t dst = smem_base + (uint32_t)s * stage_bytes;
         mbar_expect_tx(full_bar(s), stage_bytes);
         if (AMN) {
@@ -466,7 +515,6 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
         }
         tma_load_3d(dst + A_BYTES, &mapB, full_bar(s), ks * BK, n0, z);
       }
-      __syncwarp();
       if (++s == p.stages) {
         s = 0;
         phase ^= 1u;
@@ -476,52 +524,73 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
     if (!ok) {
       for (int i = 0; i < 2000; ++i) __nanosleep(1000);
     }
+    }
+    __syncwarp();
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMA issuer
+    if (elect_one()) {
     uint32_t idesc = 0;
     idesc |= 1u << 4;  // D fp32
     if (!p.f16) idesc |= (1u << 7) | (1u << 10);  // both operands bf16 (0: both fp16)
     if (AMN) idesc |= 1u << 15;
     idesc |= (uint32_t)(p.nt >> 3) << 17;
     idesc |= (uint32_t)(TM >> 4) << 24;
+    const uint64_t ad0 = AMN ? make_desc(smem_base, A_BYTES / 2, 1024, SW128)
+                             : make_desc(smem_base, 16, 1024, SW128);
+    const uint64_t bd0 = make_desc(smem_base + A_BYTES, 16, 1024, SW128);
+    const uint64_t hop = (uint64_t)(stage_bytes >> 4);
     int s = 0;
     uint32_t phase = 0;
+    uint64_t at = 0;  // stage s in descriptor units
     bool ok = true;
     for (int ks = ks0; ks < ks1 && ok; ++ks) {
       ok = mbar_wait(full_bar(s), phase, abort_flag);
       tc_fence_after();
-      if (ok && lane == 0) {
-        const uint32_t sa = smem_base + (uint32_t)s * stage_bytes;
-        const uint32_t sb = sa + A_BYTES;
-#pragma unroll
-        for (int k4 = 0; k4 < BK / 16; ++k4) {
-          const uint64_t ad = AMN ? make_desc(sa + k4 * 2048, A_BYTES / 2, 1024, SW128)
-                                  : make_desc(sa + k4 * 32, 16, 1024, SW128);
-          tc_mma_bf16(tmem_base, ad, make_desc(sb + k4 * 32, 16, 1024, SW128), idesc,
-                      (ks > ks0 || k4 > 0) ? 1u : 0u);
-        }
+      if (ok) {
+        mma_step<AMN, false>(tmem_base, ad0 + at, bd0 + at, idesc, ks > ks0 ? 1u : 0u);
         tc_commit(empty_bar(s));
       }
-      __syncwarp();
+      at += hop;
       if (++s == p.stages) {
         s = 0;
+        at = 0;
         phase ^= 1u;
       }
     }
-    if (ok && lane == 0) tc_commit(done_bar);
+    if (ok) tc_commit(done_bar);
+    }
     __syncwarp();
   } else {
     const int g = warp & 3, half = (warp - 2) >> 2;
-    const int row = 32 * g + lane;
+    const int row = 32 * g + lane, m = m0 + row;
+    const uint32_t taddr = tmem_base + ((uint32_t)(32 * g) << 16);
+    // All loops below are kept rolled: the code runs once per CTA, and straight-line code of a few
+    // thousand instructions costs more in instruction fetches than it saves.
+    bool used = false;
     if constexpr (EPI == PROJ_OUT) {
       // ---------------------------------------------------------- adapter part
-#pragma unroll
-      for (int q = 0; q < Q; ++q)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) own[q][e] = 0.f;
+      if (p.n_adapters > 0 && p.early) {
+        // the rows of the wide factors that this thread will read are on their way to L2 while the
+        // previous launch still computes V
+#pragma unroll 1
+        for (int q = 0; m < p.M; ++q) {
+          const int c = tile_column(S, rank, half, q);
+          if (c >= p.nt || n0 + c >= p.N) break;
+          for (int e = 0; e < 8 && n0 + c + e < p.N; ++e) {
+            const int i = valid_adapter(p, n0 + c + e);
+            if (i < 0 || (e > 0 && p.index[n0 + c + e - 1] == i)) continue;
+            const __nv_bfloat16* a = p.P + (int64_t)i * p.p_adapter;
+            if (AMN) {
+              for (int j = 0; j < p.r; ++j) prefetch_l2(a + (int64_t)j * p.ldp + m);
+            } else {
+              for (int j = 0; j < p.r; j += 16) prefetch_l2(a + (int64_t)m * p.ldp + j);
+            }
+          }
+        }
+      }
       if (p.early) grid_dependency_wait();
       if (p.n_adapters > 0) {
-        const int tid = threadIdx.x - 64, m = m0 + row;
+        const int tid = threadIdx.x - 64;
         bool any = false;
         if (tid < p.nt) {
           const int t = n0 + tid;
@@ -531,15 +600,11 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
           if (tm == 0 && rank == 0 && t < p.N && i < 0 && p.index[t] != -1)
             atomicCAS(p.status, 0, (int)THANOS_ERR_INVALID_ARG);
         }
-        int used;
-        asm volatile(
-            "{\n.reg .pred a, b;\nsetp.ne.u32 a, %1, 0;\n"
-            "barrier.cta.red.or.aligned.pred b, 1, 256, a;\nselp.u32 %0, 1, 0, b;\n}"
-            : "=r"(used)
-            : "r"((int)any)
-            : "memory");
+        used = epilogue_any(any);
+#pragma unroll 1
         for (int j0 = 0; j0 < p.r && used; j0 += 16) {
           if (j0 > 0) epilogue_sync();
+#pragma unroll 1
           for (int e = tid; e < p.nt * 16; e += 256) {
             const int t = n0 + (e >> 4), j = j0 + (e & 15), i = ids[e >> 4];
             float v = 0.f;
@@ -550,35 +615,41 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
             factor[e] = v;
           }
           epilogue_sync();
-          if (m < p.M) {
+#pragma unroll 1
+          for (int q = 0;; ++q) {
+            const int c = tile_column(S, rank, half, q);
+            if (c >= p.nt || n0 + c >= p.N) break;
+            float own[8] = {};
+            const int first = ids[c];
+            bool same = true;
 #pragma unroll
-            for (int q = 0; q < Q; ++q) {
-              const int c = tile_column(S, rank, half, q);
-              if (c >= p.nt || n0 + c >= p.N) continue;
-              const int first = ids[c];
-              bool same = true;
-#pragma unroll
-              for (int e = 1; e < 8; ++e) same = same && ids[c + e] == first;
+            for (int e = 1; e < 8; ++e) same = same && ids[c + e] == first;
+            if (m < p.M) {
               if (same) {  // a run of one request's tokens (or none): its row is read once
                 if (first >= 0) {
                   uint32_t w[8];
                   wide_row<AMN>(p, first, m, j0, w);
 #pragma unroll
-                  for (int e = 0; e < 8; ++e) own[q][e] = dot16(w, factor + (c + e) * 16, own[q][e]);
+                  for (int e = 0; e < 8; ++e) own[e] = dot16(w, factor + (c + e) * 16, 0.f);
                 }
               } else {
+                uint32_t w[8][8];  // eight rows in flight
 #pragma unroll
-                for (int e4 = 0; e4 < 8; e4 += 4) {  // four rows in flight
-                  uint32_t w[4][8];
+                for (int e = 0; e < 8; ++e) wide_row<AMN>(p, ids[c + e], m, j0, w[e]);
 #pragma unroll
-                  for (int e = 0; e < 4; ++e) wide_row<AMN>(p, ids[c + e4 + e], m, j0, w[e]);
-#pragma unroll
-                  for (int e = 0; e < 4; ++e)
-                    if (ids[c + e4 + e] >= 0)
-                      own[q][e4 + e] = dot16(w[e], factor + (c + e4 + e) * 16, own[q][e4 + e]);
-                }
+                for (int e = 0; e < 8; ++e)
+                  if (ids[c + e] >= 0) own[e] = dot16(w[e], factor + (c + e) * 16, 0.f);
               }
             }
+            __syncwarp();
+            // kept in tensor memory beside the accumulator, at the columns it belongs to
+            if (j0 > 0) {
+              float before[8];
+              tc_ld8(taddr + p.nt + c, before);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) own[e] += before[e];
+            }
+            tc_st8(taddr + p.nt + c, own);
           }
         }
       }
@@ -586,67 +657,75 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
     // ------------------------------------------------------------ epilogue, one slice of k
     const bool ok = mbar_wait(done_bar, 0, abort_flag);
     tc_fence_after();
-    const uint32_t taddr = tmem_base + ((uint32_t)(32 * g) << 16);
-    if (ok) {
+    if (ok && S == 1) {
+#pragma unroll 1
+      for (int q = 0;; ++q) {
+        const int c = tile_column(1, 0, half, q);
+        if (c >= p.nt || n0 + c >= p.N) break;
+        float v[8];
+        tc_ld8(taddr + c, v);
+        if (used) {
+          float own[8];
+          tc_ld8(taddr + p.nt + c, own);
 #pragma unroll
-      for (int c2 = 0; c2 < 4; ++c2) {
-        const int cc = 32 * half + 64 * c2;
-        if (cc >= p.nt) break;
-        uint32_t u[32];
-        tc_ld32(taddr + cc, u);
-        tc_wait_ld();
-        float v[32];
-#pragma unroll
-        for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(u[e]);
-        if (S == 1) {
-          if constexpr (EPI == PROJ_OUT) {
-            if (c2 < Q / 4) {
-#pragma unroll
-              for (int e = 0; e < 32; ++e) v[e] += own[(c2 & 1) * 4 + e / 8][e & 7];
-            }
-          }
-          emit<AMN, EPI, 32>(p, z, m0 + row, n0 + cc, v, tn != tm, false);
-        } else {
-          // partial sums [n][m] in the ring, whose operands have all been consumed
-          float* part = reinterpret_cast<float*>(smem);
-#pragma unroll
-          for (int e = 0; e < 32; ++e) part[(cc + e) * TM + row] = v[e];
+          for (int e = 0; e < 8; ++e) v[e] += own[e];
         }
+        emit<AMN, EPI, 8>(p, z, m, n0 + c, v, mirror, false);
+        __syncwarp();
+      }
+    } else if (ok) {
+      // partial sums [n][m] in the ring, whose operands have all been consumed
+      float* part = reinterpret_cast<float*>(smem);
+#pragma unroll 1
+      for (int c = 8 * half; c < p.nt; c += 16) {
+        float v[8];
+        tc_ld8(taddr + c, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) part[(c + e) * TM + row] = v[e];
       }
     }
-  }
-  tc_fence_before();
-  __syncthreads();
-  if (warp == 1) {
-    tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(p.nt)
-                 : "memory");
-  }
-  if (threadIdx.x == 0 && *abort_flag) atomicCAS(p.status, 0, (int)THANOS_ERR_TIMEOUT);
-  if (S > 1) {
-    cluster_sync_all();
-    if (warp >= 2) {
+    if (S > 1) {
+      cluster_sync_all();
       bool bad = false;
       for (int q = 0; q < S; ++q)
         bad = bad || ld_cluster_u32(map_to_cta(smem_u32((const void*)abort_flag), q)) != 0;
-      const int half = (warp - 2) >> 2, row = 32 * (warp & 3) + lane;
+#pragma unroll 1
+      for (int q = 0; !bad; ++q) {
+        const int c = tile_column(S, rank, half, q);
+        if (c >= p.nt || n0 + c >= p.N) break;
+        float f[8] = {};
+        if (used) tc_ld8(taddr + p.nt + c, f);
+#pragma unroll 1
+        for (int k = 0; k < S; k += 2) {
+          const uint32_t a0 = map_to_cta(smem_base, k) + (uint32_t)(c * TM + row) * 4u;
+          const uint32_t a1 = map_to_cta(smem_base, k + 1) + (uint32_t)(c * TM + row) * 4u;
+          float x[8], y[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int c = tile_column(S, rank, half, k);
-        if (c >= p.nt || bad) continue;
-        float f[8];
+          for (int e = 0; e < 8; ++e) x[e] = ld_cluster(a0 + e * TM * 4);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = EPI == PROJ_OUT ? own[k % Q][e] : 0.f;
-        for (int q = 0; q < S; ++q) {
-          const uint32_t src = map_to_cta(smem_base, q) + (uint32_t)(c * TM + row) * 4u;
+          for (int e = 0; e < 8; ++e) y[e] = ld_cluster(a1 + e * TM * 4);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] += ld_cluster(src + e * TM * 4);
+          for (int e = 0; e < 8; ++e) f[e] = (f[e] + x[e]) + y[e];
         }
-        emit<AMN, EPI, 8>(p, z, m0 + row, n0 + c, f, tn != tm, false);
+        emit<AMN, EPI, 8>(p, z, m, n0 + c, f, mirror, false);
+        __syncwarp();
       }
     }
-    cluster_sync_all();  // no CTA leaves while another may still read its partial sums
   }
+  if (S > 1 && warp < 2) {
+    __syncwarp();
+    cluster_sync_all();  // the partial sums are there
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (S > 1) cluster_sync_all();  // no CTA leaves while another may still read its partial sums
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base),
+                 "r"(p.tmem_cols)
+                 : "memory");
+  }
+  if (threadIdx.x == 0 && *abort_flag) atomicCAS(p.status, 0, (int)THANOS_ERR_TIMEOUT);
 }
 
 // ------------------------------------------------------------------------------- CTA pairs
@@ -784,6 +863,7 @@ pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
 
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
+    if (elect_one()) {
     int s = 0;
     uint32_t phase = 0;
     bool ok = true;
@@ -792,7 +872,7 @@ pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
       const int m0 = tl.tm * PTM + 128 * (int)rank, n0 = tl.tn * p.nt + half * (int)rank;
       for (int ks = 0; ks < nk && ok; ++ks) {
         ok = mbar_wait(empty_bar(s), phase ^ 1u, abort_flag);
-        if (ok && lane == 0) {
+        if (ok) {
           const uint32_t dst = smem_base + (uint32_t)s * PSTAGE_BYTES;
           const uint32_t lead = map_to_cta(full_bar(s), 0);
           if (rank == 0) mbar_expect_tx(full_bar(s), 2 * (A_BYTES + half * BK * 2));
@@ -804,7 +884,6 @@ pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
           }
           tma_load_3d_pair(dst + A_BYTES, &mapB, lead, ks * BK, n0, tl.z);
         }
-        __syncwarp();
         if (++s == STAGES) {
           s = 0;
           phase ^= 1u;
@@ -815,15 +894,20 @@ pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
     if (!ok) {
       for (int i = 0; i < 2000; ++i) __nanosleep(1000);
     }
+    }
+    __syncwarp();
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMA issuer (first CTA only)
-    if (rank == 0) {
+    if (rank == 0 && elect_one()) {
       uint32_t idesc = 0;
       idesc |= 1u << 4;  // D fp32
       if (!p.f16) idesc |= (1u << 7) | (1u << 10);
       if (AMN) idesc |= 1u << 15;
       idesc |= (uint32_t)(p.nt >> 3) << 17;
       idesc |= (uint32_t)(PTM >> 4) << 24;
+      const uint64_t ad0 = AMN ? make_desc(smem_base, A_BYTES / 2, 1024, SW128)
+                               : make_desc(smem_base, 16, 1024, SW128);
+      const uint64_t bd0 = make_desc(smem_base + A_BYTES, 16, 1024, SW128);
       int s = 0, q = 0, e = 0;
       uint32_t phase = 0, tphase = 0, ephase = 0;
       bool ok = true, waited = false;
@@ -835,19 +919,11 @@ pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
         for (int ks = 0; ks < nk && ok; ++ks) {
           ok = mbar_wait(full_bar(s), phase, abort_flag);
           tc_fence_after();
-          if (ok && lane == 0) {
-            const uint32_t sa = smem_base + (uint32_t)s * PSTAGE_BYTES;
-            const uint32_t sb = sa + A_BYTES;
-#pragma unroll
-            for (int k4 = 0; k4 < BK / 16; ++k4) {
-              const uint64_t ad = AMN ? make_desc(sa + k4 * 2048, A_BYTES / 2, 1024, SW128)
-                                      : make_desc(sa + k4 * 32, 16, 1024, SW128);
-              tc_mma_bf16_pair(d, ad, make_desc(sb + k4 * 32, 16, 1024, SW128), idesc,
-                               (ks > 0 || k4 > 0) ? 1u : 0u);
-            }
+          if (ok) {
+            const uint64_t at = (uint64_t)s * (PSTAGE_BYTES >> 4);
+            mma_step<AMN, true>(d, ad0 + at, bd0 + at, idesc, ks > 0 ? 1u : 0u);
             tc_commit_pair(empty_bar(s));
           }
-          __syncwarp();
           if (++s == STAGES) {
             s = 0;
             phase ^= 1u;
@@ -860,7 +936,7 @@ pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
           for (int c0 = 0; c0 < total && ok; c0 += CHUNKS) {
             ok = mbar_wait(ready_bar(e), ephase, abort_flag);
             tc_fence_after();
-            if (ok && lane == 0) {
+            if (ok) {
               const uint32_t sa = ering_base + (uint32_t)e * PSTAGE_BYTES;
               const uint32_t sb = sa + A_BYTES;
               const int nc = min(CHUNKS, total - c0);
@@ -872,21 +948,20 @@ pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
               }
               tc_commit_pair(eempty_bar(e));
             }
-            __syncwarp();
             if (++e == ESTAGES) {
               e = 0;
               ephase ^= 1u;
             }
           }
         }
-        if (ok && lane == 0) tc_commit_pair(tfull_bar(q));
-        __syncwarp();
+        if (ok) tc_commit_pair(tfull_bar(q));
         if (++q == 2) {
           q = 0;
           tphase ^= 1u;
         }
       }
     }
+    __syncwarp();
   } else if (warp < EPI_WARP) {
     // ------------------------------------------------------------ adapter stages
     if (ext) {
@@ -1117,6 +1192,22 @@ bool use_pairs(int64_t M, int64_t N, int64_t batch, bool symmetric) {
 
 }  // namespace
 
+namespace {
+// Width of tile_kernel's tiles: the widest of 128, 64, 32 whose tiles occupy most of the device,
+// no wider than the next step above N.
+int tile_width(int64_t M, int64_t N, int64_t batch, bool symmetric, bool two_per_sm) {
+  int nt = 128;
+  const int64_t want = (two_per_sm ? 2 : 1) * (int64_t)sm_count() * 3 / 4;
+  while (nt > 32) {
+    int64_t tiles = ceil_div(M, TM) * ceil_div(N, nt) * batch;
+    if (symmetric) tiles /= 2;
+    if (N > nt / 2 && (tiles >= want || N <= 64)) break;
+    nt /= 2;
+  }
+  return nt;
+}
+}  // namespace
+
 int proj_pair_tile(int64_t N, int64_t M) { return use_pairs(M, N, 1, false) ? PTM : 0; }
 
 thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
@@ -1129,7 +1220,7 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
   p.N = a.N;
   p.K = a.K;
   const bool pairs = a.epi != PROJ_SHRINK && use_pairs(a.M, a.N, a.batch, symmetric);
-  p.nt = pairs ? PTM : symmetric || a.N > 64 ? TM : a.N > 32 ? 64 : 32;
+  p.nt = pairs ? PTM : tile_width(a.M, a.N, a.batch, symmetric, a.epi <= PROJ_SHRINK);
   p.tiles_m = (a.M + (pairs ? PTM : TM) - 1) / (pairs ? PTM : TM);
   p.tiles_n = (a.N + p.nt - 1) / p.nt;
   p.batch_z = a.batch;
@@ -1138,17 +1229,19 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
   p.early = a.early;
   p.status = a.status;
   int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * a.batch;
-  if (symmetric) tiles = (int64_t)p.tiles_m * (p.tiles_m + 1) / 2 * a.batch;
+  if (symmetric) tiles = (tiles + (int64_t)p.tiles_m * a.batch * (TM / p.nt)) / 2;
   const int nk = (a.K + BK - 1) / BK;
   p.splits = 1;
-  // the projections run two CTAs per SM
-  const int slots = a.epi <= PROJ_SHRINK ? 2 * sm_count() : sm_count();
+  // A split fills SMs that have no tile; beyond a quarter more CTAs than SMs it costs more in
+  // partial sums than it brings (4096 x 4096, 1 token: 4 slices 12.4 us, 8 slices 14.4 us).
+  const int64_t slots = a.epi <= PROJ_SHRINK ? sm_count() * 5 / 4 : sm_count();
   while (p.splits < 8 && tiles * p.splits * 2 <= slots && nk >= 8 * p.splits) p.splits *= 2;
   if (tiles > (1 << 27) || a.batch > 65535) return THANOS_ERR_SHAPE;
   const int stage_bytes = A_BYTES + p.nt * BK * 2;
   p.stages = (a.epi <= PROJ_SHRINK ? 100 : 200) * 1024 / stage_bytes;
   if (p.stages > MAX_STAGES) p.stages = MAX_STAGES;
   p.ring_bytes = p.stages * stage_bytes;
+  p.tmem_cols = a.epi == PROJ_OUT ? 2 * p.nt : p.nt;  // the adapter part sits beside the sums
   p.out = a.out;
   p.ldo = a.ldo;
   p.V = a.V;
