@@ -1,0 +1,331 @@
+// The adapted projection on fp32 operands.
+//
+// The wide product runs on the tensor cores with fp32 accuracy: three bf16 planes per operand, six
+// products of planes (proj_gemm.cu, whose epilogue adds the adapter's part in fp32 as well).  The
+// planes are made here, in the same launch that computes the skinny product V (or U) in fp32.  The
+// adapters' gradients are plain fp32 sums, bound by reading their operands.
+//
+//   front_f32_kernel    planes of the activations and of W; V or U, a warp per token and eight ranks
+//   proj_gemm           out = in W^T (or in W) + the adapter's part
+//   grad_f32_kernel     both gradients: 32 features and up to 8 ranks of one adapter per CTA, eight
+//                       warps share the adapter's tokens, in the order of sort_tokens
+#include "adapter_grad.cuh"
+#include "proj_gemm.cuh"
+#include "recovery.cuh"
+
+namespace thanos {
+namespace {
+
+__device__ __forceinline__ int adapter_of(const int32_t* __restrict__ index, int64_t t, int n) {
+  const int i = n > 0 ? index[t] : -1;
+  return i >= 0 && i < n ? i : -1;
+}
+
+struct SplitJob {
+  const float* src = nullptr;
+  int64_t ld = 0;
+  int64_t rows = 0;
+  int cols = 0;
+  __nv_bfloat16* planes = nullptr;  // [3][rows, ldp]
+  int64_t ldp = 0;
+  int blocks = 0;
+};
+
+struct Front32Params {
+  SplitJob in, w;
+  int32_t* status;       // cleared here unless the sort did (then null)
+  float* R;              // [T, r]
+  const float* P;        // forward: A [n, r, K]; backward: B [n, K, r]
+  const int32_t* index;
+  const float* scale;    // backward: s_i
+  int64_t T;
+  int K, n, r, back;
+};
+
+// A warp per row in turn, so that no index has to be divided.
+__device__ void split_job(const SplitJob& s, int blk) {
+  const int64_t plane = s.rows * s.ldp;
+  const int lane = threadIdx.x & 31;
+  const bool wide = s.cols % 4 == 0 && s.ld % 4 == 0;
+  for (int64_t row = (int64_t)blk * 8 + (threadIdx.x >> 5); row < s.rows; row += 8ll * s.blocks) {
+    const float* src = s.src + row * s.ld;
+    __nv_bfloat16* dst = s.planes + row * s.ldp;
+    if (wide) {
+#pragma unroll 4
+      for (int c = 4 * lane; c < s.cols; c += 128) {
+        const float4 x = *reinterpret_cast<const float4*>(src + c);
+        float o[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int pl = 0; pl < 3; ++pl) {
+          uint32_t h[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const __nv_bfloat16 b = __float2bfloat16_rn(o[k]);
+            h[k] = __bfloat16_as_ushort(b);
+            o[k] -= __bfloat162float(b);
+          }
+          *reinterpret_cast<uint2*>(dst + pl * plane + c) =
+              make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
+        }
+      }
+    } else {
+      for (int c = lane; c < s.cols; c += 32) store_split3(dst + c, plane, src[c]);
+    }
+  }
+}
+
+constexpr int RANKS = 8;
+
+__global__ void __launch_bounds__(256) front_f32_kernel(const Front32Params p) {
+  if (blockIdx.x == 0 && threadIdx.x == 0 && p.status) *p.status = 0;
+  int blk = blockIdx.x;
+  if (blk < p.in.blocks) {
+    split_job(p.in, blk);
+    return;
+  }
+  blk -= p.in.blocks;
+  if (blk < p.w.blocks) {
+    split_job(p.w, blk);
+    return;
+  }
+  blk -= p.w.blocks;
+  const int lane = threadIdx.x & 31;
+  const int groups = (p.r + RANKS - 1) / RANKS;
+  const int64_t w = (int64_t)blk * 8 + (threadIdx.x >> 5);
+  if (w >= p.T * groups) return;
+  const int64_t t = w / groups;
+  const int j0 = (int)(w - t * groups) * RANKS, nj = min(RANKS, p.r - j0);
+  const int i = adapter_of(p.index, t, p.n);
+  float s[RANKS] = {};
+  if (i >= 0) {
+    const float* x = p.in.src + t * p.in.ld;
+    const float* a = p.P + (int64_t)i * p.r * p.K + (p.back ? (int64_t)j0 : (int64_t)j0 * p.K);
+    const int64_t dj = p.back ? 1 : p.K, dk = p.back ? p.r : 1;
+#pragma unroll 4
+    for (int k = lane; k < p.K; k += 32) {
+      const float xv = x[k];
+#pragma unroll
+      for (int j = 0; j < RANKS; ++j)
+        if (j < nj) s[j] = fmaf(xv, a[j * dj + k * dk], s[j]);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < RANKS; ++j) {
+    for (int o = 16; o > 0; o >>= 1) s[j] += __shfl_xor_sync(0xffffffffu, s[j], o);
+    if (lane == 0 && j < nj) p.R[t * p.r + j0 + j] = p.back && i >= 0 ? p.scale[i] * s[j] : s[j];
+  }
+}
+
+constexpr int GRAD_TOKENS = 512;
+
+struct Grad32Side {
+  const float* Z;
+  int64_t ldz;
+  const float* R;
+  const float* scale;
+  float* out;
+  int F, by_feature;
+};
+struct Grad32Params {
+  Grad32Side side[2];
+  int tiles0;
+  const int32_t* order;
+  const int32_t* off;
+  int n, r, accumulate;
+};
+
+__global__ void __launch_bounds__(256) grad_f32_kernel(const Grad32Params p) {
+  __shared__ float red[8][RANKS][33];
+  __shared__ int tok[GRAD_TOKENS];
+  __shared__ __align__(16) float fac[GRAD_TOKENS * RANKS];
+  const Grad32Side& sd = blockIdx.x < p.tiles0 ? p.side[0] : p.side[1];
+  const int f = ((int)blockIdx.x - (blockIdx.x < p.tiles0 ? 0 : p.tiles0)) * 32 + (threadIdx.x & 31);
+  const int g = threadIdx.x >> 5;
+  const int j0 = blockIdx.z * RANKS, nj = min(RANKS, p.r - j0);
+  for (int64_t i = blockIdx.y; i < p.n; i += gridDim.y) {
+    const int lo = p.off[i], hi = p.off[i + 1];
+    float s[RANKS] = {};
+    for (int q0 = lo; q0 < hi; q0 += GRAD_TOKENS) {
+      // the tokens of this round and their factors once through shared memory
+      const int nq = min(GRAD_TOKENS, hi - q0);
+      __syncthreads();
+      for (int e = threadIdx.x; e < nq; e += 256) tok[e] = p.order[q0 + e];
+      __syncthreads();
+      for (int e = threadIdx.x; e < nq * RANKS; e += 256) {
+        const int j = e & (RANKS - 1);
+        fac[e] = j < nj ? sd.R[(int64_t)tok[e / RANKS] * p.r + j0 + j] : 0.f;
+      }
+      __syncthreads();
+      if (f < sd.F) {
+#pragma unroll 8
+        for (int q = g; q < nq; q += 8) {
+          const float z = sd.Z[(int64_t)tok[q] * sd.ldz + f];
+#pragma unroll
+          for (int j = 0; j < RANKS; ++j) s[j] = fmaf(fac[q * RANKS + j], z, s[j]);
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < RANKS; ++j) red[g][j][threadIdx.x & 31] = s[j];
+    __syncthreads();
+    // thread (g, lane) adds rank g of its feature over the eight groups, in their order
+    if (g < nj && f < sd.F) {
+      float v = 0.f;
+      for (int k = 0; k < 8; ++k) v += red[k][g][threadIdx.x & 31];
+      if (sd.scale) v *= sd.scale[i];
+      float* o = sd.out + (sd.by_feature ? (i * sd.F + f) * p.r + j0 + g
+                                         : (i * p.r + j0 + g) * (int64_t)sd.F + f);
+      *o = p.accumulate ? *o + v : v;
+    }
+    __syncthreads();
+  }
+}
+
+struct Layout32 {
+  int32_t* status;
+  float* R;
+  __nv_bfloat16* in;
+  __nv_bfloat16* w;
+  int32_t* order;
+  int32_t* spare;
+  int32_t* off;
+  int64_t k8, w8;
+};
+
+template <typename Take>
+void layout32(Layout32& L, bool back, int64_t T, int64_t c, int64_t b, int64_t n, int r, Take take) {
+  const int64_t K = back ? c : b;
+  L.k8 = (int64_t)round_up((size_t)K, 8);
+  L.w8 = back ? (int64_t)round_up((size_t)b, 8) : L.k8;   // W's planes keep W's own rows
+  L.status = static_cast<int32_t*>(take(256));
+  L.R = static_cast<float*>(take((size_t)T * r * 4));
+  L.in = static_cast<__nv_bfloat16*>(take((size_t)3 * T * L.k8 * 2));
+  L.w = static_cast<__nv_bfloat16*>(take((size_t)3 * c * L.w8 * 2));
+  L.order = L.spare = L.off = nullptr;
+  if (back) {
+    L.order = static_cast<int32_t*>(take((size_t)T * 4));
+    L.spare = static_cast<int32_t*>(take((size_t)T * 4));
+    L.off = static_cast<int32_t*>(take(((size_t)n + 1) * 4));
+  }
+}
+
+int split_blocks(int64_t rows) {
+  const int64_t want = ceil_div(rows, 8);
+  return (int)(want < 8 * NUM_SMS ? want : 8 * NUM_SMS);
+}
+
+}  // namespace
+
+size_t adapter_f32_workspace_bytes(bool back, int64_t T, int64_t c, int64_t b, int64_t n, int r) {
+  size_t total = 0;
+  Layout32 L;
+  layout32(L, back, T, c, b, n, r, [&](size_t bytes) -> void* {
+    total += round_up(bytes, 256);
+    return nullptr;
+  });
+  return total;
+}
+
+// forward: in = X, out = Y; backward: in = dY, out = dX (may be null)
+thanos_status_t adapter_f32(bool back, const AdapterArgs& a, void* workspace, size_t ws_bytes,
+                            cudaStream_t stream) {
+  if (ws_bytes < adapter_f32_workspace_bytes(back, a.T, a.c, a.b, a.n, a.r))
+    return THANOS_ERR_WORKSPACE;
+  char* at = static_cast<char*>(workspace);
+  Layout32 L;
+  layout32(L, back, a.T, a.c, a.b, a.n, a.r, [&](size_t bytes) -> void* {
+    void* q = at;
+    at += round_up(bytes, 256);
+    return q;
+  });
+  const int K = (int)(back ? a.c : a.b), F = (int)(back ? a.b : a.c);
+  float* R = !back && a.V ? a.V : L.R;
+  Front32Params f = {};
+  f.status = L.status;
+  if (a.dA) {
+    THANOS_TRY(sort_tokens(a.index, a.T, a.n, L.order, L.spare, L.off, L.status, stream));
+    f.status = nullptr;
+  }
+  f.in.src = static_cast<const float*>(a.in);
+  f.in.ld = a.ldi;
+  if (a.out) {
+    f.in.rows = a.T;
+    f.in.cols = K;
+    f.in.planes = L.in;
+    f.in.ldp = L.k8;
+    f.in.blocks = split_blocks(a.T);
+    f.w.src = static_cast<const float*>(a.W);
+    f.w.ld = a.ldw;
+    f.w.rows = a.c;
+    f.w.cols = (int)a.b;
+    f.w.planes = L.w;
+    f.w.ldp = L.w8;
+    f.w.blocks = split_blocks(a.c);
+  }
+  int64_t skinny = 0;
+  if (a.n > 0) {
+    f.R = R;
+    f.P = static_cast<const float*>(back ? a.B : a.A);
+    f.index = a.index;
+    f.scale = a.scale;
+    f.T = a.T;
+    f.K = K;
+    f.n = (int)a.n;
+    f.r = a.r;
+    f.back = back;
+    skinny = ceil_div(a.T * ceil_div(a.r, RANKS), 8);
+  }
+  const int64_t blocks = f.in.blocks + f.w.blocks + skinny;
+  if (blocks > 0) {
+    front_f32_kernel<<<(unsigned)blocks, 256, 0, stream>>>(f);
+    THANOS_CHECK_LAUNCH();
+  } else if (f.status) {
+    THANOS_CUDA(cudaMemsetAsync(L.status, 0, 16, stream));
+  }
+  if (a.out) {
+    ProjArgs g;
+    g.f32 = 1;
+    g.M = F;
+    g.N = (int)a.T;
+    g.K = K;
+    g.A = L.w;
+    g.lda = L.w8;
+    g.a_batch = a.c * L.w8;
+    g.a_mn = back ? 1 : 0;
+    g.B = L.in;
+    g.ldb = L.k8;
+    g.b_batch = a.T * L.k8;
+    g.status = L.status;
+    g.out = a.out;
+    g.ldo = a.ldo;
+    if (a.n > 0) {
+      g.V = R;
+      g.index = a.index;
+      g.scale = back ? nullptr : a.scale;
+      g.n_adapters = (int)a.n;
+      g.r = a.r;
+      g.P = back ? a.A : a.B;
+      g.ldp = back ? a.b : a.r;
+      g.p_adapter = back ? a.r * a.b : a.c * a.r;
+    }
+    THANOS_TRY(proj_gemm(g, stream));
+  }
+  if (a.dA) {
+    Grad32Params g = {};
+    g.side[0] = {static_cast<const float*>(a.X), a.ldx, L.R, nullptr, a.dA, (int)a.b, 0};
+    g.side[1] = {static_cast<const float*>(a.in), a.ldi, a.Vin, a.scale, a.dB, (int)a.c, 1};
+    g.tiles0 = (int)ceil_div(a.b, 32);
+    g.order = L.order;
+    g.off = L.off;
+    g.n = (int)a.n;
+    g.r = a.r;
+    g.accumulate = a.accumulate;
+    const dim3 grid((unsigned)(g.tiles0 + ceil_div(a.c, 32)), (unsigned)(a.n < 65535 ? a.n : 65535),
+                    (unsigned)ceil_div(a.r, RANKS));
+    grad_f32_kernel<<<grid, 256, 0, stream>>>(g);
+    THANOS_CHECK_LAUNCH();
+  }
+  return THANOS_OK;
+}
+
+}  // namespace thanos

@@ -30,7 +30,7 @@ constexpr int FACTOR_BYTES = 128 * 16 * 4;    // 16 ranks of up to 128 tokens, f
 
 struct Params {
   int M, N, K, tiles_m, tiles_n, nt, stages, splits, batch_z, ring_bytes, tmem_cols;
-  int symmetric, f16, early;
+  int symmetric, f16, early, f32;     // f32: three bf16 planes per operand, fp32 result
   int32_t* status;
   // adapter part
   void* out;
@@ -41,7 +41,7 @@ struct Params {
   int n_adapters, r, chunks;          // chunks of 16 per adapter
   const int32_t* tile_count;
   const int32_t* tile_list;
-  const __nv_bfloat16* P;
+  const __nv_bfloat16* P;             // f32: fp32 values
   int64_t ldp, p_adapter;
   // iteration
   float alpha, beta;
@@ -109,6 +109,20 @@ __device__ __forceinline__ void tc_ld8(uint32_t taddr, float (&v)[8]) {
   tc_wait_ld();
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(u[e]);
+}
+__device__ __forceinline__ void tc_ld16(uint32_t taddr, float (&v)[16]) {
+  uint32_t u[16];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]),
+        "=r"(u[7]), "=r"(u[8]), "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]),
+        "=r"(u[14]), "=r"(u[15])
+      : "r"(taddr)
+      : "memory");
+  tc_wait_ld();
+#pragma unroll
+  for (int e = 0; e < 16; ++e) v[e] = __uint_as_float(u[e]);
 }
 __device__ __forceinline__ void tc_st8(uint32_t taddr, const float (&v)[8]) {
   asm volatile(
@@ -222,6 +236,13 @@ __device__ __forceinline__ void emit(const Params& p, int z, int m, int n0, floa
   if (m >= p.M || n0 >= p.N) return;
   const int nc = p.N - n0;  // columns that exist
   if constexpr (EPI == PROJ_OUT) {
+    if (p.f32) {
+      float* out = static_cast<float*>(p.out) + (int64_t)n0 * p.ldo + m;
+#pragma unroll
+      for (int e = 0; e < NC; ++e)
+        if (e < nc) out[(int64_t)e * p.ldo] = v[e];
+      return;
+    }
     __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + (int64_t)n0 * p.ldo + m;
     if (poisoned) {
 #pragma unroll
@@ -318,28 +339,120 @@ __device__ __forceinline__ void emit(const Params& p, int z, int m, int n0, floa
       } else {
         // loads first: W_in may be W_out, so the compiler cannot move them over the stores
         float w[NC];
+        uint32_t gone = 0;  // bit e: removed
+        if (p.tall && p.N % 8 == 0) {
+          // the thread's columns are consecutive in memory, and whole groups of eight exist or not
 #pragma unroll
-        for (int e = 0; e < NC; ++e) {
-          w[e] = 0.f;
-          if (e < nc)
-            w[e] = p.w_bf16 ? __bfloat162float(
-                                  static_cast<const __nv_bfloat16*>(p.W_in)[at0 + e * step])
-                            : static_cast<const float*>(p.W_in)[at0 + e * step];
-        }
-        uint32_t gone = 0;
-        if (p.mask) {
+          for (int e8 = 0; e8 < NC; e8 += 8) {
+            if (e8 >= nc) break;
+            if (p.w_bf16) {
+              const uint4 q = *reinterpret_cast<const uint4*>(
+                  static_cast<const __nv_bfloat16*>(p.W_in) + at0 + e8);
+              const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                w[e8 + 2 * e] = __uint_as_float(u[e] << 16);
+                w[e8 + 2 * e + 1] = __uint_as_float(u[e] & 0xFFFF0000u);
+              }
+            } else {
+#pragma unroll
+              for (int e4 = 0; e4 < 8; e4 += 4) {
+                const float4 q = *reinterpret_cast<const float4*>(
+                    static_cast<const float*>(p.W_in) + at0 + e8 + e4);
+                w[e8 + e4] = q.x;
+                w[e8 + e4 + 1] = q.y;
+                w[e8 + e4 + 2] = q.z;
+                w[e8 + e4 + 3] = q.w;
+              }
+            }
+            if (p.mask) {
+              const uint2 q = *reinterpret_cast<const uint2*>(p.mask + at0 + e8);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                if ((q.x >> (8 * e)) & 0xFFu) gone |= 1u << (e8 + e);
+                if ((q.y >> (8 * e)) & 0xFFu) gone |= 1u << (e8 + 4 + e);
+              }
+            }
+          }
 #pragma unroll
           for (int e = 0; e < NC; ++e)
-            if (e < nc && p.mask[at0 + e * step] != 0) gone |= 1u << e;
-        }
+            v[e] = (gone >> e) & 1u ? 0.f : fmaf(-p.rate, v[e], p.keep * w[e]);
 #pragma unroll
-        for (int e = 0; e < NC; ++e) {
-          if (e >= nc) break;
-          const float x = (gone >> e) & 1u ? 0.f : fmaf(-p.rate, v[e], p.keep * w[e]);
-          if (p.w_bf16)
-            static_cast<__nv_bfloat16*>(p.W_out)[at0 + e * step] = __float2bfloat16_rn(x);
-          else
-            static_cast<float*>(p.W_out)[at0 + e * step] = x;
+          for (int e8 = 0; e8 < NC; e8 += 8) {
+            if (e8 >= nc) break;
+            if (p.w_bf16) {
+              uint4 q;
+              uint32_t* u = reinterpret_cast<uint32_t*>(&q);
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                u[e] = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(v[e8 + 2 * e])) |
+                       ((uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(v[e8 + 2 * e + 1])) << 16);
+              *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.W_out) + at0 + e8) = q;
+            } else {
+#pragma unroll
+              for (int e4 = 0; e4 < 8; e4 += 4)
+                *reinterpret_cast<float4*>(static_cast<float*>(p.W_out) + at0 + e8 + e4) =
+                    make_float4(v[e8 + e4], v[e8 + e4 + 1], v[e8 + e4 + 2], v[e8 + e4 + 3]);
+            }
+          }
+        } else {
+          // the type is asked once, not per element: a branch between two loads would keep them from
+          // being in flight together
+          if (p.w_bf16) {
+            const __nv_bfloat16* W = static_cast<const __nv_bfloat16*>(p.W_in) + at0;
+            __nv_bfloat16 h[NC];
+#pragma unroll
+            for (int e = 0; e < NC; ++e) h[e] = e < nc ? W[e * step] : __float2bfloat16_rn(0.f);
+#pragma unroll
+            for (int e = 0; e < NC; ++e) w[e] = __bfloat162float(h[e]);
+          } else {
+            const float* W = static_cast<const float*>(p.W_in) + at0;
+#pragma unroll
+            for (int e = 0; e < NC; ++e) w[e] = e < nc ? W[e * step] : 0.f;
+          }
+          if (p.mask && !p.tall && p.M % 16 == 0 && m - (int)(threadIdx.x & 31) + 32 <= p.M &&
+              nc >= NC) {
+            // 32 mask bytes of each of the NC columns, 16 by a lane in one load; one bit per byte is
+            // then handed to the lane that it belongs to (a byte load per column took twice the time
+            // of everything else here)
+            const int lane = threadIdx.x & 31;
+            uint32_t bits = 0;
+            if (lane < 2 * NC) {
+              const uint4 q = *reinterpret_cast<const uint4*>(
+                  p.mask + at0 - lane + (int64_t)(lane >> 1) * step + 16 * (lane & 1));
+              const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+                  if ((u[e] >> (8 * b)) & 0xFFu) bits |= 1u << (4 * e + b);
+            }
+#pragma unroll
+            for (int e = 0; e < NC; ++e) {
+              const uint32_t of = __shfl_sync(0xffffffffu, bits, 2 * e + (lane >> 4));
+              gone |= ((of >> (lane & 15)) & 1u) << e;
+            }
+          } else if (p.mask) {
+            uint8_t k[NC];
+#pragma unroll
+            for (int e = 0; e < NC; ++e) k[e] = e < nc ? p.mask[at0 + e * step] : (uint8_t)0;
+#pragma unroll
+            for (int e = 0; e < NC; ++e) gone |= (k[e] ? 1u : 0u) << e;
+          }
+#pragma unroll
+          for (int e = 0; e < NC; ++e)
+            v[e] = (gone >> e) & 1u ? 0.f : fmaf(-p.rate, v[e], p.keep * w[e]);
+          if (p.w_bf16) {
+            __nv_bfloat16* W = static_cast<__nv_bfloat16*>(p.W_out) + at0;
+#pragma unroll
+            for (int e = 0; e < NC; ++e)
+              if (e < nc) W[e * step] = __float2bfloat16_rn(v[e]);
+          } else {
+            float* W = static_cast<float*>(p.W_out) + at0;
+#pragma unroll
+            for (int e = 0; e < NC; ++e)
+              if (e < nc) W[e * step] = v[e];
+          }
         }
       }
     }
@@ -418,6 +531,38 @@ __device__ __forceinline__ float dot16(const uint32_t (&w)[8], const float* __re
   return s;
 }
 
+// The same part in fp32 for eight tokens, columns c.. of the tile.
+template <bool AMN>
+__device__ __forceinline__ void wide_part_f32(const Params& p, const int* ids, const float* factor,
+                                              int c, int m, int j0, float (&own)[8]) {
+  const float* P = reinterpret_cast<const float*>(p.P);
+  const int nj = min(16, p.r - j0);
+#pragma unroll 1
+  for (int e = 0; e < 8; ++e) {
+    const int i = ids[c + e];
+    if (i < 0) continue;
+    const float* q = P + (int64_t)i * p.p_adapter +
+                     (AMN ? (int64_t)j0 * p.ldp + m : (int64_t)m * p.ldp + j0);
+    const int64_t dj = AMN ? p.ldp : 1;
+    const float* f = factor + (c + e) * 16;
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+      if (j < nj) s = fmaf(q[j * dj], f[j], s);
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (k == e) own[k] = s;
+  }
+}
+
+// Planes of the six products that make up an fp32 product, the smallest first: the tensor cores cut
+// what they add to an accumulator, by up to 2^-23 of it each time, so the products that are 2^-9 and
+// 2^-18 of the whole go in before the accumulator has its size.
+__device__ __forceinline__ void plane_pair(int combo, int& a, int& b) {
+  a = (0x010201 >> (4 * combo)) & 15;  // nibbles from the right: mm, hl, lh, hm, mh, hh
+  b = (0x001021 >> (4 * combo)) & 15;
+}
+
 template <bool AMN, int EPI>
 __global__ void __launch_bounds__(TILE_THREADS, EPI <= PROJ_SHRINK ? 2 : 1)
 tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
@@ -494,7 +639,8 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
     grid_dependents_launch();
   }
 
-  const int nk = (p.K + BK - 1) / BK;
+  const int nk1 = (p.K + BK - 1) / BK;
+  const int nk = EPI == PROJ_OUT && p.f32 ? 6 * nk1 : nk1;
   const int ks0 = (int)((int64_t)nk * rank / S), ks1 = (int)((int64_t)nk * (rank + 1) / S);
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
@@ -506,14 +652,20 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
       ok = mbar_wait(empty_bar(s), phase ^ 1u, abort_flag);
       if (ok) {
         const uint32_t dst = smem_base + (uint32_t)s * stage_bytes;
+        int k0 = ks * BK, za = z, zb = z;
+        if (EPI == PROJ_OUT && p.f32) {
+          const int combo = ks / nk1;
+          k0 = (ks - combo * nk1) * BK;
+          plane_pair(combo, za, zb);
+        }
         mbar_expect_tx(full_bar(s), stage_bytes);
         if (AMN) {
-          tma_load_3d(dst, &mapA, full_bar(s), m0, ks * BK, z);
-          tma_load_3d(dst + A_BYTES / 2, &mapA, full_bar(s), m0 + 64, ks * BK, z);
+          tma_load_3d(dst, &mapA, full_bar(s), m0, k0, za);
+          tma_load_3d(dst + A_BYTES / 2, &mapA, full_bar(s), m0 + 64, k0, za);
         } else {
-          tma_load_3d(dst, &mapA, full_bar(s), ks * BK, m0, z);
+          tma_load_3d(dst, &mapA, full_bar(s), k0, m0, za);
         }
-        tma_load_3d(dst + A_BYTES, &mapB, full_bar(s), ks * BK, n0, z);
+        tma_load_3d(dst + A_BYTES, &mapB, full_bar(s), k0, n0, zb);
       }
       if (++s == p.stages) {
         s = 0;
@@ -569,7 +721,7 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
     bool used = false;
     if constexpr (EPI == PROJ_OUT) {
       // ---------------------------------------------------------- adapter part
-      if (p.n_adapters > 0 && p.early) {
+      if (p.n_adapters > 0 && p.early && !p.f32) {
         // the rows of the wide factors that this thread will read are on their way to L2 while the
         // previous launch still computes V
 #pragma unroll 1
@@ -624,7 +776,9 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
             bool same = true;
 #pragma unroll
             for (int e = 1; e < 8; ++e) same = same && ids[c + e] == first;
-            if (m < p.M) {
+            if (m < p.M && p.f32) {
+              wide_part_f32<AMN>(p, ids, factor, c, m, j0, own);
+            } else if (m < p.M) {
               if (same) {  // a run of one request's tokens (or none): its row is read once
                 if (first >= 0) {
                   uint32_t w[8];
@@ -1047,15 +1201,24 @@ pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
         }
         const bool poisoned = ext && *(volatile int*)poison != 0;
         const uint32_t taddr = tmem_base + ((uint32_t)(32 * g) << 16) + (uint32_t)q * 256;
+        if constexpr (EPI == PROJ_FINAL) {  // its operands leave room for half as many columns
 #pragma unroll 1
-        for (int cc = 32 * h; cc < p.nt; cc += 64) {
-          uint32_t u[32];
-          tc_ld32(taddr + cc, u);
-          tc_wait_ld();
-          float v[32];
+          for (int cc = 16 * h; cc < p.nt; cc += 32) {
+            float v[16];
+            tc_ld16(taddr + cc, v);
+            emit<AMN, EPI, 16>(p, tl.z, m, n0 + cc, v, false, false);
+          }
+        } else {
+#pragma unroll 1
+          for (int cc = 32 * h; cc < p.nt; cc += 64) {
+            uint32_t u[32];
+            tc_ld32(taddr + cc, u);
+            tc_wait_ld();
+            float v[32];
 #pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(u[i]);
-          emit<AMN, EPI, 32>(p, tl.z, m, n0 + cc, v, tl.tm != tl.tn, poisoned);
+            for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(u[i]);
+            emit<AMN, EPI, 32>(p, tl.z, m, n0 + cc, v, tl.tm != tl.tn, poisoned);
+          }
         }
       }
       tc_fence_before();
@@ -1219,18 +1382,19 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
   p.M = a.M;
   p.N = a.N;
   p.K = a.K;
-  const bool pairs = a.epi != PROJ_SHRINK && use_pairs(a.M, a.N, a.batch, symmetric);
+  const bool pairs = a.epi != PROJ_SHRINK && !a.f32 && use_pairs(a.M, a.N, a.batch, symmetric);
   p.nt = pairs ? PTM : tile_width(a.M, a.N, a.batch, symmetric, a.epi <= PROJ_SHRINK);
   p.tiles_m = (a.M + (pairs ? PTM : TM) - 1) / (pairs ? PTM : TM);
   p.tiles_n = (a.N + p.nt - 1) / p.nt;
   p.batch_z = a.batch;
   p.symmetric = symmetric;
   p.f16 = a.f16;
+  p.f32 = a.f32;
   p.early = a.early;
   p.status = a.status;
   int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * a.batch;
   if (symmetric) tiles = (tiles + (int64_t)p.tiles_m * a.batch * (TM / p.nt)) / 2;
-  const int nk = (a.K + BK - 1) / BK;
+  const int nk = (a.K + BK - 1) / BK * (a.f32 ? 6 : 1);
   p.splits = 1;
   // A split fills SMs that have no tile; beyond a quarter more CTAs than SMs it costs more in
   // partial sums than it brings (4096 x 4096, 1 token: 4 slices 12.4 us, 8 slices 14.4 us).
@@ -1278,9 +1442,10 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
 
   CUtensorMap mA, mB, mP;
   const CUtensorMapSwizzle sw = CU_TENSOR_MAP_SWIZZLE_128B;
-  const bool okA = a.a_mn ? make_map3(&mA, a.A, a.f16, a.M, a.K, a.lda, a.batch, a.a_batch, 64, BK, sw)
-                          : make_map3(&mA, a.A, a.f16, a.K, a.M, a.lda, a.batch, a.a_batch, BK, TM, sw);
-  if (!okA || !make_map3(&mB, a.B, a.f16, a.K, a.N, a.ldb, a.batch, a.b_batch, BK,
+  const int64_t slabs = a.f32 ? 3 : a.batch;
+  const bool okA = a.a_mn ? make_map3(&mA, a.A, a.f16, a.M, a.K, a.lda, slabs, a.a_batch, 64, BK, sw)
+                          : make_map3(&mA, a.A, a.f16, a.K, a.M, a.lda, slabs, a.a_batch, BK, TM, sw);
+  if (!okA || !make_map3(&mB, a.B, a.f16, a.K, a.N, a.ldb, slabs, a.b_batch, BK,
                          pairs ? p.nt / 2 : p.nt, sw))
     return THANOS_ERR_CUDA;
   mP = mA;

@@ -31,11 +31,13 @@ struct ProjArgs {
   const void* B = nullptr;
   int64_t ldb = 0, b_batch = 0;
   int f16 = 0;                   // operands fp16 instead of bf16
+  int f32 = 0;                   // PROJ_OUT with fp32 accuracy: A and B are three bf16 planes (a_batch,
+                                 // b_batch apart), out and P are fp32
   int epi = PROJ_OUT;
   int early = 0;                 // operands do not depend on the previous launch of the stream
   int32_t* status = nullptr;
   // PROJ_OUT, PROJ_SHRINK
-  void* out = nullptr;           // bf16 [N, ldo]
+  void* out = nullptr;           // [N, ldo], bf16 (fp32 if f32)
   int64_t ldo = 0;
   float* V = nullptr;            // [N, r]: PROJ_OUT reads it (forward: V, backward: U); SHRINK writes
   const int32_t* index = nullptr;

@@ -36,6 +36,11 @@ thanos_status_t adapter_forward_impl(const AdapterArgs& a, void* workspace, size
 thanos_status_t adapter_backward_impl(const AdapterArgs& a, void* workspace, size_t ws_bytes,
                                       cudaStream_t stream);
 
+// fp32 operands (adapter_f32.cu)
+size_t adapter_f32_workspace_bytes(bool back, int64_t T, int64_t c, int64_t b, int64_t n, int r);
+thanos_status_t adapter_f32(bool back, const AdapterArgs& a, void* workspace, size_t ws_bytes,
+                            cudaStream_t stream);
+
 struct OrthogonalArgs {
   const void* G = nullptr;
   thanos_dtype_t gdtype = THANOS_F32;
