@@ -51,7 +51,7 @@ __device__ void split_job(const SplitJob& s, int blk) {
     const float* src = s.src + row * s.ld;
     __nv_bfloat16* dst = s.planes + row * s.ldp;
     if (wide) {
-#pragma unroll 4
+#pragma unroll 2
       for (int c = 4 * lane; c < s.cols; c += 128) {
         const float4 x = *reinterpret_cast<const float4*>(src + c);
         float o[4] = {x.x, x.y, x.z, x.w};

@@ -206,14 +206,15 @@ __global__ void __launch_bounds__(256) split_kernel(const StepParams p) {
 //   steps_kernel  one CTA per matrix: sums the partials in order, iterates, Q / (norm + eps)
 //   apply_kernel  Q X_0 over chunks of the long side, into O or the new weights
 constexpr int SMALL_SIDE = 64;
-constexpr int GRAM_COLS = 64;    // long-side columns staged at a time
 constexpr int SMALL_LD = SMALL_SIDE + 4;
+constexpr int STAGE_FLOATS = 10240;  // a tile of the long side, padded rows: 512 columns of 16 rows
 
 struct SmallParams {
   StepParams u;
   float* part;       // [batch][chunks][s][s]
   float* Q;          // [batch][s][s]
-  int s, l, chunks, chunk_cols, steps;
+  int s, l, chunks, chunk_cols, tile_cols, steps;
+  uint32_t inv_s;    // ceil(2^32 / s) for s > 1: e / s is the high word of e inv_s
   float a, b, c;
   __nv_bfloat16* O;
   void* W_out;
@@ -222,58 +223,62 @@ struct SmallParams {
   float keep, rate;
 };
 
-// stages columns [c0, c0 + GRAM_COLS) as Xs[column][row]; FIRST also writes the momentum
-template <bool FIRST>
-__device__ __forceinline__ void stage_columns(const SmallParams& p, int64_t base, int c0, int c1,
-                                              float (*Xs)[SMALL_LD]) {
-  const int s4 = (p.s + 3) & ~3;
-  for (int e = threadIdx.x; e < GRAM_COLS * s4; e += 256) {
-    // consecutive threads along the contiguous axis of the matrix
-    int r, c;
-    if (p.u.tall) {
-      c = e / s4;
-      r = e - c * s4;
-    } else {
-      r = e / GRAM_COLS;
-      c = e - r * GRAM_COLS;
+__device__ __forceinline__ int over_s(const SmallParams& p, int e) {
+  return p.s == 1 ? e : (int)__umulhi((uint32_t)e, p.inv_s);
+}
+
+// Stages columns [c0, c0 + cols) of the long side as Xs[column * ld + row]; FIRST also writes the
+// momentum.  Consecutive threads go along the matrix' contiguous axis.
+template <int VEC, bool FIRST>
+__device__ __forceinline__ void stage_columns(const SmallParams& p, int64_t base, int c0, int cols,
+                                              float* Xs, int ld) {
+  if (p.u.tall) {
+    const int total = cols * p.s;
+    const int64_t at0 = base + (int64_t)c0 * p.s;
+#pragma unroll 2
+    for (int e = threadIdx.x * VEC; e < total; e += 256 * VEC) {
+      const int c = over_s(p, e), r = e - c * p.s;
+      float v[VEC];
+      update_vec<VEC, FIRST>(p.u, at0 + e, v);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) Xs[c * ld + r + i] = v[i];
     }
-    float v = 0.f;
-    if (r < p.s && c0 + c < c1) {
-      const int64_t at = base + (p.u.tall ? (int64_t)(c0 + c) * p.s + r : (int64_t)r * p.l + c0 + c);
-      float mo = 0.f;
-      if (p.u.M_out) {
-        if (FIRST) {
-          const bool gone = p.u.mask && p.u.mask[at] != 0;
-          mo = fmaf(p.u.momentum, p.u.M_in[at], gone ? 0.f : load_any(p.u.G, p.u.g_bf16, at));
-          p.u.M_out[at] = mo;
-        } else {
-          mo = p.u.M_out[at];
-        }
+  } else {
+    for (int r = threadIdx.x >> 5; r < p.s; r += 8) {
+      const int64_t at0 = base + (int64_t)r * p.l + c0;
+#pragma unroll 4
+      for (int c = (threadIdx.x & 31) * VEC; c < cols; c += 32 * VEC) {
+        float v[VEC];
+        update_vec<VEC, FIRST>(p.u, at0 + c, v);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) Xs[(c + i) * ld + r] = v[i];
       }
-      v = update_of(p.u, at, mo);
     }
-    Xs[c][r] = v;
   }
 }
 
+template <int VEC>
 __global__ void __launch_bounds__(256) gram_kernel(const SmallParams p) {
-  __shared__ __align__(16) float Xs[GRAM_COLS][SMALL_LD];
+  extern __shared__ __align__(16) float Xs[];
   grid_dependents_launch();
   if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.u.status = 0;
   const int64_t base = (int64_t)blockIdx.y * p.s * p.l;
-  const int q = (p.s + 3) / 4, tiles = q * q, groups = 256 / tiles;
+  const int q = (p.s + 3) / 4, tiles = q * q, groups = 256 / tiles, ld = 4 * q + 4;
   const int g = threadIdx.x / tiles, tile = threadIdx.x - g * tiles;
   const int ti = tile / q, tj = tile - ti * q;
   const int c_lo = blockIdx.x * p.chunk_cols, c_hi = min(p.l, c_lo + p.chunk_cols);
+  for (int e = threadIdx.x; e < STAGE_FLOATS; e += 256) Xs[e] = 0.f;  // rows beyond s stay zero
   float acc[4][4] = {};
-  for (int c0 = c_lo; c0 < c_hi; c0 += GRAM_COLS) {
+  for (int c0 = c_lo; c0 < c_hi; c0 += p.tile_cols) {
+    const int cols = min(p.tile_cols, c_hi - c0);
     __syncthreads();
-    stage_columns<true>(p, base, c0, c_hi, Xs);
+    stage_columns<VEC, true>(p, base, c0, cols, Xs, ld);
     __syncthreads();
     if (g < groups) {
-      for (int c = g; c < GRAM_COLS; c += groups) {
-        const float4 x = *reinterpret_cast<const float4*>(&Xs[c][4 * ti]);
-        const float4 y = *reinterpret_cast<const float4*>(&Xs[c][4 * tj]);
+#pragma unroll 2
+      for (int c = g; c < cols; c += groups) {
+        const float4 x = *reinterpret_cast<const float4*>(Xs + c * ld + 4 * ti);
+        const float4 y = *reinterpret_cast<const float4*>(Xs + c * ld + 4 * tj);
         const float xv[4] = {x.x, x.y, x.z, x.w}, yv[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -282,155 +287,158 @@ __global__ void __launch_bounds__(256) gram_kernel(const SmallParams p) {
       }
     }
   }
-  // the groups' sums, in order of the group, through shared memory
-  float* red = &Xs[0][0];
-  float* out = p.part + ((int64_t)blockIdx.y * p.chunks + blockIdx.x) * p.s * p.s;
-  for (int k = 0; k < 16; k += 4) {
-    __syncthreads();
-    if (g < groups) {
+  // the groups' sums, in order of the group
+  __syncthreads();
+  if (g < groups) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) red[threadIdx.x * 4 + j] = acc[k / 4][j];
-    }
-    __syncthreads();
-    for (int e = threadIdx.x; e < tiles * 4; e += 256) {
-      const int tl = e >> 2, j = e & 3;
-      float v = 0.f;
-      for (int gg = 0; gg < groups; ++gg) v += red[(gg * tiles + tl) * 4 + j];
-      const int r = 4 * (tl / q) + k / 4, c = 4 * (tl % q) + j;
-      if (r < p.s && c < p.s) out[r * p.s + c] = v;
-    }
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<float4*>(Xs + (g * tiles + tile) * 16 + 4 * i) =
+          make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+  }
+  __syncthreads();
+  float* out = p.part + ((int64_t)blockIdx.y * p.chunks + blockIdx.x) * p.s * p.s;
+  for (int e = threadIdx.x; e < tiles * 16; e += 256) {
+    float v = 0.f;
+    for (int k = 0; k < groups; ++k) v += Xs[k * tiles * 16 + e];
+    const int tl = e >> 4, tr = tl / q;
+    const int r = 4 * tr + ((e >> 2) & 3), c = 4 * (tl - tr * q) + (e & 3);
+    if (r < p.s && c < p.s) out[r * p.s + c] = v;
   }
 }
 
-// D = A^T B for s x s matrices in shared memory (rows padded to SMALL_LD, zeros beyond s); ADD:
-// D = a I + b A + c A^T B.  S and P are symmetric up to rounding, S P and Q are not: what is left
-// of a rounding in them grows by a = 3.4 per step on one side only, so a transpose of Q in its
-// place is wrong by 1e-2 and more on matrices of low rank.
-template <bool ADD>
-__device__ __forceinline__ void small_product(float (*D)[SMALL_LD], const float (*A)[SMALL_LD],
-                                              const float (*B)[SMALL_LD], int s, float a, float b,
-                                              float c) {
-  const int q = (s + 3) / 4, tiles = q * q;
-  if (threadIdx.x < tiles) {
+// D = A^T B for s x s matrices in shared memory (rows padded to SMALL_LD, zeros beyond s); with
+// `add`, D = a I + b A + c A^T B.  S and P are symmetric up to rounding, S P and Q are not: what is
+// left of a rounding in them grows by a = 3.4 per step on one side only, so a transpose of Q in its
+// place is wrong by 1e-2 and more on matrices of low rank.  TS x TS outputs a thread; one copy of the
+// code for all the products of a step, which run one after another on one CTA.
+template <int TS>
+__device__ __noinline__ void small_product(float* D, const float* A, const float* B, int s, bool add,
+                                           float a, float b, float c) {
+  const int q = (s + TS - 1) / TS;
+  if (threadIdx.x < q * q) {
     const int ti = threadIdx.x / q, tj = threadIdx.x - ti * q;
-    float acc[4][4] = {};
+    const float* x = A + TS * ti;
+    const float* y = B + TS * tj;
+    float acc[TS][TS] = {};
+#pragma unroll 4
     for (int k = 0; k < s; ++k) {
-      const float4 x = *reinterpret_cast<const float4*>(&A[k][4 * ti]);
-      const float4 y = *reinterpret_cast<const float4*>(&B[k][4 * tj]);
-      const float xv[4] = {x.x, x.y, x.z, x.w}, yv[4] = {y.x, y.y, y.z, y.w};
+      float xv[TS], yv[TS];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < TS; ++i) {
+        xv[i] = x[k * SMALL_LD + i];
+        yv[i] = y[k * SMALL_LD + i];
+      }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(xv[i], yv[j], acc[i][j]);
+      for (int i = 0; i < TS; ++i)
+#pragma unroll
+        for (int j = 0; j < TS; ++j) acc[i][j] = fmaf(xv[i], yv[j], acc[i][j]);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < TS; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int r = 4 * ti + i, cc = 4 * tj + j;
+      for (int j = 0; j < TS; ++j) {
+        const int r = TS * ti + i, cc = TS * tj + j;
         float v = acc[i][j];
-        if (ADD) v = fmaf(c, v, fmaf(b, A[r][cc], r == cc ? a : 0.f));
-        D[r][cc] = v;
+        if (add) v = fmaf(c, v, fmaf(b, A[r * SMALL_LD + cc], r == cc ? a : 0.f));
+        if (r < s && cc < s) D[r * SMALL_LD + cc] = v;
       }
   }
   __syncthreads();
 }
 
+template <int TS>
 __global__ void __launch_bounds__(256) steps_kernel(const SmallParams p) {
   extern __shared__ __align__(16) float mats[];
-  float(*M[5])[SMALL_LD];
-  for (int i = 0; i < 5; ++i)
-    M[i] = reinterpret_cast<float(*)[SMALL_LD]>(mats + i * SMALL_SIDE * SMALL_LD);
+  constexpr int SZ = SMALL_SIDE * SMALL_LD;
+  float *S = mats, *P = mats + SZ, *Q = mats + 2 * SZ, *T = mats + 3 * SZ, *U = mats + 4 * SZ;
   __shared__ float norm;
+  const int s = p.s, ss = s * s;
+  for (int e = threadIdx.x; e < 5 * SZ; e += 256) mats[e] = 0.f;
+  __syncthreads();
   grid_dependency_wait();
   grid_dependents_launch();
-  const int s = p.s, s4 = (s + 3) & ~3;
-  const float* part = p.part + (int64_t)blockIdx.x * p.chunks * s * s;
-  for (int e = threadIdx.x; e < s4 * s4; e += 256) {
-    const int r = e / s4, c = e - r * s4;
+  const float* part = p.part + (int64_t)blockIdx.x * p.chunks * ss;
+  for (int e = threadIdx.x; e < ss; e += 256) {
     float v = 0.f;
-    if (r < s && c < s)
-      for (int k = 0; k < p.chunks; ++k) v += part[(int64_t)k * s * s + r * s + c];
-    M[0][r][c] = v;
+#pragma unroll 8
+    for (int k = 0; k < p.chunks; ++k) v += part[k * ss + e];
+    const int r = over_s(p, e);
+    S[r * SMALL_LD + e - r * s] = v;
   }
   __syncthreads();
-  if (threadIdx.x == 0) {
+  if (threadIdx.x < 32) {
     float t = 0.f;
-    for (int i = 0; i < s; ++i) t += M[0][i][i];
-    norm = sqrtf(t) + p.u.eps;
+    for (int i = threadIdx.x; i < s; i += 32) t += S[i * SMALL_LD + i];
+    for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+    if (threadIdx.x == 0) norm = sqrtf(t) + p.u.eps;
   }
   __syncthreads();
   const float inv = 1.f / norm;
-  for (int e = threadIdx.x; e < s4 * s4; e += 256) {
-    const int r = e / s4, c = e - r * s4;
-    M[0][r][c] = M[0][r][c] * inv * inv;
-  }
+  for (int e = threadIdx.x; e < s * SMALL_LD; e += 256) S[e] = S[e] * inv * inv;
   __syncthreads();
-  float(*S)[SMALL_LD] = M[0], (*P)[SMALL_LD] = M[1], (*Q)[SMALL_LD] = M[2], (*T)[SMALL_LD] = M[3],
-  (*U)[SMALL_LD] = M[4];
+#pragma unroll 1
   for (int it = 0; it < p.steps; ++it) {
-    small_product<true>(P, S, S, s, p.a, p.b, p.c);
-    if (it == 0) {
-      for (int e = threadIdx.x; e < s4 * s4; e += 256) Q[e / s4][e % s4] = P[e / s4][e % s4];
-      __syncthreads();
-    } else {
-      small_product<false>(U, P, Q, s, 0.f, 0.f, 0.f);
-      float(*t)[SMALL_LD] = Q;
+    float* first = it == 0 ? Q : P;                       // Q_1 = P_0
+    small_product<TS>(first, S, S, s, true, p.a, p.b, p.c);
+    if (it > 0) {
+      small_product<TS>(U, P, Q, s, false, 0.f, 0.f, 0.f);
+      float* t = Q;
       Q = U;
       U = t;
     }
     if (it + 1 < p.steps) {
-      small_product<false>(T, S, P, s, 0.f, 0.f, 0.f);   // S P
-      small_product<false>(S, T, P, s, 0.f, 0.f, 0.f);   // (S P)^T P = P S P
+      small_product<TS>(T, S, first, s, false, 0.f, 0.f, 0.f);  // S P
+      small_product<TS>(S, T, first, s, false, 0.f, 0.f, 0.f);  // (S P)^T P = P S P
     }
   }
-  float* out = p.Q + (int64_t)blockIdx.x * s * s;
-  for (int e = threadIdx.x; e < s * s; e += 256) out[e] = Q[e / s][e % s] * inv;
+  float* out = p.Q + (int64_t)blockIdx.x * ss;
+  for (int e = threadIdx.x; e < ss; e += 256) {
+    const int r = over_s(p, e);
+    out[e] = Q[r * SMALL_LD + e - r * s] * inv;
+  }
 }
 
+template <int VEC>
 __global__ void __launch_bounds__(256) apply_kernel(const SmallParams p) {
-  __shared__ __align__(16) float Xs[GRAM_COLS][SMALL_LD];
-  __shared__ __align__(16) float Qs[SMALL_SIDE][SMALL_LD];
-  grid_dependency_wait();
+  extern __shared__ __align__(16) float Xs[];               // odd rows: a lane per column
+  float* Qs = Xs + STAGE_FLOATS;                            // Qs[k][row]
   const int64_t base = (int64_t)blockIdx.y * p.s * p.l;
+  const int s4 = (p.s + 3) & ~3, ld = s4 + 1, q = s4 / 4;
+  for (int e = threadIdx.x; e < p.s * SMALL_LD; e += 256) Qs[e] = 0.f;
+  __syncthreads();
+  grid_dependency_wait();
   const float* Q = p.Q + (int64_t)blockIdx.y * p.s * p.s;
-  const int s4 = (p.s + 3) & ~3;
-  for (int e = threadIdx.x; e < s4 * s4; e += 256) {
-    const int r = e / s4, c = e - r * s4;
-    Qs[c][r] = r < p.s && c < p.s ? Q[r * p.s + c] : 0.f;
+  for (int e = threadIdx.x; e < p.s * p.s; e += 256) {
+    const int r = over_s(p, e);
+    Qs[(e - r * p.s) * SMALL_LD + r] = Q[e];
   }
-  for (int64_t t = blockIdx.x; t * GRAM_COLS < p.l; t += gridDim.x) {
-    const int c0 = (int)t * GRAM_COLS;
+  for (int c0 = blockIdx.x * p.tile_cols; c0 < p.l; c0 += gridDim.x * p.tile_cols) {
+    const int cols = min(p.tile_cols, p.l - c0);
     __syncthreads();
-    stage_columns<false>(p, base, c0, p.l, Xs);
+    stage_columns<VEC, false>(p, base, c0, cols, Xs, ld);
     __syncthreads();
-    // four rows of one column a thread
-    const int q = s4 / 4;
-    for (int e = threadIdx.x; e < q * GRAM_COLS; e += 256) {
-      int rq, c;
-      if (p.u.tall) {
-        c = e / q;
-        rq = e - c * q;
-      } else {
-        rq = e / GRAM_COLS;
-        c = e - rq * GRAM_COLS;
-      }
+    // four rows of one column a thread: columns on the lanes, or rows first in a tall matrix
+    for (int e = threadIdx.x; e < q * cols; e += 256) {
+      const int hi = p.u.tall ? e / q : e / cols;
+      const int c = p.u.tall ? hi : e - hi * cols, rq = p.u.tall ? e - hi * q : hi;
       float o[4] = {};
+      const float* x = Xs + c * ld;
+      const float* y = Qs + 4 * rq;
+#pragma unroll 4
       for (int k = 0; k < p.s; ++k) {
-        const float4 y = *reinterpret_cast<const float4*>(&Qs[k][4 * rq]);
-        const float x = Xs[c][k];
-        o[0] = fmaf(y.x, x, o[0]);
-        o[1] = fmaf(y.y, x, o[1]);
-        o[2] = fmaf(y.z, x, o[2]);
-        o[3] = fmaf(y.w, x, o[3]);
+        const float4 w = *reinterpret_cast<const float4*>(y + k * SMALL_LD);
+        o[0] = fmaf(w.x, x[k], o[0]);
+        o[1] = fmaf(w.y, x[k], o[1]);
+        o[2] = fmaf(w.z, x[k], o[2]);
+        o[3] = fmaf(w.w, x[k], o[3]);
       }
-      if (c0 + c >= p.l) continue;
+      const int64_t step = p.u.tall ? 1 : p.l;
+      const int64_t at0 =
+          base + (p.u.tall ? (int64_t)(c0 + c) * p.s + 4 * rq : (int64_t)4 * rq * p.l + c0 + c);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int r = 4 * rq + i;
-        if (r >= p.s) break;
-        const int64_t at =
-            base + (p.u.tall ? (int64_t)(c0 + c) * p.s + r : (int64_t)r * p.l + c0 + c);
+        if (4 * rq + i >= p.s) break;
+        const int64_t at = at0 + i * step;
         if (p.O) {
           p.O[at] = __float2bfloat16_rn(o[i]);
         } else {
@@ -444,10 +452,16 @@ __global__ void __launch_bounds__(256) apply_kernel(const SmallParams p) {
   }
 }
 
-// chunks of the long side per matrix: enough CTAs for the device, at most 64 partial matrices
-int small_chunks(int64_t batch, int64_t l) {
+// long-side columns staged at a time
+int small_tile(int64_t s) {
+  const int ld = (int)round_up((size_t)s, 4) + 4;
+  return STAGE_FLOATS / ld / 4 * 4;
+}
+
+// chunks of the long side per matrix: two CTAs per SM, at most 64 partial matrices
+int small_chunks(int64_t batch, int64_t s, int64_t l) {
   int64_t want = ceil_div(2 * NUM_SMS, batch);
-  const int64_t most = ceil_div(l, GRAM_COLS);
+  const int64_t most = ceil_div(l, 64);
   if (want > most) want = most;
   if (want > 64) want = 64;
   return (int)want;
@@ -479,8 +493,10 @@ thanos_status_t small_side(const OrthogonalArgs& a, StepParams u, int s, int l, 
   p.Q = Q;
   p.s = s;
   p.l = l;
-  p.chunk_cols = (int)round_up((size_t)ceil_div(l, chunks), GRAM_COLS);
+  p.chunk_cols = (int)round_up((size_t)ceil_div(l, chunks), 4);
   p.chunks = (int)ceil_div(l, p.chunk_cols);
+  p.tile_cols = small_tile(s);
+  p.inv_s = (uint32_t)(((1ull << 32) + s - 1) / s);
   p.steps = a.steps;
   p.a = a.coef[0];
   p.b = a.coef[1];
@@ -491,15 +507,37 @@ thanos_status_t small_side(const OrthogonalArgs& a, StepParams u, int s, int l, 
   p.w_bf16 = a.wdtype == THANOS_BF16;
   p.keep = a.keep;
   p.rate = a.rate;
-  gram_kernel<<<dim3((unsigned)p.chunks, (unsigned)a.batch), 256, 0, stream>>>(p);
+  const bool wide = a.n % 4 == 0;
+  const size_t stage = STAGE_FLOATS * 4, squares = 5 * SMALL_SIDE * SMALL_LD * 4;
+  const dim3 chunks_grid((unsigned)p.chunks, (unsigned)a.batch), one((unsigned)a.batch);
+  if (wide) gram_kernel<4><<<chunks_grid, 256, stage, stream>>>(p);
+  else gram_kernel<1><<<chunks_grid, 256, stage, stream>>>(p);
   THANOS_CHECK_LAUNCH();
-  constexpr int kSmem = 5 * SMALL_SIDE * SMALL_LD * 4;
-  static std::atomic<unsigned long long> done{0};
-  THANOS_CUDA(ensure_max_dyn_smem(steps_kernel, kSmem, done));
-  THANOS_TRY(launch_after(steps_kernel, dim3((unsigned)a.batch), kSmem, p, stream));
-  int64_t blocks = ceil_div(l, GRAM_COLS);
+  static std::atomic<unsigned long long> done1{0}, done2{0}, done4{0}, done_a{0}, done_b{0};
+  if (s <= 16) {
+    THANOS_CUDA(ensure_max_dyn_smem(steps_kernel<1>, (int)squares, done1));
+    THANOS_TRY(launch_after(steps_kernel<1>, one, squares, p, stream));
+  } else if (s <= 32) {
+    THANOS_CUDA(ensure_max_dyn_smem(steps_kernel<2>, (int)squares, done2));
+    THANOS_TRY(launch_after(steps_kernel<2>, one, squares, p, stream));
+  } else {
+    THANOS_CUDA(ensure_max_dyn_smem(steps_kernel<4>, (int)squares, done4));
+    THANOS_TRY(launch_after(steps_kernel<4>, one, squares, p, stream));
+  }
+  // tiles of the apply pass: enough for the device, four to a thread at least
+  int tile = p.tile_cols;
+  while (tile > 64 && ceil_div(l, tile) * a.batch < 2 * NUM_SMS) tile = tile / 2 / 4 * 4;
+  p.tile_cols = tile;
+  int64_t blocks = ceil_div(l, tile);
   if (blocks * a.batch > 4 * NUM_SMS) blocks = ceil_div(4 * NUM_SMS, a.batch);
-  return launch_after(apply_kernel, dim3((unsigned)blocks, (unsigned)a.batch), 0, p, stream);
+  const dim3 grid((unsigned)blocks, (unsigned)a.batch);
+  const size_t apply = stage + SMALL_SIDE * SMALL_LD * 4;
+  if (wide) {
+    THANOS_CUDA(ensure_max_dyn_smem(apply_kernel<4>, (int)apply, done_a));
+    return launch_after(apply_kernel<4>, grid, apply, p, stream);
+  }
+  THANOS_CUDA(ensure_max_dyn_smem(apply_kernel<1>, (int)apply, done_b));
+  return launch_after(apply_kernel<1>, grid, apply, p, stream);
 }
 
 float pow2_at_most(double x, int most) {
@@ -518,7 +556,7 @@ int norm_parts(int64_t mn) {
 size_t orthogonal_workspace_bytes(int64_t batch, int64_t m, int64_t n) {
   const size_t s = (size_t)(m < n ? m : n), l = (size_t)(m < n ? n : m), k = (size_t)batch;
   if (s <= SMALL_SIDE)
-    return 256 + round_up(k * small_chunks(batch > 0 ? batch : 1, l) * s * s * 4, 256) +
+    return 256 + round_up(k * small_chunks(batch > 0 ? batch : 1, s, l) * s * s * 4, 256) +
            round_up(k * s * s * 4, 256);
   return 256 + round_up(k * MAX_PARTS * 8, 256) + 4 * round_up(k * s * round_up(l, 8) * 2, 256) +
          2 * round_up(k * s * round_up(s, 8) * 2, 256);
@@ -545,7 +583,7 @@ thanos_status_t orthogonal_impl(const OrthogonalArgs& a, void* workspace, size_t
   sp.m = (int)a.m;
   sp.n = (int)a.n;
   if (s <= SMALL_SIDE) {
-    const int chunks = small_chunks(a.batch, l);
+    const int chunks = small_chunks(a.batch, s, l);
     float* parts = ar.take<float>(k * chunks * s * s);
     float* Q = ar.take<float>(k * s * s);
     if (!ar.ok()) return THANOS_ERR_WORKSPACE;
