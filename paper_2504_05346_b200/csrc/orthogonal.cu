@@ -46,25 +46,12 @@ __device__ __forceinline__ double block_sum(double v, double* red) {
   return s;
 }
 
-// The iteration's input at one element; `mo` is the new momentum.
-__device__ __forceinline__ float update_of(const StepParams& p, int64_t e, float mo) {
-  if (p.mask && p.mask[e] != 0) return 0.f;
-  if (!p.M_out) return load_any(p.G, p.g_bf16, e);
-  return p.nesterov ? fmaf(p.momentum, mo, load_any(p.G, p.g_bf16, e)) : mo;
-}
-
 template <int VEC>
-__device__ __forceinline__ void load_vec(const void* p, int bf16, int64_t e, float (&v)[VEC]) {
+__device__ __forceinline__ void load_f32(const float* p, float (&v)[VEC]) {
   if constexpr (VEC == 1) {
-    v[0] = load_any(p, bf16, e);
-  } else if (bf16) {
-    const uint2 q = *reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(p) + e);
-    v[0] = __uint_as_float(q.x << 16);
-    v[1] = __uint_as_float(q.x & 0xFFFF0000u);
-    v[2] = __uint_as_float(q.y << 16);
-    v[3] = __uint_as_float(q.y & 0xFFFF0000u);
+    v[0] = *p;
   } else {
-    const float4 q = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + e);
+    const float4 q = *reinterpret_cast<const float4*>(p);
     v[0] = q.x;
     v[1] = q.y;
     v[2] = q.z;
@@ -72,41 +59,91 @@ __device__ __forceinline__ void load_vec(const void* p, int bf16, int64_t e, flo
   }
 }
 
-// VEC consecutive elements of the iteration's input; FIRST reads the old momentum and writes the
-// new one, else the new one is read.
-template <int VEC, bool FIRST>
-__device__ __forceinline__ void update_vec(const StepParams& p, int64_t at, float (&v)[VEC]) {
-  uint32_t gone = 0;
-  if (p.mask) {
-    if constexpr (VEC == 4) {
-      const uint32_t w = *reinterpret_cast<const uint32_t*>(p.mask + at);
+// N vectors of the iteration's input, the first at `at`, the others `step` elements apart; those from
+// `count` on are zero.  FIRST reads the old momentum and writes the new one, else the new one is
+// read.  Every operand is loaded for all N vectors before any is used: which operands there are is
+// asked once, since a branch between two loads keeps them from being in flight together.
+template <int VEC, int N, bool FIRST>
+__device__ __forceinline__ void update_batch(const StepParams& p, int64_t at, int64_t step, int count,
+                                             float (&v)[N][VEC]) {
+  uint32_t gone[N] = {};
+  float mo[N][VEC] = {};
 #pragma unroll
-      for (int e = 0; e < 4; ++e) gone |= ((w >> (8 * e)) & 0xFFu ? 1u : 0u) << e;
+  for (int u = 0; u < N; ++u)
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) v[u][e] = 0.f;
+  if (FIRST || !p.M_out || p.nesterov) {
+    if (p.g_bf16) {
+      const __nv_bfloat16* G = static_cast<const __nv_bfloat16*>(p.G) + at;
+      uint2 q[N] = {};
+#pragma unroll
+      for (int u = 0; u < N; ++u)
+        if (u < count) {
+          if constexpr (VEC == 1) q[u].x = *reinterpret_cast<const unsigned short*>(G + u * step);
+          else q[u] = *reinterpret_cast<const uint2*>(G + u * step);
+        }
+#pragma unroll
+      for (int u = 0; u < N; ++u) {
+        v[u][0] = __uint_as_float(q[u].x << 16);
+        if constexpr (VEC == 4) {
+          v[u][1] = __uint_as_float(q[u].x & 0xFFFF0000u);
+          v[u][2] = __uint_as_float(q[u].y << 16);
+          v[u][3] = __uint_as_float(q[u].y & 0xFFFF0000u);
+        }
+      }
     } else {
-      gone = p.mask[at] != 0;
+      const float* G = static_cast<const float*>(p.G) + at;
+#pragma unroll
+      for (int u = 0; u < N; ++u)
+        if (u < count) load_f32<VEC>(G + u * step, v[u]);
     }
   }
-  float g[VEC];
-  if (FIRST || !p.M_out || p.nesterov) load_vec<VEC>(p.G, p.g_bf16, at, g);
+  if (p.M_out) {
+    const float* M = (FIRST ? p.M_in : p.M_out) + at;
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) {
-    if ((gone >> e) & 1u) g[e] = 0.f;
-    v[e] = g[e];
+    for (int u = 0; u < N; ++u)
+      if (u < count) load_f32<VEC>(M + u * step, mo[u]);
   }
+  if (p.mask) {
+    const uint8_t* k = p.mask + at;
+    uint32_t w[N] = {};
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+      if (u < count) {
+        if constexpr (VEC == 1) w[u] = k[u * step];
+        else w[u] = *reinterpret_cast<const uint32_t*>(k + u * step);
+      }
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) gone[u] |= ((w[u] >> (8 * e)) & 0xFFu ? 1u : 0u) << e;
+  }
+#pragma unroll
+  for (int u = 0; u < N; ++u)
+#pragma unroll
+    for (int e = 0; e < VEC; ++e)
+      if ((gone[u] >> e) & 1u) v[u][e] = 0.f;
   if (!p.M_out) return;
-  float mo[VEC];
   if (FIRST) {
-    load_vec<VEC>(p.M_in, 0, at, mo);
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) mo[e] = fmaf(p.momentum, mo[e], g[e]);
-    if constexpr (VEC == 4) *reinterpret_cast<float4*>(p.M_out + at) = make_float4(mo[0], mo[1], mo[2], mo[3]);
-    else p.M_out[at] = mo[0];
-  } else {
-    load_vec<VEC>(p.M_out, 0, at, mo);
+    for (int u = 0; u < N; ++u) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) mo[u][e] = fmaf(p.momentum, mo[u][e], v[u][e]);
+      if (u < count) {
+        float* M = p.M_out + at + u * step;
+        if constexpr (VEC == 4)
+          *reinterpret_cast<float4*>(M) = make_float4(mo[u][0], mo[u][1], mo[u][2], mo[u][3]);
+        else *M = mo[u][0];
+      }
+    }
   }
 #pragma unroll
-  for (int e = 0; e < VEC; ++e)
-    v[e] = (gone >> e) & 1u ? 0.f : p.nesterov ? fmaf(p.momentum, mo[e], g[e]) : mo[e];
+  for (int u = 0; u < N; ++u)
+#pragma unroll
+    for (int e = 0; e < VEC; ++e)
+      v[u][e] = (gone[u] >> e) & 1u ? 0.f
+                : p.nesterov       ? fmaf(p.momentum, mo[u][e], v[u][e])
+                                   : mo[u][e];
 }
 
 // New momentum and the sums of squares of the iteration's input (fp32 over a thread's share, fp64
@@ -119,16 +156,14 @@ __global__ void __launch_bounds__(256) norm_kernel(const StepParams p) {
   double sum = 0.0;
   const int64_t step = 256ll * VEC * p.parts;
   for (int64_t e0 = ((int64_t)blockIdx.x * 256 + threadIdx.x) * VEC; e0 < mn; e0 += 4 * step) {
+    float v[4][VEC];
+    const int count = e0 + 3 * step < mn ? 4 : (int)((mn - e0 + step - 1) / step);
+    update_batch<VEC, 4, true>(p, base + e0, step, count, v);
     float part = 0.f;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int64_t e = e0 + u * step;
-      if (e >= mn) break;
-      float v[VEC];
-      update_vec<VEC, true>(p, base + e, v);
+    for (int u = 0; u < 4; ++u)
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) part = fmaf(v[i], v[i], part);
-    }
+      for (int i = 0; i < VEC; ++i) part = fmaf(v[u][i], v[u][i], part);
     sum += (double)part;
   }
   sum = block_sum(sum, red);
@@ -155,43 +190,53 @@ __global__ void __launch_bounds__(256) split_kernel(const StepParams p) {
   const int64_t tiles = (int64_t)((p.m + 63) / 64) * tn;
   for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
     const int r0 = (int)(t / tn) * 64, c0 = (int)(t % tn) * 64;
-#pragma unroll 4
-    for (int e = threadIdx.x * VEC; e < 4096; e += 256 * VEC) {
-      const int r = e >> 6, c = e & 63;
-      if (r0 + r >= p.m || c0 + c >= p.n) continue;
-      float x[VEC];
-      update_vec<VEC, false>(p, base + (int64_t)(r0 + r) * p.n + c0 + c, x);
+    // a thread's column, and the rows it takes, 4 VEC apart
+    const int c = (threadIdx.x * VEC) & 63;
+    constexpr int HOP = 4 * VEC;
+#pragma unroll 1
+    for (int r = (threadIdx.x * VEC) >> 6; r < 64; r += 4 * HOP) {
+      const int left = p.m - r0 - r;   // rows from here on
+      const int count = c0 + c >= p.n || left <= 0 ? 0 : min(4, (left + HOP - 1) / HOP);
+      float x[4][VEC];
+      update_batch<VEC, 4, false>(p, base + (int64_t)(r0 + r) * p.n + c0 + c, (int64_t)HOP * p.n,
+                                  count, x);
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) x[i] *= f;
-      if (p.tall) {
+      for (int u = 0; u < 4; ++u) {
+        if (u >= count) break;
+        const int rr = r + u * HOP;
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) tile[c + i][r] = x[i];
-      } else {
-        const int64_t o = (int64_t)blockIdx.y * p.x_batch + (int64_t)(r0 + r) * p.ldx + c0 + c;
-        uint32_t hi[VEC], lo[VEC];
+        for (int i = 0; i < VEC; ++i) x[u][i] *= f;
+        if (p.tall) {
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) split_half(x[i], hi[i], lo[i]);
-        if constexpr (VEC == 4) {
-          *reinterpret_cast<uint2*>(p.Xh + o) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
-          *reinterpret_cast<uint2*>(p.Xl + o) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+          for (int i = 0; i < VEC; ++i) tile[c + i][rr] = x[u][i];
         } else {
-          p.Xh[o] = __ushort_as_half((unsigned short)hi[0]);
-          p.Xl[o] = __ushort_as_half((unsigned short)lo[0]);
+          const int64_t o = (int64_t)blockIdx.y * p.x_batch + (int64_t)(r0 + rr) * p.ldx + c0 + c;
+          uint32_t hi[VEC], lo[VEC];
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) split_half(x[u][i], hi[i], lo[i]);
+          if constexpr (VEC == 4) {
+            *reinterpret_cast<uint2*>(p.Xh + o) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+            *reinterpret_cast<uint2*>(p.Xl + o) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+          } else {
+            p.Xh[o] = __ushort_as_half((unsigned short)hi[0]);
+            p.Xl[o] = __ushort_as_half((unsigned short)lo[0]);
+          }
         }
       }
     }
     if (p.tall) {
       __syncthreads();
-      for (int e = threadIdx.x * 2; e < 4096; e += 512) {
-        const int c = e >> 6, r = e & 63;
+      const int r = (threadIdx.x * 4) & 63;
+#pragma unroll 2
+      for (int c = threadIdx.x >> 4; c < 64; c += 16) {
         if (r0 + r >= p.m || c0 + c >= p.n) continue;
         const int64_t o = (int64_t)blockIdx.y * p.x_batch + (int64_t)(c0 + c) * p.ldx + r0 + r;
-        uint32_t hi[2], lo[2];
-        split_half(tile[c][r], hi[0], lo[0]);
-        split_half(tile[c][r + 1], hi[1], lo[1]);
-        // a last row without a partner fills the padding of the leading dimension
-        *reinterpret_cast<uint32_t*>(p.Xh + o) = hi[0] | hi[1] << 16;
-        *reinterpret_cast<uint32_t*>(p.Xl + o) = lo[0] | lo[1] << 16;
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) split_half(tile[c][r + i], hi[i], lo[i]);
+        // rows beyond the last fill the padding of the leading dimension (a multiple of 8)
+        *reinterpret_cast<uint2*>(p.Xh + o) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+        *reinterpret_cast<uint2*>(p.Xl + o) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
       }
       __syncthreads();
     }
@@ -211,7 +256,7 @@ constexpr int STAGE_FLOATS = 10240;  // a tile of the long side, padded rows: 51
 
 struct SmallParams {
   StepParams u;
-  float* part;       // [batch][chunks][s][s]
+  float* part;       // [batch][chunks][4 x 4 tiles of the Gram matrix]
   float* Q;          // [batch][s][s]
   int s, l, chunks, chunk_cols, tile_cols, steps;
   uint32_t inv_s;    // ceil(2^32 / s) for s > 1: e / s is the high word of e inv_s
@@ -235,23 +280,34 @@ __device__ __forceinline__ void stage_columns(const SmallParams& p, int64_t base
   if (p.u.tall) {
     const int total = cols * p.s;
     const int64_t at0 = base + (int64_t)c0 * p.s;
-#pragma unroll 2
-    for (int e = threadIdx.x * VEC; e < total; e += 256 * VEC) {
-      const int c = over_s(p, e), r = e - c * p.s;
-      float v[VEC];
-      update_vec<VEC, FIRST>(p.u, at0 + e, v);
+#pragma unroll 1
+    for (int e0 = threadIdx.x * VEC; e0 < total; e0 += 1024 * VEC) {
+      float v[4][VEC];
+      const int count = min(4, (total - e0 + 256 * VEC - 1) / (256 * VEC));
+      update_batch<VEC, 4, FIRST>(p.u, at0 + e0, 256 * VEC, count, v);
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) Xs[c * ld + r + i] = v[i];
+      for (int u = 0; u < 4; ++u) {
+        if (u >= count) break;
+        const int e = e0 + u * 256 * VEC, c = over_s(p, e), r = e - c * p.s;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) Xs[c * ld + r + i] = v[u][i];
+      }
     }
   } else {
+#pragma unroll 1
     for (int r = threadIdx.x >> 5; r < p.s; r += 8) {
       const int64_t at0 = base + (int64_t)r * p.l + c0;
-#pragma unroll 4
-      for (int c = (threadIdx.x & 31) * VEC; c < cols; c += 32 * VEC) {
-        float v[VEC];
-        update_vec<VEC, FIRST>(p.u, at0 + c, v);
+#pragma unroll 1
+      for (int c = (threadIdx.x & 31) * VEC; c < cols; c += 128 * VEC) {
+        float v[4][VEC];
+        const int count = min(4, (cols - c + 32 * VEC - 1) / (32 * VEC));
+        update_batch<VEC, 4, FIRST>(p.u, at0 + c, 32 * VEC, count, v);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) Xs[(c + i) * ld + r] = v[i];
+        for (int u = 0; u < 4; ++u) {
+          if (u >= count) break;
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) Xs[(c + u * 32 * VEC + i) * ld + r] = v[u][i];
+        }
       }
     }
   }
@@ -296,13 +352,18 @@ __global__ void __launch_bounds__(256) gram_kernel(const SmallParams p) {
           make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
   }
   __syncthreads();
-  float* out = p.part + ((int64_t)blockIdx.y * p.chunks + blockIdx.x) * p.s * p.s;
-  for (int e = threadIdx.x; e < tiles * 16; e += 256) {
-    float v = 0.f;
-    for (int k = 0; k < groups; ++k) v += Xs[k * tiles * 16 + e];
-    const int tl = e >> 4, tr = tl / q;
-    const int r = 4 * tr + ((e >> 2) & 3), c = 4 * (tl - tr * q) + (e & 3);
-    if (r < p.s && c < p.s) out[r * p.s + c] = v;
+  float4* out = reinterpret_cast<float4*>(
+      p.part + ((int64_t)blockIdx.y * p.chunks + blockIdx.x) * (tiles * 16));
+  for (int e = threadIdx.x; e < tiles * 4; e += 256) {
+    float4 v = reinterpret_cast<const float4*>(Xs)[e];
+    for (int k = 1; k < groups; ++k) {
+      const float4 w = reinterpret_cast<const float4*>(Xs)[k * tiles * 4 + e];
+      v.x += w.x;
+      v.y += w.y;
+      v.z += w.z;
+      v.w += w.w;
+    }
+    out[e] = v;
   }
 }
 
@@ -320,7 +381,7 @@ __device__ __noinline__ void small_product(float* D, const float* A, const float
     const float* x = A + TS * ti;
     const float* y = B + TS * tj;
     float acc[TS][TS] = {};
-#pragma unroll 4
+#pragma unroll 8
     for (int k = 0; k < s; ++k) {
       float xv[TS], yv[TS];
 #pragma unroll
@@ -346,24 +407,47 @@ __device__ __noinline__ void small_product(float* D, const float* A, const float
   __syncthreads();
 }
 
+constexpr int STEP_THREADS = 1024;
+
 template <int TS>
-__global__ void __launch_bounds__(256) steps_kernel(const SmallParams p) {
+__global__ void __launch_bounds__(STEP_THREADS) steps_kernel(const SmallParams p) {
   extern __shared__ __align__(16) float mats[];
   constexpr int SZ = SMALL_SIDE * SMALL_LD;
   float *S = mats, *P = mats + SZ, *Q = mats + 2 * SZ, *T = mats + 3 * SZ, *U = mats + 4 * SZ;
   __shared__ float norm;
   const int s = p.s, ss = s * s;
-  for (int e = threadIdx.x; e < 5 * SZ; e += 256) mats[e] = 0.f;
+  for (int e = threadIdx.x; e < 5 * SZ; e += STEP_THREADS) mats[e] = 0.f;
   __syncthreads();
   grid_dependency_wait();
   grid_dependents_launch();
-  const float* part = p.part + (int64_t)blockIdx.x * p.chunks * ss;
-  for (int e = threadIdx.x; e < ss; e += 256) {
-    float v = 0.f;
+  // the partial matrices, four entries a thread; threads to spare take every groups-th of them
+  const int q = (s + 3) / 4, vecs = q * q * 4;
+  const int groups = STEP_THREADS / vecs;
+  const int g = threadIdx.x / vecs, e = threadIdx.x - g * vecs;
+  const float4* part = reinterpret_cast<const float4*>(p.part) + (int64_t)blockIdx.x * p.chunks * vecs;
+  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (g < groups) {
 #pragma unroll 8
-    for (int k = 0; k < p.chunks; ++k) v += part[k * ss + e];
-    const int r = over_s(p, e);
-    S[r * SMALL_LD + e - r * s] = v;
+    for (int k = g; k < p.chunks; k += groups) {
+      const float4 w = part[(int64_t)k * vecs + e];
+      sum.x += w.x;
+      sum.y += w.y;
+      sum.z += w.z;
+      sum.w += w.w;
+    }
+    reinterpret_cast<float4*>(T)[threadIdx.x] = sum;  // T and U together hold 1024 of them
+  }
+  __syncthreads();
+  if (threadIdx.x < vecs) {
+    for (int k = 1; k < groups; ++k) {
+      const float4 w = reinterpret_cast<const float4*>(T)[k * vecs + e];
+      sum.x += w.x;
+      sum.y += w.y;
+      sum.z += w.z;
+      sum.w += w.w;
+    }
+    const int tl = e >> 2, tr = tl / q;
+    *reinterpret_cast<float4*>(S + (4 * tr + (e & 3)) * SMALL_LD + 4 * (tl - tr * q)) = sum;
   }
   __syncthreads();
   if (threadIdx.x < 32) {
@@ -374,7 +458,7 @@ __global__ void __launch_bounds__(256) steps_kernel(const SmallParams p) {
   }
   __syncthreads();
   const float inv = 1.f / norm;
-  for (int e = threadIdx.x; e < s * SMALL_LD; e += 256) S[e] = S[e] * inv * inv;
+  for (int i = threadIdx.x; i < s * SMALL_LD; i += STEP_THREADS) S[i] = S[i] * inv * inv;
   __syncthreads();
 #pragma unroll 1
   for (int it = 0; it < p.steps; ++it) {
@@ -392,9 +476,9 @@ __global__ void __launch_bounds__(256) steps_kernel(const SmallParams p) {
     }
   }
   float* out = p.Q + (int64_t)blockIdx.x * ss;
-  for (int e = threadIdx.x; e < ss; e += 256) {
-    const int r = over_s(p, e);
-    out[e] = Q[r * SMALL_LD + e - r * s] * inv;
+  for (int i = threadIdx.x; i < ss; i += STEP_THREADS) {
+    const int r = over_s(p, i);
+    out[i] = Q[r * SMALL_LD + i - r * s] * inv;
   }
 }
 
@@ -468,11 +552,11 @@ int small_chunks(int64_t batch, int64_t s, int64_t l) {
 }
 
 template <typename K>
-thanos_status_t launch_after(K kernel, dim3 grid, size_t smem, const SmallParams& p,
+thanos_status_t launch_after(K kernel, dim3 grid, int threads, size_t smem, const SmallParams& p,
                              cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
-  cfg.blockDim = dim3(256, 1, 1);
+  cfg.blockDim = dim3((unsigned)threads, 1, 1);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
@@ -513,16 +597,13 @@ thanos_status_t small_side(const OrthogonalArgs& a, StepParams u, int s, int l, 
   if (wide) gram_kernel<4><<<chunks_grid, 256, stage, stream>>>(p);
   else gram_kernel<1><<<chunks_grid, 256, stage, stream>>>(p);
   THANOS_CHECK_LAUNCH();
-  static std::atomic<unsigned long long> done1{0}, done2{0}, done4{0}, done_a{0}, done_b{0};
-  if (s <= 16) {
+  static std::atomic<unsigned long long> done1{0}, done2{0}, done_a{0}, done_b{0};
+  if (s <= 32) {  // one entry of a product a thread, or four
     THANOS_CUDA(ensure_max_dyn_smem(steps_kernel<1>, (int)squares, done1));
-    THANOS_TRY(launch_after(steps_kernel<1>, one, squares, p, stream));
-  } else if (s <= 32) {
-    THANOS_CUDA(ensure_max_dyn_smem(steps_kernel<2>, (int)squares, done2));
-    THANOS_TRY(launch_after(steps_kernel<2>, one, squares, p, stream));
+    THANOS_TRY(launch_after(steps_kernel<1>, one, STEP_THREADS, squares, p, stream));
   } else {
-    THANOS_CUDA(ensure_max_dyn_smem(steps_kernel<4>, (int)squares, done4));
-    THANOS_TRY(launch_after(steps_kernel<4>, one, squares, p, stream));
+    THANOS_CUDA(ensure_max_dyn_smem(steps_kernel<2>, (int)squares, done2));
+    THANOS_TRY(launch_after(steps_kernel<2>, one, STEP_THREADS, squares, p, stream));
   }
   // tiles of the apply pass: enough for the device, four to a thread at least
   int tile = p.tile_cols;
@@ -534,10 +615,10 @@ thanos_status_t small_side(const OrthogonalArgs& a, StepParams u, int s, int l, 
   const size_t apply = stage + SMALL_SIDE * SMALL_LD * 4;
   if (wide) {
     THANOS_CUDA(ensure_max_dyn_smem(apply_kernel<4>, (int)apply, done_a));
-    return launch_after(apply_kernel<4>, grid, apply, p, stream);
+    return launch_after(apply_kernel<4>, grid, 256, apply, p, stream);
   }
   THANOS_CUDA(ensure_max_dyn_smem(apply_kernel<1>, (int)apply, done_b));
-  return launch_after(apply_kernel<1>, grid, apply, p, stream);
+  return launch_after(apply_kernel<1>, grid, 256, apply, p, stream);
 }
 
 float pow2_at_most(double x, int most) {
@@ -556,7 +637,9 @@ int norm_parts(int64_t mn) {
 size_t orthogonal_workspace_bytes(int64_t batch, int64_t m, int64_t n) {
   const size_t s = (size_t)(m < n ? m : n), l = (size_t)(m < n ? n : m), k = (size_t)batch;
   if (s <= SMALL_SIDE)
-    return 256 + round_up(k * small_chunks(batch > 0 ? batch : 1, s, l) * s * s * 4, 256) +
+    return 256 +
+           round_up(k * small_chunks(batch > 0 ? batch : 1, s, l) * round_up(s, 4) * round_up(s, 4) * 4,
+                    256) +
            round_up(k * s * s * 4, 256);
   return 256 + round_up(k * MAX_PARTS * 8, 256) + 4 * round_up(k * s * round_up(l, 8) * 2, 256) +
          2 * round_up(k * s * round_up(s, 8) * 2, 256);
@@ -584,7 +667,8 @@ thanos_status_t orthogonal_impl(const OrthogonalArgs& a, void* workspace, size_t
   sp.n = (int)a.n;
   if (s <= SMALL_SIDE) {
     const int chunks = small_chunks(a.batch, s, l);
-    float* parts = ar.take<float>(k * chunks * s * s);
+    const size_t s4 = round_up((size_t)s, 4);
+    float* parts = ar.take<float>(k * chunks * s4 * s4);
     float* Q = ar.take<float>(k * s * s);
     if (!ar.ok()) return THANOS_ERR_WORKSPACE;
     return small_side(a, sp, s, l, parts, Q, chunks, stream);
