@@ -243,14 +243,15 @@ __global__ void __launch_bounds__(256) split_kernel(const StepParams p) {
   }
 }
 
-// ------------------------------------------------------------------ a short side of up to 64
+// ------------------------------------------------------------------ a short side of up to 32
 // X_k = Q_k X_0 with Q_k a polynomial in S_0 = X_0 X_0^T, so the matrix is read twice and all steps
 // run on s x s matrices: Q' = P Q, S' = P S P with P = a I + b S + c S S.  In fp32 throughout (a
-// rounding of S_0 is amplified by a^2 per step; 16-bit operands would not do here).
+// rounding of S_0 is amplified by a^2 per step; 16-bit operands would not do here).  The s x s
+// products are a chain on one CTA: beyond 32 that costs more than the wide products do.
 //   gram_kernel   new momentum, partial Gram matrices over chunks of the long side
 //   steps_kernel  one CTA per matrix: sums the partials in order, iterates, Q / (norm + eps)
 //   apply_kernel  Q X_0 over chunks of the long side, into O or the new weights
-constexpr int SMALL_SIDE = 64;
+constexpr int SMALL_SIDE = 32;
 constexpr int SMALL_LD = SMALL_SIDE + 4;
 constexpr int STAGE_FLOATS = 10240;  // a tile of the long side, padded rows: 512 columns of 16 rows
 
@@ -259,7 +260,7 @@ struct SmallParams {
   float* part;       // [batch][chunks][4 x 4 tiles of the Gram matrix]
   float* Q;          // [batch][s][s]
   int s, l, chunks, chunk_cols, tile_cols, steps;
-  uint32_t inv_s;    // ceil(2^32 / s) for s > 1: e / s is the high word of e inv_s
+  uint32_t inv_q;    // ceil(2^32 / q) for q = ceil(s / 4) > 1: e / q is the high word of e inv_q
   float a, b, c;
   __nv_bfloat16* O;
   void* W_out;
@@ -268,47 +269,39 @@ struct SmallParams {
   float keep, rate;
 };
 
-__device__ __forceinline__ int over_s(const SmallParams& p, int e) {
-  return p.s == 1 ? e : (int)__umulhi((uint32_t)e, p.inv_s);
-}
-
-// Stages columns [c0, c0 + cols) of the long side as Xs[column * ld + row]; FIRST also writes the
-// momentum.  Consecutive threads go along the matrix' contiguous axis.
+// Stages columns [c0, c0 + cols) of the long side as Xs[column * ld + row], rows up to the next
+// multiple of four (zeros beyond s); FIRST also writes the momentum.  A thread takes blocks of four
+// rows x VEC columns, turns them in registers and writes whole 16-byte rows; neighbours take the
+// row blocks of a column first, which keeps both the loads and the shared-memory stores wide.
 template <int VEC, bool FIRST>
 __device__ __forceinline__ void stage_columns(const SmallParams& p, int64_t base, int c0, int cols,
                                               float* Xs, int ld) {
-  if (p.u.tall) {
-    const int total = cols * p.s;
-    const int64_t at0 = base + (int64_t)c0 * p.s;
+  const int q = (p.s + 3) / 4;
+  const int blocks = q * (p.u.tall ? cols : (cols + VEC - 1) / VEC);
 #pragma unroll 1
-    for (int e0 = threadIdx.x * VEC; e0 < total; e0 += 1024 * VEC) {
+  for (int it = threadIdx.x; it < blocks; it += 256) {
+    const int cb = q == 1 ? it : (int)__umulhi((uint32_t)it, p.inv_q), r = 4 * (it - cb * q);
+    if (p.u.tall) {     // [l, s]: the four rows of a column are neighbours
+      const int64_t at = base + (int64_t)(c0 + cb) * p.s + r;
+      float4 x;
+      if constexpr (VEC == 4) {
+        float v[1][4];
+        update_batch<4, 1, FIRST>(p.u, at, 0, 1, v);
+        x = make_float4(v[0][0], v[0][1], v[0][2], v[0][3]);
+      } else {
+        float v[4][1];
+        update_batch<1, 4, FIRST>(p.u, at, 1, min(4, p.s - r), v);
+        x = make_float4(v[0][0], v[1][0], v[2][0], v[3][0]);
+      }
+      *reinterpret_cast<float4*>(Xs + cb * ld + r) = x;
+    } else {
+      const int c = cb * VEC;
       float v[4][VEC];
-      const int count = min(4, (total - e0 + 256 * VEC - 1) / (256 * VEC));
-      update_batch<VEC, 4, FIRST>(p.u, at0 + e0, 256 * VEC, count, v);
+      update_batch<VEC, 4, FIRST>(p.u, base + (int64_t)r * p.l + c0 + c, p.l, min(4, p.s - r), v);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        if (u >= count) break;
-        const int e = e0 + u * 256 * VEC, c = over_s(p, e), r = e - c * p.s;
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) Xs[c * ld + r + i] = v[u][i];
-      }
-    }
-  } else {
-#pragma unroll 1
-    for (int r = threadIdx.x >> 5; r < p.s; r += 8) {
-      const int64_t at0 = base + (int64_t)r * p.l + c0;
-#pragma unroll 1
-      for (int c = (threadIdx.x & 31) * VEC; c < cols; c += 128 * VEC) {
-        float v[4][VEC];
-        const int count = min(4, (cols - c + 32 * VEC - 1) / (32 * VEC));
-        update_batch<VEC, 4, FIRST>(p.u, at0 + c, 32 * VEC, count, v);
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          if (u >= count) break;
-#pragma unroll
-          for (int i = 0; i < VEC; ++i) Xs[(c + u * 32 * VEC + i) * ld + r] = v[u][i];
-        }
-      }
+      for (int i = 0; i < VEC; ++i)
+        *reinterpret_cast<float4*>(Xs + (c + i) * ld + r) =
+            make_float4(v[0][i], v[1][i], v[2][i], v[3][i]);
     }
   }
 }
@@ -323,7 +316,6 @@ __global__ void __launch_bounds__(256) gram_kernel(const SmallParams p) {
   const int g = threadIdx.x / tiles, tile = threadIdx.x - g * tiles;
   const int ti = tile / q, tj = tile - ti * q;
   const int c_lo = blockIdx.x * p.chunk_cols, c_hi = min(p.l, c_lo + p.chunk_cols);
-  for (int e = threadIdx.x; e < STAGE_FLOATS; e += 256) Xs[e] = 0.f;  // rows beyond s stay zero
   float acc[4][4] = {};
   for (int c0 = c_lo; c0 < c_hi; c0 += p.tile_cols) {
     const int cols = min(p.tile_cols, c_hi - c0);
@@ -331,7 +323,7 @@ __global__ void __launch_bounds__(256) gram_kernel(const SmallParams p) {
     stage_columns<VEC, true>(p, base, c0, cols, Xs, ld);
     __syncthreads();
     if (g < groups) {
-#pragma unroll 2
+#pragma unroll 4
       for (int c = g; c < cols; c += groups) {
         const float4 x = *reinterpret_cast<const float4*>(Xs + c * ld + 4 * ti);
         const float4 y = *reinterpret_cast<const float4*>(Xs + c * ld + 4 * tj);
@@ -356,6 +348,7 @@ __global__ void __launch_bounds__(256) gram_kernel(const SmallParams p) {
       p.part + ((int64_t)blockIdx.y * p.chunks + blockIdx.x) * (tiles * 16));
   for (int e = threadIdx.x; e < tiles * 4; e += 256) {
     float4 v = reinterpret_cast<const float4*>(Xs)[e];
+#pragma unroll 4
     for (int k = 1; k < groups; ++k) {
       const float4 w = reinterpret_cast<const float4*>(Xs)[k * tiles * 4 + e];
       v.x += w.x;
@@ -384,10 +377,16 @@ __device__ __noinline__ void small_product(float* D, const float* A, const float
 #pragma unroll 8
     for (int k = 0; k < s; ++k) {
       float xv[TS], yv[TS];
-#pragma unroll
-      for (int i = 0; i < TS; ++i) {
-        xv[i] = x[k * SMALL_LD + i];
-        yv[i] = y[k * SMALL_LD + i];
+      if constexpr (TS == 2) {
+        const float2 xx = *reinterpret_cast<const float2*>(x + k * SMALL_LD);
+        const float2 yy = *reinterpret_cast<const float2*>(y + k * SMALL_LD);
+        xv[0] = xx.x;
+        xv[1] = xx.y;
+        yv[0] = yy.x;
+        yv[1] = yy.y;
+      } else {
+        xv[0] = x[k * SMALL_LD];
+        yv[0] = y[k * SMALL_LD];
       }
 #pragma unroll
       for (int i = 0; i < TS; ++i)
@@ -407,7 +406,7 @@ __device__ __noinline__ void small_product(float* D, const float* A, const float
   __syncthreads();
 }
 
-constexpr int STEP_THREADS = 1024;
+constexpr int STEP_THREADS = 256;
 
 template <int TS>
 __global__ void __launch_bounds__(STEP_THREADS) steps_kernel(const SmallParams p) {
@@ -435,7 +434,7 @@ __global__ void __launch_bounds__(STEP_THREADS) steps_kernel(const SmallParams p
       sum.z += w.z;
       sum.w += w.w;
     }
-    reinterpret_cast<float4*>(T)[threadIdx.x] = sum;  // T and U together hold 1024 of them
+    reinterpret_cast<float4*>(T)[threadIdx.x] = sum;  // T holds 288 of them
   }
   __syncthreads();
   if (threadIdx.x < vecs) {
@@ -476,60 +475,92 @@ __global__ void __launch_bounds__(STEP_THREADS) steps_kernel(const SmallParams p
     }
   }
   float* out = p.Q + (int64_t)blockIdx.x * ss;
-  for (int i = threadIdx.x; i < ss; i += STEP_THREADS) {
-    const int r = over_s(p, i);
-    out[i] = Q[r * SMALL_LD + i - r * s] * inv;
-  }
+  for (int r = threadIdx.x >> 5; r < s; r += STEP_THREADS / 32)
+    if ((threadIdx.x & 31) < s) out[r * s + (threadIdx.x & 31)] = Q[r * SMALL_LD + (threadIdx.x & 31)] * inv;
 }
 
 template <int VEC>
 __global__ void __launch_bounds__(256) apply_kernel(const SmallParams p) {
-  extern __shared__ __align__(16) float Xs[];               // odd rows: a lane per column
-  float* Qs = Xs + STAGE_FLOATS;                            // Qs[k][row]
+  extern __shared__ __align__(16) float Xs[];
+  float* Qs = Xs + STAGE_FLOATS;                            // Qs[k][row], zeros beyond s
   const int64_t base = (int64_t)blockIdx.y * p.s * p.l;
-  const int s4 = (p.s + 3) & ~3, ld = s4 + 1, q = s4 / 4;
-  for (int e = threadIdx.x; e < p.s * SMALL_LD; e += 256) Qs[e] = 0.f;
+  const int q = (p.s + 3) / 4, ld = 4 * q + 4;
+  for (int e = threadIdx.x; e < SMALL_SIDE * SMALL_LD; e += 256) Qs[e] = 0.f;
   __syncthreads();
-  grid_dependency_wait();
+  grid_dependency_wait();   // the momentum, too, is an earlier launch's
   const float* Q = p.Q + (int64_t)blockIdx.y * p.s * p.s;
-  for (int e = threadIdx.x; e < p.s * p.s; e += 256) {
-    const int r = over_s(p, e);
-    Qs[(e - r * p.s) * SMALL_LD + r] = Q[e];
-  }
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int r = warp; r < p.s; r += 8)
+    if (lane < p.s) Qs[lane * SMALL_LD + r] = Q[r * p.s + lane];
   for (int c0 = blockIdx.x * p.tile_cols; c0 < p.l; c0 += gridDim.x * p.tile_cols) {
     const int cols = min(p.tile_cols, p.l - c0);
     __syncthreads();
     stage_columns<VEC, false>(p, base, c0, cols, Xs, ld);
     __syncthreads();
-    // four rows of one column a thread: columns on the lanes, or rows first in a tall matrix
-    for (int e = threadIdx.x; e < q * cols; e += 256) {
-      const int hi = p.u.tall ? e / q : e / cols;
-      const int c = p.u.tall ? hi : e - hi * cols, rq = p.u.tall ? e - hi * q : hi;
-      float o[4] = {};
-      const float* x = Xs + c * ld;
-      const float* y = Qs + 4 * rq;
-#pragma unroll 4
-      for (int k = 0; k < p.s; ++k) {
-        const float4 w = *reinterpret_cast<const float4*>(y + k * SMALL_LD);
-        o[0] = fmaf(w.x, x[k], o[0]);
-        o[1] = fmaf(w.y, x[k], o[1]);
-        o[2] = fmaf(w.z, x[k], o[2]);
-        o[3] = fmaf(w.w, x[k], o[3]);
+    // a warp takes four rows of 64 columns, a lane two of the columns
+    const int items = q * ((cols + 63) >> 6);
+#pragma unroll 1
+    for (int it = warp; it < items; it += 8) {
+      const int cb = q == 1 ? it : (int)__umulhi((uint32_t)it, p.inv_q), r = 4 * (it - cb * q);
+      const int c = 64 * cb + lane;
+      float o[2][4] = {};
+#pragma unroll 2
+      for (int k = 0; k < 4 * q; k += 4) {
+        float4 x[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          x[u] = *reinterpret_cast<const float4*>(Xs + min(c + 32 * u, cols - 1) * ld + k);
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+          const float4 w = *reinterpret_cast<const float4*>(Qs + (k + kk) * SMALL_LD + r);
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const float xv = kk == 0 ? x[u].x : kk == 1 ? x[u].y : kk == 2 ? x[u].z : x[u].w;
+            o[u][0] = fmaf(w.x, xv, o[u][0]);
+            o[u][1] = fmaf(w.y, xv, o[u][1]);
+            o[u][2] = fmaf(w.z, xv, o[u][2]);
+            o[u][3] = fmaf(w.w, xv, o[u][3]);
+          }
+        }
       }
       const int64_t step = p.u.tall ? 1 : p.l;
-      const int64_t at0 =
-          base + (p.u.tall ? (int64_t)(c0 + c) * p.s + 4 * rq : (int64_t)4 * rq * p.l + c0 + c);
+      const int nr = min(4, p.s - r);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (4 * rq + i >= p.s) break;
-        const int64_t at = at0 + i * step;
+      for (int u = 0; u < 2; ++u) {
+        const int cc = c + 32 * u;
+        if (cc >= cols) break;
+        const int64_t at =
+            base + (p.u.tall ? (int64_t)(c0 + cc) * p.s + r : (int64_t)r * p.l + c0 + cc);
         if (p.O) {
-          p.O[at] = __float2bfloat16_rn(o[i]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (i < nr) p.O[at + i * step] = __float2bfloat16_rn(o[u][i]);
+          continue;
+        }
+        float w[4] = {};
+        uint32_t gone = 0;
+        if (p.w_bf16) {
+          const __nv_bfloat16* W = static_cast<const __nv_bfloat16*>(p.W_in) + at;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (i < nr) w[i] = __bfloat162float(W[i * step]);
         } else {
-          float w = fmaf(-p.rate, o[i], p.keep * load_any(p.W_in, p.w_bf16, at));
-          if (p.u.mask && p.u.mask[at] != 0) w = 0.f;
-          if (p.w_bf16) static_cast<__nv_bfloat16*>(p.W_out)[at] = __float2bfloat16_rn(w);
-          else static_cast<float*>(p.W_out)[at] = w;
+          const float* W = static_cast<const float*>(p.W_in) + at;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (i < nr) w[i] = W[i * step];
+        }
+        if (p.u.mask) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (i < nr && p.u.mask[at + i * step] != 0) gone |= 1u << i;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (i >= nr) break;
+          const float v = (gone >> i) & 1u ? 0.f : fmaf(-p.rate, o[u][i], p.keep * w[i]);
+          if (p.w_bf16) static_cast<__nv_bfloat16*>(p.W_out)[at + i * step] = __float2bfloat16_rn(v);
+          else static_cast<float*>(p.W_out)[at + i * step] = v;
         }
       }
     }
@@ -542,12 +573,12 @@ int small_tile(int64_t s) {
   return STAGE_FLOATS / ld / 4 * 4;
 }
 
-// chunks of the long side per matrix: two CTAs per SM, at most 64 partial matrices
+// chunks of the long side per matrix: two CTAs per SM, at most 32 partial matrices
 int small_chunks(int64_t batch, int64_t s, int64_t l) {
   int64_t want = ceil_div(2 * NUM_SMS, batch);
   const int64_t most = ceil_div(l, 64);
   if (want > most) want = most;
-  if (want > 64) want = 64;
+  if (want > 32) want = 32;
   return (int)want;
 }
 
@@ -580,7 +611,8 @@ thanos_status_t small_side(const OrthogonalArgs& a, StepParams u, int s, int l, 
   p.chunk_cols = (int)round_up((size_t)ceil_div(l, chunks), 4);
   p.chunks = (int)ceil_div(l, p.chunk_cols);
   p.tile_cols = small_tile(s);
-  p.inv_s = (uint32_t)(((1ull << 32) + s - 1) / s);
+  const int q = (s + 3) / 4;
+  p.inv_q = (uint32_t)(((1ull << 32) + q - 1) / q);
   p.steps = a.steps;
   p.a = a.coef[0];
   p.b = a.coef[1];
@@ -598,7 +630,7 @@ thanos_status_t small_side(const OrthogonalArgs& a, StepParams u, int s, int l, 
   else gram_kernel<1><<<chunks_grid, 256, stage, stream>>>(p);
   THANOS_CHECK_LAUNCH();
   static std::atomic<unsigned long long> done1{0}, done2{0}, done_a{0}, done_b{0};
-  if (s <= 32) {  // one entry of a product a thread, or four
+  if (s <= 16) {  // one entry of a product a thread, or four
     THANOS_CUDA(ensure_max_dyn_smem(steps_kernel<1>, (int)squares, done1));
     THANOS_TRY(launch_after(steps_kernel<1>, one, STEP_THREADS, squares, p, stream));
   } else {
@@ -607,7 +639,7 @@ thanos_status_t small_side(const OrthogonalArgs& a, StepParams u, int s, int l, 
   }
   // tiles of the apply pass: enough for the device, four to a thread at least
   int tile = p.tile_cols;
-  while (tile > 64 && ceil_div(l, tile) * a.batch < 2 * NUM_SMS) tile = tile / 2 / 4 * 4;
+  while (tile > 128 && ceil_div(l, tile) * a.batch < 2 * NUM_SMS) tile = tile / 2 / 4 * 4;
   p.tile_cols = tile;
   int64_t blocks = ceil_div(l, tile);
   if (blocks * a.batch > 4 * NUM_SMS) blocks = ceil_div(4 * NUM_SMS, a.batch);
