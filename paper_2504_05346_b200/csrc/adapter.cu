@@ -23,6 +23,7 @@ using bf16 = __nv_bfloat16;
 //   [0, n_list)          the distinct adapters of a token tile, by first occurrence
 //   next n_copy          16-byte aligned copies: rows of dY, or the adapters' B with padded ranks
 //   next n_turn          B_i [c, r] -> [r, c] (the skinny product's operand in the backward pass)
+//   next n_planes        backward: V as two bf16 planes for dB, and the zeros beyond the rank of U's
 //   the rest             V of a few tokens, a CTA per token and four ranks
 struct FrontParams {
   int32_t* status;             // cleared here unless the sort did (then null)
@@ -38,6 +39,10 @@ struct FrontParams {
   bf16* turn_dst;
   int64_t turn_ld;
   int c, r, n_turn;
+  const float* Vin;
+  bf16* v_planes;
+  bf16* u_planes;
+  int n_planes;
   const bf16* X;
   int64_t ldx;
   const bf16* A;
@@ -127,6 +132,21 @@ __global__ void __launch_bounds__(256) front_kernel(const FrontParams p) {
     return;
   }
   blk -= p.n_turn;
+  if (blk < p.n_planes) {
+    const int r16 = (p.r + 15) & ~15, lane = tid & 31;
+    for (int64_t t = (int64_t)blk * 8 + (tid >> 5); t < p.T; t += 8ll * p.n_planes) {
+      for (int j = lane; j < r16; j += 32) {
+        bf16* v = p.v_planes + t * 2 * r16 + j;
+        split2(j < p.r ? p.Vin[t * p.r + j] : 0.f, v[0], v[r16]);
+        if (j >= p.r) {
+          bf16* u = p.u_planes + t * 2 * r16 + j;
+          u[0] = u[r16] = __float2bfloat16_rn(0.f);
+        }
+      }
+    }
+    return;
+  }
+  blk -= p.n_planes;
   // V[t, j0 .. j0 + 3]: the warps take k in turns of 256, eight elements a lane
   const int groups = (p.r + SHRINK_RANKS - 1) / SHRINK_RANKS;
   const int t = blk / groups, j0 = (blk - t * groups) * SHRINK_RANKS;
@@ -159,7 +179,7 @@ __global__ void __launch_bounds__(256) front_kernel(const FrontParams p) {
 
 thanos_status_t launch_front(const FrontParams& p, int64_t shrink_blocks, bool beside_sort,
                              cudaStream_t stream) {
-  const int64_t blocks = (int64_t)p.n_list + p.n_copy + p.n_turn + shrink_blocks;
+  const int64_t blocks = (int64_t)p.n_list + p.n_copy + p.n_turn + p.n_planes + shrink_blocks;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)blocks, 1, 1);
   cfg.blockDim = dim3(256, 1, 1);
@@ -186,6 +206,8 @@ struct Layout {
   int32_t* list;
   bf16* copy;        // padded B (forward) or dY (backward)
   bf16* turned;      // backward: B_i transposed
+  bf16* v_planes;    // backward: V and U as two bf16 planes
+  bf16* u_planes;
   int32_t* order;    // backward: tokens by adapter
   int32_t* spare;
   int32_t* off;
@@ -205,6 +227,8 @@ bool carve(Arena& ar, Layout& L, bool backward, int64_t T, int64_t c, int64_t b,
   if (backward && copy_dy) L.copy = ar.take<bf16>((size_t)T * round_up(c, 8));
   if (backward) {
     L.turned = ar.take<bf16>((size_t)n * r * round_up(c, 8));
+    L.v_planes = ar.take<bf16>((size_t)T * 2 * round_up(r, 16));
+    L.u_planes = ar.take<bf16>((size_t)T * 2 * round_up(r, 16));
     L.order = ar.take<int32_t>((size_t)T);
     L.spare = ar.take<int32_t>((size_t)T);
     L.off = ar.take<int32_t>((size_t)n + 1);
@@ -342,8 +366,13 @@ thanos_status_t backward16(const AdapterArgs& a, void* workspace, size_t ws_byte
   if (sorts) {
     THANOS_TRY(sort_tokens(a.index, a.T, a.n, L.order, L.spare, L.off, L.status, stream));
     f.status = nullptr;
+    f.Vin = a.Vin;
+    f.v_planes = L.v_planes;
+    f.u_planes = L.u_planes;
+    const int64_t want = ceil_div(a.T, 8);
+    f.n_planes = (int)(want < 2 * NUM_SMS ? want : 2 * NUM_SMS);
   }
-  if (f.n_list + f.n_copy + f.n_turn > 0) THANOS_TRY(launch_front(f, 0, sorts, stream));
+  if (f.n_list + f.n_copy + f.n_turn + f.n_planes > 0) THANOS_TRY(launch_front(f, 0, sorts, stream));
   else THANOS_CUDA(cudaMemsetAsync(L.status, 0, 16, stream));
   if (a.n > 0) {
     g.V = L.R;
@@ -359,6 +388,7 @@ thanos_status_t backward16(const AdapterArgs& a, void* workspace, size_t ws_byte
     s.lda = c8;
     s.M = (int)(a.n * a.r);
     s.scale = a.scale;
+    s.planes = sorts ? L.u_planes : nullptr;
     THANOS_TRY(proj_gemm(s, stream));
     g.P = a.A;
     g.ldp = a.b;
@@ -370,12 +400,12 @@ thanos_status_t backward16(const AdapterArgs& a, void* workspace, size_t ws_byte
     AdapterGradSide sa, sb;
     sa.Z = static_cast<const bf16*>(a.X);
     sa.ldz = a.ldx;
-    sa.R = L.R;
+    sa.R = L.u_planes;
     sa.out = a.dA;
     sa.F = (int)a.b;
     sb.Z = static_cast<const bf16*>(dY);
     sb.ldz = lddy;
-    sb.R = a.Vin;
+    sb.R = L.v_planes;
     sb.scale = a.scale;
     sb.out = a.dB;
     sb.F = (int)a.c;
@@ -398,7 +428,8 @@ size_t adapter_workspace_bytes(bool backward, int64_t T, int64_t c, int64_t b, i
   // room for a copy of dY whose rows are not 16-byte aligned
   if (backward)
     need += round_up((size_t)T * c8 * 2, 256) + round_up((size_t)n * r * c8 * 2, 256) +
-            2 * round_up((size_t)T * 4, 256) + round_up(((size_t)n + 1) * 4, 256);
+            2 * round_up((size_t)T * 2 * round_up(r, 16) * 2, 256) + 2 * round_up((size_t)T * 4, 256) +
+            round_up(((size_t)n + 1) * 4, 256);
   return need;
 }
 

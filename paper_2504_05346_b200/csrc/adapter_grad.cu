@@ -4,10 +4,10 @@
 // bound (r up to 128: at most 256 flops per 2 bytes, below the tensor cores' balance of about 500).
 // A CTA owns one adapter and 128 features; tokens come in the order of sort_tokens, so a tile never
 // mixes adapters (nothing that is not finite crosses from one to another) and needs no mask.
-//   warps 0..3   gather 64 tokens per stage: rows of Z by cp.async into the MN-major layout of the
-//                tensor cores (64 features x 64 tokens, 128-byte swizzle); the fp32 rows of R are
-//                split into two bf16 planes hi + lo (16 significant bits, so that the result keeps
-//                fp32 quality with exact 16-bit products) side by side in n: [hi | lo]
+//   warps 0..3   gather 64 tokens per stage by cp.async, in the MN-major layouts of the tensor cores:
+//                rows of Z (64 features x 64 tokens, 128-byte swizzle) and of R, which comes as two
+//                bf16 planes hi + lo side by side in n (16 significant bits, so that the result keeps
+//                fp32 quality with exact 16-bit products)
 //   warp 4       tcgen05.mma issuer, 128 x 2 r x 16
 //   warps 4..7   epilogue: hi + lo columns added, written (or added) to the gradient
 // A cluster of up to eight CTAs splits the adapter's tokens when there are few tiles; the partial
@@ -246,37 +246,13 @@ __global__ void __launch_bounds__(G_THREADS) grad_tc_kernel(const GradParams p) 
             cp_async16(dst + ((c ^ (row & 7)) << 4), bytes ? z + f : sd.Z, bytes);
           }
         }
+        // R's row [hi | lo], every second 16-byte group by this thread, into boxes of 32 n x 64 k: 64
+        // bytes per k row, 64-byte swizzle
+        const __nv_bfloat16* R = sd.R + t * N;
+        for (int g8 = sub; g8 < N / 8; g8 += 2)
+          cp_async16(st + GA_BYTES + (g8 >> 2) * 4096 + row * 64 + (((g8 & 3) ^ ((row >> 1) & 3)) << 4),
+                     R + 8 * g8, live ? 16u : 0u);
         asm volatile("cp.async.commit_group;" ::: "memory");
-        // hi and lo planes of R's row; this thread takes half of the 8-wide groups
-        const float* R = sd.R + t * r;
-        for (int g8 = sub; g8 < r16 / 8; g8 += 2) {
-          uint32_t hi[4], lw[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            uint32_t h2[2], l2[2];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              const int j = 8 * g8 + 2 * e + u;
-              const float x = live && j < r ? R[j] : 0.f;
-              const __nv_bfloat16 h = __float2bfloat16_rn(x);
-              h2[u] = __bfloat16_as_ushort(h);
-              // an infinity has no second plane (inf - inf)
-              const float hf = __bfloat162float(h);
-              l2[u] = __bfloat16_as_ushort(__float2bfloat16_rn(isfinite(hf) ? x - hf : 0.f));
-            }
-            hi[e] = h2[0] | h2[1] << 16;
-            lw[e] = l2[0] | l2[1] << 16;
-          }
-          unsigned char* B = smem + (size_t)s * stage_bytes + GA_BYTES;
-          auto put = [&](int nn, const uint32_t(&w)[4]) {
-            // boxes of 32 n x 64 k, 64 bytes per k row, 64-byte swizzle
-            unsigned char* q = B + (nn >> 5) * 4096 + row * 64 +
-                               ((((nn & 31) >> 3) ^ ((row >> 1) & 3)) << 4);
-            *reinterpret_cast<uint4*>(q) = make_uint4(w[0], w[1], w[2], w[3]);
-          };
-          put(8 * g8, hi);
-          put(r16 + 8 * g8, lw);
-        }
         if (++pending > lag) {
           if (lag == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
           else asm volatile("cp.async.wait_group 1;" ::: "memory");

@@ -13,6 +13,7 @@
 // Every wait is bounded (see tc_common.cuh); on expiry the status word gets THANOS_ERR_TIMEOUT.
 #include "proj_gemm.cuh"
 
+#include "adapter_grad.cuh"
 #include "tc_common.cuh"
 
 namespace thanos {
@@ -36,6 +37,7 @@ struct Params {
   void* out;
   int64_t ldo;
   float* V;
+  __nv_bfloat16* planes;
   const int32_t* index;
   const float* scale;
   int n_adapters, r, chunks;          // chunks of 16 per adapter
@@ -259,8 +261,15 @@ __device__ __forceinline__ void emit(const Params& p, int z, int m, int n0, floa
       const int t = n0 + e;
       if (e >= nc) break;
       const int own = valid_adapter(p, t);
-      if (own == i) p.V[(int64_t)t * p.r + j] = p.scale ? p.scale[i] * v[e] : v[e];
-      else if (own < 0 && i == 0) p.V[(int64_t)t * p.r + j] = 0.f;
+      if (own == i) {
+        const float x = p.scale ? p.scale[i] * v[e] : v[e];
+        p.V[(int64_t)t * p.r + j] = x;
+        if (p.planes) {
+          const int r16 = 16 * p.chunks;
+          __nv_bfloat16* row = p.planes + (int64_t)t * 2 * r16 + j;
+          split2(x, row[0], row[r16]);
+        }
+      } else if (own < 0 && i == 0) p.V[(int64_t)t * p.r + j] = 0.f;
     }
   } else if constexpr (EPI == PROJ_GRAM || EPI == PROJ_POLY) {
     __half* D = (EPI == PROJ_GRAM ? p.S : p.Pm) + (int64_t)z * p.s_batch;
@@ -1409,6 +1418,7 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
   p.out = a.out;
   p.ldo = a.ldo;
   p.V = a.V;
+  p.planes = a.planes;
   p.index = a.index;
   p.scale = a.scale;
   p.n_adapters = a.n_adapters;
