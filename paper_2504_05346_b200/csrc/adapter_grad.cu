@@ -227,12 +227,15 @@ __global__ void __launch_bounds__(G_THREADS) grad_tc_kernel(const GradParams p) 
       const int row = threadIdx.x >> 1, sub = threadIdx.x & 1;
       const int lag = p.stages > 2 ? 2 : 1;
       int pending = 0;
+      // the token of the next stage is looked up while this one's copies are issued
+      int t_next = ks0 * GK + row < len ? p.order[lo + ks0 * GK + row] : 0;
       for (int ks = ks0; ks < ks1 && ok; ++ks) {
-        ok = mbar_wait(empty_bar(s), phase ^ 1u, abort_flag);
-        if (!ok) break;
         const int at = ks * GK + row;
         const bool live = at < len;
-        const int64_t t = live ? p.order[lo + at] : 0;
+        const int64_t t = t_next;
+        t_next = at + GK < len ? p.order[lo + at + GK] : 0;
+        ok = mbar_wait(empty_bar(s), phase ^ 1u, abort_flag);
+        if (!ok) break;
         const uint32_t st = smem_base + (uint32_t)s * stage_bytes;
         {
           const int fb = f0 + 64 * sub;
@@ -401,10 +404,18 @@ thanos_status_t adapter_grads(const AdapterGradSide& a, const AdapterGradSide& b
   if (p.stages > G_MAX_STAGES) p.stages = G_MAX_STAGES;
   p.ring_bytes = p.stages * stage_bytes;
   if (p.ring_bytes < p.r16 * GF * 4) p.ring_bytes = p.r16 * GF * 4;
-  // token slices: fill two CTAs per SM, but leave a slice some hundred tokens
-  const int64_t units = (int64_t)p.tiles * n;
+  // Token slices: the number whose rounds over two CTAs per SM leave the least idle, as long as a
+  // slice keeps some hundred tokens.
+  const int64_t units = (int64_t)p.tiles * n, slots = 2 * sm_count();
   p.splits = 1;
-  while (p.splits < 8 && units * p.splits < 2 * sm_count() && T >= n * p.splits * 512) p.splits *= 2;
+  double best = (double)ceil_div(units, slots);
+  for (int k = 2; k <= 8 && T >= n * k * 256; ++k) {
+    const double rounds = (double)ceil_div(units * k, slots) / k;
+    if (rounds < best - 1e-9) {
+      best = rounds;
+      p.splits = k;
+    }
+  }
   const size_t smem = (size_t)p.ring_bytes + 1024 + 256;
   {
     static std::atomic<unsigned long long> done{0};
