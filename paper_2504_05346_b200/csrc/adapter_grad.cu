@@ -224,37 +224,49 @@ __global__ void __launch_bounds__(G_THREADS) grad_tc_kernel(const GradParams p) 
 
     if (warp < 4) {
       // ---------------------------------------------------------- gather
-      const int row = threadIdx.x >> 1, sub = threadIdx.x & 1;
+      // eight lanes a row, so that a copy instruction of a warp covers four whole lines; a thread
+      // takes rows r8 + 16 i and, in them, every eighth 16-byte piece
+      const int r8 = threadIdx.x >> 3, piece = threadIdx.x & 7;
       const int lag = p.stages > 2 ? 2 : 1;
       int pending = 0;
-      // the token of the next stage is looked up while this one's copies are issued
-      int t_next = ks0 * GK + row < len ? p.order[lo + ks0 * GK + row] : 0;
+      // the tokens of the next stage are looked up while this one's copies are issued
+      int next[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int at = ks0 * GK + r8 + 16 * i;
+        next[i] = at < len ? p.order[lo + at] : -1;
+      }
       for (int ks = ks0; ks < ks1 && ok; ++ks) {
-        const int at = ks * GK + row;
-        const bool live = at < len;
-        const int64_t t = t_next;
-        t_next = at + GK < len ? p.order[lo + at + GK] : 0;
+        int tok[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          tok[i] = next[i];
+          const int at = (ks + 1) * GK + r8 + 16 * i;
+          next[i] = at < len ? p.order[lo + at] : -1;
+        }
         ok = mbar_wait(empty_bar(s), phase ^ 1u, abort_flag);
         if (!ok) break;
         const uint32_t st = smem_base + (uint32_t)s * stage_bytes;
-        {
-          const int fb = f0 + 64 * sub;
-          const __nv_bfloat16* z = sd.Z + t * sd.ldz;
-          const uint32_t dst = st + sub * (GA_BYTES / 2) + row * 128;
 #pragma unroll
-          for (int c = 0; c < 8; ++c) {
-            const int f = fb + 8 * c;
-            const int left = live ? (F - f) * 2 : 0;
+        for (int i = 0; i < 4; ++i) {
+          const int row = r8 + 16 * i;
+          const int64_t t = tok[i] < 0 ? 0 : tok[i];
+          const __nv_bfloat16* z = sd.Z + t * sd.ldz;
+#pragma unroll
+          for (int box = 0; box < 2; ++box) {
+            const int f = f0 + 64 * box + 8 * piece;
+            const int left = tok[i] < 0 ? 0 : (F - f) * 2;
             const uint32_t bytes = left <= 0 ? 0u : left < 16 ? (uint32_t)left : 16u;
-            cp_async16(dst + ((c ^ (row & 7)) << 4), bytes ? z + f : sd.Z, bytes);
+            cp_async16(st + box * (GA_BYTES / 2) + row * 128 + ((piece ^ (row & 7)) << 4),
+                       bytes ? z + f : sd.Z, bytes);
           }
+          // R's row [hi | lo] into boxes of 32 n x 64 k: 64 bytes per k row, 64-byte swizzle
+          const __nv_bfloat16* R = sd.R + t * N;
+          for (int g8 = piece; g8 < N / 8; g8 += 8)
+            cp_async16(st + GA_BYTES + (g8 >> 2) * 4096 + row * 64 +
+                           (((g8 & 3) ^ ((row >> 1) & 3)) << 4),
+                       R + 8 * g8, tok[i] < 0 ? 0u : 16u);
         }
-        // R's row [hi | lo], every second 16-byte group by this thread, into boxes of 32 n x 64 k: 64
-        // bytes per k row, 64-byte swizzle
-        const __nv_bfloat16* R = sd.R + t * N;
-        for (int g8 = sub; g8 < N / 8; g8 += 2)
-          cp_async16(st + GA_BYTES + (g8 >> 2) * 4096 + row * 64 + (((g8 & 3) ^ ((row >> 1) & 3)) << 4),
-                     R + 8 * g8, live ? 16u : 0u);
         asm volatile("cp.async.commit_group;" ::: "memory");
         if (++pending > lag) {
           if (lag == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
