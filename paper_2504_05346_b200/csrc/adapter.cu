@@ -26,7 +26,7 @@ using bf16 = __nv_bfloat16;
 //   next n_planes        backward: V as two bf16 planes for dB, and the zeros beyond the rank of U's
 //   the rest             V of a few tokens, a CTA per token and four ranks
 struct FrontParams {
-  int32_t* status;             // cleared here unless the sort did (then null)
+  int32_t* status;             // cleared here
   const int32_t* index;
   int32_t* count;
   int32_t* list;
@@ -64,14 +64,10 @@ __device__ __forceinline__ float dot8(const uint4& a, const uint4& b, float s) {
 
 __global__ void __launch_bounds__(256) front_kernel(const FrontParams p) {
   __shared__ float sh[64 * 65];
-  // Launched plainly, or beside the sort of the tokens, which this does not depend on and which
-  // was itself launched plainly: what came before in the stream is done.  Block 0 waits for the sort
-  // so that whoever waits for this launch finds it finished too.
   grid_dependents_launch();
   const int tid = threadIdx.x;
   int blk = blockIdx.x;
-  if (blk == 0) grid_dependency_wait();
-  if (blk == 0 && tid == 0 && p.status) *p.status = 0;
+  if (blk == 0 && tid == 0) *p.status = 0;
   if (blk < p.n_list) {
     int* ids = reinterpret_cast<int*>(sh);
     int* base = ids + 256;
@@ -177,20 +173,12 @@ __global__ void __launch_bounds__(256) front_kernel(const FrontParams p) {
   }
 }
 
-thanos_status_t launch_front(const FrontParams& p, int64_t shrink_blocks, bool beside_sort,
-                             cudaStream_t stream) {
+thanos_status_t launch_front(const FrontParams& p, int64_t shrink_blocks, cudaStream_t stream) {
   const int64_t blocks = (int64_t)p.n_list + p.n_copy + p.n_turn + p.n_planes + shrink_blocks;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)blocks, 1, 1);
   cfg.blockDim = dim3(256, 1, 1);
   cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  if (beside_sort) {
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-  }
   count_launch();
   THANOS_CUDA(cudaLaunchKernelEx(&cfg, front_kernel, p));
   return THANOS_OK;
@@ -288,7 +276,7 @@ thanos_status_t forward16(const AdapterArgs& a, void* workspace, size_t ws_bytes
     f.b = (int)a.b;
     shrink = a.T * ceil_div(a.r, SHRINK_RANKS);
   }
-  if (f.n_list + f.n_copy + shrink > 0) THANOS_TRY(launch_front(f, shrink, false, stream));
+  if (f.n_list + f.n_copy + shrink > 0) THANOS_TRY(launch_front(f, shrink, stream));
   else THANOS_CUDA(cudaMemsetAsync(L.status, 0, 16, stream));
   g.V = V;
   g.index = a.index;
@@ -364,15 +352,13 @@ thanos_status_t backward16(const AdapterArgs& a, void* workspace, size_t ws_byte
   }
   const bool sorts = a.dA != nullptr;
   if (sorts) {
-    THANOS_TRY(sort_tokens(a.index, a.T, a.n, L.order, L.spare, L.off, L.status, stream));
-    f.status = nullptr;
     f.Vin = a.Vin;
     f.v_planes = L.v_planes;
     f.u_planes = L.u_planes;
     const int64_t want = ceil_div(a.T, 8);
     f.n_planes = (int)(want < 2 * NUM_SMS ? want : 2 * NUM_SMS);
   }
-  if (f.n_list + f.n_copy + f.n_turn + f.n_planes > 0) THANOS_TRY(launch_front(f, 0, sorts, stream));
+  if (f.n_list + f.n_copy + f.n_turn + f.n_planes > 0) THANOS_TRY(launch_front(f, 0, stream));
   else THANOS_CUDA(cudaMemsetAsync(L.status, 0, 16, stream));
   if (a.n > 0) {
     g.V = L.R;
@@ -390,6 +376,8 @@ thanos_status_t backward16(const AdapterArgs& a, void* workspace, size_t ws_byte
     s.scale = a.scale;
     s.planes = sorts ? L.u_planes : nullptr;
     THANOS_TRY(proj_gemm(s, stream));
+    if (sorts)
+      THANOS_TRY(sort_tokens(a.index, a.T, a.n, L.order, L.spare, L.off, L.status, stream));
     g.P = a.A;
     g.ldp = a.b;
     g.p_adapter = (int64_t)a.r * a.b;

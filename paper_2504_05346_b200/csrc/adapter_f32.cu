@@ -33,7 +33,7 @@ struct SplitJob {
 
 struct Front32Params {
   SplitJob in, w;
-  int32_t* status;       // cleared here unless the sort did (then null)
+  int32_t* status;       // cleared here
   float* R;              // [T, r]
   const float* P;        // forward: A [n, r, K]; backward: B [n, K, r]
   const int32_t* index;
@@ -77,7 +77,8 @@ __device__ void split_job(const SplitJob& s, int blk) {
 constexpr int RANKS = 8;
 
 __global__ void __launch_bounds__(256) front_f32_kernel(const Front32Params p) {
-  if (blockIdx.x == 0 && threadIdx.x == 0 && p.status) *p.status = 0;
+  grid_dependents_launch();
+  if (blockIdx.x == 0 && threadIdx.x == 0) *p.status = 0;
   int blk = blockIdx.x;
   if (blk < p.in.blocks) {
     split_job(p.in, blk);
@@ -242,10 +243,6 @@ thanos_status_t adapter_f32(bool back, const AdapterArgs& a, void* workspace, si
   float* R = !back && a.V ? a.V : L.R;
   Front32Params f = {};
   f.status = L.status;
-  if (a.dA) {
-    THANOS_TRY(sort_tokens(a.index, a.T, a.n, L.order, L.spare, L.off, L.status, stream));
-    f.status = nullptr;
-  }
   f.in.src = static_cast<const float*>(a.in);
   f.in.ld = a.ldi;
   if (a.out) {
@@ -279,7 +276,8 @@ thanos_status_t adapter_f32(bool back, const AdapterArgs& a, void* workspace, si
   if (blocks > 0) {
     front_f32_kernel<<<(unsigned)blocks, 256, 0, stream>>>(f);
     THANOS_CHECK_LAUNCH();
-  } else if (f.status) {
+    if (a.dA) THANOS_TRY(sort_tokens(a.index, a.T, a.n, L.order, L.spare, L.off, L.status, stream));
+  } else {
     THANOS_CUDA(cudaMemsetAsync(L.status, 0, 16, stream));
   }
   if (a.out) {

@@ -6,7 +6,8 @@
 namespace thanos {
 
 // Tokens by adapter: order[off[i] .. off[i + 1]) are the tokens of adapter i in ascending order.
-// One CTA; also clears the call's status word and reports an index that names no adapter.
+// One CTA, which runs beside the launch before it in the stream (it reads nothing but index, which has
+// to be there when that launch starts); also reports an index that names no adapter.
 thanos_status_t sort_tokens(const int32_t* index, int64_t T, int64_t n, int32_t* order,
                             int32_t* spare, int32_t* off, int32_t* status, cudaStream_t stream);
 
