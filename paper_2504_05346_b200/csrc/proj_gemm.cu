@@ -1365,15 +1365,18 @@ bool use_pairs(int64_t M, int64_t N, int64_t batch, bool symmetric) {
 }  // namespace
 
 namespace {
-// Width of tile_kernel's tiles: the widest of 128, 64, 32 whose tiles occupy most of the device,
-// no wider than the next step above N.
-int tile_width(int64_t M, int64_t N, int64_t batch, bool symmetric, bool two_per_sm) {
+// Width of tile_kernel's tiles: the widest of 128, 64, 32 whose tiles occupy most of the device, no
+// wider than the next step above N.  Up to 64 tokens of a projection stay in one tile, so that the
+// weights are read once.  The skinny product has few rows and a long k, which is split first.
+int tile_width(int64_t M, int64_t N, int64_t batch, bool symmetric, int epi) {
+  int64_t want = (int64_t)sm_count() * 3 / 4;
+  if (epi == PROJ_OUT) want *= 2;           // two CTAs per SM
+  if (epi == PROJ_SHRINK) want = sm_count() / 10;
   int nt = 128;
-  const int64_t want = (two_per_sm ? 2 : 1) * (int64_t)sm_count() * 3 / 4;
   while (nt > 32) {
     int64_t tiles = ceil_div(M, TM) * ceil_div(N, nt) * batch;
     if (symmetric) tiles /= 2;
-    if (N > nt / 2 && (tiles >= want || N <= 64)) break;
+    if (N > nt / 2 && (tiles >= want || (epi == PROJ_OUT && N <= 64))) break;
     nt /= 2;
   }
   return nt;
@@ -1392,7 +1395,7 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
   p.N = a.N;
   p.K = a.K;
   const bool pairs = a.epi != PROJ_SHRINK && !a.f32 && use_pairs(a.M, a.N, a.batch, symmetric);
-  p.nt = pairs ? PTM : tile_width(a.M, a.N, a.batch, symmetric, a.epi <= PROJ_SHRINK);
+  p.nt = pairs ? PTM : tile_width(a.M, a.N, a.batch, symmetric, a.epi);
   p.tiles_m = (a.M + (pairs ? PTM : TM) - 1) / (pairs ? PTM : TM);
   p.tiles_n = (a.N + p.nt - 1) / p.nt;
   p.batch_z = a.batch;
