@@ -366,16 +366,17 @@ __global__ void __launch_bounds__(256) gram_kernel(const SmallParams p) {
 // place is wrong by 1e-2 and more on matrices of low rank.  TS x TS outputs a thread; one copy of the
 // code for all the products of a step, which run one after another on one CTA.
 template <int TS>
-__device__ __noinline__ void small_product(float* D, const float* A, const float* B, int s, bool add,
-                                           float a, float b, float c) {
+__device__ __noinline__ void small_product(int D_at, int A_at, int B_at, int s, bool add, float a,
+                                           float b, float c) {
+  extern __shared__ __align__(16) float mats[];
   const int q = (s + TS - 1) / TS;
-  if (threadIdx.x < q * q) {
-    const int ti = threadIdx.x / q, tj = threadIdx.x - ti * q;
-    const float* x = A + TS * ti;
-    const float* y = B + TS * tj;
-    float acc[TS][TS] = {};
+  const int ti = threadIdx.x >> 4, tj = threadIdx.x & 15;  // 16 x 16 threads
+  if (ti < q && tj < q) {
+    const float* x = mats + A_at + TS * ti;
+    const float* y = mats + B_at + TS * tj;
+    float acc[2][TS][TS] = {};   // even and odd k apart: half the chain of dependent additions
 #pragma unroll 8
-    for (int k = 0; k < s; ++k) {
+    for (int k = 0; k < ((s + 1) & ~1); ++k) {   // row s is zero
       float xv[TS], yv[TS];
       if constexpr (TS == 2) {
         const float2 xx = *reinterpret_cast<const float2*>(x + k * SMALL_LD);
@@ -391,16 +392,16 @@ __device__ __noinline__ void small_product(float* D, const float* A, const float
 #pragma unroll
       for (int i = 0; i < TS; ++i)
 #pragma unroll
-        for (int j = 0; j < TS; ++j) acc[i][j] = fmaf(xv[i], yv[j], acc[i][j]);
+        for (int j = 0; j < TS; ++j) acc[k & 1][i][j] = fmaf(xv[i], yv[j], acc[k & 1][i][j]);
     }
 #pragma unroll
     for (int i = 0; i < TS; ++i)
 #pragma unroll
       for (int j = 0; j < TS; ++j) {
         const int r = TS * ti + i, cc = TS * tj + j;
-        float v = acc[i][j];
-        if (add) v = fmaf(c, v, fmaf(b, A[r * SMALL_LD + cc], r == cc ? a : 0.f));
-        if (r < s && cc < s) D[r * SMALL_LD + cc] = v;
+        float v = acc[0][i][j] + acc[1][i][j];
+        if (add) v = fmaf(c, v, fmaf(b, mats[A_at + r * SMALL_LD + cc], r == cc ? a : 0.f));
+        if (r < s && cc < s) mats[D_at + r * SMALL_LD + cc] = v;
       }
   }
   __syncthreads();
@@ -411,8 +412,10 @@ constexpr int STEP_THREADS = 256;
 template <int TS>
 __global__ void __launch_bounds__(STEP_THREADS) steps_kernel(const SmallParams p) {
   extern __shared__ __align__(16) float mats[];
-  constexpr int SZ = SMALL_SIDE * SMALL_LD;
-  float *S = mats, *P = mats + SZ, *Q = mats + 2 * SZ, *T = mats + 3 * SZ, *U = mats + 4 * SZ;
+  // S, P, Q, T, U: a row more than they need, which stays zero
+  constexpr int SZ = (SMALL_SIDE + 1) * SMALL_LD;
+  float *S = mats, *T = mats + 3 * SZ;
+  int Q = 2 * SZ, U = 4 * SZ;
   __shared__ float norm;
   const int s = p.s, ss = s * s;
   for (int e = threadIdx.x; e < 5 * SZ; e += STEP_THREADS) mats[e] = 0.f;
@@ -459,24 +462,28 @@ __global__ void __launch_bounds__(STEP_THREADS) steps_kernel(const SmallParams p
   const float inv = 1.f / norm;
   for (int i = threadIdx.x; i < s * SMALL_LD; i += STEP_THREADS) S[i] = S[i] * inv * inv;
   __syncthreads();
+  // T held partial sums: its row s has to be zero again
+  for (int i = threadIdx.x; i < SZ; i += STEP_THREADS) T[i] = 0.f;
+  __syncthreads();
 #pragma unroll 1
   for (int it = 0; it < p.steps; ++it) {
-    float* first = it == 0 ? Q : P;                       // Q_1 = P_0
-    small_product<TS>(first, S, S, s, true, p.a, p.b, p.c);
+    const int P = it == 0 ? Q : SZ;                         // Q_1 = P_0
+    small_product<TS>(P, 0, 0, s, true, p.a, p.b, p.c);
     if (it > 0) {
       small_product<TS>(U, P, Q, s, false, 0.f, 0.f, 0.f);
-      float* t = Q;
+      const int t = Q;
       Q = U;
       U = t;
     }
     if (it + 1 < p.steps) {
-      small_product<TS>(T, S, first, s, false, 0.f, 0.f, 0.f);  // S P
-      small_product<TS>(S, T, first, s, false, 0.f, 0.f, 0.f);  // (S P)^T P = P S P
+      small_product<TS>(3 * SZ, 0, P, s, false, 0.f, 0.f, 0.f);       // S P
+      small_product<TS>(0, 3 * SZ, P, s, false, 0.f, 0.f, 0.f);       // (S P)^T P = P S P
     }
   }
   float* out = p.Q + (int64_t)blockIdx.x * ss;
   for (int r = threadIdx.x >> 5; r < s; r += STEP_THREADS / 32)
-    if ((threadIdx.x & 31) < s) out[r * s + (threadIdx.x & 31)] = Q[r * SMALL_LD + (threadIdx.x & 31)] * inv;
+    if ((threadIdx.x & 31) < s) 
+      out[r * s + (threadIdx.x & 31)] = mats[Q + r * SMALL_LD + (threadIdx.x & 31)] * inv;
 }
 
 template <int VEC>
@@ -624,7 +631,7 @@ thanos_status_t small_side(const OrthogonalArgs& a, StepParams u, int s, int l, 
   p.keep = a.keep;
   p.rate = a.rate;
   const bool wide = a.n % 4 == 0;
-  const size_t stage = STAGE_FLOATS * 4, squares = 5 * SMALL_SIDE * SMALL_LD * 4;
+  const size_t stage = STAGE_FLOATS * 4, squares = 5 * (SMALL_SIDE + 1) * SMALL_LD * 4;
   const dim3 chunks_grid((unsigned)p.chunks, (unsigned)a.batch), one((unsigned)a.batch);
   if (wide) gram_kernel<4><<<chunks_grid, 256, stage, stream>>>(p);
   else gram_kernel<1><<<chunks_grid, 256, stage, stream>>>(p);
