@@ -375,24 +375,27 @@ __device__ __noinline__ void small_product(int D_at, int A_at, int B_at, int s, 
     const float* x = mats + A_at + TS * ti;
     const float* y = mats + B_at + TS * tj;
     float acc[2][TS][TS] = {};   // even and odd k apart: half the chain of dependent additions
-#pragma unroll 8
-    for (int k = 0; k < ((s + 1) & ~1); ++k) {   // row s is zero
-      float xv[TS], yv[TS];
-      if constexpr (TS == 2) {
-        const float2 xx = *reinterpret_cast<const float2*>(x + k * SMALL_LD);
-        const float2 yy = *reinterpret_cast<const float2*>(y + k * SMALL_LD);
-        xv[0] = xx.x;
-        xv[1] = xx.y;
-        yv[0] = yy.x;
-        yv[1] = yy.y;
-      } else {
-        xv[0] = x[k * SMALL_LD];
-        yv[0] = y[k * SMALL_LD];
+#pragma unroll 4
+    for (int k = 0; k < s; k += 2) {   // row s is zero
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float xv[TS], yv[TS];
+        if constexpr (TS == 2) {
+          const float2 xx = *reinterpret_cast<const float2*>(x + (k + h) * SMALL_LD);
+          const float2 yy = *reinterpret_cast<const float2*>(y + (k + h) * SMALL_LD);
+          xv[0] = xx.x;
+          xv[1] = xx.y;
+          yv[0] = yy.x;
+          yv[1] = yy.y;
+        } else {
+          xv[0] = x[(k + h) * SMALL_LD];
+          yv[0] = y[(k + h) * SMALL_LD];
+        }
+#pragma unroll
+        for (int i = 0; i < TS; ++i)
+#pragma unroll
+          for (int j = 0; j < TS; ++j) acc[h][i][j] = fmaf(xv[i], yv[j], acc[h][i][j]);
       }
-#pragma unroll
-      for (int i = 0; i < TS; ++i)
-#pragma unroll
-        for (int j = 0; j < TS; ++j) acc[k & 1][i][j] = fmaf(xv[i], yv[j], acc[k & 1][i][j]);
     }
 #pragma unroll
     for (int i = 0; i < TS; ++i)
@@ -631,7 +634,10 @@ thanos_status_t small_side(const OrthogonalArgs& a, StepParams u, int s, int l, 
   p.keep = a.keep;
   p.rate = a.rate;
   const bool wide = a.n % 4 == 0;
-  const size_t stage = STAGE_FLOATS * 4, squares = 5 * (SMALL_SIDE + 1) * SMALL_LD * 4;
+  // The steps are a chain on one CTA per matrix: CTAs that share an SM slow one another down, so they
+  // ask for more shared memory than half of an SM's, and spread out.
+  const size_t stage = STAGE_FLOATS * 4, squares = 116 * 1024;
+  static_assert(5 * (SMALL_SIDE + 1) * SMALL_LD * 4 <= 116 * 1024, "five matrices");
   const dim3 chunks_grid((unsigned)p.chunks, (unsigned)a.batch), one((unsigned)a.batch);
   if (wide) gram_kernel<4><<<chunks_grid, 256, stage, stream>>>(p);
   else gram_kernel<1><<<chunks_grid, 256, stage, stream>>>(p);
