@@ -19,14 +19,17 @@ __device__ __forceinline__ int adapter_of(const int32_t* __restrict__ index, int
 // ---------------------------------------------------------------------------- 16-bit operands
 using bf16 = __nv_bfloat16;
 
-// What the tensor-core kernels need of a call before they start; blocks by number:
+// What the tensor-core kernels need besides a call's operands.  Launched once in front of them (what
+// the skinny product reads) and once beside the skinny product (what only later launches read);
+// blocks by number:
 //   [0, n_list)          the distinct adapters of a token tile, by first occurrence
 //   next n_copy          16-byte aligned copies: rows of dY, or the adapters' B with padded ranks
 //   next n_turn          B_i [c, r] -> [r, c] (the skinny product's operand in the backward pass)
 //   next n_planes        backward: V as two bf16 planes for dB, and the zeros beyond the rank of U's
 //   the rest             V of a few tokens, a CTA per token and four ranks
 struct FrontParams {
-  int32_t* status;             // cleared here
+  int32_t* status;             // cleared here, or null
+  int beside;                  // runs beside the launch before it, on whose results it does not depend
   const int32_t* index;
   int32_t* count;
   int32_t* list;
@@ -62,12 +65,9 @@ __device__ __forceinline__ float dot8(const uint4& a, const uint4& b, float s) {
   return s;
 }
 
-__global__ void __launch_bounds__(256) front_kernel(const FrontParams p) {
-  __shared__ float sh[64 * 65];
-  grid_dependents_launch();
+__device__ __forceinline__ void front_block(const FrontParams& p, float* sh) {
   const int tid = threadIdx.x;
   int blk = blockIdx.x;
-  if (blk == 0 && tid == 0) *p.status = 0;
   if (blk < p.n_list) {
     int* ids = reinterpret_cast<int*>(sh);
     int* base = ids + 256;
@@ -173,12 +173,28 @@ __global__ void __launch_bounds__(256) front_kernel(const FrontParams p) {
   }
 }
 
+__global__ void __launch_bounds__(256) front_kernel(const FrontParams p) {
+  __shared__ float sh[64 * 65];
+  grid_dependents_launch();
+  if (blockIdx.x == 0 && threadIdx.x == 0 && p.status) *p.status = 0;
+  front_block(p, sh);
+  // whoever waits for this launch finds the one before it finished too
+  if (p.beside && blockIdx.x == 0) grid_dependency_wait();
+}
+
 thanos_status_t launch_front(const FrontParams& p, int64_t shrink_blocks, cudaStream_t stream) {
   const int64_t blocks = (int64_t)p.n_list + p.n_copy + p.n_turn + p.n_planes + shrink_blocks;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)blocks, 1, 1);
   cfg.blockDim = dim3(256, 1, 1);
   cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  if (p.beside) {
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+  }
   count_launch();
   THANOS_CUDA(cudaLaunchKernelEx(&cfg, front_kernel, p));
   return THANOS_OK;
@@ -267,30 +283,30 @@ thanos_status_t forward16(const AdapterArgs& a, void* workspace, size_t ws_bytes
     const int64_t want = ceil_div(f.copy_rows * a.r, 1024);
     f.n_copy = (int)(want < 4 * NUM_SMS ? want : 4 * NUM_SMS);
   }
-  int64_t shrink = 0;
-  if (few_tokens(a)) {
-    f.X = static_cast<const bf16*>(a.in);
-    f.ldx = a.ldi;
-    f.A = static_cast<const bf16*>(a.A);
-    f.V = V;
-    f.b = (int)a.b;
-    shrink = a.T * ceil_div(a.r, SHRINK_RANKS);
-  }
-  if (f.n_list + f.n_copy + shrink > 0) THANOS_TRY(launch_front(f, shrink, stream));
-  else THANOS_CUDA(cudaMemsetAsync(L.status, 0, 16, stream));
   g.V = V;
   g.index = a.index;
   g.n_adapters = (int)a.n;
   g.r = a.r;
   g.tile_count = L.count;
   g.tile_list = L.list;
-  if (!few_tokens(a)) {
+  if (few_tokens(a)) {
+    f.X = static_cast<const bf16*>(a.in);
+    f.ldx = a.ldi;
+    f.A = static_cast<const bf16*>(a.A);
+    f.V = V;
+    f.b = (int)a.b;
+    THANOS_TRY(launch_front(f, a.T * ceil_div(a.r, SHRINK_RANKS), stream));
+  } else {
     ProjArgs s = g;
     s.epi = PROJ_SHRINK;
+    s.first = 1;
     s.A = a.A;
     s.lda = a.b;
     s.M = (int)(a.n * a.r);
     THANOS_TRY(proj_gemm(s, stream));
+    f.status = nullptr;
+    f.beside = 1;
+    if (f.n_list + f.n_copy > 0) THANOS_TRY(launch_front(f, 0, stream));
   }
   g.scale = a.scale;
   g.P = pad ? static_cast<const void*>(L.copy) : a.B;
@@ -358,7 +374,13 @@ thanos_status_t backward16(const AdapterArgs& a, void* workspace, size_t ws_byte
     const int64_t want = ceil_div(a.T, 8);
     f.n_planes = (int)(want < 2 * NUM_SMS ? want : 2 * NUM_SMS);
   }
-  if (f.n_list + f.n_copy + f.n_turn + f.n_planes > 0) THANOS_TRY(launch_front(f, 0, stream));
+  // in front: the copy of dY and the turned B; the rest beside the skinny product
+  FrontParams later = f;
+  later.status = nullptr;
+  later.beside = 1;
+  later.n_copy = later.n_turn = 0;
+  f.n_list = f.n_planes = 0;
+  if (f.n_copy + f.n_turn > 0) THANOS_TRY(launch_front(f, 0, stream));
   else THANOS_CUDA(cudaMemsetAsync(L.status, 0, 16, stream));
   if (a.n > 0) {
     g.V = L.R;
@@ -376,6 +398,7 @@ thanos_status_t backward16(const AdapterArgs& a, void* workspace, size_t ws_byte
     s.scale = a.scale;
     s.planes = sorts ? L.u_planes : nullptr;
     THANOS_TRY(proj_gemm(s, stream));
+    if (later.n_list + later.n_planes > 0) THANOS_TRY(launch_front(later, 0, stream));
     if (sorts)
       THANOS_TRY(sort_tokens(a.index, a.T, a.n, L.order, L.spare, L.off, L.status, stream));
     g.P = a.A;

@@ -31,7 +31,7 @@ constexpr int FACTOR_BYTES = 128 * 16 * 4;    // 16 ranks of up to 128 tokens, f
 
 struct Params {
   int M, N, K, tiles_m, tiles_n, nt, stages, splits, batch_z, ring_bytes, tmem_cols;
-  int symmetric, f16, early, f32;     // f32: three bf16 planes per operand, fp32 result
+  int symmetric, f16, early, first, f32;     // f32: three bf16 planes per operand, fp32 result
   int32_t* status;
   // adapter part
   void* out;
@@ -611,6 +611,7 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
     // zeros of tokens without adapter)
     grid_dependency_wait();
     grid_dependents_launch();
+    if (p.first && blockIdx.x == 0 && threadIdx.x == 0) *p.status = 0;
     if (tm > 0) {
       const int lo = m0 / p.r, hi = (min(m0 + TM, p.M) - 1) / p.r;
       bool hit = false;
@@ -1286,7 +1287,7 @@ thanos_status_t launch(const CUtensorMap& mA, const CUtensorMap& mB, const Param
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 2;
+  cfg.numAttrs = p.first ? 1 : 2;   // what runs beside a first launch relies on its plain start
   count_launch();
   THANOS_CUDA(cudaLaunchKernelEx(&cfg, tile_kernel<AMN, EPI>, mA, mB, p));
   return THANOS_OK;
@@ -1403,6 +1404,7 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
   p.f16 = a.f16;
   p.f32 = a.f32;
   p.early = a.early;
+  p.first = a.first;
   p.status = a.status;
   int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * a.batch;
   if (symmetric) tiles = (tiles + (int64_t)p.tiles_m * a.batch * (TM / p.nt)) / 2;
