@@ -4,6 +4,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 from typing import Optional, Tuple
@@ -547,10 +548,20 @@ def _adapters(X, W, A, B, index, scale, dev):
     return T, c, b, n, r, dt
 
 
+@functools.lru_cache(maxsize=256)
+def _adapter_workspace(backward, T, c, b, n, r, dt):
+    return max(int(load_library().thanos_adapter_workspace_bytes(backward, T, c, b, n, r, dt)), 256)
+
+
+@functools.lru_cache(maxsize=256)
+def _orthogonal_workspace(k, m, n):
+    return max(int(load_library().thanos_orthogonal_workspace_bytes(k, m, n)), 256)
+
+
 def _scratch(workspace: Optional[torch.Tensor], nbytes: int, like: torch.Tensor) -> torch.Tensor:
     """The caller's workspace, or a new one."""
     if workspace is None:
-        return _ws(nbytes, like.device)
+        return like.new_empty(nbytes, dtype=torch.uint8)
     if workspace.get_device() != like.get_device() or workspace.dtype != torch.uint8 \
             or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous uint8 tensor on the call's device")
@@ -584,16 +595,15 @@ def adapter_forward(X: torch.Tensor, W: torch.Tensor, A: Optional[torch.Tensor] 
     with _on(X):
         with _alloc_scope(stream):
             if out is None:
-                out = torch.empty((T, c), dtype=X.dtype, device=X.device)
+                out = X.new_empty((T, c))
             elif out.dtype != X.dtype or out.shape[0] != T:
                 raise ValueError("out must be a [T, c] tensor of X's dtype")
             if n > 0:
                 if V is None:
-                    V = torch.empty((T, r), dtype=torch.float32, device=X.device)
+                    V = scale.new_empty((T, r))
                 else:
                     _dense(V, (T, r), torch.float32, dev, "V")
-            workspace = _scratch(workspace,
-                                 lib.thanos_adapter_workspace_bytes(0, T, c, b, n, r, dt), X)
+            workspace = _scratch(workspace, _adapter_workspace(0, T, c, b, n, r, dt), X)
         ldy = _rows(out, c, dev, "out")
         _check(lib.thanos_adapter_forward(out.data_ptr(), ldy, _ptr(V), X.data_ptr(), ldx,
                                           W.data_ptr(), ldw, _ptr(A), _ptr(B), _ptr(index),
@@ -640,20 +650,19 @@ def adapter_backward(dY: torch.Tensor, X: Optional[torch.Tensor], V: Optional[to
             if not need_dx:
                 dX = None
             elif dX is None:
-                dX = torch.empty((T, b), dtype=dY.dtype, device=dY.device)
+                dX = dY.new_empty((T, b))
             elif dX.dtype != dY.dtype or dX.shape[0] != T:
                 raise ValueError("dX must be a [T, b] tensor of dY's dtype")
             if need_grads:
                 if dA is None:
-                    dA = torch.empty((n, r, b), dtype=torch.float32, device=dY.device)
+                    dA = scale.new_empty((n, r, b))
                 else:
                     _dense(dA, (n, r, b), torch.float32, dev, "dA")
                 if dB is None:
-                    dB = torch.empty((n, c, r), dtype=torch.float32, device=dY.device)
+                    dB = scale.new_empty((n, c, r))
                 else:
                     _dense(dB, (n, c, r), torch.float32, dev, "dB")
-            workspace = _scratch(workspace,
-                                 lib.thanos_adapter_workspace_bytes(1, T, c, b, n, r, dt), dY)
+            workspace = _scratch(workspace, _adapter_workspace(1, T, c, b, n, r, dt), dY)
         if need_dx:
             lddx = _rows(dX, b, dev, "dX")
         _check(lib.thanos_adapter_backward(_ptr(dX), lddx, _ptr(dA), _ptr(dB),
@@ -691,7 +700,7 @@ def orthogonalise(G: torch.Tensor, steps: int = 5, coef=NEWTON_SCHULZ, eps: floa
                 out = torch.empty(G.shape, dtype=torch.bfloat16, device=G.device)
             else:
                 _dense(out, G.shape, torch.bfloat16, dev, "out")
-            workspace = _scratch(workspace, lib.thanos_orthogonal_workspace_bytes(k, m, n), G)
+            workspace = _scratch(workspace, _orthogonal_workspace(k, m, n), G)
         abc = (ctypes.c_float * 3)(*coef)
         _check(lib.thanos_orthogonalise(out.data_ptr(), G.data_ptr(), dt, k, m, n, abc, steps,
                                         float(eps), workspace.data_ptr(), workspace.numel(),
@@ -729,7 +738,7 @@ def orthogonal_step(W: torch.Tensor, M: torch.Tensor, G: torch.Tensor,
                 M_out = torch.empty_like(M)
             else:
                 _dense(M_out, G.shape, torch.float32, dev, "M_out")
-            workspace = _scratch(workspace, lib.thanos_orthogonal_workspace_bytes(k, m, n), G)
+            workspace = _scratch(workspace, _orthogonal_workspace(k, m, n), G)
         abc = (ctypes.c_float * 3)(*coef)
         _check(lib.thanos_orthogonal_step(W_out.data_ptr(), W.data_ptr(), wdt, M_out.data_ptr(),
                                           M.data_ptr(), G.data_ptr(), gdt, _ptr(mask), k, m, n,

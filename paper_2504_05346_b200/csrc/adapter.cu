@@ -200,6 +200,11 @@ thanos_status_t launch_front(const FrontParams& p, int64_t shrink_blocks, cudaSt
   return THANOS_OK;
 }
 
+// A handful of tokens: V on the way, in the CTAs that need it.  Every one of them reads the tokens'
+// A_i, so these may be no more than a fraction of the weights that a CTA reads (1 token, 4096 x 4096,
+// r = 16: 128 KB beside 256 KB).
+bool handful(const AdapterArgs& a) { return a.T <= 8 && a.T * a.r * a.b <= (1 << 17); }
+
 // Few tokens: V by dot products in the first launch; more: one more launch on the tensor cores.
 bool few_tokens(const AdapterArgs& a) { return a.T <= 64; }
 
@@ -289,7 +294,11 @@ thanos_status_t forward16(const AdapterArgs& a, void* workspace, size_t ws_bytes
   g.r = a.r;
   g.tile_count = L.count;
   g.tile_list = L.list;
-  if (few_tokens(a)) {
+  if (handful(a)) {
+    g.V = a.V;
+    g.skinny = a.A;
+    g.first = 1;
+  } else if (few_tokens(a)) {
     f.X = static_cast<const bf16*>(a.in);
     f.ldx = a.ldi;
     f.A = static_cast<const bf16*>(a.A);
@@ -312,7 +321,7 @@ thanos_status_t forward16(const AdapterArgs& a, void* workspace, size_t ws_bytes
   g.P = pad ? static_cast<const void*>(L.copy) : a.B;
   g.ldp = pad ? (int64_t)round_up(a.r, 8) : a.r;
   g.p_adapter = a.c * g.ldp;
-  g.early = 1;
+  g.early = !handful(a);
   return proj_gemm(g, stream);
 }
 

@@ -38,6 +38,9 @@ struct Params {
   int64_t ldo;
   float* V;
   __nv_bfloat16* planes;
+  const __nv_bfloat16* skinny;        // A, for V on the way; the tokens are at x, ld_tok apart
+  const __nv_bfloat16* x;
+  int64_t ld_tok;
   const int32_t* index;
   const float* scale;
   int n_adapters, r, chunks;          // chunks of 16 per adapter
@@ -527,6 +530,17 @@ __device__ __forceinline__ void wide_row(const Params& p, int i, int m, int j0, 
   }
 }
 
+__device__ __forceinline__ float dot8(const uint4& a, const uint4& b, float s) {
+  const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float2 u = unpack2(x[e]), v = unpack2(y[e]);
+    s = fmaf(u.x, v.x, s);
+    s = fmaf(u.y, v.y, s);
+  }
+  return s;
+}
+
 __device__ __forceinline__ float dot16(const uint32_t (&w)[8], const float* __restrict__ v, float s) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
@@ -602,6 +616,7 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
   const int z = blockIdx.y;
   const int stage_bytes = A_BYTES + p.nt * BK * 2;
 
+  if (p.first && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.status = 0;
   // symmetric results: tiles left of the diagonal blocks are the mirror of those right of them
   // (nt divides TM)
   if (p.symmetric && n0 < m0) return;
@@ -611,7 +626,6 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
     // zeros of tokens without adapter)
     grid_dependency_wait();
     grid_dependents_launch();
-    if (p.first && blockIdx.x == 0 && threadIdx.x == 0) *p.status = 0;
     if (tm > 0) {
       const int lo = m0 / p.r, hi = (min(m0 + TM, p.M) - 1) / p.r;
       bool hit = false;
@@ -763,18 +777,48 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
             atomicCAS(p.status, 0, (int)THANOS_ERR_INVALID_ARG);
         }
         used = epilogue_any(any);
+        int ldf = 16;                      // row of `factor`
+        if (p.skinny) {
+          // V of the few tokens, by the CTAs that write their outputs: a warp per dot product
+          ldf = (p.r + 15) & ~15;
+          const int live = min(p.nt, p.N - n0);
+          const bool mine = tile_column(S, rank, 0, 0) < live;
+#pragma unroll 1
+          for (int e = warp - 2; mine && e < live * ldf; e += 8) {
+            const int c = e / ldf, j = e - c * ldf, i = ids[c];
+            float s = 0.f;
+            if (i >= 0 && j < p.r) {
+              const __nv_bfloat16* xr = p.x + (int64_t)(n0 + c) * p.ld_tok;
+              const __nv_bfloat16* ar = p.skinny + ((int64_t)i * p.r + j) * p.K;
+#pragma unroll 8
+              for (int k = lane * 8; k < p.K; k += 256)
+                s = dot8(*reinterpret_cast<const uint4*>(xr + k),
+                         *reinterpret_cast<const uint4*>(ar + k), s);
+              for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+            }
+            if (lane == 0) {
+              if (tm == 0 && p.V && j < p.r) p.V[(int64_t)(n0 + c) * p.r + j] = s;
+              factor[e] = i >= 0 && p.scale ? p.scale[i] * s : s;
+            }
+          }
+        }
 #pragma unroll 1
         for (int j0 = 0; j0 < p.r && used; j0 += 16) {
           if (j0 > 0) epilogue_sync();
+          const float* fac = factor;
+          if (p.skinny) {
+            fac += j0;
+          } else {
 #pragma unroll 1
-          for (int e = tid; e < p.nt * 16; e += 256) {
-            const int t = n0 + (e >> 4), j = j0 + (e & 15), i = ids[e >> 4];
-            float v = 0.f;
-            if (i >= 0 && j < p.r) {
-              v = p.V[(int64_t)t * p.r + j];
-              if (p.scale) v *= p.scale[i];
+            for (int e = tid; e < p.nt * 16; e += 256) {
+              const int t = n0 + (e >> 4), j = j0 + (e & 15), i = ids[e >> 4];
+              float v = 0.f;
+              if (i >= 0 && j < p.r) {
+                v = p.V[(int64_t)t * p.r + j];
+                if (p.scale) v *= p.scale[i];
+              }
+              factor[e] = v;
             }
-            factor[e] = v;
           }
           epilogue_sync();
 #pragma unroll 1
@@ -787,14 +831,14 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
 #pragma unroll
             for (int e = 1; e < 8; ++e) same = same && ids[c + e] == first;
             if (m < p.M && p.f32) {
-              wide_part_f32<AMN>(p, ids, factor, c, m, j0, own);
+              wide_part_f32<AMN>(p, ids, fac, c, m, j0, own);
             } else if (m < p.M) {
               if (same) {  // a run of one request's tokens (or none): its row is read once
                 if (first >= 0) {
                   uint32_t w[8];
                   wide_row<AMN>(p, first, m, j0, w);
 #pragma unroll
-                  for (int e = 0; e < 8; ++e) own[e] = dot16(w, factor + (c + e) * 16, 0.f);
+                  for (int e = 0; e < 8; ++e) own[e] = dot16(w, fac + (c + e) * ldf, 0.f);
                 }
               } else {
                 uint32_t w[8][8];  // eight rows in flight
@@ -802,7 +846,7 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
                 for (int e = 0; e < 8; ++e) wide_row<AMN>(p, ids[c + e], m, j0, w[e]);
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                  if (ids[c + e] >= 0) own[e] = dot16(w[e], factor + (c + e) * 16, 0.f);
+                  if (ids[c + e] >= 0) own[e] = dot16(w[e], fac + (c + e) * ldf, 0.f);
               }
             }
             __syncwarp();
@@ -1424,6 +1468,9 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
   p.ldo = a.ldo;
   p.V = a.V;
   p.planes = a.planes;
+  p.skinny = static_cast<const __nv_bfloat16*>(a.skinny);
+  p.x = static_cast<const __nv_bfloat16*>(a.B);
+  p.ld_tok = a.ldb;
   p.index = a.index;
   p.scale = a.scale;
   p.n_adapters = a.n_adapters;

@@ -35,7 +35,9 @@ struct ProjArgs {
                                  // b_batch apart), out and P are fp32
   int epi = PROJ_OUT;
   int early = 0;                 // operands do not depend on the previous launch of the stream
-  int first = 0;                 // SHRINK: first launch of its call, clears the status word
+  int first = 0;                 // first launch of its call: plain, and clears the status word
+  const void* skinny = nullptr;  // PROJ_OUT of a few tokens: A [n, r, K], V is computed on the way (and
+                                 // written, if wanted)
   int32_t* status = nullptr;
   // PROJ_OUT, PROJ_SHRINK
   void* out = nullptr;           // [N, ldo], bf16 (fp32 if f32)
