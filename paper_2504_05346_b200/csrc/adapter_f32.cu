@@ -101,13 +101,50 @@ __global__ void __launch_bounds__(256) front_f32_kernel(const Front32Params p) {
   if (i >= 0) {
     const float* x = p.in.src + t * p.in.ld;
     const float* a = p.P + (int64_t)i * p.r * p.K + (p.back ? (int64_t)j0 : (int64_t)j0 * p.K);
-    const int64_t dj = p.back ? 1 : p.K, dk = p.back ? p.r : 1;
+    // ranks beyond the last read the last one again: a load under a condition is not issued ahead
+    int at[RANKS];
+    if (p.back && p.r % 4 == 0) {
+      const int second = nj > 4 ? 4 : 0;
 #pragma unroll 4
-    for (int k = lane; k < p.K; k += 32) {
-      const float xv = x[k];
+      for (int k = lane; k < p.K; k += 32) {
+        const float xv = x[k];
+        const float* ak = a + (int64_t)k * p.r;
+        const float4 u = *reinterpret_cast<const float4*>(ak);
+        const float4 w = *reinterpret_cast<const float4*>(ak + second);
+        s[0] = fmaf(xv, u.x, s[0]);
+        s[1] = fmaf(xv, u.y, s[1]);
+        s[2] = fmaf(xv, u.z, s[2]);
+        s[3] = fmaf(xv, u.w, s[3]);
+        s[4] = fmaf(xv, w.x, s[4]);
+        s[5] = fmaf(xv, w.y, s[5]);
+        s[6] = fmaf(xv, w.z, s[6]);
+        s[7] = fmaf(xv, w.w, s[7]);
+      }
+    } else if (p.back) {
 #pragma unroll
-      for (int j = 0; j < RANKS; ++j)
-        if (j < nj) s[j] = fmaf(xv, a[j * dj + k * dk], s[j]);
+      for (int j = 0; j < RANKS; ++j) at[j] = min(j, nj - 1);
+#pragma unroll 4
+      for (int k = lane; k < p.K; k += 32) {
+        const float xv = x[k];
+        const float* ak = a + (int64_t)k * p.r;
+#pragma unroll
+        for (int j = 0; j < RANKS; ++j) s[j] = fmaf(xv, ak[at[j]], s[j]);
+      }
+    } else {  // K is a multiple of 8
+#pragma unroll
+      for (int j = 0; j < RANKS; ++j) at[j] = min(j, nj - 1) * p.K;
+#pragma unroll 2
+      for (int k = 4 * lane; k < p.K; k += 128) {
+        const float4 xv = *reinterpret_cast<const float4*>(x + k);
+#pragma unroll
+        for (int j = 0; j < RANKS; ++j) {
+          const float4 av = *reinterpret_cast<const float4*>(a + at[j] + k);
+          s[j] = fmaf(xv.x, av.x, s[j]);
+          s[j] = fmaf(xv.y, av.y, s[j]);
+          s[j] = fmaf(xv.z, av.z, s[j]);
+          s[j] = fmaf(xv.w, av.w, s[j]);
+        }
+      }
     }
   }
 #pragma unroll

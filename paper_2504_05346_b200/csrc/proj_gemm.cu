@@ -779,26 +779,34 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
         used = epilogue_any(any);
         int ldf = 16;                      // row of `factor`
         if (p.skinny) {
-          // V of the few tokens, by the CTAs that write their outputs: a warp per dot product
+          // V of the few tokens, by the CTAs that write their outputs: a warp per pair of ranks
           ldf = (p.r + 15) & ~15;
           const int live = min(p.nt, p.N - n0);
           const bool mine = tile_column(S, rank, 0, 0) < live;
 #pragma unroll 1
-          for (int e = warp - 2; mine && e < live * ldf; e += 8) {
+          for (int e = 2 * (warp - 2); mine && e < live * ldf; e += 16) {
             const int c = e / ldf, j = e - c * ldf, i = ids[c];
-            float s = 0.f;
+            float s0 = 0.f, s1 = 0.f;
             if (i >= 0 && j < p.r) {
               const __nv_bfloat16* xr = p.x + (int64_t)(n0 + c) * p.ld_tok;
-              const __nv_bfloat16* ar = p.skinny + ((int64_t)i * p.r + j) * p.K;
+              const __nv_bfloat16* a0 = p.skinny + ((int64_t)i * p.r + j) * p.K;
+              const __nv_bfloat16* a1 = a0 + (j + 1 < p.r ? p.K : 0);
 #pragma unroll 8
-              for (int k = lane * 8; k < p.K; k += 256)
-                s = dot8(*reinterpret_cast<const uint4*>(xr + k),
-                         *reinterpret_cast<const uint4*>(ar + k), s);
-              for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+              for (int k = lane * 8; k < p.K; k += 256) {
+                const uint4 x = *reinterpret_cast<const uint4*>(xr + k);
+                s0 = dot8(x, *reinterpret_cast<const uint4*>(a0 + k), s0);
+                s1 = dot8(x, *reinterpret_cast<const uint4*>(a1 + k), s1);
+              }
+              for (int o = 16; o > 0; o >>= 1) {
+                s0 += __shfl_xor_sync(0xffffffffu, s0, o);
+                s1 += __shfl_xor_sync(0xffffffffu, s1, o);
+              }
+              if (j + 1 >= p.r) s1 = 0.f;
             }
-            if (lane == 0) {
-              if (tm == 0 && p.V && j < p.r) p.V[(int64_t)(n0 + c) * p.r + j] = s;
-              factor[e] = i >= 0 && p.scale ? p.scale[i] * s : s;
+            if (lane < 2 && j + lane < ldf) {
+              const float v = lane ? s1 : s0;
+              if (tm == 0 && p.V && j + lane < p.r) p.V[(int64_t)(n0 + c) * p.r + j + lane] = v;
+              factor[e + lane] = i >= 0 && p.scale ? p.scale[i] * v : v;
             }
           }
         }
