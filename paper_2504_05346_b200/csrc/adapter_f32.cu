@@ -319,7 +319,7 @@ thanos_status_t adapter_f32(bool back, const AdapterArgs& a, void* workspace, si
   }
   if (a.out) {
     ProjArgs g;
-    g.f32 = 1;
+    g.epi = PROJ_OUT32;
     g.M = F;
     g.N = (int)a.T;
     g.K = K;

@@ -31,7 +31,7 @@ constexpr int FACTOR_BYTES = 128 * 16 * 4;    // 16 ranks of up to 128 tokens, f
 
 struct Params {
   int M, N, K, tiles_m, tiles_n, nt, stages, splits, batch_z, ring_bytes, tmem_cols;
-  int symmetric, f16, early, first, f32;     // f32: three bf16 planes per operand, fp32 result
+  int symmetric, f16, early, first;
   int32_t* status;
   // adapter part
   void* out;
@@ -46,7 +46,7 @@ struct Params {
   int n_adapters, r, chunks;          // chunks of 16 per adapter
   const int32_t* tile_count;
   const int32_t* tile_list;
-  const __nv_bfloat16* P;             // f32: fp32 values
+  const __nv_bfloat16* P;             // OUT32: fp32 values
   int64_t ldp, p_adapter;
   // iteration
   float alpha, beta;
@@ -240,14 +240,12 @@ __device__ __forceinline__ void emit(const Params& p, int z, int m, int n0, floa
                                      bool mirror, bool poisoned) {
   if (m >= p.M || n0 >= p.N) return;
   const int nc = p.N - n0;  // columns that exist
-  if constexpr (EPI == PROJ_OUT) {
-    if (p.f32) {
-      float* out = static_cast<float*>(p.out) + (int64_t)n0 * p.ldo + m;
+  if constexpr (EPI == PROJ_OUT32) {
+    float* out = static_cast<float*>(p.out) + (int64_t)n0 * p.ldo + m;
 #pragma unroll
-      for (int e = 0; e < NC; ++e)
-        if (e < nc) out[(int64_t)e * p.ldo] = v[e];
-      return;
-    }
+    for (int e = 0; e < NC; ++e)
+      if (e < nc) out[(int64_t)e * p.ldo] = v[e];
+  } else if constexpr (EPI == PROJ_OUT) {
     __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + (int64_t)n0 * p.ldo + m;
     if (poisoned) {
 #pragma unroll
@@ -554,24 +552,52 @@ __device__ __forceinline__ float dot16(const uint32_t (&w)[8], const float* __re
   return s;
 }
 
-// The same part in fp32 for eight tokens, columns c.. of the tile.
+// The same in fp32.
+template <bool AMN>
+__device__ __forceinline__ void wide_row_f32(const Params& p, int i, int m, int j0, float (&w)[16]) {
+  const float* P = reinterpret_cast<const float*>(p.P) + (int64_t)(i < 0 ? 0 : i) * p.p_adapter;
+  const int last = p.r - 1 - j0;  // ranks beyond it are read again there, and not used
+  if (!AMN && p.r % 4 == 0) {
+    const float* q = P + (int64_t)m * p.ldp + j0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float4 f = *reinterpret_cast<const float4*>(q + min(4 * e, last & ~3));
+      w[4 * e] = f.x;
+      w[4 * e + 1] = f.y;
+      w[4 * e + 2] = f.z;
+      w[4 * e + 3] = f.w;
+    }
+  } else {
+    const float* q = P + (AMN ? (int64_t)j0 * p.ldp + m : (int64_t)m * p.ldp + j0);
+    const int64_t dj = AMN ? p.ldp : 1;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) w[j] = q[min(j, last) * dj];
+  }
+  if (last < 15) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+      if (j > last) w[j] = 0.f;
+  }
+}
+
+// The adapter part of eight tokens, columns c.. of the tile; a run of one request's tokens reads its
+// row once.
 template <bool AMN>
 __device__ __forceinline__ void wide_part_f32(const Params& p, const int* ids, const float* factor,
-                                              int c, int m, int j0, float (&own)[8]) {
-  const float* P = reinterpret_cast<const float*>(p.P);
-  const int nj = min(16, p.r - j0);
+                                              int c, int m, int j0, bool same, float (&own)[8]) {
+  float w[16];
+  if (same) {
+    if (ids[c] < 0) return;
+    wide_row_f32<AMN>(p, ids[c], m, j0, w);
+  }
 #pragma unroll 1
   for (int e = 0; e < 8; ++e) {
-    const int i = ids[c + e];
-    if (i < 0) continue;
-    const float* q = P + (int64_t)i * p.p_adapter +
-                     (AMN ? (int64_t)j0 * p.ldp + m : (int64_t)m * p.ldp + j0);
-    const int64_t dj = AMN ? p.ldp : 1;
+    if (ids[c + e] < 0) continue;
+    if (!same) wide_row_f32<AMN>(p, ids[c + e], m, j0, w);
     const float* f = factor + (c + e) * 16;
     float s = 0.f;
 #pragma unroll
-    for (int j = 0; j < 16; ++j)
-      if (j < nj) s = fmaf(q[j * dj], f[j], s);
+    for (int j = 0; j < 16; ++j) s = fmaf(w[j], f[j], s);
 #pragma unroll
     for (int k = 0; k < 8; ++k)
       if (k == e) own[k] = s;
@@ -586,10 +612,13 @@ __device__ __forceinline__ void plane_pair(int combo, int& a, int& b) {
   b = (0x001021 >> (4 * combo)) & 15;
 }
 
+__host__ __device__ constexpr bool two_per_sm(int epi) { return epi <= PROJ_SHRINK || epi == PROJ_OUT32; }
+
 template <bool AMN, int EPI>
-__global__ void __launch_bounds__(TILE_THREADS, EPI <= PROJ_SHRINK ? 2 : 1)
+__global__ void __launch_bounds__(TILE_THREADS, two_per_sm(EPI) ? 2 : 1)
 tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
             const Params p) {
+  constexpr bool F32 = EPI == PROJ_OUT32, OUT = EPI == PROJ_OUT || F32;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -664,7 +693,7 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
   }
 
   const int nk1 = (p.K + BK - 1) / BK;
-  const int nk = EPI == PROJ_OUT && p.f32 ? 6 * nk1 : nk1;
+  const int nk = F32 ? 6 * nk1 : nk1;
   const int ks0 = (int)((int64_t)nk * rank / S), ks1 = (int)((int64_t)nk * (rank + 1) / S);
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
@@ -677,7 +706,7 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
       if (ok) {
         const uint32_t dst = smem_base + (uint32_t)s * stage_bytes;
         int k0 = ks * BK, za = z, zb = z;
-        if (EPI == PROJ_OUT && p.f32) {
+        if (F32) {
           const int combo = ks / nk1;
           k0 = (ks - combo * nk1) * BK;
           plane_pair(combo, za, zb);
@@ -743,9 +772,9 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
     // All loops below are kept rolled: the code runs once per CTA, and straight-line code of a few
     // thousand instructions costs more in instruction fetches than it saves.
     bool used = false;
-    if constexpr (EPI == PROJ_OUT) {
+    if constexpr (OUT) {
       // ---------------------------------------------------------- adapter part
-      if (p.n_adapters > 0 && p.early && !p.f32) {
+      if (!F32 && p.n_adapters > 0 && p.early) {
         // the rows of the wide factors that this thread will read are on their way to L2 while the
         // previous launch still computes V
 #pragma unroll 1
@@ -778,7 +807,7 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
         }
         used = epilogue_any(any);
         int ldf = 16;                      // row of `factor`
-        if (p.skinny) {
+        if (!F32 && p.skinny) {
           // V of the few tokens, by the CTAs that write their outputs: a warp per pair of ranks
           ldf = (p.r + 15) & ~15;
           const int live = min(p.nt, p.N - n0);
@@ -814,7 +843,7 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
         for (int j0 = 0; j0 < p.r && used; j0 += 16) {
           if (j0 > 0) epilogue_sync();
           const float* fac = factor;
-          if (p.skinny) {
+          if (!F32 && p.skinny) {
             fac += j0;
           } else {
 #pragma unroll 1
@@ -838,8 +867,8 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
             bool same = true;
 #pragma unroll
             for (int e = 1; e < 8; ++e) same = same && ids[c + e] == first;
-            if (m < p.M && p.f32) {
-              wide_part_f32<AMN>(p, ids, fac, c, m, j0, own);
+            if constexpr (F32) {
+              if (m < p.M) wide_part_f32<AMN>(p, ids, fac, c, m, j0, same, own);
             } else if (m < p.M) {
               if (same) {  // a run of one request's tokens (or none): its row is read once
                 if (first >= 0) {
@@ -914,14 +943,14 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
 #pragma unroll 1
         for (int k = 0; k < S; k += 2) {
           const uint32_t a0 = map_to_cta(smem_base, k) + (uint32_t)(c * TM + row) * 4u;
-          const uint32_t a1 = map_to_cta(smem_base, k + 1) + (uint32_t)(c * TM + row) * 4u;
+          const uint32_t a1 = map_to_cta(smem_base, min(k + 1, S - 1)) + (uint32_t)(c * TM + row) * 4u;
           float x[8], y[8];
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[e] = ld_cluster(a0 + e * TM * 4);
 #pragma unroll
           for (int e = 0; e < 8; ++e) y[e] = ld_cluster(a1 + e * TM * 4);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] = (f[e] + x[e]) + y[e];
+          for (int e = 0; e < 8; ++e) f[e] = (f[e] + x[e]) + (k + 1 < S ? y[e] : 0.f);
         }
         emit<AMN, EPI, 8>(p, z, m, n0 + c, f, mirror, false);
         __syncwarp();
@@ -1425,6 +1454,7 @@ int tile_width(int64_t M, int64_t N, int64_t batch, bool symmetric, int epi) {
   int64_t want = (int64_t)sm_count() * 3 / 4;
   if (epi == PROJ_OUT) want *= 2;           // two CTAs per SM
   if (epi == PROJ_SHRINK) want = sm_count() / 10;
+  if (epi == PROJ_OUT32) want = sm_count() / 4;   // six times the k of the others
   int nt = 128;
   while (nt > 32) {
     int64_t tiles = ceil_div(M, TM) * ceil_div(N, nt) * batch;
@@ -1447,31 +1477,36 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
   p.M = a.M;
   p.N = a.N;
   p.K = a.K;
-  const bool pairs = a.epi != PROJ_SHRINK && !a.f32 && use_pairs(a.M, a.N, a.batch, symmetric);
+  const bool f32 = a.epi == PROJ_OUT32;
+  const bool pairs = a.epi != PROJ_SHRINK && !f32 && use_pairs(a.M, a.N, a.batch, symmetric);
   p.nt = pairs ? PTM : tile_width(a.M, a.N, a.batch, symmetric, a.epi);
   p.tiles_m = (a.M + (pairs ? PTM : TM) - 1) / (pairs ? PTM : TM);
   p.tiles_n = (a.N + p.nt - 1) / p.nt;
   p.batch_z = a.batch;
   p.symmetric = symmetric;
   p.f16 = a.f16;
-  p.f32 = a.f32;
   p.early = a.early;
   p.first = a.first;
   p.status = a.status;
   int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * a.batch;
   if (symmetric) tiles = (tiles + (int64_t)p.tiles_m * a.batch * (TM / p.nt)) / 2;
-  const int nk = (a.K + BK - 1) / BK * (a.f32 ? 6 : 1);
+  const int nk = (a.K + BK - 1) / BK * (f32 ? 6 : 1);
   p.splits = 1;
-  // A split fills SMs that have no tile; beyond a quarter more CTAs than SMs it costs more in
-  // partial sums than it brings (4096 x 4096, 1 token: 4 slices 12.4 us, 8 slices 14.4 us).
-  const int64_t slots = a.epi <= PROJ_SHRINK ? sm_count() * 5 / 4 : sm_count();
-  while (p.splits < 8 && tiles * p.splits * 2 <= slots && nk >= 8 * p.splits) p.splits *= 2;
+  // A split gives the SMs that have no tile a slice of k, one CTA to an SM; more cost more in partial
+  // sums than they bring (4096 x 4096, 1 token: 4 slices 12.4 us, 8 slices 14.4 us), but two slices may
+  // go a little over (11008 x 4096, 64 tokens, 86 tiles: 31 us instead of 37 us).
+  if (tiles < sm_count()) {
+    const int64_t most = sm_count() / tiles;
+    p.splits = (int)(most < 8 ? most : 8);
+    if (p.splits == 1 && two_per_sm(a.epi) && tiles * 2 <= sm_count() * 5 / 4) p.splits = 2;
+    if (p.splits > 1 && nk < 4 * p.splits) p.splits = nk / 4 > 1 ? nk / 4 : 1;
+  }
   if (tiles > (1 << 27) || a.batch > 65535) return THANOS_ERR_SHAPE;
   const int stage_bytes = A_BYTES + p.nt * BK * 2;
-  p.stages = (a.epi <= PROJ_SHRINK ? 100 : 200) * 1024 / stage_bytes;
+  p.stages = (two_per_sm(a.epi) ? 100 : 200) * 1024 / stage_bytes;
   if (p.stages > MAX_STAGES) p.stages = MAX_STAGES;
   p.ring_bytes = p.stages * stage_bytes;
-  p.tmem_cols = a.epi == PROJ_OUT ? 2 * p.nt : p.nt;  // the adapter part sits beside the sums
+  p.tmem_cols = a.epi == PROJ_OUT || f32 ? 2 * p.nt : p.nt;  // the adapter part sits beside the sums
   p.out = a.out;
   p.ldo = a.ldo;
   p.V = a.V;
@@ -1512,7 +1547,7 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
 
   CUtensorMap mA, mB, mP;
   const CUtensorMapSwizzle sw = CU_TENSOR_MAP_SWIZZLE_128B;
-  const int64_t slabs = a.f32 ? 3 : a.batch;
+  const int64_t slabs = f32 ? 3 : a.batch;
   const bool okA = a.a_mn ? make_map3(&mA, a.A, a.f16, a.M, a.K, a.lda, slabs, a.a_batch, 64, BK, sw)
                           : make_map3(&mA, a.A, a.f16, a.K, a.M, a.lda, slabs, a.a_batch, BK, TM, sw);
   if (!okA || !make_map3(&mB, a.B, a.f16, a.K, a.N, a.ldb, slabs, a.b_batch, BK,
@@ -1531,6 +1566,9 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
     case PROJ_OUT:
       return a.a_mn ? launch_any<true, PROJ_OUT>(pairs, mA, mB, mP, p, stream)
                     : launch_any<false, PROJ_OUT>(pairs, mA, mB, mP, p, stream);
+    case PROJ_OUT32:
+      return a.a_mn ? launch<true, PROJ_OUT32>(mA, mB, p, stream)
+                    : launch<false, PROJ_OUT32>(mA, mB, p, stream);
     case PROJ_SHRINK:
       return launch<false, PROJ_SHRINK>(mA, mB, p, stream);
     case PROJ_GRAM:

@@ -20,7 +20,9 @@ enum ProjEpilogue {
   PROJ_GRAM = 2,    // S = alpha D, fp16, symmetric: upper tiles computed, mirror written
   PROJ_POLY = 3,    // P = beta S + alpha D, fp16, symmetric
   PROJ_NEXT = 4,    // X' = beta (hi + lo) + alpha D, as two fp16 planes
-  PROJ_FINAL = 5    // the same value, unscaled, into O (bf16) or the new weights
+  PROJ_FINAL = 5,   // the same value, unscaled, into O (bf16) or the new weights
+  PROJ_OUT32 = 6    // PROJ_OUT with fp32 accuracy: A and B are three bf16 planes (a_batch, b_batch
+                    // apart), out and P are fp32
 };
 
 struct ProjArgs {
@@ -31,16 +33,14 @@ struct ProjArgs {
   const void* B = nullptr;
   int64_t ldb = 0, b_batch = 0;
   int f16 = 0;                   // operands fp16 instead of bf16
-  int f32 = 0;                   // PROJ_OUT with fp32 accuracy: A and B are three bf16 planes (a_batch,
-                                 // b_batch apart), out and P are fp32
   int epi = PROJ_OUT;
   int early = 0;                 // operands do not depend on the previous launch of the stream
   int first = 0;                 // first launch of its call: plain, and clears the status word
   const void* skinny = nullptr;  // PROJ_OUT of a few tokens: A [n, r, K], V is computed on the way (and
                                  // written, if wanted)
   int32_t* status = nullptr;
-  // PROJ_OUT, PROJ_SHRINK
-  void* out = nullptr;           // [N, ldo], bf16 (fp32 if f32)
+  // PROJ_OUT, PROJ_OUT32, PROJ_SHRINK
+  void* out = nullptr;           // [N, ldo], bf16 (OUT32: fp32)
   int64_t ldo = 0;
   float* V = nullptr;            // [N, r]: PROJ_OUT reads it (forward: V, backward: U); SHRINK writes
   __nv_bfloat16* planes = nullptr;  // SHRINK: V also as two bf16 planes, [N, 2 r16] (or null)
@@ -50,7 +50,7 @@ struct ProjArgs {
   // distinct adapters of every token tile of proj_pair_tile() tokens, [tiles] and [tiles, width]
   const int32_t* tile_count = nullptr;
   const int32_t* tile_list = nullptr;
-  const void* P = nullptr;       // PROJ_OUT: the adapters' wide factor, bf16
+  const void* P = nullptr;       // the adapters' wide factor, bf16 (OUT32: fp32)
   int64_t ldp = 0, p_adapter = 0;       // a_mn == 0: [n][M][ldp]; else [n][r][ldp].  On CTA pairs
                                         // ldp and p_adapter are multiples of 8
   // PROJ_GRAM .. PROJ_FINAL
