@@ -13,6 +13,8 @@
 // Every wait is bounded (see tc_common.cuh); on expiry the status word gets THANOS_ERR_TIMEOUT.
 #include "proj_gemm.cuh"
 
+#include <math.h>
+
 #include "adapter_grad.cuh"
 #include "tc_common.cuh"
 
@@ -475,9 +477,6 @@ __device__ __forceinline__ int tile_column(int S, int rank, int half, int q) {
   return 8 * (rank + S * (half + 2 * q));
 }
 
-__device__ __forceinline__ void prefetch_l2(const void* p) {
-  asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
-}
 __device__ __forceinline__ void epilogue_sync() {  // the eight epilogue warps of tile_kernel
   asm volatile("bar.sync 1, 256;" ::: "memory");
 }
@@ -539,15 +538,23 @@ __device__ __forceinline__ float dot8(const uint4& a, const uint4& b, float s) {
   return s;
 }
 
-__device__ __forceinline__ float dot16(const uint32_t (&w)[8], const float* __restrict__ v, float s) {
+__device__ __forceinline__ void unpack16(const uint32_t (&w)[8], float (&f)[16]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float2 u = unpack2(w[e]);
+    f[2 * e] = u.x;
+    f[2 * e + 1] = u.y;
+  }
+}
+__device__ __forceinline__ float dot16(const float (&w)[16], const float* __restrict__ v) {
+  float s = 0.f;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const float4 f = reinterpret_cast<const float4*>(v)[e];
-    const float2 a = unpack2(w[2 * e]), b = unpack2(w[2 * e + 1]);
-    s = fmaf(a.x, f.x, s);
-    s = fmaf(a.y, f.y, s);
-    s = fmaf(b.x, f.z, s);
-    s = fmaf(b.y, f.w, s);
+    s = fmaf(w[4 * e], f.x, s);
+    s = fmaf(w[4 * e + 1], f.y, s);
+    s = fmaf(w[4 * e + 2], f.z, s);
+    s = fmaf(w[4 * e + 3], f.w, s);
   }
   return s;
 }
@@ -577,30 +584,6 @@ __device__ __forceinline__ void wide_row_f32(const Params& p, int i, int m, int 
 #pragma unroll
     for (int j = 0; j < 16; ++j)
       if (j > last) w[j] = 0.f;
-  }
-}
-
-// The adapter part of eight tokens, columns c.. of the tile; a run of one request's tokens reads its
-// row once.
-template <bool AMN>
-__device__ __forceinline__ void wide_part_f32(const Params& p, const int* ids, const float* factor,
-                                              int c, int m, int j0, bool same, float (&own)[8]) {
-  float w[16];
-  if (same) {
-    if (ids[c] < 0) return;
-    wide_row_f32<AMN>(p, ids[c], m, j0, w);
-  }
-#pragma unroll 1
-  for (int e = 0; e < 8; ++e) {
-    if (ids[c + e] < 0) continue;
-    if (!same) wide_row_f32<AMN>(p, ids[c + e], m, j0, w);
-    const float* f = factor + (c + e) * 16;
-    float s = 0.f;
-#pragma unroll
-    for (int j = 0; j < 16; ++j) s = fmaf(w[j], f[j], s);
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-      if (k == e) own[k] = s;
   }
 }
 
@@ -687,16 +670,14 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
 
-  if constexpr (EPI != PROJ_SHRINK) {
-    if (!p.early) grid_dependency_wait();
-    grid_dependents_launch();
-  }
+  if constexpr (EPI != PROJ_SHRINK) grid_dependents_launch();
 
   const int nk1 = (p.K + BK - 1) / BK;
   const int nk = F32 ? 6 * nk1 : nk1;
   const int ks0 = (int)((int64_t)nk * rank / S), ks1 = (int)((int64_t)nk * (rank + 1) / S);
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
+    if (!p.early) grid_dependency_wait();
     if (elect_one()) {
     int s = 0;
     uint32_t phase = 0;
@@ -774,130 +755,149 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
     bool used = false;
     if constexpr (OUT) {
       // ---------------------------------------------------------- adapter part
-      if (!F32 && p.n_adapters > 0 && p.early) {
-        // the rows of the wide factors that this thread will read are on their way to L2 while the
-        // previous launch still computes V
-#pragma unroll 1
-        for (int q = 0; m < p.M; ++q) {
-          const int c = tile_column(S, rank, half, q);
-          if (c >= p.nt || n0 + c >= p.N) break;
-          for (int e = 0; e < 8 && n0 + c + e < p.N; ++e) {
-            const int i = valid_adapter(p, n0 + c + e);
-            if (i < 0 || (e > 0 && p.index[n0 + c + e - 1] == i)) continue;
-            const __nv_bfloat16* a = p.P + (int64_t)i * p.p_adapter;
-            if (AMN) {
-              for (int j = 0; j < p.r; ++j) prefetch_l2(a + (int64_t)j * p.ldp + m);
-            } else {
-              for (int j = 0; j < p.r; j += 16) prefetch_l2(a + (int64_t)m * p.ldp + j);
-            }
-          }
-        }
-      }
-      if (p.early) grid_dependency_wait();
+      const int tid = threadIdx.x - 64;
       if (p.n_adapters > 0) {
-        const int tid = threadIdx.x - 64;
         bool any = false;
         if (tid < p.nt) {
           const int t = n0 + tid;
           const int i = t < p.N ? valid_adapter(p, t) : -1;
           ids[tid] = i;
           any = i >= 0;
-          if (tm == 0 && rank == 0 && t < p.N && i < 0 && p.index[t] != -1)
-            atomicCAS(p.status, 0, (int)THANOS_ERR_INVALID_ARG);
         }
         used = epilogue_any(any);
-        int ldf = 16;                      // row of `factor`
-        if (!F32 && p.skinny) {
-          // V of the few tokens, by the CTAs that write their outputs: a warp per pair of ranks
-          ldf = (p.r + 15) & ~15;
-          const int live = min(p.nt, p.N - n0);
-          const bool mine = tile_column(S, rank, 0, 0) < live;
+      }
+      int ldf = 16;                      // row of `factor`
+      if (used && !F32 && p.skinny) {
+        // V of the few tokens, by the CTAs that write their outputs: a warp per pair of ranks
+        ldf = (p.r + 15) & ~15;
+        const int live = min(p.nt, p.N - n0);
+        const bool mine = tile_column(S, rank, 0, 0) < live;
 #pragma unroll 1
-          for (int e = 2 * (warp - 2); mine && e < live * ldf; e += 16) {
-            const int c = e / ldf, j = e - c * ldf, i = ids[c];
-            float s0 = 0.f, s1 = 0.f;
-            if (i >= 0 && j < p.r) {
-              const __nv_bfloat16* xr = p.x + (int64_t)(n0 + c) * p.ld_tok;
-              const __nv_bfloat16* a0 = p.skinny + ((int64_t)i * p.r + j) * p.K;
-              const __nv_bfloat16* a1 = a0 + (j + 1 < p.r ? p.K : 0);
+        for (int e = 2 * (warp - 2); mine && e < live * ldf; e += 16) {
+          const int c = e / ldf, j = e - c * ldf, i = ids[c];
+          float s0 = 0.f, s1 = 0.f;
+          if (i >= 0 && j < p.r) {
+            const __nv_bfloat16* xr = p.x + (int64_t)(n0 + c) * p.ld_tok;
+            const __nv_bfloat16* a0 = p.skinny + ((int64_t)i * p.r + j) * p.K;
+            const __nv_bfloat16* a1 = a0 + (j + 1 < p.r ? p.K : 0);
 #pragma unroll 8
-              for (int k = lane * 8; k < p.K; k += 256) {
-                const uint4 x = *reinterpret_cast<const uint4*>(xr + k);
-                s0 = dot8(x, *reinterpret_cast<const uint4*>(a0 + k), s0);
-                s1 = dot8(x, *reinterpret_cast<const uint4*>(a1 + k), s1);
-              }
-              for (int o = 16; o > 0; o >>= 1) {
-                s0 += __shfl_xor_sync(0xffffffffu, s0, o);
-                s1 += __shfl_xor_sync(0xffffffffu, s1, o);
-              }
-              if (j + 1 >= p.r) s1 = 0.f;
+            for (int k = lane * 8; k < p.K; k += 256) {
+              const uint4 x = *reinterpret_cast<const uint4*>(xr + k);
+              s0 = dot8(x, *reinterpret_cast<const uint4*>(a0 + k), s0);
+              s1 = dot8(x, *reinterpret_cast<const uint4*>(a1 + k), s1);
             }
-            if (lane < 2 && j + lane < ldf) {
-              const float v = lane ? s1 : s0;
-              if (tm == 0 && p.V && j + lane < p.r) p.V[(int64_t)(n0 + c) * p.r + j + lane] = v;
-              factor[e + lane] = i >= 0 && p.scale ? p.scale[i] * v : v;
+            for (int o = 16; o > 0; o >>= 1) {
+              s0 += __shfl_xor_sync(0xffffffffu, s0, o);
+              s1 += __shfl_xor_sync(0xffffffffu, s1, o);
             }
+            if (j + 1 >= p.r) s1 = 0.f;
           }
-        }
-#pragma unroll 1
-        for (int j0 = 0; j0 < p.r && used; j0 += 16) {
-          if (j0 > 0) epilogue_sync();
-          const float* fac = factor;
-          if (!F32 && p.skinny) {
-            fac += j0;
-          } else {
-#pragma unroll 1
-            for (int e = tid; e < p.nt * 16; e += 256) {
-              const int t = n0 + (e >> 4), j = j0 + (e & 15), i = ids[e >> 4];
-              float v = 0.f;
-              if (i >= 0 && j < p.r) {
-                v = p.V[(int64_t)t * p.r + j];
-                if (p.scale) v *= p.scale[i];
-              }
-              factor[e] = v;
-            }
-          }
-          epilogue_sync();
-#pragma unroll 1
-          for (int q = 0;; ++q) {
-            const int c = tile_column(S, rank, half, q);
-            if (c >= p.nt || n0 + c >= p.N) break;
-            float own[8] = {};
-            const int first = ids[c];
-            bool same = true;
-#pragma unroll
-            for (int e = 1; e < 8; ++e) same = same && ids[c + e] == first;
-            if constexpr (F32) {
-              if (m < p.M) wide_part_f32<AMN>(p, ids, fac, c, m, j0, same, own);
-            } else if (m < p.M) {
-              if (same) {  // a run of one request's tokens (or none): its row is read once
-                if (first >= 0) {
-                  uint32_t w[8];
-                  wide_row<AMN>(p, first, m, j0, w);
-#pragma unroll
-                  for (int e = 0; e < 8; ++e) own[e] = dot16(w, fac + (c + e) * ldf, 0.f);
-                }
-              } else {
-                uint32_t w[8][8];  // eight rows in flight
-#pragma unroll
-                for (int e = 0; e < 8; ++e) wide_row<AMN>(p, ids[c + e], m, j0, w[e]);
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                  if (ids[c + e] >= 0) own[e] = dot16(w[e], fac + (c + e) * ldf, 0.f);
-              }
-            }
-            __syncwarp();
-            // kept in tensor memory beside the accumulator, at the columns it belongs to
-            if (j0 > 0) {
-              float before[8];
-              tc_ld8(taddr + p.nt + c, before);
-#pragma unroll
-              for (int e = 0; e < 8; ++e) own[e] += before[e];
-            }
-            tc_st8(taddr + p.nt + c, own);
+          if (lane < 2 && j + lane < ldf) {
+            const float v = lane ? s1 : s0;
+            if (tm == 0 && p.V && j + lane < p.r) p.V[(int64_t)(n0 + c) * p.r + j + lane] = v;
+            factor[e + lane] = i >= 0 && p.scale ? p.scale[i] * v : v;
           }
         }
       }
+      // While the launch before this one still computes V, one round over the first ranks goes ahead
+      // with whatever is in `factor`: its result is written over, but it brings the rows of the wide
+      // factors and the code itself nearer (64 tokens of 64 adapters: the round that counts then takes
+      // 2 us instead of 9 us).
+      const bool ahead = used && (F32 || !p.skinny);
+      if (!ahead) grid_dependency_wait();
+#pragma unroll 1
+      for (int pass = ahead ? -1 : 0; used && pass * 16 < p.r; ++pass) {
+        const int j0 = max(pass, 0) * 16;
+        const float* fac = factor;
+        if (!F32 && p.skinny) {
+          fac += j0;
+          if (pass == 0) epilogue_sync();
+        } else if (pass >= 0) {
+          if (pass == 0) grid_dependency_wait();
+          epilogue_sync();
+#pragma unroll 4
+          for (int e = tid; e < p.nt * 16; e += 256) {
+            const int i = ids[e >> 4], j = j0 + (e & 15);
+            const bool live = i >= 0 && j < p.r;
+            const float v = live ? p.V[(int64_t)(n0 + (e >> 4)) * p.r + j] : 0.f;
+            const float f = live && p.scale ? p.scale[i] : 1.f;
+            factor[e] = f * v;
+          }
+          epilogue_sync();
+        }
+#pragma unroll 1
+        for (int q = 0;; ++q) {
+          const int c = tile_column(S, rank, half, q);
+          if (c >= p.nt || n0 + c >= p.N) break;
+          float own[8] = {};
+          // eight tokens of one request, some perhaps without adapter, share a row
+          int one = -1;
+          bool same = true;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int i = ids[c + e];
+            same = same && (i < 0 || one < 0 || i == one);
+            one = max(one, i);
+          }
+          if (m < p.M && one >= 0) {
+            if constexpr (F32) {
+              float w[16];
+              if (same) wide_row_f32<AMN>(p, one, m, j0, w);
+#pragma unroll 1
+              for (int e = 0; e < 8; ++e) {
+                if (ids[c + e] < 0) continue;
+                if (!same) wide_row_f32<AMN>(p, ids[c + e], m, j0, w);
+                const float d = dot16(w, fac + (c + e) * 16);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) own[k] = k == e ? d : own[k];
+              }
+            } else if (same) {
+              uint32_t w[8];
+              float f[16];
+              wide_row<AMN>(p, one, m, j0, w);
+              unpack16(w, f);
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if (ids[c + e] >= 0) own[e] = dot16(f, fac + (c + e) * ldf);
+            } else {
+#pragma unroll 1
+              for (int e4 = 0; e4 < 8; e4 += 4) {
+                uint32_t w[4][8];  // four rows in flight
+                float d[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) wide_row<AMN>(p, ids[c + e4 + e], m, j0, w[e]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  float f[16];
+                  unpack16(w[e], f);
+                  d[e] = ids[c + e4 + e] >= 0 ? dot16(f, fac + (c + e4 + e) * ldf) : 0.f;
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  own[e] = e4 == 0 ? d[e] : own[e];
+                  own[4 + e] = e4 == 4 ? d[e] : own[4 + e];
+                }
+              }
+            }
+          }
+          __syncwarp();
+          // kept in tensor memory beside the accumulator, at the columns it belongs to
+          if (pass > 0) {
+            float before[8];
+            tc_ld8(taddr + p.nt + c, before);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) own[e] += before[e];
+          }
+          tc_st8(taddr + p.nt + c, own);
+        }
+      }
+      // an index that names no adapter (after the status word was cleared)
+      if (p.n_adapters > 0 && tm == 0 && rank == 0 && tid < p.nt && n0 + tid < p.N) {
+        const int i = p.index[n0 + tid];
+        if (i != -1 && (i < 0 || i >= p.n_adapters)) atomicCAS(p.status, 0, (int)THANOS_ERR_INVALID_ARG);
+      }
+    } else {
+      grid_dependency_wait();
     }
     // ------------------------------------------------------------ epilogue, one slice of k
     const bool ok = mbar_wait(done_bar, 0, abort_flag);
@@ -1447,22 +1447,40 @@ bool use_pairs(int64_t M, int64_t N, int64_t batch, bool symmetric) {
 }  // namespace
 
 namespace {
-// Width of tile_kernel's tiles: the widest of 128, 64, 32 whose tiles occupy most of the device, no
-// wider than the next step above N.  Up to 64 tokens of a projection stay in one tile, so that the
-// weights are read once.  The skinny product has few rows and a long k, which is split first.
-int tile_width(int64_t M, int64_t N, int64_t batch, bool symmetric, int epi) {
-  int64_t want = (int64_t)sm_count() * 3 / 4;
-  if (epi == PROJ_OUT) want *= 2;           // two CTAs per SM
-  if (epi == PROJ_SHRINK) want = sm_count() / 10;
-  if (epi == PROJ_OUT32) want = sm_count() / 4;   // six times the k of the others
-  int nt = 128;
-  while (nt > 32) {
-    int64_t tiles = ceil_div(M, TM) * ceil_div(N, nt) * batch;
-    if (symmetric) tiles /= 2;
-    if (N > nt / 2 && (tiles >= want || (epi == PROJ_OUT && N <= 64))) break;
-    nt /= 2;
+// Width and k slices of tile_kernel's tiles, by the clocks that the busiest SM takes, as measured on
+// 768 x 768 products and on single tokens:
+//   a k step     what it brings in at 60 bytes per clock, at least 250 (issue and barriers)
+//   a CTA        2000 to start, 400 for eight columns of its epilogue (700 with operands to read)
+//   a cluster    1500, and 44 a column for the partial sums over distributed shared memory, more with
+//                more slices
+// Up to 64 tokens of a projection stay in one tile, so that the weights are read once.
+struct TileShape {
+  int nt, splits;
+};
+TileShape tile_shape(int64_t M, int64_t N, int64_t batch, int64_t nk, bool symmetric, int epi) {
+  const int64_t sms = sm_count(), tm = ceil_div(M, TM);
+  const bool one_tile = (epi == PROJ_OUT || epi == PROJ_OUT32) && N <= 64;
+  const double column = epi >= PROJ_POLY && epi <= PROJ_FINAL ? 700.0 : 400.0;
+  TileShape best = {128, 1};
+  double least = 0.0;
+  for (int nt = 128; nt >= 32; nt /= 2) {
+    if (nt > 32 && N <= nt / 2) continue;   // the next narrower one holds all of N
+    if (one_tile && N > nt) break;
+    int64_t tiles = tm * ceil_div(N, nt) * batch;
+    if (symmetric) tiles = (tiles + tm * batch * (TM / nt)) / 2;
+    const double step = fmax(250.0, (A_BYTES + nt * BK * 2) / 60.0);
+    for (int s = 1; s <= 8 && (s == 1 || nk >= 4 * s); ++s) {
+      const double load = (double)(tiles * s) / (double)sms;
+      const double rounds = load <= 1.0 ? 1.0 : two_per_sm(epi) && load <= 2.0 ? load : ceil(load);
+      double cta = (double)ceil_div(nk, s) * step + 2000.0 + column * (double)ceil_div(nt, 16 * s);
+      if (s > 1) cta += 1500.0 + 44.0 * nt * (1.0 + s / 8.0);
+      if (least == 0.0 || rounds * cta < least) {
+        least = rounds * cta;
+        best = {nt, s};
+      }
+    }
   }
-  return nt;
+  return best;
 }
 }  // namespace
 
@@ -1479,7 +1497,11 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
   p.K = a.K;
   const bool f32 = a.epi == PROJ_OUT32;
   const bool pairs = a.epi != PROJ_SHRINK && !f32 && use_pairs(a.M, a.N, a.batch, symmetric);
-  p.nt = pairs ? PTM : tile_width(a.M, a.N, a.batch, symmetric, a.epi);
+  const int nk = (a.K + BK - 1) / BK * (f32 ? 6 : 1);
+  const TileShape shape =
+      pairs ? TileShape{PTM, 1} : tile_shape(a.M, a.N, a.batch, nk, symmetric, a.epi);
+  p.nt = shape.nt;
+  p.splits = shape.splits;
   p.tiles_m = (a.M + (pairs ? PTM : TM) - 1) / (pairs ? PTM : TM);
   p.tiles_n = (a.N + p.nt - 1) / p.nt;
   p.batch_z = a.batch;
@@ -1488,19 +1510,7 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
   p.early = a.early;
   p.first = a.first;
   p.status = a.status;
-  int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * a.batch;
-  if (symmetric) tiles = (tiles + (int64_t)p.tiles_m * a.batch * (TM / p.nt)) / 2;
-  const int nk = (a.K + BK - 1) / BK * (f32 ? 6 : 1);
-  p.splits = 1;
-  // A split gives the SMs that have no tile a slice of k, one CTA to an SM; more cost more in partial
-  // sums than they bring (4096 x 4096, 1 token: 4 slices 12.4 us, 8 slices 14.4 us), but two slices may
-  // go a little over (11008 x 4096, 64 tokens, 86 tiles: 31 us instead of 37 us).
-  if (tiles < sm_count()) {
-    const int64_t most = sm_count() / tiles;
-    p.splits = (int)(most < 8 ? most : 8);
-    if (p.splits == 1 && two_per_sm(a.epi) && tiles * 2 <= sm_count() * 5 / 4) p.splits = 2;
-    if (p.splits > 1 && nk < 4 * p.splits) p.splits = nk / 4 > 1 ? nk / 4 : 1;
-  }
+  const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * a.batch;
   if (tiles > (1 << 27) || a.batch > 65535) return THANOS_ERR_SHAPE;
   const int stage_bytes = A_BYTES + p.nt * BK * 2;
   p.stages = (two_per_sm(a.epi) ? 100 : 200) * 1024 / stage_bytes;
