@@ -94,10 +94,8 @@ __device__ __forceinline__ void mma_step(uint32_t d, uint64_t ad, uint64_t bd, u
   }
 }
 
-__device__ __forceinline__ float ld_cluster(uint32_t addr) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr));
-  return v;
+__device__ __forceinline__ void st_cluster(uint32_t addr, float v) {
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
 }
 __device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t addr) {
   uint32_t v;
@@ -131,16 +129,20 @@ __device__ __forceinline__ void tc_ld16(uint32_t taddr, float (&v)[16]) {
 #pragma unroll
   for (int e = 0; e < 16; ++e) v[e] = __uint_as_float(u[e]);
 }
-__device__ __forceinline__ void tc_st8(uint32_t taddr, const float (&v)[8]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr),
-      "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])),
-      "r"(__float_as_uint(v[3])), "r"(__float_as_uint(v[4])), "r"(__float_as_uint(v[5])),
-      "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7]))
-      : "memory");
+__device__ __forceinline__ float tc_ld1(uint32_t taddr) {
+  uint32_t u;
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(u) : "r"(taddr) : "memory");
+  tc_wait_ld();
+  return __uint_as_float(u);
+}
+__device__ __forceinline__ void tc_st1(uint32_t taddr, float v) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(taddr),
+               "r"(__float_as_uint(v))
+               : "memory");
+}
+__device__ __forceinline__ void tc_wait_st() {
   asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
-
 __device__ __forceinline__ bool bf16_nonfinite(uint32_t h) { return (h & 0x7F80u) == 0x7F80u; }
 // any non-finite bf16 in a 16-byte vector
 __device__ __forceinline__ bool any_nonfinite(const uint4& q) {
@@ -477,6 +479,9 @@ __device__ __forceinline__ int tile_column(int S, int rank, int half, int q) {
   return 8 * (rank + S * (half + 2 * q));
 }
 
+__device__ __forceinline__ void prefetch_l2(const void* p) {
+  asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
+}
 __device__ __forceinline__ void epilogue_sync() {  // the eight epilogue warps of tile_kernel
   asm volatile("bar.sync 1, 256;" ::: "memory");
 }
@@ -519,6 +524,10 @@ __device__ __forceinline__ void wide_row(const Params& p, int i, int m, int j0, 
           w[4 * h + 2] = v.z;
           w[4 * h + 3] = v.w;
         }
+    } else if (p.r % 2 == 0) {
+#pragma unroll
+      for (int h = 0; h < 8; ++h)
+        if (j0 + 2 * h < p.r) w[h] = *reinterpret_cast<const uint32_t*>(q + 2 * h);
     } else {
 #pragma unroll
       for (int j = 0; j < 16; ++j)
@@ -799,21 +808,31 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
           }
         }
       }
-      // While the launch before this one still computes V, one round over the first ranks goes ahead
-      // with whatever is in `factor`: its result is written over, but it brings the rows of the wide
-      // factors and the code itself nearer (64 tokens of 64 adapters: the round that counts then takes
-      // 2 us instead of 9 us).
-      const bool ahead = used && (F32 || !p.skinny);
-      if (!ahead) grid_dependency_wait();
+      if (used && !F32 && p.early) {
+        // while the launch before this one still computes V, the rows of the wide factors that this
+        // thread will read are on their way to L2
 #pragma unroll 1
-      for (int pass = ahead ? -1 : 0; used && pass * 16 < p.r; ++pass) {
-        const int j0 = max(pass, 0) * 16;
+        for (int q = 0; m < p.M; ++q) {
+          const int c = tile_column(S, rank, half, q);
+          if (c >= p.nt || n0 + c >= p.N) break;
+#pragma unroll 1
+          for (int e = 0; e < 8; ++e) {
+            const int i = ids[c + e];
+            if (i < 0 || (e > 0 && ids[c + e - 1] == i)) continue;
+            const __nv_bfloat16* a =
+                p.P + (int64_t)i * p.p_adapter + (AMN ? (int64_t)m : (int64_t)m * p.ldp);
+            for (int jj = 0; jj < p.r; jj += AMN ? 1 : 16) prefetch_l2(a + jj * (AMN ? p.ldp : 1));
+          }
+        }
+      }
+      grid_dependency_wait();
+#pragma unroll 1
+      for (int j0 = 0; used && j0 < p.r; j0 += 16) {
         const float* fac = factor;
         if (!F32 && p.skinny) {
           fac += j0;
-          if (pass == 0) epilogue_sync();
-        } else if (pass >= 0) {
-          if (pass == 0) grid_dependency_wait();
+          if (j0 == 0) epilogue_sync();
+        } else {
           epilogue_sync();
 #pragma unroll 4
           for (int e = tid; e < p.nt * 16; e += 256) {
@@ -829,7 +848,6 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
         for (int q = 0;; ++q) {
           const int c = tile_column(S, rank, half, q);
           if (c >= p.nt || n0 + c >= p.N) break;
-          float own[8] = {};
           // eight tokens of one request, some perhaps without adapter, share a row
           int one = -1;
           bool same = true;
@@ -839,62 +857,48 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
             same = same && (i < 0 || one < 0 || i == one);
             one = max(one, i);
           }
-          if (m < p.M && one >= 0) {
-            if constexpr (F32) {
-              float w[16];
-              if (same) wide_row_f32<AMN>(p, one, m, j0, w);
+          if constexpr (F32) {
+            float w[16];
+            if (same && m < p.M) wide_row_f32<AMN>(p, one, m, j0, w);
 #pragma unroll 1
-              for (int e = 0; e < 8; ++e) {
-                if (ids[c + e] < 0) continue;
-                if (!same) wide_row_f32<AMN>(p, ids[c + e], m, j0, w);
-                const float d = dot16(w, fac + (c + e) * 16);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) own[k] = k == e ? d : own[k];
-              }
-            } else if (same) {
-              uint32_t w[8];
-              float f[16];
-              wide_row<AMN>(p, one, m, j0, w);
-              unpack16(w, f);
-#pragma unroll
-              for (int e = 0; e < 8; ++e)
-                if (ids[c + e] >= 0) own[e] = dot16(f, fac + (c + e) * ldf);
-            } else {
+            for (int e = 0; e < 8; ++e) {
+              const int i = ids[c + e];
+              if (!same && m < p.M && i >= 0) wide_row_f32<AMN>(p, i, m, j0, w);
+              float d = m < p.M && i >= 0 ? dot16(w, fac + (c + e) * 16) : 0.f;
+              if (j0 > 0) d += tc_ld1(taddr + p.nt + c + e);
+              tc_st1(taddr + p.nt + c + e, d);
+            }
+          } else if (same) {
+            uint32_t w[8];
+            float f[16];
+            wide_row<AMN>(p, m < p.M ? one : -1, m, j0, w);
+            unpack16(w, f);
 #pragma unroll 1
-              for (int e4 = 0; e4 < 8; e4 += 4) {
-                uint32_t w[4][8];  // four rows in flight
-                float d[4];
+            for (int e = 0; e < 8; ++e) {
+              float d = ids[c + e] >= 0 ? dot16(f, fac + (c + e) * ldf) : 0.f;
+              if (j0 > 0) d += tc_ld1(taddr + p.nt + c + e);
+              tc_st1(taddr + p.nt + c + e, d);
+            }
+          } else {
+#pragma unroll 1
+            for (int e4 = 0; e4 < 8; e4 += 4) {
+              uint32_t w[4][8];  // four rows in flight
 #pragma unroll
-                for (int e = 0; e < 4; ++e) wide_row<AMN>(p, ids[c + e4 + e], m, j0, w[e]);
+              for (int e = 0; e < 4; ++e)
+                wide_row<AMN>(p, m < p.M ? ids[c + e4 + e] : -1, m, j0, w[e]);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  float f[16];
-                  unpack16(w[e], f);
-                  d[e] = ids[c + e4 + e] >= 0 ? dot16(f, fac + (c + e4 + e) * ldf) : 0.f;
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  own[e] = e4 == 0 ? d[e] : own[e];
-                  own[4 + e] = e4 == 4 ? d[e] : own[4 + e];
-                }
+              for (int e = 0; e < 4; ++e) {
+                float f[16];
+                unpack16(w[e], f);
+                float d = ids[c + e4 + e] >= 0 ? dot16(f, fac + (c + e4 + e) * ldf) : 0.f;
+                if (j0 > 0) d += tc_ld1(taddr + p.nt + c + e4 + e);
+                tc_st1(taddr + p.nt + c + e4 + e, d);
               }
             }
           }
-          __syncwarp();
-          // kept in tensor memory beside the accumulator, at the columns it belongs to
-          if (pass > 0) {
-            float before[8];
-            tc_ld8(taddr + p.nt + c, before);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) own[e] += before[e];
-          }
-          tc_st8(taddr + p.nt + c, own);
         }
-      }
-      // an index that names no adapter (after the status word was cleared)
-      if (p.n_adapters > 0 && tm == 0 && rank == 0 && tid < p.nt && n0 + tid < p.N) {
-        const int i = p.index[n0 + tid];
-        if (i != -1 && (i < 0 || i >= p.n_adapters)) atomicCAS(p.status, 0, (int)THANOS_ERR_INVALID_ARG);
+        // the sums are kept in tensor memory beside the accumulator, at the columns they belong to
+        tc_wait_st();
       }
     } else {
       grid_dependency_wait();
@@ -918,52 +922,56 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
         emit<AMN, EPI, 8>(p, z, m, n0 + c, v, mirror, false);
         __syncwarp();
       }
-    } else if (ok) {
-      // partial sums [n][m] in the ring, whose operands have all been consumed
-      float* part = reinterpret_cast<float*>(smem);
-#pragma unroll 1
-      for (int c = 8 * half; c < p.nt; c += 16) {
-        float v[8];
-        tc_ld8(taddr + c, v);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) part[(c + e) * TM + row] = v[e];
-      }
     }
     if (S > 1) {
+      // Every CTA writes the sums of a group of eight columns to the CTA that owns it, into the ring
+      // there: [CTA][group][column][m].  The first barrier says that all rings are free.
       cluster_sync_all();
       bool bad = false;
+#pragma unroll 1
       for (int q = 0; q < S; ++q)
         bad = bad || ld_cluster_u32(map_to_cta(smem_u32((const void*)abort_flag), q)) != 0;
+      const int G = (p.nt / 8 + S - 1) / S;
+#pragma unroll 1
+      for (int c = 8 * half; c < p.nt && !bad; c += 16) {
+        float v[8];
+        tc_ld8(taddr + c, v);
+        const uint32_t dst = map_to_cta(smem_base, (c >> 3) % S) +
+                             (uint32_t)((((rank * G + (c >> 3) / S) * 8) * TM + row) * 4);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) st_cluster(dst + e * TM * 4, v[e]);
+      }
+      cluster_sync_all();
 #pragma unroll 1
       for (int q = 0; !bad; ++q) {
         const int c = tile_column(S, rank, half, q);
         if (c >= p.nt || n0 + c >= p.N) break;
         float f[8] = {};
         if (used) tc_ld8(taddr + p.nt + c, f);
-#pragma unroll 1
-        for (int k = 0; k < S; k += 2) {
-          const uint32_t a0 = map_to_cta(smem_base, k) + (uint32_t)(c * TM + row) * 4u;
-          const uint32_t a1 = map_to_cta(smem_base, min(k + 1, S - 1)) + (uint32_t)(c * TM + row) * 4u;
-          float x[8], y[8];
+        const float* part = reinterpret_cast<const float*>(smem) + ((c >> 3) / S * 8) * TM + row;
+#pragma unroll 2
+        for (int k = 0; k < S; ++k)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = ld_cluster(a0 + e * TM * 4);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] = ld_cluster(a1 + e * TM * 4);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] = (f[e] + x[e]) + (k + 1 < S ? y[e] : 0.f);
-        }
+          for (int e = 0; e < 8; ++e) f[e] += part[(k * G * 8 + e) * TM];
         emit<AMN, EPI, 8>(p, z, m, n0 + c, f, mirror, false);
         __syncwarp();
       }
     }
+    if constexpr (OUT) {
+      // an index that names no adapter (the status word has long been cleared)
+      const int t = n0 + (int)threadIdx.x - 64;
+      if (p.n_adapters > 0 && tm == 0 && rank == 0 && t < min(n0 + p.nt, p.N) && p.index[t] != -1 &&
+          valid_adapter(p, t) < 0)
+        atomicCAS(p.status, 0, (int)THANOS_ERR_INVALID_ARG);
+    }
   }
   if (S > 1 && warp < 2) {
     __syncwarp();
-    cluster_sync_all();  // the partial sums are there
+    cluster_sync_all();
+    cluster_sync_all();
   }
   tc_fence_before();
   __syncthreads();
-  if (S > 1) cluster_sync_all();  // no CTA leaves while another may still read its partial sums
   if (warp == 1) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base),
