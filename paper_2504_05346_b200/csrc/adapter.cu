@@ -25,7 +25,7 @@ using bf16 = __nv_bfloat16;
 //   [0, n_list)          the distinct adapters of a token tile, by first occurrence
 //   next n_copy          16-byte aligned copies: rows of dY, or the adapters' B with padded ranks
 //   next n_turn          B_i [c, r] -> [r, c] (the skinny product's operand in the backward pass)
-//   next n_planes        backward: V as two bf16 planes for dB, and the zeros beyond the rank of U's
+//   next n_planes        backward: V as three bf16 planes for dB, and the zeros beyond the rank of U's
 //   the rest             V of a few tokens, a CTA per token and four ranks
 struct FrontParams {
   int32_t* status;             // cleared here, or null
@@ -132,11 +132,11 @@ __device__ __forceinline__ void front_block(const FrontParams& p, float* sh) {
     const int r16 = (p.r + 15) & ~15, lane = tid & 31;
     for (int64_t t = (int64_t)blk * 8 + (tid >> 5); t < p.T; t += 8ll * p.n_planes) {
       for (int j = lane; j < r16; j += 32) {
-        bf16* v = p.v_planes + t * 2 * r16 + j;
-        split2(j < p.r ? p.Vin[t * p.r + j] : 0.f, v[0], v[r16]);
+        bf16* v = p.v_planes + t * 3 * r16 + j;
+        split3(j < p.r ? p.Vin[t * p.r + j] : 0.f, v[0], v[r16], v[2 * r16]);
         if (j >= p.r) {
-          bf16* u = p.u_planes + t * 2 * r16 + j;
-          u[0] = u[r16] = __float2bfloat16_rn(0.f);
+          bf16* u = p.u_planes + t * 3 * r16 + j;
+          u[0] = u[r16] = u[2 * r16] = __float2bfloat16_rn(0.f);
         }
       }
     }
@@ -215,7 +215,7 @@ struct Layout {
   int32_t* list;
   bf16* copy;        // padded B (forward) or dY (backward)
   bf16* turned;      // backward: B_i transposed
-  bf16* v_planes;    // backward: V and U as two bf16 planes
+  bf16* v_planes;    // backward: V and U as three bf16 planes
   bf16* u_planes;
   int32_t* order;    // backward: tokens by adapter
   int32_t* spare;
@@ -236,8 +236,8 @@ bool carve(Arena& ar, Layout& L, bool backward, int64_t T, int64_t c, int64_t b,
   if (backward && copy_dy) L.copy = ar.take<bf16>((size_t)T * round_up(c, 8));
   if (backward) {
     L.turned = ar.take<bf16>((size_t)n * r * round_up(c, 8));
-    L.v_planes = ar.take<bf16>((size_t)T * 2 * round_up(r, 16));
-    L.u_planes = ar.take<bf16>((size_t)T * 2 * round_up(r, 16));
+    L.v_planes = ar.take<bf16>((size_t)T * 3 * round_up(r, 16));
+    L.u_planes = ar.take<bf16>((size_t)T * 3 * round_up(r, 16));
     L.order = ar.take<int32_t>((size_t)T);
     L.spare = ar.take<int32_t>((size_t)T);
     L.off = ar.take<int32_t>((size_t)n + 1);
@@ -448,7 +448,7 @@ size_t adapter_workspace_bytes(bool backward, int64_t T, int64_t c, int64_t b, i
   // room for a copy of dY whose rows are not 16-byte aligned
   if (backward)
     need += round_up((size_t)T * c8 * 2, 256) + round_up((size_t)n * r * c8 * 2, 256) +
-            2 * round_up((size_t)T * 2 * round_up(r, 16) * 2, 256) + 2 * round_up((size_t)T * 4, 256) +
+            2 * round_up((size_t)T * 3 * round_up(r, 16) * 2, 256) + 2 * round_up((size_t)T * 4, 256) +
             round_up(((size_t)n + 1) * 4, 256);
   return need;
 }

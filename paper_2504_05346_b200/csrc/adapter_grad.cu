@@ -5,11 +5,12 @@
 // A CTA owns one adapter and 128 features; tokens come in the order of sort_tokens, so a tile never
 // mixes adapters (nothing that is not finite crosses from one to another) and needs no mask.
 //   warps 0..3   gather 64 tokens per stage by cp.async, in the MN-major layouts of the tensor cores:
-//                rows of Z (64 features x 64 tokens, 128-byte swizzle) and of R, which comes as two
-//                bf16 planes hi + lo side by side in n (16 significant bits, so that the result keeps
-//                fp32 quality with exact 16-bit products)
-//   warp 4       tcgen05.mma issuer, 128 x 2 r x 16
-//   warps 4..7   epilogue: hi + lo columns added, written (or added) to the gradient
+//                rows of Z (64 features x 64 tokens, 128-byte swizzle) and of R, which comes as three
+//                bf16 planes side by side in n (all 24 bits: the products with Z are exact)
+//   warp 4       tcgen05.mma issuer, 128 x 3 r x 16
+//   warps 4..7   epilogue: the planes' columns added, written (or added) to the gradient
+// The tensor cores cut what they add to an accumulator, by up to 2^-23 each time, so a CTA takes its
+// tokens in rounds of ROUND_TOKENS and adds the rounds' results rounded to nearest.
 // A cluster of up to eight CTAs splits the adapter's tokens when there are few tiles; the partial
 // sums are added over distributed shared memory in rank order (same inputs, same bits).
 #include "adapter_grad.cuh"
@@ -113,6 +114,7 @@ constexpr int GK = 64;                   // tokens per stage
 constexpr int GA_BYTES = GF * GK * 2;
 constexpr int G_MAX_STAGES = 6;
 constexpr int G_THREADS = 256;
+constexpr int ROUND_TOKENS = 512;
 
 struct GradParams {
   AdapterGradSide side[2];
@@ -120,7 +122,7 @@ struct GradParams {
   const int32_t* order;
   const int32_t* off;
   int32_t* status;
-  int n, r, r16, stages, splits, accumulate, ring_bytes;
+  int n, r, r16, stages, splits, accumulate, ring_bytes, stage_bytes;
   int tmem_cols;
 };
 
@@ -179,7 +181,7 @@ __global__ void __launch_bounds__(G_THREADS) grad_tc_kernel(const GradParams p) 
   const int tile = (int)(blockIdx.x / S);
   const AdapterGradSide& sd = tile < p.tiles0 ? p.side[0] : p.side[1];
   const int f0 = (tile < p.tiles0 ? tile : tile - p.tiles0) * GF;
-  const int F = sd.F, r = p.r, r16 = p.r16, N = 2 * r16;
+  const int F = sd.F, r = p.r, r16 = p.r16, N = 3 * r16;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.stages; ++s) {
@@ -201,7 +203,7 @@ __global__ void __launch_bounds__(G_THREADS) grad_tc_kernel(const GradParams p) 
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  const int stage_bytes = GA_BYTES + N * GK * 2;
+  const int stage_bytes = p.stage_bytes;
   // the ring and the barriers run on from adapter to adapter
   int s = 0, s_pub = 0;
   uint32_t phase = 0, done_phase = 0;
@@ -209,7 +211,7 @@ __global__ void __launch_bounds__(G_THREADS) grad_tc_kernel(const GradParams p) 
 
   grid_dependency_wait();
   for (int64_t i = blockIdx.y; i < p.n; i += gridDim.y) {
-    const int lo = p.off[i], len = p.off[i + 1] - lo;
+    const int first = p.off[i], len = p.off[i + 1] - first;
     if (len == 0) {
       // an adapter without tokens: zeros, or nothing to add
       if (!p.accumulate && rank == 0) {
@@ -220,7 +222,11 @@ __global__ void __launch_bounds__(G_THREADS) grad_tc_kernel(const GradParams p) 
       }
       continue;
     }
-    const int nk = (len + GK - 1) / GK;
+    for (int from = 0; from < len; from += S * ROUND_TOKENS) {
+    const int to = min(len, from + S * ROUND_TOKENS);   // tokens of this round
+    const int lo = first + from, len_r = to - from;
+    const bool add = p.accumulate || from > 0;
+    const int nk = (len_r + GK - 1) / GK;
     const int ks0 = (int)((int64_t)nk * rank / S), ks1 = (int)((int64_t)nk * (rank + 1) / S);
 
 
@@ -236,7 +242,7 @@ __global__ void __launch_bounds__(G_THREADS) grad_tc_kernel(const GradParams p) 
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int at = ks0 * GK + r8 + 16 * i;
-        next[i] = at < len ? p.order[lo + at] : -1;
+        next[i] = at < len_r ? p.order[lo + at] : -1;
       }
       for (int ks = ks0; ks < ks1 && ok; ++ks) {
         int tok[4];
@@ -244,7 +250,7 @@ __global__ void __launch_bounds__(G_THREADS) grad_tc_kernel(const GradParams p) 
         for (int i = 0; i < 4; ++i) {
           tok[i] = next[i];
           const int at = (ks + 1) * GK + r8 + 16 * i;
-          next[i] = at < len ? p.order[lo + at] : -1;
+          next[i] = at < len_r ? p.order[lo + at] : -1;
         }
         ok = mbar_wait(empty_bar(s), phase ^ 1u, abort_flag);
         if (!ok) break;
@@ -262,7 +268,7 @@ __global__ void __launch_bounds__(G_THREADS) grad_tc_kernel(const GradParams p) 
             cp_async16(st + box * (GA_BYTES / 2) + row * 128 + ((piece ^ (row & 7)) << 4),
                        bytes ? z + f : sd.Z, bytes);
           }
-          // R's row [hi | lo] into boxes of 32 n x 64 k: 64 bytes per k row, 64-byte swizzle
+          // R's row into boxes of 32 n x 64 k: 64 bytes per k row, 64-byte swizzle
           const __nv_bfloat16* R = sd.R + t * N;
           for (int g8 = piece; g8 < N / 8; g8 += 8)
             cp_async16(st + GA_BYTES + (g8 >> 2) * 4096 + row * 64 +
@@ -290,9 +296,11 @@ __global__ void __launch_bounds__(G_THREADS) grad_tc_kernel(const GradParams p) 
     } else {
       if (warp == 4) {
         // -------------------------------------------------------- MMA issuer
+        // an instruction has at most 256 columns
+        const int n1 = min(N, 256), n2 = N - n1;
         uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16);
-        idesc |= (uint32_t)(N >> 3) << 17;
         idesc |= (uint32_t)(GF >> 4) << 24;
+        const uint32_t id1 = idesc | (uint32_t)(n1 >> 3) << 17, id2 = idesc | (uint32_t)(n2 >> 3) << 17;
         if (elect_one()) {  // the same lane every time: it alone follows the ring
           for (int ks = ks0; ks < ks1 && ok; ++ks) {
             ok = mbar_wait(full_bar(s), phase, abort_flag);
@@ -300,10 +308,14 @@ __global__ void __launch_bounds__(G_THREADS) grad_tc_kernel(const GradParams p) 
             if (ok) {
               const uint32_t sa = smem_base + (uint32_t)s * stage_bytes, sb = sa + GA_BYTES;
 #pragma unroll
-              for (int k4 = 0; k4 < GK / 16; ++k4)
-                tc_mma_bf16(tmem_base, grad_desc(sa + k4 * 2048, GA_BYTES / 2, 1024, 2),
-                            grad_desc(sb + k4 * 1024, 4096, 512, 4), idesc,
-                            (ks > ks0 || k4 > 0) ? 1u : 0u);
+              for (int k4 = 0; k4 < GK / 16; ++k4) {
+                const uint64_t ad = grad_desc(sa + k4 * 2048, GA_BYTES / 2, 1024, 2);
+                const uint32_t acc = ks > ks0 || k4 > 0 ? 1u : 0u;
+                tc_mma_bf16(tmem_base, ad, grad_desc(sb + k4 * 1024, 4096, 512, 4), id1, acc);
+                if (n2 > 0)
+                  tc_mma_bf16(tmem_base + 256, ad, grad_desc(sb + 8 * 4096 + k4 * 1024, 4096, 512, 4),
+                              id2, acc);
+              }
               tc_commit(empty_bar(s));
             }
             if (++s == p.stages) {
@@ -326,12 +338,14 @@ __global__ void __launch_bounds__(G_THREADS) grad_tc_kernel(const GradParams p) 
         for (int j0 = 0; j0 < r16; j0 += 16) {
           float v[16];
           if (ks1 > ks0) {
-            uint32_t h[16], l[16];
+            uint32_t h[16], m[16], l[16];
             tc_ld16(taddr + j0, h);
-            tc_ld16(taddr + r16 + j0, l);
+            tc_ld16(taddr + r16 + j0, m);
+            tc_ld16(taddr + 2 * r16 + j0, l);
             tc_wait_ld();
 #pragma unroll
-            for (int e = 0; e < 16; ++e) v[e] = __uint_as_float(h[e]) + __uint_as_float(l[e]);
+            for (int e = 0; e < 16; ++e)
+              v[e] = __uint_as_float(h[e]) + (__uint_as_float(m[e]) + __uint_as_float(l[e]));
           } else {
 #pragma unroll
             for (int e = 0; e < 16; ++e) v[e] = 0.f;
@@ -344,7 +358,7 @@ __global__ void __launch_bounds__(G_THREADS) grad_tc_kernel(const GradParams p) 
                 if (j0 + e >= r) break;
                 float* o = sd.out + (sd.by_feature ? (i * F + f) * r + j0 + e
                                                    : (i * r + j0 + e) * (int64_t)F + f);
-                *o = p.accumulate ? *o + k * v[e] : k * v[e];
+                *o = add ? *o + k * v[e] : k * v[e];
               }
             }
           } else {
@@ -367,12 +381,13 @@ __global__ void __launch_bounds__(G_THREADS) grad_tc_kernel(const GradParams p) 
           v += grad_ld_cluster(map_to_cta(smem_base, q) + (uint32_t)(j * GF + row) * 4u);
         if (f < F) {
           float* o = sd.out + (sd.by_feature ? (i * F + f) * r + j : (i * r + j) * (int64_t)F + f);
-          *o = p.accumulate ? *o + k * v : k * v;
+          *o = add ? *o + k * v : k * v;
         }
       }
       cluster_sync_all();  // no CTA goes on while another may still read its partial sums
     }
     tc_fence_after();
+    }
   }
   tc_fence_before();
   __syncthreads();
@@ -418,19 +433,22 @@ thanos_status_t adapter_grads(const AdapterGradSide& a, const AdapterGradSide& b
   p.r = r;
   p.r16 = (r + 15) / 16 * 16;
   p.accumulate = accumulate;
-  const int N = 2 * p.r16;
+  const int N = 3 * p.r16;
   p.tmem_cols = 32;
   while (p.tmem_cols < N) p.tmem_cols *= 2;
-  const int stage_bytes = GA_BYTES + N * GK * 2;
-  // two CTAs share an SM, so that one gathers while the other finishes
-  p.stages = 100 * 1024 / stage_bytes;
+  p.stage_bytes = GA_BYTES + (int)round_up((size_t)N, 32) * GK * 2;
+  // Two CTAs share an SM, so that one gathers while the other finishes.  A CTA that needs all of
+  // tensor memory has to have the SM to itself: two clusters, each with a CTA that waits for the
+  // other's, would wait for ever.  Its ring is too large for two.
+  const int ring = p.tmem_cols > 256 ? 200 * 1024 : 100 * 1024;
+  p.stages = ring / p.stage_bytes;
   if (p.stages > G_MAX_STAGES) p.stages = G_MAX_STAGES;
-  p.ring_bytes = p.stages * stage_bytes;
+  p.ring_bytes = p.tmem_cols > 256 ? ring : p.stages * p.stage_bytes;
   if (p.ring_bytes < p.r16 * GF * 4) p.ring_bytes = p.r16 * GF * 4;
   const size_t smem = (size_t)p.ring_bytes + 1024 + 256;
   {
     static std::atomic<unsigned long long> done{0};
-    THANOS_CUDA(ensure_max_dyn_smem(grad_tc_kernel, 113 * 1024, done));
+    THANOS_CUDA(ensure_max_dyn_smem(grad_tc_kernel, 203 * 1024, done));
   }
   // Token slices: an SM takes in some 60 bytes per clock however many CTAs it holds, so the slices
   // are chosen for the SM with the most work (8192 tokens, 118 tiles: 5 slices 129 us, 2 slices

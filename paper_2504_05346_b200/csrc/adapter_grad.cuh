@@ -14,8 +14,8 @@ thanos_status_t sort_tokens(const int32_t* index, int64_t T, int64_t n, int32_t*
 struct AdapterGradSide {
   const __nv_bfloat16* Z = nullptr;  // [T, F], leading dimension ldz (multiple of 8)
   int64_t ldz = 0;
-  const __nv_bfloat16* R = nullptr;  // [T, 2 r16] with r16 = r rounded up to 16: R[t] as two bf16
-                                     // planes hi | lo, zeros beyond r
+  const __nv_bfloat16* R = nullptr;  // [T, 3 r16] with r16 = r rounded up to 16: R[t] as three bf16
+                                     // planes side by side, zeros beyond r
   const float* scale = nullptr;      // factor by adapter, or null
   float* out = nullptr;              // [n, r, F], or [n, F, r] if by_feature
   int F = 0;
@@ -27,11 +27,14 @@ thanos_status_t adapter_grads(const AdapterGradSide& a, const AdapterGradSide& b
                               const int32_t* order, const int32_t* off, int64_t T, int64_t n, int r,
                               int accumulate, int32_t* status, cudaStream_t stream);
 
-// x = hi + lo to 16 significant bits; what is not finite is in hi alone.
-__device__ __forceinline__ void split2(float x, __nv_bfloat16& hi, __nv_bfloat16& lo) {
-  hi = __float2bfloat16_rn(x);
-  const float h = __bfloat162float(hi);
-  lo = __float2bfloat16_rn(isfinite(h) ? x - h : 0.f);
+// x = h + m + l, all 24 bits; what is not finite is in h alone.
+__device__ __forceinline__ void split3(float x, __nv_bfloat16& h, __nv_bfloat16& m,
+                                       __nv_bfloat16& l) {
+  h = __float2bfloat16_rn(x);
+  const float hf = __bfloat162float(h);
+  const float rest = isfinite(hf) ? x - hf : 0.f;
+  m = __float2bfloat16_rn(rest);
+  l = __float2bfloat16_rn(rest - __bfloat162float(m));
 }
 
 }  // namespace thanos

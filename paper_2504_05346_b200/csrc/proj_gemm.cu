@@ -29,6 +29,7 @@ constexpr int BK = 64;
 constexpr int A_BYTES = TM * BK * 2;
 constexpr int MAX_STAGES = 10;
 constexpr int TILE_THREADS = 320;
+constexpr int DRAIN_STEPS = 8;
 constexpr int FACTOR_BYTES = 128 * 16 * 4;    // 16 ranks of up to 128 tokens, fp32
 
 struct Params {
@@ -139,6 +140,14 @@ __device__ __forceinline__ void tc_st1(uint32_t taddr, float v) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(taddr),
                "r"(__float_as_uint(v))
                : "memory");
+}
+__device__ __forceinline__ void tc_st8(uint32_t taddr, const float (&v)[8]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr),
+      "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])),
+      "r"(__float_as_uint(v[3])), "r"(__float_as_uint(v[4])), "r"(__float_as_uint(v[5])),
+      "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7]))
+      : "memory");
 }
 __device__ __forceinline__ void tc_wait_st() {
   asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
@@ -271,8 +280,8 @@ __device__ __forceinline__ void emit(const Params& p, int z, int m, int n0, floa
         p.V[(int64_t)t * p.r + j] = x;
         if (p.planes) {
           const int r16 = 16 * p.chunks;
-          __nv_bfloat16* row = p.planes + (int64_t)t * 2 * r16 + j;
-          split2(x, row[0], row[r16]);
+          __nv_bfloat16* row = p.planes + (int64_t)t * 3 * r16 + j;
+          split3(x, row[0], row[r16], row[2 * r16]);
         }
       } else if (own < 0 && i == 0) p.V[(int64_t)t * p.r + j] = 0.f;
     }
@@ -610,16 +619,16 @@ template <bool AMN, int EPI>
 __global__ void __launch_bounds__(TILE_THREADS, two_per_sm(EPI) ? 2 : 1)
 tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
             const Params p) {
-  constexpr bool F32 = EPI == PROJ_OUT32, OUT = EPI == PROJ_OUT || F32;
+  constexpr bool F32 = EPI == PROJ_OUT32, OUT = EPI == PROJ_OUT || F32, DRAIN = EPI == PROJ_SHRINK;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   float* factor = reinterpret_cast<float*>(smem + p.ring_bytes);             // [nt][16]
   int* ids = reinterpret_cast<int*>(smem + p.ring_bytes + FACTOR_BYTES);     // [nt]
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + p.ring_bytes + FACTOR_BYTES + 512);
-  // full [MAX_STAGES], empty [MAX_STAGES], accumulator ready
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * MAX_STAGES + 1);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 2 * MAX_STAGES + 2);
+  // full [MAX_STAGES], empty [MAX_STAGES], accumulator ready; SHRINK: accumulator full and empty (2)
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * MAX_STAGES + 5);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 2 * MAX_STAGES + 6);
 
   const int warp = threadIdx.x >> 5;
   const int lane = threadIdx.x & 31;
@@ -628,6 +637,8 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
   auto full_bar = [&](int s) { return bar_base + 8u * s; };
   auto empty_bar = [&](int s) { return bar_base + 8u * (MAX_STAGES + s); };
   const uint32_t done_bar = bar_base + 8u * (2 * MAX_STAGES);
+  auto tfull_bar = [&](int q) { return bar_base + 8u * (2 * MAX_STAGES + 1 + q); };
+  auto tempty_bar = [&](int q) { return bar_base + 8u * (2 * MAX_STAGES + 3 + q); };
 
   const int S = p.splits;
   const int rank = S > 1 ? (int)cluster_ctarank() : 0;
@@ -664,6 +675,10 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
       mbar_init(empty_bar(s), 1);
     }
     mbar_init(done_bar, 1);
+    for (int q = 0; q < 2; ++q) {
+      mbar_init(tfull_bar(q), 1);
+      mbar_init(tempty_bar(q), 8);
+    }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -738,12 +753,25 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
     uint32_t phase = 0;
     uint64_t at = 0;  // stage s in descriptor units
     bool ok = true;
+    int q = 0;
+    uint32_t tphase = 0;
     for (int ks = ks0; ks < ks1 && ok; ++ks) {
-      ok = mbar_wait(full_bar(s), phase, abort_flag);
+      const bool start = DRAIN ? (ks - ks0) % DRAIN_STEPS == 0 : ks == ks0;
+      if (DRAIN && start) {
+        ok = mbar_wait(tempty_bar(q), tphase ^ 1u, abort_flag);
+        tc_fence_after();
+      }
+      ok = ok && mbar_wait(full_bar(s), phase, abort_flag);
       tc_fence_after();
       if (ok) {
-        mma_step<AMN, false>(tmem_base, ad0 + at, bd0 + at, idesc, ks > ks0 ? 1u : 0u);
+        mma_step<AMN, false>(tmem_base + (uint32_t)(q * p.nt), ad0 + at, bd0 + at, idesc,
+                             start ? 0u : 1u);
         tc_commit(empty_bar(s));
+      }
+      if (DRAIN && ((ks - ks0) % DRAIN_STEPS == DRAIN_STEPS - 1 || ks + 1 == ks1)) {
+        if (ok) tc_commit(tfull_bar(q));
+        tphase ^= (uint32_t)q;
+        q ^= 1;
       }
       at += hop;
       if (++s == p.stages) {
@@ -904,8 +932,45 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
       grid_dependency_wait();
     }
     // ------------------------------------------------------------ epilogue, one slice of k
-    const bool ok = mbar_wait(done_bar, 0, abort_flag);
-    tc_fence_after();
+    bool ok = true;
+    if constexpr (DRAIN) {
+      // The tensor cores cut what they add to an accumulator, so a long chain of them drifts (128 of
+      // them: 2e-6 of V); after every DRAIN_STEPS steps the sums move on in registers, rounded.
+      float own[8][8] = {};
+      int q = 0;
+      uint32_t tphase = 0;
+      for (int ks = ks0; ks < ks1 && ok; ks += DRAIN_STEPS) {
+        ok = mbar_wait(tfull_bar(q), tphase, abort_flag);
+        tc_fence_after();
+        if (!ok) break;
+#pragma unroll
+        for (int g8 = 0; g8 < 8; ++g8) {
+          const int c = 8 * (half + 2 * g8);
+          if (c >= p.nt) break;
+          float v[8];
+          tc_ld8(taddr + q * p.nt + c, v);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) own[g8][e] += v[e];
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(tempty_bar(q));
+        tphase ^= (uint32_t)q;
+        q ^= 1;
+      }
+      // all products are done: the first accumulator takes the totals
+      if (ok) {
+#pragma unroll
+        for (int g8 = 0; g8 < 8; ++g8) {
+          const int c = 8 * (half + 2 * g8);
+          if (c < p.nt) tc_st8(taddr + c, own[g8]);
+        }
+        tc_wait_st();
+      }
+    } else {
+      ok = mbar_wait(done_bar, 0, abort_flag);
+      tc_fence_after();
+    }
     if (ok && S == 1) {
 #pragma unroll 1
       for (int q = 0;; ++q) {
@@ -1524,7 +1589,8 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
   p.stages = (two_per_sm(a.epi) ? 100 : 200) * 1024 / stage_bytes;
   if (p.stages > MAX_STAGES) p.stages = MAX_STAGES;
   p.ring_bytes = p.stages * stage_bytes;
-  p.tmem_cols = a.epi == PROJ_OUT || f32 ? 2 * p.nt : p.nt;  // the adapter part sits beside the sums
+  // the adapter part sits beside the sums; the skinny product has two accumulators
+  p.tmem_cols = two_per_sm(a.epi) ? 2 * p.nt : p.nt;
   p.out = a.out;
   p.ldo = a.ldo;
   p.V = a.V;

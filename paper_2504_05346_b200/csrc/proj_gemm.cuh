@@ -43,7 +43,7 @@ struct ProjArgs {
   void* out = nullptr;           // [N, ldo], bf16 (OUT32: fp32)
   int64_t ldo = 0;
   float* V = nullptr;            // [N, r]: PROJ_OUT reads it (forward: V, backward: U); SHRINK writes
-  __nv_bfloat16* planes = nullptr;  // SHRINK: V also as two bf16 planes, [N, 2 r16] (or null)
+  __nv_bfloat16* planes = nullptr;  // SHRINK: V also as three bf16 planes, [N, 3 r16] (or null)
   const int32_t* index = nullptr;
   const float* scale = nullptr;  // factor of a row of V by its adapter, or null
   int n_adapters = 0, r = 0;
