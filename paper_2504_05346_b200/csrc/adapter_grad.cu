@@ -4,13 +4,13 @@
 // bound (r up to 128: at most 256 flops per 2 bytes, below the tensor cores' balance of about 500).
 // A CTA owns one adapter and 128 features; tokens come in the order of sort_tokens, so a tile never
 // mixes adapters (nothing that is not finite crosses from one to another) and needs no mask.
-//   warps 0..3   gather 64 tokens per stage by cp.async, in the MN-major layouts of the tensor cores:
-//                rows of Z (64 features x 64 tokens, 128-byte swizzle) and of R, which comes as three
+//   warps 0..3   gather 32 tokens per stage by cp.async, in the MN-major layouts of the tensor cores:
+//                rows of Z (64 features x 32 tokens, 128-byte swizzle) and of R, which comes as three
 //                bf16 planes side by side in n (all 24 bits: the products with Z are exact)
 //   warp 4       tcgen05.mma issuer, 128 x 3 r x 16
-//   warps 4..7   epilogue: the planes' columns added, written (or added) to the gradient
-// The tensor cores cut what they add to an accumulator, by up to 2^-23 each time, so a CTA takes its
-// tokens in rounds of ROUND_TOKENS and adds the rounds' results rounded to nearest.
+//   warps 5..8   the sums: the tensor cores cut what they add to an accumulator, by up to 2^-23 each
+//                time, so it is drained into registers, rounded to nearest, every 512 tokens; at the
+//                end written (or added) to the gradient
 // A cluster of up to eight CTAs splits the adapter's tokens when there are few tiles; the partial
 // sums are added over distributed shared memory in rank order (same inputs, same bits).
 #include "adapter_grad.cuh"
@@ -110,11 +110,13 @@ sort_kernel(const int32_t* __restrict__ index, int T, int n, int32_t* order, int
 
 // ----------------------------------------------------------------------------------- gradients
 constexpr int GF = 128;                  // features per CTA
-constexpr int GK = 64;                   // tokens per stage
-constexpr int GA_BYTES = GF * GK * 2;
-constexpr int G_MAX_STAGES = 6;
-constexpr int G_THREADS = 256;
-constexpr int ROUND_TOKENS = 512;
+constexpr int GK = 32;                   // tokens per stage
+constexpr int BOX_BYTES = 64 * GK * 2;   // 64 features x GK tokens
+constexpr int RBOX_BYTES = 32 * GK * 2;  // 32 columns of R x GK tokens
+constexpr int GA_BYTES = 2 * BOX_BYTES;
+constexpr int G_MAX_STAGES = 8;
+constexpr int G_THREADS = 288;
+constexpr int DRAIN_STAGES = 16;         // 512 tokens between two drains of the accumulator
 
 struct GradParams {
   AdapterGradSide side[2];
@@ -123,7 +125,7 @@ struct GradParams {
   const int32_t* off;
   int32_t* status;
   int n, r, r16, stages, splits, accumulate, ring_bytes, stage_bytes;
-  int tmem_cols;
+  int tmem_cols, buffers;                // accumulators: 2 where they fit half of tensor memory
 };
 
 __device__ __forceinline__ uint64_t grad_desc(uint32_t addr, uint32_t lbo, uint32_t sbo,
@@ -163,18 +165,22 @@ __device__ __forceinline__ void publish(uint32_t bar, int lane) {
   if (lane == 0) mbar_arrive(bar);
 }
 
-__global__ void __launch_bounds__(G_THREADS) grad_tc_kernel(const GradParams p) {
+// RMAX: ranks whose sums a thread holds: 32, 64 (two CTAs per SM) or 128.
+template <int RMAX>
+__global__ void __launch_bounds__(G_THREADS, RMAX <= 64 ? 2 : 1) grad_tc_kernel(const GradParams p) {
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + p.ring_bytes);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * G_MAX_STAGES + 1);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 2 * G_MAX_STAGES + 2);
+  // full, empty (G_MAX_STAGES each), accumulator full (2), accumulator empty (2)
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * G_MAX_STAGES + 4);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 2 * G_MAX_STAGES + 5);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t smem_base = smem_u32(smem), bar_base = smem_u32(bars);
   auto full_bar = [&](int s) { return bar_base + 8u * s; };
   auto empty_bar = [&](int s) { return bar_base + 8u * (G_MAX_STAGES + s); };
-  const uint32_t done_bar = bar_base + 8u * (2 * G_MAX_STAGES);
+  auto tfull_bar = [&](int q) { return bar_base + 8u * (2 * G_MAX_STAGES + q); };
+  auto tempty_bar = [&](int q) { return bar_base + 8u * (2 * G_MAX_STAGES + 2 + q); };
 
   const int S = p.splits;
   const int rank = S > 1 ? (int)cluster_ctarank() : 0;
@@ -188,7 +194,10 @@ __global__ void __launch_bounds__(G_THREADS) grad_tc_kernel(const GradParams p) 
       mbar_init(full_bar(s), 4);
       mbar_init(empty_bar(s), 1);
     }
-    mbar_init(done_bar, 1);
+    for (int q = 0; q < 2; ++q) {
+      mbar_init(tfull_bar(q), 1);
+      mbar_init(tempty_bar(q), 4);
+    }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -204,14 +213,14 @@ __global__ void __launch_bounds__(G_THREADS) grad_tc_kernel(const GradParams p) 
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
   const int stage_bytes = p.stage_bytes;
-  // the ring and the barriers run on from adapter to adapter
-  int s = 0, s_pub = 0;
-  uint32_t phase = 0, done_phase = 0;
+  // the ring, the accumulators and their barriers run on from adapter to adapter
+  int s = 0, s_pub = 0, q = 0;
+  uint32_t phase = 0, tphase = 0;
   bool ok = true;
 
   grid_dependency_wait();
   for (int64_t i = blockIdx.y; i < p.n; i += gridDim.y) {
-    const int first = p.off[i], len = p.off[i + 1] - first;
+    const int lo = p.off[i], len = p.off[i + 1] - lo;
     if (len == 0) {
       // an adapter without tokens: zeros, or nothing to add
       if (!p.accumulate && rank == 0) {
@@ -222,62 +231,58 @@ __global__ void __launch_bounds__(G_THREADS) grad_tc_kernel(const GradParams p) 
       }
       continue;
     }
-    for (int from = 0; from < len; from += S * ROUND_TOKENS) {
-    const int to = min(len, from + S * ROUND_TOKENS);   // tokens of this round
-    const int lo = first + from, len_r = to - from;
-    const bool add = p.accumulate || from > 0;
-    const int nk = (len_r + GK - 1) / GK;
+    const int nk = (len + GK - 1) / GK;
     const int ks0 = (int)((int64_t)nk * rank / S), ks1 = (int)((int64_t)nk * (rank + 1) / S);
-
 
     if (warp < 4) {
       // ---------------------------------------------------------- gather
       // eight lanes a row, so that a copy instruction of a warp covers four whole lines; a thread
-      // takes rows r8 + 16 i and, in them, every eighth 16-byte piece
+      // takes rows r8 and r8 + 16 and, in them, every eighth 16-byte piece
       const int r8 = threadIdx.x >> 3, piece = threadIdx.x & 7;
-      const int lag = p.stages > 2 ? 2 : 1;
+      const int lag = p.stages > 4 ? 3 : p.stages - 1;
       int pending = 0;
       // the tokens of the next stage are looked up while this one's copies are issued
-      int next[4];
+      int next[2];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int at = ks0 * GK + r8 + 16 * i;
-        next[i] = at < len_r ? p.order[lo + at] : -1;
+      for (int u = 0; u < 2; ++u) {
+        const int at = ks0 * GK + r8 + 16 * u;
+        next[u] = at < len ? p.order[lo + at] : -1;
       }
       for (int ks = ks0; ks < ks1 && ok; ++ks) {
-        int tok[4];
+        int tok[2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          tok[i] = next[i];
-          const int at = (ks + 1) * GK + r8 + 16 * i;
-          next[i] = at < len_r ? p.order[lo + at] : -1;
+        for (int u = 0; u < 2; ++u) {
+          tok[u] = next[u];
+          const int at = (ks + 1) * GK + r8 + 16 * u;
+          next[u] = at < len ? p.order[lo + at] : -1;
         }
         ok = mbar_wait(empty_bar(s), phase ^ 1u, abort_flag);
         if (!ok) break;
         const uint32_t st = smem_base + (uint32_t)s * stage_bytes;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int row = r8 + 16 * i;
-          const int64_t t = tok[i] < 0 ? 0 : tok[i];
+        for (int u = 0; u < 2; ++u) {
+          const int row = r8 + 16 * u;
+          const int64_t t = tok[u] < 0 ? 0 : tok[u];
           const __nv_bfloat16* z = sd.Z + t * sd.ldz;
 #pragma unroll
           for (int box = 0; box < 2; ++box) {
             const int f = f0 + 64 * box + 8 * piece;
-            const int left = tok[i] < 0 ? 0 : (F - f) * 2;
+            const int left = tok[u] < 0 ? 0 : (F - f) * 2;
             const uint32_t bytes = left <= 0 ? 0u : left < 16 ? (uint32_t)left : 16u;
-            cp_async16(st + box * (GA_BYTES / 2) + row * 128 + ((piece ^ (row & 7)) << 4),
+            cp_async16(st + box * BOX_BYTES + row * 128 + ((piece ^ (row & 7)) << 4),
                        bytes ? z + f : sd.Z, bytes);
           }
-          // R's row into boxes of 32 n x 64 k: 64 bytes per k row, 64-byte swizzle
+          // R's row into boxes of 32 n: 64 bytes per k row, 64-byte swizzle
           const __nv_bfloat16* R = sd.R + t * N;
           for (int g8 = piece; g8 < N / 8; g8 += 8)
-            cp_async16(st + GA_BYTES + (g8 >> 2) * 4096 + row * 64 +
+            cp_async16(st + GA_BYTES + (g8 >> 2) * RBOX_BYTES + row * 64 +
                            (((g8 & 3) ^ ((row >> 1) & 3)) << 4),
-                       R + 8 * g8, tok[i] < 0 ? 0u : 16u);
+                       R + 8 * g8, tok[u] < 0 ? 0u : 16u);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
         if (++pending > lag) {
-          if (lag == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
+          if (lag == 3) asm volatile("cp.async.wait_group 3;" ::: "memory");
+          else if (lag == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
           else asm volatile("cp.async.wait_group 1;" ::: "memory");
           publish(full_bar(s_pub), lane);
           if (++s_pub == p.stages) s_pub = 0;
@@ -293,100 +298,122 @@ __global__ void __launch_bounds__(G_THREADS) grad_tc_kernel(const GradParams p) 
         publish(full_bar(s_pub), lane);
         if (++s_pub == p.stages) s_pub = 0;
       }
-    } else {
-      if (warp == 4) {
-        // -------------------------------------------------------- MMA issuer
-        // an instruction has at most 256 columns
-        const int n1 = min(N, 256), n2 = N - n1;
-        uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16);
-        idesc |= (uint32_t)(GF >> 4) << 24;
-        const uint32_t id1 = idesc | (uint32_t)(n1 >> 3) << 17, id2 = idesc | (uint32_t)(n2 >> 3) << 17;
-        if (elect_one()) {  // the same lane every time: it alone follows the ring
-          for (int ks = ks0; ks < ks1 && ok; ++ks) {
-            ok = mbar_wait(full_bar(s), phase, abort_flag);
-            tc_fence_after();
-            if (ok) {
-              const uint32_t sa = smem_base + (uint32_t)s * stage_bytes, sb = sa + GA_BYTES;
+    } else if (warp == 4) {
+      // ---------------------------------------------------------- MMA issuer
+      // an instruction has at most 256 columns
+      const int n1 = min(N, 256), n2 = N - n1;
+      uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16);
+      idesc |= (uint32_t)(GF >> 4) << 24;
+      const uint32_t id1 = idesc | (uint32_t)(n1 >> 3) << 17, id2 = idesc | (uint32_t)(n2 >> 3) << 17;
+      if (elect_one()) {  // the same lane every time: it alone follows the ring
+        for (int ks = ks0; ks < ks1 && ok; ++ks) {
+          const bool start = (ks - ks0) % DRAIN_STAGES == 0;
+          if (start) ok = mbar_wait(tempty_bar(q), tphase ^ 1u, abort_flag);
+          ok = ok && mbar_wait(full_bar(s), phase, abort_flag);
+          tc_fence_after();
+          if (ok) {
+            const uint32_t sa = smem_base + (uint32_t)s * stage_bytes, sb = sa + GA_BYTES;
+            const uint32_t d = tmem_base + (uint32_t)(q * N);
 #pragma unroll
-              for (int k4 = 0; k4 < GK / 16; ++k4) {
-                const uint64_t ad = grad_desc(sa + k4 * 2048, GA_BYTES / 2, 1024, 2);
-                const uint32_t acc = ks > ks0 || k4 > 0 ? 1u : 0u;
-                tc_mma_bf16(tmem_base, ad, grad_desc(sb + k4 * 1024, 4096, 512, 4), id1, acc);
-                if (n2 > 0)
-                  tc_mma_bf16(tmem_base + 256, ad, grad_desc(sb + 8 * 4096 + k4 * 1024, 4096, 512, 4),
-                              id2, acc);
-              }
-              tc_commit(empty_bar(s));
+            for (int k2 = 0; k2 < GK / 16; ++k2) {
+              const uint64_t ad = grad_desc(sa + k2 * 2048, BOX_BYTES, 1024, 2);
+              const uint32_t acc = start && k2 == 0 ? 0u : 1u;
+              tc_mma_bf16(d, ad, grad_desc(sb + k2 * 1024, RBOX_BYTES, 512, 4), id1, acc);
+              if (n2 > 0)
+                tc_mma_bf16(d + 256, ad,
+                            grad_desc(sb + 8 * RBOX_BYTES + k2 * 1024, RBOX_BYTES, 512, 4), id2, acc);
             }
-            if (++s == p.stages) {
-              s = 0;
-              phase ^= 1u;
+            tc_commit(empty_bar(s));
+          }
+          if (++s == p.stages) {
+            s = 0;
+            phase ^= 1u;
+          }
+          if ((ks - ks0) % DRAIN_STAGES == DRAIN_STAGES - 1 || ks + 1 == ks1) {
+            if (ok) tc_commit(tfull_bar(q));
+            if (++q == p.buffers) {
+              q = 0;
+              tphase ^= 1u;
             }
           }
-          if (ok) tc_commit(done_bar);
         }
-        __syncwarp();
       }
-      // ---------------------------------------------------------- epilogue, one slice of tokens
-      ok = ok && mbar_wait(done_bar, done_phase, abort_flag);
-      done_phase ^= 1u;
-      tc_fence_after();
+      __syncwarp();
+    } else {
+      // ---------------------------------------------------------- sums of this slice of tokens
       const int g = warp & 3;
       const uint32_t taddr = tmem_base + ((uint32_t)(32 * g) << 16);
       const int row = 32 * g + lane, f = f0 + row;
+      float acc[RMAX / 16][16] = {};
+      for (int ks = ks0; ks < ks1 && ok; ks += DRAIN_STAGES) {
+        ok = mbar_wait(tfull_bar(q), tphase, abort_flag);
+        tc_fence_after();
+        if (!ok) break;
+#pragma unroll
+        for (int j16 = 0; j16 < RMAX / 16; ++j16) {
+          if (16 * j16 >= r16) break;
+          const uint32_t at = taddr + (uint32_t)(q * N + 16 * j16);
+          uint32_t h[16], m[16], l[16];
+          tc_ld16(at, h);
+          tc_ld16(at + r16, m);
+          tc_ld16(at + 2 * r16, l);
+          tc_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            acc[j16][e] += __uint_as_float(h[e]) + (__uint_as_float(m[e]) + __uint_as_float(l[e]));
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(tempty_bar(q));
+        if (++q == p.buffers) {
+          q = 0;
+          tphase ^= 1u;
+        }
+      }
       if (ok) {
-        for (int j0 = 0; j0 < r16; j0 += 16) {
-          float v[16];
-          if (ks1 > ks0) {
-            uint32_t h[16], m[16], l[16];
-            tc_ld16(taddr + j0, h);
-            tc_ld16(taddr + r16 + j0, m);
-            tc_ld16(taddr + 2 * r16 + j0, l);
-            tc_wait_ld();
+        const float k = sd.scale ? sd.scale[i] : 1.f;
+        float* part = reinterpret_cast<float*>(smem);  // the ring, whose operands are consumed
 #pragma unroll
-            for (int e = 0; e < 16; ++e)
-              v[e] = __uint_as_float(h[e]) + (__uint_as_float(m[e]) + __uint_as_float(l[e]));
-          } else {
+        for (int j16 = 0; j16 < RMAX / 16; ++j16) {
+          if (16 * j16 >= r16) break;
+          if (S > 1) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) v[e] = 0.f;
-          }
-          if (S == 1) {
-            if (f < F) {
-              const float k = sd.scale ? sd.scale[i] : 1.f;
+            for (int e = 0; e < 16; ++e) part[(16 * j16 + e) * GF + row] = acc[j16][e];
+          } else if (f < F) {
+            float* o = sd.out + (sd.by_feature ? (i * F + f) * r + 16 * j16
+                                               : (i * r + 16 * j16) * (int64_t)F + f);
+            const int64_t step = sd.by_feature ? 1 : F;
 #pragma unroll
-              for (int e = 0; e < 16; ++e) {
-                if (j0 + e >= r) break;
-                float* o = sd.out + (sd.by_feature ? (i * F + f) * r + j0 + e
-                                                   : (i * r + j0 + e) * (int64_t)F + f);
-                *o = add ? *o + k * v[e] : k * v[e];
-              }
+            for (int e = 0; e < 16; ++e) {
+              if (16 * j16 + e >= r) break;
+              o[e * step] = p.accumulate ? o[e * step] + k * acc[j16][e] : k * acc[j16][e];
             }
-          } else {
-            float* part = reinterpret_cast<float*>(smem);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) part[(j0 + e) * GF + row] = v[e];
           }
         }
       }
     }
-    tc_fence_before();
     __syncthreads();
     if (S > 1) {
       cluster_sync_all();
       const float k = sd.scale ? sd.scale[i] : 1.f;
-      const int row = threadIdx.x & 127, f = f0 + row;
-      for (int j = rank + S * (threadIdx.x >> 7); j < r; j += 2 * S) {
+      // ranks in turn to the CTAs, a feature a thread; the slices' sums are in flight together
+#pragma unroll 1
+      for (int e = threadIdx.x; e < (r - rank + S - 1) / S * GF; e += G_THREADS) {
+        const int j = rank + S * (e / GF), row = e % GF, f = f0 + row;
+        float part[8];
+#pragma unroll
+        for (int w = 0; w < 8; ++w)
+          part[w] = w < S ? grad_ld_cluster(map_to_cta(smem_base, w) + (uint32_t)(j * GF + row) * 4u)
+                          : 0.f;
         float v = 0.f;
-        for (int q = 0; q < S; ++q)
-          v += grad_ld_cluster(map_to_cta(smem_base, q) + (uint32_t)(j * GF + row) * 4u);
+#pragma unroll
+        for (int w = 0; w < 8; ++w) v += part[w];
         if (f < F) {
           float* o = sd.out + (sd.by_feature ? (i * F + f) * r + j : (i * r + j) * (int64_t)F + f);
-          *o = add ? *o + k * v : k * v;
+          *o = p.accumulate ? *o + k * v : k * v;
         }
       }
       cluster_sync_all();  // no CTA goes on while another may still read its partial sums
-    }
-    tc_fence_after();
     }
   }
   tc_fence_before();
@@ -398,6 +425,29 @@ __global__ void __launch_bounds__(G_THREADS) grad_tc_kernel(const GradParams p) 
                  : "memory");
   }
   if (threadIdx.x == 0 && *abort_flag) atomicCAS(p.status, 0, (int)THANOS_ERR_TIMEOUT);
+}
+
+template <int RMAX>
+thanos_status_t launch_grads(const GradParams& p, cudaStream_t stream) {
+  static std::atomic<unsigned long long> done{0};
+  THANOS_CUDA(ensure_max_dyn_smem(grad_tc_kernel<RMAX>, 203 * 1024, done));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(p.tiles * p.splits), (unsigned)(p.n < 65535 ? p.n : 65535), 1);
+  cfg.blockDim = dim3(G_THREADS, 1, 1);
+  cfg.dynamicSmemBytes = (size_t)p.ring_bytes + 1024 + 256;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)p.splits;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  count_launch();
+  THANOS_CUDA(cudaLaunchKernelEx(&cfg, grad_tc_kernel<RMAX>, p));
+  return THANOS_OK;
 }
 
 }  // namespace
@@ -434,8 +484,9 @@ thanos_status_t adapter_grads(const AdapterGradSide& a, const AdapterGradSide& b
   p.r16 = (r + 15) / 16 * 16;
   p.accumulate = accumulate;
   const int N = 3 * p.r16;
+  p.buffers = 2 * N <= 256 ? 2 : 1;
   p.tmem_cols = 32;
-  while (p.tmem_cols < N) p.tmem_cols *= 2;
+  while (p.tmem_cols < p.buffers * N) p.tmem_cols *= 2;
   p.stage_bytes = GA_BYTES + (int)round_up((size_t)N, 32) * GK * 2;
   // Two CTAs share an SM, so that one gathers while the other finishes.  A CTA that needs all of
   // tensor memory has to have the SM to itself: two clusters, each with a CTA that waits for the
@@ -445,11 +496,6 @@ thanos_status_t adapter_grads(const AdapterGradSide& a, const AdapterGradSide& b
   if (p.stages > G_MAX_STAGES) p.stages = G_MAX_STAGES;
   p.ring_bytes = p.tmem_cols > 256 ? ring : p.stages * p.stage_bytes;
   if (p.ring_bytes < p.r16 * GF * 4) p.ring_bytes = p.r16 * GF * 4;
-  const size_t smem = (size_t)p.ring_bytes + 1024 + 256;
-  {
-    static std::atomic<unsigned long long> done{0};
-    THANOS_CUDA(ensure_max_dyn_smem(grad_tc_kernel, 203 * 1024, done));
-  }
   // Token slices: an SM takes in some 60 bytes per clock however many CTAs it holds, so the slices
   // are chosen for the SM with the most work (8192 tokens, 118 tiles: 5 slices 129 us, 2 slices
   // 181 us), as long as a slice keeps some hundred tokens.
@@ -463,23 +509,9 @@ thanos_status_t adapter_grads(const AdapterGradSide& a, const AdapterGradSide& b
       p.splits = k;
     }
   }
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(p.tiles * p.splits), (unsigned)(n < 65535 ? n : 65535), 1);
-  cfg.blockDim = dim3(G_THREADS, 1, 1);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = (unsigned)p.splits;
-  attr[0].val.clusterDim.y = 1;
-  attr[0].val.clusterDim.z = 1;
-  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[1].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 2;
-  count_launch();
-  THANOS_CUDA(cudaLaunchKernelEx(&cfg, grad_tc_kernel, p));
-  return THANOS_OK;
+  return p.r16 <= 32   ? launch_grads<32>(p, stream)
+         : p.r16 <= 64 ? launch_grads<64>(p, stream)
+                       : launch_grads<128>(p, stream);
 }
 
 }  // namespace thanos
