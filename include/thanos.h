@@ -346,11 +346,14 @@ thanos_status_t thanos_fp32_fma_probe(float* out, int64_t out_elems, int32_t cta
  *  A        device [n_adapters, r, b] of dtype, dense.   B  device [n_adapters, c, r], dense.
  *  index    device int32 [n_tok], -1 or 0 <= index < n_adapters, in any order.  Any other value is
  *           taken as -1 and reported in the status word (THANOS_ERR_INVALID_ARG).
- *  scale    device fp32 [n_adapters]: s_i.
+ *  scale    device fp32 [n_adapters]: s_i.  index and scale may start anywhere (4-byte aligned: a
+ *           slice of a batch's index will do), every other pointer on 16 bytes.
  *  n_adapters may be 0: then A, B, scale, index are not read and V is not written (all may be NULL).
  *  8 <= b <= 65536, b % 8 == 0; 1 <= c <= 2^20; 0 <= n_tok <= 2^24 (0 is a no-op);
- *  1 <= r <= 128 (ignored when n_adapters is 0).
- *  Sums are fp32.  With 16-bit types s_i V[t] is rounded to bf16 before it meets B_i, and Y once.
+ *  1 <= r <= 128 (ignored when n_adapters is 0); ceil(max(c, b, n_adapters r) / 128) *
+ *  ceil(n_tok / 32) <= 2^27.
+ *  Sums are fp32.  With 16-bit types s_i V[t] is rounded to bf16 before it meets B_i where the
+ *  product is large (its 256 x 256 tiles give half of the SM pairs work), and Y once.
  *  workspace: thanos_adapter_workspace_bytes(0, ...) bytes.  Its first int32 is the device status
  *           word of the call, cleared when the call starts.
  * The result does not depend on the order of concurrent work: the same inputs give the same bits.

@@ -12,6 +12,10 @@ constexpr int64_t MAX_FEATURES_OUT = 1 << 20;
 constexpr int64_t MAX_TOKENS = 1 << 24;
 constexpr int64_t MAX_ADAPTERS = 1 << 20;
 constexpr int MAX_RANK = 128;
+constexpr int64_t MAX_TILES = 1 << 27;
+
+// index and scale are read one value at a time: a slice of a batch's index is taken as it is
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 bool known_dtype(thanos_dtype_t d) { return d == THANOS_F32 || d == THANOS_BF16; }
 
@@ -22,6 +26,10 @@ thanos_status_t adapter_shape(int64_t T, int64_t c, int64_t b, int64_t n, int32_
       T > MAX_TOKENS || n < 0 || n > MAX_ADAPTERS)
     return THANOS_ERR_SHAPE;
   if (n > 0 && (r < 1 || r > MAX_RANK)) return THANOS_ERR_SHAPE;
+  // what a launch's grid holds, with the narrowest tiles
+  int64_t rows = c > b ? c : b;
+  if (n > 0 && n * r > rows) rows = n * r;
+  if (ceil_div(rows, 128) * ceil_div(T, 32) > MAX_TILES) return THANOS_ERR_SHAPE;
   return THANOS_OK;
 }
 
@@ -86,7 +94,7 @@ thanos_status_t thanos_adapter_forward(void* Y, int64_t ldy, float* V, const voi
   if (ldy < c || ldx < b || ldw < b) return THANOS_ERR_SHAPE;
   if (ldx % 8 || ldw % 8) return THANOS_ERR_ALIGNMENT;
   if (!aligned16(Y) || !aligned16(V) || !aligned16(X) || !aligned16(W) || !aligned16(A) ||
-      !aligned16(B) || !aligned16(index) || !aligned16(scale) || !aligned16(workspace))
+      !aligned16(B) || !aligned4(index) || !aligned4(scale) || !aligned16(workspace))
     return THANOS_ERR_ALIGNMENT;
   if (!workspace ||
       ws_bytes < thanos_adapter_workspace_bytes(0, n_tok, c, b, n_adapters, r, dtype))
@@ -134,8 +142,8 @@ thanos_status_t thanos_adapter_backward(void* dX, int64_t lddx, float* dA, float
   if (lddy < c || ldw < b || (dX && lddx < b) || (grads && ldx < b)) return THANOS_ERR_SHAPE;
   if (ldw % 8 || (grads && ldx % 8)) return THANOS_ERR_ALIGNMENT;
   if (!aligned16(dX) || !aligned16(dA) || !aligned16(dB) || !aligned16(dY) || !aligned16(V) ||
-      !aligned16(X) || !aligned16(W) || !aligned16(A) || !aligned16(B) || !aligned16(index) ||
-      !aligned16(scale) || !aligned16(workspace))
+      !aligned16(X) || !aligned16(W) || !aligned16(A) || !aligned16(B) || !aligned4(index) ||
+      !aligned4(scale) || !aligned16(workspace))
     return THANOS_ERR_ALIGNMENT;
   if (!workspace ||
       ws_bytes < thanos_adapter_workspace_bytes(1, n_tok, c, b, n_adapters, r, dtype))
