@@ -5,7 +5,8 @@
 // planes are made here, in the same launch that computes the skinny product V (or U) in fp32.  The
 // adapters' gradients are plain fp32 sums, bound by reading their operands.
 //
-//   front_f32_kernel    planes of the activations and of W; V or U, a warp per token and eight ranks
+//   front_f32_kernel    planes of the activations and of W; V or U, a warp per token and eight ranks, or
+//                       the planes that PROJ_SHRINK32 computes it from
 //   proj_gemm           out = in W^T (or in W) + the adapter's part
 //   grad_f32_kernel     both gradients: 32 features and up to 8 ranks of one adapter per CTA, eight
 //                       warps share the adapter's tokens, in the order of sort_tokens
@@ -32,7 +33,10 @@ struct SplitJob {
 };
 
 struct Front32Params {
-  SplitJob in, w;
+  SplitJob in, w, p;     // p: the narrow factor A, where the skinny product runs on the tensor cores
+  int n_turn;            // or B_i^T, turned on the way: blocks
+  __nv_bfloat16* turned; // [3][n r, turn_ld]
+  int64_t turn_ld;
   int32_t* status;       // cleared here
   float* R;              // [T, r]
   const float* P;        // forward: A [n, r, K]; backward: B [n, K, r]
@@ -74,6 +78,31 @@ __device__ void split_job(const SplitJob& s, int blk) {
   }
 }
 
+// Planes of every B_i [K, r] turned round, 64 rows at a time through shared memory.
+__device__ void turn_job(const Front32Params& p, int blk) {
+  __shared__ float sh[32][65];
+  const int tiles = (p.K + 63) / 64;
+  const int64_t units = (int64_t)p.n * tiles, plane = (int64_t)p.n * p.r * p.turn_ld;
+  for (int64_t u = blk; u < units; u += p.n_turn) {
+    const int64_t i = u / tiles;
+    const int k0 = (int)(u - i * tiles) * 64;
+    for (int j0 = 0; j0 < p.r; j0 += 32) {
+      const int nj = min(32, p.r - j0);
+      __syncthreads();
+      for (int e = threadIdx.x; e < 64 * nj; e += 256) {
+        const int row = e / nj, j = e - row * nj;
+        if (k0 + row < p.K) sh[j][row] = p.P[(i * p.K + k0 + row) * p.r + j0 + j];
+      }
+      __syncthreads();
+      for (int e = threadIdx.x; e < 64 * nj; e += 256) {
+        const int j = e >> 6, row = e & 63;
+        if (k0 + row < p.K)
+          store_split3(p.turned + (i * p.r + j0 + j) * p.turn_ld + k0 + row, plane, sh[j][row]);
+      }
+    }
+  }
+}
+
 constexpr int RANKS = 8;
 
 __global__ void __launch_bounds__(256) front_f32_kernel(const Front32Params p) {
@@ -90,6 +119,16 @@ __global__ void __launch_bounds__(256) front_f32_kernel(const Front32Params p) {
     return;
   }
   blk -= p.w.blocks;
+  if (blk < p.p.blocks) {
+    split_job(p.p, blk);
+    return;
+  }
+  blk -= p.p.blocks;
+  if (blk < p.n_turn) {
+    turn_job(p, blk);
+    return;
+  }
+  blk -= p.n_turn;
   const int lane = threadIdx.x & 31;
   const int groups = (p.r + RANKS - 1) / RANKS;
   const int64_t w = (int64_t)blk * 8 + (threadIdx.x >> 5);
@@ -224,21 +263,39 @@ struct Layout32 {
   float* R;
   __nv_bfloat16* in;
   __nv_bfloat16* w;
+  __nv_bfloat16* p;
   int32_t* order;
   int32_t* spare;
   int32_t* off;
   int64_t k8, w8;
 };
 
+// Where the skinny product is computed.  On the ALUs every token reads its adapter's narrow factor
+// anew, whole lines of A_i forward, pieces of rows of B_i backward; on the tensor cores
+// (PROJ_SHRINK32) the factors are split into planes first and the product is a launch of its own.
+// 2000 tokens, K = 2048, one adapter, launch with the planes (25 us) and the product:
+//   rank          16    32    64
+//   forward   ALUs 41    54    75 us     tensor cores 32 to 35 us, but a launch that the wide product
+//   backward  ALUs 62   157   282 us     waits for (16 adapters of rank 16, forward: 74 against 58 us)
+// Adapters in excess of the tokens that use them are not worth their planes.
+bool shrink_on_tensor_cores(bool back, int64_t T, int64_t n, int r) {
+  return T * r >= (back ? 16384 : 65536) && n * r <= 2 * T;
+}
+
 template <typename Take>
 void layout32(Layout32& L, bool back, int64_t T, int64_t c, int64_t b, int64_t n, int r, Take take) {
   const int64_t K = back ? c : b;
-  L.k8 = (int64_t)round_up((size_t)K, 8);
-  L.w8 = back ? (int64_t)round_up((size_t)b, 8) : L.k8;   // W's planes keep W's own rows
+  // Rows of whole 128-byte lines: TMA fetches a tile's row that straddles two lines twice (c = b =
+  // 1000, 2000 tokens: the wide product takes 46 us instead of 78).
+  L.k8 = (int64_t)round_up((size_t)K, 64);
+  L.w8 = back ? (int64_t)round_up((size_t)b, 64) : L.k8;  // W's planes keep W's own rows
   L.status = static_cast<int32_t*>(take(256));
   L.R = static_cast<float*>(take((size_t)T * r * 4));
   L.in = static_cast<__nv_bfloat16*>(take((size_t)3 * T * L.k8 * 2));
   L.w = static_cast<__nv_bfloat16*>(take((size_t)3 * c * L.w8 * 2));
+  L.p = nullptr;
+  if (shrink_on_tensor_cores(back, T, n, r))
+    L.p = static_cast<__nv_bfloat16*>(take((size_t)3 * n * r * L.k8 * 2));
   L.order = L.spare = L.off = nullptr;
   if (back) {
     L.order = static_cast<int32_t*>(take((size_t)T * 4));
@@ -282,12 +339,15 @@ thanos_status_t adapter_f32(bool back, const AdapterArgs& a, void* workspace, si
   f.status = L.status;
   f.in.src = static_cast<const float*>(a.in);
   f.in.ld = a.ldi;
-  if (a.out) {
+  const bool tc = a.n > 0 && shrink_on_tensor_cores(back, a.T, a.n, a.r);
+  if (a.out || tc) {
     f.in.rows = a.T;
     f.in.cols = K;
     f.in.planes = L.in;
     f.in.ldp = L.k8;
     f.in.blocks = split_blocks(a.T);
+  }
+  if (a.out) {
     f.w.src = static_cast<const float*>(a.W);
     f.w.ld = a.ldw;
     f.w.rows = a.c;
@@ -307,12 +367,47 @@ thanos_status_t adapter_f32(bool back, const AdapterArgs& a, void* workspace, si
     f.n = (int)a.n;
     f.r = a.r;
     f.back = back;
-    skinny = ceil_div(a.T * ceil_div(a.r, RANKS), 8);
+    if (!tc) {
+      skinny = ceil_div(a.T * ceil_div(a.r, RANKS), 8);
+    } else if (back) {
+      const int64_t units = a.n * ceil_div(K, 64);
+      f.n_turn = (int)(units < 4 * NUM_SMS ? units : 4 * NUM_SMS);
+      f.turned = L.p;
+      f.turn_ld = L.k8;
+    } else {
+      f.p.src = f.P;
+      f.p.ld = K;
+      f.p.rows = a.n * a.r;
+      f.p.cols = K;
+      f.p.planes = L.p;
+      f.p.ldp = L.k8;
+      f.p.blocks = split_blocks(f.p.rows);
+    }
   }
-  const int64_t blocks = f.in.blocks + f.w.blocks + skinny;
+  const int64_t blocks = f.in.blocks + f.w.blocks + f.p.blocks + f.n_turn + skinny;
   if (blocks > 0) {
     front_f32_kernel<<<(unsigned)blocks, 256, 0, stream>>>(f);
     THANOS_CHECK_LAUNCH();
+    if (tc) {
+      ProjArgs s;
+      s.epi = PROJ_SHRINK32;
+      s.M = (int)(a.n * a.r);
+      s.N = (int)a.T;
+      s.K = K;
+      s.A = L.p;
+      s.lda = L.k8;
+      s.a_batch = a.n * a.r * L.k8;
+      s.B = L.in;
+      s.ldb = L.k8;
+      s.b_batch = a.T * L.k8;
+      s.status = L.status;
+      s.V = R;
+      s.index = a.index;
+      s.scale = back ? a.scale : nullptr;
+      s.n_adapters = (int)a.n;
+      s.r = a.r;
+      THANOS_TRY(proj_gemm(s, stream));
+    }
     if (a.dA) THANOS_TRY(sort_tokens(a.index, a.T, a.n, L.order, L.spare, L.off, L.status, stream));
   } else {
     THANOS_CUDA(cudaMemsetAsync(L.status, 0, 16, stream));

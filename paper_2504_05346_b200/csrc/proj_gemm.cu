@@ -268,7 +268,7 @@ __device__ __forceinline__ void emit(const Params& p, int z, int m, int n0, floa
 #pragma unroll
     for (int e = 0; e < NC; ++e)
       if (e < nc) out[(int64_t)e * p.ldo] = __float2bfloat16_rn(v[e]);
-  } else if constexpr (EPI == PROJ_SHRINK) {
+  } else if constexpr (EPI == PROJ_SHRINK || EPI == PROJ_SHRINK32) {
     const int i = m / p.r, j = m - i * p.r;
 #pragma unroll
     for (int e = 0; e < NC; ++e) {
@@ -613,13 +613,17 @@ __device__ __forceinline__ void plane_pair(int combo, int& a, int& b) {
   b = (0x001021 >> (4 * combo)) & 15;
 }
 
-__host__ __device__ constexpr bool two_per_sm(int epi) { return epi <= PROJ_SHRINK || epi == PROJ_OUT32; }
+__host__ __device__ constexpr bool two_per_sm(int epi) {
+  return epi <= PROJ_SHRINK || epi >= PROJ_OUT32;
+}
 
 template <bool AMN, int EPI>
 __global__ void __launch_bounds__(TILE_THREADS, two_per_sm(EPI) ? 2 : 1)
 tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
             const Params p) {
-  constexpr bool F32 = EPI == PROJ_OUT32, OUT = EPI == PROJ_OUT || F32, DRAIN = EPI == PROJ_SHRINK;
+  constexpr bool F32 = EPI == PROJ_OUT32, OUT = EPI == PROJ_OUT || F32;
+  constexpr bool DRAIN = EPI == PROJ_SHRINK || EPI == PROJ_SHRINK32;
+  constexpr bool PLANES = F32 || EPI == PROJ_SHRINK32;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -653,7 +657,7 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
   // (nt divides TM)
   if (p.symmetric && n0 < m0) return;
   const bool mirror = n0 >= m0 + TM;
-  if constexpr (EPI == PROJ_SHRINK) {
+  if constexpr (DRAIN) {
     // rows of adapters that no token of the tile uses are not needed (tile row 0 also writes the
     // zeros of tokens without adapter)
     grid_dependency_wait();
@@ -694,10 +698,10 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
 
-  if constexpr (EPI != PROJ_SHRINK) grid_dependents_launch();
+  if constexpr (!DRAIN) grid_dependents_launch();
 
   const int nk1 = (p.K + BK - 1) / BK;
-  const int nk = F32 ? 6 * nk1 : nk1;
+  const int nk = PLANES ? 6 * nk1 : nk1;
   const int ks0 = (int)((int64_t)nk * rank / S), ks1 = (int)((int64_t)nk * (rank + 1) / S);
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
@@ -711,7 +715,7 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
       if (ok) {
         const uint32_t dst = smem_base + (uint32_t)s * stage_bytes;
         int k0 = ks * BK, za = z, zb = z;
-        if (F32) {
+        if (PLANES) {
           const int combo = ks / nk1;
           k0 = (ks - combo * nk1) * BK;
           plane_pair(combo, za, zb);
@@ -872,6 +876,8 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
           }
           epilogue_sync();
         }
+        float w[16];
+        int held = -1;  // the adapter whose row w is
 #pragma unroll 1
         for (int q = 0;; ++q) {
           const int c = tile_column(S, rank, half, q);
@@ -885,39 +891,50 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
             same = same && (i < 0 || one < 0 || i == one);
             one = max(one, i);
           }
-          if constexpr (F32) {
-            float w[16];
-            if (same && m < p.M) wide_row_f32<AMN>(p, one, m, j0, w);
-#pragma unroll 1
-            for (int e = 0; e < 8; ++e) {
-              const int i = ids[c + e];
-              if (!same && m < p.M && i >= 0) wide_row_f32<AMN>(p, i, m, j0, w);
-              float d = m < p.M && i >= 0 ? dot16(w, fac + (c + e) * 16) : 0.f;
-              if (j0 > 0) d += tc_ld1(taddr + p.nt + c + e);
-              tc_st1(taddr + p.nt + c + e, d);
+          if (F32 || same) {
+            // the row stays in registers from one eight to the next while the request stays the same
+            if (same && one >= 0 && one != held && m < p.M) {
+              if constexpr (F32) {
+                wide_row_f32<AMN>(p, one, m, j0, w);
+              } else {
+                uint32_t u[8];
+                wide_row<AMN>(p, one, m, j0, u);
+                unpack16(u, w);
+              }
+              held = one;
             }
-          } else if (same) {
-            uint32_t w[8];
-            float f[16];
-            wide_row<AMN>(p, m < p.M ? one : -1, m, j0, w);
-            unpack16(w, f);
+            if (same && j0 > 0) {
+              // further ranks: eight columns of sums are fetched, added to and put back together
+              float d[8];
+              tc_ld8(taddr + p.nt + c, d);
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if (m < p.M && ids[c + e] >= 0) d[e] += dot16(w, fac + (c + e) * ldf);
+              tc_st8(taddr + p.nt + c, d);
+            } else {
 #pragma unroll 1
-            for (int e = 0; e < 8; ++e) {
-              float d = ids[c + e] >= 0 ? dot16(f, fac + (c + e) * ldf) : 0.f;
-              if (j0 > 0) d += tc_ld1(taddr + p.nt + c + e);
-              tc_st1(taddr + p.nt + c + e, d);
+              for (int e = 0; e < 8; ++e) {
+                const int i = ids[c + e];
+                if constexpr (F32) {
+                  if (!same && m < p.M && i >= 0) wide_row_f32<AMN>(p, i, m, j0, w);
+                }
+                float d = m < p.M && i >= 0 ? dot16(w, fac + (c + e) * ldf) : 0.f;
+                if (F32 && j0 > 0) d += tc_ld1(taddr + p.nt + c + e);
+                tc_st1(taddr + p.nt + c + e, d);
+              }
+              if (!same) held = -1;
             }
           } else {
 #pragma unroll 1
             for (int e4 = 0; e4 < 8; e4 += 4) {
-              uint32_t w[4][8];  // four rows in flight
+              uint32_t u[4][8];  // four rows in flight
 #pragma unroll
               for (int e = 0; e < 4; ++e)
-                wide_row<AMN>(p, m < p.M ? ids[c + e4 + e] : -1, m, j0, w[e]);
+                wide_row<AMN>(p, m < p.M ? ids[c + e4 + e] : -1, m, j0, u[e]);
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
                 float f[16];
-                unpack16(w[e], f);
+                unpack16(u[e], f);
                 float d = ids[c + e4 + e] >= 0 ? dot16(f, fac + (c + e4 + e) * ldf) : 0.f;
                 if (j0 > 0) d += tc_ld1(taddr + p.nt + c + e4 + e);
                 tc_st1(taddr + p.nt + c + e4 + e, d);
@@ -1568,7 +1585,7 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
   p.M = a.M;
   p.N = a.N;
   p.K = a.K;
-  const bool f32 = a.epi == PROJ_OUT32;
+  const bool f32 = a.epi >= PROJ_OUT32;
   const bool pairs = a.epi != PROJ_SHRINK && !f32 && use_pairs(a.M, a.N, a.batch, symmetric);
   const int nk = (a.K + BK - 1) / BK * (f32 ? 6 : 1);
   const TileShape shape =
@@ -1655,6 +1672,8 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
                     : launch<false, PROJ_OUT32>(mA, mB, p, stream);
     case PROJ_SHRINK:
       return launch<false, PROJ_SHRINK>(mA, mB, p, stream);
+    case PROJ_SHRINK32:
+      return launch<false, PROJ_SHRINK32>(mA, mB, p, stream);
     case PROJ_GRAM:
       return launch_any<false, PROJ_GRAM>(pairs, mA, mB, mP, p, stream);
     case PROJ_POLY:

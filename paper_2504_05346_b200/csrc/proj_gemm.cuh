@@ -21,8 +21,9 @@ enum ProjEpilogue {
   PROJ_POLY = 3,    // P = beta S + alpha D, fp16, symmetric
   PROJ_NEXT = 4,    // X' = beta (hi + lo) + alpha D, as two fp16 planes
   PROJ_FINAL = 5,   // the same value, unscaled, into O (bf16) or the new weights
-  PROJ_OUT32 = 6    // PROJ_OUT with fp32 accuracy: A and B are three bf16 planes (a_batch, b_batch
+  PROJ_OUT32 = 6,   // PROJ_OUT with fp32 accuracy: A and B are three bf16 planes (a_batch, b_batch
                     // apart), out and P are fp32
+  PROJ_SHRINK32 = 7 // PROJ_SHRINK with fp32 accuracy, planes as in OUT32
 };
 
 struct ProjArgs {
@@ -39,7 +40,7 @@ struct ProjArgs {
   const void* skinny = nullptr;  // PROJ_OUT of a few tokens: A [n, r, K], V is computed on the way (and
                                  // written, if wanted)
   int32_t* status = nullptr;
-  // PROJ_OUT, PROJ_OUT32, PROJ_SHRINK
+  // PROJ_OUT, PROJ_SHRINK and their fp32 forms
   void* out = nullptr;           // [N, ldo], bf16 (OUT32: fp32)
   int64_t ldo = 0;
   float* V = nullptr;            // [N, r]: PROJ_OUT reads it (forward: V, backward: U); SHRINK writes
