@@ -686,8 +686,8 @@ size_t orthogonal_workspace_bytes(int64_t batch, int64_t m, int64_t n) {
            round_up(k * small_chunks(batch > 0 ? batch : 1, s, l) * round_up(s, 4) * round_up(s, 4) * 4,
                     256) +
            round_up(k * s * s * 4, 256);
-  return 256 + round_up(k * MAX_PARTS * 8, 256) + 4 * round_up(k * s * round_up(l, 8) * 2, 256) +
-         2 * round_up(k * s * round_up(s, 8) * 2, 256);
+  return 256 + round_up(k * MAX_PARTS * 8, 256) + 2 * round_up(2 * k * s * round_up(l, 8) * 2, 256) +
+         2 * round_up(2 * k * s * round_up(s, 8) * 2, 256);
 }
 
 thanos_status_t orthogonal_impl(const OrthogonalArgs& a, void* workspace, size_t ws_bytes,
@@ -720,10 +720,12 @@ thanos_status_t orthogonal_impl(const OrthogonalArgs& a, void* workspace, size_t
   }
   double* part = ar.take<double>(k * MAX_PARTS);
   __half* X[2][2];
-  for (auto& x : X)
-    for (auto& plane : x) plane = ar.take<__half>(k * s * ldx);
-  __half* S = ar.take<__half>(k * s * lds);
-  __half* P = ar.take<__half>(k * s * lds);
+  for (auto& x : X) {
+    x[0] = ar.take<__half>(2 * k * s * ldx);
+    x[1] = x[0] + k * s * ldx;
+  }
+  __half* S = ar.take<__half>(2 * k * s * lds);
+  __half* P = ar.take<__half>(2 * k * s * lds);
   if (!ar.ok()) return THANOS_ERR_WORKSPACE;
   // Entries of X are at most the spectral norm (about 1.2), on average (s l)^-1/2 at the start;
   // entries of S at most its square, on average 1 / s; P is up to some ten times S.
@@ -752,6 +754,7 @@ thanos_status_t orthogonal_impl(const OrthogonalArgs& a, void* workspace, size_t
   ProjArgs g;
   g.batch = (int)k;
   g.f16 = 1;
+  g.fine = a.W_out && a.wdtype == THANOS_F32;
   g.status = status;
   g.S = S;
   g.Pm = P;

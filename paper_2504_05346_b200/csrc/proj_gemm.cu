@@ -34,7 +34,7 @@ constexpr int FACTOR_BYTES = 128 * 16 * 4;    // 16 ranks of up to 128 tokens, f
 
 struct Params {
   int M, N, K, tiles_m, tiles_n, nt, stages, splits, batch_z, ring_bytes, tmem_cols;
-  int symmetric, f16, early, first;
+  int symmetric, f16, early, first, fine;
   int32_t* status;
   // adapter part
   void* out;
@@ -289,34 +289,46 @@ __device__ __forceinline__ void emit(const Params& p, int z, int m, int n0, floa
     __half* D = (EPI == PROJ_GRAM ? p.S : p.Pm) + (int64_t)z * p.s_batch;
     if constexpr (EPI == PROJ_POLY) {
       const __half* S = p.S + (int64_t)z * p.s_batch + (int64_t)n0 * p.lds + m;
-      __half old[NC];
+      __half old[NC], rest[NC];
 #pragma unroll
       for (int e = 0; e < NC; ++e) old[e] = e < nc ? S[(int64_t)e * p.lds] : __half(0.f);
+      const int64_t second = (int64_t)p.batch_z * p.s_batch;
 #pragma unroll
-      for (int e = 0; e < NC; ++e) v[e] = fmaf(p.beta, __half2float(old[e]), p.alpha * v[e]);
+      for (int e = 0; e < NC; ++e)
+        rest[e] = p.fine && e < nc ? S[second + (int64_t)e * p.lds] : __half(0.f);
+#pragma unroll
+      for (int e = 0; e < NC; ++e)
+        v[e] = fmaf(p.beta, __half2float(old[e]) + __half2float(rest[e]), p.alpha * v[e]);
     } else {
 #pragma unroll
       for (int e = 0; e < NC; ++e) v[e] *= p.alpha;
     }
-    __half* col = D + (int64_t)n0 * p.lds + m;
+#pragma unroll 1
+    for (int plane = 0;; ++plane) {
+      __half* col = D + (int64_t)n0 * p.lds + m;
 #pragma unroll
-    for (int e = 0; e < NC; ++e)
-      if (e < nc) col[(int64_t)e * p.lds] = __float2half_rn(v[e]);
-    if (mirror) {
-      __half* row = D + (int64_t)m * p.lds + n0;
+      for (int e = 0; e < NC; ++e)
+        if (e < nc) col[(int64_t)e * p.lds] = __float2half_rn(v[e]);
+      if (mirror) {
+        __half* row = D + (int64_t)m * p.lds + n0;
 #pragma unroll
-      for (int e8 = 0; e8 < NC; e8 += 8) {
-        if (e8 + 8 <= nc) {
-          float f[8];
+        for (int e8 = 0; e8 < NC; e8 += 8) {
+          if (e8 + 8 <= nc) {
+            float f[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] = v[e8 + e];
-          *reinterpret_cast<uint4*>(row + e8) = pack8_half(f);
-        } else {
+            for (int e = 0; e < 8; ++e) f[e] = v[e8 + e];
+            *reinterpret_cast<uint4*>(row + e8) = pack8_half(f);
+          } else {
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (e8 + e < nc) row[e8 + e] = __float2half_rn(v[e8 + e]);
+            for (int e = 0; e < 8; ++e)
+              if (e8 + e < nc) row[e8 + e] = __float2half_rn(v[e8 + e]);
+          }
         }
       }
+      if (plane == 1 || !p.fine) break;
+      D += (int64_t)p.batch_z * p.s_batch;
+#pragma unroll
+      for (int e = 0; e < NC; ++e) v[e] -= __half2float(__float2half_rn(v[e]));
     }
   } else {
     const int64_t at = (int64_t)z * p.x_batch + (int64_t)n0 * p.ldx + m;
@@ -624,6 +636,7 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
   constexpr bool F32 = EPI == PROJ_OUT32, OUT = EPI == PROJ_OUT || F32;
   constexpr bool DRAIN = EPI == PROJ_SHRINK || EPI == PROJ_SHRINK32;
   constexpr bool PLANES = F32 || EPI == PROJ_SHRINK32;
+  constexpr bool ITER = EPI >= PROJ_GRAM && EPI <= PROJ_FINAL;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -702,6 +715,7 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
 
   const int nk1 = (p.K + BK - 1) / BK;
   const int nk = PLANES ? 6 * nk1 : nk1;
+  const int planes = ITER && p.fine ? 2 : 1;  // stages of a k step: hi planes, then lo planes
   const int ks0 = (int)((int64_t)nk * rank / S), ks1 = (int)((int64_t)nk * (rank + 1) / S);
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
@@ -710,11 +724,12 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
     int s = 0;
     uint32_t phase = 0;
     bool ok = true;
-    for (int ks = ks0; ks < ks1 && ok; ++ks) {
+    for (int q = planes * ks0; q < planes * ks1 && ok; ++q) {
+      const int ks = planes == 2 ? q >> 1 : q, second = planes == 2 && (q & 1) ? p.batch_z : 0;
       ok = mbar_wait(empty_bar(s), phase ^ 1u, abort_flag);
       if (ok) {
         const uint32_t dst = smem_base + (uint32_t)s * stage_bytes;
-        int k0 = ks * BK, za = z, zb = z;
+        int k0 = ks * BK, za = z + second, zb = z + second;
         if (PLANES) {
           const int combo = ks / nk1;
           k0 = (ks - combo * nk1) * BK;
@@ -767,9 +782,28 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
       }
       ok = ok && mbar_wait(full_bar(s), phase, abort_flag);
       tc_fence_after();
-      if (ok) {
-        mma_step<AMN, false>(tmem_base + (uint32_t)(q * p.nt), ad0 + at, bd0 + at, idesc,
-                             start ? 0u : 1u);
+      const uint32_t d = tmem_base + (uint32_t)(q * p.nt);
+      if (ITER && planes == 2) {
+        // hi and lo planes lie in this stage and the next: hi lo + lo hi + hi hi
+        const uint64_t hi = at;
+        const int s_hi = s;
+        at += hop;
+        if (++s == p.stages) {
+          s = 0;
+          at = 0;
+          phase ^= 1u;
+        }
+        ok = ok && mbar_wait(full_bar(s), phase, abort_flag);
+        tc_fence_after();
+        if (ok) {
+          mma_step<AMN, false>(d, ad0 + hi, bd0 + at, idesc, start ? 0u : 1u);
+          mma_step<AMN, false>(d, ad0 + at, bd0 + hi, idesc, 1u);
+          mma_step<AMN, false>(d, ad0 + hi, bd0 + hi, idesc, 1u);
+          tc_commit(empty_bar(s_hi));
+          tc_commit(empty_bar(s));
+        }
+      } else if (ok) {
+        mma_step<AMN, false>(d, ad0 + at, bd0 + at, idesc, start ? 0u : 1u);
         tc_commit(empty_bar(s));
       }
       if (DRAIN && ((ks - ks0) % DRAIN_STEPS == DRAIN_STEPS - 1 || ks + 1 == ks1)) {
@@ -1193,6 +1227,7 @@ pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
   grid_dependents_launch();
 
   const int nk = (p.K + BK - 1) / BK;
+  const int planes = !EXT && p.fine ? 2 : 1;  // stages of a k step: hi planes, then lo planes
   const int half = p.nt / 2;  // n rows that this CTA loads
   const bool ext = EXT && p.n_adapters > 0;
 
@@ -1205,19 +1240,21 @@ pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
     for (int t = pair; t < n_tiles && ok; t += npairs) {
       const PairTile tl = pair_tile(p, t);
       const int m0 = tl.tm * PTM + 128 * (int)rank, n0 = tl.tn * p.nt + half * (int)rank;
-      for (int ks = 0; ks < nk && ok; ++ks) {
+      for (int u = 0; u < planes * nk && ok; ++u) {
         ok = mbar_wait(empty_bar(s), phase ^ 1u, abort_flag);
         if (ok) {
+          const int kb = (planes == 2 ? u >> 1 : u) * BK;
+          const int slab = tl.z + (planes == 2 && (u & 1) ? p.batch_z : 0);
           const uint32_t dst = smem_base + (uint32_t)s * PSTAGE_BYTES;
           const uint32_t lead = map_to_cta(full_bar(s), 0);
           if (rank == 0) mbar_expect_tx(full_bar(s), 2 * (A_BYTES + half * BK * 2));
           if (AMN) {
-            tma_load_3d_pair(dst, &mapA, lead, m0, ks * BK, tl.z);
-            tma_load_3d_pair(dst + A_BYTES / 2, &mapA, lead, m0 + 64, ks * BK, tl.z);
+            tma_load_3d_pair(dst, &mapA, lead, m0, kb, slab);
+            tma_load_3d_pair(dst + A_BYTES / 2, &mapA, lead, m0 + 64, kb, slab);
           } else {
-            tma_load_3d_pair(dst, &mapA, lead, ks * BK, m0, tl.z);
+            tma_load_3d_pair(dst, &mapA, lead, kb, m0, slab);
           }
-          tma_load_3d_pair(dst + A_BYTES, &mapB, lead, ks * BK, n0, tl.z);
+          tma_load_3d_pair(dst + A_BYTES, &mapB, lead, kb, n0, slab);
         }
         if (++s == STAGES) {
           s = 0;
@@ -1254,9 +1291,26 @@ pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
         for (int ks = 0; ks < nk && ok; ++ks) {
           ok = mbar_wait(full_bar(s), phase, abort_flag);
           tc_fence_after();
-          if (ok) {
-            const uint64_t at = (uint64_t)s * (PSTAGE_BYTES >> 4);
-            mma_step<AMN, true>(d, ad0 + at, bd0 + at, idesc, ks > 0 ? 1u : 0u);
+          const uint64_t at = (uint64_t)s * (PSTAGE_BYTES >> 4);
+          const uint32_t add = ks > 0 ? 1u : 0u;
+          if (!EXT && planes == 2) {
+            const int s_hi = s;
+            if (++s == STAGES) {
+              s = 0;
+              phase ^= 1u;
+            }
+            ok = ok && mbar_wait(full_bar(s), phase, abort_flag);
+            tc_fence_after();
+            if (ok) {
+              const uint64_t lo = (uint64_t)s * (PSTAGE_BYTES >> 4);
+              mma_step<AMN, true>(d, ad0 + at, bd0 + lo, idesc, add);
+              mma_step<AMN, true>(d, ad0 + lo, bd0 + at, idesc, 1u);
+              mma_step<AMN, true>(d, ad0 + at, bd0 + at, idesc, 1u);
+              tc_commit_pair(empty_bar(s_hi));
+              tc_commit_pair(empty_bar(s));
+            }
+          } else if (ok) {
+            mma_step<AMN, true>(d, ad0 + at, bd0 + at, idesc, add);
             tc_commit_pair(empty_bar(s));
           }
           if (++s == STAGES) {
@@ -1587,7 +1641,7 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
   p.K = a.K;
   const bool f32 = a.epi >= PROJ_OUT32;
   const bool pairs = a.epi != PROJ_SHRINK && !f32 && use_pairs(a.M, a.N, a.batch, symmetric);
-  const int nk = (a.K + BK - 1) / BK * (f32 ? 6 : 1);
+  const int nk = (a.K + BK - 1) / BK * (f32 ? 6 : a.fine ? 2 : 1);
   const TileShape shape =
       pairs ? TileShape{PTM, 1} : tile_shape(a.M, a.N, a.batch, nk, symmetric, a.epi);
   p.nt = shape.nt;
@@ -1599,6 +1653,7 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
   p.f16 = a.f16;
   p.early = a.early;
   p.first = a.first;
+  p.fine = a.fine;
   p.status = a.status;
   const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * a.batch;
   if (tiles > (1 << 27) || a.batch > 65535) return THANOS_ERR_SHAPE;
@@ -1648,7 +1703,7 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
 
   CUtensorMap mA, mB, mP;
   const CUtensorMapSwizzle sw = CU_TENSOR_MAP_SWIZZLE_128B;
-  const int64_t slabs = f32 ? 3 : a.batch;
+  const int64_t slabs = f32 ? 3 : a.fine ? 2 * a.batch : a.batch;
   const bool okA = a.a_mn ? make_map3(&mA, a.A, a.f16, a.M, a.K, a.lda, slabs, a.a_batch, 64, BK, sw)
                           : make_map3(&mA, a.A, a.f16, a.K, a.M, a.lda, slabs, a.a_batch, BK, TM, sw);
   if (!okA || !make_map3(&mB, a.B, a.f16, a.K, a.N, a.ldb, slabs, a.b_batch, BK,

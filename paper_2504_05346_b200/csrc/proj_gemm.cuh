@@ -55,6 +55,8 @@ struct ProjArgs {
   int64_t ldp = 0, p_adapter = 0;       // a_mn == 0: [n][M][ldp]; else [n][r][ldp].  On CTA pairs
                                         // ldp and p_adapter are multiples of 8
   // PROJ_GRAM .. PROJ_FINAL
+  int fine = 0;                  // A, B, S and P have a second plane of what fp16 leaves over, batch
+                                 // matrices behind the first; three products of planes
   float alpha = 1.f, beta = 0.f;
   __half* S = nullptr;           // GRAM: written, POLY: read
   int64_t lds = 0, s_batch = 0;
