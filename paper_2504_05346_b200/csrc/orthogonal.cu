@@ -8,12 +8,24 @@
 // rounding of X that mixes a strong direction into them grows too (on a low-rank gradient with
 // noise 1e-1 of the result with hi alone, 2e-4 with both).  The product P X reads hi only: P acts
 // on the strong directions, whose rounding errors are not amplified.
+//
+// That is 1 to 2e-3 of the result, as much as the bf16 rounding of O or of bf16 weights.  A step on
+// fp32 weights carries S and P as two planes too and takes three products of planes for each (fine):
+// 1e-5 of the update, below the rounding of the weights themselves.  It costs three times the tensor
+// work and twice the operand traffic: 768 x 768 in 173 us instead of 97, 4096 x 4096 in 2.97 ms
+// instead of 1.28.
 #include "proj_gemm.cuh"
 #include "recovery.cuh"
 
 namespace thanos {
 namespace {
 
+// Sides up to which the diagonals of S and P are kept apart in fp32.  The rows of a long matrix are
+// nearly orthogonal, S nearly its diagonal, and a rounding of a diagonal entry is a factor of a whole
+// row that a + b s + c s^2 = 3.4 - 4.8 + 2.0 makes four times as large (7697 x 40: error 2.7e-3 of
+// the result beside the rounding of O, 1.2e-3 with them apart).  With larger sides the rest of S
+// outweighs its diagonal (4096 x 4096: no difference, and 60 of 1330 us for reading it).
+constexpr int DIAG_SIDE = 512;
 constexpr int MAX_PARTS = 1024;  // partial sums of squares per matrix
 
 __device__ __forceinline__ float load_any(const void* p, int bf16, int64_t e) {
@@ -686,7 +698,8 @@ size_t orthogonal_workspace_bytes(int64_t batch, int64_t m, int64_t n) {
            round_up(k * small_chunks(batch > 0 ? batch : 1, s, l) * round_up(s, 4) * round_up(s, 4) * 4,
                     256) +
            round_up(k * s * s * 4, 256);
-  return 256 + round_up(k * MAX_PARTS * 8, 256) + 2 * round_up(2 * k * s * round_up(l, 8) * 2, 256) +
+  return 256 + round_up(k * MAX_PARTS * 8, 256) + 2 * round_up(k * round_up(s, 8) * 4, 256) +
+         2 * round_up(2 * k * s * round_up(l, 8) * 2, 256) +
          2 * round_up(2 * k * s * round_up(s, 8) * 2, 256);
 }
 
@@ -726,6 +739,8 @@ thanos_status_t orthogonal_impl(const OrthogonalArgs& a, void* workspace, size_t
   }
   __half* S = ar.take<__half>(2 * k * s * lds);
   __half* P = ar.take<__half>(2 * k * s * lds);
+  float* s_diag = ar.take<float>(k * lds);
+  float* p_diag = ar.take<float>(k * lds);
   if (!ar.ok()) return THANOS_ERR_WORKSPACE;
   // Entries of X are at most the spectral norm (about 1.2), on average (s l)^-1/2 at the start;
   // entries of S at most its square, on average 1 / s; P is up to some ten times S.
@@ -758,6 +773,10 @@ thanos_status_t orthogonal_impl(const OrthogonalArgs& a, void* workspace, size_t
   g.status = status;
   g.S = S;
   g.Pm = P;
+  if (s <= DIAG_SIDE) {
+    g.s_diag = s_diag;
+    g.p_diag = p_diag;
+  }
   g.lds = lds;
   g.s_batch = s * lds;
   g.ldx = ldx;

@@ -56,6 +56,8 @@ struct Params {
   __half* S;
   int64_t lds, s_batch;
   __half* Pm;
+  float* s_diag;
+  float* p_diag;
   const __half* Xh;
   const __half* Xl;
   __half* Yh;
@@ -247,6 +249,19 @@ __device__ __forceinline__ uint4 pack8_half(const float (&v)[8]) {
   return q;
 }
 
+// Diagonal entries of NC columns; rows of lds (a multiple of eight) hold them, so whole eights exist.
+template <int NC>
+__device__ __forceinline__ void load_diag(const float* d, int nc, float (&v)[NC]) {
+#pragma unroll
+  for (int e = 0; e < NC; e += 4) {
+    const float4 q = *reinterpret_cast<const float4*>(d + (e / 8 * 8 < nc ? e : 0));
+    v[e] = q.x;
+    v[e + 1] = q.y;
+    v[e + 2] = q.z;
+    v[e + 3] = q.w;
+  }
+}
+
 // NC consecutive n of one m (a lane); n0 is a multiple of 8.
 template <bool AMN, int EPI, int NC>
 __device__ __forceinline__ void emit(const Params& p, int z, int m, int n0, float (&v)[NC],
@@ -296,12 +311,36 @@ __device__ __forceinline__ void emit(const Params& p, int z, int m, int n0, floa
 #pragma unroll
       for (int e = 0; e < NC; ++e)
         rest[e] = p.fine && e < nc ? S[second + (int64_t)e * p.lds] : __half(0.f);
+      if (p.s_diag) {
+        // S = S' + diag(d): S S = S' S' + (d_m + d_n) S' + diag(d^2), of which the product gave the
+        // first
+        const float* d = p.s_diag + (int64_t)z * p.lds;
+        float dn[NC];
+        load_diag<NC>(d + n0, nc, dn);
+        const float dm = d[m];
 #pragma unroll
-      for (int e = 0; e < NC; ++e)
-        v[e] = fmaf(p.beta, __half2float(old[e]) + __half2float(rest[e]), p.alpha * v[e]);
+        for (int e = 0; e < NC; ++e) {
+          const float x = n0 + e == m ? dm : __half2float(old[e]) + __half2float(rest[e]);
+          const float y = n0 + e == m ? dm : dm + dn[e];
+          v[e] = fmaf(fmaf(p.alpha, y, p.beta), x, p.alpha * v[e]);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < NC; ++e)
+          v[e] = fmaf(p.beta, __half2float(old[e]) + __half2float(rest[e]), p.alpha * v[e]);
+      }
     } else {
 #pragma unroll
       for (int e = 0; e < NC; ++e) v[e] *= p.alpha;
+    }
+    if (p.s_diag && m >= n0 && m < n0 + NC) {
+      float* diag = EPI == PROJ_GRAM ? p.s_diag : p.p_diag;
+#pragma unroll
+      for (int e = 0; e < NC; ++e)
+        if (n0 + e == m) {
+          diag[(int64_t)z * p.lds + m] = v[e];
+          v[e] = 0.f;
+        }
     }
 #pragma unroll 1
     for (int plane = 0;; ++plane) {
@@ -337,6 +376,14 @@ __device__ __forceinline__ void emit(const Params& p, int z, int m, int n0, floa
     for (int e = 0; e < NC; ++e) {
       hi[e] = e < nc ? p.Xh[at + (int64_t)e * p.ldx] : __half(0.f);
       lo[e] = e < nc ? p.Xl[at + (int64_t)e * p.ldx] : __half(0.f);
+    }
+    if (p.p_diag) {
+      // with what the product read of X: P acts on nearly parallel rows of X then as a whole
+      float dn[NC];
+      load_diag<NC>(p.p_diag + (int64_t)z * p.lds + n0, nc, dn);
+#pragma unroll
+      for (int e = 0; e < NC; ++e)
+        v[e] = fmaf(dn[e], __half2float(hi[e]) + (p.fine ? __half2float(lo[e]) : 0.f), v[e]);
     }
 #pragma unroll
     for (int e = 0; e < NC; ++e)
@@ -1686,6 +1733,8 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
   p.lds = a.lds;
   p.s_batch = a.s_batch;
   p.Pm = a.Pm;
+  p.s_diag = a.s_diag;
+  p.p_diag = a.p_diag;
   p.Xh = a.Xh;
   p.Xl = a.Xl;
   p.Yh = a.Yh;

@@ -17,9 +17,10 @@ namespace thanos {
 enum ProjEpilogue {
   PROJ_OUT = 0,     // out[n, m] = bf16(D + adapter part)
   PROJ_SHRINK = 1,  // m = (adapter, rank): V[n, rank] where the token's adapter is the row's
-  PROJ_GRAM = 2,    // S = alpha D, fp16, symmetric: upper tiles computed, mirror written
-  PROJ_POLY = 3,    // P = beta S + alpha D, fp16, symmetric
-  PROJ_NEXT = 4,    // X' = beta (hi + lo) + alpha D, as two fp16 planes
+  PROJ_GRAM = 2,    // S = alpha D, fp16, symmetric: upper tiles computed, mirror written; with
+                    // s_diag the diagonal goes there in fp32 and is zero in S
+  PROJ_POLY = 3,    // P = beta S + alpha S S, fp16, symmetric, its diagonal in p_diag likewise
+  PROJ_NEXT = 4,    // X' = beta (hi + lo) + alpha P X, as two fp16 planes
   PROJ_FINAL = 5,   // the same value, unscaled, into O (bf16) or the new weights
   PROJ_OUT32 = 6,   // PROJ_OUT with fp32 accuracy: A and B are three bf16 planes (a_batch, b_batch
                     // apart), out and P are fp32
@@ -61,6 +62,8 @@ struct ProjArgs {
   __half* S = nullptr;           // GRAM: written, POLY: read
   int64_t lds = 0, s_batch = 0;
   __half* Pm = nullptr;          // POLY: written (strides as S)
+  float* s_diag = nullptr;       // [batch, lds], or both null
+  float* p_diag = nullptr;
   const __half* Xh = nullptr;
   const __half* Xl = nullptr;
   __half* Yh = nullptr;
