@@ -22,8 +22,8 @@ namespace {
 
 // Sides up to which the diagonals of S and P are kept apart in fp32.  The rows of a long matrix are
 // nearly orthogonal, S nearly its diagonal, and a rounding of a diagonal entry is a factor of a whole
-// row that a + b s + c s^2 = 3.4 - 4.8 + 2.0 makes four times as large (7697 x 40: error 2.7e-3 of
-// the result beside the rounding of O, 1.2e-3 with them apart).  With larger sides the rest of S
+// row that a + b s + c s^2 = 3.4 - 4.8 + 2.0 makes four times as large (8000 x 128: error 1.8e-3 of
+// the result beside the rounding of O, 0.9e-3 with them apart).  With larger sides the rest of S
 // outweighs its diagonal (4096 x 4096: no difference, and 60 of 1330 us for reading it).
 constexpr int DIAG_SIDE = 512;
 constexpr int MAX_PARTS = 1024;  // partial sums of squares per matrix
@@ -255,16 +255,24 @@ __global__ void __launch_bounds__(256) split_kernel(const StepParams p) {
   }
 }
 
-// ------------------------------------------------------------------ a short side of up to 32
+// ------------------------------------------------------------------ a short side of up to 64
 // X_k = Q_k X_0 with Q_k a polynomial in S_0 = X_0 X_0^T, so the matrix is read twice and all steps
 // run on s x s matrices: Q' = P Q, S' = P S P with P = a I + b S + c S S.  In fp32 throughout (a
 // rounding of S_0 is amplified by a^2 per step; 16-bit operands would not do here).  The s x s
-// products are a chain on one CTA: beyond 32 that costs more than the wide products do.
+// products are a chain on one CTA: 64 x 64 takes 60 us alone, of which the wide products take twice
+// the time whatever the size (4096 x 64: 94 against 123 us, 3 x 7697 x 40: 70 against 178), but a side
+// of 128 would take eight times as much.  What S_0 loses of directions 20 times weaker than the
+// strongest is 5e-4 of the result, which bf16 does not show: fp32 weights with a side above 32 go by
+// the wide products and two planes (4e-5).
 //   gram_kernel   new momentum, partial Gram matrices over chunks of the long side
 //   steps_kernel  one CTA per matrix: sums the partials in order, iterates, Q / (norm + eps)
 //   apply_kernel  Q X_0 over chunks of the long side, into O or the new weights
-constexpr int SMALL_SIDE = 32;
-constexpr int SMALL_LD = SMALL_SIDE + 4;
+constexpr int SMALL_SIDE = 64, SMALL_SIDE_FINE = 32;  // FINE: fp32 weights
+// TS x TS entries of a product a thread on 16 x 16 threads: TS = 1 and 2 share a layout
+__host__ __device__ constexpr int small_ld(int ts) { return (ts <= 2 ? 32 : 64) + 4; }
+__host__ __device__ constexpr int small_size(int ts) {  // and a row of zeros
+  return (small_ld(ts) - 3) * small_ld(ts);
+}
 constexpr int STAGE_FLOATS = 10240;  // a tile of the long side, padded rows: 512 columns of 16 rows
 
 struct SmallParams {
@@ -372,7 +380,7 @@ __global__ void __launch_bounds__(256) gram_kernel(const SmallParams p) {
   }
 }
 
-// D = A^T B for s x s matrices in shared memory (rows padded to SMALL_LD, zeros beyond s); with
+// D = A^T B for s x s matrices in shared memory (rows padded to LD, zeros beyond s); with
 // `add`, D = a I + b A + c A^T B.  S and P are symmetric up to rounding, S P and Q are not: what is
 // left of a rounding in them grows by a = 3.4 per step on one side only, so a transpose of Q in its
 // place is wrong by 1e-2 and more on matrices of low rank.  TS x TS outputs a thread; one copy of the
@@ -381,6 +389,7 @@ template <int TS>
 __device__ __noinline__ void small_product(int D_at, int A_at, int B_at, int s, bool add, float a,
                                            float b, float c) {
   extern __shared__ __align__(16) float mats[];
+  constexpr int LD = small_ld(TS);
   const int q = (s + TS - 1) / TS;
   const int ti = threadIdx.x >> 4, tj = threadIdx.x & 15;  // 16 x 16 threads
   if (ti < q && tj < q) {
@@ -392,16 +401,27 @@ __device__ __noinline__ void small_product(int D_at, int A_at, int B_at, int s, 
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         float xv[TS], yv[TS];
-        if constexpr (TS == 2) {
-          const float2 xx = *reinterpret_cast<const float2*>(x + (k + h) * SMALL_LD);
-          const float2 yy = *reinterpret_cast<const float2*>(y + (k + h) * SMALL_LD);
+        if constexpr (TS == 4) {
+          const float4 xx = *reinterpret_cast<const float4*>(x + (k + h) * LD);
+          const float4 yy = *reinterpret_cast<const float4*>(y + (k + h) * LD);
+          xv[0] = xx.x;
+          xv[1] = xx.y;
+          xv[2] = xx.z;
+          xv[3] = xx.w;
+          yv[0] = yy.x;
+          yv[1] = yy.y;
+          yv[2] = yy.z;
+          yv[3] = yy.w;
+        } else if constexpr (TS == 2) {
+          const float2 xx = *reinterpret_cast<const float2*>(x + (k + h) * LD);
+          const float2 yy = *reinterpret_cast<const float2*>(y + (k + h) * LD);
           xv[0] = xx.x;
           xv[1] = xx.y;
           yv[0] = yy.x;
           yv[1] = yy.y;
         } else {
-          xv[0] = x[(k + h) * SMALL_LD];
-          yv[0] = y[(k + h) * SMALL_LD];
+          xv[0] = x[(k + h) * LD];
+          yv[0] = y[(k + h) * LD];
         }
 #pragma unroll
         for (int i = 0; i < TS; ++i)
@@ -415,8 +435,8 @@ __device__ __noinline__ void small_product(int D_at, int A_at, int B_at, int s, 
       for (int j = 0; j < TS; ++j) {
         const int r = TS * ti + i, cc = TS * tj + j;
         float v = acc[0][i][j] + acc[1][i][j];
-        if (add) v = fmaf(c, v, fmaf(b, mats[A_at + r * SMALL_LD + cc], r == cc ? a : 0.f));
-        if (r < s && cc < s) mats[D_at + r * SMALL_LD + cc] = v;
+        if (add) v = fmaf(c, v, fmaf(b, mats[A_at + r * LD + cc], r == cc ? a : 0.f));
+        if (r < s && cc < s) mats[D_at + r * LD + cc] = v;
       }
   }
   __syncthreads();
@@ -424,11 +444,26 @@ __device__ __noinline__ void small_product(int D_at, int A_at, int B_at, int s, 
 
 constexpr int STEP_THREADS = 256;
 
+__device__ __forceinline__ void add4(float4& a, const float4& b) {
+  a.x += b.x;
+  a.y += b.y;
+  a.z += b.z;
+  a.w += b.w;
+}
+// Every hop-th of the chunks' partial matrices from the first-th on.
+__device__ __forceinline__ float4 sum_parts(const float4* part, int first, int hop, int chunks,
+                                            int vecs) {
+  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+  for (int k = first; k < chunks; k += hop) add4(sum, part[(int64_t)k * vecs]);
+  return sum;
+}
+
 template <int TS>
 __global__ void __launch_bounds__(STEP_THREADS) steps_kernel(const SmallParams p) {
   extern __shared__ __align__(16) float mats[];
   // S, P, Q, T, U: a row more than they need, which stays zero
-  constexpr int SZ = (SMALL_SIDE + 1) * SMALL_LD;
+  constexpr int LD = small_ld(TS), SZ = small_size(TS);
   float *S = mats, *T = mats + 3 * SZ;
   int Q = 2 * SZ, U = 4 * SZ;
   __shared__ float norm;
@@ -439,43 +474,38 @@ __global__ void __launch_bounds__(STEP_THREADS) steps_kernel(const SmallParams p
   grid_dependents_launch();
   // the partial matrices, four entries a thread; threads to spare take every groups-th of them
   const int q = (s + 3) / 4, vecs = q * q * 4;
-  const int groups = STEP_THREADS / vecs;
-  const int g = threadIdx.x / vecs, e = threadIdx.x - g * vecs;
   const float4* part = reinterpret_cast<const float4*>(p.part) + (int64_t)blockIdx.x * p.chunks * vecs;
-  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (g < groups) {
-#pragma unroll 8
-    for (int k = g; k < p.chunks; k += groups) {
-      const float4 w = part[(int64_t)k * vecs + e];
-      sum.x += w.x;
-      sum.y += w.y;
-      sum.z += w.z;
-      sum.w += w.w;
+  if constexpr (TS <= 2) {
+    const int groups = STEP_THREADS / vecs;
+    const int g = threadIdx.x / vecs, e = threadIdx.x - g * vecs;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (g < groups) {
+      sum = sum_parts(part + e, g, groups, p.chunks, vecs);
+      reinterpret_cast<float4*>(T)[threadIdx.x] = sum;  // T holds 297 of them
     }
-    reinterpret_cast<float4*>(T)[threadIdx.x] = sum;  // T holds 288 of them
-  }
-  __syncthreads();
-  if (threadIdx.x < vecs) {
-    for (int k = 1; k < groups; ++k) {
-      const float4 w = reinterpret_cast<const float4*>(T)[k * vecs + e];
-      sum.x += w.x;
-      sum.y += w.y;
-      sum.z += w.z;
-      sum.w += w.w;
+    __syncthreads();
+    if (threadIdx.x < vecs) {
+      for (int k = 1; k < groups; ++k) add4(sum, reinterpret_cast<const float4*>(T)[k * vecs + e]);
+      const int tl = e >> 2, tr = tl / q;
+      *reinterpret_cast<float4*>(S + (4 * tr + (e & 3)) * LD + 4 * (tl - tr * q)) = sum;
     }
-    const int tl = e >> 2, tr = tl / q;
-    *reinterpret_cast<float4*>(S + (4 * tr + (e & 3)) * SMALL_LD + 4 * (tl - tr * q)) = sum;
+  } else {
+    for (int e = threadIdx.x; e < vecs; e += STEP_THREADS) {
+      const int tl = e >> 2, tr = tl / q;
+      *reinterpret_cast<float4*>(S + (4 * tr + (e & 3)) * LD + 4 * (tl - tr * q)) =
+          sum_parts(part + e, 0, 1, p.chunks, vecs);
+    }
   }
   __syncthreads();
   if (threadIdx.x < 32) {
     float t = 0.f;
-    for (int i = threadIdx.x; i < s; i += 32) t += S[i * SMALL_LD + i];
+    for (int i = threadIdx.x; i < s; i += 32) t += S[i * LD + i];
     for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
     if (threadIdx.x == 0) norm = sqrtf(t) + p.u.eps;
   }
   __syncthreads();
   const float inv = 1.f / norm;
-  for (int i = threadIdx.x; i < s * SMALL_LD; i += STEP_THREADS) S[i] = S[i] * inv * inv;
+  for (int i = threadIdx.x; i < s * LD; i += STEP_THREADS) S[i] = S[i] * inv * inv;
   __syncthreads();
   // T held partial sums: its row s has to be zero again
   for (int i = threadIdx.x; i < SZ; i += STEP_THREADS) T[i] = 0.f;
@@ -497,23 +527,27 @@ __global__ void __launch_bounds__(STEP_THREADS) steps_kernel(const SmallParams p
   }
   float* out = p.Q + (int64_t)blockIdx.x * ss;
   for (int r = threadIdx.x >> 5; r < s; r += STEP_THREADS / 32)
-    if ((threadIdx.x & 31) < s) 
-      out[r * s + (threadIdx.x & 31)] = mats[Q + r * SMALL_LD + (threadIdx.x & 31)] * inv;
+#pragma unroll
+    for (int c = threadIdx.x & 31; c < LD - 4; c += 32)
+      if (c < s) out[r * s + c] = mats[Q + r * LD + c] * inv;
 }
 
-template <int VEC>
+template <int VEC, int TS>
 __global__ void __launch_bounds__(256) apply_kernel(const SmallParams p) {
   extern __shared__ __align__(16) float Xs[];
+  constexpr int LD = small_ld(TS);
   float* Qs = Xs + STAGE_FLOATS;                            // Qs[k][row], zeros beyond s
   const int64_t base = (int64_t)blockIdx.y * p.s * p.l;
   const int q = (p.s + 3) / 4, ld = 4 * q + 4;
-  for (int e = threadIdx.x; e < SMALL_SIDE * SMALL_LD; e += 256) Qs[e] = 0.f;
+  for (int e = threadIdx.x; e < (LD - 4) * LD; e += 256) Qs[e] = 0.f;
   __syncthreads();
   grid_dependency_wait();   // the momentum, too, is an earlier launch's
   const float* Q = p.Q + (int64_t)blockIdx.y * p.s * p.s;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int r = warp; r < p.s; r += 8)
-    if (lane < p.s) Qs[lane * SMALL_LD + r] = Q[r * p.s + lane];
+#pragma unroll
+    for (int k = lane; k < LD - 4; k += 32)
+      if (k < p.s) Qs[k * LD + r] = Q[r * p.s + k];
   for (int c0 = blockIdx.x * p.tile_cols; c0 < p.l; c0 += gridDim.x * p.tile_cols) {
     const int cols = min(p.tile_cols, p.l - c0);
     __syncthreads();
@@ -534,7 +568,7 @@ __global__ void __launch_bounds__(256) apply_kernel(const SmallParams p) {
           x[u] = *reinterpret_cast<const float4*>(Xs + min(c + 32 * u, cols - 1) * ld + k);
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) {
-          const float4 w = *reinterpret_cast<const float4*>(Qs + (k + kk) * SMALL_LD + r);
+          const float4 w = *reinterpret_cast<const float4*>(Qs + (k + kk) * LD + r);
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
             const float xv = kk == 0 ? x[u].x : kk == 1 ? x[u].y : kk == 2 ? x[u].z : x[u].w;
@@ -622,6 +656,14 @@ thanos_status_t launch_after(K kernel, dim3 grid, int threads, size_t smem, cons
   return THANOS_OK;
 }
 
+template <int VEC, int TS>
+thanos_status_t launch_apply(const SmallParams& p, dim3 grid, cudaStream_t stream) {
+  static std::atomic<unsigned long long> done{0};
+  const size_t smem = STAGE_FLOATS * 4 + (small_ld(TS) - 4) * small_ld(TS) * 4;
+  THANOS_CUDA(ensure_max_dyn_smem(apply_kernel<VEC, TS>, (int)smem, done));
+  return launch_after(apply_kernel<VEC, TS>, grid, 256, smem, p, stream);
+}
+
 thanos_status_t small_side(const OrthogonalArgs& a, StepParams u, int s, int l, float* part,
                            float* Q, int chunks, cudaStream_t stream) {
   SmallParams p = {};
@@ -649,18 +691,21 @@ thanos_status_t small_side(const OrthogonalArgs& a, StepParams u, int s, int l, 
   // The steps are a chain on one CTA per matrix: CTAs that share an SM slow one another down, so they
   // ask for more shared memory than half of an SM's, and spread out.
   const size_t stage = STAGE_FLOATS * 4, squares = 116 * 1024;
-  static_assert(5 * (SMALL_SIDE + 1) * SMALL_LD * 4 <= 116 * 1024, "five matrices");
+  static_assert(5 * small_size(4) * 4 <= 116 * 1024, "five matrices");
   const dim3 chunks_grid((unsigned)p.chunks, (unsigned)a.batch), one((unsigned)a.batch);
   if (wide) gram_kernel<4><<<chunks_grid, 256, stage, stream>>>(p);
   else gram_kernel<1><<<chunks_grid, 256, stage, stream>>>(p);
   THANOS_CHECK_LAUNCH();
-  static std::atomic<unsigned long long> done1{0}, done2{0}, done_a{0}, done_b{0};
-  if (s <= 16) {  // one entry of a product a thread, or four
+  static std::atomic<unsigned long long> done1{0}, done2{0}, done4{0};
+  if (s <= 16) {  // one entry of a product a thread, four or sixteen
     THANOS_CUDA(ensure_max_dyn_smem(steps_kernel<1>, (int)squares, done1));
     THANOS_TRY(launch_after(steps_kernel<1>, one, STEP_THREADS, squares, p, stream));
-  } else {
+  } else if (s <= 32) {
     THANOS_CUDA(ensure_max_dyn_smem(steps_kernel<2>, (int)squares, done2));
     THANOS_TRY(launch_after(steps_kernel<2>, one, STEP_THREADS, squares, p, stream));
+  } else {
+    THANOS_CUDA(ensure_max_dyn_smem(steps_kernel<4>, (int)squares, done4));
+    THANOS_TRY(launch_after(steps_kernel<4>, one, STEP_THREADS, squares, p, stream));
   }
   // tiles of the apply pass: enough for the device, four to a thread at least
   int tile = p.tile_cols;
@@ -669,13 +714,8 @@ thanos_status_t small_side(const OrthogonalArgs& a, StepParams u, int s, int l, 
   int64_t blocks = ceil_div(l, tile);
   if (blocks * a.batch > 4 * NUM_SMS) blocks = ceil_div(4 * NUM_SMS, a.batch);
   const dim3 grid((unsigned)blocks, (unsigned)a.batch);
-  const size_t apply = stage + SMALL_SIDE * SMALL_LD * 4;
-  if (wide) {
-    THANOS_CUDA(ensure_max_dyn_smem(apply_kernel<4>, (int)apply, done_a));
-    return launch_after(apply_kernel<4>, grid, 256, apply, p, stream);
-  }
-  THANOS_CUDA(ensure_max_dyn_smem(apply_kernel<1>, (int)apply, done_b));
-  return launch_after(apply_kernel<1>, grid, 256, apply, p, stream);
+  if (wide) return s <= 32 ? launch_apply<4, 2>(p, grid, stream) : launch_apply<4, 4>(p, grid, stream);
+  return s <= 32 ? launch_apply<1, 2>(p, grid, stream) : launch_apply<1, 4>(p, grid, stream);
 }
 
 float pow2_at_most(double x, int most) {
@@ -693,14 +733,17 @@ int norm_parts(int64_t mn) {
 
 size_t orthogonal_workspace_bytes(int64_t batch, int64_t m, int64_t n) {
   const size_t s = (size_t)(m < n ? m : n), l = (size_t)(m < n ? n : m), k = (size_t)batch;
+  size_t small = 0, wide = 0;
   if (s <= SMALL_SIDE)
-    return 256 +
-           round_up(k * small_chunks(batch > 0 ? batch : 1, s, l) * round_up(s, 4) * round_up(s, 4) * 4,
-                    256) +
-           round_up(k * s * s * 4, 256);
-  return 256 + round_up(k * MAX_PARTS * 8, 256) + 2 * round_up(k * round_up(s, 8) * 4, 256) +
-         2 * round_up(2 * k * s * round_up(l, 8) * 2, 256) +
-         2 * round_up(2 * k * s * round_up(s, 8) * 2, 256);
+    small = 256 +
+            round_up(k * small_chunks(batch > 0 ? batch : 1, s, l) * round_up(s, 4) * round_up(s, 4) * 4,
+                     256) +
+            round_up(k * s * s * 4, 256);
+  if (s > SMALL_SIDE_FINE)
+    wide = 256 + round_up(k * MAX_PARTS * 8, 256) + 2 * round_up(k * round_up(s, 8) * 4, 256) +
+           2 * round_up(2 * k * s * round_up(l, 8) * 2, 256) +
+           2 * round_up(2 * k * s * round_up(s, 8) * 2, 256);
+  return small > wide ? small : wide;
 }
 
 thanos_status_t orthogonal_impl(const OrthogonalArgs& a, void* workspace, size_t ws_bytes,
@@ -723,7 +766,8 @@ thanos_status_t orthogonal_impl(const OrthogonalArgs& a, void* workspace, size_t
   sp.eps = a.eps;
   sp.m = (int)a.m;
   sp.n = (int)a.n;
-  if (s <= SMALL_SIDE) {
+  const bool fine = a.W_out && a.wdtype == THANOS_F32;
+  if (s <= (fine ? SMALL_SIDE_FINE : SMALL_SIDE)) {
     const int chunks = small_chunks(a.batch, s, l);
     const size_t s4 = round_up((size_t)s, 4);
     float* parts = ar.take<float>(k * chunks * s4 * s4);
@@ -769,7 +813,7 @@ thanos_status_t orthogonal_impl(const OrthogonalArgs& a, void* workspace, size_t
   ProjArgs g;
   g.batch = (int)k;
   g.f16 = 1;
-  g.fine = a.W_out && a.wdtype == THANOS_F32;
+  g.fine = fine;
   g.status = status;
   g.S = S;
   g.Pm = P;
