@@ -304,13 +304,17 @@ __device__ __forceinline__ void emit(const Params& p, int z, int m, int n0, floa
     __half* D = (EPI == PROJ_GRAM ? p.S : p.Pm) + (int64_t)z * p.s_batch;
     if constexpr (EPI == PROJ_POLY) {
       const __half* S = p.S + (int64_t)z * p.s_batch + (int64_t)n0 * p.lds + m;
+      // columns beyond the last read the first one again: a load under a condition is not issued ahead
       __half old[NC], rest[NC];
 #pragma unroll
-      for (int e = 0; e < NC; ++e) old[e] = e < nc ? S[(int64_t)e * p.lds] : __half(0.f);
-      const int64_t second = (int64_t)p.batch_z * p.s_batch;
+      for (int e = 0; e < NC; ++e) old[e] = S[(int64_t)(e < nc ? e : 0) * p.lds];
 #pragma unroll
-      for (int e = 0; e < NC; ++e)
-        rest[e] = p.fine && e < nc ? S[second + (int64_t)e * p.lds] : __half(0.f);
+      for (int e = 0; e < NC; ++e) rest[e] = __half(0.f);
+      if (p.fine) {
+        const __half* S2 = S + (int64_t)p.batch_z * p.s_batch;
+#pragma unroll
+        for (int e = 0; e < NC; ++e) rest[e] = S2[(int64_t)(e < nc ? e : 0) * p.lds];
+      }
       if (p.s_diag) {
         // S = S' + diag(d): S S = S' S' + (d_m + d_n) S' + diag(d^2), of which the product gave the
         // first
@@ -374,8 +378,8 @@ __device__ __forceinline__ void emit(const Params& p, int z, int m, int n0, floa
     __half hi[NC], lo[NC];
 #pragma unroll
     for (int e = 0; e < NC; ++e) {
-      hi[e] = e < nc ? p.Xh[at + (int64_t)e * p.ldx] : __half(0.f);
-      lo[e] = e < nc ? p.Xl[at + (int64_t)e * p.ldx] : __half(0.f);
+      hi[e] = p.Xh[at + (int64_t)(e < nc ? e : 0) * p.ldx];
+      lo[e] = p.Xl[at + (int64_t)(e < nc ? e : 0) * p.ldx];
     }
     if (p.p_diag) {
       // with what the product read of X: P acts on nearly parallel rows of X then as a whole
