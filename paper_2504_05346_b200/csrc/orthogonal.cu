@@ -527,9 +527,12 @@ __global__ void __launch_bounds__(STEP_THREADS) steps_kernel(const SmallParams p
   }
   float* out = p.Q + (int64_t)blockIdx.x * ss;
   for (int r = threadIdx.x >> 5; r < s; r += STEP_THREADS / 32)
-#pragma unroll
-    for (int c = threadIdx.x & 31; c < LD - 4; c += 32)
-      if (c < s) out[r * s + c] = mats[Q + r * LD + c] * inv;
+    if constexpr (TS <= 2) {
+      if ((threadIdx.x & 31) < s)
+        out[r * s + (threadIdx.x & 31)] = mats[Q + r * LD + (threadIdx.x & 31)] * inv;
+    } else {
+      for (int c = threadIdx.x & 31; c < s; c += 32) out[r * s + c] = mats[Q + r * LD + c] * inv;
+    }
 }
 
 template <int VEC, int TS>
@@ -545,9 +548,11 @@ __global__ void __launch_bounds__(256) apply_kernel(const SmallParams p) {
   const float* Q = p.Q + (int64_t)blockIdx.y * p.s * p.s;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int r = warp; r < p.s; r += 8)
-#pragma unroll
-    for (int k = lane; k < LD - 4; k += 32)
-      if (k < p.s) Qs[k * LD + r] = Q[r * p.s + k];
+    if constexpr (TS <= 2) {
+      if (lane < p.s) Qs[lane * LD + r] = Q[r * p.s + lane];
+    } else {
+      for (int k = lane; k < p.s; k += 32) Qs[k * LD + r] = Q[r * p.s + k];
+    }
   for (int c0 = blockIdx.x * p.tile_cols; c0 < p.l; c0 += gridDim.x * p.tile_cols) {
     const int cols = min(p.tile_cols, p.l - c0);
     __syncthreads();
