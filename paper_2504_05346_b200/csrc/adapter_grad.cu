@@ -13,6 +13,11 @@
 //                end written (or added) to the gradient
 // A cluster of up to eight CTAs splits the adapter's tokens when there are few tiles; the partial
 // sums are added over distributed shared memory in rank order (same inputs, same bits).
+//
+// What bounds it: an SM takes in some 60 bytes per clock, and 16-byte copies that are gathered come near
+// (two CTAs: 53, 777 of 1440 cycles of a stage in issuing them); the planes of R are 12 of a stage's 20
+// KB at rank 64.  Tiles of 256 features, which share them among more, leave one CTA per SM and were
+// slower.  2048 tokens, 4096 + 4096 features, 4 adapters of rank 16: 28 us (cold).
 #include "adapter_grad.cuh"
 
 #include "proj_gemm.cuh"

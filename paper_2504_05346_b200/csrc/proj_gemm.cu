@@ -10,6 +10,9 @@
 //               weights stream in (2 r flops per output, next to 2 K in the product), then the
 //               epilogue: a quarter of the TMEM lanes and half of the columns each
 // pair_kernel: large products, see there.
+// Few tokens are bound by reading the weights, and short of that by one wave of CTAs: 64 tokens, 11008
+// x 4096, 64 adapters of rank 16 (123 MB): 31 us, 4.0 TB/s; 1 token, 4096 x 4096 (34 MB): 12.6 us,
+// 2.7 TB/s, of which start and the partial sums are half.
 // Every wait is bounded (see tc_common.cuh); on expiry the status word gets THANOS_ERR_TIMEOUT.
 #include "proj_gemm.cuh"
 
@@ -765,9 +768,10 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
   if constexpr (!DRAIN) grid_dependents_launch();
 
   const int nk1 = (p.K + BK - 1) / BK;
-  const int nk = PLANES ? 6 * nk1 : nk1;
   const int planes = ITER && p.fine ? 2 : 1;  // stages of a k step: hi planes, then lo planes
-  const int ks0 = (int)((int64_t)nk * rank / S), ks1 = (int)((int64_t)nk * (rank + 1) / S);
+  // this CTA's k blocks; three planes: all six products of planes of each, one product after another
+  const int b0 = (int)((int64_t)nk1 * rank / S), b1 = (int)((int64_t)nk1 * (rank + 1) / S);
+  const int ks0 = PLANES ? 6 * b0 : b0, ks1 = PLANES ? 6 * b1 : b1;
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
     if (!p.early) grid_dependency_wait();
@@ -782,8 +786,8 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
         const uint32_t dst = smem_base + (uint32_t)s * stage_bytes;
         int k0 = ks * BK, za = z + second, zb = z + second;
         if (PLANES) {
-          const int combo = ks / nk1;
-          k0 = (ks - combo * nk1) * BK;
+          const int combo = (ks - ks0) / (b1 - b0);
+          k0 = (b0 + ks - ks0 - combo * (b1 - b0)) * BK;
           plane_pair(combo, za, zb);
         }
         mbar_expect_tx(full_bar(s), stage_bytes);
@@ -1160,6 +1164,10 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
 // tokens, s_i V[t], is built in bf16 with zero rows for tokens of other adapters.  0 times a
 // non-finite weight would reach those tokens, so the chunk is scanned, non-finite weights become
 // zeros and the epilogue adds their products to the adapter's own tokens.
+//
+// Bound by the tensor cores and the power cap.  4096 tokens, 4096 x 4096, 7 adapters of rank 32: 118 us
+// with the skinny product, 1.18 PFLOP/s (256 tiles are 3.46 rounds of 74 pairs; 105 us and 68 % of the
+// tensor cycles in this kernel alone, cold).  8192 x 11008 x 4096: 1.3 PFLOP/s of 1.43 sustained.
 constexpr int PTM = 256;
 constexpr int PSTAGE_BYTES = 2 * A_BYTES;
 constexpr int CHUNK_BYTES = TM * 16 * 2;      // a 16-wide chunk of an adapter's wide factor
@@ -1632,7 +1640,9 @@ thanos_status_t launch_any(bool pairs, const CUtensorMap& mA, const CUtensorMap&
                : launch<AMN, EPI>(mA, mB, p, stream);
 }
 
-// Whether a product runs on CTA pairs: once its 256 x 256 tiles occupy at least half of the pairs.
+// Whether a product runs on CTA pairs: once its 256 x 256 tiles occupy at least half of the pairs (512
+// tokens, K = 4096: 32 tiles take 37 us on lone CTAs and 41 on pairs, 36 tiles 43 and 41; 64 tiles of
+// 1024 tokens 52 and 47).
 bool use_pairs(int64_t M, int64_t N, int64_t batch, bool symmetric) {
   const int64_t tm = ceil_div(M, PTM), tn = ceil_div(N, PTM);
   const int64_t tiles = (symmetric ? tm * (tm + 1) / 2 : tm * tn) * batch;
@@ -1648,26 +1658,34 @@ namespace {
 //   a CTA        2000 to start, 400 for eight columns of its epilogue (700 with operands to read)
 //   a cluster    1500, and 44 a column for the partial sums over distributed shared memory, more with
 //                more slices
-// Up to 64 tokens of a projection stay in one tile, so that the weights are read once.
+// Up to 64 tokens of a projection stay in one tile, so that the weights are read once.  A k block takes
+// `loads` stages; six of them are three planes, whose products stay with the slice of their block.  The
+// tensor cores cut what they add to an accumulator, so an fp32 product's k goes to slices of at most 16
+// blocks as far as eight slices go (64 additions of full size; K = 2048 in two slices: 1.0e-6 of the
+// result, in four 4.8e-7; the second slice costs 2000 x 2048 x 2048 a tenth of its time).
 struct TileShape {
   int nt, splits;
 };
-TileShape tile_shape(int64_t M, int64_t N, int64_t batch, int64_t nk, bool symmetric, int epi) {
+TileShape tile_shape(int64_t M, int64_t N, int64_t batch, int64_t blocks, int loads, bool symmetric,
+                     int epi) {
   const int64_t sms = sm_count(), tm = ceil_div(M, TM);
   const bool one_tile = (epi == PROJ_OUT || epi == PROJ_OUT32) && N <= 64;
   const double column = epi >= PROJ_POLY && epi <= PROJ_FINAL ? 700.0 : 400.0;
   TileShape best = {128, 1};
   double least = 0.0;
+  const int64_t unit = loads == 6 ? 6 : 1, parts = blocks * loads / unit;
+  const int64_t most = loads == 6 ? blocks : parts / 4;   // slices that the work is enough for
+  const int64_t need = epi == PROJ_OUT32 ? ceil_div(blocks, 16) : 1;
   for (int nt = 128; nt >= 32; nt /= 2) {
     if (nt > 32 && N <= nt / 2) continue;   // the next narrower one holds all of N
     if (one_tile && N > nt) break;
     int64_t tiles = tm * ceil_div(N, nt) * batch;
     if (symmetric) tiles = (tiles + tm * batch * (TM / nt)) / 2;
     const double step = fmax(250.0, (A_BYTES + nt * BK * 2) / 60.0);
-    for (int s = 1; s <= 8 && (s == 1 || nk >= 4 * s); ++s) {
+    for (int s = need < 8 ? (int)need : 8; s <= 8 && (s == 1 || s <= most); ++s) {
       const double load = (double)(tiles * s) / (double)sms;
       const double rounds = load <= 1.0 ? 1.0 : two_per_sm(epi) && load <= 2.0 ? load : ceil(load);
-      double cta = (double)ceil_div(nk, s) * step + 2000.0 + column * (double)ceil_div(nt, 16 * s);
+      double cta = (double)(ceil_div(parts, s) * unit) * step + 2000.0 + column * (double)ceil_div(nt, 16 * s);
       if (s > 1) cta += 1500.0 + 44.0 * nt * (1.0 + s / 8.0);
       if (least == 0.0 || rounds * cta < least) {
         least = rounds * cta;
@@ -1692,9 +1710,9 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
   p.K = a.K;
   const bool f32 = a.epi >= PROJ_OUT32;
   const bool pairs = a.epi != PROJ_SHRINK && !f32 && use_pairs(a.M, a.N, a.batch, symmetric);
-  const int nk = (a.K + BK - 1) / BK * (f32 ? 6 : a.fine ? 2 : 1);
   const TileShape shape =
-      pairs ? TileShape{PTM, 1} : tile_shape(a.M, a.N, a.batch, nk, symmetric, a.epi);
+      pairs ? TileShape{PTM, 1} : tile_shape(a.M, a.N, a.batch, ceil_div(a.K, BK), f32 ? 6 : a.fine ? 2 : 1,
+                                                 symmetric, a.epi);
   p.nt = shape.nt;
   p.splits = shape.splits;
   p.tiles_m = (a.M + (pairs ? PTM : TM) - 1) / (pairs ? PTM : TM);

@@ -56,3 +56,28 @@ def test_long_narrow_matrices(T, shape):
         assert rel(O[i], ref[i]) <= TOL_NARROW
     s = min(shape[1:])
     assert abs(O.float().norm().item() / math.sqrt(shape[0] * s) - 0.95) < 0.25
+
+
+@pytest.mark.parametrize("side", [31, 32, 33, 36, 37, 63, 64, 65])
+@pytest.mark.parametrize("tall", [False, True], ids=["wide", "tall"])
+def test_sides_around_the_short_ones(T, side, tall):
+    """Bounds of the layouts: sides of whole vectors and others, a few columns and many."""
+    gen = torch.Generator(device="cuda").manual_seed(47)
+    for k, l in ((1, side), (3, 100), (2, 1030)):
+        l = max(l, side)
+        G = torch.randn((k, l, side) if tall else (k, side, l), generator=gen, device="cuda")
+        G[0, :, 0] = 0
+        O, ref = T.orthogonalise(G), ref_ns(G)
+        for i in range(k):
+            assert rel(O[i], ref[i]) <= 4e-3   # as for every shape in 16 bits
+        W = torch.zeros_like(G, dtype=torch.bfloat16)
+        mask = torch.zeros(G.shape, dtype=torch.uint8, device="cuda")
+        mask[:, 1:] = torch.randint(0, 2, mask[:, 1:].shape, generator=gen, device="cuda").to(torch.uint8)
+        bad = torch.where(mask != 0, torch.full_like(G, float("nan")), G)
+        Wo, Mo = T.orthogonal_step(W, torch.zeros_like(G), bad, mask=mask, lr=1.0, momentum=0.0,
+                                   check=True)
+        want = ref_ns(torch.where(mask != 0, 0.0, G))
+        assert not Wo[mask != 0].any() and torch.isfinite(Wo.float()).all()
+        want = torch.where(mask != 0, 0.0, want)
+        for i in range(k):
+            assert rel(-Wo[i], want[i]) <= 4e-3
