@@ -897,6 +897,11 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
         used = epilogue_any(any);
       }
       int ldf = 16;                      // row of `factor`
+      if (!used && !F32 && p.skinny && p.V && tm == 0 && rank == 0) {
+        // no token of the tile has an adapter: there is nothing to compute, but V is an output
+        const int e1 = min(n0 + p.nt, p.N) * p.r;
+        for (int e = n0 * p.r + tid; e < e1; e += 256) p.V[e] = 0.f;
+      }
       if (used && !F32 && p.skinny) {
         // V of the few tokens, by the CTAs that write their outputs: a warp per pair of ranks
         ldf = (p.r + 15) & ~15;
