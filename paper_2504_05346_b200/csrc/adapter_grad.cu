@@ -261,7 +261,7 @@ __global__ void __launch_bounds__(G_THREADS, RMAX <= 64 ? 2 : 1) grad_tc_kernel(
           const int at = (ks + 1) * GK + r8 + 16 * u;
           next[u] = at < len ? p.order[lo + at] : -1;
         }
-        ok = mbar_wait(empty_bar(s), phase ^ 1u, abort_flag);
+        ok = mbar_wait_warp(empty_bar(s), phase ^ 1u, abort_flag);
         if (!ok) break;
         const uint32_t st = smem_base + (uint32_t)s * stage_bytes;
 #pragma unroll
@@ -351,7 +351,7 @@ __global__ void __launch_bounds__(G_THREADS, RMAX <= 64 ? 2 : 1) grad_tc_kernel(
       const int row = 32 * g + lane, f = f0 + row;
       float acc[RMAX / 16][16] = {};
       for (int ks = ks0; ks < ks1 && ok; ks += DRAIN_STAGES) {
-        ok = mbar_wait(tfull_bar(q), tphase, abort_flag);
+        ok = mbar_wait_warp(tfull_bar(q), tphase, abort_flag);
         tc_fence_after();
         if (!ok) break;
 #pragma unroll
@@ -418,6 +418,7 @@ __global__ void __launch_bounds__(G_THREADS, RMAX <= 64 ? 2 : 1) grad_tc_kernel(
           *o = p.accumulate ? *o + k * v : k * v;
         }
       }
+      __syncwarp();
       cluster_sync_all();  // no CTA goes on while another may still read its partial sums
     }
   }

@@ -558,10 +558,12 @@ __device__ __forceinline__ void prefetch_l2(const void* p) {
   asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
 }
 __device__ __forceinline__ void epilogue_sync() {  // the eight epilogue warps of tile_kernel
+  __syncwarp();
   asm volatile("bar.sync 1, 256;" ::: "memory");
 }
 __device__ __forceinline__ bool epilogue_any(bool mine) {  // whether any of the 256 says yes
   int r;
+  __syncwarp();
   asm volatile(
       "{\n.reg .pred a, b;\nsetp.ne.u32 a, %1, 0;\n"
       "barrier.cta.red.or.aligned.pred b, 1, 256, a;\nselp.u32 %0, 1, 0, b;\n}"
@@ -882,6 +884,10 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
     const uint32_t taddr = tmem_base + ((uint32_t)(32 * g) << 16);
     // All loops below are kept rolled: the code runs once per CTA, and straight-line code of a few
     // thousand instructions costs more in instruction fetches than it saves.
+    // Instructions of tensor memory want the whole warp, so its lanes take the same way: a lane
+    // beyond the last row does what the last row does, and only emit() leaves it out.
+    const bool live_warp = m0 + 32 * g < p.M;
+    const int mr = min(m, p.M - 1);
     bool used = false;
     if constexpr (OUT) {
       // ---------------------------------------------------------- adapter part
@@ -938,7 +944,7 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
         // while the launch before this one still computes V, the rows of the wide factors that this
         // thread will read are on their way to L2
 #pragma unroll 1
-        for (int q = 0; m < p.M; ++q) {
+        for (int q = 0; live_warp; ++q) {
           const int c = tile_column(S, rank, half, q);
           if (c >= p.nt || n0 + c >= p.N) break;
 #pragma unroll 1
@@ -946,7 +952,7 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
             const int i = ids[c + e];
             if (i < 0 || (e > 0 && ids[c + e - 1] == i)) continue;
             const __nv_bfloat16* a =
-                p.P + (int64_t)i * p.p_adapter + (AMN ? (int64_t)m : (int64_t)m * p.ldp);
+                p.P + (int64_t)i * p.p_adapter + (AMN ? (int64_t)mr : (int64_t)mr * p.ldp);
             for (int jj = 0; jj < p.r; jj += AMN ? 1 : 16) prefetch_l2(a + jj * (AMN ? p.ldp : 1));
           }
         }
@@ -973,7 +979,7 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
         float w[16];
         int held = -1;  // the adapter whose row w is
 #pragma unroll 1
-        for (int q = 0;; ++q) {
+        for (int q = 0; live_warp; ++q) {
           const int c = tile_column(S, rank, half, q);
           if (c >= p.nt || n0 + c >= p.N) break;
           // eight tokens of one request, some perhaps without adapter, share a row
@@ -987,12 +993,12 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
           }
           if (F32 || same) {
             // the row stays in registers from one eight to the next while the request stays the same
-            if (same && one >= 0 && one != held && m < p.M) {
+            if (same && one >= 0 && one != held) {
               if constexpr (F32) {
-                wide_row_f32<AMN>(p, one, m, j0, w);
+                wide_row_f32<AMN>(p, one, mr, j0, w);
               } else {
                 uint32_t u[8];
-                wide_row<AMN>(p, one, m, j0, u);
+                wide_row<AMN>(p, one, mr, j0, u);
                 unpack16(u, w);
               }
               held = one;
@@ -1003,16 +1009,16 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
               tc_ld8(taddr + p.nt + c, d);
 #pragma unroll
               for (int e = 0; e < 8; ++e)
-                if (m < p.M && ids[c + e] >= 0) d[e] += dot16(w, fac + (c + e) * ldf);
+                if (ids[c + e] >= 0) d[e] += dot16(w, fac + (c + e) * ldf);
               tc_st8(taddr + p.nt + c, d);
             } else {
 #pragma unroll 1
               for (int e = 0; e < 8; ++e) {
                 const int i = ids[c + e];
                 if constexpr (F32) {
-                  if (!same && m < p.M && i >= 0) wide_row_f32<AMN>(p, i, m, j0, w);
+                  if (!same && i >= 0) wide_row_f32<AMN>(p, i, mr, j0, w);
                 }
-                float d = m < p.M && i >= 0 ? dot16(w, fac + (c + e) * ldf) : 0.f;
+                float d = i >= 0 ? dot16(w, fac + (c + e) * ldf) : 0.f;
                 if (F32 && j0 > 0) d += tc_ld1(taddr + p.nt + c + e);
                 tc_st1(taddr + p.nt + c + e, d);
               }
@@ -1024,7 +1030,7 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
               uint32_t u[4][8];  // four rows in flight
 #pragma unroll
               for (int e = 0; e < 4; ++e)
-                wide_row<AMN>(p, m < p.M ? ids[c + e4 + e] : -1, m, j0, u[e]);
+                wide_row<AMN>(p, ids[c + e4 + e], mr, j0, u[e]);
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
                 float f[16];
@@ -1051,7 +1057,7 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
       int q = 0;
       uint32_t tphase = 0;
       for (int ks = ks0; ks < ks1 && ok; ks += DRAIN_STEPS) {
-        ok = mbar_wait(tfull_bar(q), tphase, abort_flag);
+        ok = mbar_wait_warp(tfull_bar(q), tphase, abort_flag);
         tc_fence_after();
         if (!ok) break;
 #pragma unroll
@@ -1079,7 +1085,7 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
         tc_wait_st();
       }
     } else {
-      ok = mbar_wait(done_bar, 0, abort_flag);
+      ok = mbar_wait_warp(done_bar, 0, abort_flag);
       tc_fence_after();
     }
     if (ok && S == 1) {
@@ -1431,7 +1437,7 @@ pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
         const float sc = mine >= 0 && p.scale ? p.scale[mine] : 1.f;
         const int total = p.tile_count[tl.tn] * p.chunks;
         for (int c0 = 0; c0 < total && ok; c0 += CHUNKS) {
-          ok = mbar_wait(eempty_bar(e), ephase ^ 1u, abort_flag);
+          ok = mbar_wait_warp(eempty_bar(e), ephase ^ 1u, abort_flag);
           if (!ok) break;
           unsigned char* st = ering + (size_t)e * PSTAGE_BYTES;
           const uint32_t dst = ering_base + (uint32_t)e * PSTAGE_BYTES;
@@ -1461,7 +1467,7 @@ pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
             *reinterpret_cast<uint4*>(fac + sw) = make_uint4(w[0], w[1], w[2], w[3]);
             *reinterpret_cast<uint4*>(fac + (16 ^ sw)) = make_uint4(w[4], w[5], w[6], w[7]);
           }
-          ok = mbar_wait(land_bar(e), ephase, abort_flag);
+          ok = mbar_wait_warp(land_bar(e), ephase, abort_flag);
           if (!ok) break;
           for (int q = row; q < nc * (CHUNK_BYTES / 16); q += 128)
             clean_vector(reinterpret_cast<uint4*>(st) + q, poison);
@@ -1488,7 +1494,7 @@ pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
     bool ok = true;
     for (int t = pair; t < n_tiles; t += npairs) {
       const PairTile tl = pair_tile(p, t);
-      ok = ok && mbar_wait(tfull_bar(q), tphase, abort_flag);
+      ok = ok && mbar_wait_warp(tfull_bar(q), tphase, abort_flag);
       tc_fence_after();
       if (ok) {
         const int n0 = tl.tn * p.nt;
@@ -1506,6 +1512,7 @@ pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
             float v[16];
             tc_ld16(taddr + cc, v);
             emit<AMN, EPI, 16>(p, tl.z, m, n0 + cc, v, false, false);
+            __syncwarp();  // lanes beyond the last row have left emit() early
           }
         } else {
 #pragma unroll 1
@@ -1517,6 +1524,7 @@ pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(u[i]);
             emit<AMN, EPI, 32>(p, tl.z, m, n0 + cc, v, tl.tm != tl.tn, poisoned);
+            __syncwarp();
           }
         }
       }

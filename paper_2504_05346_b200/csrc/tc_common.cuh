@@ -45,6 +45,12 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
   *abort_flag = 1;
   return false;
 }
+// The same for all lanes of a warp, which go on together and with one answer, as the `.aligned`
+// instructions that follow such a wait need them.
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity,
+                                               volatile int* abort_flag) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag)) != 0;
+}
 // One lane of a converged warp, the same for every caller.  Producer and issuer loops
 // that run on that lane alone issue faster: with all lanes in the loop and a lane test around each
 // instruction, four products of 128 x 32 x 16 took some 500 clocks.
