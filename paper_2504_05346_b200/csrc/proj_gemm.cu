@@ -814,6 +814,8 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
     __syncwarp();
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMA issuer
+    // its bounded waits begin when the operands can come, however long the launch before takes
+    if (!p.early) grid_dependency_wait();
     if (elect_one()) {
     uint32_t idesc = 0;
     idesc |= 1u << 4;  // D fp32
@@ -1331,6 +1333,9 @@ pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
           phase ^= 1u;
         }
       }
+      // The products of the next tile wait for this one's adapter stages, and those for the launch
+      // before, which may take long (the sort of all tokens, on one CTA): no bounded wait spans it.
+      if (ext && t == pair) grid_dependency_wait();
     }
     // let copies that are still in flight land before the CTA's shared memory goes away
     if (!ok) {
