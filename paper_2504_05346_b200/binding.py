@@ -572,8 +572,9 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _status(workspace: torch.Tensor, where: str) -> None:
-    st = int(workspace[:4].view(torch.int32).item())
+def _status(workspace: torch.Tensor, where: str, stream) -> None:
+    with _alloc_scope(stream):   # behind the call, on the stream that it runs on
+        st = int(workspace[:4].view(torch.int32).item())
     if st != 0:
         raise ThanosError(st, where + " (device)")
 
@@ -611,7 +612,7 @@ def adapter_forward(X: torch.Tensor, W: torch.Tensor, A: Optional[torch.Tensor] 
                                           workspace.numel(), _stream_ptr(stream)),
                "thanos_adapter_forward")
         if check:
-            _status(workspace, "thanos_adapter_forward")
+            _status(workspace, "thanos_adapter_forward", stream)
     return out, V
 
 
@@ -672,7 +673,7 @@ def adapter_backward(dY: torch.Tensor, X: Optional[torch.Tensor], V: Optional[to
                                            workspace.numel(), _stream_ptr(stream)),
                "thanos_adapter_backward")
         if check:
-            _status(workspace, "thanos_adapter_backward")
+            _status(workspace, "thanos_adapter_backward", stream)
     return dX, dA, dB
 
 
@@ -706,7 +707,7 @@ def orthogonalise(G: torch.Tensor, steps: int = 5, coef=NEWTON_SCHULZ, eps: floa
                                         float(eps), workspace.data_ptr(), workspace.numel(),
                                         _stream_ptr(stream)), "thanos_orthogonalise")
         if check:
-            _status(workspace, "thanos_orthogonalise")
+            _status(workspace, "thanos_orthogonalise", stream)
     return out
 
 
@@ -747,5 +748,5 @@ def orthogonal_step(W: torch.Tensor, M: torch.Tensor, G: torch.Tensor,
                                           float(eps), workspace.data_ptr(), workspace.numel(),
                                           _stream_ptr(stream)), "thanos_orthogonal_step")
         if check:
-            _status(workspace, "thanos_orthogonal_step")
+            _status(workspace, "thanos_orthogonal_step", stream)
     return W_out, M_out
