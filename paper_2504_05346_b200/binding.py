@@ -706,7 +706,7 @@ def orthogonalise(G: torch.Tensor, steps: int = 5, coef=NEWTON_SCHULZ, eps: floa
         _check(lib.thanos_orthogonalise(out.data_ptr(), G.data_ptr(), dt, k, m, n, abc, steps,
                                         float(eps), workspace.data_ptr(), workspace.numel(),
                                         _stream_ptr(stream)), "thanos_orthogonalise")
-        if check:
+        if check and k > 0:   # nothing runs for an empty batch, and nothing writes the word
             _status(workspace, "thanos_orthogonalise", stream)
     return out
 
@@ -747,6 +747,6 @@ def orthogonal_step(W: torch.Tensor, M: torch.Tensor, G: torch.Tensor,
                                           1 if nesterov else 0, float(weight_decay), abc, steps,
                                           float(eps), workspace.data_ptr(), workspace.numel(),
                                           _stream_ptr(stream)), "thanos_orthogonal_step")
-        if check:
+        if check and k > 0:   # nothing runs for an empty batch, and nothing writes the word
             _status(workspace, "thanos_orthogonal_step", stream)
     return W_out, M_out

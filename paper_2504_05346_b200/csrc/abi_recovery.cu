@@ -42,7 +42,7 @@ thanos_status_t orthogonal_shape(int64_t batch, int64_t m, int64_t n) {
 thanos_status_t orthogonal_common(OrthogonalArgs& a, const void* G, thanos_dtype_t gdtype,
                                   int64_t batch, int64_t m, int64_t n, const float* coef,
                                   int32_t steps, float eps) {
-  if (!G || !coef) return THANOS_ERR_INVALID_ARG;
+  if ((!G && batch != 0) || !coef) return THANOS_ERR_INVALID_ARG;
   if (!known_dtype(gdtype)) return THANOS_ERR_DTYPE;
   THANOS_TRY(orthogonal_shape(batch, m, n));
   if (steps < 1 || steps > 32 || !(eps >= 0.f) || !isfinite(eps)) return THANOS_ERR_INVALID_ARG;
@@ -192,7 +192,7 @@ thanos_status_t thanos_orthogonalise(void* O, const void* G, thanos_dtype_t gdty
                                      int64_t m, int64_t n, const float* coef, int32_t steps,
                                      float eps, void* workspace, size_t ws_bytes, void* stream) {
   OrthogonalArgs a;
-  if (!O) return THANOS_ERR_INVALID_ARG;
+  if (!O && batch != 0) return THANOS_ERR_INVALID_ARG;
   THANOS_TRY(orthogonal_common(a, G, gdtype, batch, m, n, coef, steps, eps));
   if (!aligned16(O)) return THANOS_ERR_ALIGNMENT;
   a.O = static_cast<__nv_bfloat16*>(O);
@@ -207,7 +207,7 @@ thanos_status_t thanos_orthogonal_step(void* W_out, const void* W_in, thanos_dty
                                        int32_t steps, float eps, void* workspace, size_t ws_bytes,
                                        void* stream) {
   OrthogonalArgs a;
-  if (!W_out || !W_in || !M_out || !M_in) return THANOS_ERR_INVALID_ARG;
+  if (batch != 0 && (!W_out || !W_in || !M_out || !M_in)) return THANOS_ERR_INVALID_ARG;
   if (!known_dtype(wdtype)) return THANOS_ERR_DTYPE;
   THANOS_TRY(orthogonal_common(a, G, gdtype, batch, m, n, coef, steps, eps));
   if (!isfinite(lr) || !isfinite(gain) || !isfinite(momentum) || !isfinite(weight_decay))

@@ -47,3 +47,21 @@ def test_check_reads_the_status_behind_a_call_on_another_stream(T, Tn, dtype):
             with torch.cuda.stream(stream):
                 torch.cuda._sleep(20_000_000)
             call(good)       # and not the status of the call before
+
+
+def test_empty_batches(T):
+    """No matrices: nothing runs, nothing is refused, and a workspace's old status word is not read."""
+    ws = torch.full((4096,), 255, dtype=torch.uint8, device=DEV)
+    before = T.launch_count()
+    for shape in ((0, 16, 300), (0, 200, 130)):
+        G = torch.empty(shape, device=DEV)
+        O = T.orthogonalise(G, workspace=ws, check=True)
+        assert O.shape == shape and O.dtype == BF16
+        for dtype in (BF16, F32):
+            mask = torch.empty(shape, dtype=torch.uint8, device=DEV)
+            W, M = T.orthogonal_step(G.to(dtype), G, G, mask, workspace=ws, check=True)
+            assert W.shape == shape and W.dtype == dtype and M.shape == shape
+        assert T.orthogonalise(G).shape == shape
+    assert T.launch_count() == before
+    with pytest.raises(T.ThanosError):
+        T.orthogonalise(torch.empty((3, 0, 8), device=DEV))
