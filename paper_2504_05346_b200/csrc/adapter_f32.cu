@@ -249,7 +249,7 @@ __global__ void __launch_bounds__(256) grad_f32_kernel(const Grad32Params p) {
     if (g < nj && f < sd.F) {
       float v = 0.f;
       for (int k = 0; k < 8; ++k) v += red[k][g][threadIdx.x & 31];
-      if (sd.scale) v *= sd.scale[i];
+      if (sd.scale && hi > lo) v *= sd.scale[i];  // without tokens 0, whatever the scale
       float* o = sd.out + (sd.by_feature ? (i * sd.F + f) * p.r + j0 + g
                                          : (i * p.r + j0 + g) * (int64_t)sd.F + f);
       *o = p.accumulate ? *o + v : v;

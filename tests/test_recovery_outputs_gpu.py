@@ -94,3 +94,24 @@ def test_every_output_of_the_update_is_written(T, shape):
                                    W_out=nan(*shape, dtype=dtype), M_out=nan(*shape), check=True)
         assert torch.equal(Mo, torch.where(mask != 0, 0.0, G))
         assert bool(torch.isfinite(Wo.float()).all()) and bool((Wo[mask != 0] == 0).all())
+
+
+@TYPES
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_scale_of_an_adapter_without_tokens_does_not_matter(T, bad, dtype):
+    X, W, A, B, index, scale, dY = make(90, 136, 72, 4, 12, dtype, seed=3)
+    index[index == 1] = 2
+    odd = scale.clone()
+    odd[1] = bad
+    for u, v in zip(T.adapter_forward(X, W, A, B, index, odd), T.adapter_forward(X, W, A, B, index, scale)):
+        assert torch.equal(u, v)
+    V = T.adapter_forward(X, W, A, B, index, scale)[1]
+    for accumulate in (False, True):
+        out = []
+        for s in (odd, scale):
+            dA, dB = torch.ones(4, 12, 72, device=DEV), torch.ones(4, 136, 12, device=DEV)
+            out.append(T.adapter_backward(dY, X, V, W, A, B, index, s, dA=dA, dB=dB,
+                                          accumulate=accumulate))
+        for u, v in zip(*out):
+            assert torch.equal(u, v)
+        assert bool((out[0][1][1] == accumulate).all()) and bool((out[0][2][1] == accumulate).all())
