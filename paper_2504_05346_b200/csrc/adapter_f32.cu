@@ -46,6 +46,32 @@ struct Front32Params {
   int K, n, r, back;
 };
 
+// What bf16 cannot hold by rounding alone.  Infinities and NaN: the planes are +-1, 0 and the value
+// itself, because the last plane meets only the first one of the other operand (the products are mm,
+// hl, lh, hm, mh and hh), so the value is multiplied by the other operand once, and never by a zero
+// that is only one of its planes: infinity times 2 is infinity and infinity times 0 is NaN, as in
+// fp32.  (Factors below 2^-133 count as zeros here.)  Finite values that would round to infinity:
+// the first plane is bf16's largest, the others hold the rest.
+constexpr float BF16_LARGEST = 0x1.FEp127f;
+__device__ __forceinline__ bool fits_bf16(float x) { return fabsf(x) <= BF16_LARGEST; }
+__device__ __forceinline__ void store_split_odd(__nv_bfloat16* p, int64_t plane, float x) {
+  if (isfinite(x)) {
+    const float h = fits_bf16(x) ? __bfloat162float(__float2bfloat16_rn(x)) : copysignf(BF16_LARGEST, x);
+    const __nv_bfloat16 m = __float2bfloat16_rn(x - h);
+    p[0] = __float2bfloat16_rn(h);
+    p[plane] = m;
+    p[2 * plane] = __float2bfloat16_rn(x - h - __bfloat162float(m));
+  } else {
+    p[0] = __float2bfloat16_rn(copysignf(1.f, x));
+    p[plane] = __float2bfloat16_rn(0.f);
+    p[2 * plane] = __float2bfloat16_rn(x);
+  }
+}
+__device__ __forceinline__ void store_split(__nv_bfloat16* p, int64_t plane, float x) {
+  if (fits_bf16(x)) store_split3(p, plane, x);
+  else store_split_odd(p, plane, x);
+}
+
 // A warp per row in turn, so that no index has to be divided.
 __device__ void split_job(const SplitJob& s, int blk) {
   const int64_t plane = s.rows * s.ldp;
@@ -59,6 +85,11 @@ __device__ void split_job(const SplitJob& s, int blk) {
       for (int c = 4 * lane; c < s.cols; c += 128) {
         const float4 x = *reinterpret_cast<const float4*>(src + c);
         float o[4] = {x.x, x.y, x.z, x.w};
+        if (!(fits_bf16(x.x) && fits_bf16(x.y) && fits_bf16(x.z) && fits_bf16(x.w))) {
+#pragma unroll 1
+          for (int k = 0; k < 4; ++k) store_split_odd(dst + c + k, plane, src[c + k]);
+          continue;
+        }
 #pragma unroll
         for (int pl = 0; pl < 3; ++pl) {
           uint32_t h[4];
@@ -73,7 +104,7 @@ __device__ void split_job(const SplitJob& s, int blk) {
         }
       }
     } else {
-      for (int c = lane; c < s.cols; c += 32) store_split3(dst + c, plane, src[c]);
+      for (int c = lane; c < s.cols; c += 32) store_split(dst + c, plane, src[c]);
     }
   }
 }
@@ -97,7 +128,7 @@ __device__ void turn_job(const Front32Params& p, int blk) {
       for (int e = threadIdx.x; e < 64 * nj; e += 256) {
         const int j = e >> 6, row = e & 63;
         if (k0 + row < p.K)
-          store_split3(p.turned + (i * p.r + j0 + j) * p.turn_ld + k0 + row, plane, sh[j][row]);
+          store_split(p.turned + (i * p.r + j0 + j) * p.turn_ld + k0 + row, plane, sh[j][row]);
       }
     }
   }

@@ -1,0 +1,73 @@
+"""Values at the ends of the types: infinities, NaN, the largest numbers, against float64, where they
+stand and what sign they have; finite rows beside them keep their accuracy.
+
+Tolerances as in test_recovery_gpu.py (sums in fp32: 1e-5, a rounding to bf16: 3e-3)."""
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from tests.test_recovery_gpu import TOL_F32, make, ref_backward, ref_forward  # noqa: E402
+
+DEV = "cuda"
+BF16, F32 = torch.bfloat16, torch.float32
+INF, NAN, LARGE = float("inf"), float("nan"), 3.4e38   # LARGE is above bf16's largest, 3.39e38
+
+
+@pytest.fixture(scope="module")
+def T():
+    import paper_2504_05346_b200 as T_
+    from paper_2504_05346_b200 import build as B_
+
+    B_.build()
+    T_.load_library()
+    return T_
+
+
+def same_rows(x, ref, tol):
+    """Infinities and NaN as in the reference, rounded to the result's type (what no fp32 number is near
+    is an infinity there too), the rest close to it, row by row."""
+    ref = ref.to(x.dtype).double().reshape(ref.shape[0], -1)
+    x = x.double().reshape(ref.shape[0], -1)
+    for kind in (torch.isnan, torch.isposinf, torch.isneginf):
+        assert torch.equal(kind(x), kind(ref))
+    fin = torch.isfinite(ref)
+    d = torch.where(fin, x - ref, 0.0).norm(dim=1)
+    assert bool((d <= tol * torch.where(fin, ref, 0.0).norm(dim=1)).all())
+
+
+def strange(X):
+    """Rows with an infinity, two of them, a NaN, and a number that no bf16 is near; a plain one last."""
+    X[1, 5], X[2, 5], X[2, 9], X[3, 2], X[4, 1] = INF, -INF, INF, NAN, LARGE
+    X[5, 1], X[6] = -LARGE, 0.0
+    X[6, 3] = -INF
+    return X
+
+
+# ranks and tokens that take the skinny product on the ALUs and, from 2^14 and 2^16 on, on the tensor
+# cores; rows of whole vectors and others (c is the length of the backward sums)
+@pytest.mark.parametrize("shape", [(40, 136, 72, 3, 4), (300, 131, 200, 2, 20), (2100, 136, 264, 3, 32),
+                                   (2100, 133, 72, 3, 33)], ids=lambda s: "x".join(map(str, s)))
+def test_f32_values(T, shape):
+    Tn, c, b, n, r = shape
+    X, W, A, B, index, scale, dY = make(Tn, c, b, n, r, F32, seed=Tn + r)
+    W[W == 0] = 0.01
+    index[:7] = torch.tensor([0, -1, 0, 1, 0, -1, -1], device=DEV)
+    X, dY = strange(X.clone()), strange(dY.clone())
+    for w in (W, W.clone()):
+        if w is not W:            # and an infinite weight, which meets an infinite value in row 1
+            w[7, 11], w[9, 5], w[5, 8] = INF, -INF, INF
+        Y, V = T.adapter_forward(X, w, A, B, index, scale, check=True)
+        Yr, Vr = ref_forward(X, w, A, B, index, scale)
+        same_rows(V, Vr, 3 * TOL_F32)
+        same_rows(Y, Yr, 3 * TOL_F32)
+        dX, _, _ = T.adapter_backward(dY, X, Vr.float(), w, A, B, index, scale, check=True)
+        same_rows(dX, ref_backward(dY, X, Vr, w, A, B, index, scale)[0], 3 * TOL_F32)
+    # the narrow factors
+    A2, B2 = A.clone(), B.clone()
+    A2[0, 1, 4], B2[1, 3, 2], A2[1, 0, 0] = INF, -INF, LARGE
+    _, V = T.adapter_forward(X, W, A2, B, index, scale)
+    same_rows(V, ref_forward(X, W, A2, B, index, scale)[1], 3 * TOL_F32)
+    dX, _, _ = T.adapter_backward(dY, X, Vr.float(), W, A, B2, index, scale)
+    same_rows(dX, ref_backward(dY, X, Vr, W, A, B2, index, scale)[0], 3 * TOL_F32)
