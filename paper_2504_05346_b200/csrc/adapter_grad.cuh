@@ -27,14 +27,20 @@ thanos_status_t adapter_grads(const AdapterGradSide& a, const AdapterGradSide& b
                               const int32_t* order, const int32_t* off, int64_t T, int64_t n, int r,
                               int accumulate, int32_t* status, cudaStream_t stream);
 
-// x = h + m + l, all 24 bits; what is not finite is in h alone.
+// x = h + m + l, all 24 bits, cut and not rounded: all three have x's sign, and none is zero beside
+// another, so that an infinite factor of x meets three numbers of x's sign (a zero would make a NaN
+// of it; what stands in for one is 2^-40 of x).  What is not finite is in l, beside two ones: a finite
+// factor meets it once.
 __device__ __forceinline__ void split3(float x, __nv_bfloat16& h, __nv_bfloat16& m,
                                        __nv_bfloat16& l) {
-  h = __float2bfloat16_rn(x);
-  const float hf = __bfloat162float(h);
-  const float rest = isfinite(hf) ? x - hf : 0.f;
-  m = __float2bfloat16_rn(rest);
-  l = __float2bfloat16_rn(rest - __bfloat162float(m));
+  const bool odd = !isfinite(x);
+  const float hf = odd ? copysignf(1.f, x) : __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
+  const float rest = odd ? 0.f : x - hf;
+  const float mf = __uint_as_float(__float_as_uint(rest) & 0xFFFF0000u), lf = rest - mf;
+  const float stand_in = hf * 0x1p-40f;
+  h = __float2bfloat16_rn(hf);
+  m = __float2bfloat16_rn(odd ? hf : mf != 0.f ? mf : stand_in);
+  l = __float2bfloat16_rn(odd ? x : lf != 0.f ? lf : stand_in);
 }
 
 }  // namespace thanos

@@ -71,3 +71,36 @@ def test_f32_values(T, shape):
     same_rows(V, ref_forward(X, W, A2, B, index, scale)[1], 3 * TOL_F32)
     dX, _, _ = T.adapter_backward(dY, X, Vr.float(), W, A, B2, index, scale)
     same_rows(dX, ref_backward(dY, X, Vr, W, A, B2, index, scale)[0], 3 * TOL_F32)
+
+
+@pytest.mark.parametrize("shape", [(5, 136, 72, 5, 4), (40, 136, 72, 5, 4), (300, 131, 200, 5, 20),
+                                   (2100, 1290, 1544, 5, 12), (700, 264, 136, 5, 100)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_bf16_values(T, shape):
+    """The gradients' factor is three planes that meet the activations one by one."""
+    Tn, c, b, n, r = shape
+    X, W, A, B, index, scale, dY = make(max(Tn, 7), c, b, n, r, BF16, seed=Tn + r)
+    index[:7] = torch.tensor([0, 1, 2, 3, 4, 0, 1], device=DEV)
+    W[W == 0], B[B == 0], A[A == 0] = 0.01, 0.01, 0.01
+    lim = 6e-3     # a rounding of the result, one of the adapter's factor, row by row
+    for bad_x, bad_y in ((True, False), (False, True), (True, True)):
+        X2, dY2 = X.clone(), dY.clone()
+        if bad_x:
+            strange(X2)
+            X2[4, 1], X2[5, 1] = 3.3e38, -3.3e38    # nearest bf16 of LARGE would be an infinity
+        if bad_y:
+            strange(dY2)
+            dY2[4, 1], dY2[5, 1] = 3.3e38, -3.3e38
+        Y, V = T.adapter_forward(X2[:Tn], W, A, B, index[:Tn], scale, check=True)
+        Yr, Vr = ref_forward(X2[:Tn], W, A, B, index[:Tn], scale)
+        same_rows(V, Vr, 3 * TOL_F32)
+        same_rows(Y, Yr, lim)
+        Vf = Vr.float()
+        dX, dA, dB = T.adapter_backward(dY2[:Tn], X2[:Tn], Vf, W, A, B, index[:Tn], scale, check=True)
+        rX, rA, _ = ref_backward(dY2[:Tn], X2[:Tn], Vf, W, A, B, index[:Tn], scale)
+        # dB = s_i times an fp32 sum, which may be an infinity where the product would not
+        rB = ref_backward(dY2[:Tn], X2[:Tn], Vf, W, A, B, index[:Tn], torch.ones_like(scale))[2]
+        rB = rB.float().double() * scale.double()[:, None, None]
+        same_rows(dX, rX, lim)
+        same_rows(dA, rA, 3 * TOL_F32)
+        same_rows(dB, rB, 3 * TOL_F32)
