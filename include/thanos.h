@@ -352,8 +352,8 @@ thanos_status_t thanos_fp32_fma_probe(float* out, int64_t out_elems, int32_t cta
  *  8 <= b <= 65536, b % 8 == 0; 1 <= c <= 2^20; 0 <= n_tok <= 2^24 (0 is a no-op);
  *  1 <= r <= 128 (ignored when n_adapters is 0); ceil(max(c, b, n_adapters r) / 128) *
  *  ceil(n_tok / 32) <= 2^27.
- *  Sums are fp32.  With 16-bit types s_i V[t] is rounded to bf16 before it meets B_i where the
- *  product is large (its 256 x 256 tiles give half of the SM pairs work), and Y once.
+ *  Sums are fp32, and so is s_i V[t] where it meets B_i (two bf16 planes, 2^-16 of it, where the
+ *  product is large: its 256 x 256 tiles give half of the SM pairs work).  A 16-bit Y is rounded once.
  *  workspace: thanos_adapter_workspace_bytes(0, ...) bytes.  Its first int32 is the device status
  *           word of the call, cleared when the call starts.
  * The result does not depend on the order of concurrent work: the same inputs give the same bits.

@@ -178,41 +178,46 @@ __device__ __forceinline__ int valid_adapter(const Params& p, int t) {
   return i >= 0 && i < p.n_adapters ? i : -1;
 }
 
-// The factor of a token's row: fp32 s_i V[t, j] rounded to bf16, as the tensor cores see it.
-__device__ __forceinline__ __nv_bfloat16 token_factor(const Params& p, int t, int i, int j) {
-  const float v = p.V[(int64_t)t * p.r + j];
-  return __float2bfloat16_rn(p.scale ? p.scale[i] * v : v);
-}
-
-// The 16 columns j0.. of a token's factor as packed bf16: s_i V[t, j] for the adapter's own tokens,
-// zeros for all others and beyond the rank.
-__device__ __forceinline__ void factor_row(const Params& p, int t, bool own, float sc, int j0,
-                                           uint32_t (&w)[8]) {
-  float v[16];
+// The 16 columns j0.. of a token's factor, sc V[t, j], zeros beyond the rank.
+__device__ __forceinline__ void token_factor(const Params& p, int t, float sc, int j0, float (&v)[16]) {
+  const float* src = p.V + (int64_t)t * p.r + j0;
 #pragma unroll
   for (int j = 0; j < 16; ++j) v[j] = 0.f;
-  if (own) {
-    const float* src = p.V + (int64_t)t * p.r + j0;
-    if (p.r % 4 == 0) {
+  if (p.r % 4 == 0) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (j0 + 4 * e < p.r) {
-          const float4 f = *reinterpret_cast<const float4*>(src + 4 * e);
-          v[4 * e] = f.x;
-          v[4 * e + 1] = f.y;
-          v[4 * e + 2] = f.z;
-          v[4 * e + 3] = f.w;
-        }
-    } else {
+    for (int e = 0; e < 4; ++e)
+      if (j0 + 4 * e < p.r) {
+        const float4 f = *reinterpret_cast<const float4*>(src + 4 * e);
+        v[4 * e] = sc * f.x;
+        v[4 * e + 1] = sc * f.y;
+        v[4 * e + 2] = sc * f.z;
+        v[4 * e + 3] = sc * f.w;
+      }
+  } else {
 #pragma unroll
-      for (int j = 0; j < 16; ++j)
-        if (j0 + j < p.r) v[j] = src[j];
-    }
+    for (int j = 0; j < 16; ++j)
+      if (j0 + j < p.r) v[j] = sc * src[j];
   }
+}
+
+// Sixteen values as two planes of packed bf16: what the first cuts off (nothing of an infinity or NaN)
+// is rounded in the second, 2^-16 of the value, far below the rounding of the result.
+__device__ __forceinline__ void factor_planes(const float (&v)[16], uint32_t (&hi)[8],
+                                              uint32_t (&lo)[8]) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e)
-    w[e] = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(sc * v[2 * e])) |
-           ((uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(sc * v[2 * e + 1])) << 16);
+  for (int e = 0; e < 8; ++e) {
+    uint32_t h[2], l[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const float x = v[2 * e + k];
+      const bool odd = !isfinite(x);
+      h[k] = odd ? __bfloat16_as_ushort(__float2bfloat16_rn(x)) : __float_as_uint(x) >> 16;
+      const float rest = odd ? 0.f : x - __uint_as_float(h[k] << 16);
+      l[k] = __bfloat16_as_ushort(__float2bfloat16_rn(rest));
+    }
+    hi[e] = h[0] | h[1] << 16;
+    lo[e] = l[0] | l[1] << 16;
+  }
 }
 
 __device__ __forceinline__ void clean_vector(uint4* at, int* poison) {
@@ -235,8 +240,10 @@ __device__ __noinline__ float poison_terms(const Params& p, int m, int t) {
   for (int j = 0; j < p.r; ++j) {
     const __nv_bfloat16 w =
         p.P[(int64_t)i * p.p_adapter + (AMN ? (int64_t)j * p.ldp + m : (int64_t)m * p.ldp + j)];
-    if (bf16_nonfinite(__bfloat16_as_ushort(w)))
-      s += __bfloat162float(token_factor(p, t, i, j)) * __bfloat162float(w);
+    if (bf16_nonfinite(__bfloat16_as_ushort(w))) {
+      const float v = p.V[(int64_t)t * p.r + j];
+      s += (p.scale ? p.scale[i] * v : v) * __bfloat162float(w);
+    }
   }
   return s;
 }
@@ -1172,9 +1179,12 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
 // tile.  Two accumulators: the epilogue of a tile runs beside the next tile's products.
 //
 // Adapter part (PROJ_OUT): for every adapter that occurs in the token tile, k is extended by its rank
-// in chunks of 16, four chunks a stage, in a ring of their own that four more warps fill a tile
+// in chunks of 16, two to a stage, in a ring of their own that four more warps fill a tile
 // ahead: the wide factor's rows come by TMA (32-byte swizzle; MN-major: 128-byte), the factor of the
-// tokens, s_i V[t], is built in bf16 with zero rows for tokens of other adapters.  0 times a
+// tokens, s_i V[t], is built as two bf16 planes with zero rows for tokens of other adapters.  (One
+// plane would give a token a result in a large batch that is 2^-9 of the adapter part off what it gets
+// in a small one.  The second costs 1 to 2 % where a tile has few adapters, 8 % with 16 adapters mixed
+// token by token, 12 % at rank 128.)  0 times a
 // non-finite weight would reach those tokens, so the chunk is scanned, non-finite weights become
 // zeros and the epilogue adds their products to the adapter's own tokens.
 //
@@ -1184,12 +1194,16 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
 constexpr int PTM = 256;
 constexpr int PSTAGE_BYTES = 2 * A_BYTES;
 constexpr int CHUNK_BYTES = TM * 16 * 2;      // a 16-wide chunk of an adapter's wide factor
-constexpr int CHUNKS = 4;                     // chunks per stage
+constexpr int EPLANE_BYTES = 128 * 16 * 2;    // a plane of the tokens' factors
+constexpr int CHUNKS = 2;                     // chunks per stage
 constexpr int ESTAGES = 2;
+constexpr int FACTORS = CHUNKS * CHUNK_BYTES; // offset of the factors in a stage
 __host__ __device__ constexpr int pair_stages(int epi) { return epi == PROJ_OUT ? 5 : 7; }
 __host__ __device__ constexpr int pair_threads(int epi) { return epi == PROJ_OUT ? 448 : 320; }
 constexpr size_t PSMEM_BYTES = (size_t)7 * PSTAGE_BYTES + 1024 + 512;
-static_assert(pair_stages(PROJ_OUT) + ESTAGES == 7, "shared memory of the rings");
+static_assert(pair_stages(PROJ_OUT) + ESTAGES == 7 &&
+                  FACTORS + 2 * CHUNKS * EPLANE_BYTES <= PSTAGE_BYTES,
+              "shared memory of the rings");
 
 __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap* map,
                                                  uint32_t lead_bar, int x, int y, int z) {
@@ -1401,14 +1415,14 @@ pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
             ok = mbar_wait(ready_bar(e), ephase, abort_flag);
             tc_fence_after();
             if (ok) {
-              const uint32_t sa = ering_base + (uint32_t)e * PSTAGE_BYTES;
-              const uint32_t sb = sa + A_BYTES;
+              const uint32_t st = ering_base + (uint32_t)e * PSTAGE_BYTES;
               const int nc = min(CHUNKS, total - c0);
               for (int c = 0; c < nc; ++c) {
-                const uint32_t ca = sa + c * CHUNK_BYTES;
-                const uint64_t ad = AMN ? make_desc(ca, CHUNK_BYTES / 2, 1024, SW128)
-                                        : make_desc(ca, 16, 256, SW32);
-                tc_mma_bf16_pair(d, ad, make_desc(sb + c * 128 * 32, 16, 256, SW32), idesc, 1u);
+                const uint32_t sa = st + c * CHUNK_BYTES, sb = st + FACTORS + 2 * c * EPLANE_BYTES;
+                const uint64_t ad = AMN ? make_desc(sa, CHUNK_BYTES / 2, 1024, SW128)
+                                        : make_desc(sa, 16, 256, SW32);
+                tc_mma_bf16_pair(d, ad, make_desc(sb, 16, 256, SW32), idesc, 1u);
+                tc_mma_bf16_pair(d, ad, make_desc(sb + EPLANE_BYTES, 16, 256, SW32), idesc, 1u);
               }
               tc_commit_pair(eempty_bar(e));
             }
@@ -1434,43 +1448,108 @@ pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
       int e = 0;
       uint32_t ephase = 0;
       bool ok = true;
+      // Thread 64 brings the wide factors, ahead of the stage that is worked on as far as the ring is
+      // free: what follows ranks ij.. of the iat-th adapter of tile it goes to slot ie next.
+      int ahead = 0, it = pair, iat = 0, ij = 0, icount = 0, im0 = 0, ie = 0;
+      const int32_t* ilist = nullptr;
+      uint32_t iphase = 0;
+      auto open_tile = [&]() {  // the next tile with adapters, from `it` on
+        for (; it < n_tiles; it += npairs) {
+          const PairTile tl = pair_tile(p, it);
+          icount = p.tile_count[tl.tn];
+          if (icount == 0) continue;
+          im0 = tl.tm * PTM + 128 * (int)rank;
+          ilist = p.tile_list + (int64_t)tl.tn * p.nt;
+          return;
+        }
+      };
+      auto bring = [&](bool is_free) {
+        if (it >= n_tiles || !(is_free || mbar_test(eempty_bar(ie), iphase ^ 1u))) return false;
+        const int nc = min(CHUNKS, (icount - iat) * p.chunks - (ij >> 4));
+        mbar_expect_tx(land_bar(ie), nc * CHUNK_BYTES);
+        uint32_t dst = ering_base + (uint32_t)ie * PSTAGE_BYTES;
+        for (int q = 0; q < nc; ++q, dst += CHUNK_BYTES) {
+          const int who = ilist[iat];
+          if (AMN) {
+            tma_load_3d(dst, &mapP, land_bar(ie), im0, ij, who);
+            tma_load_3d(dst + CHUNK_BYTES / 2, &mapP, land_bar(ie), im0 + 64, ij, who);
+          } else {
+            tma_load_3d(dst, &mapP, land_bar(ie), ij, im0, who);
+          }
+          ij += 16;
+          if (ij >= p.r) {
+            ij = 0;
+            ++iat;
+          }
+        }
+        if (++ie == ESTAGES) {
+          ie = 0;
+          iphase ^= 1u;
+        }
+        if (iat == icount) {
+          iat = 0;
+          it += npairs;
+          open_tile();
+        }
+        return true;
+      };
+      if (threadIdx.x == 64) open_tile();
+      __syncwarp();
       for (int t = pair; t < n_tiles && ok; t += npairs) {
         const PairTile tl = pair_tile(p, t);
-        const int m0 = tl.tm * PTM + 128 * (int)rank;
         const int tok = tl.tn * p.nt + half * (int)rank + row;
         const int mine = row < half && tok < p.N ? valid_adapter(p, tok) : -1;
         const float sc = mine >= 0 && p.scale ? p.scale[mine] : 1.f;
-        const int total = p.tile_count[tl.tn] * p.chunks;
-        for (int c0 = 0; c0 < total && ok; c0 += CHUNKS) {
-          ok = mbar_wait_warp(eempty_bar(e), ephase ^ 1u, abort_flag);
-          if (!ok) break;
-          unsigned char* st = ering + (size_t)e * PSTAGE_BYTES;
-          const uint32_t dst = ering_base + (uint32_t)e * PSTAGE_BYTES;
+        const int count = p.tile_count[tl.tn], total = count * p.chunks;
+        const int32_t* list = p.tile_list + (int64_t)tl.tn * p.nt;
+        float v0[16];                    // the token's first sixteen ranks, all of them up to rank 16
+        if (count > 0 && mine >= 0) token_factor(p, tok, sc, 0, v0);
+        int j0 = 0, at = 0, seen = 0;    // the next chunk: ranks j0.. of the at-th adapter of the tile
+        for (int c0 = 0; c0 < total; c0 += CHUNKS) {
           const int nc = min(CHUNKS, total - c0);
-          if (threadIdx.x == 64) {
-            mbar_expect_tx(land_bar(e), nc * CHUNK_BYTES);
-            for (int q = 0; q < nc; ++q) {
-              const int who = p.tile_list[(int64_t)tl.tn * p.nt + (c0 + q) / p.chunks];
-              const int j = 16 * ((c0 + q) % p.chunks);
-              if (AMN) {
-                tma_load_3d(dst + q * CHUNK_BYTES, &mapP, land_bar(e), m0, j, who);
-                tma_load_3d(dst + q * CHUNK_BYTES + CHUNK_BYTES / 2, &mapP, land_bar(e), m0 + 64, j,
-                            who);
+          // the factors of the stage's chunks, loaded while the stage before is on its way
+          uint32_t hi[CHUNKS][8] = {}, lo[CHUNKS][8] = {};
+#pragma unroll
+          for (int q = 0; q < CHUNKS; ++q) {
+            if (j0 == 0 && (at & 31) == 0) seen = at + lane < count ? list[at + lane] : -1;
+            const int who = __shfl_sync(0xffffffffu, seen, at & 31);
+            if (q < nc && who == mine) {
+              if (j0 == 0) {
+                factor_planes(v0, hi[q], lo[q]);
               } else {
-                tma_load_3d(dst + q * CHUNK_BYTES, &mapP, land_bar(e), j, m0, who);
+                float v[16];
+                token_factor(p, tok, sc, j0, v);
+                factor_planes(v, hi[q], lo[q]);
               }
             }
+            j0 += 16;
+            if (j0 >= p.r) {
+              j0 = 0;
+              ++at;
+            }
+          }
+          ok = mbar_wait_warp(eempty_bar(e), ephase ^ 1u, abort_flag);
+          if (!ok) break;
+          if (threadIdx.x == 64) {
+            if (ahead == 0 && bring(true)) ++ahead;
+            while (ahead < ESTAGES && bring(false)) ++ahead;
+            --ahead;
           }
           __syncwarp();
-          for (int q = 0; q < nc; ++q) {
-            const int who = p.tile_list[(int64_t)tl.tn * p.nt + (c0 + q) / p.chunks];
-            uint32_t w[8];
-            factor_row(p, tok, who == mine, sc, 16 * ((c0 + q) % p.chunks), w);
+          unsigned char* st = ering + (size_t)e * PSTAGE_BYTES;
+#pragma unroll
+          for (int q = 0; q < CHUNKS; ++q) {
+            if (q >= nc) break;
             // 32-byte rows, 32-byte swizzle: the 16-byte halves swap every four rows
-            unsigned char* fac = st + A_BYTES + (size_t)q * 128 * 32 + row * 32;
+            unsigned char* fac = st + FACTORS + (size_t)(2 * q) * EPLANE_BYTES + row * 32;
             const int sw = ((row >> 2) & 1) << 4;
-            *reinterpret_cast<uint4*>(fac + sw) = make_uint4(w[0], w[1], w[2], w[3]);
-            *reinterpret_cast<uint4*>(fac + (16 ^ sw)) = make_uint4(w[4], w[5], w[6], w[7]);
+            *reinterpret_cast<uint4*>(fac + sw) = make_uint4(hi[q][0], hi[q][1], hi[q][2], hi[q][3]);
+            *reinterpret_cast<uint4*>(fac + (16 ^ sw)) =
+                make_uint4(hi[q][4], hi[q][5], hi[q][6], hi[q][7]);
+            fac += EPLANE_BYTES;
+            *reinterpret_cast<uint4*>(fac + sw) = make_uint4(lo[q][0], lo[q][1], lo[q][2], lo[q][3]);
+            *reinterpret_cast<uint4*>(fac + (16 ^ sw)) =
+                make_uint4(lo[q][4], lo[q][5], lo[q][6], lo[q][7]);
           }
           ok = mbar_wait_warp(land_bar(e), ephase, abort_flag);
           if (!ok) break;

@@ -180,3 +180,37 @@ def test_masked_step_on_pairs(T, shape, kind, wd):
     Wo, Mo = T.orthogonal_step(W, M, Gp, mask, lr=lr, gain=gain, momentum=mu, weight_decay=dec,
                                W_out=nan(*shape, dtype=wd), M_out=nan(*shape))
     assert torch.equal(Wo, Wi) and torch.equal(Mo, Mi)
+
+
+@pytest.mark.parametrize("shape", SHAPES[:6] + [(40, 1290, 1544, 6, 12, "mixed")],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_adapter_part_is_rounded_once_whatever_the_batch(T, shape):
+    """Without the frozen part, every entry of a bf16 result is within half a unit of itself (8 bits: at
+    most 2^-8 of it) and 2^-14 of its terms' magnitudes: 2^-16 for two planes of the factor, the rest for fp32 sums."""
+    Tn, c, b, n, r, order = shape
+    X, W, A, B, index, scale, dY = make(Tn, c, b, n, r, BF16, seed=c + r, order=order)
+    W = torch.zeros_like(W)
+    D = torch.float64
+    i = index.long().clamp(min=0)
+    s = torch.where(index >= 0, scale[i], 0.0).to(D)[:, None]
+
+    def terms(v, wide):     # sum over ranks of factor times wide, and of their magnitudes
+        out = torch.zeros(Tn, wide.shape[1], dtype=D, device=DEV)
+        size = torch.zeros_like(out)
+        for k in range(n):
+            own = (index == k).nonzero()[:, 0]
+            out[own] = v[own] @ wide[k].to(D).T
+            size[own] = v[own].abs() @ wide[k].to(D).T.abs()
+        return out, size
+
+    Y, V = forward(T, X, W, A, B, index, scale)
+    ref, size = terms(s * ref_forward(X, W, A, B, index, scale)[1], B)
+    assert bool(((Y.to(D) - ref).abs() <= 2.0 ** -8 * ref.abs() + 2.0 ** -14 * size).all())
+    dX, _, _ = backward(T, dY, X, V, W, A, B, index, scale)
+    u = torch.zeros(Tn, r, dtype=D, device=DEV)
+    for k in range(n):
+        own = (index == k).nonzero()[:, 0]
+        u[own] = dY[own].to(D) @ B[k].to(D)
+    # U is an fp32 sum of c terms: 2^-24 c^0.5 of their magnitudes goes into it, here below 2^-14 of size
+    ref, size = terms(s * u, A.transpose(1, 2))
+    assert bool(((dX.to(D) - ref).abs() <= 2.0 ** -8 * ref.abs() + 2.0 ** -14 * size).all())
