@@ -416,7 +416,9 @@ size_t thanos_adapter_workspace_bytes(int32_t backward, int64_t n_tok, int64_t c
  *           shorter side of up to 64, or 32 with fp32 weights, is computed in fp32.)
  *  1 <= steps <= 32, eps >= 0; 0 <= batch <= 65535 (0 is a no-op: the matrices may be NULL and the
  *  status word is not written), 1 <= m, n <= 65536.
- *  A zero matrix gives zeros (eps > 0); a matrix with an infinity or NaN gives NaN.
+ *  A zero matrix gives zeros (eps > 0); a matrix with an infinity or NaN gives NaN.  Squares may
+ *  leave fp32's range.  Where a side is above 64 (32 with fp32 weights), a matrix whose norm is some
+ *  10^4 times below eps loses bits, and smaller ones become zeros: eps says what counts as zero.
  *  workspace: thanos_orthogonal_workspace_bytes(batch, m, n) bytes; its first int32 is the device
  *           status word of the call.
  * Same inputs, same bits.

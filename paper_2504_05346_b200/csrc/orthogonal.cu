@@ -158,6 +158,25 @@ __device__ __forceinline__ void update_batch(const StepParams& p, int64_t at, in
                                    : mo[u][e];
 }
 
+// Whether fp32 squares that add up to this may have left fp32's range: beyond it, or below it where
+// eps does not hide that.
+__device__ __forceinline__ bool squares_out_of_range(float sum, float eps) {
+  return !(sum < 1e36f) || (sum < 1e-28f && eps < 1e-8f);
+}
+
+// A block's sum of squares once more, in fp64.
+template <int VEC>
+__device__ __noinline__ double squares_again(const StepParams& p, int64_t base, int64_t step,
+                                             int64_t mn) {
+  double sum = 0.0;
+  for (int64_t e0 = ((int64_t)blockIdx.x * 256 + threadIdx.x) * VEC; e0 < mn; e0 += step) {
+    float v[1][VEC];
+    update_batch<VEC, 1, false>(p, base + e0, step, 1, v);
+    for (int i = 0; i < VEC; ++i) sum = fma((double)v[0][i], (double)v[0][i], sum);
+  }
+  return sum;
+}
+
 // New momentum and the sums of squares of the iteration's input (fp32 over a thread's share, fp64
 // from there).
 template <int VEC>
@@ -179,6 +198,10 @@ __global__ void __launch_bounds__(256) norm_kernel(const StepParams p) {
     sum += (double)part;
   }
   sum = block_sum(sum, red);
+  if (squares_out_of_range((float)sum, p.eps)) {
+    __syncthreads();
+    sum = block_sum(squares_again<VEC>(p, base, step, mn), red);
+  }
   if (threadIdx.x == 0) p.part[(int64_t)blockIdx.y * p.parts + blockIdx.x] = sum;
 }
 
@@ -196,7 +219,9 @@ __global__ void __launch_bounds__(256) split_kernel(const StepParams p) {
   double sq = 0.0;
   for (int i = threadIdx.x; i < p.parts; i += 256) sq += p.part[(int64_t)blockIdx.y * p.parts + i];
   sq = block_sum(sq, red);
-  const float f = p.unit / ((float)sqrt(sq) + p.eps);
+  const double norm = sqrt(sq);
+  float f = p.unit / ((float)norm + p.eps);
+  if (norm > 1e38) f = (float)((double)p.unit / (norm + (double)p.eps));  // beyond fp32, or nearly
   const int64_t base = (int64_t)blockIdx.y * (int64_t)p.m * p.n;
   const int tn = (p.n + 63) / 64;
   const int64_t tiles = (int64_t)((p.m + 63) / 64) * tn;
@@ -461,6 +486,63 @@ __device__ __forceinline__ float4 sum_parts(const float4* part, int first, int h
   return sum;
 }
 
+// The Gram matrix of a matrix whose squares leave fp32's range, once more by this one CTA: X scaled by
+// the power of two that brings its largest value to between one and two.  Returns that exponent (the
+// product is 2^(-2 e) of what it stands for); with infinities or NaN everything stays as it is.
+// The matrices behind the first are used for staging and left zero.
+template <int TS>
+__device__ __noinline__ int gram_again(const SmallParams& p) {
+  extern __shared__ __align__(16) float mats[];
+  __shared__ uint32_t tops[STEP_THREADS / 32];
+  constexpr int LD = small_ld(TS), SZ = small_size(TS);
+  float* Xs = mats + SZ;
+  const int64_t base = (int64_t)blockIdx.x * p.s * p.l;
+  const int q = (p.s + 3) / 4, ld = 4 * q + 4, ti = threadIdx.x / q, tj = threadIdx.x - ti * q;
+  uint32_t top = 0;  // largest magnitude, as bits
+  for (int c0 = 0; c0 < p.l; c0 += p.tile_cols) {
+    const int cols = min(p.tile_cols, p.l - c0);
+    __syncthreads();
+    stage_columns<1, false>(p, base, c0, cols, Xs, ld);
+    __syncthreads();
+    for (int e = threadIdx.x; e < cols * 4 * q; e += STEP_THREADS)
+      top = max(top, __float_as_uint(Xs[e / (4 * q) * ld + e % (4 * q)]) & 0x7FFFFFFFu);
+  }
+  top = __reduce_max_sync(0xffffffffu, top);
+  if ((threadIdx.x & 31) == 0) tops[threadIdx.x >> 5] = top;
+  __syncthreads();
+  for (int w = 0; w < STEP_THREADS / 32; ++w) top = max(top, tops[w]);
+  int e = 0;
+  if (top > 0 && top < 0x7F800000u) {
+    e = max((int)(top >> 23) - 127, -120);
+    const float scale = ldexpf(1.f, -e);
+    float acc[4][4] = {};
+    for (int c0 = 0; c0 < p.l; c0 += p.tile_cols) {
+      const int cols = min(p.tile_cols, p.l - c0);
+      __syncthreads();
+      stage_columns<1, false>(p, base, c0, cols, Xs, ld);
+      __syncthreads();
+      if (ti >= q) continue;
+      for (int c = 0; c < cols; ++c) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            acc[i][j] = fmaf(scale * Xs[c * ld + 4 * ti + i], scale * Xs[c * ld + 4 * tj + j], acc[i][j]);
+      }
+    }
+    if (ti < q) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) mats[(4 * ti + i) * LD + 4 * tj + j] = acc[i][j];
+    }
+  }
+  __syncthreads();
+  for (int k = SZ + threadIdx.x; k < 5 * SZ; k += STEP_THREADS) mats[k] = 0.f;
+  __syncthreads();
+  return e;
+}
+
 template <int TS>
 __global__ void __launch_bounds__(STEP_THREADS) steps_kernel(const SmallParams p) {
   extern __shared__ __align__(16) float mats[];
@@ -468,7 +550,7 @@ __global__ void __launch_bounds__(STEP_THREADS) steps_kernel(const SmallParams p
   constexpr int LD = small_ld(TS), SZ = small_size(TS);
   float *S = mats, *T = mats + 3 * SZ;
   int Q = 2 * SZ, U = 4 * SZ;
-  __shared__ float norm;
+  __shared__ float square;
   const int s = p.s, ss = s * s;
   for (int e = threadIdx.x; e < 5 * SZ; e += STEP_THREADS) mats[e] = 0.f;
   __syncthreads();
@@ -499,14 +581,24 @@ __global__ void __launch_bounds__(STEP_THREADS) steps_kernel(const SmallParams p
     }
   }
   __syncthreads();
-  if (threadIdx.x < 32) {
-    float t = 0.f;
-    for (int i = threadIdx.x; i < s; i += 32) t += S[i * LD + i];
-    for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
-    if (threadIdx.x == 0) norm = sqrtf(t) + p.u.eps;
+  auto trace = [&]() {
+    if (threadIdx.x < 32) {
+      float t = 0.f;
+      for (int i = threadIdx.x; i < s; i += 32) t += S[i * LD + i];
+      for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+      if (threadIdx.x == 0) square = t;
+    }
+    __syncthreads();
+  };
+  trace();
+  int exponent = 0;
+  float eps = p.u.eps;
+  if (squares_out_of_range(square, eps)) {
+    exponent = gram_again<TS>(p);
+    eps = ldexpf(eps, -exponent);
+    trace();
   }
-  __syncthreads();
-  const float inv = 1.f / norm;
+  const float inv = 1.f / (sqrtf(square) + eps);
   for (int i = threadIdx.x; i < s * LD; i += STEP_THREADS) S[i] = S[i] * inv * inv;
   __syncthreads();
   // T held partial sums: its row s has to be zero again
@@ -528,12 +620,13 @@ __global__ void __launch_bounds__(STEP_THREADS) steps_kernel(const SmallParams p
     }
   }
   float* out = p.Q + (int64_t)blockIdx.x * ss;
+  const float inv_out = exponent == 0 ? inv : ldexpf(inv, -exponent);
   for (int r = threadIdx.x >> 5; r < s; r += STEP_THREADS / 32)
     if constexpr (TS <= 2) {
       if ((threadIdx.x & 31) < s)
-        out[r * s + (threadIdx.x & 31)] = mats[Q + r * LD + (threadIdx.x & 31)] * inv;
+        out[r * s + (threadIdx.x & 31)] = mats[Q + r * LD + (threadIdx.x & 31)] * inv_out;
     } else {
-      for (int c = threadIdx.x & 31; c < s; c += 32) out[r * s + c] = mats[Q + r * LD + c] * inv;
+      for (int c = threadIdx.x & 31; c < s; c += 32) out[r * s + c] = mats[Q + r * LD + c] * inv_out;
     }
 }
 

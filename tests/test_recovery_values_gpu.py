@@ -104,3 +104,59 @@ def test_bf16_values(T, shape):
         same_rows(dX, rX, lim)
         same_rows(dA, rA, 3 * TOL_F32)
         same_rows(dB, rB, 3 * TOL_F32)
+
+
+def iterate(G, eps, steps=5, coef=(3.4445, -4.7750, 2.0315)):
+    a, b, c = coef
+    X = G.double()
+    tall = X.shape[-2] > X.shape[-1]
+    X = X.mT if tall else X
+    X = X / (torch.linalg.matrix_norm(X, keepdim=True) + eps)
+    for _ in range(steps):
+        S = X @ X.mT
+        X = a * X + (b * S + c * (S @ S)) @ X
+    return X.mT if tall else X
+
+
+# sides of up to 16, 32 and 64, and beyond, where other kernels take the norm; several chunks
+MATRICES = [(3, 16, 4096), (1, 9000, 20), (1, 48, 300), (2, 64, 1000), (1, 7, 3), (1, 300, 260), (2, 65, 130)]
+
+
+@pytest.mark.parametrize("scale", [1e19, 1e25, 1e37, 1e-18, 1e-25, 1e-35])
+@pytest.mark.parametrize("shape", MATRICES, ids=lambda s: "x".join(map(str, s)))
+def test_update_of_matrices_whose_squares_leave_fp32(T, shape, scale):
+    """fp16 operands and a bf16 result: 4e-3, as for every matrix; fp32 weights 4e-4 (at the ends of
+    fp32 the reciprocal of the norm has at least 14 bits)."""
+    gen = torch.Generator(device=DEV).manual_seed(23)
+    G = torch.randn(shape, generator=gen, device=DEV) * scale
+    mixed = G.clone()          # chunks of another size, some of nothing: the first part decides
+    half = shape[2] // 2 if shape[2] >= shape[1] else shape[1] // 2
+    if shape[2] >= shape[1]:
+        mixed[..., half:] *= 1e-8
+        mixed[..., 3 * half // 2:] = 0
+    else:
+        mixed[:, half:] *= 1e-8
+        mixed[:, 3 * half // 2:] = 0
+    for M in (G, mixed):
+        for eps in (0.0, 1e-7 * scale):
+            eps = torch.tensor(eps).item()
+            ref = iterate(M, eps)
+            O = T.orthogonalise(M, eps=eps, check=True)
+            W, _ = T.orthogonal_step(torch.zeros_like(M), torch.zeros_like(M), M, lr=1.0, momentum=0.0,
+                                     eps=eps, check=True)
+            for i in range(shape[0]):
+                n = ref[i].norm()
+                assert (O[i].double() - ref[i]).norm() <= 4e-3 * n
+                assert (W[i].double() + ref[i]).norm() <= 4e-4 * n
+
+
+@pytest.mark.parametrize("shape", MATRICES, ids=lambda s: "x".join(map(str, s)))
+def test_update_of_zeros_and_of_what_is_not_finite(T, shape):
+    z = torch.zeros(shape, device=DEV)
+    assert not T.orthogonalise(z, check=True).any()
+    for bad in (INF, NAN):
+        G = torch.randn(shape, device=DEV)
+        G[0, -1, -1] = bad
+        O = T.orthogonalise(G, check=True)
+        assert torch.isnan(O[0].float()).all()
+        assert torch.isfinite(O[1:].float()).all()
