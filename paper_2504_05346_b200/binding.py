@@ -604,6 +604,8 @@ def adapter_forward(X: torch.Tensor, W: torch.Tensor, A: Optional[torch.Tensor] 
                     V = scale.new_empty((T, r))
                 else:
                     _dense(V, (T, r), torch.float32, dev, "V")
+            else:
+                V = None     # a buffer that was passed in is not written
             workspace = _scratch(workspace, _adapter_workspace(0, T, c, b, n, r, dt), X)
         ldy = _rows(out, c, dev, "out")
         _check(lib.thanos_adapter_forward(out.data_ptr(), ldy, _ptr(V), X.data_ptr(), ldx,

@@ -65,3 +65,13 @@ def test_empty_batches(T):
     assert T.launch_count() == before
     with pytest.raises(T.ThanosError):
         T.orthogonalise(torch.empty((3, 0, 8), device=DEV))
+
+
+def test_no_adapters_no_v(T):
+    """Without adapters there is no V, also where a buffer for one or an empty set of adapters is given."""
+    X, W, A, B, index, scale, _ = make(40, 96, 128, 3, 8, BF16, seed=9)
+    buf = torch.full((40, 8), 7.0, device=DEV)
+    Y, V = T.adapter_forward(X, W, V=buf, check=True)
+    Y2, V2 = T.adapter_forward(X, W, A[:0], B[:0], torch.full_like(index, -1), scale[:0], V=buf,
+                               check=True)
+    assert V is None and V2 is None and torch.equal(Y, Y2) and bool((buf == 7.0).all())
