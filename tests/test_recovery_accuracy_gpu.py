@@ -1,0 +1,56 @@
+"""Accuracy of what the recovery operators keep in fp32, tighter than the tests of their paths: it
+would show the loss of an operand plane or of the drains of the tensor cores' accumulators.
+
+A product is exact; the tensor cores cut up to 2^-23 of an accumulator each time they add to it, half of
+that on average, and between two drains they add 32 times (512 terms; 64 times in fp32 products) to sums
+that grow like the square root: 32 2^-24 2/3 = 1.3e-6 of the result, always towards zero, and the fp32
+additions behind the drains add some 2^-24.  2e-6 in all.  (Sums over 8192 terms without drains cut 512
+times; without the third plane of the fp32 factor each term is off by 2^-17.)"""
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from tests.test_recovery_gpu import make, ref_backward, ref_forward, rel  # noqa: E402
+
+TOL = 2e-6
+
+
+@pytest.fixture(scope="module")
+def T():
+    import paper_2504_05346_b200 as T_
+    from paper_2504_05346_b200 import build as B_
+
+    B_.build()
+    T_.load_library()
+    return T_
+
+
+@pytest.mark.parametrize("shape", [(8192, 520, 8192, 1, 16, "one"), (8192, 4096, 1032, 2, 64, "blocks"),
+                                   (4096, 2056, 4096, 3, 128, "mixed"), (60, 256, 8192, 4, 12, "mixed"),
+                                   (1, 512, 4096, 2, 16, "one"), (300, 8200, 520, 5, 20, "blocks")],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_bf16_factors_and_gradients(T, shape):
+    Tn, c, b, n, r, order = shape
+    X, W, A, B, index, scale, dY = make(Tn, c, b, n, r, torch.bfloat16, seed=51, order=order)
+    _, V = T.adapter_forward(X, W, A, B, index, scale, check=True)
+    assert rel(V, ref_forward(X, W, A, B, index, scale)[1]) <= TOL
+    _, dA, dB = T.adapter_backward(dY, X, V, W, A, B, index, scale, need_dx=False, check=True)
+    _, rA, rB = ref_backward(dY, X, V, W, A, B, index, scale)
+    assert rel(dA, rA) <= TOL and rel(dB, rB) <= TOL
+
+
+@pytest.mark.parametrize("shape", [(500, 768, 768, 3, 8, "blocks"), (2100, 768, 4096, 3, 8, "mixed"),
+                                   (1024, 4096, 768, 1, 64, "one"), (2100, 1000, 2056, 2, 40, "mixed"),
+                                   (33, 1024, 8192, 2, 16, "mixed"), (1, 4096, 1024, 2, 16, "one")],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_f32(T, shape):
+    Tn, c, b, n, r, order = shape
+    X, W, A, B, index, scale, dY = make(Tn, c, b, n, r, torch.float32, seed=53, order=order)
+    Y, V = T.adapter_forward(X, W, A, B, index, scale, check=True)
+    Yr, Vr = ref_forward(X, W, A, B, index, scale)
+    assert rel(Y, Yr) <= TOL and rel(V, Vr) <= TOL
+    got = T.adapter_backward(dY, X, V, W, A, B, index, scale, check=True)
+    for x, ref in zip(got, ref_backward(dY, X, V, W, A, B, index, scale)):
+        assert rel(x, ref) <= TOL
