@@ -1,6 +1,6 @@
 // See proj_gemm.cuh.  Two kernels share the operand layouts and the epilogues.
 //
-// tile_kernel: one CTA per 128 x nt output tile and slice of k.  A cluster of 1, 2, 4 or 8 CTAs
+// tile_kernel: one CTA per 128 x nt output tile and slice of k.  A cluster of up to eight CTAs
 // splits the k range of a tile when there are fewer tiles than SMs and adds the partial sums over
 // distributed shared memory in rank order (same inputs, same bits).  Roles of its 320 threads:
 //   warp 0      TMA producer: per 64-wide k step the A tile (128 x 64, 128-byte swizzle; K-major, or
@@ -1188,8 +1188,8 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
 // non-finite weight would reach those tokens, so the chunk is scanned, non-finite weights become
 // zeros and the epilogue adds their products to the adapter's own tokens.
 //
-// Bound by the tensor cores and the power cap.  4096 tokens, 4096 x 4096, 7 adapters of rank 32: 118 us
-// with the skinny product, 1.18 PFLOP/s (256 tiles are 3.46 rounds of 74 pairs; 105 us and 68 % of the
+// Bound by the tensor cores and the power cap.  4096 tokens, 4096 x 4096, 7 adapters of rank 32: 117 us
+// with the skinny product, 1.19 PFLOP/s (256 tiles are 3.46 rounds of 74 pairs; 107 us and 69 % of the
 // tensor cycles in this kernel alone, cold).  8192 x 11008 x 4096: 1.3 PFLOP/s of 1.43 sustained.
 constexpr int PTM = 256;
 constexpr int PSTAGE_BYTES = 2 * A_BYTES;
@@ -1750,7 +1750,10 @@ bool use_pairs(int64_t M, int64_t N, int64_t batch, bool symmetric) {
 
 namespace {
 // Width and k slices of tile_kernel's tiles, by the clocks that the busiest SM takes, as measured on
-// 768 x 768 products and on single tokens:
+// 768 x 768 products and on single tokens.  Elsewhere the choice is up to a fifth off the best (16
+// tokens, 2048 x 2048: 12.4 us with 8 slices, 10.3 with 2; 333 tokens, 1001 x 1752: 19.6 and 17.2; 200
+// and 500 tokens: the best).  Clusters of 5 and 7 are no worse than their neighbours here (64 tokens,
+// 4096 x 11008: 5 slices 30.6 us, 7 30.1, 8 30.0).
 //   a k step     what it brings in at 60 bytes per clock, at least 250 (issue and barriers)
 //   a CTA        2000 to start, 400 for eight columns of its epilogue (700 with operands to read)
 //   a cluster    1500, and 44 a column for the partial sums over distributed shared memory, more with
