@@ -37,7 +37,7 @@ constexpr int FACTOR_BYTES = 128 * 16 * 4;    // 16 ranks of up to 128 tokens, f
 
 struct Params {
   int M, N, K, tiles_m, tiles_n, nt, stages, splits, batch_z, ring_bytes, tmem_cols;
-  int symmetric, f16, early, first, fine;
+  int symmetric, f16, early, first, fine, add;
   int32_t* status;
   // adapter part
   void* out;
@@ -280,6 +280,13 @@ __device__ __forceinline__ void emit(const Params& p, int z, int m, int n0, floa
   const int nc = p.N - n0;  // columns that exist
   if constexpr (EPI == PROJ_OUT32) {
     float* out = static_cast<float*>(p.out) + (int64_t)n0 * p.ldo + m;
+    if (p.add) {
+      float old[NC];
+#pragma unroll
+      for (int e = 0; e < NC; ++e) old[e] = out[(int64_t)(e < nc ? e : 0) * p.ldo];
+#pragma unroll
+      for (int e = 0; e < NC; ++e) v[e] += old[e];
+    }
 #pragma unroll
     for (int e = 0; e < NC; ++e)
       if (e < nc) out[(int64_t)e * p.ldo] = v[e];
@@ -1823,6 +1830,7 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
   p.early = a.early;
   p.first = a.first;
   p.fine = a.fine;
+  p.add = a.add;
   p.status = a.status;
   const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * a.batch;
   if (tiles > (1 << 27) || a.batch > 65535) return THANOS_ERR_SHAPE;

@@ -54,3 +54,33 @@ def test_f32(T, shape):
     got = T.adapter_backward(dY, X, V, W, A, B, index, scale, check=True)
     for x, ref in zip(got, ref_backward(dY, X, V, W, A, B, index, scale)):
         assert rel(x, ref) <= TOL
+
+
+@pytest.mark.parametrize("shape", [(100, 256, 16384), (33, 200, 65536), (700, 300, 24584), (5, 129, 8200)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_f32_long_sums(T, shape):
+    """As many inputs as the projection takes, and as many outputs for the backward sums; on positive
+    numbers, where every cut goes the same way, 64 additions of full size cut 64 2^-24 = 3.9e-6."""
+    Tn, c, b = shape
+    X, W, A, B, index, scale, dY = make(Tn, c, b, 2, 12, torch.float32, seed=57)
+    Y, V = T.adapter_forward(X, W, A, B, index, scale, check=True)
+    Yr, Vr = ref_forward(X, W, A, B, index, scale)
+    assert rel(Y, Yr) <= TOL and rel(V, Vr) <= TOL
+    P, Q = X.abs(), W.abs()
+    assert rel(T.adapter_forward(P, Q, check=True)[0], P.double() @ Q.double().T) <= 2 * TOL
+    # the same matrices the other way round: c is the long side
+    Wt, dY2 = W.t().contiguous(), X
+    At = torch.randn(2, 12, Wt.shape[1] // 8 * 8, device="cuda") / 16
+    Wt = Wt[:, :At.shape[2]].contiguous()
+    Bt = 0.1 * torch.randn(2, Wt.shape[0], 12, device="cuda")
+    dX, _, _ = T.adapter_backward(dY2, None, None, Wt, At, Bt, index, scale, need_grads=False, check=True)
+    zero = torch.zeros(Tn, At.shape[2], device="cuda")
+    assert rel(dX, ref_backward(dY2, zero, torch.zeros(Tn, 12, device="cuda"), Wt, At, Bt, index, scale)[0]) <= TOL
+
+
+def test_f32_longest_backward_sum(T):
+    gen = torch.Generator(device="cuda").manual_seed(59)
+    dY = torch.randn(40, 1 << 20, generator=gen, device="cuda")
+    W = torch.randn(1 << 20, 72, generator=gen, device="cuda")
+    dX, _, _ = T.adapter_backward(dY, None, None, W, need_grads=False, check=True)
+    assert rel(dX, dY.double() @ W.double()) <= TOL
