@@ -252,7 +252,9 @@ __global__ void __launch_bounds__(256) grad_f32_kernel(const Grad32Params p) {
   const int j0 = blockIdx.z * RANKS, nj = min(RANKS, p.r - j0);
   for (int64_t i = blockIdx.y; i < p.n; i += gridDim.y) {
     const int lo = p.off[i], hi = p.off[i + 1];
-    float s[RANKS] = {};
+    // sums of a round, and of rounds: with many tokens one chain of additions would round away more
+    // than it may (2^24 tokens: 3.5e-5 of the result)
+    float s[RANKS] = {}, total[RANKS] = {};
     for (int q0 = lo; q0 < hi; q0 += GRAD_TOKENS) {
       // the tokens of this round and their factors once through shared memory
       const int nq = min(GRAD_TOKENS, hi - q0);
@@ -272,9 +274,14 @@ __global__ void __launch_bounds__(256) grad_f32_kernel(const Grad32Params p) {
           for (int j = 0; j < RANKS; ++j) s[j] = fmaf(fac[q * RANKS + j], z, s[j]);
         }
       }
+#pragma unroll
+      for (int j = 0; j < RANKS; ++j) {
+        total[j] += s[j];
+        s[j] = 0.f;
+      }
     }
 #pragma unroll
-    for (int j = 0; j < RANKS; ++j) red[g][j][threadIdx.x & 31] = s[j];
+    for (int j = 0; j < RANKS; ++j) red[g][j][threadIdx.x & 31] = total[j];
     __syncthreads();
     // thread (g, lane) adds rank g of its feature over the eight groups, in their order
     if (g < nj && f < sd.F) {

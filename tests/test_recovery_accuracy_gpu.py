@@ -84,3 +84,22 @@ def test_f32_longest_backward_sum(T):
     W = torch.randn(1 << 20, 72, generator=gen, device="cuda")
     dX, _, _ = T.adapter_backward(dY, None, None, W, need_grads=False, check=True)
     assert rel(dX, dY.double() @ W.double()) <= TOL
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("positive", [False, True], ids=["signs", "positive"])
+def test_gradients_over_many_tokens(T, dtype, positive):
+    """2^22 tokens of one adapter: chains of at most 64 and then 2^22 / 512 additions, which round 2^-24
+    each, in random directions: 2^-24 (64^0.5 + 8192^0.5) = 5.9e-6 (in one chain of positive terms
+    roundings of one direction add up: 8e-5)."""
+    Tn, c, b, r = 1 << 22, 24, 16, 9
+    gen = torch.Generator(device="cuda").manual_seed(61)
+    rn = lambda *s: torch.randn(s, generator=gen, device="cuda")  # noqa: E731
+    data = [rn(Tn, b).to(dtype), rn(Tn, c).to(dtype), rn(Tn, r), rn(1, r, b).to(dtype), rn(1, c, r).to(dtype)]
+    X, dY, V, A, B = (d.abs() for d in data) if positive else data
+    W = torch.zeros(c, b, dtype=dtype, device="cuda")
+    index, scale = torch.zeros(Tn, dtype=torch.int32, device="cuda"), torch.ones(1, device="cuda")
+    _, dA, dB = T.adapter_backward(dY, X, V, W, A, B, index, scale, need_dx=False, check=True)
+    D = torch.float64
+    assert rel(dB[0], dY.to(D).T @ V.to(D)) <= 5.9e-6
+    assert rel(dA[0], (dY.to(D) @ B[0].to(D)).T @ X.to(D)) <= 5.9e-6
