@@ -413,7 +413,8 @@ size_t thanos_adapter_workspace_bytes(int32_t backward, int64_t n_tok, int64_t c
  *  coef     HOST float[3]: a, b, c.  Finite; they have to keep the iteration bounded: operands of
  *           the products are held in fp16, scaled for singular values up to about 2.
  *           (thanos_orthogonal_step on fp32 weights holds them as two fp16 planes, 22 bits; a
- *           shorter side of up to 64, or 32 with fp32 weights, is computed in fp32.)
+ *           shorter side of up to 64 is computed in fp32, one of up to 32 with fp32 weights in fp32
+ *           with the Gram matrix in fp64.)
  *  1 <= steps <= 32, eps >= 0; 0 <= batch <= 65535 (0 is a no-op: the matrices may be NULL and the
  *  status word is not written), 1 <= m, n <= 65536.
  *  A zero matrix gives zeros (eps > 0); a matrix with an infinity or NaN gives NaN.  Squares may

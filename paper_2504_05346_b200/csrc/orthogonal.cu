@@ -14,6 +14,8 @@
 // 1e-5 of the update, below the rounding of the weights themselves.  It costs three times the tensor
 // work and twice the operand traffic: 768 x 768 in 168 us instead of 107, 4096 x 4096 in 3.4 ms
 // instead of 1.34.
+#include <type_traits>
+
 #include "proj_gemm.cuh"
 #include "recovery.cuh"
 
@@ -282,13 +284,14 @@ __global__ void __launch_bounds__(256) split_kernel(const StepParams p) {
 
 // ------------------------------------------------------------------ a short side of up to 64
 // X_k = Q_k X_0 with Q_k a polynomial in S_0 = X_0 X_0^T, so the matrix is read twice and all steps
-// run on s x s matrices: Q' = P Q, S' = P S P with P = a I + b S + c S S.  In fp32 throughout (a
-// rounding of S_0 is amplified by a^2 per step; 16-bit operands would not do here).  The s x s
+// run on s x s matrices: Q' = P Q, S' = P S P with P = a I + b S + c S S.  In fp32 (a rounding of S_0
+// is amplified by a^2 per step; 16-bit operands would not do here).  The s x s
 // products are a chain on one CTA: 64 x 64 takes 60 us alone, of which the wide products take twice
-// the time whatever the size (4096 x 64: 94 against 123 us, 3 x 7697 x 40: 70 against 178), but a side
-// of 128 would take eight times as much.  What S_0 loses of directions 20 times weaker than the
-// strongest is 5e-4 of the result, which bf16 does not show: fp32 weights with a side above 32 go by
-// the wide products and two planes (4e-5).
+// the time whatever the size (4096 x 64: 90 against 123 us, 3 x 7697 x 40: 70 against 178), but a side
+// of 128 would take eight times as much.  What fp32 loses of directions 20 times weaker than the
+// strongest is 5e-4 of the result, which bf16 does not show.  For fp32 weights the Gram matrix and its
+// powers are fp64 (below 6e-5; 32 steps of 16 x 4096: 37 us instead of 33), and a side above 32 goes by
+// the wide products and two planes (2 to 6e-5).
 //   gram_kernel   new momentum, partial Gram matrices over chunks of the long side
 //   steps_kernel  one CTA per matrix: sums the partials in order, iterates, Q / (norm + eps)
 //   apply_kernel  Q X_0 over chunks of the long side, into O or the new weights
@@ -302,9 +305,19 @@ __host__ __device__ constexpr int small_size(int ts) {  // and a row of zeros
 }
 constexpr int STAGE_FLOATS = 10240;  // a tile of the long side, padded rows: 512 columns of 16 rows
 
+template <typename Real, int N>
+struct alignas(sizeof(Real) * N < 16 ? sizeof(Real) * N : 16) Vec {
+  Real v[N];
+};
+template <typename Real>
+__device__ __forceinline__ void add4(Vec<Real, 4>& a, const Vec<Real, 4>& b) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) a.v[i] += b.v[i];
+}
+
 struct SmallParams {
   StepParams u;
-  float* part;       // [batch][chunks][4 x 4 tiles of the Gram matrix]
+  void* part;        // [batch][chunks][4 x 4 tiles of the Gram matrix], fp32, fp64 for fp32 weights
   float* Q;          // [batch][s][s]
   int s, l, chunks, chunk_cols, tile_cols, steps;
   uint32_t inv_q;    // ceil(2^32 / q) for q = ceil(s / 4) > 1: e / q is the high word of e inv_q
@@ -353,8 +366,11 @@ __device__ __forceinline__ void stage_columns(const SmallParams& p, int64_t base
   }
 }
 
-template <int VEC>
+// FINE (fp32 weights): a thread's products are added in fp64, sixteen at a time.
+template <int VEC, bool FINE>
 __global__ void __launch_bounds__(256) gram_kernel(const SmallParams p) {
+  using Real = std::conditional_t<FINE, double, float>;
+  constexpr int RUN = 16;
   extern __shared__ __align__(16) float Xs[];
   grid_dependents_launch();
   if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.u.status = 0;
@@ -363,46 +379,55 @@ __global__ void __launch_bounds__(256) gram_kernel(const SmallParams p) {
   const int g = threadIdx.x / tiles, tile = threadIdx.x - g * tiles;
   const int ti = tile / q, tj = tile - ti * q;
   const int c_lo = blockIdx.x * p.chunk_cols, c_hi = min(p.l, c_lo + p.chunk_cols);
-  float acc[4][4] = {};
+  Real acc[4][4] = {};
+  // acc += the products of columns c, c + groups, .. below `end`
+  auto columns = [&](int c, int end, auto& sums) {
+#pragma unroll 4
+    for (; c < end; c += groups) {
+      const float4 x = *reinterpret_cast<const float4*>(Xs + c * ld + 4 * ti);
+      const float4 y = *reinterpret_cast<const float4*>(Xs + c * ld + 4 * tj);
+      const float xv[4] = {x.x, x.y, x.z, x.w}, yv[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sums[i][j] = fmaf(xv[i], yv[j], sums[i][j]);
+    }
+  };
   for (int c0 = c_lo; c0 < c_hi; c0 += p.tile_cols) {
     const int cols = min(p.tile_cols, c_hi - c0);
     __syncthreads();
     stage_columns<VEC, true>(p, base, c0, cols, Xs, ld);
     __syncthreads();
     if (g < groups) {
-#pragma unroll 4
-      for (int c = g; c < cols; c += groups) {
-        const float4 x = *reinterpret_cast<const float4*>(Xs + c * ld + 4 * ti);
-        const float4 y = *reinterpret_cast<const float4*>(Xs + c * ld + 4 * tj);
-        const float xv[4] = {x.x, x.y, x.z, x.w}, yv[4] = {y.x, y.y, y.z, y.w};
+      if constexpr (FINE) {
+        for (int c = g; c < cols; c += RUN * groups) {
+          float run[4][4] = {};
+          columns(c, min(cols, c + RUN * groups), run);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+          for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(xv[i], yv[j], acc[i][j]);
+            for (int j = 0; j < 4; ++j) acc[i][j] += (double)run[i][j];
+        }
+      } else {
+        columns(g, cols, acc);
       }
     }
   }
   // the groups' sums, in order of the group
   __syncthreads();
+  using Four = Vec<Real, 4>;
+  Four* sums = reinterpret_cast<Four*>(Xs);
   if (g < groups) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      *reinterpret_cast<float4*>(Xs + (g * tiles + tile) * 16 + 4 * i) =
-          make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+      sums[(g * tiles + tile) * 4 + i] = Four{acc[i][0], acc[i][1], acc[i][2], acc[i][3]};
   }
   __syncthreads();
-  float4* out = reinterpret_cast<float4*>(
-      p.part + ((int64_t)blockIdx.y * p.chunks + blockIdx.x) * (tiles * 16));
+  Four* out = static_cast<Four*>(p.part) + ((int64_t)blockIdx.y * p.chunks + blockIdx.x) * (tiles * 4);
   for (int e = threadIdx.x; e < tiles * 4; e += 256) {
-    float4 v = reinterpret_cast<const float4*>(Xs)[e];
+    Four v = sums[e];
 #pragma unroll 4
-    for (int k = 1; k < groups; ++k) {
-      const float4 w = reinterpret_cast<const float4*>(Xs)[k * tiles * 4 + e];
-      v.x += w.x;
-      v.y += w.y;
-      v.z += w.z;
-      v.w += w.w;
-    }
+    for (int k = 1; k < groups; ++k) add4(v, sums[k * tiles * 4 + e]);
     out[e] = v;
   }
 }
@@ -412,48 +437,28 @@ __global__ void __launch_bounds__(256) gram_kernel(const SmallParams p) {
 // left of a rounding in them grows by a = 3.4 per step on one side only, so a transpose of Q in its
 // place is wrong by 1e-2 and more on matrices of low rank.  TS x TS outputs a thread; one copy of the
 // code for all the products of a step, which run one after another on one CTA.
-template <int TS>
-__device__ __noinline__ void small_product(int D_at, int A_at, int B_at, int s, bool add, float a,
-                                           float b, float c) {
-  extern __shared__ __align__(16) float mats[];
+template <int TS, typename Real>
+__device__ __noinline__ void small_product(int D_at, int A_at, int B_at, int s, bool add, Real a, Real b,
+                                           Real c) {
+  extern __shared__ __align__(16) unsigned char small_smem[];
+  Real* mats = reinterpret_cast<Real*>(small_smem);
   constexpr int LD = small_ld(TS);
   const int q = (s + TS - 1) / TS;
   const int ti = threadIdx.x >> 4, tj = threadIdx.x & 15;  // 16 x 16 threads
   if (ti < q && tj < q) {
-    const float* x = mats + A_at + TS * ti;
-    const float* y = mats + B_at + TS * tj;
-    float acc[2][TS][TS] = {};   // even and odd k apart: half the chain of dependent additions
+    const Real* x = mats + A_at + TS * ti;
+    const Real* y = mats + B_at + TS * tj;
+    Real acc[2][TS][TS] = {};   // even and odd k apart: half the chain of dependent additions
 #pragma unroll 4
     for (int k = 0; k < s; k += 2) {   // row s is zero
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        float xv[TS], yv[TS];
-        if constexpr (TS == 4) {
-          const float4 xx = *reinterpret_cast<const float4*>(x + (k + h) * LD);
-          const float4 yy = *reinterpret_cast<const float4*>(y + (k + h) * LD);
-          xv[0] = xx.x;
-          xv[1] = xx.y;
-          xv[2] = xx.z;
-          xv[3] = xx.w;
-          yv[0] = yy.x;
-          yv[1] = yy.y;
-          yv[2] = yy.z;
-          yv[3] = yy.w;
-        } else if constexpr (TS == 2) {
-          const float2 xx = *reinterpret_cast<const float2*>(x + (k + h) * LD);
-          const float2 yy = *reinterpret_cast<const float2*>(y + (k + h) * LD);
-          xv[0] = xx.x;
-          xv[1] = xx.y;
-          yv[0] = yy.x;
-          yv[1] = yy.y;
-        } else {
-          xv[0] = x[(k + h) * LD];
-          yv[0] = y[(k + h) * LD];
-        }
+        const Vec<Real, TS> xv = *reinterpret_cast<const Vec<Real, TS>*>(x + (k + h) * LD);
+        const Vec<Real, TS> yv = *reinterpret_cast<const Vec<Real, TS>*>(y + (k + h) * LD);
 #pragma unroll
         for (int i = 0; i < TS; ++i)
 #pragma unroll
-          for (int j = 0; j < TS; ++j) acc[h][i][j] = fmaf(xv[i], yv[j], acc[h][i][j]);
+          for (int j = 0; j < TS; ++j) acc[h][i][j] = fma(xv.v[i], yv.v[j], acc[h][i][j]);
       }
     }
 #pragma unroll
@@ -461,8 +466,8 @@ __device__ __noinline__ void small_product(int D_at, int A_at, int B_at, int s, 
 #pragma unroll
       for (int j = 0; j < TS; ++j) {
         const int r = TS * ti + i, cc = TS * tj + j;
-        float v = acc[0][i][j] + acc[1][i][j];
-        if (add) v = fmaf(c, v, fmaf(b, mats[A_at + r * LD + cc], r == cc ? a : 0.f));
+        Real v = acc[0][i][j] + acc[1][i][j];
+        if (add) v = fma(c, v, fma(b, mats[A_at + r * LD + cc], r == cc ? a : (Real)0));
         if (r < s && cc < s) mats[D_at + r * LD + cc] = v;
       }
   }
@@ -471,16 +476,11 @@ __device__ __noinline__ void small_product(int D_at, int A_at, int B_at, int s, 
 
 constexpr int STEP_THREADS = 256;
 
-__device__ __forceinline__ void add4(float4& a, const float4& b) {
-  a.x += b.x;
-  a.y += b.y;
-  a.z += b.z;
-  a.w += b.w;
-}
 // Every hop-th of the chunks' partial matrices from the first-th on.
-__device__ __forceinline__ float4 sum_parts(const float4* part, int first, int hop, int chunks,
-                                            int vecs) {
-  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+template <typename Real>
+__device__ __forceinline__ Vec<Real, 4> sum_parts(const Vec<Real, 4>* part, int first, int hop,
+                                                  int chunks, int vecs) {
+  Vec<Real, 4> sum = {};
 #pragma unroll 8
   for (int k = first; k < chunks; k += hop) add4(sum, part[(int64_t)k * vecs]);
   return sum;
@@ -490,12 +490,13 @@ __device__ __forceinline__ float4 sum_parts(const float4* part, int first, int h
 // the power of two that brings its largest value to between one and two.  Returns that exponent (the
 // product is 2^(-2 e) of what it stands for); with infinities or NaN everything stays as it is.
 // The matrices behind the first are used for staging and left zero.
-template <int TS>
+template <int TS, typename Real>
 __device__ __noinline__ int gram_again(const SmallParams& p) {
-  extern __shared__ __align__(16) float mats[];
+  extern __shared__ __align__(16) unsigned char small_smem[];
+  Real* mats = reinterpret_cast<Real*>(small_smem);
   __shared__ uint32_t tops[STEP_THREADS / 32];
   constexpr int LD = small_ld(TS), SZ = small_size(TS);
-  float* Xs = mats + SZ;
+  float* Xs = reinterpret_cast<float*>(mats + SZ);
   const int64_t base = (int64_t)blockIdx.x * p.s * p.l;
   const int q = (p.s + 3) / 4, ld = 4 * q + 4, ti = threadIdx.x / q, tj = threadIdx.x - ti * q;
   uint32_t top = 0;  // largest magnitude, as bits
@@ -515,7 +516,7 @@ __device__ __noinline__ int gram_again(const SmallParams& p) {
   if (top > 0 && top < 0x7F800000u) {
     e = max((int)(top >> 23) - 127, -120);
     const float scale = ldexpf(1.f, -e);
-    float acc[4][4] = {};
+    Real acc[4][4] = {};
     for (int c0 = 0; c0 < p.l; c0 += p.tile_cols) {
       const int cols = min(p.tile_cols, p.l - c0);
       __syncthreads();
@@ -527,7 +528,8 @@ __device__ __noinline__ int gram_again(const SmallParams& p) {
         for (int i = 0; i < 4; ++i)
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            acc[i][j] = fmaf(scale * Xs[c * ld + 4 * ti + i], scale * Xs[c * ld + 4 * tj + j], acc[i][j]);
+            acc[i][j] = fma((Real)(scale * Xs[c * ld + 4 * ti + i]),
+                            (Real)(scale * Xs[c * ld + 4 * tj + j]), acc[i][j]);
       }
     }
     if (ti < q) {
@@ -538,52 +540,54 @@ __device__ __noinline__ int gram_again(const SmallParams& p) {
     }
   }
   __syncthreads();
-  for (int k = SZ + threadIdx.x; k < 5 * SZ; k += STEP_THREADS) mats[k] = 0.f;
+  for (int k = SZ + threadIdx.x; k < 5 * SZ; k += STEP_THREADS) mats[k] = (Real)0;
   __syncthreads();
   return e;
 }
 
-template <int TS>
+template <int TS, typename Real>
 __global__ void __launch_bounds__(STEP_THREADS) steps_kernel(const SmallParams p) {
-  extern __shared__ __align__(16) float mats[];
+  extern __shared__ __align__(16) unsigned char small_smem[];
+  Real* mats = reinterpret_cast<Real*>(small_smem);
+  using Four = Vec<Real, 4>;
   // S, P, Q, T, U: a row more than they need, which stays zero
   constexpr int LD = small_ld(TS), SZ = small_size(TS);
-  float *S = mats, *T = mats + 3 * SZ;
+  Real *S = mats, *T = mats + 3 * SZ;
   int Q = 2 * SZ, U = 4 * SZ;
-  __shared__ float square;
+  __shared__ Real square;
   const int s = p.s, ss = s * s;
-  for (int e = threadIdx.x; e < 5 * SZ; e += STEP_THREADS) mats[e] = 0.f;
+  for (int e = threadIdx.x; e < 5 * SZ; e += STEP_THREADS) mats[e] = (Real)0;
   __syncthreads();
   grid_dependency_wait();
   grid_dependents_launch();
   // the partial matrices, four entries a thread; threads to spare take every groups-th of them
   const int q = (s + 3) / 4, vecs = q * q * 4;
-  const float4* part = reinterpret_cast<const float4*>(p.part) + (int64_t)blockIdx.x * p.chunks * vecs;
+  const Four* part = static_cast<const Four*>(p.part) + (int64_t)blockIdx.x * p.chunks * vecs;
   if constexpr (TS <= 2) {
     const int groups = STEP_THREADS / vecs;
     const int g = threadIdx.x / vecs, e = threadIdx.x - g * vecs;
-    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    Four sum = {};
     if (g < groups) {
       sum = sum_parts(part + e, g, groups, p.chunks, vecs);
-      reinterpret_cast<float4*>(T)[threadIdx.x] = sum;  // T holds 297 of them
+      reinterpret_cast<Four*>(T)[threadIdx.x] = sum;  // T holds 297 of them
     }
     __syncthreads();
     if (threadIdx.x < vecs) {
-      for (int k = 1; k < groups; ++k) add4(sum, reinterpret_cast<const float4*>(T)[k * vecs + e]);
+      for (int k = 1; k < groups; ++k) add4(sum, reinterpret_cast<const Four*>(T)[k * vecs + e]);
       const int tl = e >> 2, tr = tl / q;
-      *reinterpret_cast<float4*>(S + (4 * tr + (e & 3)) * LD + 4 * (tl - tr * q)) = sum;
+      *reinterpret_cast<Four*>(S + (4 * tr + (e & 3)) * LD + 4 * (tl - tr * q)) = sum;
     }
   } else {
     for (int e = threadIdx.x; e < vecs; e += STEP_THREADS) {
       const int tl = e >> 2, tr = tl / q;
-      *reinterpret_cast<float4*>(S + (4 * tr + (e & 3)) * LD + 4 * (tl - tr * q)) =
+      *reinterpret_cast<Four*>(S + (4 * tr + (e & 3)) * LD + 4 * (tl - tr * q)) =
           sum_parts(part + e, 0, 1, p.chunks, vecs);
     }
   }
   __syncthreads();
   auto trace = [&]() {
     if (threadIdx.x < 32) {
-      float t = 0.f;
+      Real t = 0;
       for (int i = threadIdx.x; i < s; i += 32) t += S[i * LD + i];
       for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
       if (threadIdx.x == 0) square = t;
@@ -592,41 +596,41 @@ __global__ void __launch_bounds__(STEP_THREADS) steps_kernel(const SmallParams p
   };
   trace();
   int exponent = 0;
-  float eps = p.u.eps;
-  if (squares_out_of_range(square, eps)) {
-    exponent = gram_again<TS>(p);
-    eps = ldexpf(eps, -exponent);
+  Real eps = p.u.eps;
+  if (squares_out_of_range((float)square, p.u.eps)) {
+    exponent = gram_again<TS, Real>(p);
+    eps = ldexpf(p.u.eps, -exponent);
     trace();
   }
-  const float inv = 1.f / (sqrtf(square) + eps);
+  const Real inv = (Real)1 / (sqrt(square) + eps);
   for (int i = threadIdx.x; i < s * LD; i += STEP_THREADS) S[i] = S[i] * inv * inv;
   __syncthreads();
   // T held partial sums: its row s has to be zero again
-  for (int i = threadIdx.x; i < SZ; i += STEP_THREADS) T[i] = 0.f;
+  for (int i = threadIdx.x; i < SZ; i += STEP_THREADS) T[i] = (Real)0;
   __syncthreads();
 #pragma unroll 1
   for (int it = 0; it < p.steps; ++it) {
     const int P = it == 0 ? Q : SZ;                         // Q_1 = P_0
-    small_product<TS>(P, 0, 0, s, true, p.a, p.b, p.c);
+    small_product<TS, Real>(P, 0, 0, s, true, p.a, p.b, p.c);
     if (it > 0) {
-      small_product<TS>(U, P, Q, s, false, 0.f, 0.f, 0.f);
+      small_product<TS, Real>(U, P, Q, s, false, 0.f, 0.f, 0.f);
       const int t = Q;
       Q = U;
       U = t;
     }
     if (it + 1 < p.steps) {
-      small_product<TS>(3 * SZ, 0, P, s, false, 0.f, 0.f, 0.f);       // S P
-      small_product<TS>(0, 3 * SZ, P, s, false, 0.f, 0.f, 0.f);       // (S P)^T P = P S P
+      small_product<TS, Real>(3 * SZ, 0, P, s, false, 0.f, 0.f, 0.f);       // S P
+      small_product<TS, Real>(0, 3 * SZ, P, s, false, 0.f, 0.f, 0.f);       // (S P)^T P = P S P
     }
   }
   float* out = p.Q + (int64_t)blockIdx.x * ss;
-  const float inv_out = exponent == 0 ? inv : ldexpf(inv, -exponent);
+  const float inv_out = exponent == 0 ? (float)inv : ldexpf((float)inv, -exponent);
   for (int r = threadIdx.x >> 5; r < s; r += STEP_THREADS / 32)
     if constexpr (TS <= 2) {
       if ((threadIdx.x & 31) < s)
-        out[r * s + (threadIdx.x & 31)] = mats[Q + r * LD + (threadIdx.x & 31)] * inv_out;
+        out[r * s + (threadIdx.x & 31)] = (float)mats[Q + r * LD + (threadIdx.x & 31)] * inv_out;
     } else {
-      for (int c = threadIdx.x & 31; c < s; c += 32) out[r * s + c] = mats[Q + r * LD + c] * inv_out;
+      for (int c = threadIdx.x & 31; c < s; c += 32) out[r * s + c] = (float)mats[Q + r * LD + c] * inv_out;
     }
 }
 
@@ -768,7 +772,7 @@ thanos_status_t launch_apply(const SmallParams& p, dim3 grid, cudaStream_t strea
   return launch_after(apply_kernel<VEC, TS>, grid, 256, smem, p, stream);
 }
 
-thanos_status_t small_side(const OrthogonalArgs& a, StepParams u, int s, int l, float* part,
+thanos_status_t small_side(const OrthogonalArgs& a, StepParams u, int s, int l, bool fine, void* part,
                            float* Q, int chunks, cudaStream_t stream) {
   SmallParams p = {};
   p.u = u;
@@ -797,19 +801,27 @@ thanos_status_t small_side(const OrthogonalArgs& a, StepParams u, int s, int l, 
   const size_t stage = STAGE_FLOATS * 4, squares = 116 * 1024;
   static_assert(5 * small_size(4) * 4 <= 116 * 1024, "five matrices");
   const dim3 chunks_grid((unsigned)p.chunks, (unsigned)a.batch), one((unsigned)a.batch);
-  if (wide) gram_kernel<4><<<chunks_grid, 256, stage, stream>>>(p);
-  else gram_kernel<1><<<chunks_grid, 256, stage, stream>>>(p);
-  THANOS_CHECK_LAUNCH();
-  static std::atomic<unsigned long long> done1{0}, done2{0}, done4{0};
-  if (s <= 16) {  // one entry of a product a thread, four or sixteen
-    THANOS_CUDA(ensure_max_dyn_smem(steps_kernel<1>, (int)squares, done1));
-    THANOS_TRY(launch_after(steps_kernel<1>, one, STEP_THREADS, squares, p, stream));
-  } else if (s <= 32) {
-    THANOS_CUDA(ensure_max_dyn_smem(steps_kernel<2>, (int)squares, done2));
-    THANOS_TRY(launch_after(steps_kernel<2>, one, STEP_THREADS, squares, p, stream));
+  if (fine) {
+    if (wide) gram_kernel<4, true><<<chunks_grid, 256, stage, stream>>>(p);
+    else gram_kernel<1, true><<<chunks_grid, 256, stage, stream>>>(p);
   } else {
-    THANOS_CUDA(ensure_max_dyn_smem(steps_kernel<4>, (int)squares, done4));
-    THANOS_TRY(launch_after(steps_kernel<4>, one, STEP_THREADS, squares, p, stream));
+    if (wide) gram_kernel<4, false><<<chunks_grid, 256, stage, stream>>>(p);
+    else gram_kernel<1, false><<<chunks_grid, 256, stage, stream>>>(p);
+  }
+  THANOS_CHECK_LAUNCH();
+  static_assert(5 * small_size(2) * 8 <= 116 * 1024, "five matrices in fp64");
+  static std::atomic<unsigned long long> done1{0}, done2{0}, done4{0}, fine1{0}, fine2{0};
+  const auto steps = [&](auto kernel, std::atomic<unsigned long long>& done) -> thanos_status_t {
+    THANOS_CUDA(ensure_max_dyn_smem(kernel, (int)squares, done));
+    return launch_after(kernel, one, STEP_THREADS, squares, p, stream);
+  };
+  // one entry of a product a thread, four or sixteen
+  if (s <= 16) {
+    THANOS_TRY(fine ? steps(steps_kernel<1, double>, fine1) : steps(steps_kernel<1, float>, done1));
+  } else if (s <= 32) {
+    THANOS_TRY(fine ? steps(steps_kernel<2, double>, fine2) : steps(steps_kernel<2, float>, done2));
+  } else {
+    THANOS_TRY(steps(steps_kernel<4, float>, done4));
   }
   // tiles of the apply pass: enough for the device, four to a thread at least
   int tile = p.tile_cols;
@@ -840,7 +852,8 @@ size_t orthogonal_workspace_bytes(int64_t batch, int64_t m, int64_t n) {
   size_t small = 0, wide = 0;
   if (s <= SMALL_SIDE)
     small = 256 +
-            round_up(k * small_chunks(batch > 0 ? batch : 1, s, l) * round_up(s, 4) * round_up(s, 4) * 4,
+            round_up(k * small_chunks(batch > 0 ? batch : 1, s, l) * round_up(s, 4) * round_up(s, 4) *
+                         (s <= SMALL_SIDE_FINE ? 8 : 4),
                      256) +
             round_up(k * s * s * 4, 256);
   if (s > SMALL_SIDE_FINE)
@@ -874,10 +887,10 @@ thanos_status_t orthogonal_impl(const OrthogonalArgs& a, void* workspace, size_t
   if (s <= (fine ? SMALL_SIDE_FINE : SMALL_SIDE)) {
     const int chunks = small_chunks(a.batch, s, l);
     const size_t s4 = round_up((size_t)s, 4);
-    float* parts = ar.take<float>(k * chunks * s4 * s4);
+    char* parts = ar.take<char>(k * chunks * s4 * s4 * (fine ? 8 : 4));
     float* Q = ar.take<float>(k * s * s);
     if (!ar.ok()) return THANOS_ERR_WORKSPACE;
-    return small_side(a, sp, s, l, parts, Q, chunks, stream);
+    return small_side(a, sp, s, l, fine, parts, Q, chunks, stream);
   }
   double* part = ar.take<double>(k * MAX_PARTS);
   __half* X[2][2];

@@ -103,3 +103,37 @@ def test_gradients_over_many_tokens(T, dtype, positive):
     D = torch.float64
     assert rel(dB[0], dY.to(D).T @ V.to(D)) <= 5.9e-6
     assert rel(dA[0], (dY.to(D) @ B[0].to(D)).T @ X.to(D)) <= 5.9e-6
+
+
+def spectrum(kind, k, m, n, gen):
+    rn = lambda *s: torch.randn(s, generator=gen, device="cuda")  # noqa: E731
+    q = max(1, min(m, n) // 16)
+    if kind == "flat":
+        return rn(k, m, n)
+    lead = rn(k, m, q) @ rn(k, q, n)
+    return lead if kind == "low rank" else lead + 0.05 * rn(k, m, n)
+
+
+@pytest.mark.parametrize("kind", ["flat", "lead", "low rank"])
+@pytest.mark.parametrize("shape", [(1, 16, 65536), (1, 32, 65536), (32, 16, 4096), (3, 11008, 24), (5, 7, 100),
+                                   (1, 17, 4099), (2, 1000, 31), (1, 1, 9)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_fp32_step_on_short_sides(T, shape, kind):
+    """Where the iteration runs on the Gram matrix and the weights are fp32, that matrix and its powers
+    are fp64; what is left is the rounding of X and of the factor that is applied to it, 2^-24 of terms
+    up to 3.4445^5 = 485 times the result, 2.9e-5, and as much again for their fp32 sums."""
+    gen = torch.Generator(device="cuda").manual_seed(67)
+    G = spectrum(kind, *shape, gen)
+    Z = torch.zeros_like(G)
+    W, _ = T.orthogonal_step(Z, Z, G, lr=1.0, momentum=0.0, check=True)
+    X = G.double()
+    tall = shape[1] > shape[2]
+    X = X.mT if tall else X
+    X = X / (torch.linalg.matrix_norm(X, keepdim=True) + 1e-7)
+    a, b, c = T.NEWTON_SCHULZ
+    for _ in range(5):
+        S = X @ X.mT
+        X = a * X + (b * S + c * (S @ S)) @ X
+    X = X.mT if tall else X
+    for i in range(shape[0]):
+        assert rel(-W[i], X[i]) <= 5.8e-5
