@@ -353,12 +353,24 @@ __device__ __forceinline__ void emit(const Params& p, int z, int m, int n0, floa
     } else {
 #pragma unroll
       for (int e = 0; e < NC; ++e) v[e] *= p.alpha;
+      if (p.add) {  // to both planes of what is there
+#pragma unroll 1
+        for (int pl = 0; pl < 2; ++pl) {
+          const __half* S = D + (int64_t)(pl * p.batch_z) * p.s_batch + (int64_t)n0 * p.lds + m;
+          __half old[NC];
+#pragma unroll
+          for (int e = 0; e < NC; ++e) old[e] = S[(int64_t)(e < nc ? e : 0) * p.lds];
+#pragma unroll
+          for (int e = 0; e < NC; ++e) v[e] += __half2float(old[e]);
+        }
+      }
     }
     if (p.s_diag && m >= n0 && m < n0 + NC) {
       float* diag = EPI == PROJ_GRAM ? p.s_diag : p.p_diag;
 #pragma unroll
       for (int e = 0; e < NC; ++e)
         if (n0 + e == m) {
+          if (EPI == PROJ_GRAM && p.add) v[e] += diag[(int64_t)z * p.lds + m];
           diag[(int64_t)z * p.lds + m] = v[e];
           v[e] = 0.f;
         }
@@ -1804,6 +1816,12 @@ TileShape tile_shape(int64_t M, int64_t N, int64_t batch, int64_t blocks, int lo
 }
 }  // namespace
 
+// Terms that an entry of S sums in one accumulator for fp32 weights; a longer k goes in pieces, each
+// added to what is there.  The tensor cores cut what they add, of the squares on the diagonal always in
+// one direction (2048 x 20000, 65536: 1.8e-4, 2.3e-4 of the update, 4096 x 65536: 3.8e-4; in pieces of 4096
+// 2e-5, but 4096 x 11008, 4.5e-5 in one, then took 9.1 ms instead of 7.3).
+constexpr int64_t LONGEST_GRAM = 16384;
+
 int proj_pair_tile(int64_t N, int64_t M) { return use_pairs(M, N, 1, false) ? PTM : 0; }
 
 thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
@@ -1820,6 +1838,19 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
   const TileShape shape =
       pairs ? TileShape{PTM, 1} : tile_shape(a.M, a.N, a.batch, ceil_div(a.K, BK), f32 ? 6 : a.fine ? 2 : 1,
                                                  symmetric, a.epi);
+  if (a.epi == PROJ_GRAM && a.fine && ceil_div(a.K, shape.splits) > LONGEST_GRAM) {
+    const int64_t pieces = ceil_div(ceil_div(a.K, shape.splits), LONGEST_GRAM), blocks = ceil_div(a.K, BK);
+    for (int64_t i = 0; i < pieces; ++i) {
+      const int64_t k0 = BK * (blocks * i / pieces), k1 = BK * (blocks * (i + 1) / pieces);
+      ProjArgs s = a;
+      s.A = static_cast<const __half*>(a.A) + k0;
+      s.B = static_cast<const __half*>(a.B) + k0;
+      s.K = (int)((k1 < a.K ? k1 : a.K) - k0);
+      s.add = i > 0;
+      THANOS_TRY(proj_gemm(s, stream));
+    }
+    return THANOS_OK;
+  }
   p.nt = shape.nt;
   p.splits = shape.splits;
   p.tiles_m = (a.M + (pairs ? PTM : TM) - 1) / (pairs ? PTM : TM);

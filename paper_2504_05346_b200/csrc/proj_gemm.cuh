@@ -44,7 +44,7 @@ struct ProjArgs {
   // PROJ_OUT, PROJ_SHRINK and their fp32 forms
   void* out = nullptr;           // [N, ldo], bf16 (OUT32: fp32)
   int64_t ldo = 0;
-  int add = 0;                   // OUT32: to what is there
+  int add = 0;                   // OUT32, GRAM with two planes: to what is there
   float* V = nullptr;            // [N, r]: PROJ_OUT reads it (forward: V, backward: U); SHRINK writes
   __nv_bfloat16* planes = nullptr;  // SHRINK: V also as three bf16 planes, [N, 3 r16] (or null)
   const int32_t* index = nullptr;

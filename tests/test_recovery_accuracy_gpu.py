@@ -137,3 +137,26 @@ def test_fp32_step_on_short_sides(T, shape, kind):
     X = X.mT if tall else X
     for i in range(shape[0]):
         assert rel(-W[i], X[i]) <= 5.8e-5
+
+
+@pytest.mark.parametrize("kind", ["flat", "lead"])
+@pytest.mark.parametrize("shape", [(2048, 65536), (65536, 2100), (1300, 32776), (200, 65536)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_fp32_step_on_long_sides(T, shape, kind):
+    """The diagonal of S is a sum of squares of which an accumulator cuts 2^-24 on average each of its
+    three products per 16 terms, 3 16384 / 16 times at most, and half of them, on average, at full size:
+    9e-5 of the diagonal; the polynomial's slope makes up to four times that of the last step's factor
+    and less of the others', on the strong half of the directions: 2e-4."""
+    gen = torch.Generator(device="cuda").manual_seed(71)
+    G = spectrum(kind, 1, *shape, gen)[0]
+    Z = torch.zeros_like(G)
+    W, _ = T.orthogonal_step(Z, Z, G, lr=1.0, momentum=0.0, check=True)
+    X = G.double()
+    tall = shape[0] > shape[1]
+    X = X.mT if tall else X
+    X = X / (X.norm() + 1e-7)
+    a, b, c = T.NEWTON_SCHULZ
+    for _ in range(5):
+        S = X @ X.mT
+        X = a * X + (b * S + c * (S @ S)) @ X
+    assert rel(-(W.mT if tall else W), X) <= 2e-4
