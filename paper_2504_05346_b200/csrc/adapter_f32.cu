@@ -252,6 +252,12 @@ __global__ void __launch_bounds__(256) grad_f32_kernel(const Grad32Params p) {
   const int j0 = blockIdx.z * RANKS, nj = min(RANKS, p.r - j0);
   for (int64_t i = blockIdx.y; i < p.n; i += gridDim.y) {
     const int lo = p.off[i], hi = p.off[i + 1];
+    const int64_t at = sd.by_feature ? (i * sd.F + f) * p.r + j0 + g
+                                     : (i * p.r + j0 + g) * (int64_t)sd.F + f;
+    if (hi == lo) {  // no tokens: zero, whatever the scale
+      if (g < nj && f < sd.F && !p.accumulate) sd.out[at] = 0.f;
+      continue;
+    }
     // sums of a round, and of rounds: with many tokens one chain of additions would round away more
     // than it may (2^24 tokens: 3.5e-5 of the result)
     float s[RANKS] = {}, total[RANKS] = {};
@@ -287,9 +293,8 @@ __global__ void __launch_bounds__(256) grad_f32_kernel(const Grad32Params p) {
     if (g < nj && f < sd.F) {
       float v = 0.f;
       for (int k = 0; k < 8; ++k) v += red[k][g][threadIdx.x & 31];
-      if (sd.scale && hi > lo) v *= sd.scale[i];  // without tokens 0, whatever the scale
-      float* o = sd.out + (sd.by_feature ? (i * sd.F + f) * p.r + j0 + g
-                                         : (i * p.r + j0 + g) * (int64_t)sd.F + f);
+      if (sd.scale) v *= sd.scale[i];
+      float* o = sd.out + at;
       *o = p.accumulate ? *o + v : v;
     }
     __syncthreads();
