@@ -253,7 +253,7 @@ __global__ void __launch_bounds__(G_THREADS, RMAX <= 64 ? 2 : 1) grad_tc_kernel(
         const int at = ks0 * GK + r8 + 16 * u;
         next[u] = at < len ? p.order[lo + at] : -1;
       }
-      for (int ks = ks0; ks < ks1 && ok; ++ks) {
+      for (int ks = ks0; ks < ks1; ++ks) {
         int tok[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -261,8 +261,9 @@ __global__ void __launch_bounds__(G_THREADS, RMAX <= 64 ? 2 : 1) grad_tc_kernel(
           const int at = (ks + 1) * GK + r8 + 16 * u;
           next[u] = at < len ? p.order[lo + at] : -1;
         }
-        ok = mbar_wait_warp(empty_bar(s), phase ^ 1u, abort_flag);
-        if (!ok) break;
+        // lanes whose wait ran out go on, without waiting: the warp stays together with no vote, which
+        // takes 3 %, and the stages that are overwritten belong to a call that reports the timeout
+        if (ok) ok = mbar_wait(empty_bar(s), phase ^ 1u, abort_flag);
         const uint32_t st = smem_base + (uint32_t)s * stage_bytes;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
