@@ -317,8 +317,8 @@ __device__ __forceinline__ void emit(const Params& p, int z, int m, int n0, floa
         }
       } else if (own < 0 && i == 0) p.V[(int64_t)t * p.r + j] = 0.f;
     }
-  } else if constexpr (EPI == PROJ_GRAM || EPI == PROJ_POLY) {
-    __half* D = (EPI == PROJ_GRAM ? p.S : p.Pm) + (int64_t)z * p.s_batch;
+  } else if constexpr (EPI == PROJ_GRAM || EPI == PROJ_GRAM_ADD || EPI == PROJ_POLY) {
+    __half* D = (EPI == PROJ_POLY ? p.Pm : p.S) + (int64_t)z * p.s_batch;
     if constexpr (EPI == PROJ_POLY) {
       const __half* S = p.S + (int64_t)z * p.s_batch + (int64_t)n0 * p.lds + m;
       // columns beyond the last read the first one again: a load under a condition is not issued ahead
@@ -353,7 +353,7 @@ __device__ __forceinline__ void emit(const Params& p, int z, int m, int n0, floa
     } else {
 #pragma unroll
       for (int e = 0; e < NC; ++e) v[e] *= p.alpha;
-      if (p.add) {  // to both planes of what is there
+      if constexpr (EPI == PROJ_GRAM_ADD) {
 #pragma unroll 1
         for (int pl = 0; pl < 2; ++pl) {
           const __half* S = D + (int64_t)(pl * p.batch_z) * p.s_batch + (int64_t)n0 * p.lds + m;
@@ -366,11 +366,11 @@ __device__ __forceinline__ void emit(const Params& p, int z, int m, int n0, floa
       }
     }
     if (p.s_diag && m >= n0 && m < n0 + NC) {
-      float* diag = EPI == PROJ_GRAM ? p.s_diag : p.p_diag;
+      float* diag = EPI == PROJ_POLY ? p.p_diag : p.s_diag;
 #pragma unroll
       for (int e = 0; e < NC; ++e)
         if (n0 + e == m) {
-          if (EPI == PROJ_GRAM && p.add) v[e] += diag[(int64_t)z * p.lds + m];
+          if (EPI == PROJ_GRAM_ADD) v[e] += diag[(int64_t)z * p.lds + m];
           diag[(int64_t)z * p.lds + m] = v[e];
           v[e] = 0.f;
         }
@@ -1828,7 +1828,7 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
   if (a.M <= 0 || a.N <= 0 || a.batch <= 0) return THANOS_OK;
   if (a.lda % 8 || a.ldb % 8 || a.a_batch % 8 || a.b_batch % 8 || !aligned16(a.A) || !aligned16(a.B))
     return THANOS_ERR_ALIGNMENT;
-  const bool symmetric = a.epi == PROJ_GRAM || a.epi == PROJ_POLY;
+  const bool symmetric = a.epi == PROJ_GRAM || a.epi == PROJ_GRAM_ADD || a.epi == PROJ_POLY;
   Params p = {};
   p.M = a.M;
   p.N = a.N;
@@ -1846,7 +1846,7 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
       s.A = static_cast<const __half*>(a.A) + k0;
       s.B = static_cast<const __half*>(a.B) + k0;
       s.K = (int)((k1 < a.K ? k1 : a.K) - k0);
-      s.add = i > 0;
+      if (i > 0) s.epi = PROJ_GRAM_ADD;
       THANOS_TRY(proj_gemm(s, stream));
     }
     return THANOS_OK;
@@ -1941,6 +1941,8 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
       return launch<false, PROJ_SHRINK32>(mA, mB, p, stream);
     case PROJ_GRAM:
       return launch_any<false, PROJ_GRAM>(pairs, mA, mB, mP, p, stream);
+    case PROJ_GRAM_ADD:
+      return launch_any<false, PROJ_GRAM_ADD>(pairs, mA, mB, mP, p, stream);
     case PROJ_POLY:
       return launch_any<false, PROJ_POLY>(pairs, mA, mB, mP, p, stream);
     case PROJ_NEXT:

@@ -19,12 +19,14 @@ enum ProjEpilogue {
   PROJ_SHRINK = 1,  // m = (adapter, rank): V[n, rank] where the token's adapter is the row's
   PROJ_GRAM = 2,    // S = alpha D, fp16, symmetric: upper tiles computed, mirror written; with
                     // s_diag the diagonal goes there in fp32 and is zero in S
-  PROJ_POLY = 3,    // P = beta S + alpha S S, fp16, symmetric, its diagonal in p_diag likewise
-  PROJ_NEXT = 4,    // X' = beta (hi + lo) + alpha P X, as two fp16 planes
-  PROJ_FINAL = 5,   // the same value, unscaled, into O (bf16) or the new weights
-  PROJ_OUT32 = 6,   // PROJ_OUT with fp32 accuracy: A and B are three bf16 planes (a_batch, b_batch
+  PROJ_GRAM_ADD = 3,  // the same, added to both planes of the S that is there (a form of its own: the
+                    // code for it costs PROJ_GRAM 3 us of 110 where its products are small)
+  PROJ_POLY = 4,    // P = beta S + alpha S S, fp16, symmetric, its diagonal in p_diag likewise
+  PROJ_NEXT = 5,    // X' = beta (hi + lo) + alpha P X, as two fp16 planes
+  PROJ_FINAL = 6,   // the same value, unscaled, into O (bf16) or the new weights
+  PROJ_OUT32 = 7,   // PROJ_OUT with fp32 accuracy: A and B are three bf16 planes (a_batch, b_batch
                     // apart), out and P are fp32
-  PROJ_SHRINK32 = 7 // PROJ_SHRINK with fp32 accuracy, planes as in OUT32
+  PROJ_SHRINK32 = 8 // PROJ_SHRINK with fp32 accuracy, planes as in OUT32
 };
 
 struct ProjArgs {
@@ -44,7 +46,7 @@ struct ProjArgs {
   // PROJ_OUT, PROJ_SHRINK and their fp32 forms
   void* out = nullptr;           // [N, ldo], bf16 (OUT32: fp32)
   int64_t ldo = 0;
-  int add = 0;                   // OUT32, GRAM with two planes: to what is there
+  int add = 0;                   // OUT32: to what is there
   float* V = nullptr;            // [N, r]: PROJ_OUT reads it (forward: V, backward: U); SHRINK writes
   __nv_bfloat16* planes = nullptr;  // SHRINK: V also as three bf16 planes, [N, 3 r16] (or null)
   const int32_t* index = nullptr;
