@@ -121,8 +121,9 @@ def prepare(case, seed):
     s = dict(case=case)
     if op in ("logp", "dlogp"):
         T, V, k = case["T"], case["V"], case["k"]
-        # a broad floor, a few candidates above it, some of the vocabulary masked out
-        Z = 2.5 * rn(T, V) - 4.0
+        # a broad floor whose weight does not go by the vocabulary, a few candidates above it, some
+        # of the vocabulary masked out
+        Z = 2.5 * rn(T, V) - 4.0 + math.log(32000 / V)
         cand = torch.randint(0, V // 12, (T, 12), generator=gen, device="cuda")
         cand = cand + torch.arange(12, device="cuda") * (V // 12)
         Z.scatter_(1, cand, 6.0 + 3.0 * rn(T, 12))
