@@ -456,6 +456,61 @@ thanos_status_t thanos_orthogonal_step(void* W_out, const void* W_in, thanos_dty
  * accepted. */
 size_t thanos_orthogonal_workspace_bytes(int64_t batch, int64_t m, int64_t n);
 
+/*
+ * Recovery of a pruned layer, 3: what a model answers with.
+ *
+ * Log probabilities of given tokens, the entropy of every row and its k most likely tokens, from
+ * logits Z [n_tok, vocab] in one pass:
+ *
+ *     log p_j = z_j - log sum_i exp(z_i),   logp[t] = log p_target[t],   H = -sum_j p_j log p_j
+ *
+ *  logp     device fp32 [n_tok], or NULL without targets; 0 for a negative target (a token that is
+ *           left out), NaN for a target >= vocab.
+ *  entropy  device fp32 [n_tok].
+ *  stats    device fp32 [n_tok, 2]: a row's largest logit and the log of its sum of exp(z - largest),
+ *           for thanos_token_logprobs_backward.  Their sum is log sum exp(z).
+ *  top_index, top_logp   device int64 and fp32 [n_tok, k], not read or written for k == 0: the k most
+ *           likely tokens, the likeliest first, equal logits by index (zeros of both signs are equal,
+ *           a NaN comes before everything), and their log probabilities.
+ *  Z        device [n_tok, vocab] of dtype, leading dimension ldz >= vocab.
+ *  target   device int64 [n_tok] or NULL.
+ *  Logits of -infinity have probability 0 and take no part in H.  In a row of nothing else, logp and
+ *  top_logp are -infinity, H is 0, and stats are -infinity and 0.  A NaN or +infinity makes logp (of a
+ *  token that is not left out), H and top_logp of its row NaN.
+ *  0 <= n_tok <= 2^24 (0 is a no-op), 1 <= vocab <= 2^24, 0 <= k <= min(64, vocab),
+ *  n_tok (vocab / 4096 + 2) < 2^31.  Pointers need the alignment of what they point to, no more.
+ * Sums are fp32.  Same inputs, same bits.  No workspace.
+ */
+thanos_status_t thanos_token_logprobs(float* logp, float* entropy, float* stats, int64_t* top_index,
+                                      float* top_logp, const void* Z, int64_t ldz,
+                                      thanos_dtype_t dtype, const int64_t* target, int64_t n_tok,
+                                      int64_t vocab, int32_t k, void* stream);
+
+/*
+ * Gradient of sum_t (dlogp[t] logp[t] + dentropy[t] H[t] + sum_i dtop[t, i] log p_top_index[t, i]):
+ *
+ *     dZ_j = -p_j (G + dentropy (log p_j + H)) + dlogp [j = target] + sum_i dtop_i [j = top_index_i],
+ *     G = dlogp + sum_i dtop_i
+ *
+ *  dZ       device [n_tok, vocab] of dtype, leading dimension lddz >= vocab.  May be Z itself (the same
+ *           pointer and leading dimension), otherwise must not overlap it.
+ *  stats, entropy   what thanos_token_logprobs wrote for Z; entropy is read with dentropy only.
+ *  target, dlogp    both or neither NULL.  dlogp of a negative target is not read; a target >= vocab
+ *           makes its row NaN.
+ *  dentropy, dtop   fp32 [n_tok] and [n_tok, k], or NULL.
+ *  top_index   int64 [n_tok, k], read with dtop only; any tokens, also the same one several times; one
+ *           that is negative or >= vocab is left out.
+ *  A row with nothing to pass on (all its gradients are 0) and a row of -infinities get zeros.
+ * The rest as above.
+ */
+thanos_status_t thanos_token_logprobs_backward(void* dZ, int64_t lddz, const void* Z, int64_t ldz,
+                                               thanos_dtype_t dtype, const float* stats,
+                                               const int64_t* target, const float* dlogp,
+                                               const float* entropy, const float* dentropy,
+                                               const int64_t* top_index, const float* dtop,
+                                               int64_t n_tok, int64_t vocab, int32_t k,
+                                               void* stream);
+
 /* Minimum workspace in bytes for a call (see thanos_ws_which_t); 0 for unsupported shapes. */
 size_t thanos_workspace_bytes(int32_t which, int64_t c, int64_t b, int32_t B, thanos_dtype_t dtype);
 

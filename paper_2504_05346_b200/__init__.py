@@ -35,3 +35,8 @@ from .binding import (  # noqa: F401
     UNSTRUCTURED,
     NM,
 )
+from .logprobs import (  # noqa: F401
+    TokenLogprobs,
+    token_logprobs,
+    token_logprobs_backward,
+)

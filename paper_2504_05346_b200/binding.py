@@ -132,6 +132,11 @@ def load_library():
     lib.thanos_orthogonal_step.restype = i32
     lib.thanos_orthogonal_workspace_bytes.argtypes = [i64, i64, i64]
     lib.thanos_orthogonal_workspace_bytes.restype = sz
+    lib.thanos_token_logprobs.argtypes = [vp, vp, vp, vp, vp, vp, i64, i32, vp, i64, i64, i32, vp]
+    lib.thanos_token_logprobs.restype = i32
+    lib.thanos_token_logprobs_backward.argtypes = [vp, i64, vp, i64, i32, vp, vp, vp, vp, vp, vp, vp,
+                                                   i64, i64, i32, vp]
+    lib.thanos_token_logprobs_backward.restype = i32
     lib.thanos_fp32_fma_probe.argtypes = [vp, i64, i32, i32, ctypes.POINTER(ctypes.c_double), vp]
     lib.thanos_fp32_fma_probe.restype = i32
     lib.thanos_workspace_bytes.argtypes = [i32, i64, i64, i32, i32]
