@@ -511,6 +511,90 @@ thanos_status_t thanos_token_logprobs_backward(void* dZ, int64_t lddz, const voi
                                                int64_t n_tok, int64_t vocab, int32_t k,
                                                void* stream);
 
+/*
+ * Recovery of a pruned layer, 4: what is stored, in few bits.
+ *
+ * Weights in 4 bits.  Groups of 64 or 128 columns of a row share a scale:
+ *
+ *     w^ = code scale,   code in -8 .. 7
+ *
+ *  codes    device uint8 [c, ldq]: column 2 j in the low half of byte j, column 2 j + 1 in the high
+ *           half, each as code + 8.  ldq in bytes, ldq % 16 == 0, ldq >= 32 ceil(b / 64): rows are whole
+ *           blocks of 64 columns, whose codes beyond b may be anything (packing writes zeros there).
+ *  scales   device bf16 [ceil(b / group), c].  Five significant bits: the three lowest bits are taken
+ *           as zeros.  Then code scale has eight bits at most and is a bf16 number.
+ *  thanos_pack_weights takes scale = max |w| / 7 of the group, rounded to five bits (0 below the normal
+ *  numbers), and code = w / scale, rounded, in -7 .. 7 (0 where the scale is).  A zero stays a zero: a
+ *  pruned weight stays pruned.  A group with an infinity or NaN reads back as NaN.
+ *  W        device [c, b] of dtype, leading dimension ldw >= b, ldw % 8 == 0.
+ *  b and c as in thanos_adapter_forward, group 64 or 128.
+ */
+thanos_status_t thanos_pack_weights(uint8_t* codes, int64_t ldq, void* scales, const void* W,
+                                    int64_t ldw, thanos_dtype_t dtype, int64_t c, int64_t b,
+                                    int32_t group, void* stream);
+thanos_status_t thanos_unpack_weights(void* W, int64_t ldw, thanos_dtype_t dtype,
+                                      const uint8_t* codes, int64_t ldq, const void* scales,
+                                      int64_t c, int64_t b, int32_t group, void* stream);
+
+/*
+ * Activations in 8 bits, as they are kept for a backward pass.  Groups of 32 columns of a row share a
+ * power of two:
+ *
+ *     x^ = code 2^(e - 127),   code in -127 .. 127
+ *
+ *  codes    device int8 [n_tok, b], leading dimension ldc >= b, ldc % 16 == 0.
+ *  exps     device uint8 [n_tok, ceil(b / 32)], leading dimension lde, lde % 4 == 0, 4-byte aligned.
+ *           0 stands for a group of zeros, 255 for one that holds an infinity or NaN: its infinities
+ *           read back with their sign, everything else in it as NaN.
+ *  thanos_pack_activations takes the smallest power of two, 2^-126 at least, for which no code leaves
+ *  the range (2^121 at most, where a code that would be 128 stays 127), and rounds to nearest, ties to
+ *  even.  bf16 holds every x^.
+ *  X        device [n_tok, b] of dtype, leading dimension ldx >= b, ldx % 8 == 0.
+ *  n_tok and b as in thanos_adapter_forward.
+ */
+thanos_status_t thanos_pack_activations(int8_t* codes, int64_t ldc, uint8_t* exps, int64_t lde,
+                                        const void* X, int64_t ldx, thanos_dtype_t dtype,
+                                        int64_t n_tok, int64_t b, void* stream);
+thanos_status_t thanos_unpack_activations(void* X, int64_t ldx, thanos_dtype_t dtype,
+                                          const int8_t* codes, int64_t ldc, const uint8_t* exps,
+                                          int64_t lde, int64_t n_tok, int64_t b, void* stream);
+
+/*
+ * thanos_adapter_forward with packed weights (w_codes, ldq, w_scales and group as above) in the place
+ * of W, ldw.  The weights are w^, exactly: 32-bit results are those of 32-bit weights.  Everything else
+ * as there; workspace: thanos_adapter_packed_workspace_bytes(0, 1, 0, ...) bytes.
+ */
+thanos_status_t thanos_adapter_forward_packed(void* Y, int64_t ldy, float* V, const void* X,
+                                              int64_t ldx, const uint8_t* w_codes, int64_t ldq,
+                                              const void* w_scales, int32_t group, const void* A,
+                                              const void* B, const int32_t* index,
+                                              const float* scale, thanos_dtype_t dtype,
+                                              int64_t n_tok, int64_t c, int64_t b,
+                                              int64_t n_adapters, int32_t r, void* workspace,
+                                              size_t ws_bytes, void* stream);
+
+/*
+ * thanos_adapter_backward with packed weights, packed activations or both.  w_scales == NULL: W and ldw
+ * as there (group is not read), else W are packed codes and ldw is their ldq.  x_exps == NULL: X and ldx
+ * as there, else X are packed codes, ldx is their ldc, and x_exps and lde go with them.
+ * workspace: thanos_adapter_packed_workspace_bytes(1, w_scales != NULL, x_exps != NULL, ...) bytes.
+ */
+thanos_status_t thanos_adapter_backward_packed(void* dX, int64_t lddx, float* dA, float* dB,
+                                               int32_t accumulate, const void* dY, int64_t lddy,
+                                               const void* X, int64_t ldx, const uint8_t* x_exps,
+                                               int64_t lde, const float* V, const void* W,
+                                               int64_t ldw, const void* w_scales, int32_t group,
+                                               const void* A, const void* B, const int32_t* index,
+                                               const float* scale, thanos_dtype_t dtype,
+                                               int64_t n_tok, int64_t c, int64_t b,
+                                               int64_t n_adapters, int32_t r, void* workspace,
+                                               size_t ws_bytes, void* stream);
+
+/* Workspace of the two calls above; 0 if the arguments are not accepted. */
+size_t thanos_adapter_packed_workspace_bytes(int32_t backward, int32_t packed_w, int32_t packed_x,
+                                             int64_t n_tok, int64_t c, int64_t b,
+                                             int64_t n_adapters, int32_t r, thanos_dtype_t dtype);
+
 /* Minimum workspace in bytes for a call (see thanos_ws_which_t); 0 for unsupported shapes. */
 size_t thanos_workspace_bytes(int32_t which, int64_t c, int64_t b, int32_t B, thanos_dtype_t dtype);
 

@@ -26,6 +26,8 @@ from .binding import (  # noqa: F401
     orthogonalise,
     orthogonal_step,
     NEWTON_SCHULZ,
+    PackedWeights,
+    PackedActivations,
     workspace_bytes,
     launch_count,
     status_string,
@@ -39,4 +41,10 @@ from .logprobs import (  # noqa: F401
     TokenLogprobs,
     token_logprobs,
     token_logprobs_backward,
+)
+from .packed import (  # noqa: F401
+    pack_weights,
+    unpack_weights,
+    pack_activations,
+    unpack_activations,
 )

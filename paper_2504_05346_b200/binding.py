@@ -7,7 +7,7 @@ import ctypes
 import functools
 import os
 from dataclasses import dataclass
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple, Union
 
 import torch
 
@@ -125,6 +125,23 @@ def load_library():
     lib.thanos_adapter_backward.restype = i32
     lib.thanos_adapter_workspace_bytes.argtypes = [i32, i64, i64, i64, i64, i32, i32]
     lib.thanos_adapter_workspace_bytes.restype = sz
+    lib.thanos_adapter_forward_packed.argtypes = [vp, i64, vp, vp, i64, vp, i64, vp, i32, vp, vp, vp,
+                                                  vp, i32, i64, i64, i64, i64, i32, vp, sz, vp]
+    lib.thanos_adapter_forward_packed.restype = i32
+    lib.thanos_adapter_backward_packed.argtypes = [vp, i64, vp, vp, i32, vp, i64, vp, i64, vp, i64, vp,
+                                                   vp, i64, vp, i32, vp, vp, vp, vp, i32, i64, i64, i64,
+                                                   i64, i32, vp, sz, vp]
+    lib.thanos_adapter_backward_packed.restype = i32
+    lib.thanos_adapter_packed_workspace_bytes.argtypes = [i32, i32, i32, i64, i64, i64, i64, i32, i32]
+    lib.thanos_adapter_packed_workspace_bytes.restype = sz
+    lib.thanos_pack_weights.argtypes = [vp, i64, vp, vp, i64, i32, i64, i64, i32, vp]
+    lib.thanos_pack_weights.restype = i32
+    lib.thanos_unpack_weights.argtypes = [vp, i64, i32, vp, i64, vp, i64, i64, i32, vp]
+    lib.thanos_unpack_weights.restype = i32
+    lib.thanos_pack_activations.argtypes = [vp, i64, vp, i64, vp, i64, i32, i64, i64, vp]
+    lib.thanos_pack_activations.restype = i32
+    lib.thanos_unpack_activations.argtypes = [vp, i64, i32, vp, i64, vp, i64, i64, i64, vp]
+    lib.thanos_unpack_activations.restype = i32
     lib.thanos_orthogonalise.argtypes = [vp, vp, i32, i64, i64, i64, vp, i32, f32, vp, sz, vp]
     lib.thanos_orthogonalise.restype = i32
     lib.thanos_orthogonal_step.argtypes = [vp, vp, i32, vp, vp, vp, i32, vp, i64, i64, i64, f32, f32,
@@ -531,18 +548,69 @@ def _device_of(t: torch.Tensor, name: str) -> int:
     return t.get_device()
 
 
+class PackedWeights(NamedTuple):
+    """Weights [c, cols] in 4 bits, from pack_weights: codes uint8 [c, ldq] (two a byte, the even
+    column in the low half, each as code + 8; rows of whole 64-column blocks), scales bfloat16
+    [ceil(cols / group), c] of five significant bits.  Takes the place of W."""
+
+    codes: torch.Tensor
+    scales: torch.Tensor
+    group: int
+    cols: int
+
+
+class PackedActivations(NamedTuple):
+    """Activations in 8 bits, from pack_activations: codes int8 [n_tok, b] (leading dimension a
+    multiple of 16), exps uint8 [n_tok, ceil(b / 32)] (leading dimension a multiple of 4):
+    x = code 2^(e - 127).  Takes the place of X in adapter_backward."""
+
+    codes: torch.Tensor
+    exps: torch.Tensor
+
+
+def _packed_weights(W: PackedWeights, dev: int):
+    """Checked (c, b, ldq) of packed weights."""
+    codes, scales, group, b = W
+    if codes.get_device() != dev or codes.dtype != torch.uint8 or codes.dim() != 2:
+        raise ValueError("the weights' codes must be a uint8 matrix on CUDA device %d" % dev)
+    (c, wide), (ldq, inner) = codes.shape, codes.stride()
+    if inner != 1 or wide < -(-b // 64) * 32:
+        raise ValueError("the weights' codes must have unit inner stride and whole 64-column blocks")
+    if group not in (64, 128):
+        raise ValueError("the weights' group must be 64 or 128")
+    _dense(scales, (-(-b // group), c), torch.bfloat16, dev, "the weights' scales")
+    return c, b, ldq if c > 1 else -(-wide // 16) * 16
+
+
+def _packed_activations(X: PackedActivations, b: int, dev: int):
+    """Checked (T, ldc, lde) of packed activations."""
+    codes, exps = X
+    if codes.dtype != torch.int8 or exps.dtype != torch.uint8 or exps.dim() != 2 \
+            or exps.shape[0] != codes.shape[0]:
+        raise ValueError("packed activations are int8 codes [n_tok, b] and uint8 exps [n_tok, b / 32]")
+    ldc = _rows(codes, b, dev, "the activations' codes")
+    lde = _rows(exps, -(-b // 32), dev, "the activations' exps")
+    if codes.shape[0] <= 1:       # one row: its strides are never used
+        ldc, lde = -(-b // 16) * 16, -(-lde // 4) * 4
+    return codes.shape[0], ldc, lde
+
+
 def _adapters(X, W, A, B, index, scale, dev):
-    """Checked sizes (T, c, b, n, r) and dtype code of an adapted projection."""
+    """Checked sizes (T, c, b, n, r), W's leading dimension and dtype code of an adapted projection."""
     dtype = X.dtype
     dt = _dtype_code(X)
-    if W.dim() != 2 or W.dtype != dtype:
-        raise ValueError("W must be a matrix of X's dtype")
-    c, b = W.shape
+    if type(W) is PackedWeights:
+        c, b, ldw = _packed_weights(W, dev)
+    else:
+        if W.dim() != 2 or W.dtype != dtype:
+            raise ValueError("W must be a matrix of X's dtype")
+        c, b = W.shape
+        ldw = _rows(W, b, dev, "W")
     T = X.shape[0]
     if A is None:
         if not (B is None and index is None and scale is None):
             raise ValueError("without A there is no B, index or scale either")
-        return T, c, b, 0, 0, dt
+        return T, c, b, 0, 0, ldw, dt
     if A.dim() != 3:
         raise ValueError("A must have the shape [n_adapters, r, b]")
     n, r, _ = A.shape
@@ -550,12 +618,18 @@ def _adapters(X, W, A, B, index, scale, dev):
     _dense(B, (n, c, r), dtype, dev, "B")
     _dense(index, (T,), torch.int32, dev, "index")
     _dense(scale, (n,), torch.float32, dev, "scale")
-    return T, c, b, n, r, dt
+    return T, c, b, n, r, ldw, dt
 
 
 @functools.lru_cache(maxsize=256)
 def _adapter_workspace(backward, T, c, b, n, r, dt):
     return max(int(load_library().thanos_adapter_workspace_bytes(backward, T, c, b, n, r, dt)), 256)
+
+
+@functools.lru_cache(maxsize=256)
+def _packed_workspace(backward, packed_w, packed_x, T, c, b, n, r, dt):
+    return max(int(load_library().thanos_adapter_packed_workspace_bytes(
+        backward, packed_w, packed_x, T, c, b, n, r, dt)), 256)
 
 
 @functools.lru_cache(maxsize=256)
@@ -584,7 +658,7 @@ def _status(workspace: torch.Tensor, where: str, stream) -> None:
         raise ThanosError(st, where + " (device)")
 
 
-def adapter_forward(X: torch.Tensor, W: torch.Tensor, A: Optional[torch.Tensor] = None,
+def adapter_forward(X: torch.Tensor, W: Union[torch.Tensor, PackedWeights], A: Optional[torch.Tensor] = None,
                     B: Optional[torch.Tensor] = None, index: Optional[torch.Tensor] = None,
                     scale: Optional[torch.Tensor] = None, stream=None,
                     workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
@@ -592,12 +666,14 @@ def adapter_forward(X: torch.Tensor, W: torch.Tensor, A: Optional[torch.Tensor] 
     """thanos_adapter_forward: Y[t] = X[t] W^T + scale[i] (X[t] A[i]^T) B[i]^T with i = index[t],
     -1 for a token without adapter.  X [T, b], W [c, b], A [n, r, b], B [n, c, r] share a dtype
     (float32 or bfloat16); index int32 [T], scale float32 [n].  Returns (Y, V): V float32 [T, r]
-    holds X[t] A[i]^T for adapter_backward (None without adapters).  With check=True the call's
-    device status word is read back (this waits for the call)."""
+    holds X[t] A[i]^T for adapter_backward (None without adapters).  W may be PackedWeights
+    (thanos_adapter_forward_packed).  With check=True the call's device status word is read back (this
+    waits for the call)."""
     lib = load_library()
     dev = _device_of(X, "X")
-    T, c, b, n, r, dt = _adapters(X, W, A, B, index, scale, dev)
-    ldx, ldw = _rows(X, b, dev, "X"), _rows(W, b, dev, "W")
+    T, c, b, n, r, ldw, dt = _adapters(X, W, A, B, index, scale, dev)
+    packed = type(W) is PackedWeights
+    ldx = _rows(X, b, dev, "X")
     with _on(X):
         with _alloc_scope(stream):
             if out is None:
@@ -611,20 +687,29 @@ def adapter_forward(X: torch.Tensor, W: torch.Tensor, A: Optional[torch.Tensor] 
                     _dense(V, (T, r), torch.float32, dev, "V")
             else:
                 V = None     # a buffer that was passed in is not written
-            workspace = _scratch(workspace, _adapter_workspace(0, T, c, b, n, r, dt), X)
+            workspace = _scratch(workspace, _packed_workspace(0, 1, 0, T, c, b, n, r, dt) if packed
+                                 else _adapter_workspace(0, T, c, b, n, r, dt), X)
         ldy = _rows(out, c, dev, "out")
-        _check(lib.thanos_adapter_forward(out.data_ptr(), ldy, _ptr(V), X.data_ptr(), ldx,
-                                          W.data_ptr(), ldw, _ptr(A), _ptr(B), _ptr(index),
-                                          _ptr(scale), dt, T, c, b, n, r, workspace.data_ptr(),
-                                          workspace.numel(), _stream_ptr(stream)),
-               "thanos_adapter_forward")
+        if packed:
+            _check(lib.thanos_adapter_forward_packed(
+                out.data_ptr(), ldy, _ptr(V), X.data_ptr(), ldx, W.codes.data_ptr(), ldw,
+                W.scales.data_ptr(), W.group, _ptr(A), _ptr(B), _ptr(index), _ptr(scale), dt, T, c, b,
+                n, r, workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)),
+                "thanos_adapter_forward_packed")
+        else:
+            _check(lib.thanos_adapter_forward(out.data_ptr(), ldy, _ptr(V), X.data_ptr(), ldx,
+                                              W.data_ptr(), ldw, _ptr(A), _ptr(B), _ptr(index),
+                                              _ptr(scale), dt, T, c, b, n, r, workspace.data_ptr(),
+                                              workspace.numel(), _stream_ptr(stream)),
+                   "thanos_adapter_forward")
         if check:
             _status(workspace, "thanos_adapter_forward", stream)
     return out, V
 
 
-def adapter_backward(dY: torch.Tensor, X: Optional[torch.Tensor], V: Optional[torch.Tensor],
-                     W: torch.Tensor, A: Optional[torch.Tensor] = None,
+def adapter_backward(dY: torch.Tensor, X: Union[torch.Tensor, PackedActivations, None],
+                     V: Optional[torch.Tensor], W: Union[torch.Tensor, PackedWeights],
+                     A: Optional[torch.Tensor] = None,
                      B: Optional[torch.Tensor] = None, index: Optional[torch.Tensor] = None,
                      scale: Optional[torch.Tensor] = None, need_dx: bool = True,
                      dA: Optional[torch.Tensor] = None, dB: Optional[torch.Tensor] = None,
@@ -634,19 +719,28 @@ def adapter_backward(dY: torch.Tensor, X: Optional[torch.Tensor], V: Optional[to
     """thanos_adapter_backward: (dX, dA, dB) of adapter_forward for the output gradient dY [T, c].
     V is what adapter_forward returned.  dA, dB are float32, shaped like A and B; with
     accumulate=True they are added to (pass them in).  need_dx=False / need_grads=False leave a
-    part out (None is returned for it; X and V may then be None without gradients)."""
+    part out (None is returned for it; X and V may then be None without gradients).  X may be
+    PackedActivations and W PackedWeights, one or both (thanos_adapter_backward_packed)."""
     lib = load_library()
     dev = _device_of(dY, "dY")
-    T, c, b, n, r, dt = _adapters(dY, W, A, B, index, scale, dev)
-    lddy, ldw = _rows(dY, c, dev, "dY"), _rows(W, b, dev, "W")
+    T, c, b, n, r, ldw, dt = _adapters(dY, W, A, B, index, scale, dev)
+    packed_w = type(W) is PackedWeights
+    lddy = _rows(dY, c, dev, "dY")
     need_grads = need_grads and n > 0
-    ldx = 0
+    ldx = lde = 0
+    packed_x = need_grads and type(X) is PackedActivations
     if need_grads:
         if X is None or V is None:
             raise ValueError("the adapters' gradients need X and V")
-        if X.dtype != dY.dtype or X.shape[0] != T:
+        if packed_x:
+            rows, ldx, lde = _packed_activations(X, b, dev)
+            if rows != T:
+                raise ValueError("X must have n_tok rows")
+            X, exps = X
+        elif X.dtype != dY.dtype or X.shape[0] != T:
             raise ValueError("X must be a [T, b] tensor of dY's dtype")
-        ldx = _rows(X, b, dev, "X")
+        if not packed_x:
+            ldx = _rows(X, b, dev, "X")
         _dense(V, (T, r), torch.float32, dev, "V")
         if accumulate and (dA is None or dB is None):
             raise ValueError("accumulate=True needs dA and dB")
@@ -670,15 +764,26 @@ def adapter_backward(dY: torch.Tensor, X: Optional[torch.Tensor], V: Optional[to
                     dB = scale.new_empty((n, c, r))
                 else:
                     _dense(dB, (n, c, r), torch.float32, dev, "dB")
-            workspace = _scratch(workspace, _adapter_workspace(1, T, c, b, n, r, dt), dY)
+            workspace = _scratch(workspace,
+                                 _packed_workspace(1, int(packed_w), int(packed_x), T, c, b, n, r, dt)
+                                 if packed_w or packed_x else _adapter_workspace(1, T, c, b, n, r, dt),
+                                 dY)
         if need_dx:
             lddx = _rows(dX, b, dev, "dX")
-        _check(lib.thanos_adapter_backward(_ptr(dX), lddx, _ptr(dA), _ptr(dB),
-                                           1 if accumulate else 0, dY.data_ptr(), lddy, _ptr(X), ldx,
-                                           _ptr(V), W.data_ptr(), ldw, _ptr(A), _ptr(B), _ptr(index),
-                                           _ptr(scale), dt, T, c, b, n, r, workspace.data_ptr(),
-                                           workspace.numel(), _stream_ptr(stream)),
-               "thanos_adapter_backward")
+        if packed_w or packed_x:
+            _check(lib.thanos_adapter_backward_packed(
+                _ptr(dX), lddx, _ptr(dA), _ptr(dB), 1 if accumulate else 0, dY.data_ptr(), lddy,
+                _ptr(X), ldx, exps.data_ptr() if packed_x else None, lde, _ptr(V),
+                W.codes.data_ptr() if packed_w else W.data_ptr(), ldw,
+                W.scales.data_ptr() if packed_w else None, W.group if packed_w else 0, _ptr(A),
+                _ptr(B), _ptr(index), _ptr(scale), dt, T, c, b, n, r, workspace.data_ptr(),
+                workspace.numel(), _stream_ptr(stream)), "thanos_adapter_backward_packed")
+        else:
+            _check(lib.thanos_adapter_backward(
+                _ptr(dX), lddx, _ptr(dA), _ptr(dB), 1 if accumulate else 0, dY.data_ptr(), lddy,
+                _ptr(X), ldx, _ptr(V), W.data_ptr(), ldw, _ptr(A), _ptr(B), _ptr(index), _ptr(scale),
+                dt, T, c, b, n, r, workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)),
+                "thanos_adapter_backward")
         if check:
             _status(workspace, "thanos_adapter_backward", stream)
     return dX, dA, dB

@@ -1,6 +1,7 @@
 // extern "C" entry points of the recovery operators: argument checks and dispatch.
 #include <math.h>
 
+#include "packed.cuh"
 #include "recovery.cuh"
 
 using namespace thanos;
@@ -70,6 +71,191 @@ thanos_status_t orthogonal_run(const OrthogonalArgs& a, void* workspace, size_t 
   return orthogonal_impl(a, workspace, ws_bytes, static_cast<cudaStream_t>(stream));
 }
 
+// ---- packed operands
+constexpr int64_t PACKED_LINE = 64;   // columns: rows of what is unpacked start on whole lines
+
+thanos_status_t packed_weights_ok(const PackedWeights& w, int64_t b) {
+  if (w.group != 64 && w.group != 128) return THANOS_ERR_SHAPE;
+  if (w.ldq < (int64_t)round_up((size_t)b, 64) / 2) return THANOS_ERR_SHAPE;
+  if (w.ldq % 16 || !aligned16(w.codes) || (reinterpret_cast<uintptr_t>(w.scales) & 1u))
+    return THANOS_ERR_ALIGNMENT;
+  return THANOS_OK;
+}
+
+thanos_status_t packed_activations_ok(const PackedActivations& x, int64_t b) {
+  if (x.ldc < b || x.lde < ceil_div(b, ACT_GROUP)) return THANOS_ERR_SHAPE;
+  if (x.ldc % 16 || x.lde % 4 || !aligned16(x.codes) || !aligned4(x.exps))
+    return THANOS_ERR_ALIGNMENT;
+  return THANOS_OK;
+}
+
+size_t unpacked_bytes(int64_t rows, int64_t b, thanos_dtype_t dtype) {
+  return round_up((size_t)rows * round_up((size_t)b, PACKED_LINE) * (dtype == THANOS_BF16 ? 2 : 4),
+                  256);
+}
+
+// What a call on packed operands needs beside what the call itself does.
+size_t packed_extra_bytes(bool w, bool x, int64_t T, int64_t c, int64_t b, thanos_dtype_t dtype) {
+  return (w ? unpacked_bytes(c, b, dtype) : 0) + (x ? unpacked_bytes(T, b, dtype) : 0);
+}
+
+// Where W is: as it is, or packed (W null).
+struct Weights {
+  const void* W;
+  int64_t ldw;
+  PackedWeights packed;
+  bool is_packed;
+};
+
+thanos_status_t weights_ok(const Weights& w, int64_t b) {
+  if (w.is_packed) return packed_weights_ok(w.packed, b);
+  if (w.ldw < b) return THANOS_ERR_SHAPE;
+  if (w.ldw % 8 || !aligned16(w.W)) return THANOS_ERR_ALIGNMENT;
+  return THANOS_OK;
+}
+
+bool weights_there(const Weights& w) {
+  return w.is_packed ? w.packed.codes && w.packed.scales : w.W != nullptr;
+}
+
+thanos_status_t forward_call(void* Y, int64_t ldy, float* V, const void* X, int64_t ldx,
+                             const Weights& w, const void* A, const void* B, const int32_t* index,
+                             const float* scale, thanos_dtype_t dtype, int64_t n_tok, int64_t c,
+                             int64_t b, int64_t n_adapters, int32_t r, void* workspace,
+                             size_t ws_bytes, cudaStream_t stream) {
+  if (!weights_there(w) || (n_tok > 0 && (!Y || !X))) return THANOS_ERR_INVALID_ARG;
+  if (n_adapters > 0 && (!A || !B || !scale || (n_tok > 0 && !index)))
+    return THANOS_ERR_INVALID_ARG;
+  THANOS_TRY(adapter_shape(n_tok, c, b, n_adapters, r, dtype));
+  if (ldy < c || ldx < b || (!w.is_packed && w.ldw < b)) return THANOS_ERR_SHAPE;
+  if (ldx % 8) return THANOS_ERR_ALIGNMENT;
+  THANOS_TRY(weights_ok(w, b));
+  if (!aligned16(Y) || !aligned16(V) || !aligned16(X) || !aligned16(A) || !aligned16(B) ||
+      !aligned4(index) || !aligned4(scale) || !aligned16(workspace))
+    return THANOS_ERR_ALIGNMENT;
+  const size_t need =
+      w.is_packed ? thanos_adapter_packed_workspace_bytes(0, 1, 0, n_tok, c, b, n_adapters, r, dtype)
+                  : thanos_adapter_workspace_bytes(0, n_tok, c, b, n_adapters, r, dtype);
+  if (!workspace || ws_bytes < need) return THANOS_ERR_WORKSPACE;
+  if (n_tok == 0) {
+    THANOS_CUDA(cudaMemsetAsync(workspace, 0, 16, stream));
+    return THANOS_OK;
+  }
+  AdapterArgs a;
+  a.out = Y;
+  a.ldo = ldy;
+  a.in = X;
+  a.ldi = ldx;
+  a.W = w.W;
+  a.ldw = w.ldw;
+  a.A = A;
+  a.B = B;
+  a.index = index;
+  a.scale = scale;
+  a.V = n_adapters > 0 ? V : nullptr;
+  a.dtype = dtype;
+  a.T = n_tok;
+  a.c = c;
+  a.b = b;
+  a.n = n_adapters;
+  a.r = n_adapters > 0 ? r : 1;
+  if (w.is_packed) {
+    if (packed_few_tokens(a)) return packed_forward_few(a, w.packed, workspace, stream);
+    // many tokens: the weights are read back once, the product is theirs
+    const size_t extra = unpacked_bytes(c, b, dtype);
+    void* full = static_cast<char*>(workspace) + (need - extra);
+    a.W = full;
+    a.ldw = (int64_t)round_up((size_t)b, PACKED_LINE);
+    THANOS_TRY(unpack_weights(full, a.ldw, dtype, w.packed, c, b, stream));
+    ws_bytes = need - extra;
+  }
+  return adapter_forward_impl(a, workspace, ws_bytes, stream);
+}
+
+thanos_status_t backward_call(void* dX, int64_t lddx, float* dA, float* dB, int32_t accumulate,
+                              const void* dY, int64_t lddy, const void* X, int64_t ldx,
+                              const PackedActivations& x8, bool x_packed, const float* V,
+                              const Weights& w, const void* A, const void* B, const int32_t* index,
+                              const float* scale, thanos_dtype_t dtype, int64_t n_tok, int64_t c,
+                              int64_t b, int64_t n_adapters, int32_t r, void* workspace,
+                              size_t ws_bytes, cudaStream_t stream) {
+  const bool grads = dA != nullptr || dB != nullptr;
+  const bool x_there = x_packed ? x8.codes && x8.exps : X != nullptr;
+  if (!weights_there(w) || (n_tok > 0 && !dY)) return THANOS_ERR_INVALID_ARG;
+  if (grads && (!dA || !dB || n_adapters == 0 || (n_tok > 0 && (!x_there || !V))))
+    return THANOS_ERR_INVALID_ARG;
+  if (n_adapters > 0 && (!A || !B || !scale || (n_tok > 0 && !index)))
+    return THANOS_ERR_INVALID_ARG;
+  THANOS_TRY(adapter_shape(n_tok, c, b, n_adapters, r, dtype));
+  if (lddy < c || (!w.is_packed && w.ldw < b) || (dX && lddx < b) || (grads && !x_packed && ldx < b))
+    return THANOS_ERR_SHAPE;
+  if (grads && !x_packed && ldx % 8) return THANOS_ERR_ALIGNMENT;
+  if (grads && x_packed) THANOS_TRY(packed_activations_ok(x8, b));
+  THANOS_TRY(weights_ok(w, b));
+  if (!aligned16(dX) || !aligned16(dA) || !aligned16(dB) || !aligned16(dY) || !aligned16(V) ||
+      !aligned16(X) || !aligned16(A) || !aligned16(B) || !aligned4(index) || !aligned4(scale) ||
+      !aligned16(workspace))
+    return THANOS_ERR_ALIGNMENT;
+  const bool packed = w.is_packed || x_packed;
+  const size_t need =
+      packed ? thanos_adapter_packed_workspace_bytes(1, w.is_packed, x_packed, n_tok, c, b, n_adapters,
+                                                     r, dtype)
+             : thanos_adapter_workspace_bytes(1, n_tok, c, b, n_adapters, r, dtype);
+  if (!workspace || ws_bytes < need) return THANOS_ERR_WORKSPACE;
+  if (n_tok == 0) {
+    THANOS_CUDA(cudaMemsetAsync(workspace, 0, 16, stream));
+    if (grads && !accumulate) {
+      const size_t nr = (size_t)n_adapters * (size_t)r;
+      THANOS_CUDA(cudaMemsetAsync(dA, 0, nr * (size_t)b * 4, stream));
+      THANOS_CUDA(cudaMemsetAsync(dB, 0, nr * (size_t)c * 4, stream));
+    }
+    return THANOS_OK;
+  }
+  AdapterArgs a;
+  a.out = dX;
+  a.ldo = lddx;
+  a.in = dY;
+  a.ldi = lddy;
+  a.X = X;
+  a.ldx = ldx;
+  a.W = w.W;
+  a.ldw = w.ldw;
+  a.A = A;
+  a.B = B;
+  a.index = index;
+  a.scale = scale;
+  a.Vin = V;
+  a.dA = dA;
+  a.dB = dB;
+  a.accumulate = accumulate ? 1 : 0;
+  a.dtype = dtype;
+  a.T = n_tok;
+  a.c = c;
+  a.b = b;
+  a.n = n_adapters;
+  a.r = n_adapters > 0 ? r : 1;
+  if (packed) {
+    size_t at = need - packed_extra_bytes(w.is_packed, x_packed, n_tok, c, b, dtype);
+    ws_bytes = at;
+    const int64_t ld = (int64_t)round_up((size_t)b, PACKED_LINE);
+    if (w.is_packed) {
+      void* full = static_cast<char*>(workspace) + at;
+      at += unpacked_bytes(c, b, dtype);
+      a.W = full;
+      a.ldw = ld;
+      if (dX) THANOS_TRY(unpack_weights(full, ld, dtype, w.packed, c, b, stream));
+    }
+    if (x_packed && grads) {
+      void* full = static_cast<char*>(workspace) + at;
+      a.X = full;
+      a.ldx = ld;
+      THANOS_TRY(unpack_activations(full, ld, dtype, x8.codes, x8.ldc, x8.exps, x8.lde, n_tok, b,
+                                    stream));
+    }
+  }
+  return adapter_backward_impl(a, workspace, ws_bytes, stream);
+}
+
 }  // namespace
 
 extern "C" {
@@ -87,41 +273,9 @@ thanos_status_t thanos_adapter_forward(void* Y, int64_t ldy, float* V, const voi
                                        thanos_dtype_t dtype, int64_t n_tok, int64_t c, int64_t b,
                                        int64_t n_adapters, int32_t r, void* workspace,
                                        size_t ws_bytes, void* stream) {
-  if (!W || (n_tok > 0 && (!Y || !X))) return THANOS_ERR_INVALID_ARG;
-  if (n_adapters > 0 && (!A || !B || !scale || (n_tok > 0 && !index)))
-    return THANOS_ERR_INVALID_ARG;
-  THANOS_TRY(adapter_shape(n_tok, c, b, n_adapters, r, dtype));
-  if (ldy < c || ldx < b || ldw < b) return THANOS_ERR_SHAPE;
-  if (ldx % 8 || ldw % 8) return THANOS_ERR_ALIGNMENT;
-  if (!aligned16(Y) || !aligned16(V) || !aligned16(X) || !aligned16(W) || !aligned16(A) ||
-      !aligned16(B) || !aligned4(index) || !aligned4(scale) || !aligned16(workspace))
-    return THANOS_ERR_ALIGNMENT;
-  if (!workspace ||
-      ws_bytes < thanos_adapter_workspace_bytes(0, n_tok, c, b, n_adapters, r, dtype))
-    return THANOS_ERR_WORKSPACE;
-  if (n_tok == 0) {
-    THANOS_CUDA(cudaMemsetAsync(workspace, 0, 16, static_cast<cudaStream_t>(stream)));
-    return THANOS_OK;
-  }
-  AdapterArgs a;
-  a.out = Y;
-  a.ldo = ldy;
-  a.in = X;
-  a.ldi = ldx;
-  a.W = W;
-  a.ldw = ldw;
-  a.A = A;
-  a.B = B;
-  a.index = index;
-  a.scale = scale;
-  a.V = n_adapters > 0 ? V : nullptr;
-  a.dtype = dtype;
-  a.T = n_tok;
-  a.c = c;
-  a.b = b;
-  a.n = n_adapters;
-  a.r = n_adapters > 0 ? r : 1;
-  return adapter_forward_impl(a, workspace, ws_bytes, static_cast<cudaStream_t>(stream));
+  return forward_call(Y, ldy, V, X, ldx, Weights{W, ldw, PackedWeights{}, false}, A, B, index, scale,
+                      dtype, n_tok, c, b, n_adapters, r, workspace, ws_bytes,
+                      static_cast<cudaStream_t>(stream));
 }
 
 thanos_status_t thanos_adapter_backward(void* dX, int64_t lddx, float* dA, float* dB,
@@ -132,55 +286,113 @@ thanos_status_t thanos_adapter_backward(void* dX, int64_t lddx, float* dA, float
                                         thanos_dtype_t dtype, int64_t n_tok, int64_t c, int64_t b,
                                         int64_t n_adapters, int32_t r, void* workspace,
                                         size_t ws_bytes, void* stream) {
-  const bool grads = dA != nullptr || dB != nullptr;
-  if (!W || (n_tok > 0 && !dY)) return THANOS_ERR_INVALID_ARG;
-  if (grads && (!dA || !dB || n_adapters == 0 || (n_tok > 0 && (!X || !V))))
-    return THANOS_ERR_INVALID_ARG;
-  if (n_adapters > 0 && (!A || !B || !scale || (n_tok > 0 && !index)))
-    return THANOS_ERR_INVALID_ARG;
-  THANOS_TRY(adapter_shape(n_tok, c, b, n_adapters, r, dtype));
-  if (lddy < c || ldw < b || (dX && lddx < b) || (grads && ldx < b)) return THANOS_ERR_SHAPE;
-  if (ldw % 8 || (grads && ldx % 8)) return THANOS_ERR_ALIGNMENT;
-  if (!aligned16(dX) || !aligned16(dA) || !aligned16(dB) || !aligned16(dY) || !aligned16(V) ||
-      !aligned16(X) || !aligned16(W) || !aligned16(A) || !aligned16(B) || !aligned4(index) ||
-      !aligned4(scale) || !aligned16(workspace))
-    return THANOS_ERR_ALIGNMENT;
-  if (!workspace ||
-      ws_bytes < thanos_adapter_workspace_bytes(1, n_tok, c, b, n_adapters, r, dtype))
-    return THANOS_ERR_WORKSPACE;
-  if (n_tok == 0) {
-    THANOS_CUDA(cudaMemsetAsync(workspace, 0, 16, static_cast<cudaStream_t>(stream)));
-    if (grads && !accumulate) {
-      const size_t nr = (size_t)n_adapters * (size_t)r;
-      THANOS_CUDA(cudaMemsetAsync(dA, 0, nr * (size_t)b * 4, static_cast<cudaStream_t>(stream)));
-      THANOS_CUDA(cudaMemsetAsync(dB, 0, nr * (size_t)c * 4, static_cast<cudaStream_t>(stream)));
-    }
-    return THANOS_OK;
-  }
+  return backward_call(dX, lddx, dA, dB, accumulate, dY, lddy, X, ldx, PackedActivations{}, false, V,
+                       Weights{W, ldw, PackedWeights{}, false}, A, B, index, scale, dtype, n_tok, c, b,
+                       n_adapters, r, workspace, ws_bytes, static_cast<cudaStream_t>(stream));
+}
+
+size_t thanos_adapter_packed_workspace_bytes(int32_t backward, int32_t packed_w, int32_t packed_x,
+                                             int64_t n_tok, int64_t c, int64_t b,
+                                             int64_t n_adapters, int32_t r, thanos_dtype_t dtype) {
+  if (adapter_shape(n_tok, c, b, n_adapters, r, dtype) != THANOS_OK) return 0;
   AdapterArgs a;
-  a.out = dX;
-  a.ldo = lddx;
-  a.in = dY;
-  a.ldi = lddy;
-  a.X = X;
-  a.ldx = ldx;
-  a.W = W;
-  a.ldw = ldw;
-  a.A = A;
-  a.B = B;
-  a.index = index;
-  a.scale = scale;
-  a.Vin = V;
-  a.dA = dA;
-  a.dB = dB;
-  a.accumulate = accumulate ? 1 : 0;
-  a.dtype = dtype;
   a.T = n_tok;
   a.c = c;
   a.b = b;
   a.n = n_adapters;
   a.r = n_adapters > 0 ? r : 1;
-  return adapter_backward_impl(a, workspace, ws_bytes, static_cast<cudaStream_t>(stream));
+  a.dtype = dtype;
+  if (!backward && packed_w && packed_few_tokens(a)) return packed_few_workspace_bytes(n_tok, a.r);
+  return round_up(thanos_adapter_workspace_bytes(backward, n_tok, c, b, n_adapters, r, dtype), 256) +
+         packed_extra_bytes(packed_w != 0, backward && packed_x, n_tok, c, b, dtype);
+}
+
+thanos_status_t thanos_adapter_forward_packed(void* Y, int64_t ldy, float* V, const void* X,
+                                              int64_t ldx, const uint8_t* w_codes, int64_t ldq,
+                                              const void* w_scales, int32_t group, const void* A,
+                                              const void* B, const int32_t* index,
+                                              const float* scale, thanos_dtype_t dtype,
+                                              int64_t n_tok, int64_t c, int64_t b,
+                                              int64_t n_adapters, int32_t r, void* workspace,
+                                              size_t ws_bytes, void* stream) {
+  const PackedWeights w{w_codes, ldq, static_cast<const __nv_bfloat16*>(w_scales), group};
+  return forward_call(Y, ldy, V, X, ldx, Weights{nullptr, 0, w, true}, A, B, index, scale, dtype,
+                      n_tok, c, b, n_adapters, r, workspace, ws_bytes,
+                      static_cast<cudaStream_t>(stream));
+}
+
+thanos_status_t thanos_adapter_backward_packed(void* dX, int64_t lddx, float* dA, float* dB,
+                                               int32_t accumulate, const void* dY, int64_t lddy,
+                                               const void* X, int64_t ldx, const uint8_t* x_exps,
+                                               int64_t lde, const float* V, const void* W,
+                                               int64_t ldw, const void* w_scales, int32_t group,
+                                               const void* A, const void* B, const int32_t* index,
+                                               const float* scale, thanos_dtype_t dtype,
+                                               int64_t n_tok, int64_t c, int64_t b,
+                                               int64_t n_adapters, int32_t r, void* workspace,
+                                               size_t ws_bytes, void* stream) {
+  Weights w{W, ldw, PackedWeights{}, false};
+  if (w_scales)
+    w = Weights{nullptr, 0,
+                PackedWeights{static_cast<const uint8_t*>(W), ldw,
+                              static_cast<const __nv_bfloat16*>(w_scales), group},
+                true};
+  PackedActivations x8;
+  if (x_exps) x8 = PackedActivations{static_cast<const int8_t*>(X), ldx, x_exps, lde};
+  return backward_call(dX, lddx, dA, dB, accumulate, dY, lddy, x_exps ? nullptr : X, ldx, x8,
+                       x_exps != nullptr, V, w, A, B, index, scale, dtype, n_tok, c, b, n_adapters, r,
+                       workspace, ws_bytes, static_cast<cudaStream_t>(stream));
+}
+
+thanos_status_t thanos_pack_weights(uint8_t* codes, int64_t ldq, void* scales, const void* W,
+                                    int64_t ldw, thanos_dtype_t dtype, int64_t c, int64_t b,
+                                    int32_t group, void* stream) {
+  if (!codes || !scales || !W) return THANOS_ERR_INVALID_ARG;
+  THANOS_TRY(adapter_shape(0, c, b, 0, 0, dtype));
+  const PackedWeights w{codes, ldq, static_cast<const __nv_bfloat16*>(scales), group};
+  if (ldw < b) return THANOS_ERR_SHAPE;
+  THANOS_TRY(packed_weights_ok(w, b));
+  if (ldw % 8 || !aligned16(W)) return THANOS_ERR_ALIGNMENT;
+  return pack_weights(codes, ldq, static_cast<__nv_bfloat16*>(scales), W, ldw, dtype, c, b, group,
+                      static_cast<cudaStream_t>(stream));
+}
+
+thanos_status_t thanos_unpack_weights(void* W, int64_t ldw, thanos_dtype_t dtype,
+                                      const uint8_t* codes, int64_t ldq, const void* scales,
+                                      int64_t c, int64_t b, int32_t group, void* stream) {
+  if (!codes || !scales || !W) return THANOS_ERR_INVALID_ARG;
+  THANOS_TRY(adapter_shape(0, c, b, 0, 0, dtype));
+  const PackedWeights w{codes, ldq, static_cast<const __nv_bfloat16*>(scales), group};
+  if (ldw < b) return THANOS_ERR_SHAPE;
+  THANOS_TRY(packed_weights_ok(w, b));
+  if (ldw % 8 || !aligned16(W)) return THANOS_ERR_ALIGNMENT;
+  return unpack_weights(W, ldw, dtype, w, c, b, static_cast<cudaStream_t>(stream));
+}
+
+thanos_status_t thanos_pack_activations(int8_t* codes, int64_t ldc, uint8_t* exps, int64_t lde,
+                                        const void* X, int64_t ldx, thanos_dtype_t dtype,
+                                        int64_t n_tok, int64_t b, void* stream) {
+  if (n_tok > 0 && (!codes || !exps || !X)) return THANOS_ERR_INVALID_ARG;
+  THANOS_TRY(adapter_shape(n_tok, 1, b, 0, 0, dtype));
+  if (ldx < b) return THANOS_ERR_SHAPE;
+  THANOS_TRY(packed_activations_ok(PackedActivations{codes, ldc, exps, lde}, b));
+  if (ldx % 8 || !aligned16(X)) return THANOS_ERR_ALIGNMENT;
+  if (n_tok == 0) return THANOS_OK;
+  return pack_activations(codes, ldc, exps, lde, X, ldx, dtype, n_tok, b,
+                          static_cast<cudaStream_t>(stream));
+}
+
+thanos_status_t thanos_unpack_activations(void* X, int64_t ldx, thanos_dtype_t dtype,
+                                          const int8_t* codes, int64_t ldc, const uint8_t* exps,
+                                          int64_t lde, int64_t n_tok, int64_t b, void* stream) {
+  if (n_tok > 0 && (!codes || !exps || !X)) return THANOS_ERR_INVALID_ARG;
+  THANOS_TRY(adapter_shape(n_tok, 1, b, 0, 0, dtype));
+  if (ldx < b) return THANOS_ERR_SHAPE;
+  THANOS_TRY(packed_activations_ok(PackedActivations{codes, ldc, exps, lde}, b));
+  if (ldx % 8 || !aligned16(X)) return THANOS_ERR_ALIGNMENT;
+  if (n_tok == 0) return THANOS_OK;
+  return unpack_activations(X, ldx, dtype, codes, ldc, exps, lde, n_tok, b,
+                            static_cast<cudaStream_t>(stream));
 }
 
 size_t thanos_orthogonal_workspace_bytes(int64_t batch, int64_t m, int64_t n) {

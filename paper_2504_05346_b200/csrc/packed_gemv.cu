@@ -1,0 +1,367 @@
+// The adapted projection of few tokens on 4-bit weights:
+//   Y[t] = X[t] w^T + s_i V[t] B_i^T,   V[t] = X[t] A_i^T,   w^ = code scale
+//
+// Bound by reading the weights, half a byte each.  A warp takes 16 MT rows and 8 NT tokens, and of k a
+// run of 64-column blocks; the warps of a CTA, and the CTAs of a cluster, split k and add up in a fixed
+// order (same inputs, same bits).  In a block a lane reads eight bytes of each of its rows, which are 16
+// consecutive columns: which k a lane holds at which place of the operand does not matter, as long as
+// both operands agree, so the activations are read the same way, straight from memory, once per warp.
+//   code   (nibble | 0x4300) is the bf16 number 128 + nibble; less 136 it is the code
+//   scale  the block's products are summed apart and multiplied by the row's scale in fp32: four
+//          multiplications per 16 x 8 tile and block instead of one per weight
+// fp32 activations go as three bf16 planes (cut, not rounded: 24 bits in all), three products.
+#include "packed.cuh"
+#include "proj_gemm.cuh"
+#include "tc_common.cuh"
+
+namespace thanos {
+namespace {
+
+using namespace tc;
+using bf16 = __nv_bfloat16;
+
+constexpr int GW = 8;            // warps of a CTA
+constexpr int GT = 32 * GW;
+constexpr int SHRINK_RANKS = 4;
+
+struct FewParams {
+  void* Y;
+  int64_t ldy;
+  const void* X;
+  int64_t ldx;
+  const uint8_t* codes;
+  int64_t ldq;
+  const bf16* scales;
+  const void* A;
+  const void* B;
+  const int32_t* index;
+  const float* scale;
+  float* V;
+  int32_t* status;
+  int c, b, T, n, r, shift, split;  // group = 2^shift columns
+};
+
+__device__ __forceinline__ int adapter_of(const int32_t* index, int t, int n) {
+  const int i = index[t];
+  return i >= 0 && i < n ? i : -1;
+}
+
+// ------------------------------------------------------------------------------ V[t] = X[t] A_i^T
+// A CTA per token and four ranks; clears the status word of the call.
+template <typename T>
+__global__ void __launch_bounds__(256) shrink_kernel(const FewParams p) {
+  __shared__ float sh[SHRINK_RANKS][8];
+  grid_dependents_launch();
+  const int tid = threadIdx.x;
+  if (blockIdx.x == 0 && tid == 0) *p.status = 0;
+  const int groups = (p.r + SHRINK_RANKS - 1) / SHRINK_RANKS;
+  const int t = blockIdx.x / groups, j0 = (blockIdx.x - t * groups) * SHRINK_RANKS;
+  const int i = adapter_of(p.index, t, p.n);
+  float s[SHRINK_RANKS] = {};
+  if (i >= 0) {
+    constexpr int VEC = 16 / sizeof(T);
+    const T* x = static_cast<const T*>(p.X) + (int64_t)t * p.ldx;
+    const T* a = static_cast<const T*>(p.A) + ((int64_t)i * p.r + j0) * p.b;
+    for (int k = tid * VEC; k < p.b; k += 256 * VEC) {
+      const uint4 xv = *reinterpret_cast<const uint4*>(x + k);
+      const uint32_t xw[4] = {xv.x, xv.y, xv.z, xv.w};
+#pragma unroll
+      for (int j = 0; j < SHRINK_RANKS; ++j) {
+        if (j0 + j < p.r) {
+          const uint4 av = *reinterpret_cast<const uint4*>(a + (int64_t)j * p.b + k);
+          const uint32_t aw[4] = {av.x, av.y, av.z, av.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if constexpr (VEC == 8) {
+              s[j] = fmaf(__uint_as_float(xw[e] << 16), __uint_as_float(aw[e] << 16), s[j]);
+              s[j] = fmaf(__uint_as_float(xw[e] & 0xFFFF0000u),
+                          __uint_as_float(aw[e] & 0xFFFF0000u), s[j]);
+            } else {
+              s[j] = fmaf(__uint_as_float(xw[e]), __uint_as_float(aw[e]), s[j]);
+            }
+          }
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < SHRINK_RANKS; ++j) {
+    for (int o = 16; o > 0; o >>= 1) s[j] += __shfl_xor_sync(0xffffffffu, s[j], o);
+    if ((tid & 31) == 0) sh[j][tid >> 5] = s[j];
+  }
+  __syncthreads();
+  if (tid < SHRINK_RANKS && j0 + tid < p.r) {
+    float v = 0.f;
+    for (int w = 0; w < 8; ++w) v += sh[tid][w];
+    p.V[(int64_t)t * p.r + j0 + tid] = v;
+  }
+}
+
+// --------------------------------------------------------------------------------------- products
+__device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0,
+                                          uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
+      "{%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// Codes j and j + 4 of a word of eight as a pair of bf16.
+__device__ __forceinline__ uint32_t codes_of(uint32_t w, int j) {
+  const uint32_t v = ((w >> (4 * j)) & 0x000F000Fu) | 0x43004300u;
+  const uint32_t off = 0x43084308u;  // 136
+  const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v),
+                                   *reinterpret_cast<const __nv_bfloat162*>(&off));
+  return *reinterpret_cast<const uint32_t*>(&d);
+}
+// Eight activations as four pairs (x_j, x_j+4), in one plane or in three.
+__device__ __forceinline__ void pairs_of(const bf16* x, bool in, uint32_t (&o)[1][4]) {
+  uint4 v = make_uint4(0u, 0u, 0u, 0u);
+  if (in) v = *reinterpret_cast<const uint4*>(x);
+  o[0][0] = __byte_perm(v.x, v.z, 0x5410);
+  o[0][1] = __byte_perm(v.x, v.z, 0x7632);
+  o[0][2] = __byte_perm(v.y, v.w, 0x5410);
+  o[0][3] = __byte_perm(v.y, v.w, 0x7632);
+}
+__device__ __forceinline__ void pairs_of(const float* x, bool in, uint32_t (&o)[3][4]) {
+  float v[8] = {};
+  if (in) {
+    const float4 a = reinterpret_cast<const float4*>(x)[0], b = reinterpret_cast<const float4*>(x)[1];
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
+    v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+  }
+  // The first plane keeps an infinity or NaN and the others are zero beside it: the codes are finite.
+#pragma unroll
+  for (int pl = 0; pl < 3; ++pl) {
+    uint32_t h[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const bool odd = pl == 0 && !isfinite(v[e]);
+      // cut to bf16; a NaN stays one
+      h[e] = odd && isnan(v[e]) ? 0x7FFF0000u : __float_as_uint(v[e]) & 0xFFFF0000u;
+      v[e] = odd ? 0.f : v[e] - __uint_as_float(h[e]);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[pl][j] = __byte_perm(h[j], h[j + 4], 0x7632);
+  }
+}
+
+__device__ __forceinline__ uint2 load_codes(const uint8_t* p) {
+  uint2 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];"
+               : "=r"(v.x), "=r"(v.y)
+               : "l"(p));
+  return v;
+}
+
+template <typename T, int MT, int NT>
+__global__ void __launch_bounds__(GT) few_kernel(const FewParams p) {
+  constexpr int PL = sizeof(T) == 2 ? 1 : 3;
+  constexpr int ROWS = 16 * MT, TOKS = 8 * NT;
+  __shared__ float part[GW][TOKS][ROWS + 4];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int g = lane >> 2, t4 = lane & 3;
+  const int S = p.split, rank = S > 1 ? (int)cluster_ctarank() : 0;
+  const int m0 = (int)(blockIdx.x / S) * ROWS, t0 = blockIdx.y * TOKS;
+  const int kb = (p.b + 63) >> 6, W = S * GW, w = rank * GW + warp;
+  const int kb0 = (int)((int64_t)kb * w / W), kb1 = (int)((int64_t)kb * (w + 1) / W);
+
+  const uint8_t* q[MT][2];
+  const bf16* sc[MT][2];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {  // rows beyond the last read the last one's codes
+      const int row = min(m0 + 16 * i + 8 * h + g, p.c - 1);
+      q[i][h] = p.codes + (int64_t)row * p.ldq + 8 * t4;
+      sc[i][h] = p.scales + row;
+    }
+  }
+  const T* x[NT];
+  bool tok[NT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    const int t = t0 + 8 * j + g;
+    tok[j] = t < p.T;
+    x[j] = static_cast<const T*>(p.X) + (int64_t)(tok[j] ? t : 0) * p.ldx;
+  }
+  float acc[MT][NT][4] = {};
+  uint2 next[MT][2];
+  auto fetch = [&](int k) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) next[i][h] = load_codes(q[i][h] + (int64_t)k * 32);
+  };
+  if (kb0 < kb1) fetch(kb0);
+  for (int k = kb0; k < kb1; ++k) {
+    uint2 now[MT][2];
+    float s[MT][2];
+    const int64_t sg = (int64_t)((k << 6) >> p.shift) * p.c;
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        now[i][h] = next[i][h];
+        s[i][h] = __uint_as_float(
+            ((uint32_t)__bfloat16_as_ushort(sc[i][h][sg]) & SCALE_BITS) << 16);
+      }
+    if (k + 1 < kb1) fetch(k + 1);
+    float sum[MT][NT][4] = {};
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {  // the lane's eight columns of the first, the second word
+      uint32_t xb[NT][PL][4];
+      const int col = 64 * k + 16 * t4 + 8 * half;
+#pragma unroll
+      for (int j = 0; j < NT; ++j) pairs_of(x[j] + col, tok[j] && col < p.b, xb[j]);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const uint32_t lo = half ? now[i][0].y : now[i][0].x, hi = half ? now[i][1].y : now[i][1].x;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const uint32_t a[4] = {codes_of(lo, 2 * u), codes_of(hi, 2 * u), codes_of(lo, 2 * u + 1),
+                                 codes_of(hi, 2 * u + 1)};
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int pl = PL - 1; pl >= 0; --pl)
+              mma_16816(sum[i][j], a, xb[j][pl][2 * u], xb[j][pl][2 * u + 1]);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(s[i][e >> 1], sum[i][j][e], acc[i][j][e]);
+  }
+  // ---- sums over the warps, then over the cluster's CTAs
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        part[warp][8 * j + 2 * t4 + (e & 1)][16 * i + g + 8 * (e >> 1)] = acc[i][j][e];
+  __syncthreads();
+  if (p.n > 0) grid_dependency_wait();
+  if (S > 1) {
+    for (int e = threadIdx.x; e < TOKS * ROWS; e += GT) {
+      const int t = e / ROWS, m = e % ROWS;
+      float v = 0.f;
+#pragma unroll
+      for (int u = 0; u < GW; ++u) v += part[u][t][m];
+      part[0][t][m] = v;
+    }
+    cluster_sync_all();
+  }
+  const uint32_t base = smem_u32(&part[0][0][0]);
+  for (int e = rank * GT + threadIdx.x; e < TOKS * ROWS; e += S * GT) {
+    const int t = e / ROWS, m = e % ROWS;
+    float v = 0.f;
+    if (S > 1) {
+      for (int u = 0; u < S; ++u) {
+        float z;
+        asm volatile("ld.shared::cluster.f32 %0, [%1];"
+                     : "=f"(z)
+                     : "r"(map_to_cta(base, u) + 4u * (uint32_t)(t * (ROWS + 4) + m))
+                     : "memory");
+        v += z;
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < GW; ++u) v += part[u][t][m];
+    }
+    const int row = m0 + m, at = t0 + t;
+    if (row >= p.c || at >= p.T) continue;
+    if (p.n > 0) {
+      const int i = p.index[at];
+      if (i >= 0 && i < p.n) {
+        const T* bw = static_cast<const T*>(p.B) + ((int64_t)i * p.c + row) * p.r;
+        const float* vt = p.V + (int64_t)at * p.r;
+        float d = 0.f;
+        for (int j = 0; j < p.r; ++j) d = fmaf(vt[j], to_float(bw[j]), d);
+        v = fmaf(p.scale[i], d, v);
+      } else if (i != -1 && row == 0) {
+        atomicCAS(p.status, 0, (int)THANOS_ERR_INVALID_ARG);
+      }
+    } else if (row == 0 && at == 0) {
+      *p.status = 0;
+    }
+    T* y = static_cast<T*>(p.Y) + (int64_t)at * p.ldy + row;
+    if constexpr (sizeof(T) == 2) *y = __float2bfloat16_rn(v);
+    else *y = v;
+  }
+  if (S > 1) cluster_sync_all();  // no CTA leaves while another reads its sums
+}
+
+template <typename T, int MT, int NT>
+thanos_status_t launch(FewParams p, cudaStream_t stream) {
+  const int64_t tiles = ceil_div(p.c, 16 * MT), blocks = ceil_div(p.b, 64);
+  const int64_t toks = ceil_div(p.T, 8 * NT);
+  // CTAs for two to an SM, as long as every warp has a block
+  int S = 1;
+  while (S < 8 && tiles * toks * S < 2 * NUM_SMS && blocks >= 2 * S * GW) S *= 2;
+  p.split = S;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(tiles * S), (unsigned)toks, 1);
+  cfg.blockDim = dim3(GT, 1, 1);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)S;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = p.n > 0 ? 2 : 1;
+  count_launch();
+  THANOS_CUDA(cudaLaunchKernelEx(&cfg, few_kernel<T, MT, NT>, p));
+  return THANOS_OK;
+}
+
+template <typename T>
+thanos_status_t forward_few(const FewParams& p, cudaStream_t stream) {
+  if (p.n > 0) {
+    shrink_kernel<T><<<(unsigned)(p.T * ceil_div(p.r, SHRINK_RANKS)), 256, 0, stream>>>(p);
+    THANOS_CHECK_LAUNCH();
+  }
+  if (p.T <= 8) return launch<T, 4, 1>(p, stream);
+  if (sizeof(T) == 4 || p.T <= 16) return launch<T, 2, 2>(p, stream);
+  return launch<T, 2, 4>(p, stream);
+}
+
+}  // namespace
+
+bool packed_few_tokens(const AdapterArgs& a) { return a.T <= (a.dtype == THANOS_BF16 ? 64 : 32); }
+
+size_t packed_few_workspace_bytes(int64_t T, int r) { return 256 + round_up((size_t)T * r * 4, 256); }
+
+thanos_status_t packed_forward_few(const AdapterArgs& a, const PackedWeights& w, void* workspace,
+                                   cudaStream_t stream) {
+  FewParams p = {};
+  p.Y = a.out;
+  p.ldy = a.ldo;
+  p.X = a.in;
+  p.ldx = a.ldi;
+  p.codes = w.codes;
+  p.ldq = w.ldq;
+  p.scales = w.scales;
+  p.A = a.A;
+  p.B = a.B;
+  p.index = a.index;
+  p.scale = a.scale;
+  p.status = static_cast<int32_t*>(workspace);
+  p.V = a.V ? a.V : reinterpret_cast<float*>(static_cast<char*>(workspace) + 256);
+  p.c = (int)a.c;
+  p.b = (int)a.b;
+  p.T = (int)a.T;
+  p.n = (int)a.n;
+  p.r = a.r;
+  p.shift = w.group == 64 ? 6 : 7;
+  return a.dtype == THANOS_BF16 ? forward_few<bf16>(p, stream) : forward_few<float>(p, stream);
+}
+
+}  // namespace thanos
