@@ -67,28 +67,38 @@ template <typename T>
 struct Row {
   static constexpr int VEC = 16 / sizeof(T);
   const T* z;
-  int V, shift, nv;
+  int V, shift, nv, first, last;  // vectors [first, last) are whole
   __device__ Row(const T* row, int V_) : z(row), V(V_) {
     shift = (int)((reinterpret_cast<uintptr_t>(row) & 15u) / sizeof(T));
     nv = (V + shift + VEC - 1) / VEC;
+    first = shift > 0 ? 1 : 0;
+    last = (V + shift) / VEC;
   }
   __device__ __forceinline__ int column(int v) const { return v * VEC - shift; }
-  __device__ __forceinline__ bool whole(int v) const {
-    return column(v) >= 0 && column(v) + VEC <= V;
-  }
+  __device__ __forceinline__ bool whole(int v) const { return v >= first && v < last; }
   __device__ __forceinline__ uint4 load(int v) const {  // whole(v)
-    return __ldg(reinterpret_cast<const uint4*>(z + column(v)));
+    return *reinterpret_cast<const uint4*>(z + column(v));  // dZ may be Z: no read-only load
   }
-  // Any vector, `fill` where the row has no value.
-  __device__ __forceinline__ void values(int v, float (&x)[VEC], float fill) const {
-    if (whole(v)) {
-      expand(load(v), x);
-    } else {
-      const int c = column(v);
+  // Any vector; what is not of the row is -infinity.
+  __device__ __noinline__ uint4 edge(int v) const {
+    uint32_t w[4];
+    const int c = column(v);
+    auto at = [&](int e) {
+      return c + e >= 0 && c + e < V ? __float_as_uint(to_float(z[c + e])) : 0xFF800000u;
+    };
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) x[e] = c + e >= 0 && c + e < V ? to_float(z[c + e]) : fill;
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (VEC == 8) w[e] = at(2 * e) >> 16 | at(2 * e + 1);
+      else w[e] = at(e);
     }
+    return make_uint4(w[0], w[1], w[2], w[3]);
   }
+  __device__ __forceinline__ uint4 any(int v) const { return whole(v) ? load(v) : edge(v); }
+  static __device__ __forceinline__ uint4 nothing() {
+    const uint32_t x = VEC == 8 ? 0xFF80FF80u : 0xFF800000u;
+    return make_uint4(x, x, x, x);
+  }
+  __device__ __forceinline__ void values(int v, float (&x)[VEC]) const { expand(any(v), x); }
   static __device__ __forceinline__ void expand(uint4 r, float (&x)[VEC]) {
     const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
@@ -131,6 +141,7 @@ __device__ __forceinline__ float value_of(uint32_t o) {
   if (o == 0xFFFFFFFFu) return NAN;
   return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o);
 }
+constexpr uint32_t NO_ORDER = 0x007FFFFFu;  // of -infinity: what is below is no number's
 // A logit and its column as one number: the larger is the more likely, equal ones by column.
 __device__ __forceinline__ uint64_t key_of(float x, int column) {
   return (uint64_t)order_of(x) << 32 | (uint32_t)~(uint32_t)column;
@@ -153,6 +164,21 @@ struct Sums {
     o.rebase(to);
     s += o.s;
     t += o.t;
+  }
+  // Over groups of 2 * from neighbouring lanes: one common largest first, then plain sums.
+  __device__ __forceinline__ void join(int from) {
+    float to = m;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+      if (o <= from) to = fmaxf(to, __shfl_xor_sync(0xffffffffu, to, o));
+    rebase(to);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      if (o <= from) {
+        s += __shfl_xor_sync(0xffffffffu, s, o);
+        t += __shfl_xor_sync(0xffffffffu, t, o);
+      }
+    }
   }
 };
 
@@ -186,33 +212,37 @@ __device__ __forceinline__ void take(Sums& a, const uint4 (&raw)[U], float& seen
   a.t += t0 + t1;
 }
 
+constexpr int PAIRS = LT / 2;
+
 struct Shared {
   Sums warp[LT / 32];
-  float seen[LT];
-  float bound;
-  int count, threads, n_threads;
+  __align__(16) uint32_t pair[PAIRS];
+  uint32_t bound, guess;
+  int count, n_threads;
   int who[LT];
   uint64_t list[CANDIDATES];
   uint64_t best[MAX_TOP];
 };
 
-// Columns of this CTA's vectors [v0, v1) with a logit whose order is >= lo, at most CANDIDATES of them
-// in list; the count may be larger.  Threads of `who` only, each of which holds every LT-th vector.
+// Columns of this CTA's vectors [v0, v1) with a logit >= bound, at most CANDIDATES of them in list; the
+// count may be larger.  Only the vectors of the threads in `who`, each of which holds every LT-th: so
+// many threads' vectors that every thread of the CTA looks at one or two.
 template <typename T>
-__device__ void collect(const Row<T>& row, int v0, int v1, uint32_t lo, int n_who, Shared& sh) {
+__device__ __forceinline__ void collect(const Row<T>& row, int v0, int v1, float bound, int n_who,
+                                        Shared& sh) {
   constexpr int VEC = Row<T>::VEC;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int i = warp; i < n_who; i += LT / 32) {
-    for (int v = v0 + sh.who[i] + LT * lane; v < v1; v += LT * 32) {
-      float x[VEC];
-      row.values(v, x, -INFINITY);
-      const int c = row.column(v);
+  const int turns = (v1 - v0 + LT - 1) / LT;
+  for (int i = threadIdx.x; i < n_who * turns; i += LT) {
+    const int w = i / turns, v = v0 + sh.who[w] + LT * (i - w * turns);
+    if (v >= v1) continue;
+    float x[VEC];
+    row.values(v, x);
+    const int c = row.column(v);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        if (c + e >= 0 && c + e < row.V && order_of(x[e]) >= lo) {
-          const int at = atomicAdd(&sh.count, 1);
-          if (at < CANDIDATES) sh.list[at] = key_of(x[e], c + e);
-        }
+    for (int e = 0; e < VEC; ++e) {
+      if (x[e] >= bound && c + e >= 0 && c + e < row.V) {
+        const int at = atomicAdd(&sh.count, 1);
+        if (at < CANDIDATES) sh.list[at] = key_of(x[e], c + e);
       }
     }
   }
@@ -221,7 +251,7 @@ __device__ void collect(const Row<T>& row, int v0, int v1, uint32_t lo, int n_wh
 // The slow way to the k largest, for rows of which more candidates pass than the list holds: the k-th
 // largest value bit by bit, then all that are larger, and of those that equal it the first ones.
 template <typename T>
-__device__ void select_slowly(const Row<T>& row, int v0, int v1, int k, uint32_t guess, Shared& sh) {
+__device__ __noinline__ void select_slowly(const Row<T>& row, int v0, int v1, int k, uint32_t guess, Shared& sh) {
   constexpr int VEC = Row<T>::VEC;
   const int tid = threadIdx.x, lane = tid & 31;
   auto count = [&](uint32_t lo) {  // logits whose order is >= lo
@@ -231,7 +261,7 @@ __device__ void select_slowly(const Row<T>& row, int v0, int v1, int k, uint32_t
     int n = 0;
     for (int v = v0 + tid; v < v1; v += LT) {
       float x[VEC];
-      row.values(v, x, -INFINITY);
+      row.values(v, x);
       const int c = row.column(v);
 #pragma unroll
       for (int e = 0; e < VEC; ++e)
@@ -243,16 +273,23 @@ __device__ void select_slowly(const Row<T>& row, int v0, int v1, int k, uint32_t
     return sh.count;
   };
   uint32_t kth = guess;
-  if (guess != 0xFFFFFFFFu && count(guess + 1u) >= k) {
+  if (count(guess) < k || (guess != 0xFFFFFFFFu && count(guess + 1u) >= k)) {
     kth = 0;
     for (int bit = 31; bit >= 0; --bit)
       if (count(kth | 1u << bit) >= k) kth |= 1u << bit;
   }
   __syncthreads();
   if (tid == 0) sh.count = 0;
-  sh.who[tid] = tid;
   __syncthreads();
-  if (kth != 0xFFFFFFFFu) collect(row, v0, v1, kth + 1u, LT, sh);  // fewer than k
+  for (int v = v0 + tid; v < v1; v += LT) {  // what is larger: fewer than k
+    float x[VEC];
+    row.values(v, x);
+    const int c = row.column(v);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e)
+      if (c + e >= 0 && c + e < row.V && order_of(x[e]) > kth)
+        sh.list[atomicAdd(&sh.count, 1)] = key_of(x[e], c + e);
+  }
   __syncthreads();
   if (tid < 32) {
     int have = sh.count;
@@ -262,7 +299,7 @@ __device__ void select_slowly(const Row<T>& row, int v0, int v1, int k, uint32_t
       const int mine = v + lane, c = row.column(mine);
       int n = 0;
       if (mine < v1) {
-        row.values(mine, x, -INFINITY);
+        row.values(mine, x);
 #pragma unroll
         for (int e = 0; e < VEC; ++e) n += c + e >= 0 && c + e < row.V && order_of(x[e]) == kth;
       }
@@ -295,6 +332,7 @@ __device__ void rank_list(Shared& sh, int n, int k) {
   for (int i = threadIdx.x; i < n; i += LT) {
     const uint64_t mine = sh.list[i];
     int before = 0;
+#pragma unroll 8
     for (int j = 0; j < n; ++j) before += sh.list[j] > mine ? 1 : 0;
     if (before < k) sh.best[before] = mine;
   }
@@ -330,92 +368,75 @@ __global__ void __launch_bounds__(LT) logprobs_kernel(const ForwardParams p) {
     if (target >= 0 && target < p.V) zt = to_float(row.z[target]);
   }
 
-  // ---- one pass over the row
+  // ---- one pass over the row, a batch of vectors ahead
   Sums a{-FLT_MAX, 0.f, 0.f};
   float seen = -INFINITY;
-  int v = v0 + tid;
-  if (v < v1 && !row.whole(v)) {  // the row's first vector, or its only one
-    float x[VEC];
-    row.values(v, x, -INFINITY);
-    uint4 w[1];
-    if constexpr (VEC == 8) {
-      uint32_t h[4];
+  uint4 next[U];
+  const int inner = min(v1, row.last);
+  auto fetch = [&](int v) {
+    if (v >= row.first && v + (U - 1) * LT < inner) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        h[e] = __float_as_uint(x[2 * e]) >> 16 | (__float_as_uint(x[2 * e + 1]) & 0xFFFF0000u);
-      w[0] = make_uint4(h[0], h[1], h[2], h[3]);
+      for (int u = 0; u < U; ++u) next[u] = row.load(v + u * LT);
     } else {
-      w[0] = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]),
-                        __float_as_uint(x[3]));
-    }
-    take<T, 1>(a, w, seen);
-    v += LT;
-  }
-  for (; v + (U - 1) * LT < v1 && row.whole(v + (U - 1) * LT); v += U * LT) {
-    uint4 w[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) w[u] = row.load(v + u * LT);
-    take<T, U>(a, w, seen);
-  }
-  for (; v < v1; v += LT) {
-    uint4 w[1];
-    if (row.whole(v)) {
-      w[0] = row.load(v);
-    } else {
-      float x[VEC];
-      row.values(v, x, -INFINITY);
-      if constexpr (VEC == 8) {
-        uint32_t h[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          h[e] = __float_as_uint(x[2 * e]) >> 16 | (__float_as_uint(x[2 * e + 1]) & 0xFFFF0000u);
-        w[0] = make_uint4(h[0], h[1], h[2], h[3]);
-      } else {
-        w[0] = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]),
-                          __float_as_uint(x[3]));
-      }
+      for (int u = 0; u < U; ++u)
+        next[u] = v + u * LT < v1 ? row.any(v + u * LT) : Row<T>::nothing();
     }
-    take<T, 1>(a, w, seen);
+  };
+  fetch(v0 + tid);
+  for (int v = v0 + tid; v < v1; v += U * LT) {
+    uint4 now[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) now[u] = next[u];
+    if (v + U * LT < v1) fetch(v + U * LT);
+    take<T, U>(a, now, seen);
   }
 
   // ---- sums of the CTA, in a fixed order
-  sh.seen[tid] = seen;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1)
-    a.merge(__shfl_xor_sync(0xffffffffu, a.m, o), __shfl_xor_sync(0xffffffffu, a.s, o),
-            __shfl_xor_sync(0xffffffffu, a.t, o));
+  const int k = p.k;
+  uint32_t two = 0;
+  if (k > 0) {
+    // the order of the largest of two threads' logits, with the pair's number in the low bits: all
+    // different, and no more than seven bits below what it stands for
+    two = order_of(fmaxf(seen, __shfl_xor_sync(0xffffffffu, seen, 1)));
+    if ((tid & 1) == 0) sh.pair[tid >> 1] = (two & ~(uint32_t)(PAIRS - 1)) | (uint32_t)(tid >> 1);
+  }
+  a.join(16);
   if (lane == 0) sh.warp[warp] = a;
   if (tid == 0) sh.count = sh.n_threads = 0;
   __syncthreads();
-  a = sh.warp[0];
-#pragma unroll
-  for (int w = 1; w < LT / 32; ++w) a.merge(sh.warp[w].m, sh.warp[w].s, sh.warp[w].t);
+  a = sh.warp[lane & (LT / 32 - 1)];
+  a.join(LT / 64);
 
   // ---- the k largest of the CTA
-  const int k = p.k;
   if (k > 0) {
     const int mine = min(p.V, row.column(v1)) - max(0, row.column(v0));  // logits of this slice
     const int want = min(k, mine);
-    // The want-th largest of the pairs' largest is no more than the want-th largest of all.
-    constexpr int PAIRS = LT / 2;
-    if (tid < PAIRS) {
-      const float x = fmaxf(sh.seen[2 * tid], sh.seen[2 * tid + 1]);
+    // The want-th largest of the pairs' largest is no more than the want-th largest of all.  Two
+    // threads to a pair, each of which compares it with half of the others.
+    {
+      const uint32_t x = sh.pair[tid >> 1];
+      const uint4* y = reinterpret_cast<const uint4*>(&sh.pair[(tid & 1) * (PAIRS / 2)]);
       int before = 0;
-      for (int j = 0; j < PAIRS; ++j) {
-        const float y = fmaxf(sh.seen[2 * j], sh.seen[2 * j + 1]);
-        before += y > x || (y == x && j < tid) ? 1 : 0;
+#pragma unroll
+      for (int j = 0; j < PAIRS / 8; ++j) {
+        const uint4 q = y[j];
+        before += (q.x > x) + (q.y > x) + (q.z > x) + (q.w > x);
       }
-      if (before == want - 1) sh.bound = x;
+      before += __shfl_xor_sync(0xffffffffu, before, 1);
+      if (before == want - 1) {
+        sh.bound = max(x & ~(uint32_t)(PAIRS - 1), NO_ORDER);
+        sh.guess = two;
+      }
     }
     __syncthreads();
-    const float bound = sh.bound;
-    if (sh.seen[tid] >= bound) sh.who[atomicAdd(&sh.n_threads, 1)] = tid;
+    const float bound = value_of(sh.bound);
+    if (seen >= bound) sh.who[atomicAdd(&sh.n_threads, 1)] = tid;
     __syncthreads();
-    const uint32_t lo = order_of(bound);
     const bool odd = isnan(a.s);  // a NaN is no thread's largest
-    if (!odd) collect(row, v0, v1, lo, sh.n_threads, sh);
+    if (!odd) collect(row, v0, v1, bound, sh.n_threads, sh);
     __syncthreads();
-    if (odd || sh.count > CANDIDATES) select_slowly(row, v0, v1, want, lo, sh);
+    if (odd || sh.count > CANDIDATES) select_slowly(row, v0, v1, want, sh.guess, sh);
     const int n = sh.count;
     rank_list(sh, n, k);
   }
@@ -490,7 +511,27 @@ __device__ __forceinline__ float from_float<float>(float x) { return x; }
 template <>
 __device__ __forceinline__ bf16 from_float<bf16>(float x) { return __float2bfloat16_rn(x); }
 
-template <typename T>
+// What a row's logits are turned into where nothing is asked of a column by name:
+//   y = 2^d (bend d + turn),   d = (z - m) log2(e) - log2 S,   bend = -g_H ln 2,  turn = -(G + g_H H)
+struct Slope {
+  float m, low, bend, turn;
+  __device__ __forceinline__ float operator()(float z) const {
+    const float d = max_nan(fmaf(z - m, LOG2E, low), FAR);
+    return ex2(d) * fmaf(bend, d, turn);
+  }
+  __device__ __forceinline__ void two(float& z0, float& z1) const {
+    float d0, d1;
+    unpack2(fma2(add2(pack2(z0, z1), pack2(-m, -m)), pack2(LOG2E, LOG2E), pack2(low, low)), d0, d1);
+    d0 = max_nan(d0, FAR);
+    d1 = max_nan(d1, FAR);
+    const uint64_t f = fma2(pack2(bend, bend), pack2(d0, d1), pack2(turn, turn));
+    unpack2(mul2(pack2(ex2(d0), ex2(d1)), f), z0, z1);
+  }
+};
+
+// NAMED: gradients of alternatives, whose columns are put right at the end; without them the thread that
+// holds the target's column does so on the way.
+template <typename T, bool NAMED>
 __global__ void __launch_bounds__(LT) logprobs_grad_kernel(const BackwardParams p) {
   constexpr int VEC = 16 / sizeof(T);
   __shared__ int at[MAX_TOP + 1];
@@ -503,19 +544,21 @@ __global__ void __launch_bounds__(LT) logprobs_grad_kernel(const BackwardParams 
   const int v0 = chunk * (LT * BU), v1 = min(row.nv, v0 + LT * BU);
   const bool same = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(row.z)) & 15u) == 0;
 
-  float x[BU][VEC];
+  uint4 raw[BU];
 #pragma unroll
   for (int u = 0; u < BU; ++u) {
     const int v = v0 + u * LT + tid;
-    if (v < v1) row.values(v, x[u], 0.f);
+    if (v < v1) raw[u] = row.any(v);
   }
   const float m = p.stats[2 * r], logS = p.stats[2 * r + 1];
   const float gh = p.dentropy ? p.dentropy[r] : 0.f, H = p.dentropy ? p.entropy[r] : 0.f;
   // G, and whether there is anything to pass on: every warp by itself
-  int64_t t = p.target ? p.target[r] : -1;
-  float G = t < 0 ? 0.f : t < p.V ? p.dlogp[r] : NAN;
+  const int64_t target = p.target ? p.target[r] : -1;
+  const float own = target < 0 ? 0.f : target < p.V ? p.dlogp[r] : NAN;
+  const int t = target >= 0 && target < p.V ? (int)target : -1;
+  float G = own;
   bool any = G != 0.f || gh != 0.f;
-  if (p.dtop) {
+  if constexpr (NAMED) {
     float sum = 0.f;
     bool some = false;
     for (int i = lane; i < p.k; i += 32) {
@@ -532,43 +575,46 @@ __global__ void __launch_bounds__(LT) logprobs_grad_kernel(const BackwardParams 
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     any = __any_sync(0xffffffffu, some) || any;
-    const float own = G;
     G += sum;
-    if (tid == 0) grad[0] = own;
-  } else if (tid == 0) {
-    grad[0] = G;
-  }
-  if (tid == 0) at[0] = t >= 0 && t < p.V ? (int)t : -1;
-  const bool none = m == -INFINITY;  // nothing was likely: no gradient
-  any = any && !none;
-  const int points = p.dtop ? p.k + 1 : 1;
-
-  auto slope = [&](float z) {  // of a column that nothing is asked of by name
-    const float lq = (z - m) - logS;
-    const float q = ex2(max_nan(lq * LOG2E, FAR));
-    return -q * fmaf(gh, max_nan(lq, FAR) + H, G);
-  };
-  __syncthreads();
-  // dZ may be Z: what the named columns hold is read before anything is written
-  float named = 0.f;
-  int where = -1;
-  if (any && tid < points) {
-    const int j = at[tid];
-    if (j >= 0 && j >= row.column(v0) && j < row.column(v1)) {
-      where = j;
-      named = slope(to_float(row.z[j]));
-      for (int i = 0; i < points; ++i) named += at[i] == j ? grad[i] : 0.f;
+    if (tid == 0) {
+      at[0] = t;
+      grad[0] = own;
     }
   }
-  __syncthreads();
+  any = any && m != -INFINITY;  // nothing was likely: no gradient
+  const Slope slope{m, -logS * LOG2E, -gh * LN2, -fmaf(gh, H, G)};
+  float named = 0.f;
+  int where = -1;
+  if constexpr (NAMED) {
+    __syncthreads();
+    // dZ may be Z: what the named columns hold is read before anything is written
+    if (any && tid <= p.k) {
+      const int j = at[tid];
+      if (j >= 0 && j >= row.column(v0) && j < row.column(v1)) {
+        where = j;
+        named = slope(to_float(row.z[j]));
+        for (int i = 0; i <= p.k; ++i) named += at[i] == j ? grad[i] : 0.f;
+      }
+    }
+    __syncthreads();
+  }
 #pragma unroll
   for (int u = 0; u < BU; ++u) {
     const int v = v0 + u * LT + tid;
     if (v >= v1) break;
     const int c = row.column(v);
     float y[VEC];
+    Row<T>::expand(raw[u], y);
+    const bool mine = !NAMED && any && t >= c && t < c + VEC;
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) y[e] = any ? slope(x[u][e]) : 0.f;
+    for (int e = 0; e < VEC; e += 2) {
+      if (any) slope.two(y[e], y[e + 1]);
+      else y[e] = y[e + 1] = 0.f;
+    }
+    if (mine) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) y[e] += c + e == t ? own : 0.f;
+    }
     if (same && row.whole(v)) {
       uint32_t w[4];
 #pragma unroll
@@ -587,8 +633,10 @@ __global__ void __launch_bounds__(LT) logprobs_grad_kernel(const BackwardParams 
         if (c + e >= 0 && c + e < p.V) out[c + e] = from_float<T>(y[e]);
     }
   }
-  __syncthreads();
-  if (where >= 0) out[where] = from_float<T>(named);
+  if constexpr (NAMED) {
+    __syncthreads();
+    if (where >= 0) out[where] = from_float<T>(named);
+  }
 }
 
 template <typename T>
@@ -644,7 +692,8 @@ thanos_status_t backward(const LogprobsGradArgs& a, cudaStream_t stream) {
   p.k = a.k;
   // a row that starts between two vectors has one more
   p.chunks = (int)ceil_div(ceil_div(a.V, VEC) + 1, LT * BU);
-  logprobs_grad_kernel<T><<<(unsigned)(a.T * p.chunks), LT, 0, stream>>>(p);
+  if (p.dtop) logprobs_grad_kernel<T, true><<<(unsigned)(a.T * p.chunks), LT, 0, stream>>>(p);
+  else logprobs_grad_kernel<T, false><<<(unsigned)(a.T * p.chunks), LT, 0, stream>>>(p);
   THANOS_CHECK_LAUNCH();
   return THANOS_OK;
 }
