@@ -20,6 +20,8 @@ using bf16 = __nv_bfloat16;
 constexpr int LT = 256;               // threads of a CTA
 constexpr int MAX_TOP = 64;
 constexpr int CANDIDATES = 512;       // >= 8 MAX_TOP: a cluster's lists
+constexpr int U = 4;                  // vectors of a thread's batch
+constexpr int QUARTERS = 4;           // a thread's batches in turn, each with a largest logit of its own
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 // Exponents are cut off here: 2^-10000 is zero, and zero times a finite number stays zero where the
 // entropy's sum meets a masked logit.
@@ -212,28 +214,28 @@ __device__ __forceinline__ void take(Sums& a, const uint4 (&raw)[U], float& seen
   a.t += t0 + t1;
 }
 
-constexpr int PAIRS = LT / 2;
-
 struct Shared {
   Sums warp[LT / 32];
-  __align__(16) uint32_t pair[PAIRS];
+  __align__(16) uint32_t bin[LT];
+  uint32_t exact[LT];
   uint32_t bound, guess;
-  int count, n_threads;
-  int who[LT];
+  int count, n_who;
+  uint16_t who[LT * QUARTERS];
   uint64_t list[CANDIDATES];
   uint64_t best[MAX_TOP];
 };
 
 // Columns of this CTA's vectors [v0, v1) with a logit >= bound, at most CANDIDATES of them in list; the
-// count may be larger.  Only the vectors of the threads in `who`, each of which holds every LT-th: so
-// many threads' vectors that every thread of the CTA looks at one or two.
+// count may be larger.  Only the batches of the quarters of threads in `who`.
 template <typename T>
 __device__ __forceinline__ void collect(const Row<T>& row, int v0, int v1, float bound, int n_who,
                                         Shared& sh) {
   constexpr int VEC = Row<T>::VEC;
-  const int turns = (v1 - v0 + LT - 1) / LT;
-  for (int i = threadIdx.x; i < n_who * turns; i += LT) {
-    const int w = i / turns, v = v0 + sh.who[w] + LT * (i - w * turns);
+  const int batches = (v1 - v0 + QUARTERS * U * LT - 1) / (QUARTERS * U * LT);
+  const int shift = batches > 1 ? 32 - __clz(batches - 1) : 0;
+  for (int i = threadIdx.x; i < (n_who * U) << shift; i += LT) {
+    const int w = sh.who[i / U >> shift], j = i / U & ((1 << shift) - 1);
+    const int v = v0 + w / QUARTERS + LT * (i % U + U * (w % QUARTERS + QUARTERS * j));
     if (v >= v1) continue;
     float x[VEC];
     row.values(v, x);
@@ -352,9 +354,7 @@ struct ForwardParams {
 };
 
 template <typename T>
-__global__ void __launch_bounds__(LT) logprobs_kernel(const ForwardParams p) {
-  constexpr int VEC = 16 / sizeof(T);
-  constexpr int U = 4;
+__global__ void __launch_bounds__(LT, 5) logprobs_kernel(const ForwardParams p) {
   __shared__ Shared sh;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int S = p.split, rank = S > 1 ? (int)cluster_ctarank() : 0;
@@ -368,42 +368,55 @@ __global__ void __launch_bounds__(LT) logprobs_kernel(const ForwardParams p) {
     if (target >= 0 && target < p.V) zt = to_float(row.z[target]);
   }
 
-  // ---- one pass over the row, a batch of vectors ahead
+  // ---- one pass over the row
   Sums a{-FLT_MAX, 0.f, 0.f};
-  float seen = -INFINITY;
-  uint4 next[U];
+  float seen[QUARTERS];
+#pragma unroll
+  for (int q = 0; q < QUARTERS; ++q) seen[q] = -INFINITY;
+  auto turn = [&]() {
+    const float first = seen[0];
+#pragma unroll
+    for (int q = 0; q + 1 < QUARTERS; ++q) seen[q] = seen[q + 1];
+    seen[QUARTERS - 1] = first;
+  };
+  int batch = 0;
   const int inner = min(v1, row.last);
-  auto fetch = [&](int v) {
+  for (int v = v0 + tid; v < v1; v += U * LT, ++batch) {
+    uint4 raw[U];
     if (v >= row.first && v + (U - 1) * LT < inner) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) next[u] = row.load(v + u * LT);
+      for (int u = 0; u < U; ++u) raw[u] = row.load(v + u * LT);
     } else {
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        next[u] = v + u * LT < v1 ? row.any(v + u * LT) : Row<T>::nothing();
+        raw[u] = v + u * LT < v1 ? row.any(v + u * LT) : Row<T>::nothing();
     }
-  };
-  fetch(v0 + tid);
-  for (int v = v0 + tid; v < v1; v += U * LT) {
-    uint4 now[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) now[u] = next[u];
-    if (v + U * LT < v1) fetch(v + U * LT);
-    take<T, U>(a, now, seen);
+    take<T, U>(a, raw, seen[0]);
+    turn();
   }
+  for (; batch % QUARTERS; ++batch) turn();
 
   // ---- sums of the CTA, in a fixed order
   const int k = p.k;
-  uint32_t two = 0;
+  // Bins of logits, each of as many threads as leave two bins for one alternative.  A bin stands for the
+  // order of its largest, with its own number in the low bits: all different, and no more than eight
+  // bits below what it stands for.
+  const int held = min(v1 - v0, LT);  // threads with a vector
+  int bins = 16;
+  while (bins < LT && bins * held < 2 * k * LT) bins *= 2;
+  const int wide = LT / bins;
   if (k > 0) {
-    // the order of the largest of two threads' logits, with the pair's number in the low bits: all
-    // different, and no more than seven bits below what it stands for
-    two = order_of(fmaxf(seen, __shfl_xor_sync(0xffffffffu, seen, 1)));
-    if ((tid & 1) == 0) sh.pair[tid >> 1] = (two & ~(uint32_t)(PAIRS - 1)) | (uint32_t)(tid >> 1);
+    float most = fmaxf(fmaxf(seen[0], seen[1]), fmaxf(seen[2], seen[3]));
+    for (int o = 1; o < wide; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+    if ((tid & (wide - 1)) == 0) {
+      const int bin = tid / wide;
+      sh.bin[bin] = (order_of(most) & ~(uint32_t)(LT - 1)) | (uint32_t)bin;
+      sh.exact[bin] = order_of(most);
+    }
   }
   a.join(16);
   if (lane == 0) sh.warp[warp] = a;
-  if (tid == 0) sh.count = sh.n_threads = 0;
+  if (tid == 0) sh.count = sh.n_who = 0;
   __syncthreads();
   a = sh.warp[lane & (LT / 32 - 1)];
   a.join(LT / 64);
@@ -412,29 +425,30 @@ __global__ void __launch_bounds__(LT) logprobs_kernel(const ForwardParams p) {
   if (k > 0) {
     const int mine = min(p.V, row.column(v1)) - max(0, row.column(v0));  // logits of this slice
     const int want = min(k, mine);
-    // The want-th largest of the pairs' largest is no more than the want-th largest of all.  Two
-    // threads to a pair, each of which compares it with half of the others.
-    {
-      const uint32_t x = sh.pair[tid >> 1];
-      const uint4* y = reinterpret_cast<const uint4*>(&sh.pair[(tid & 1) * (PAIRS / 2)]);
+    // The want-th largest of the bins is no more than the want-th largest of all.
+    if (tid < bins) {
+      const uint32_t x = sh.bin[tid];
+      const uint4* y = reinterpret_cast<const uint4*>(sh.bin);
       int before = 0;
-#pragma unroll
-      for (int j = 0; j < PAIRS / 8; ++j) {
+#pragma unroll 4
+      for (int j = 0; j < bins / 4; ++j) {
         const uint4 q = y[j];
         before += (q.x > x) + (q.y > x) + (q.z > x) + (q.w > x);
       }
-      before += __shfl_xor_sync(0xffffffffu, before, 1);
       if (before == want - 1) {
-        sh.bound = max(x & ~(uint32_t)(PAIRS - 1), NO_ORDER);
-        sh.guess = two;
+        sh.bound = max(x & ~(uint32_t)(LT - 1), NO_ORDER);
+        sh.guess = sh.exact[tid];
       }
     }
     __syncthreads();
     const float bound = value_of(sh.bound);
-    if (seen >= bound) sh.who[atomicAdd(&sh.n_threads, 1)] = tid;
+#pragma unroll
+    for (int q = 0; q < QUARTERS; ++q)
+      if (seen[q] >= bound)
+        sh.who[atomicAdd(&sh.n_who, 1)] = (uint16_t)(tid * QUARTERS + q);
     __syncthreads();
     const bool odd = isnan(a.s);  // a NaN is no thread's largest
-    if (!odd) collect(row, v0, v1, bound, sh.n_threads, sh);
+    if (!odd) collect(row, v0, v1, bound, sh.n_who, sh);
     __syncthreads();
     if (odd || sh.count > CANDIDATES) select_slowly(row, v0, v1, want, sh.guess, sh);
     const int n = sh.count;
