@@ -2,8 +2,8 @@
 //   Y[t] = X[t] w^T + s_i V[t] B_i^T,   V[t] = X[t] A_i^T,   w^ = code scale
 //
 // Bound by reading the weights, half a byte each.  A warp takes 16 MT rows and 8 NT tokens, and of k a
-// run of 64-column blocks; the warps of a CTA, and the CTAs of a cluster, split k and add up in a fixed
-// order (same inputs, same bits).  In a block a lane reads eight bytes of each of its rows, which are 16
+// run of 64-column blocks; the warps of a CTA split k and add up in a fixed order (same inputs, same
+// bits).  In a block a lane reads eight bytes of each of its rows, which are 16
 // consecutive columns: which k a lane holds at which place of the operand does not matter, as long as
 // both operands agree, so the activations are read the same way, straight from memory, once per warp.
 //   code   (nibble | 0x4300) is the bf16 number 128 + nibble; less 136 it is the code
@@ -38,7 +38,7 @@ struct FewParams {
   const float* scale;
   float* V;
   int32_t* status;
-  int c, b, T, n, r, shift, split;  // group = 2^shift columns
+  int c, b, T, n, r, shift;  // group = 2^shift columns
 };
 
 __device__ __forceinline__ int adapter_of(const int32_t* index, int t, int n) {
@@ -114,36 +114,69 @@ __device__ __forceinline__ uint32_t codes_of(uint32_t w, int j) {
                                    *reinterpret_cast<const __nv_bfloat162*>(&off));
   return *reinterpret_cast<const uint32_t*>(&d);
 }
-// Eight activations as four pairs (x_j, x_j+4), in one plane or in three.
-__device__ __forceinline__ void pairs_of(const bf16* x, bool in, uint32_t (&o)[1][4]) {
-  uint4 v = make_uint4(0u, 0u, 0u, 0u);
-  if (in) v = *reinterpret_cast<const uint4*>(x);
-  o[0][0] = __byte_perm(v.x, v.z, 0x5410);
-  o[0][1] = __byte_perm(v.x, v.z, 0x7632);
-  o[0][2] = __byte_perm(v.y, v.w, 0x5410);
-  o[0][3] = __byte_perm(v.y, v.w, 0x7632);
-}
-__device__ __forceinline__ void pairs_of(const float* x, bool in, uint32_t (&o)[3][4]) {
-  float v[8] = {};
-  if (in) {
-    const float4 a = reinterpret_cast<const float4*>(x)[0], b = reinterpret_cast<const float4*>(x)[1];
-    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
-    v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+// Eight activations, and as four pairs (x_j, x_j+4) in one plane or in three.
+template <typename T>
+struct Vec8;
+template <>
+struct Vec8<bf16> {
+  uint4 v;
+  __device__ __forceinline__ void load(const bf16* x, bool in) {
+    v = in ? *reinterpret_cast<const uint4*>(x) : make_uint4(0u, 0u, 0u, 0u);
+  }
+  __device__ __forceinline__ void pairs(uint32_t (&o)[1][4]) const {
+    o[0][0] = __byte_perm(v.x, v.z, 0x5410);
+    o[0][1] = __byte_perm(v.x, v.z, 0x7632);
+    o[0][2] = __byte_perm(v.y, v.w, 0x5410);
+    o[0][3] = __byte_perm(v.y, v.w, 0x7632);
+  }
+};
+template <>
+struct Vec8<float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* x, bool in) {
+    const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+    a = in ? reinterpret_cast<const float4*>(x)[0] : zero;
+    b = in ? reinterpret_cast<const float4*>(x)[1] : zero;
   }
   // The first plane keeps an infinity or NaN and the others are zero beside it: the codes are finite.
+  __device__ __forceinline__ void pairs(uint32_t (&o)[3][4]) const {
+    float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
-  for (int pl = 0; pl < 3; ++pl) {
-    uint32_t h[8];
+    for (int pl = 0; pl < 3; ++pl) {
+      uint32_t h[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const bool odd = pl == 0 && !isfinite(v[e]);
-      // cut to bf16; a NaN stays one
-      h[e] = odd && isnan(v[e]) ? 0x7FFF0000u : __float_as_uint(v[e]) & 0xFFFF0000u;
-      v[e] = odd ? 0.f : v[e] - __uint_as_float(h[e]);
+      for (int e = 0; e < 8; ++e) {
+        const bool odd = pl == 0 && !isfinite(v[e]);
+        // cut to bf16; a NaN stays one
+        h[e] = odd && isnan(v[e]) ? 0x7FFF0000u : __float_as_uint(v[e]) & 0xFFFF0000u;
+        v[e] = odd ? 0.f : v[e] - __uint_as_float(h[e]);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[pl][j] = __byte_perm(h[j], h[j + 4], 0x7632);
     }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) o[pl][j] = __byte_perm(h[j], h[j + 4], 0x7632);
   }
+};
+
+// y of one row and token: the adapter's part, and the status word where there is nobody else to write it.
+template <typename T>
+__device__ __forceinline__ void finish(const FewParams& p, int row, int at, float v) {
+  if (p.n > 0) {
+    const int i = p.index[at];
+    if (i >= 0 && i < p.n) {
+      const T* bw = static_cast<const T*>(p.B) + ((int64_t)i * p.c + row) * p.r;
+      const float* vt = p.V + (int64_t)at * p.r;
+      float d = 0.f;
+      for (int j = 0; j < p.r; ++j) d = fmaf(vt[j], to_float(bw[j]), d);
+      v = fmaf(p.scale[i], d, v);
+    } else if (i != -1 && row == 0) {
+      atomicCAS(p.status, 0, (int)THANOS_ERR_INVALID_ARG);
+    }
+  } else if (row == 0 && at == 0) {
+    *p.status = 0;
+  }
+  T* y = static_cast<T*>(p.Y) + (int64_t)at * p.ldy + row;
+  if constexpr (sizeof(T) == 2) *y = __float2bfloat16_rn(v);
+  else *y = v;
 }
 
 __device__ __forceinline__ uint2 load_codes(const uint8_t* p) {
@@ -154,17 +187,17 @@ __device__ __forceinline__ uint2 load_codes(const uint8_t* p) {
   return v;
 }
 
-template <typename T, int MT, int NT>
+// UB: blocks whose loads are in flight together.
+template <typename T, int MT, int NT, int UB>
 __global__ void __launch_bounds__(GT) few_kernel(const FewParams p) {
   constexpr int PL = sizeof(T) == 2 ? 1 : 3;
   constexpr int ROWS = 16 * MT, TOKS = 8 * NT;
   __shared__ float part[GW][TOKS][ROWS + 4];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = lane >> 2, t4 = lane & 3;
-  const int S = p.split, rank = S > 1 ? (int)cluster_ctarank() : 0;
-  const int m0 = (int)(blockIdx.x / S) * ROWS, t0 = blockIdx.y * TOKS;
-  const int kb = (p.b + 63) >> 6, W = S * GW, w = rank * GW + warp;
-  const int kb0 = (int)((int64_t)kb * w / W), kb1 = (int)((int64_t)kb * (w + 1) / W);
+  const int m0 = blockIdx.x * ROWS, t0 = blockIdx.y * TOKS;
+  const int kb = (p.b + 63) >> 6;
+  const int kb0 = kb * warp / GW, kb1 = kb * (warp + 1) / GW;
 
   const uint8_t* q[MT][2];
   const bf16* sc[MT][2];
@@ -183,60 +216,67 @@ __global__ void __launch_bounds__(GT) few_kernel(const FewParams p) {
   for (int j = 0; j < NT; ++j) {
     const int t = t0 + 8 * j + g;
     tok[j] = t < p.T;
-    x[j] = static_cast<const T*>(p.X) + (int64_t)(tok[j] ? t : 0) * p.ldx;
+    x[j] = static_cast<const T*>(p.X) + (int64_t)(tok[j] ? t : 0) * p.ldx + 16 * t4;
   }
   float acc[MT][NT][4] = {};
-  uint2 next[MT][2];
-  auto fetch = [&](int k) {
+  for (int k0 = kb0; k0 < kb1; k0 += UB) {
+    uint2 w[UB][MT][2];
+    uint32_t s[UB][MT][2];
+    Vec8<T> xr[UB][NT][2];
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+    for (int u = 0; u < UB; ++u) {
+      const int k = min(k0 + u, kb1 - 1);  // one block more than there are is read again, for nothing
+      const int64_t sg = (int64_t)((k << 6) >> p.shift) * p.c;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) next[i][h] = load_codes(q[i][h] + (int64_t)k * 32);
-  };
-  if (kb0 < kb1) fetch(kb0);
-  for (int k = kb0; k < kb1; ++k) {
-    uint2 now[MT][2];
-    float s[MT][2];
-    const int64_t sg = (int64_t)((k << 6) >> p.shift) * p.c;
+      for (int i = 0; i < MT; ++i)
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        now[i][h] = next[i][h];
-        s[i][h] = __uint_as_float(
-            ((uint32_t)__bfloat16_as_ushort(sc[i][h][sg]) & SCALE_BITS) << 16);
-      }
-    if (k + 1 < kb1) fetch(k + 1);
-    float sum[MT][NT][4] = {};
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {  // the lane's eight columns of the first, the second word
-      uint32_t xb[NT][PL][4];
-      const int col = 64 * k + 16 * t4 + 8 * half;
-#pragma unroll
-      for (int j = 0; j < NT; ++j) pairs_of(x[j] + col, tok[j] && col < p.b, xb[j]);
-#pragma unroll
-      for (int i = 0; i < MT; ++i) {
-        const uint32_t lo = half ? now[i][0].y : now[i][0].x, hi = half ? now[i][1].y : now[i][1].x;
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const uint32_t a[4] = {codes_of(lo, 2 * u), codes_of(hi, 2 * u), codes_of(lo, 2 * u + 1),
-                                 codes_of(hi, 2 * u + 1)};
-#pragma unroll
-          for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int pl = PL - 1; pl >= 0; --pl)
-              mma_16816(sum[i][j], a, xb[j][pl][2 * u], xb[j][pl][2 * u + 1]);
+        for (int h = 0; h < 2; ++h) {
+          w[u][i][h] = load_codes(q[i][h] + (int64_t)k * 32);
+          s[u][i][h] = __bfloat16_as_ushort(sc[i][h][sg]);
         }
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
 #pragma unroll
       for (int j = 0; j < NT; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(s[i][e >> 1], sum[i][j][e], acc[i][j][e]);
+        for (int half = 0; half < 2; ++half)
+          xr[u][j][half].load(x[j] + 64 * k + 8 * half,
+                              tok[j] && 64 * k + 16 * t4 + 8 * half < p.b);
+    }
+#pragma unroll
+    for (int u = 0; u < UB; ++u) {
+      if (k0 + u >= kb1) break;
+      float sum[MT][NT][4] = {};
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {  // the lane's eight columns of the first, the second word
+        uint32_t xb[NT][PL][4];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) xr[u][j][half].pairs(xb[j]);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          const uint32_t lo = half ? w[u][i][0].y : w[u][i][0].x;
+          const uint32_t hi = half ? w[u][i][1].y : w[u][i][1].x;
+#pragma unroll
+          for (int v = 0; v < 2; ++v) {
+            const uint32_t a[4] = {codes_of(lo, 2 * v), codes_of(hi, 2 * v), codes_of(lo, 2 * v + 1),
+                                   codes_of(hi, 2 * v + 1)};
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+              for (int pl = PL - 1; pl >= 0; --pl)
+                mma_16816(sum[i][j], a, xb[j][pl][2 * v], xb[j][pl][2 * v + 1]);
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            acc[i][j][e] = fmaf(__uint_as_float((s[u][i][e >> 1] & SCALE_BITS) << 16), sum[i][j][e],
+                                acc[i][j][e]);
+    }
   }
-  // ---- sums over the warps, then over the cluster's CTAs
+  // ---- sums over the warps
 #pragma unroll
   for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -246,79 +286,29 @@ __global__ void __launch_bounds__(GT) few_kernel(const FewParams p) {
         part[warp][8 * j + 2 * t4 + (e & 1)][16 * i + g + 8 * (e >> 1)] = acc[i][j][e];
   __syncthreads();
   if (p.n > 0) grid_dependency_wait();
-  if (S > 1) {
-    for (int e = threadIdx.x; e < TOKS * ROWS; e += GT) {
-      const int t = e / ROWS, m = e % ROWS;
-      float v = 0.f;
-#pragma unroll
-      for (int u = 0; u < GW; ++u) v += part[u][t][m];
-      part[0][t][m] = v;
-    }
-    cluster_sync_all();
-  }
-  const uint32_t base = smem_u32(&part[0][0][0]);
-  for (int e = rank * GT + threadIdx.x; e < TOKS * ROWS; e += S * GT) {
+  for (int e = threadIdx.x; e < TOKS * ROWS; e += GT) {
     const int t = e / ROWS, m = e % ROWS;
     float v = 0.f;
-    if (S > 1) {
-      for (int u = 0; u < S; ++u) {
-        float z;
-        asm volatile("ld.shared::cluster.f32 %0, [%1];"
-                     : "=f"(z)
-                     : "r"(map_to_cta(base, u) + 4u * (uint32_t)(t * (ROWS + 4) + m))
-                     : "memory");
-        v += z;
-      }
-    } else {
 #pragma unroll
-      for (int u = 0; u < GW; ++u) v += part[u][t][m];
-    }
+    for (int u = 0; u < GW; ++u) v += part[u][t][m];
     const int row = m0 + m, at = t0 + t;
-    if (row >= p.c || at >= p.T) continue;
-    if (p.n > 0) {
-      const int i = p.index[at];
-      if (i >= 0 && i < p.n) {
-        const T* bw = static_cast<const T*>(p.B) + ((int64_t)i * p.c + row) * p.r;
-        const float* vt = p.V + (int64_t)at * p.r;
-        float d = 0.f;
-        for (int j = 0; j < p.r; ++j) d = fmaf(vt[j], to_float(bw[j]), d);
-        v = fmaf(p.scale[i], d, v);
-      } else if (i != -1 && row == 0) {
-        atomicCAS(p.status, 0, (int)THANOS_ERR_INVALID_ARG);
-      }
-    } else if (row == 0 && at == 0) {
-      *p.status = 0;
-    }
-    T* y = static_cast<T*>(p.Y) + (int64_t)at * p.ldy + row;
-    if constexpr (sizeof(T) == 2) *y = __float2bfloat16_rn(v);
-    else *y = v;
+    if (row < p.c && at < p.T) finish<T>(p, row, at, v);
   }
-  if (S > 1) cluster_sync_all();  // no CTA leaves while another reads its sums
 }
 
-template <typename T, int MT, int NT>
-thanos_status_t launch(FewParams p, cudaStream_t stream) {
-  const int64_t tiles = ceil_div(p.c, 16 * MT), blocks = ceil_div(p.b, 64);
-  const int64_t toks = ceil_div(p.T, 8 * NT);
-  // CTAs for two to an SM, as long as every warp has a block
-  int S = 1;
-  while (S < 8 && tiles * toks * S < 2 * NUM_SMS && blocks >= 2 * S * GW) S *= 2;
-  p.split = S;
+template <typename T, int MT, int NT, int UB>
+thanos_status_t launch(const FewParams& p, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(tiles * S), (unsigned)toks, 1);
+  cfg.gridDim = dim3((unsigned)ceil_div(p.c, 16 * MT), (unsigned)ceil_div(p.T, 8 * NT), 1);
   cfg.blockDim = dim3(GT, 1, 1);
   cfg.stream = stream;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = (unsigned)S;
-  attr[0].val.clusterDim.y = 1;
-  attr[0].val.clusterDim.z = 1;
-  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = p.n > 0 ? 2 : 1;
+  cfg.numAttrs = p.n > 0 ? 1 : 0;
   count_launch();
-  THANOS_CUDA(cudaLaunchKernelEx(&cfg, few_kernel<T, MT, NT>, p));
+  THANOS_CUDA(cudaLaunchKernelEx(&cfg, few_kernel<T, MT, NT, UB>, p));
   return THANOS_OK;
 }
 
@@ -328,9 +318,14 @@ thanos_status_t forward_few(const FewParams& p, cudaStream_t stream) {
     shrink_kernel<T><<<(unsigned)(p.T * ceil_div(p.r, SHRINK_RANKS)), 256, 0, stream>>>(p);
     THANOS_CHECK_LAUNCH();
   }
-  if (p.T <= 8) return launch<T, 4, 1>(p, stream);
-  if (sizeof(T) == 4 || p.T <= 16) return launch<T, 2, 2>(p, stream);
-  return launch<T, 2, 4>(p, stream);
+  if constexpr (sizeof(T) == 4) {
+    if (p.T <= 8) return launch<T, 1, 1, 2>(p, stream);
+    return launch<T, 2, 2, 1>(p, stream);
+  } else {
+    if (p.T <= 8) return launch<T, 1, 1, 4>(p, stream);
+    if (p.T <= 16) return launch<T, 2, 2, 2>(p, stream);
+    return launch<T, 2, 4, 1>(p, stream);
+  }
 }
 
 }  // namespace
