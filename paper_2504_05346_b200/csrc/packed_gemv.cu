@@ -10,36 +10,14 @@
 //   scale  the block's products are summed apart and multiplied by the row's scale in fp32: four
 //          multiplications per 16 x 8 tile and block instead of one per weight
 // fp32 activations go as three bf16 planes (cut, not rounded: 24 bits in all), three products.
-#include "packed.cuh"
-#include "proj_gemm.cuh"
-#include "tc_common.cuh"
+#include "packed_few.cuh"
 
 namespace thanos {
 namespace {
 
-using namespace tc;
-using bf16 = __nv_bfloat16;
-
 constexpr int GW = 8;            // warps of a CTA
 constexpr int GT = 32 * GW;
 constexpr int SHRINK_RANKS = 4;
-
-struct FewParams {
-  void* Y;
-  int64_t ldy;
-  const void* X;
-  int64_t ldx;
-  const uint8_t* codes;
-  int64_t ldq;
-  const bf16* scales;
-  const void* A;
-  const void* B;
-  const int32_t* index;
-  const float* scale;
-  float* V;
-  int32_t* status;
-  int c, b, T, n, r, shift;  // group = 2^shift columns
-};
 
 __device__ __forceinline__ int adapter_of(const int32_t* index, int t, int n) {
   const int i = index[t];
@@ -157,28 +135,6 @@ struct Vec8<float> {
   }
 };
 
-// y of one row and token: the adapter's part, and the status word where there is nobody else to write it.
-template <typename T>
-__device__ __forceinline__ void finish(const FewParams& p, int row, int at, float v) {
-  if (p.n > 0) {
-    const int i = p.index[at];
-    if (i >= 0 && i < p.n) {
-      const T* bw = static_cast<const T*>(p.B) + ((int64_t)i * p.c + row) * p.r;
-      const float* vt = p.V + (int64_t)at * p.r;
-      float d = 0.f;
-      for (int j = 0; j < p.r; ++j) d = fmaf(vt[j], to_float(bw[j]), d);
-      v = fmaf(p.scale[i], d, v);
-    } else if (i != -1 && row == 0) {
-      atomicCAS(p.status, 0, (int)THANOS_ERR_INVALID_ARG);
-    }
-  } else if (row == 0 && at == 0) {
-    *p.status = 0;
-  }
-  T* y = static_cast<T*>(p.Y) + (int64_t)at * p.ldy + row;
-  if constexpr (sizeof(T) == 2) *y = __float2bfloat16_rn(v);
-  else *y = v;
-}
-
 __device__ __forceinline__ uint2 load_codes(const uint8_t* p) {
   uint2 v;
   asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];"
@@ -193,6 +149,7 @@ __global__ void __launch_bounds__(GT) few_kernel(const FewParams p) {
   constexpr int PL = sizeof(T) == 2 ? 1 : 3;
   constexpr int ROWS = 16 * MT, TOKS = 8 * NT;
   __shared__ float part[GW][TOKS][ROWS + 4];
+  if (p.n == 0 && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.status = 0;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = lane >> 2, t4 = lane & 3;
   const int m0 = blockIdx.x * ROWS, t0 = blockIdx.y * TOKS;
@@ -323,14 +280,13 @@ thanos_status_t forward_few(const FewParams& p, cudaStream_t stream) {
     return launch<T, 2, 2, 1>(p, stream);
   } else {
     if (p.T <= 8) return launch<T, 1, 1, 4>(p, stream);
-    if (p.T <= 16) return launch<T, 2, 2, 2>(p, stream);
-    return launch<T, 2, 4, 1>(p, stream);
+    return packed_tiles(p, stream);
   }
 }
 
 }  // namespace
 
-bool packed_few_tokens(const AdapterArgs& a) { return a.T <= (a.dtype == THANOS_BF16 ? 64 : 32); }
+bool packed_few_tokens(const AdapterArgs& a) { return a.T <= (a.dtype == THANOS_BF16 ? 256 : 32); }
 
 size_t packed_few_workspace_bytes(int64_t T, int r) { return 256 + round_up((size_t)T * r * 4, 256); }
 
