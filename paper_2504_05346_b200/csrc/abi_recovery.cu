@@ -94,11 +94,6 @@ size_t unpacked_bytes(int64_t rows, int64_t b, thanos_dtype_t dtype) {
                   256);
 }
 
-// What a call on packed operands needs beside what the call itself does.
-size_t packed_extra_bytes(bool w, bool x, int64_t T, int64_t c, int64_t b, thanos_dtype_t dtype) {
-  return (w ? unpacked_bytes(c, b, dtype) : 0) + (x ? unpacked_bytes(T, b, dtype) : 0);
-}
-
 // Where W is: as it is, or packed (W null).
 struct Weights {
   const void* W;
@@ -196,11 +191,10 @@ thanos_status_t backward_call(void* dX, int64_t lddx, float* dA, float* dB, int3
       !aligned16(X) || !aligned16(A) || !aligned16(B) || !aligned4(index) || !aligned4(scale) ||
       !aligned16(workspace))
     return THANOS_ERR_ALIGNMENT;
-  const bool packed = w.is_packed || x_packed;
   const size_t need =
-      packed ? thanos_adapter_packed_workspace_bytes(1, w.is_packed, x_packed, n_tok, c, b, n_adapters,
-                                                     r, dtype)
-             : thanos_adapter_workspace_bytes(1, n_tok, c, b, n_adapters, r, dtype);
+      w.is_packed
+          ? thanos_adapter_packed_workspace_bytes(1, 1, x_packed, n_tok, c, b, n_adapters, r, dtype)
+          : thanos_adapter_workspace_bytes(1, n_tok, c, b, n_adapters, r, dtype);
   if (!workspace || ws_bytes < need) return THANOS_ERR_WORKSPACE;
   if (n_tok == 0) {
     THANOS_CUDA(cudaMemsetAsync(workspace, 0, 16, stream));
@@ -234,24 +228,18 @@ thanos_status_t backward_call(void* dX, int64_t lddx, float* dA, float* dB, int3
   a.b = b;
   a.n = n_adapters;
   a.r = n_adapters > 0 ? r : 1;
-  if (packed) {
-    size_t at = need - packed_extra_bytes(w.is_packed, x_packed, n_tok, c, b, dtype);
-    ws_bytes = at;
-    const int64_t ld = (int64_t)round_up((size_t)b, PACKED_LINE);
-    if (w.is_packed) {
-      void* full = static_cast<char*>(workspace) + at;
-      at += unpacked_bytes(c, b, dtype);
-      a.W = full;
-      a.ldw = ld;
-      if (dX) THANOS_TRY(unpack_weights(full, ld, dtype, w.packed, c, b, stream));
-    }
-    if (x_packed && grads) {
-      void* full = static_cast<char*>(workspace) + at;
-      a.X = full;
-      a.ldx = ld;
-      THANOS_TRY(unpack_activations(full, ld, dtype, x8.codes, x8.ldc, x8.exps, x8.lde, n_tok, b,
-                                    stream));
-    }
+  if (x_packed) {
+    a.X8 = x8.codes;
+    a.ldx8 = x8.ldc;
+    a.exps = x8.exps;
+    a.lde = x8.lde;
+  }
+  if (w.is_packed) {
+    ws_bytes = need - unpacked_bytes(c, b, dtype);
+    void* full = static_cast<char*>(workspace) + ws_bytes;
+    a.W = full;
+    a.ldw = (int64_t)round_up((size_t)b, PACKED_LINE);
+    if (dX) THANOS_TRY(unpack_weights(full, a.ldw, dtype, w.packed, c, b, stream));
   }
   return adapter_backward_impl(a, workspace, ws_bytes, stream);
 }
@@ -291,7 +279,7 @@ thanos_status_t thanos_adapter_backward(void* dX, int64_t lddx, float* dA, float
                        n_adapters, r, workspace, ws_bytes, static_cast<cudaStream_t>(stream));
 }
 
-size_t thanos_adapter_packed_workspace_bytes(int32_t backward, int32_t packed_w, int32_t packed_x,
+size_t thanos_adapter_packed_workspace_bytes(int32_t backward, int32_t packed_w, int32_t,
                                              int64_t n_tok, int64_t c, int64_t b,
                                              int64_t n_adapters, int32_t r, thanos_dtype_t dtype) {
   if (adapter_shape(n_tok, c, b, n_adapters, r, dtype) != THANOS_OK) return 0;
@@ -304,7 +292,7 @@ size_t thanos_adapter_packed_workspace_bytes(int32_t backward, int32_t packed_w,
   a.dtype = dtype;
   if (!backward && packed_w && packed_few_tokens(a)) return packed_few_workspace_bytes(n_tok, a.r);
   return round_up(thanos_adapter_workspace_bytes(backward, n_tok, c, b, n_adapters, r, dtype), 256) +
-         packed_extra_bytes(packed_w != 0, backward && packed_x, n_tok, c, b, dtype);
+         (packed_w ? unpacked_bytes(c, b, dtype) : 0);
 }
 
 thanos_status_t thanos_adapter_forward_packed(void* Y, int64_t ldy, float* V, const void* X,

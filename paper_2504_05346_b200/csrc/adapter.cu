@@ -421,7 +421,10 @@ thanos_status_t backward16(const AdapterArgs& a, void* workspace, size_t ws_byte
   if (a.dA) {
     AdapterGradSide sa, sb;
     sa.Z = static_cast<const bf16*>(a.X);
-    sa.ldz = a.ldx;
+    sa.ldz = a.X8 ? a.ldx8 : a.ldx;
+    sa.Z8 = a.X8;
+    sa.exps = a.exps;
+    sa.lde = a.lde;
     sa.R = L.u_planes;
     sa.out = a.dA;
     sa.F = (int)a.b;

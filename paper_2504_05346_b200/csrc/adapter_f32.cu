@@ -233,6 +233,9 @@ struct Grad32Side {
   const float* scale;
   float* out;
   int F, by_feature;
+  const int8_t* Z8;     // packed activations in the place of Z (ldz: of the codes)
+  const uint8_t* exps;
+  int64_t lde;
 };
 struct Grad32Params {
   Grad32Side side[2];
@@ -246,6 +249,7 @@ __global__ void __launch_bounds__(256) grad_f32_kernel(const Grad32Params p) {
   __shared__ float red[8][RANKS][33];
   __shared__ int tok[GRAD_TOKENS];
   __shared__ __align__(16) float fac[GRAD_TOKENS * RANKS];
+  __shared__ float step[GRAD_TOKENS];   // packed activations: 2^e of the token and these 32 features
   const Grad32Side& sd = blockIdx.x < p.tiles0 ? p.side[0] : p.side[1];
   const int f = ((int)blockIdx.x - (blockIdx.x < p.tiles0 ? 0 : p.tiles0)) * 32 + (threadIdx.x & 31);
   const int g = threadIdx.x >> 5;
@@ -271,8 +275,25 @@ __global__ void __launch_bounds__(256) grad_f32_kernel(const Grad32Params p) {
         const int j = e & (RANKS - 1);
         fac[e] = j < nj ? sd.R[(int64_t)tok[e / RANKS] * p.r + j0 + j] : 0.f;
       }
+      if (sd.Z8) {
+        const int group = blockIdx.x;   // side 0: a CTA's 32 features are one group
+        for (int e = threadIdx.x; e < nq; e += 256)
+          step[e] = __uint_as_float((uint32_t)sd.exps[(int64_t)tok[e] * sd.lde + group] << 23);
+      }
       __syncthreads();
-      if (f < sd.F) {
+      if (sd.Z8) {
+        if (f < sd.F) {
+#pragma unroll 8
+          for (int q = g; q < nq; q += 8) {
+            // the byte with its sign turned is code + 128, as the low bits of 2^23 a float; a conversion
+            // instruction takes as long as the eight products
+            const uint32_t u = (uint8_t)sd.Z8[(int64_t)tok[q] * sd.ldz + f];
+            const float z = (__uint_as_float((u ^ 0x80u) | 0x4B000000u) - 8388736.f) * step[q];
+#pragma unroll
+            for (int j = 0; j < RANKS; ++j) s[j] = fmaf(fac[q * RANKS + j], z, s[j]);
+          }
+        }
+      } else if (f < sd.F) {
 #pragma unroll 8
         for (int q = g; q < nq; q += 8) {
           const float z = sd.Z[(int64_t)tok[q] * sd.ldz + f];
@@ -508,8 +529,10 @@ thanos_status_t adapter_f32(bool back, const AdapterArgs& a, void* workspace, si
   }
   if (a.dA) {
     Grad32Params g = {};
-    g.side[0] = {static_cast<const float*>(a.X), a.ldx, L.R, nullptr, a.dA, (int)a.b, 0};
-    g.side[1] = {static_cast<const float*>(a.in), a.ldi, a.Vin, a.scale, a.dB, (int)a.c, 1};
+    g.side[0] = {static_cast<const float*>(a.X), a.X8 ? a.ldx8 : a.ldx, L.R, nullptr, a.dA, (int)a.b, 0,
+                 a.X8, a.exps, a.lde};
+    g.side[1] = {static_cast<const float*>(a.in), a.ldi, a.Vin, a.scale, a.dB, (int)a.c, 1,
+                 nullptr, nullptr, 0};
     g.tiles0 = (int)ceil_div(a.b, 32);
     g.order = L.order;
     g.off = L.off;

@@ -14,6 +14,9 @@ thanos_status_t sort_tokens(const int32_t* index, int64_t T, int64_t n, int32_t*
 struct AdapterGradSide {
   const __nv_bfloat16* Z = nullptr;  // [T, F], leading dimension ldz (multiple of 8)
   int64_t ldz = 0;
+  const int8_t* Z8 = nullptr;        // or packed activations (packed.cuh): codes, ldz a multiple of 16,
+  const uint8_t* exps = nullptr;     // and exponents, leading dimension lde
+  int64_t lde = 0;
   const __nv_bfloat16* R = nullptr;  // [T, 3 r16] with r16 = r rounded up to 16: R[t] as three bf16
                                      // planes side by side, zeros beyond r
   const float* scale = nullptr;      // factor by adapter, or null

@@ -13,6 +13,10 @@ struct AdapterArgs {
   int64_t ldi = 0;
   const void* X = nullptr;      // backward: the forward input, for dA
   int64_t ldx = 0;
+  const int8_t* X8 = nullptr;   // backward: the forward input in 8 bits, in the place of X
+  int64_t ldx8 = 0;
+  const uint8_t* exps = nullptr;
+  int64_t lde = 0;
   const void* W = nullptr;
   int64_t ldw = 0;
   const void* A = nullptr;
