@@ -64,6 +64,7 @@ class PruneStats:
 
 
 _lib = None
+_calls = None     # the short way to the calls below (csrc/calls.cpp), once the library is loaded
 _NO_SCOPE = contextlib.nullcontext()
 
 
@@ -165,7 +166,26 @@ def load_library():
     lib.thanos_launch_count.argtypes = []
     lib.thanos_launch_count.restype = i64
     _lib = lib
+    _bind_calls(lib)
     return lib
+
+
+def _bind_calls(lib):
+    """Loads _calls.so beside the library.  It only makes calls shorter: without it, or with one that
+    was built for another torch, they go the long way."""
+    global _calls
+    try:
+        from . import _calls as module
+    except ImportError:
+        return
+    names = ["thanos_" + n for n in (
+        "token_logprobs", "token_logprobs_backward", "pack_weights", "unpack_weights",
+        "pack_activations", "unpack_activations", "adapter_forward", "adapter_backward",
+        "adapter_forward_packed", "adapter_backward_packed", "adapter_workspace_bytes",
+        "adapter_packed_workspace_bytes")]
+    module.bind(PackedWeights, PackedActivations,
+                {n: ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in names})
+    _calls = module
 
 
 def status_string(code: int) -> str:
@@ -669,7 +689,11 @@ def adapter_forward(X: torch.Tensor, W: Union[torch.Tensor, PackedWeights], A: O
     holds X[t] A[i]^T for adapter_backward (None without adapters).  W may be PackedWeights
     (thanos_adapter_forward_packed).  With check=True the call's device status word is read back (this
     waits for the call)."""
-    lib = load_library()
+    lib = _lib or load_library()
+    if _calls is not None and stream is workspace is out is V is None and not check:
+        done = _calls.adapter_forward(X, W, A, B, index, scale)
+        if done is not None:
+            return done
     dev = _device_of(X, "X")
     T, c, b, n, r, ldw, dt = _adapters(X, W, A, B, index, scale, dev)
     packed = type(W) is PackedWeights
@@ -721,7 +745,12 @@ def adapter_backward(dY: torch.Tensor, X: Union[torch.Tensor, PackedActivations,
     accumulate=True they are added to (pass them in).  need_dx=False / need_grads=False leave a
     part out (None is returned for it; X and V may then be None without gradients).  X may be
     PackedActivations and W PackedWeights, one or both (thanos_adapter_backward_packed)."""
-    lib = load_library()
+    lib = _lib or load_library()
+    if _calls is not None and stream is workspace is dA is dB is dX is None and not (check or accumulate):
+        done = _calls.adapter_backward(dY, X, V, W, A, B, index, scale, bool(need_dx),
+                                       bool(need_grads))
+        if done is not None:
+            return done
     dev = _device_of(dY, "dY")
     T, c, b, n, r, ldw, dt = _adapters(dY, W, A, B, index, scale, dev)
     packed_w = type(W) is PackedWeights

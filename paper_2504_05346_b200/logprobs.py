@@ -6,6 +6,7 @@ from typing import NamedTuple, Optional
 
 import torch
 
+from . import binding
 from .binding import (_alloc_scope, _check, _dense, _device_of, _dtype_code, _on, _ptr,
                       _stream_ptr, load_library)
 
@@ -38,6 +39,10 @@ def token_logprobs(Z: torch.Tensor, target: Optional[torch.Tensor] = None, k: in
     logits Z [n_tok, vocab] (float32 or bfloat16), every row's entropy, and its k <= 64 most likely
     tokens with their log probabilities, equal logits by index."""
     lib = load_library()
+    if binding._calls is not None and stream is None:
+        done = binding._calls.token_logprobs(Z, target, k)
+        if done is not None:
+            return TokenLogprobs(*done)
     dev = _device_of(Z, "Z")
     T, V, ldz = _logits(Z, "Z")
     dt = _dtype_code(Z)
@@ -72,6 +77,11 @@ def token_logprobs_backward(Z: torch.Tensor, stats: torch.Tensor,
     entropy) + sum(dtop top_logp); stats and entropy are what token_logprobs returned.  Any of the
     three may be left out.  out may be Z itself: the gradient then takes the logits' place."""
     lib = load_library()
+    if binding._calls is not None and stream is out is None:
+        done = binding._calls.token_logprobs_backward(Z, stats, target, dlogp, entropy, dentropy,
+                                                      top_index, dtop)
+        if done is not None:
+            return done
     dev = _device_of(Z, "Z")
     T, V, ldz = _logits(Z, "Z")
     dt = _dtype_code(Z)

@@ -6,6 +6,7 @@ from typing import Optional
 
 import torch
 
+from . import binding
 from .binding import (PackedActivations, PackedWeights, _alloc_scope, _check, _device_of,
                       _dtype_code, _on, _packed_activations, _packed_weights, _rows, _stream_ptr,
                       load_library)
@@ -32,6 +33,10 @@ def pack_weights(W: torch.Tensor, group: int = 128, stream=None) -> PackedWeight
     """thanos_pack_weights: W [c, b] (float32 or bfloat16) in 4 bits, groups of 64 or 128 columns of
     a row with a scale of their own.  Zeros stay zeros."""
     lib = load_library()
+    if binding._calls is not None and stream is None:
+        done = binding._calls.pack_weights(W, group)
+        if done is not None:
+            return PackedWeights(*done, group, W.shape[1])
     c, b, dev, ldw = _matrix(W, "W")
     dt = _dtype_code(W)
     if group not in (64, 128):
@@ -50,6 +55,10 @@ def unpack_weights(W: PackedWeights, dtype=torch.bfloat16, stream=None,
                    out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """thanos_unpack_weights: the weights that the codes stand for, [c, b] (exact in either dtype)."""
     lib = load_library()
+    if binding._calls is not None and stream is out is None:
+        done = binding._calls.unpack_weights(W, dtype)
+        if done is not None:
+            return done
     dev = _device_of(W.codes, "the weights' codes")
     c, b, ldq = _packed_weights(W, dev)
     with _on(W.codes):
@@ -65,6 +74,10 @@ def pack_activations(X: torch.Tensor, stream=None) -> PackedActivations:
     """thanos_pack_activations: X [n_tok, b] (float32 or bfloat16) in 8 bits, groups of 32 columns
     of a row with a power of two of their own."""
     lib = load_library()
+    if binding._calls is not None and stream is None:
+        done = binding._calls.pack_activations(X)
+        if done is not None:
+            return PackedActivations(*done)
     T, b, dev, ldx = _matrix(X, "X")
     dt = _dtype_code(X)
     groups = -(-b // 32)
@@ -85,6 +98,10 @@ def unpack_activations(X: PackedActivations, dtype=torch.bfloat16, stream=None,
     """thanos_unpack_activations: the values that the codes stand for, [n_tok, b] (exact in either
     dtype)."""
     lib = load_library()
+    if binding._calls is not None and stream is out is None:
+        done = binding._calls.unpack_activations(X, dtype)
+        if done is not None:
+            return done
     dev = _device_of(X.codes, "the activations' codes")
     if X.codes.dim() != 2:
         raise ValueError("the activations' codes must be a matrix")

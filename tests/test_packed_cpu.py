@@ -124,3 +124,15 @@ def test_python_layer_refuses():
         T.unpack_activations(T.PackedActivations(X.to(torch.int8), torch.zeros(4, 2, dtype=torch.uint8)))
     with pytest.raises(ValueError):
         T.adapter_forward(X, P)
+
+
+def test_the_short_way_is_built(lib):
+    """csrc/calls.cpp is there, is bound to the library, and leaves host tensors to the long way."""
+    import torch
+    from paper_2504_05346_b200 import binding
+
+    assert binding._calls is not None
+    X = torch.zeros(4, 64)
+    assert binding._calls.adapter_forward(X, X, None, None, None, None) is None
+    assert binding._calls.pack_activations(X) is None and binding._calls.token_logprobs(X, None, 1) is None
+    assert binding._calls.pack_weights(None, 64) is None and binding._calls.pack_weights(X) is None
