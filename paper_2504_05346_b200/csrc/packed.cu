@@ -282,6 +282,7 @@ __global__ void __launch_bounds__(PT) unpack_w_kernel(T* __restrict__ W, int64_t
                                                       int b, int group) {
   const Place at;
   if (at.col >= b) return;
+  const Nibbles nib;
   for (int64_t row0 = at.row; row0 < c; row0 += at.rows) {
     uint32_t w[RB], s[RB];
 #pragma unroll
@@ -301,7 +302,7 @@ __global__ void __launch_bounds__(PT) unpack_w_kernel(T* __restrict__ W, int64_t
         uint32_t h[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const uint32_t v = ((w[u] >> (4 * j)) & 0x000F000Fu) | 0x43004300u;
+          const uint32_t v = nib(w[u], j);
           const __nv_bfloat162 d =
               __hmul2(__hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v),
                               *reinterpret_cast<const __nv_bfloat162*>(&off)),

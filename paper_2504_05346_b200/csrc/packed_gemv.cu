@@ -77,7 +77,15 @@ __global__ void __launch_bounds__(256) shrink_kernel(const FewParams p) {
 
 // --------------------------------------------------------------------------------------- products
 __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0,
-                                          uint32_t b1) {
+                                          uint32_t b1, bool first) {
+  if (first) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
+        "{%8, %9}, {%10, %10, %10, %10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+    return;
+  }
   asm volatile(
       "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
       "{%8, %9}, {%0, %1, %2, %3};"
@@ -85,8 +93,8 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4],
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 // Codes j and j + 4 of a word of eight as a pair of bf16.
-__device__ __forceinline__ uint32_t codes_of(uint32_t w, int j) {
-  const uint32_t v = ((w >> (4 * j)) & 0x000F000Fu) | 0x43004300u;
+__device__ __forceinline__ uint32_t codes_of(const Nibbles& nib, uint32_t w, int j) {
+  const uint32_t v = nib(w, j);
   const uint32_t off = 0x43084308u;  // 136
   const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v),
                                    *reinterpret_cast<const __nv_bfloat162*>(&off));
@@ -143,94 +151,133 @@ __device__ __forceinline__ uint2 load_codes(const uint8_t* p) {
   return v;
 }
 
-// UB: blocks whose loads are in flight together.
-template <typename T, int MT, int NT, int UB>
-__global__ void __launch_bounds__(GT) few_kernel(const FewParams p) {
+// Two blocks of 64 columns at a time (one group of 128, or two of 64).  What a lane reads of them lies at
+// fixed distances from pointers that move on, and nothing is tested: rows and tokens beyond the last are
+// the last one's, and only their results are left out.  The columns from the last whole pair of blocks on
+// are read with tests, by the last warp.  (16 rows at a time, every load with its own address and tests:
+// 131 instructions for 16 x 64 weights instead of some 70.)
+template <typename T, int MT, int NT>
+__device__ __forceinline__ void block_products(const Nibbles& nib, const uint2 (&w)[MT][2],
+                                               const uint32_t (&s)[MT][2],
+                                               const Vec8<T> (&x)[NT][2], float (&acc)[MT][NT][4]) {
   constexpr int PL = sizeof(T) == 2 ? 1 : 3;
+  float sum[MT][NT][4];
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {  // the lane's eight columns of the first, the second word
+    uint32_t xb[NT][PL][4];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) x[j][half].pairs(xb[j]);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const uint32_t lo = half ? w[i][0].y : w[i][0].x, hi = half ? w[i][1].y : w[i][1].x;
+#pragma unroll
+      for (int v = 0; v < 2; ++v) {
+        const uint32_t a[4] = {codes_of(nib, lo, 2 * v), codes_of(nib, hi, 2 * v),
+                               codes_of(nib, lo, 2 * v + 1), codes_of(nib, hi, 2 * v + 1)};
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int pl = PL - 1; pl >= 0; --pl)
+            mma_16816(sum[i][j], a, xb[j][pl][2 * v], xb[j][pl][2 * v + 1],
+                      half == 0 && v == 0 && pl == PL - 1);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        acc[i][j][e] = fmaf(__uint_as_float((s[i][e >> 1] & SCALE_BITS) << 16), sum[i][j][e],
+                            acc[i][j][e]);
+}
+
+template <typename T, int MT, int NT>
+__global__ void __launch_bounds__(GT) few_kernel(const FewParams p) {
   constexpr int ROWS = 16 * MT, TOKS = 8 * NT;
   __shared__ float part[GW][TOKS][ROWS + 4];
   if (p.n == 0 && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.status = 0;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = lane >> 2, t4 = lane & 3;
   const int m0 = blockIdx.x * ROWS, t0 = blockIdx.y * TOKS;
-  const int kb = (p.b + 63) >> 6;
-  const int kb0 = kb * warp / GW, kb1 = kb * (warp + 1) / GW;
+  const int pairs = p.b >> 7;  // whole ones
+  const int k0 = pairs * warp / GW, k1 = pairs * (warp + 1) / GW;
 
   const uint8_t* q[MT][2];
-  const bf16* sc[MT][2];
+  const unsigned short* sc[MT][2];
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {  // rows beyond the last read the last one's codes
+    for (int h = 0; h < 2; ++h) {
       const int row = min(m0 + 16 * i + 8 * h + g, p.c - 1);
-      q[i][h] = p.codes + (int64_t)row * p.ldq + 8 * t4;
-      sc[i][h] = p.scales + row;
+      q[i][h] = p.codes + (int64_t)row * p.ldq + 8 * t4 + (int64_t)k0 * 64;
+      sc[i][h] = reinterpret_cast<const unsigned short*>(p.scales) + row +
+                 (int64_t)((k0 << 7) >> p.shift) * p.c;
     }
   }
   const T* x[NT];
-  bool tok[NT];
 #pragma unroll
-  for (int j = 0; j < NT; ++j) {
-    const int t = t0 + 8 * j + g;
-    tok[j] = t < p.T;
-    x[j] = static_cast<const T*>(p.X) + (int64_t)(tok[j] ? t : 0) * p.ldx + 16 * t4;
-  }
+  for (int j = 0; j < NT; ++j)
+    x[j] = static_cast<const T*>(p.X) + (int64_t)min(t0 + 8 * j + g, p.T - 1) * p.ldx + 16 * t4 +
+           (int64_t)k0 * 128;
+  const int64_t second = p.shift == 6 ? p.c : 0, step = p.shift == 6 ? 2 * (int64_t)p.c : p.c;
+  const Nibbles nib;
   float acc[MT][NT][4] = {};
-  for (int k0 = kb0; k0 < kb1; k0 += UB) {
-    uint2 w[UB][MT][2];
-    uint32_t s[UB][MT][2];
-    Vec8<T> xr[UB][NT][2];
+#pragma unroll 1
+  for (int k = k0; k < k1; ++k) {
+    uint2 w[2][MT][2];
+    uint32_t s[2][MT][2];
+    Vec8<T> xr[2][NT][2];
 #pragma unroll
-    for (int u = 0; u < UB; ++u) {
-      const int k = min(k0 + u, kb1 - 1);  // one block more than there are is read again, for nothing
-      const int64_t sg = (int64_t)((k << 6) >> p.shift) * p.c;
+    for (int u = 0; u < 2; ++u) {
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          w[u][i][h] = load_codes(q[i][h] + (int64_t)k * 32);
-          s[u][i][h] = __bfloat16_as_ushort(sc[i][h][sg]);
+          w[u][i][h] = load_codes(q[i][h] + 32 * u);
+          s[u][i][h] = sc[i][h][u ? second : 0];
         }
 #pragma unroll
       for (int j = 0; j < NT; ++j)
 #pragma unroll
-        for (int half = 0; half < 2; ++half)
-          xr[u][j][half].load(x[j] + 64 * k + 8 * half,
-                              tok[j] && 64 * k + 16 * t4 + 8 * half < p.b);
+        for (int half = 0; half < 2; ++half) xr[u][j][half].load(x[j] + 64 * u + 8 * half, true);
     }
 #pragma unroll
-    for (int u = 0; u < UB; ++u) {
-      if (k0 + u >= kb1) break;
-      float sum[MT][NT][4] = {};
+    for (int i = 0; i < MT; ++i)
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {  // the lane's eight columns of the first, the second word
-        uint32_t xb[NT][PL][4];
-#pragma unroll
-        for (int j = 0; j < NT; ++j) xr[u][j][half].pairs(xb[j]);
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-          const uint32_t lo = half ? w[u][i][0].y : w[u][i][0].x;
-          const uint32_t hi = half ? w[u][i][1].y : w[u][i][1].x;
-#pragma unroll
-          for (int v = 0; v < 2; ++v) {
-            const uint32_t a[4] = {codes_of(lo, 2 * v), codes_of(hi, 2 * v), codes_of(lo, 2 * v + 1),
-                                   codes_of(hi, 2 * v + 1)};
-#pragma unroll
-            for (int j = 0; j < NT; ++j)
-#pragma unroll
-              for (int pl = PL - 1; pl >= 0; --pl)
-                mma_16816(sum[i][j], a, xb[j][pl][2 * v], xb[j][pl][2 * v + 1]);
-          }
-        }
+      for (int h = 0; h < 2; ++h) {
+        q[i][h] += 64;
+        sc[i][h] += step;
       }
+#pragma unroll
+    for (int j = 0; j < NT; ++j) x[j] += 128;
+    block_products<T, MT, NT>(nib, w[0], s[0], xr[0], acc);
+    block_products<T, MT, NT>(nib, w[1], s[1], xr[1], acc);
+  }
+  if (warp == GW - 1) {  // k1 is the end of the whole pairs here
+#pragma unroll 1
+    for (int col = pairs * 128; col < p.b; col += 64) {
+      uint2 w[MT][2];
+      uint32_t s[MT][2];
+      Vec8<T> xr[NT][2];
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
+        for (int h = 0; h < 2; ++h) {
+          w[i][h] = load_codes(q[i][h]);
+          s[i][h] = sc[i][h][0];
+          q[i][h] += 32;
+          sc[i][h] += second;
+        }
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            acc[i][j][e] = fmaf(__uint_as_float((s[u][i][e >> 1] & SCALE_BITS) << 16), sum[i][j][e],
-                                acc[i][j][e]);
+      for (int j = 0; j < NT; ++j) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+          xr[j][half].load(x[j] + 8 * half, col + 16 * t4 + 8 * half < p.b);
+        x[j] += 64;
+      }
+      block_products<T, MT, NT>(nib, w, s, xr, acc);
     }
   }
   // ---- sums over the warps
@@ -253,7 +300,7 @@ __global__ void __launch_bounds__(GT) few_kernel(const FewParams p) {
   }
 }
 
-template <typename T, int MT, int NT, int UB>
+template <typename T, int MT, int NT>
 thanos_status_t launch(const FewParams& p, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)ceil_div(p.c, 16 * MT), (unsigned)ceil_div(p.T, 8 * NT), 1);
@@ -265,7 +312,7 @@ thanos_status_t launch(const FewParams& p, cudaStream_t stream) {
   cfg.attrs = attr;
   cfg.numAttrs = p.n > 0 ? 1 : 0;
   count_launch();
-  THANOS_CUDA(cudaLaunchKernelEx(&cfg, few_kernel<T, MT, NT, UB>, p));
+  THANOS_CUDA(cudaLaunchKernelEx(&cfg, few_kernel<T, MT, NT>, p));
   return THANOS_OK;
 }
 
@@ -275,11 +322,13 @@ thanos_status_t forward_few(const FewParams& p, cudaStream_t stream) {
     shrink_kernel<T><<<(unsigned)(p.T * ceil_div(p.r, SHRINK_RANKS)), 256, 0, stream>>>(p);
     THANOS_CHECK_LAUNCH();
   }
+  // Two tiles of rows share a warp's activations, where there are rows enough for every SM.
+  const bool wide = p.c >= 32 * NUM_SMS;
+  if (p.T <= 8) return wide ? launch<T, 2, 1>(p, stream) : launch<T, 1, 1>(p, stream);
   if constexpr (sizeof(T) == 4) {
-    if (p.T <= 8) return launch<T, 1, 1, 2>(p, stream);
-    return launch<T, 2, 2, 1>(p, stream);
+    return launch<T, 2, 2>(p, stream);
   } else {
-    if (p.T <= 8) return launch<T, 1, 1, 4>(p, stream);
+    if (p.T <= 16) return wide ? launch<T, 2, 2>(p, stream) : launch<T, 1, 2>(p, stream);
     return packed_tiles(p, stream);
   }
 }

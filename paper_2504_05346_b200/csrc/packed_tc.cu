@@ -86,12 +86,13 @@ __device__ __forceinline__ uint4 ld_shared16(uint32_t addr) {
 }
 
 // Eight weights of a word, in the order of their columns.
-__device__ __forceinline__ void decode8(uint32_t w, uint32_t scale2, uint32_t* out) {
+__device__ __forceinline__ void decode8(const Nibbles& nib, uint32_t w, uint32_t scale2,
+                                        uint32_t* out) {
   const uint32_t off = 0x43084308u;  // 136
   uint32_t h[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const uint32_t v = ((w >> (4 * j)) & 0x000F000Fu) | 0x43004300u;  // 128 + nibbles j and j + 4
+    const uint32_t v = nib(w, j);
     const __nv_bfloat162 d = __hmul2(__hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v),
                                              *reinterpret_cast<const __nv_bfloat162*>(&off)),
                                      *reinterpret_cast<const __nv_bfloat162*>(&scale2));
@@ -216,49 +217,54 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
     // ------------------------------------------------------------ codes into tensor memory
     const int group = warp >> 2, row = 32 * (warp & 3) + lane;
     const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
-    const bf16* scales = f.scales + min(m0 + row, f.c - 1);
-    auto scale_at = [&](int i) -> uint32_t {  // of block i of this CTA, as a pair
+    const unsigned short* scales =
+        reinterpret_cast<const unsigned short*>(f.scales) + min(m0 + row, f.c - 1);
+    auto scale_of = [&](int i) {  // of block i of this CTA, as it is in memory
       const int kb = min(4 * st0 + i, p.blocks - 1);
-      const uint32_t v =
-          __bfloat16_as_ushort(scales[(int64_t)((kb * QBLOCK) >> f.shift) * f.c]) & SCALE_BITS;
-      return v | v << 16;
+      return (uint32_t)scales[(int64_t)((kb * QBLOCK) >> f.shift) * f.c];
     };
-    int s = 0;
-    uint32_t phase = 0;
-    uint32_t next[2] = {scale_at(group), scale_at(group + 2)};
+    const Nibbles nib;
+    int s = 0, q = group;         // stage; buffer of the next block: even or odd ones
+    uint32_t phase = 0, turn = 1; // parity of the buffers' barriers
+    // a stage's scales are fetched a stage ahead, and not looked at until then
+    uint32_t next[2] = {scale_of(group), scale_of(group + 2)};
     for (int i0 = 0; i0 < nblk; i0 += 4) {
-      const uint32_t scale[2] = {next[0], next[1]};
-      next[0] = scale_at(i0 + 4 + group);
-      next[1] = scale_at(i0 + 6 + group);
+      const uint32_t raw[2] = {next[0], next[1]};
+      next[0] = scale_of(i0 + 4 + group);
+      next[1] = scale_of(i0 + 6 + group);
       ok = mbar_wait_warp(full_bar(s), phase, abort_flag);
       if (!ok) break;
       const uint32_t codes = smem_base + (uint32_t)(s * stage_bytes) + row * 128;
+      uint4 c[2][2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          c[h][e] = ld_shared16(codes + (((2 * (group + 2 * h) + e) ^ (row & 7)) << 4));
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int u = group + 2 * h, i = i0 + u;
-        if (i < nblk) {
-          uint4 c[2];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) c[e] = ld_shared16(codes + (((2 * u + e) ^ (row & 7)) << 4));
+        if (i0 + group + 2 * h < nblk) {
+          const uint32_t scale = (raw[h] & SCALE_BITS) * 0x10001u;
           uint32_t v[32];
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            decode8(c[e].x, scale[h], v + 16 * e);
-            decode8(c[e].y, scale[h], v + 16 * e + 4);
-            decode8(c[e].z, scale[h], v + 16 * e + 8);
-            decode8(c[e].w, scale[h], v + 16 * e + 12);
+            decode8(nib, c[h][e].x, scale, v + 16 * e);
+            decode8(nib, c[h][e].y, scale, v + 16 * e + 4);
+            decode8(nib, c[h][e].z, scale, v + 16 * e + 8);
+            decode8(nib, c[h][e].w, scale, v + 16 * e + 12);
           }
-          const int q = i % QBUFS;
-          ok = mbar_wait_warp(wempty_bar(q), ((uint32_t)(i / QBUFS) & 1u) ^ 1u, abort_flag);
+          ok = mbar_wait_warp(wempty_bar(q), turn, abort_flag);
           if (!ok) break;
           tc_fence_after();
           tmem_st32(weights + lanes + q * 32, v);
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(wfull_bar(q));
+          q ^= 2;
         }
       }
       if (!ok) break;
+      turn ^= 1u;
       __syncwarp();
       if (lane == 0) mbar_arrive(empty_bar(s));
       if (++s == p.stages) {
