@@ -39,21 +39,28 @@ __device__ __forceinline__ void finish(const FewParams& p, int row, int at, floa
     if (i >= 0 && i < p.n) {
       const T* bw = static_cast<const T*>(p.B) + ((int64_t)i * p.c + row) * p.r;
       const float* vt = p.V + (int64_t)at * p.r;
-      constexpr int VEC = 16 / sizeof(T);
       float d = 0.f;
-      if (p.r % VEC == 0) {
+      if (p.r % 8 == 0) {  // rows of B_i and of V on whole 16-byte lines
 #pragma unroll 2
-        for (int j = 0; j < p.r; j += VEC) {
-          const uint4 q = *reinterpret_cast<const uint4*>(bw + j);
-          const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+        for (int j = 0; j < p.r; j += 8) {
+          const float4 v0 = *reinterpret_cast<const float4*>(vt + j);
+          const float4 v1 = *reinterpret_cast<const float4*>(vt + j + 4);
+          const uint4* q = reinterpret_cast<const uint4*>(bw + j);
+          if constexpr (sizeof(T) == 2) {
+            const float f[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
+            const uint32_t w[4] = {q[0].x, q[0].y, q[0].z, q[0].w};
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if constexpr (VEC == 8) {
-              d = fmaf(vt[j + 2 * e], __uint_as_float(w[e] << 16), d);
-              d = fmaf(vt[j + 2 * e + 1], __uint_as_float(w[e] & 0xFFFF0000u), d);
-            } else {
-              d = fmaf(vt[j + e], __uint_as_float(w[e]), d);
+            for (int e = 0; e < 4; ++e) {
+              d = fmaf(f[2 * e], __uint_as_float(w[e] << 16), d);
+              d = fmaf(f[2 * e + 1], __uint_as_float(w[e] & 0xFFFF0000u), d);
             }
+          } else {
+            const float4 b0 = reinterpret_cast<const float4*>(q)[0];
+            const float4 b1 = reinterpret_cast<const float4*>(q)[1];
+            d = fmaf(v0.x, b0.x, d), d = fmaf(v0.y, b0.y, d);
+            d = fmaf(v0.z, b0.z, d), d = fmaf(v0.w, b0.w, d);
+            d = fmaf(v1.x, b1.x, d), d = fmaf(v1.y, b1.y, d);
+            d = fmaf(v1.z, b1.z, d), d = fmaf(v1.w, b1.w, d);
           }
         }
       } else {

@@ -25,10 +25,12 @@ __device__ __forceinline__ int adapter_of(const int32_t* index, int t, int n) {
 }
 
 // ------------------------------------------------------------------------------ V[t] = X[t] A_i^T
-// A CTA per token and four ranks; clears the status word of the call.
+// A CTA per token and four ranks, as many threads as a row has pieces of 16 bytes (1024 at most): one
+// round of loads in flight, two at 11008 columns (256 threads, six rounds: 15 us there, beside products of
+// 14).  Clears the status word of the call.
 template <typename T>
-__global__ void __launch_bounds__(256) shrink_kernel(const FewParams p) {
-  __shared__ float sh[SHRINK_RANKS][8];
+__global__ void __launch_bounds__(1024) shrink_kernel(const FewParams p) {
+  __shared__ float sh[SHRINK_RANKS][32];
   grid_dependents_launch();
   const int tid = threadIdx.x;
   if (blockIdx.x == 0 && tid == 0) *p.status = 0;
@@ -40,7 +42,7 @@ __global__ void __launch_bounds__(256) shrink_kernel(const FewParams p) {
     constexpr int VEC = 16 / sizeof(T);
     const T* x = static_cast<const T*>(p.X) + (int64_t)t * p.ldx;
     const T* a = static_cast<const T*>(p.A) + ((int64_t)i * p.r + j0) * p.b;
-    for (int k = tid * VEC; k < p.b; k += 256 * VEC) {
+    for (int k = tid * VEC; k < p.b; k += (int)blockDim.x * VEC) {
       const uint4 xv = *reinterpret_cast<const uint4*>(x + k);
       const uint32_t xw[4] = {xv.x, xv.y, xv.z, xv.w};
 #pragma unroll
@@ -70,7 +72,7 @@ __global__ void __launch_bounds__(256) shrink_kernel(const FewParams p) {
   __syncthreads();
   if (tid < SHRINK_RANKS && j0 + tid < p.r) {
     float v = 0.f;
-    for (int w = 0; w < 8; ++w) v += sh[tid][w];
+    for (int w = 0; w < (int)blockDim.x / 32; ++w) v += sh[tid][w];
     p.V[(int64_t)t * p.r + j0 + tid] = v;
   }
 }
@@ -194,7 +196,7 @@ __device__ __forceinline__ void block_products(const Nibbles& nib, const uint2 (
 }
 
 template <typename T, int MT, int NT>
-__global__ void __launch_bounds__(GT) few_kernel(const FewParams p) {
+__global__ void __launch_bounds__(GT, MT * NT == 1 ? 4 : MT * NT == 2 ? 3 : 2) few_kernel(const FewParams p) {
   constexpr int ROWS = 16 * MT, TOKS = 8 * NT;
   __shared__ float part[GW][TOKS][ROWS + 4];
   if (p.n == 0 && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.status = 0;
@@ -319,7 +321,9 @@ thanos_status_t launch(const FewParams& p, cudaStream_t stream) {
 template <typename T>
 thanos_status_t forward_few(const FewParams& p, cudaStream_t stream) {
   if (p.n > 0) {
-    shrink_kernel<T><<<(unsigned)(p.T * ceil_div(p.r, SHRINK_RANKS)), 256, 0, stream>>>(p);
+    const size_t pieces = round_up((size_t)p.b * sizeof(T) / 16, 32);
+    shrink_kernel<T><<<(unsigned)(p.T * ceil_div(p.r, SHRINK_RANKS)),
+                       (unsigned)(pieces < 1024 ? pieces : 1024), 0, stream>>>(p);
     THANOS_CHECK_LAUNCH();
   }
   // Two tiles of rows share a warp's activations, where there are rows enough for every SM.
@@ -335,7 +339,13 @@ thanos_status_t forward_few(const FewParams& p, cudaStream_t stream) {
 
 }  // namespace
 
-bool packed_few_tokens(const AdapterArgs& a) { return a.T <= (a.dtype == THANOS_BF16 ? 256 : 32); }
+// Up to here the codes are turned into weights where they meet the activations; with more tokens they are
+// unpacked once and multiplied as they would be from memory.  Replayed, both ways:
+//   4096 x 4096, 128 tokens     14.5 and 22.7 us   (192 tokens 20.8 and 26.3, 256 tokens 23.8 and 25.9)
+//   11008 x 4096, 128 tokens    27.2 and 53.2      (192 tokens 58.7 and 61.6, 256 tokens 67.0 and 62.6)
+//   the same, 16 adapters of rank 16   58.6 and 65.3   (192 tokens 97.8 and 75.2)
+//   fp32 2048 x 2048, 64 tokens   15.8 and 31.7;  768 x 768, 64 tokens   4.9 and 15.2
+bool packed_few_tokens(const AdapterArgs& a) { return a.T <= (a.dtype == THANOS_BF16 ? 128 : 64); }
 
 size_t packed_few_workspace_bytes(int64_t T, int r) { return 256 + round_up((size_t)T * r * 4, 256); }
 
