@@ -341,11 +341,14 @@ thanos_status_t forward_few(const FewParams& p, cudaStream_t stream) {
 
 // Up to here the codes are turned into weights where they meet the activations; with more tokens they are
 // unpacked once and multiplied as they would be from memory.  Replayed, both ways:
-//   4096 x 4096, 128 tokens     14.5 and 22.7 us   (192 tokens 20.8 and 26.3, 256 tokens 23.8 and 25.9)
-//   11008 x 4096, 128 tokens    27.2 and 53.2      (192 tokens 58.7 and 61.6, 256 tokens 67.0 and 62.6)
-//   the same, 16 adapters of rank 16   58.6 and 65.3   (192 tokens 97.8 and 75.2)
+//   4096 x 4096     128 tokens   13.2 and 22.7 us    256 tokens   20.5 and 25.9 us
+//   4096 x 11008    128 tokens   22.0 and 53.9       256 tokens   37.2 and 63.8
+//   11008 x 4096    128 tokens   26.5 and 53.2       256 tokens   58.0 and 62.6
+//   the same, 16 adapters of rank 16   47.1 and 65.3;  192 tokens   97.8 and 75.2
 //   fp32 2048 x 2048, 64 tokens   15.8 and 31.7;  768 x 768, 64 tokens   4.9 and 15.2
-bool packed_few_tokens(const AdapterArgs& a) { return a.T <= (a.dtype == THANOS_BF16 ? 128 : 64); }
+bool packed_few_tokens(const AdapterArgs& a) {
+  return a.T <= (a.dtype == THANOS_F32 ? 64 : a.n > 0 ? 128 : 256);
+}
 
 size_t packed_few_workspace_bytes(int64_t T, int r) { return 256 + round_up((size_t)T * r * 4, 256); }
 

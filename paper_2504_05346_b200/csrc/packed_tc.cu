@@ -4,11 +4,12 @@
 // The weights are the operand in tensor memory: what a lane of it holds is a row's k, so a thread turns
 // the codes of its own row into bf16 (exactly: see packed.cu), with its own row's scale, and nothing is
 // exchanged between threads.
-//   warp 8       TMA: per stage 256 columns of the codes (128 rows x 128 bytes) and of the activations
+//   last but one TMA: per stage 256 columns of the codes (128 rows x 128 bytes) and of the activations
 //                (four boxes of 64 columns), both with the 128-byte swizzle
-//   warps 0..7   codes -> bf16 -> tensor memory, 64 columns at a time into one of four buffers; a warp
-//                group takes every other block
-//   warp 9       tcgen05.mma, 128 x N x 16, A from tensor memory, B from shared memory
+//   warps 0..7   codes -> bf16 -> tensor memory, 64 columns at a time into one of two buffers of the warp
+//                group, which takes every other block; 0..15 and every fourth block where a CTA has the SM
+//                to itself (these warps are what a block waits for)
+//   next warp    tcgen05.mma, 128 x N x 16, A from tensor memory, B from shared memory
 // A cluster splits k; the partial sums are added over distributed shared memory in rank order (same
 // inputs, same bits).
 #include "packed_few.cuh"
@@ -20,8 +21,8 @@ constexpr int QM = 128;                  // rows
 constexpr int QBLOCK = 64;               // columns that are turned into bf16 at a time
 constexpr int QSTAGE = 256;              // columns of a stage
 constexpr int QCODES = QM * QSTAGE / 2;  // bytes of a stage's codes
-constexpr int QBUFS = 4;                 // buffers of weights in tensor memory, 32 columns each
-constexpr int QT = 320;
+constexpr int QMAX_BUFS = 8;             // buffers of weights in tensor memory, 32 columns each
+constexpr int threads_of(int groups) { return 128 * groups + 64; }
 constexpr int QMAX_STAGES = 6;
 
 struct TilesParams {
@@ -104,23 +105,28 @@ __device__ __forceinline__ void decode8(const Nibbles& nib, uint32_t w, uint32_t
   out[3] = __byte_perm(h[2], h[3], 0x7632);
 }
 
-__global__ void __launch_bounds__(QT, 2)
+// GROUPS of four warps that turn codes into weights, with two buffers each.
+template <int GROUPS>
+__global__ void __launch_bounds__(threads_of(GROUPS), GROUPS == 2 ? 2 : 1)
 tiles_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
              const TilesParams p) {
+  constexpr int QBUFS = 2 * GROUPS, PER = 4 / GROUPS;  // blocks of a stage that a group takes
+  constexpr int PRODUCER = 4 * GROUPS, ISSUER = PRODUCER + 1;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + p.ring_bytes);
-  // full, empty (QMAX_STAGES each), weights full, weights empty (QBUFS each), done
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * QMAX_STAGES + 2 * QBUFS + 1);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 2 * QMAX_STAGES + 2 * QBUFS + 2);
+  // full, empty (QMAX_STAGES each), weights full, weights empty (QMAX_BUFS each), done
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * QMAX_STAGES + 2 * QMAX_BUFS + 1);
+  volatile int* abort_flag =
+      reinterpret_cast<volatile int*>(bars + 2 * QMAX_STAGES + 2 * QMAX_BUFS + 2);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t smem_base = smem_u32(smem), bar_base = smem_u32(bars);
   auto full_bar = [&](int s) { return bar_base + 8u * s; };
   auto empty_bar = [&](int s) { return bar_base + 8u * (QMAX_STAGES + s); };
   auto wfull_bar = [&](int q) { return bar_base + 8u * (2 * QMAX_STAGES + q); };
-  auto wempty_bar = [&](int q) { return bar_base + 8u * (2 * QMAX_STAGES + QBUFS + q); };
-  const uint32_t done_bar = bar_base + 8u * (2 * QMAX_STAGES + 2 * QBUFS);
+  auto wempty_bar = [&](int q) { return bar_base + 8u * (2 * QMAX_STAGES + QMAX_BUFS + q); };
+  const uint32_t done_bar = bar_base + 8u * (2 * QMAX_STAGES + 2 * QMAX_BUFS);
 
   const FewParams& f = p.f;
   const int S = p.split, rank = S > 1 ? (int)cluster_ctarank() : 0;
@@ -134,7 +140,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.stages; ++s) {
       mbar_init(full_bar(s), 1);
-      mbar_init(empty_bar(s), 9);
+      mbar_init(empty_bar(s), 4 * GROUPS + 1);
     }
     for (int q = 0; q < QBUFS; ++q) {
       mbar_init(wfull_bar(q), 4);
@@ -144,7 +150,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 9) {
+  if (warp == ISSUER) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
                      smem_u32(tmem_slot)),
                  "r"(p.tmem_cols)
@@ -157,7 +163,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
   const uint32_t tmem_base = *tmem_slot, weights = tmem_base + (uint32_t)(p.tmem_cols - QBUFS * 32);
   bool ok = true;
 
-  if (warp == 8) {
+  if (warp == PRODUCER) {
     // ------------------------------------------------------------ TMA producer
     if (elect_one()) {
       int s = 0;
@@ -183,7 +189,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
       }
     }
     __syncwarp();
-  } else if (warp == 9) {
+  } else if (warp == ISSUER) {
     // ------------------------------------------------------------ MMA issuer
     if (elect_one()) {
       const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (uint32_t)(N >> 3) << 17 |
@@ -224,26 +230,31 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
       return (uint32_t)scales[(int64_t)((kb * QBLOCK) >> f.shift) * f.c];
     };
     const Nibbles nib;
-    int s = 0, q = group;         // stage; buffer of the next block: even or odd ones
-    uint32_t phase = 0, turn = 1; // parity of the buffers' barriers
+    int s = 0, q = group;         // stage; buffer of the next block: this group's two in turn
+    uint32_t phase = 0, turn = 1; // parity of the buffer's barrier
     // a stage's scales are fetched a stage ahead, and not looked at until then
-    uint32_t next[2] = {scale_of(group), scale_of(group + 2)};
+    uint32_t next[PER];
+#pragma unroll
+    for (int h = 0; h < PER; ++h) next[h] = scale_of(group + GROUPS * h);
     for (int i0 = 0; i0 < nblk; i0 += 4) {
-      const uint32_t raw[2] = {next[0], next[1]};
-      next[0] = scale_of(i0 + 4 + group);
-      next[1] = scale_of(i0 + 6 + group);
+      uint32_t raw[PER];
+#pragma unroll
+      for (int h = 0; h < PER; ++h) {
+        raw[h] = next[h];
+        next[h] = scale_of(i0 + 4 + group + GROUPS * h);
+      }
       ok = mbar_wait_warp(full_bar(s), phase, abort_flag);
       if (!ok) break;
       const uint32_t codes = smem_base + (uint32_t)(s * stage_bytes) + row * 128;
-      uint4 c[2][2];
+      uint4 c[PER][2];
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < PER; ++h)
 #pragma unroll
         for (int e = 0; e < 2; ++e)
-          c[h][e] = ld_shared16(codes + (((2 * (group + 2 * h) + e) ^ (row & 7)) << 4));
+          c[h][e] = ld_shared16(codes + (((2 * (group + GROUPS * h) + e) ^ (row & 7)) << 4));
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        if (i0 + group + 2 * h < nblk) {
+      for (int h = 0; h < PER; ++h) {
+        if (i0 + group + GROUPS * h < nblk) {
           const uint32_t scale = (raw[h] & SCALE_BITS) * 0x10001u;
           uint32_t v[32];
 #pragma unroll
@@ -260,11 +271,11 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(wfull_bar(q));
-          q ^= 2;
+          q ^= GROUPS;
+          if (q == group) turn ^= 1u;  // both have been written once more
         }
       }
       if (!ok) break;
-      turn ^= 1u;
       __syncwarp();
       if (lane == 0) mbar_arrive(empty_bar(s));
       if (++s == p.stages) {
@@ -280,7 +291,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
       float* part = reinterpret_cast<float*>(smem);  // the ring, whose operands are consumed
       const int toks = min(N, f.T - t0);
 #pragma unroll 1
-      for (int j = 8 * group; j < toks; j += 16) {
+      for (int j = 8 * group; j < toks; j += 8 * GROUPS) {
         uint32_t v[8];
         tmem_ld8(tmem_base + lanes + j, v);
         tc_wait_ld();
@@ -295,9 +306,10 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
   }
   if (S > 1) {
     cluster_sync_all();
-    if (warp < 8 && ok) {
+    if (warp < PRODUCER && ok) {
       const int row = threadIdx.x & (QM - 1), toks = min(N, f.T - t0);
-      for (int t = 2 * rank + (int)(threadIdx.x / QM); t < toks && m0 + row < f.c; t += 2 * S) {
+      for (int t = GROUPS * rank + (int)(threadIdx.x / QM); t < toks && m0 + row < f.c;
+           t += GROUPS * S) {
         float v = 0.f;
         for (int u = 0; u < S; ++u) {
           float z;
@@ -315,7 +327,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 9) {
+  if (warp == ISSUER) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base),
                  "r"(p.tmem_cols)
@@ -338,44 +350,14 @@ bool make_map2(CUtensorMap* map, const void* base, CUtensorMapDataType type, int
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-}  // namespace
-
-thanos_status_t packed_tiles(const FewParams& f, cudaStream_t stream) {
-  TilesParams p = {};
-  p.f = f;
-  const int tiles_t = (int)ceil_div(f.T, 128);
-  p.N = (int)round_up((size_t)ceil_div(f.T, tiles_t), 16);
-  p.blocks = (int)ceil_div(f.b, QBLOCK);
-  const int stage_bytes = QCODES + p.N * QSTAGE * 2;
-  // two CTAs to an SM where two stages fit in half of its shared memory
-  const int per_sm = 2 * stage_bytes <= 108 * 1024 ? 2 : 1;
-  p.stages = (per_sm == 2 ? 108 * 1024 : 216 * 1024) / stage_bytes;
-  if (p.stages > QMAX_STAGES) p.stages = QMAX_STAGES;
-  p.ring_bytes = p.stages * stage_bytes;
-  p.tmem_cols = 32;
-  while (p.tmem_cols < p.N + QBUFS * 32) p.tmem_cols *= 2;
-  CUtensorMap map_w, map_x;
-  if (!make_map2(&map_w, f.codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, (int64_t)p.blocks * 32, f.c, f.ldq,
-                 QSTAGE / 2, QM) ||
-      !make_map2(&map_x, f.X, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, f.b, f.T, f.ldx * 2, QBLOCK, p.N))
-    return THANOS_ERR_CUDA;
-  const int64_t units = ceil_div(f.c, QM) * tiles_t, stages_all = ceil_div(p.blocks, 4);
-  double best = 0.0;
-  p.split = 1;
-  for (const int S : {1, 2, 3, 4, 6, 8}) {
-    if (S > stages_all) break;
-    const double cost = (double)ceil_div(units * S, per_sm * (int64_t)sm_count()) *
-                        (double)(ceil_div(stages_all, S) + (S > 1 ? 3 : 2));
-    if (S == 1 || cost < best) {
-      best = cost;
-      p.split = S;
-    }
-  }
+template <int GROUPS>
+thanos_status_t launch_tiles(const CUtensorMap& map_w, const CUtensorMap& map_x, const TilesParams& p,
+                             int tiles_t, cudaStream_t stream) {
   static std::atomic<unsigned long long> done{0};
-  THANOS_CUDA(ensure_max_dyn_smem(tiles_kernel, 227 * 1024, done));
+  THANOS_CUDA(ensure_max_dyn_smem(tiles_kernel<GROUPS>, 227 * 1024, done));
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(ceil_div(f.c, QM) * p.split), (unsigned)tiles_t, 1);
-  cfg.blockDim = dim3(QT, 1, 1);
+  cfg.gridDim = dim3((unsigned)(ceil_div(p.f.c, QM) * p.split), (unsigned)tiles_t, 1);
+  cfg.blockDim = dim3(threads_of(GROUPS), 1, 1);
   cfg.dynamicSmemBytes = (size_t)p.ring_bytes + 1024 + 512;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
@@ -386,10 +368,61 @@ thanos_status_t packed_tiles(const FewParams& f, cudaStream_t stream) {
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = f.n > 0 ? 2 : 1;
+  cfg.numAttrs = p.f.n > 0 ? 2 : 1;
   count_launch();
-  THANOS_CUDA(cudaLaunchKernelEx(&cfg, tiles_kernel, map_w, map_x, p));
+  THANOS_CUDA(cudaLaunchKernelEx(&cfg, tiles_kernel<GROUPS>, map_w, map_x, p));
   return THANOS_OK;
+}
+
+}  // namespace
+
+thanos_status_t packed_tiles(const FewParams& f, cudaStream_t stream) {
+  TilesParams p = {};
+  p.f = f;
+  const int tiles_t = (int)ceil_div(f.T, 128);
+  p.N = (int)round_up((size_t)ceil_div(f.T, tiles_t), 16);
+  p.blocks = (int)ceil_div(f.b, QBLOCK);
+  const int stage_bytes = QCODES + p.N * QSTAGE * 2;
+  CUtensorMap map_w, map_x;
+  if (!make_map2(&map_w, f.codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, (int64_t)p.blocks * 32, f.c, f.ldq,
+                 QSTAGE / 2, QM) ||
+      !make_map2(&map_x, f.X, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, f.b, f.T, f.ldx * 2, QBLOCK, p.N))
+    return THANOS_ERR_CUDA;
+  const int64_t units = ceil_div(f.c, QM) * tiles_t, stages_all = ceil_div(p.blocks, 4);
+  const int64_t sms = sm_count();
+  // Slices of k and CTAs to an SM, by the cost of a CTA's stages: 1 where it has the SM to itself (1.1 us;
+  // sixteen warps are then some 5 % faster than eight, 20 % with adapters to add), 1.75 where two share it,
+  // if two stages of each fit; 4 for start and end, 1 for the sum over a cluster, 1 more for clusters of
+  // eight two to an SM, which are hard to place.  32 tokens, replayed, slices 1 / 2 / 3 / 4 / 6 / 8:
+  //   4096 x 4096    22.5  15.4  12.9  10.3  12.5  11.3 us
+  //   11008 x 4096   22.6  20.8  17.3  20.6  22.9  26.1
+  //   28672 x 8192   58.0  64.6  64.5  65.4  78.5  83.1
+  const bool fit = 2 * stage_bytes <= 108 * 1024;
+  int groups = 2;
+  double best = 0.0;
+  p.split = 0;
+  for (const int S : {1, 2, 3, 4, 6, 8}) {
+    if (S > stages_all) break;
+    const int64_t ctas = units * S;
+    const bool alone = ctas <= sms || !fit;
+    const double fixed = 4.0 + (S > 1 ? 1.0 : 0.0) + (S == 8 && !alone ? 1.0 : 0.0);
+    const double cost = (double)ceil_div(ctas, alone ? sms : 2 * sms) *
+                        ((alone ? 1.0 : 1.75) * (double)ceil_div(stages_all, S) + fixed);
+    if (p.split == 0 || cost < best) {
+      best = cost;
+      p.split = S;
+      groups = alone ? 4 : 2;
+    }
+  }
+  const int room = (groups == 2 ? 108 : 216) * 1024;
+  p.stages = room / stage_bytes;
+  if (p.stages > QMAX_STAGES) p.stages = QMAX_STAGES;
+  // all of tensor memory: the CTA has to have the SM to itself, and a ring that is too large for two
+  p.ring_bytes = groups == 2 ? p.stages * stage_bytes : room;
+  p.tmem_cols = 32;
+  while (p.tmem_cols < p.N + 2 * groups * 32) p.tmem_cols *= 2;
+  return groups == 2 ? launch_tiles<2>(map_w, map_x, p, tiles_t, stream)
+                     : launch_tiles<4>(map_w, map_x, p, tiles_t, stream);
 }
 
 }  // namespace thanos
