@@ -89,9 +89,9 @@ thanos_status_t packed_activations_ok(const PackedActivations& x, int64_t b) {
   return THANOS_OK;
 }
 
-size_t unpacked_bytes(int64_t rows, int64_t b, thanos_dtype_t dtype) {
-  return round_up((size_t)rows * round_up((size_t)b, PACKED_LINE) * (dtype == THANOS_BF16 ? 2 : 4),
-                  256);
+// Room for packed weights in bf16, behind what the call needs itself (fp32 calls have room for planes).
+size_t packed_extra_bytes(int64_t c, int64_t b, thanos_dtype_t dtype) {
+  return dtype == THANOS_BF16 ? round_up((size_t)c * round_up((size_t)b, PACKED_LINE) * 2, 256) : 0;
 }
 
 // Where W is: as it is, or packed (W null).
@@ -156,13 +156,11 @@ thanos_status_t forward_call(void* Y, int64_t ldy, float* V, const void* X, int6
   a.r = n_adapters > 0 ? r : 1;
   if (w.is_packed) {
     if (packed_few_tokens(a)) return packed_forward_few(a, w.packed, workspace, stream);
-    // many tokens: the weights are read back once, the product is theirs
-    const size_t extra = unpacked_bytes(c, b, dtype);
-    void* full = static_cast<char*>(workspace) + (need - extra);
-    a.W = full;
+    // many tokens: the weights are unpacked once, the product is theirs
+    a.packed = &w.packed;
+    ws_bytes = need - packed_extra_bytes(c, b, dtype);
+    a.unpacked = static_cast<char*>(workspace) + ws_bytes;
     a.ldw = (int64_t)round_up((size_t)b, PACKED_LINE);
-    THANOS_TRY(unpack_weights(full, a.ldw, dtype, w.packed, c, b, stream));
-    ws_bytes = need - extra;
   }
   return adapter_forward_impl(a, workspace, ws_bytes, stream);
 }
@@ -235,11 +233,10 @@ thanos_status_t backward_call(void* dX, int64_t lddx, float* dA, float* dB, int3
     a.lde = x8.lde;
   }
   if (w.is_packed) {
-    ws_bytes = need - unpacked_bytes(c, b, dtype);
-    void* full = static_cast<char*>(workspace) + ws_bytes;
-    a.W = full;
+    a.packed = &w.packed;
+    ws_bytes = need - packed_extra_bytes(c, b, dtype);
+    a.unpacked = static_cast<char*>(workspace) + ws_bytes;
     a.ldw = (int64_t)round_up((size_t)b, PACKED_LINE);
-    if (dX) THANOS_TRY(unpack_weights(full, a.ldw, dtype, w.packed, c, b, stream));
   }
   return adapter_backward_impl(a, workspace, ws_bytes, stream);
 }
@@ -292,7 +289,7 @@ size_t thanos_adapter_packed_workspace_bytes(int32_t backward, int32_t packed_w,
   a.dtype = dtype;
   if (!backward && packed_w && packed_few_tokens(a)) return packed_few_workspace_bytes(n_tok, a.r);
   return round_up(thanos_adapter_workspace_bytes(backward, n_tok, c, b, n_adapters, r, dtype), 256) +
-         (packed_w ? unpacked_bytes(c, b, dtype) : 0);
+         (packed_w ? packed_extra_bytes(c, b, dtype) : 0);
 }
 
 thanos_status_t thanos_adapter_forward_packed(void* Y, int64_t ldy, float* V, const void* X,

@@ -3,6 +3,7 @@
 //   U[t] = s_i dY[t] B_i,  dX[t] = dY[t] W + U[t] A_i,  dA_i = sum_t U[t]^T X[t],
 //   dB_i = s_i sum_t dY[t]^T V[t]
 #include "adapter_grad.cuh"
+#include "packed.cuh"
 #include "proj_gemm.cuh"
 #include "recovery.cuh"
 #include "tc_common.cuh"
@@ -265,8 +266,11 @@ thanos_status_t forward16(const AdapterArgs& a, void* workspace, size_t ws_bytes
   g.out = a.out;
   g.ldo = a.ldo;
   const int nt = proj_pair_tile(a.T, a.c);
+  if (a.packed) g.A = a.unpacked;
   if (a.n == 0) {
     THANOS_CUDA(cudaMemsetAsync(L.status, 0, 16, stream));
+    if (a.packed)
+      THANOS_TRY(unpack_weights(a.unpacked, a.ldw, a.dtype, *a.packed, a.c, a.b, stream));
     return proj_gemm(g, stream);
   }
   FrontParams f = {};
@@ -319,11 +323,13 @@ thanos_status_t forward16(const AdapterArgs& a, void* workspace, size_t ws_bytes
     f.beside = 1;
     if (f.n_list + f.n_copy > 0) THANOS_TRY(launch_front(f, 0, stream));
   }
+  if (a.packed)
+    THANOS_TRY(unpack_weights(a.unpacked, a.ldw, a.dtype, *a.packed, a.c, a.b, stream, true));
   g.scale = a.scale;
   g.P = pad ? static_cast<const void*>(L.copy) : a.B;
   g.ldp = pad ? (int64_t)round_up(a.r, 8) : a.r;
   g.p_adapter = a.c * g.ldp;
-  g.early = !handful(a);
+  g.early = !handful(a) && !a.packed;
   return proj_gemm(g, stream);
 }
 
@@ -342,6 +348,7 @@ thanos_status_t backward16(const AdapterArgs& a, void* workspace, size_t ws_byte
   g.K = (int)a.c;
   g.A = a.W;
   g.lda = a.ldw;
+  if (a.packed) g.A = a.unpacked;
   g.a_mn = 1;
   g.B = dY;
   g.ldb = lddy;
@@ -415,8 +422,10 @@ thanos_status_t backward16(const AdapterArgs& a, void* workspace, size_t ws_byte
     g.P = a.A;
     g.ldp = a.b;
     g.p_adapter = (int64_t)a.r * a.b;
-    g.early = copy_dy ? 0 : 1;
+    g.early = copy_dy || a.packed ? 0 : 1;
   }
+  if (a.out && a.packed)
+    THANOS_TRY(unpack_weights(a.unpacked, a.ldw, a.dtype, *a.packed, a.c, a.b, stream, a.n > 0));
   if (a.out) THANOS_TRY(proj_gemm(g, stream));
   if (a.dA) {
     AdapterGradSide sa, sb;

@@ -11,6 +11,7 @@
 //   grad_f32_kernel     both gradients: 32 features and up to 8 ranks of one adapter per CTA, eight
 //                       warps share the adapter's tokens, in the order of sort_tokens
 #include "adapter_grad.cuh"
+#include "packed.cuh"
 #include "proj_gemm.cuh"
 #include "recovery.cuh"
 
@@ -415,7 +416,7 @@ thanos_status_t adapter_f32(bool back, const AdapterArgs& a, void* workspace, si
     f.in.ldp = L.k8;
     f.in.blocks = split_blocks(a.T);
   }
-  if (a.out) {
+  if (a.out && !a.packed) {
     f.w.src = static_cast<const float*>(a.W);
     f.w.ld = a.ldw;
     f.w.rows = a.c;
@@ -456,6 +457,9 @@ thanos_status_t adapter_f32(bool back, const AdapterArgs& a, void* workspace, si
   if (blocks > 0) {
     front_f32_kernel<<<(unsigned)blocks, 256, 0, stream>>>(f);
     THANOS_CHECK_LAUNCH();
+    // packed weights are bf16 numbers: one plane
+    if (a.out && a.packed)
+      THANOS_TRY(unpack_weights(L.w, L.w8, THANOS_BF16, *a.packed, a.c, a.b, stream, true));
     if (tc) {
       ProjArgs s;
       s.epi = PROJ_SHRINK32;
@@ -489,6 +493,7 @@ thanos_status_t adapter_f32(bool back, const AdapterArgs& a, void* workspace, si
     g.A = L.w;
     g.lda = L.w8;
     g.a_batch = a.c * L.w8;
+    g.one_plane = a.packed ? 1 : 0;
     g.a_mn = back ? 1 : 0;
     g.B = L.in;
     g.ldb = L.k8;

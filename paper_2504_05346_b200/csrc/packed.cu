@@ -11,6 +11,7 @@
 // Bound by memory: every value is read and written once.  A thread takes eight columns; the lanes of a
 // group share its largest value by shuffles.
 #include "packed.cuh"
+#include "proj_gemm.cuh"
 
 namespace thanos {
 namespace {
@@ -281,9 +282,9 @@ __global__ void __launch_bounds__(PT) unpack_w_kernel(T* __restrict__ W, int64_t
                                                       const bf16* __restrict__ scales, int64_t c,
                                                       int b, int group) {
   const Place at;
-  if (at.col >= b) return;
+  grid_dependents_launch();
   const Nibbles nib;
-  for (int64_t row0 = at.row; row0 < c; row0 += at.rows) {
+  for (int64_t row0 = at.row; at.col < b && row0 < c; row0 += at.rows) {
     uint32_t w[RB], s[RB];
 #pragma unroll
     for (int u = 0; u < RB; ++u) {
@@ -322,6 +323,8 @@ __global__ void __launch_bounds__(PT) unpack_w_kernel(T* __restrict__ W, int64_t
       }
     }
   }
+  // whoever waits for this launch finds the one before it finished too
+  if (blockIdx.x == 0 && blockIdx.y == 0) grid_dependency_wait();
 }
 
 // Vectors of a row beside one another (a power of two of at least a group's lanes), rows above.
@@ -359,16 +362,22 @@ thanos_status_t pack_weights(uint8_t* codes, int64_t ldq, bf16* scales, const vo
 }
 
 thanos_status_t unpack_weights(void* W, int64_t ldw, thanos_dtype_t dtype, const PackedWeights& w,
-                               int64_t c, int64_t b, cudaStream_t stream) {
-  dim3 grid, block;
-  shape_of(c, b, grid, block);
+                               int64_t c, int64_t b, cudaStream_t stream, bool beside) {
+  cudaLaunchConfig_t cfg = {};
+  shape_of(c, b, cfg.gridDim, cfg.blockDim);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = beside ? 1 : 0;
+  count_launch();
   if (dtype == THANOS_BF16)
-    unpack_w_kernel<bf16><<<grid, block, 0, stream>>>(static_cast<bf16*>(W), ldw, w.codes, w.ldq,
-                                                      w.scales, c, (int)b, w.group);
+    THANOS_CUDA(cudaLaunchKernelEx(&cfg, unpack_w_kernel<bf16>, static_cast<bf16*>(W), ldw, w.codes,
+                                   w.ldq, w.scales, c, (int)b, w.group));
   else
-    unpack_w_kernel<float><<<grid, block, 0, stream>>>(static_cast<float*>(W), ldw, w.codes, w.ldq,
-                                                       w.scales, c, (int)b, w.group);
-  THANOS_CHECK_LAUNCH();
+    THANOS_CUDA(cudaLaunchKernelEx(&cfg, unpack_w_kernel<float>, static_cast<float*>(W), ldw, w.codes,
+                                   w.ldq, w.scales, c, (int)b, w.group));
   return THANOS_OK;
 }
 

@@ -43,8 +43,10 @@ struct Nibbles {
 thanos_status_t pack_weights(uint8_t* codes, int64_t ldq, __nv_bfloat16* scales, const void* W,
                              int64_t ldw, thanos_dtype_t dtype, int64_t c, int64_t b, int group,
                              cudaStream_t stream);
+// beside: starts while the launch before it in the stream runs, on whose results it does not depend, and
+// is complete when both are.
 thanos_status_t unpack_weights(void* W, int64_t ldw, thanos_dtype_t dtype, const PackedWeights& w,
-                               int64_t c, int64_t b, cudaStream_t stream);
+                               int64_t c, int64_t b, cudaStream_t stream, bool beside = false);
 thanos_status_t pack_activations(int8_t* codes, int64_t ldc, uint8_t* exps, int64_t lde,
                                  const void* X, int64_t ldx, thanos_dtype_t dtype, int64_t T,
                                  int64_t b, cudaStream_t stream);

@@ -37,6 +37,7 @@ constexpr int FACTOR_BYTES = 128 * 16 * 4;    // 16 ranks of up to 128 tokens, f
 
 struct Params {
   int M, N, K, tiles_m, tiles_n, nt, stages, splits, batch_z, ring_bytes, tmem_cols;
+  int products;                  // of planes: six, or three where A is one plane
   int symmetric, f16, early, first, fine, add;
   int32_t* status;
   // adapter part
@@ -799,7 +800,7 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
   const int planes = ITER && p.fine ? 2 : 1;  // stages of a k step: hi planes, then lo planes
   // this CTA's k blocks; three planes: all six products of planes of each, one product after another
   const int b0 = (int)((int64_t)nk1 * rank / S), b1 = (int)((int64_t)nk1 * (rank + 1) / S);
-  const int ks0 = PLANES ? 6 * b0 : b0, ks1 = PLANES ? 6 * b1 : b1;
+  const int ks0 = PLANES ? p.products * b0 : b0, ks1 = PLANES ? p.products * b1 : b1;
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
     if (!p.early) grid_dependency_wait();
@@ -816,7 +817,7 @@ tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
         if (PLANES) {
           const int combo = (ks - ks0) / (b1 - b0);
           k0 = (b0 + ks - ks0 - combo * (b1 - b0)) * BK;
-          plane_pair(combo, za, zb);
+          plane_pair(p.products == 6 ? combo : 2 * combo + 1, za, zb);  // hl, hm, hh of the six
         }
         mbar_expect_tx(full_bar(s), stage_bytes);
         if (AMN) {
@@ -1792,8 +1793,8 @@ TileShape tile_shape(int64_t M, int64_t N, int64_t batch, int64_t blocks, int lo
   const double column = epi >= PROJ_POLY && epi <= PROJ_FINAL ? 700.0 : 400.0;
   TileShape best = {128, 1};
   double least = 0.0;
-  const int64_t unit = loads == 6 ? 6 : 1, parts = blocks * loads / unit;
-  const int64_t most = loads == 6 ? blocks : parts / 4;   // slices that the work is enough for
+  const int64_t unit = loads >= 3 ? loads : 1, parts = blocks * loads / unit;
+  const int64_t most = loads >= 3 ? blocks : parts / 4;   // slices that the work is enough for
   const int64_t need = epi == PROJ_OUT32 ? ceil_div(blocks, 16) : 1;
   for (int nt = 128; nt >= 32; nt /= 2) {
     if (nt > 32 && N <= nt / 2) continue;   // the next narrower one holds all of N
@@ -1836,7 +1837,7 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
   const bool f32 = a.epi >= PROJ_OUT32;
   const bool pairs = a.epi != PROJ_SHRINK && !f32 && use_pairs(a.M, a.N, a.batch, symmetric);
   const TileShape shape =
-      pairs ? TileShape{PTM, 1} : tile_shape(a.M, a.N, a.batch, ceil_div(a.K, BK), f32 ? 6 : a.fine ? 2 : 1,
+      pairs ? TileShape{PTM, 1} : tile_shape(a.M, a.N, a.batch, ceil_div(a.K, BK), f32 ? (a.one_plane ? 3 : 6) : a.fine ? 2 : 1,
                                                  symmetric, a.epi);
   if (a.epi == PROJ_GRAM && a.fine && ceil_div(a.K, shape.splits) > LONGEST_GRAM) {
     const int64_t pieces = ceil_div(ceil_div(a.K, shape.splits), LONGEST_GRAM), blocks = ceil_div(a.K, BK);
@@ -1856,6 +1857,7 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
   p.tiles_m = (a.M + (pairs ? PTM : TM) - 1) / (pairs ? PTM : TM);
   p.tiles_n = (a.N + p.nt - 1) / p.nt;
   p.batch_z = a.batch;
+  p.products = a.one_plane ? 3 : 6;
   p.symmetric = symmetric;
   p.f16 = a.f16;
   p.early = a.early;
@@ -1913,9 +1915,9 @@ thanos_status_t proj_gemm(const ProjArgs& a, cudaStream_t stream) {
 
   CUtensorMap mA, mB, mP;
   const CUtensorMapSwizzle sw = CU_TENSOR_MAP_SWIZZLE_128B;
-  const int64_t slabs = f32 ? 3 : a.fine ? 2 * a.batch : a.batch;
-  const bool okA = a.a_mn ? make_map3(&mA, a.A, a.f16, a.M, a.K, a.lda, slabs, a.a_batch, 64, BK, sw)
-                          : make_map3(&mA, a.A, a.f16, a.K, a.M, a.lda, slabs, a.a_batch, BK, TM, sw);
+  const int64_t slabs = f32 ? 3 : a.fine ? 2 * a.batch : a.batch, slabs_a = a.one_plane ? 1 : slabs;
+  const bool okA = a.a_mn ? make_map3(&mA, a.A, a.f16, a.M, a.K, a.lda, slabs_a, a.a_batch, 64, BK, sw)
+                          : make_map3(&mA, a.A, a.f16, a.K, a.M, a.lda, slabs_a, a.a_batch, BK, TM, sw);
   if (!okA || !make_map3(&mB, a.B, a.f16, a.K, a.N, a.ldb, slabs, a.b_batch, BK,
                          pairs ? p.nt / 2 : p.nt, sw))
     return THANOS_ERR_CUDA;

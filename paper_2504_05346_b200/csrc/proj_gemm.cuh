@@ -47,6 +47,7 @@ struct ProjArgs {
   void* out = nullptr;           // [N, ldo], bf16 (OUT32: fp32)
   int64_t ldo = 0;
   int add = 0;                   // OUT32: to what is there
+  int one_plane = 0;             // OUT32: A is bf16, one plane, and three products are enough
   float* V = nullptr;            // [N, r]: PROJ_OUT reads it (forward: V, backward: U); SHRINK writes
   __nv_bfloat16* planes = nullptr;  // SHRINK: V also as three bf16 planes, [N, 3 r16] (or null)
   const int32_t* index = nullptr;

@@ -5,6 +5,8 @@
 
 namespace thanos {
 
+struct PackedWeights;
+
 struct AdapterArgs {
   // forward: out = Y [T, c], in = X [T, b]; backward: out = dX [T, b], in = dY [T, c]
   void* out = nullptr;
@@ -19,6 +21,8 @@ struct AdapterArgs {
   int64_t lde = 0;
   const void* W = nullptr;
   int64_t ldw = 0;
+  const PackedWeights* packed = nullptr;  // in the place of W
+  void* unpacked = nullptr;     // room for them in bf16, rows of ldw (fp32 products have their own)
   const void* A = nullptr;
   const void* B = nullptr;
   const int32_t* index = nullptr;
