@@ -1,5 +1,6 @@
 """Prune one linear layer and win its answers back: calibrate -> prune 2:4 -> tune the weights that
-stay -> train an adapter per task -> serve tokens of all tasks in one call.
+stay -> train an adapter per task -> serve tokens of all tasks in one call -> keep it small: weights in
+4 bits, training from activations in 8 bits, judged by the log probabilities of the teacher's tokens.
 
     python examples/recover_layer.py [--rows 2048 --cols 2048 --tokens 4096 --tasks 4 --rank 16]
 
@@ -28,6 +29,7 @@ def parse(argv=None):
     ap.add_argument("--rank", type=int, default=16)
     ap.add_argument("--weight-steps", type=int, default=30)
     ap.add_argument("--adapter-steps", type=int, default=40)
+    ap.add_argument("--likelihood-steps", type=int, default=10)
     ap.add_argument("--seed", type=int, default=0)
     return ap.parse_args(argv)
 
@@ -106,10 +108,38 @@ def main(argv=None):
     alone = torch.cat([thanos.adapter_forward(x[t:t + 1], W, Ab, Bb, who[t:t + 1], scale)[0]
                        for t in range(n + 1)])
     out["served together against alone"] = relative(together, alone)
+
+    # ---- keep it small: the frozen weights in 4 bits (their zeros stay zeros), the activations of a
+    # training batch in 8.  The layer is taken for an output head: its rows are the tokens of a
+    # vocabulary, and a task's loss is the log probability of the token that its teacher prefers.
+    W4 = thanos.pack_weights(W)
+    assert not thanos.unpack_weights(W4)[mask != 0].any()
+    out["tasks in 4 bits"] = relative(thanos.adapter_forward(xt, W4, Ab, Bb, task_t, scale)[0], want_t)
+    wanted = want_t.float().argmax(1)
+    judge = lambda Z: -thanos.token_logprobs(Z, wanted).logp.mean().item()  # noqa: E731
+    out["loss before"] = judge(thanos.adapter_forward(xt, W4, Ab, Bb, task_t, scale)[0])
+    for i in range(a.likelihood_steps):
+        x, task, want = batch(T)
+        token = want.float().argmax(1)
+        lr = 0.02 * (1 - i / a.likelihood_steps)
+        Ab, Bb = A.to(bf), B.to(bf)
+        Z, V = thanos.adapter_forward(x, W4, Ab, Bb, task, scale)
+        kept = thanos.pack_activations(x)
+        f = thanos.token_logprobs(Z, token)
+        dlogp = torch.full((T,), -1.0 / T, device="cuda")
+        dZ = thanos.token_logprobs_backward(Z, f.stats, token, dlogp, out=Z)
+        _, dA, dB = thanos.adapter_backward(dZ, kept, V, W4, Ab, Bb, task, scale, need_dx=False)
+        thanos.orthogonal_step(A, mA, dA, lr=lr, momentum=0.9, W_out=A, M_out=mA)
+        thanos.orthogonal_step(B, mB, dB, lr=lr, momentum=0.9, W_out=B, M_out=mB)
+    Z = thanos.adapter_forward(xt, W4, A.to(bf), B.to(bf), task_t, scale)[0]
+    out["loss after"] = judge(Z)
+    out["teacher's token among the first five"] = (
+        thanos.token_logprobs(Z, k=min(5, c)).top_index == wanted[:, None]).any(1).float().mean().item()
     torch.cuda.synchronize()
     return out
 
 
 if __name__ == "__main__":
     for name, value in main().items():
-        print("%-32s relative error %.4f" % (name, value))
+        kind = "" if "loss" in name or "five" in name else "relative error "
+        print("%-38s %s%.4f" % (name, kind, value))

@@ -39,7 +39,8 @@ def _digest():
         if os.path.isfile(p):
             h.update(f.encode())
             h.update(open(p, "rb").read())
-    h.update(" ".join(NVCC_FLAGS).encode())
+    # flags, not folders: a built tree may be moved
+    h.update(" ".join(f for f in NVCC_FLAGS if f not in (INCLUDE, CSRC)).encode())
     h.update((sys.version + importlib.metadata.version("torch")).encode())
     return h.hexdigest()
 

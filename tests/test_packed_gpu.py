@@ -408,3 +408,85 @@ def test_offsets_beyond_32_bits(T):
     Xl = X.repeat(2, 1)
     T.adapter_forward(Xl, part, out=out[2044:])
     assert torch.equal(out[2044:], T.adapter_forward(Xl, part)[0])
+
+
+MORE = [
+    # T, c, b, n, r, order: every kernel, slice of k and width of token tiles
+    (1, 5000, 136, 2, 4, "one"),
+    (8, 4737, 4200, 3, 8, "mixed"),
+    (12, 4800, 264, 0, 0, "one"),
+    (16, 6000, 2056, 4, 12, "mixed"),
+    (20, 100, 16400, 2, 8, "mixed"),
+    (48, 12000, 520, 3, 16, "mixed"),
+    (80, 300, 4104, 5, 16, "mixed"),
+    (100, 2000, 1096, 0, 0, "one"),
+    (128, 1000, 1032, 3, 20, "mixed"),
+    (200, 260, 2056, 0, 0, "one"),
+    (256, 129, 72, 0, 0, "one"),
+    (256, 700, 264, 2, 8, "mixed"),
+    (3, 200, 65536, 1, 4, "one"),
+    (40, 200, 65536, 1, 4, "one"),
+]
+
+
+@BOTH
+@pytest.mark.parametrize("group", [64, 128])
+@pytest.mark.parametrize("shape", MORE, ids=lambda s: "x".join(map(str, s)))
+def test_forward_by_every_kernel(T, shape, group, dtype):
+    """As test_forward; sums of 65536 terms in fp32 may be off by a few more roundings: 2e-5."""
+    Tn, c, b, n, r, order = shape
+    X, P, W, A, B, index, scale, _ = operands(T, shape, dtype, group, seed=Tn + c, pad=0)
+    out = torch.full((Tn + 1, c + 5), math.nan, dtype=dtype, device=DEV)
+    Y, V = T.adapter_forward(X, P, A, B, index, scale, out=out[:Tn, :c], check=True)
+    if n:
+        Yr, Vr = ref_forward(X, W, A, B, index, scale)
+        assert rel(V, Vr) <= TOL[F32]
+    else:
+        Yr = X.double() @ W.double().T
+    tol = 2e-5 if dtype == F32 and b > 10000 else TOL[dtype]
+    assert rel(Y, Yr) <= tol
+    err = (Y.double() - Yr).norm(dim=1) / Yr.norm(dim=1)
+    assert err.max().item() <= 2 * tol
+    worst = (Y.double() - Yr).abs().max(0).values          # and no row of weights by itself
+    assert bool((worst <= 0.05 * Yr.abs().max()).all())
+    assert bool(out[Tn:].isnan().all()) and bool(out[:, c:].isnan().all())
+    again, _ = T.adapter_forward(X, P, A, B, index, scale)
+    assert torch.equal(again, Y)
+
+
+def test_more_rows_than_a_grid_is_high(T):
+    """65535 rounds of four rows and more: the last rows are packed and unpacked as they are alone."""
+    n, b = 4 * 65535 + 700, 2056
+    g = torch.Generator(device=DEV).manual_seed(9)
+    X = torch.empty((n, b), dtype=BF16, device=DEV).normal_(generator=g)
+    P, X8 = T.pack_weights(X, 64), T.pack_activations(X)
+    W, U = T.unpack_weights(P), T.unpack_activations(X8)
+    for rows in (slice(0, 50), slice(n - 900, n)):
+        part = X[rows].contiguous()
+        Pp, Xp = T.pack_weights(part, 64), T.pack_activations(part)
+        assert torch.equal(P.codes[rows], Pp.codes) and torch.equal(P.scales[:, rows], Pp.scales)
+        assert torch.equal(X8.codes[rows], Xp.codes) and torch.equal(X8.exps[rows], Xp.exps)
+        assert torch.equal(W[rows], T.unpack_weights(Pp))
+        assert torch.equal(U[rows], T.unpack_activations(Xp))
+
+
+def test_every_scale_and_every_code(T):
+    """All largest values of eight bits, and beside each all smaller ones down to a 32nd of a step: the
+    ties that a quotient of eight bits over five can be, both signs, against float64."""
+    tops = (torch.arange(128, device=DEV).float() / 128 + 1).to(BF16)          # [1, 2)
+    fine = torch.cat([(torch.arange(128, device=DEV).float() / 128 + 1) * 2.0 ** -e for e in range(10)])
+    cols = -(-fine.numel() // 63)
+    grid = torch.zeros(cols * 63, device=DEV)
+    grid[:fine.numel()] = fine
+    W = torch.zeros((128, cols, 64), device=DEV)
+    W[:, :, 0] = tops[:, None].float()
+    W[:, :, 1:] = torch.minimum(grid.view(1, cols, 63), tops.float()[:, None, None])
+    W = torch.cat([W.view(128, -1), -W.view(128, -1)]).to(BF16).contiguous()
+    for k in (1.0, 2.0 ** 100, 2.0 ** -100):
+        for dtype in (BF16, F32):
+            Wk = (W.float() * k).to(dtype)
+            P = T.pack_weights(Wk, 64)
+            codes, scales, values = ref_weights(Wk, 64)
+            assert torch.equal(P.scales.double(), scales)
+            assert torch.equal(nibbles(P)[:, :Wk.shape[1]], codes)
+            assert torch.equal(T.unpack_weights(P, F32).double(), values)
