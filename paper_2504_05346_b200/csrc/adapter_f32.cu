@@ -272,9 +272,18 @@ __global__ void __launch_bounds__(256) grad_f32_kernel(const Grad32Params p) {
       __syncthreads();
       for (int e = threadIdx.x; e < nq; e += 256) tok[e] = p.order[q0 + e];
       __syncthreads();
-      for (int e = threadIdx.x; e < nq * RANKS; e += 256) {
-        const int j = e & (RANKS - 1);
-        fac[e] = j < nj ? sd.R[(int64_t)tok[e / RANKS] * p.r + j0 + j] : 0.f;
+      // eight loads in flight (one at a time: 34 us for 1000 tokens, 768 + 768 features, three adapters)
+      const int j = threadIdx.x & (RANKS - 1);   // 256 is a multiple of RANKS
+      for (int e0 = threadIdx.x; e0 < nq * RANKS; e0 += 256 * 8) {
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const int e = e0 + 256 * u;
+          v[u] = e < nq * RANKS && j < nj ? sd.R[(int64_t)tok[e / RANKS] * p.r + j0 + j] : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+          if (e0 + 256 * u < nq * RANKS) fac[e0 + 256 * u] = v[u];
       }
       if (sd.Z8) {
         const int group = blockIdx.x;   // side 0: a CTA's 32 features are one group
@@ -282,24 +291,35 @@ __global__ void __launch_bounds__(256) grad_f32_kernel(const Grad32Params p) {
           step[e] = __uint_as_float((uint32_t)sd.exps[(int64_t)tok[e] * sd.lde + group] << 23);
       }
       __syncthreads();
-      if (sd.Z8) {
-        if (f < sd.F) {
-#pragma unroll 8
-          for (int q = g; q < nq; q += 8) {
-            // the byte with its sign turned is code + 128, as the low bits of 2^23 a float; a conversion
+      if (f < sd.F) {
+        // sixteen tokens of a warp in flight, added in their order
+        constexpr int FLIGHT = 16;
+        for (int q0 = g; q0 < nq; q0 += 8 * FLIGHT) {
+          float z[FLIGHT];
+          if (sd.Z8) {
+            // a byte with its sign turned is code + 128, as the low bits of 2^23 a float; a conversion
             // instruction takes as long as the eight products
-            const uint32_t u = (uint8_t)sd.Z8[(int64_t)tok[q] * sd.ldz + f];
-            const float z = (__uint_as_float((u ^ 0x80u) | 0x4B000000u) - 8388736.f) * step[q];
+            uint32_t u[FLIGHT];
 #pragma unroll
-            for (int j = 0; j < RANKS; ++j) s[j] = fmaf(fac[q * RANKS + j], z, s[j]);
+            for (int k = 0; k < FLIGHT; ++k)
+              u[k] = q0 + 8 * k < nq ? (uint8_t)sd.Z8[(int64_t)tok[q0 + 8 * k] * sd.ldz + f] : 0x80u;
+#pragma unroll
+            for (int k = 0; k < FLIGHT; ++k)
+              z[k] = (__uint_as_float((u[k] ^ 0x80u) | 0x4B000000u) - 8388736.f) *
+                     (q0 + 8 * k < nq ? step[q0 + 8 * k] : 0.f);
+          } else {
+#pragma unroll
+            for (int k = 0; k < FLIGHT; ++k)
+              z[k] = q0 + 8 * k < nq ? sd.Z[(int64_t)tok[q0 + 8 * k] * sd.ldz + f] : 0.f;
           }
-        }
-      } else if (f < sd.F) {
-#pragma unroll 8
-        for (int q = g; q < nq; q += 8) {
-          const float z = sd.Z[(int64_t)tok[q] * sd.ldz + f];
 #pragma unroll
-          for (int j = 0; j < RANKS; ++j) s[j] = fmaf(fac[q * RANKS + j], z, s[j]);
+          for (int k = 0; k < FLIGHT; ++k) {
+            if (q0 + 8 * k < nq) {
+#pragma unroll
+              for (int j = 0; j < RANKS; ++j)
+                s[j] = fmaf(fac[(q0 + 8 * k) * RANKS + j], z[k], s[j]);
+            }
+          }
         }
       }
 #pragma unroll
