@@ -98,7 +98,8 @@ def logits(Tn, V, dtype, seed, spread=3.0):
 
 SHAPES = [(1, 1, 1), (1, 2, 2), (3, 7, 5), (2, 8, 8), (5, 9, 3), (4, 63, 63), (7, 64, 64), (2, 65, 64),
           (9, 255, 20), (3, 1000, 16), (1, 2047, 1), (2, 8191, 64), (1, 16384, 10), (3, 32000, 8),
-          (1, 50021, 20), (2, 131072, 33), (1, 300001, 64), (600, 511, 7), (333, 10007, 5)]
+          (1, 50021, 20), (2, 131072, 33), (1, 300001, 64), (600, 511, 7), (333, 10007, 5),
+          (1184, 500, 20), (1300, 64, 64), (1200, 8190, 5), (1500, 3, 2)]
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
@@ -137,9 +138,9 @@ def test_strided_rows_that_start_anywhere(T, dtype, offset, V, ld):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
-@pytest.mark.parametrize("V", [37, 5000, 40000])
-def test_special_rows(T, V, dtype):
-    """Masked, constant and extreme rows, ties, infinities and NaN."""
+@pytest.mark.parametrize("V, times", [(37, 1), (5000, 1), (40000, 1), (37, 70), (5000, 70)])
+def test_special_rows(T, V, times, dtype):
+    """Masked, constant and extreme rows, ties, infinities and NaN; a few of them, and among many."""
     big = torch.finfo(dtype).max
     g = torch.Generator(device=DEV).manual_seed(V)
     Z = torch.randn((18, V), generator=g, device=DEV)
@@ -170,6 +171,7 @@ def test_special_rows(T, V, dtype):
     target = torch.randint(0, V, (18,), generator=g, device=DEV)
     target[5] = -7
     target[9] = -1
+    Z, target = Z.repeat(times, 1), target.repeat(times)
     for k in (0, 1, 20, 33):
         check_forward(T, Z, target, k)
     f = check_forward(T, Z, target, 5)
@@ -183,21 +185,21 @@ def test_special_rows(T, V, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
-def test_more_candidates_than_the_list_holds(T, dtype):
+@pytest.mark.parametrize("V, threads, times", [(60000, 256, 1), (7999, 128, 300)])
+def test_more_candidates_than_the_list_holds(T, V, threads, times, dtype):
     """Large values that all fall to one thread, in rising order, and many that tie with the k-th."""
-    V = 60000
     vec = 8 if dtype == BF16 else 4
     Z = torch.zeros((4, V), device=DEV)
-    own = (torch.arange(V, device=DEV) // vec) % 256 == 17       # columns of one thread
+    own = (torch.arange(V, device=DEV) // vec) % threads == 17       # columns of one thread
     Z[0, own] = 1.0 + torch.arange(int(own.sum()), device=DEV).float() / 64
-    own2 = (torch.arange(V, device=DEV) // vec) % 256 < 20
+    own2 = (torch.arange(V, device=DEV) // vec) % threads < 20
     Z[1, own2] = 2.0
-    Z[1, 59999] = 3.0
+    Z[1, V - 1] = 3.0
     Z[2, ::2] = 1.0
     Z[3] = -INF
     Z[3, 100:130] = 1.0
-    Z = Z.to(dtype)
-    target = torch.tensor([1, 2, 3, 4], device=DEV)
+    Z = Z.to(dtype).repeat(times, 1)
+    target = torch.tensor([1, 2, 3, 4], device=DEV).repeat(times)
     for k in (1, 19, 40, 64):
         check_forward(T, Z, target, k)
 
