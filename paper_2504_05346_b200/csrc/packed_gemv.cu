@@ -1,15 +1,21 @@
-// The adapted projection of few tokens on 4-bit weights:
+// The adapted projection of up to 16 tokens (fp32: 64) on 4-bit weights:
 //   Y[t] = X[t] w^T + s_i V[t] B_i^T,   V[t] = X[t] A_i^T,   w^ = code scale
 //
-// Bound by reading the weights, half a byte each.  A warp takes 16 MT rows and 8 NT tokens, and of k a
-// run of 64-column blocks; the warps of a CTA split k and add up in a fixed order (same inputs, same
-// bits).  In a block a lane reads eight bytes of each of its rows, which are 16
-// consecutive columns: which k a lane holds at which place of the operand does not matter, as long as
-// both operands agree, so the activations are read the same way, straight from memory, once per warp.
+// Floor: reading the weights, half a byte each.  A warp takes 16 MT rows and 8 NT tokens, and of k a run
+// of 64-column blocks; the warps of a CTA split k and add up in a fixed order (same inputs, same bits).
+// In a block a lane reads eight bytes of each of its rows, which are 16 consecutive columns: which k a
+// lane holds at which place of the operand does not matter, as long as both operands agree, so the
+// activations are read the same way, straight from memory, once per warp.
 //   code   (nibble | 0x4300) is the bf16 number 128 + nibble; less 136 it is the code
 //   scale  the block's products are summed apart and multiplied by the row's scale in fp32: four
 //          multiplications per 16 x 8 tile and block instead of one per weight
 // fp32 activations go as three bf16 planes (cut, not rounded: 24 bits in all), three products.
+//
+// mma.sync and not tcgen05: at this width the tensor cores are a fifth busy, and codes that go to tensor
+// memory need a permutation and a multiplication per pair more (packed_tc.cu, 16 tokens of 4096 x 4096:
+// 10.9 us, here 6.5).  What bounds it is turning codes into numbers: of some 85 instructions for 16 x 64
+// weights 42 are integer and 32 bf16 ones, at half rate both.  One token: 4096 x 4096 4.5 us, 11008 x 4096
+// 9.7, 28672 x 8192 38 us (3.2 TB/s; with everything but the arithmetic 24, with the arithmetic alone 35).
 #include "packed_few.cuh"
 
 namespace thanos {
