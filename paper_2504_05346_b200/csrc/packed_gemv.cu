@@ -12,10 +12,10 @@
 // fp32 activations go as three bf16 planes (cut, not rounded: 24 bits in all), three products.
 //
 // mma.sync and not tcgen05: at this width the tensor cores are a fifth busy, and codes that go to tensor
-// memory need a permutation and a multiplication per pair more (packed_tc.cu, 16 tokens of 4096 x 4096:
-// 10.9 us, here 6.5).  What bounds it is turning codes into numbers: of some 85 instructions for 16 x 64
-// weights 42 are integer and 32 bf16 ones, at half rate both.  One token: 4096 x 4096 4.5 us, 11008 x 4096
-// 9.7, 28672 x 8192 38 us (3.2 TB/s; with everything but the arithmetic 24, with the arithmetic alone 35).
+// memory need a permutation and a multiplication per pair more (packed_tc.cu).  What bounds it is turning
+// codes into numbers: of some 89 instructions for 16 x 64 weights 42 are integer and 32 bf16 ones, at half
+// rate both.  One token: 4096 x 4096 4.7 us, 11008 x 4096 9.6, 28672 x 8192 38 us (3.2 TB/s; without the
+// arithmetic 24, with all loads from L1 35); 16 tokens: 6.8, 12.8 and 48 us.
 #include "packed_few.cuh"
 
 namespace thanos {

@@ -15,9 +15,9 @@
 //
 // What bounds it is turning codes into bf16: 19 instructions for eight weights (shift, mask, subtract,
 // multiply, and a permutation, because a word gives the columns j and j + 4 at once and an activation's
-// columns come as they are), most of them at half rate; 128 x 64 weights take an SM some 480 clocks,
-// whether 8 or 16 warps share them, and the tensor cores are a quarter busy.  64 tokens: 4096 x 4096 10.9
-// us, 11008 x 4096 20.5, 28672 x 8192 60 us.
+// columns come as they are), most of them at half rate; 128 x 64 weights take an SM some 480 clocks, and
+// the tensor cores are a quarter busy.  64 tokens: 4096 x 4096 10.9 us, 11008 x 4096 20.6, 28672 x 8192
+// 60 us.
 #include "packed_few.cuh"
 
 namespace thanos {
