@@ -94,6 +94,18 @@ struct Call {
   void* stream() const { return c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)dev).stream(); }
 };
 
+// Makes outputs and launches, without the interpreter's lock: an allocation may wait for the device and a
+// launch for room in the stream's queue, which may be for a thread that wants the lock.
+struct Unlocked {
+  PyThreadState* state = PyEval_SaveThread();
+  ~Unlocked() { PyEval_RestoreThread(state); }
+};
+template <typename F>
+bool done(const F& call) {
+  const Unlocked unlocked;
+  return call() == THANOS_OK;
+}
+
 void* at_or_null(const Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
 PyObject* wrap(const Tensor& t) { return t.defined() ? THPVariable_Wrap(t) : Py_NewRef(Py_None); }
 
@@ -128,17 +140,21 @@ PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t given) {
   const int64_t T = Z->size(0), V = Z->size(1), ld = T > 1 ? Z->stride(0) : std::max<int64_t>(V, 1);
   const void* tp = c.dense(target, I64, {T});
   if (!c.ok) LONG_WAY();
-  Tensor logp, top_index, top_logp, stats = c.make({T, 2}, F32), entropy = c.make({T}, F32);
-  if (target) logp = c.make({T}, F32);
-  if (k > 0) {
-    top_index = c.make({T, k}, I64);
-    top_logp = c.make({T, k}, F32);
-  }
-  if (p_thanos_token_logprobs(
-          (float*)at_or_null(logp), (float*)entropy.data_ptr(), (float*)stats.data_ptr(),
-          (int64_t*)at_or_null(top_index), (float*)at_or_null(top_logp), Z->data_ptr(), ld,
-          (thanos_dtype_t)dt, (const int64_t*)tp, T, V, (int32_t)std::min<int64_t>(k, INT32_MAX),
-          c.stream()) != THANOS_OK)
+  Tensor logp, top_index, top_logp, stats, entropy;
+  if (!done([&] {
+        stats = c.make({T, 2}, F32);
+        entropy = c.make({T}, F32);
+        if (target) logp = c.make({T}, F32);
+        if (k > 0) {
+          top_index = c.make({T, k}, I64);
+          top_logp = c.make({T, k}, F32);
+        }
+        return p_thanos_token_logprobs(
+            (float*)at_or_null(logp), (float*)entropy.data_ptr(), (float*)stats.data_ptr(),
+            (int64_t*)at_or_null(top_index), (float*)at_or_null(top_logp), Z->data_ptr(), ld,
+            (thanos_dtype_t)dt, (const int64_t*)tp, T, V, (int32_t)std::min<int64_t>(k, INT32_MAX),
+            c.stream());
+      }))
     LONG_WAY();
   return tuple_of({logp, entropy, stats, top_index, top_logp});
   END_HANDLE_TH_ERRORS
@@ -166,12 +182,14 @@ PyObject* token_logprobs_backward(PyObject*, PyObject* const* a, Py_ssize_t give
   const void* pi = dtop ? c.dense(top, I64, {T, k}) : nullptr;
   const void* pd = c.dense(dtop, F32, {T, k});
   if (!c.ok) LONG_WAY();
-  const Tensor out = c.make({T, V}, Z->scalar_type());
-  if (p_thanos_token_logprobs_backward(
-          out.data_ptr(), std::max<int64_t>(V, 1), Z->data_ptr(), ld, (thanos_dtype_t)dt,
-          (const float*)ps, (const int64_t*)pt, (const float*)pl, (const float*)ph,
-          (const float*)pdh, (const int64_t*)pi, (const float*)pd, T, V, (int32_t)k,
-          c.stream()) != THANOS_OK)
+  Tensor out;
+  if (!done([&] {
+        out = c.make({T, V}, Z->scalar_type());
+        return p_thanos_token_logprobs_backward(
+            out.data_ptr(), std::max<int64_t>(V, 1), Z->data_ptr(), ld, (thanos_dtype_t)dt,
+            (const float*)ps, (const int64_t*)pt, (const float*)pl, (const float*)ph,
+            (const float*)pdh, (const int64_t*)pi, (const float*)pd, T, V, (int32_t)k, c.stream());
+      }))
     LONG_WAY();
   return wrap(out);
   END_HANDLE_TH_ERRORS
@@ -192,7 +210,7 @@ struct Weights {
     group = k.number(PyTuple_GET_ITEM(o, 2));
     b = k.number(PyTuple_GET_ITEM(o, 3));
     if (!k.ok) return;
-    k.ok = codes->scalar_type() == U8 && codes->dim() == 2 && codes->stride(1) == 1 && b > 0 &&
+    k.ok = codes->scalar_type() == U8 && codes->dim() == 2 && codes->stride(1) == 1 && b > 0 && b < (1 << 30) &&
            codes->size(1) >= (b + 63) / 64 * 32 && (group == 64 || group == 128);
     if (!k.ok) return;
     c = codes->size(0);
@@ -235,9 +253,14 @@ PyObject* pack_weights(PyObject*, PyObject* const* a, Py_ssize_t given) {
   const int64_t c = W->size(0), b = W->size(1), ldw = k.rows(W, b, W->scalar_type());
   if (!k.ok) LONG_WAY();
   const int64_t ldq = (b + 63) / 64 * 32;
-  const Tensor codes = k.make({c, ldq}, U8), scales = k.make({(b + group - 1) / group, c}, BF16);
-  if (p_thanos_pack_weights((uint8_t*)codes.data_ptr(), ldq, scales.data_ptr(), W->data_ptr(), ldw,
-                            (thanos_dtype_t)dt, c, b, (int32_t)group, k.stream()) != THANOS_OK)
+  Tensor codes, scales;
+  if (!done([&] {
+        codes = k.make({c, ldq}, U8);
+        scales = k.make({(b + group - 1) / group, c}, BF16);
+        return p_thanos_pack_weights((uint8_t*)codes.data_ptr(), ldq, scales.data_ptr(),
+                                     W->data_ptr(), ldw, (thanos_dtype_t)dt, c, b, (int32_t)group,
+                                     k.stream());
+      }))
     LONG_WAY();
   return tuple_of({codes, scales});
   END_HANDLE_TH_ERRORS
@@ -259,11 +282,14 @@ PyObject* unpack_weights(PyObject*, PyObject* const* a, Py_ssize_t given) {
   Weights w;
   w.read(k, a[0]);
   if (!k.ok) LONG_WAY();
-  const Tensor out = k.make({w.c, w.b}, type);
-  if (p_thanos_unpack_weights(out.data_ptr(), (w.b + 7) / 8 * 8,
-                              type == F32 ? THANOS_F32 : THANOS_BF16,
-                              (const uint8_t*)w.codes->data_ptr(), w.ldq, w.scales->data_ptr(), w.c,
-                              w.b, (int32_t)w.group, k.stream()) != THANOS_OK)
+  Tensor out;
+  if (!done([&] {
+        out = k.make({w.c, w.b}, type);
+        return p_thanos_unpack_weights(out.data_ptr(), (w.b + 7) / 8 * 8,
+                                       type == F32 ? THANOS_F32 : THANOS_BF16,
+                                       (const uint8_t*)w.codes->data_ptr(), w.ldq,
+                                       w.scales->data_ptr(), w.c, w.b, (int32_t)w.group, k.stream());
+      }))
     LONG_WAY();
   return wrap(out);
   END_HANDLE_TH_ERRORS
@@ -280,10 +306,14 @@ PyObject* pack_activations(PyObject*, PyObject* const* a, Py_ssize_t given) {
   const int64_t T = X->size(0), b = X->size(1), ldx = k.rows(X, b, X->scalar_type());
   if (!k.ok) LONG_WAY();
   const int64_t groups = (b + 31) / 32, ldc = (b + 15) / 16 * 16, lde = (groups + 3) / 4 * 4;
-  const Tensor codes = k.make({T, ldc}, I8), exps = k.make({T, lde}, U8);
-  if (p_thanos_pack_activations((int8_t*)codes.data_ptr(), ldc, (uint8_t*)exps.data_ptr(), lde,
-                                X->data_ptr(), ldx, (thanos_dtype_t)dt, T, b,
-                                k.stream()) != THANOS_OK)
+  Tensor codes, exps;
+  if (!done([&] {
+        codes = k.make({T, ldc}, I8);
+        exps = k.make({T, lde}, U8);
+        return p_thanos_pack_activations((int8_t*)codes.data_ptr(), ldc, (uint8_t*)exps.data_ptr(),
+                                         lde, X->data_ptr(), ldx, (thanos_dtype_t)dt, T, b,
+                                         k.stream());
+      }))
     LONG_WAY();
   return tuple_of({ldc == b ? codes : codes.narrow(1, 0, b),
                    lde == groups ? exps : exps.narrow(1, 0, groups)});
@@ -303,12 +333,15 @@ PyObject* unpack_activations(PyObject*, PyObject* const* a, Py_ssize_t given) {
   Activations x;
   x.read(k, a[0], b);
   if (!k.ok) LONG_WAY();
-  const Tensor out = k.make({x.T, b}, type);
-  if (p_thanos_unpack_activations(out.data_ptr(), (b + 7) / 8 * 8,
-                                  type == F32 ? THANOS_F32 : THANOS_BF16,
-                                  (const int8_t*)x.codes->data_ptr(), x.ldc,
-                                  (const uint8_t*)x.exps->data_ptr(), x.lde, x.T, b,
-                                  k.stream()) != THANOS_OK)
+  Tensor out;
+  if (!done([&] {
+        out = k.make({x.T, b}, type);
+        return p_thanos_unpack_activations(out.data_ptr(), (b + 7) / 8 * 8,
+                                           type == F32 ? THANOS_F32 : THANOS_BF16,
+                                           (const int8_t*)x.codes->data_ptr(), x.ldc,
+                                           (const uint8_t*)x.exps->data_ptr(), x.lde, x.T, b,
+                                           k.stream());
+      }))
     LONG_WAY();
   return wrap(out);
   END_HANDLE_TH_ERRORS
@@ -381,23 +414,26 @@ PyObject* adapter_forward(PyObject*, PyObject* const* a, Py_ssize_t given) {
           ? p_thanos_adapter_packed_workspace_bytes(0, 1, 0, p.T, p.c, p.b, p.n, (int32_t)p.r, dt)
           : p_thanos_adapter_workspace_bytes(0, p.T, p.c, p.b, p.n, (int32_t)p.r, dt);
   if (need == 0) LONG_WAY();
-  Tensor V;
-  const Tensor Y = k.make({p.T, p.c}, X->scalar_type());
-  if (p.n > 0) V = k.make({p.T, p.r}, F32);
-  const Tensor ws = k.make({(int64_t)need}, U8);
+  Tensor Y, V;
   const int64_t ldy = p.T > 1 ? p.c : (p.c + 7) / 8 * 8;
-  const thanos_status_t st =
-      p.is_packed
-          ? p_thanos_adapter_forward_packed(
-                Y.data_ptr(), ldy, (float*)at_or_null(V), X->data_ptr(), ldx,
-                (const uint8_t*)p.weights(), p.ldw, p.packed.scales->data_ptr(),
-                (int32_t)p.packed.group, p.A, p.B, (const int32_t*)p.index, (const float*)p.scale,
-                dt, p.T, p.c, p.b, p.n, (int32_t)p.r, ws.data_ptr(), need, k.stream())
-          : p_thanos_adapter_forward(Y.data_ptr(), ldy, (float*)at_or_null(V), X->data_ptr(), ldx,
-                                     p.weights(), p.ldw, p.A, p.B, (const int32_t*)p.index,
-                                     (const float*)p.scale, dt, p.T, p.c, p.b, p.n, (int32_t)p.r,
-                                     ws.data_ptr(), need, k.stream());
-  if (st != THANOS_OK) LONG_WAY();
+  if (!done([&] {
+        Y = k.make({p.T, p.c}, X->scalar_type());
+        if (p.n > 0) V = k.make({p.T, p.r}, F32);
+        const Tensor ws = k.make({(int64_t)need}, U8);
+        return p.is_packed
+                   ? p_thanos_adapter_forward_packed(
+                         Y.data_ptr(), ldy, (float*)at_or_null(V), X->data_ptr(), ldx,
+                         (const uint8_t*)p.weights(), p.ldw, p.packed.scales->data_ptr(),
+                         (int32_t)p.packed.group, p.A, p.B, (const int32_t*)p.index,
+                         (const float*)p.scale, dt, p.T, p.c, p.b, p.n, (int32_t)p.r, ws.data_ptr(),
+                         need, k.stream())
+                   : p_thanos_adapter_forward(Y.data_ptr(), ldy, (float*)at_or_null(V),
+                                              X->data_ptr(), ldx, p.weights(), p.ldw, p.A, p.B,
+                                              (const int32_t*)p.index, (const float*)p.scale, dt,
+                                              p.T, p.c, p.b, p.n, (int32_t)p.r, ws.data_ptr(), need,
+                                              k.stream());
+      }))
+    LONG_WAY();
   return tuple_of({Y, V});
   END_HANDLE_TH_ERRORS
 }
@@ -440,29 +476,32 @@ PyObject* adapter_backward(PyObject*, PyObject* const* a, Py_ssize_t given) {
              : p_thanos_adapter_workspace_bytes(1, p.T, p.c, p.b, p.n, (int32_t)p.r, dt);
   if (need == 0) LONG_WAY();
   Tensor dX, dA, dB;
-  if (need_dx) dX = k.make({p.T, p.b}, dY->scalar_type());
-  if (grads) {
-    dA = k.make({p.n, p.r, p.b}, F32);
-    dB = k.make({p.n, p.c, p.r}, F32);
-  }
-  const Tensor ws = k.make({(int64_t)need}, U8);
   const int64_t lddx = need_dx ? (p.T > 1 ? p.b : (p.b + 7) / 8 * 8) : 0;
   void* xp = x_packed ? x.codes->data_ptr() : X ? X->data_ptr() : nullptr;
-  const thanos_status_t st =
-      packed
-          ? p_thanos_adapter_backward_packed(
-                at_or_null(dX), lddx, (float*)at_or_null(dA), (float*)at_or_null(dB), 0,
-                dY->data_ptr(), lddy, xp, ldx, x_packed ? (const uint8_t*)x.exps->data_ptr() : nullptr,
-                x.lde, (const float*)V, p.weights(), p.ldw,
-                p.is_packed ? p.packed.scales->data_ptr() : nullptr, (int32_t)p.packed.group, p.A,
-                p.B, (const int32_t*)p.index, (const float*)p.scale, dt, p.T, p.c, p.b, p.n,
-                (int32_t)p.r, ws.data_ptr(), need, k.stream())
-          : p_thanos_adapter_backward(at_or_null(dX), lddx, (float*)at_or_null(dA),
-                                      (float*)at_or_null(dB), 0, dY->data_ptr(), lddy, xp, ldx,
-                                      (const float*)V, p.weights(), p.ldw, p.A, p.B,
-                                      (const int32_t*)p.index, (const float*)p.scale, dt, p.T, p.c,
-                                      p.b, p.n, (int32_t)p.r, ws.data_ptr(), need, k.stream());
-  if (st != THANOS_OK) LONG_WAY();
+  if (!done([&] {
+        if (need_dx) dX = k.make({p.T, p.b}, dY->scalar_type());
+        if (grads) {
+          dA = k.make({p.n, p.r, p.b}, F32);
+          dB = k.make({p.n, p.c, p.r}, F32);
+        }
+        const Tensor ws = k.make({(int64_t)need}, U8);
+        return packed
+                   ? p_thanos_adapter_backward_packed(
+                         at_or_null(dX), lddx, (float*)at_or_null(dA), (float*)at_or_null(dB), 0,
+                         dY->data_ptr(), lddy, xp, ldx,
+                         x_packed ? (const uint8_t*)x.exps->data_ptr() : nullptr, x.lde,
+                         (const float*)V, p.weights(), p.ldw,
+                         p.is_packed ? p.packed.scales->data_ptr() : nullptr,
+                         (int32_t)p.packed.group, p.A, p.B, (const int32_t*)p.index,
+                         (const float*)p.scale, dt, p.T, p.c, p.b, p.n, (int32_t)p.r, ws.data_ptr(),
+                         need, k.stream())
+                   : p_thanos_adapter_backward(
+                         at_or_null(dX), lddx, (float*)at_or_null(dA), (float*)at_or_null(dB), 0,
+                         dY->data_ptr(), lddy, xp, ldx, (const float*)V, p.weights(), p.ldw, p.A,
+                         p.B, (const int32_t*)p.index, (const float*)p.scale, dt, p.T, p.c, p.b, p.n,
+                         (int32_t)p.r, ws.data_ptr(), need, k.stream());
+      }))
+    LONG_WAY();
   return tuple_of({dX, dA, dB});
   END_HANDLE_TH_ERRORS
 }

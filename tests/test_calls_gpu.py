@@ -130,3 +130,37 @@ def test_the_short_way_takes_the_current_stream(T):
         got = T.adapter_forward(X, P)[0]
     side.synchronize()
     assert torch.equal(got, want)
+
+
+def test_other_threads_run_while_a_launch_waits(T):
+    """A launch waits when the stream's queue is full.  Whoever has to run before it empties (a callback
+    of another library, say) must not have to wait for the interpreter's lock meanwhile."""
+    import threading
+    import time
+
+    Z = torch.zeros((1, 8), device=DEV)
+    T.token_logprobs(Z)
+    torch.cuda.synchronize()
+    ticks, stop = [], threading.Event()
+
+    def tick():
+        while not stop.is_set():
+            ticks.append(time.perf_counter())
+            time.sleep(0.001)
+
+    other = threading.Thread(target=tick)
+    other.start()
+    try:
+        torch.cuda._sleep(1_000_000_000)          # about half a second
+        longest = 0.0
+        for _ in range(6000):
+            a = time.perf_counter()
+            T.token_logprobs(Z)
+            longest = max(longest, time.perf_counter() - a)
+        torch.cuda.synchronize()
+    finally:
+        stop.set()
+        other.join()
+    if longest < 0.1:
+        pytest.skip("the queue held every launch")
+    assert max(b - a for a, b in zip(ticks, ticks[1:])) < longest / 2
