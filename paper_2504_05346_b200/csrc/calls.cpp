@@ -136,7 +136,7 @@ PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t given) {
   const Tensor *Z = c.tensor(a[0]), *target = c.maybe(a[1]);
   const int64_t k = c.number(a[2]);
   const int dt = c.dtype(Z);
-  if (!c.ok || Z->dim() != 2 || k < 0 || (Z->stride(1) != 1 && Z->size(1) > 1)) LONG_WAY();
+  if (!c.ok || Z->dim() != 2 || k < 0 || k > 64 || (Z->stride(1) != 1 && Z->size(1) > 1)) LONG_WAY();
   const int64_t T = Z->size(0), V = Z->size(1), ld = T > 1 ? Z->stride(0) : std::max<int64_t>(V, 1);
   const void* tp = c.dense(target, I64, {T});
   if (!c.ok) LONG_WAY();
@@ -152,8 +152,7 @@ PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t given) {
         return p_thanos_token_logprobs(
             (float*)at_or_null(logp), (float*)entropy.data_ptr(), (float*)stats.data_ptr(),
             (int64_t*)at_or_null(top_index), (float*)at_or_null(top_logp), Z->data_ptr(), ld,
-            (thanos_dtype_t)dt, (const int64_t*)tp, T, V, (int32_t)std::min<int64_t>(k, INT32_MAX),
-            c.stream());
+            (thanos_dtype_t)dt, (const int64_t*)tp, T, V, (int32_t)k, c.stream());
       }))
     LONG_WAY();
   return tuple_of({logp, entropy, stats, top_index, top_logp});

@@ -48,6 +48,7 @@ def token_logprobs(Z: torch.Tensor, target: Optional[torch.Tensor] = None, k: in
     dt = _dtype_code(Z)
     if target is not None:
         _dense(target, (T,), torch.int64, dev, "target")
+    k = max(-1, min(k, 65))       # the library refuses both ends, before any room is made for more
     with _on(Z):
         with _alloc_scope(stream):
             f32 = torch.float32

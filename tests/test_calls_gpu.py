@@ -164,3 +164,14 @@ def test_other_threads_run_while_a_launch_waits(T):
     if longest < 0.1:
         pytest.skip("the queue held every launch")
     assert max(b - a for a, b in zip(ticks, ticks[1:])) < longest / 2
+
+
+@pytest.mark.parametrize("k", [65, 1 << 20, (1 << 31) + 3, (1 << 32) + 3, 1 << 50])
+def test_far_too_many_alternatives_are_refused(T, k):
+    """By the library, as a shape: no room is made for them first."""
+    Z = torch.zeros((4096, 100), device=DEV)
+    free = torch.cuda.memory_reserved()
+    with pytest.raises(T.ThanosError) as e:
+        T.token_logprobs(Z, None, k)
+    assert "shape" in str(e.value).lower()
+    assert torch.cuda.memory_reserved() - free < 1 << 26
