@@ -12,7 +12,8 @@
 // in flight together; the lanes of a group share its largest value by shuffles; numbers become codes and
 // codes numbers by additions to 2^23 and byte permutations (a value at a time, with conversion instructions
 // and divisions, weights took 132 us both ways).  11008 x 4096 in bf16: weights packed in 26.5 us (4.3
-// TB/s) and unpacked in 26.2, activations in 26.4 (5.1 TB/s) and 24.6.  Packing weights issues in 82 % of the cycles.
+// TB/s) and unpacked in 26.2, activations in 26.4 (5.1 TB/s) and 24.6.  Packing weights issues in 82 % of
+// the cycles.
 #include "packed.cuh"
 #include "proj_gemm.cuh"
 

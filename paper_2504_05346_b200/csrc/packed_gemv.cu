@@ -8,7 +8,8 @@
 // activations are read the same way, straight from memory, once per warp.
 //   code   (nibble | 0x4300) is the bf16 number 128 + nibble; less 136 it is the code
 //   scale  the block's products are summed apart and multiplied by the row's scale in fp32: four
-//          multiplications per 16 x 8 tile and block instead of one per weight
+//          multiplications per 16 x 8 tile and block instead of one per weight (64 products of up to 8 x:
+//          no overflow that w^ would not have, as long as |x| < 2^119)
 // fp32 activations go as three bf16 planes (cut, not rounded: 24 bits in all), three products.
 //
 // mma.sync and not tcgen05: at this width the tensor cores are a fifth busy, and codes that go to tensor
@@ -163,7 +164,7 @@ __device__ __forceinline__ uint2 load_codes(const uint8_t* p) {
 // fixed distances from pointers that move on, and nothing is tested: rows and tokens beyond the last are
 // the last one's, and only their results are left out.  The columns from the last whole pair of blocks on
 // are read with tests, by the last warp.  (16 rows at a time, every load with its own address and tests:
-// 131 instructions for 16 x 64 weights instead of some 70.)
+// 131 instructions for 16 x 64 weights instead of 89.)
 template <typename T, int MT, int NT>
 __device__ __forceinline__ void block_products(const Nibbles& nib, const uint2 (&w)[MT][2],
                                                const uint32_t (&s)[MT][2],

@@ -285,6 +285,19 @@ def test_a_token_that_is_not_finite_stays_alone(T, Tn, dtype):
 
 
 @BOTH
+@pytest.mark.parametrize("Tn", [3, 20, 50, 200])
+def test_activations_up_to_the_stated_limit(T, Tn, dtype):
+    """Few tokens: 64 products of a code (8 at most) and an activation are summed before the scale is
+    applied, 2^9 times the largest activation: below 2^119 no sum overflows that is finite in the end."""
+    X, P, W, *_ = operands(T, (Tn, 96, 328, 2, 8, "mixed"), dtype, 64, seed=5)
+    X = (X.double() / X.double().abs().max() * 2.0 ** 119 * (1 - 2.0 ** -8)).to(dtype)
+    want = X.double() @ W.double().t()
+    assert float(want.abs().max()) < 2.0 ** 126
+    Y, _ = T.adapter_forward(X, P)
+    assert rel(Y.double() * 2.0 ** -119, want * 2.0 ** -119) < TOL[dtype]
+
+
+@BOTH
 def test_gradients_of_packed_activations_that_are_not_finite(T, dtype):
     """An infinity in a token of adapter 0 reaches dA of adapter 0 in that column's group, nothing else."""
     shape = (90, 64, 136, 3, 8, "blocks")
