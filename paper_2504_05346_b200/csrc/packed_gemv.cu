@@ -16,14 +16,12 @@
 // memory need a permutation and a multiplication per pair more (packed_tc.cu).  What bounds it is turning
 // codes into numbers: of some 89 instructions for 16 x 64 weights 42 are integer and 32 bf16 ones, at half
 // rate both.  One token: 4096 x 4096 4.7 us, 11008 x 4096 9.6, 28672 x 8192 38 us (3.2 TB/s; without the
-// arithmetic 24, with all loads from L1 35); 16 tokens: 6.8, 12.8 and 48 us.
+// arithmetic 24, with all loads from L1 35); 16 tokens: 6.8, 11.7 and 45 us.
 #include "packed_few.cuh"
 
 namespace thanos {
 namespace {
 
-constexpr int GW = 8;            // warps of a CTA
-constexpr int GT = 32 * GW;
 constexpr int SHRINK_RANKS = 4;
 
 __device__ __forceinline__ int adapter_of(const int32_t* index, int t, int n) {
@@ -85,22 +83,6 @@ __global__ void __launch_bounds__(1024) shrink_kernel(const FewParams p) {
 }
 
 // --------------------------------------------------------------------------------------- products
-__device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0,
-                                          uint32_t b1, bool first) {
-  if (first) {
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
-        "{%8, %9}, {%10, %10, %10, %10};"
-        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
-    return;
-  }
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
-      "{%8, %9}, {%0, %1, %2, %3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
 // Codes j and j + 4 of a word of eight as a pair of bf16.
 __device__ __forceinline__ uint32_t codes_of(const Nibbles& nib, uint32_t w, int j) {
   const uint32_t v = nib(w, j);
@@ -202,9 +184,10 @@ __device__ __forceinline__ void block_products(const Nibbles& nib, const uint2 (
                             acc[i][j][e]);
 }
 
-template <typename T, int MT, int NT>
-__global__ void __launch_bounds__(GT, MT * NT == 1 ? 4 : MT * NT == 2 ? 3 : 2) few_kernel(const FewParams p) {
-  constexpr int ROWS = 16 * MT, TOKS = 8 * NT;
+template <typename T, int MT, int NT, int GW>
+__global__ void __launch_bounds__(32 * GW, (MT * NT == 1 ? 4 : MT * NT == 2 ? 3 : 2) * 8 / GW)
+few_kernel(const FewParams p) {
+  constexpr int ROWS = 16 * MT, TOKS = 8 * NT, GT = 32 * GW;
   __shared__ float part[GW][TOKS][ROWS + 4];
   if (p.n == 0 && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.status = 0;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -301,19 +284,19 @@ __global__ void __launch_bounds__(GT, MT * NT == 1 ? 4 : MT * NT == 2 ? 3 : 2) f
   if (p.n > 0) grid_dependency_wait();
   for (int e = threadIdx.x; e < TOKS * ROWS; e += GT) {
     const int t = e / ROWS, m = e % ROWS;
-    float v = 0.f;
+    float v[1] = {};
 #pragma unroll
-    for (int u = 0; u < GW; ++u) v += part[u][t][m];
-    const int row = m0 + m, at = t0 + t;
-    if (row < p.c && at < p.T) finish<T>(p, row, at, v);
+    for (int u = 0; u < GW; ++u) v[0] += part[u][t][m];
+    const int row[1] = {m0 + m}, at[1] = {t0 + t};
+    if (row[0] < p.c && at[0] < p.T) finish<T>(p, row, at, v);
   }
 }
 
-template <typename T, int MT, int NT>
+template <typename T, int MT, int NT, int GW = 8>
 thanos_status_t launch(const FewParams& p, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)ceil_div(p.c, 16 * MT), (unsigned)ceil_div(p.T, 8 * NT), 1);
-  cfg.blockDim = dim3(GT, 1, 1);
+  cfg.blockDim = dim3(32 * GW, 1, 1);
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -321,7 +304,7 @@ thanos_status_t launch(const FewParams& p, cudaStream_t stream) {
   cfg.attrs = attr;
   cfg.numAttrs = p.n > 0 ? 1 : 0;
   count_launch();
-  THANOS_CUDA(cudaLaunchKernelEx(&cfg, few_kernel<T, MT, NT>, p));
+  THANOS_CUDA(cudaLaunchKernelEx(&cfg, few_kernel<T, MT, NT, GW>, p));
   return THANOS_OK;
 }
 
@@ -333,13 +316,16 @@ thanos_status_t forward_few(const FewParams& p, cudaStream_t stream) {
                        (unsigned)(pieces < 1024 ? pieces : 1024), 0, stream>>>(p);
     THANOS_CHECK_LAUNCH();
   }
-  // Two tiles of rows share a warp's activations, where there are rows enough for every SM.
+  // Two tiles of rows share a warp's activations, where there are rows enough for every SM.  With 16 tokens
+  // these are then four warps to a CTA, more and smaller pieces for two CTAs' worth of registers: 11008 x
+  // 4096 11.7 and 12.9 us, 28672 x 8192 45.4 and 48.8; below, eight: 4096 x 4096 6.8 and 7.1, 4096 x 11008
+  // 13.7 and 15.2.
   const bool wide = p.c >= 32 * NUM_SMS;
   if (p.T <= 8) return wide ? launch<T, 2, 1>(p, stream) : launch<T, 1, 1>(p, stream);
   if constexpr (sizeof(T) == 4) {
-    return launch<T, 2, 2>(p, stream);
+    return wide ? launch<T, 2, 2, 4>(p, stream) : launch<T, 2, 2>(p, stream);
   } else {
-    if (p.T <= 16) return wide ? launch<T, 2, 2>(p, stream) : launch<T, 1, 2>(p, stream);
+    if (p.T <= 16) return wide ? launch<T, 2, 2, 4>(p, stream) : launch<T, 1, 2>(p, stream);
     return packed_tiles(p, stream);
   }
 }

@@ -16,8 +16,10 @@
 // What bounds it is turning codes into bf16: 19 instructions for eight weights (shift, mask, subtract,
 // multiply, and a permutation, because a word gives the columns j and j + 4 at once and an activation's
 // columns come as they are), most of them at half rate; 128 x 64 weights take an SM some 480 clocks, and
-// the tensor cores are a quarter busy.  64 tokens: 4096 x 4096 10.9 us, 11008 x 4096 20.6, 28672 x 8192
+// the tensor cores are a quarter busy.  64 tokens: 4096 x 4096 10.5 us, 11008 x 4096 17.6, 28672 x 8192
 // 60 us.
+#include <type_traits>
+
 #include "packed_few.cuh"
 
 namespace thanos {
@@ -30,6 +32,7 @@ constexpr int QCODES = QM * QSTAGE / 2;  // bytes of a stage's codes
 constexpr int QMAX_BUFS = 8;             // buffers of weights in tensor memory, 32 columns each
 constexpr int threads_of(int groups) { return 128 * groups + 64; }
 constexpr int QMAX_STAGES = 6;
+constexpr int OUT = 4;                   // results that a thread finishes at a time
 
 struct TilesParams {
   FewParams f;
@@ -111,11 +114,164 @@ __device__ __forceinline__ void decode8(const Nibbles& nib, uint32_t w, uint32_t
   out[3] = __byte_perm(h[2], h[3], 0x7632);
 }
 
+// Sums over a cluster of a row's tokens first, first + step, ..., O at a time (with few to a thread the
+// larger O is slower: 4096 x 4096, 32 tokens, two to a thread, 10.2 and 10.8 us; 11008 x 4096, 64 tokens,
+// eleven to a thread, 20.7 and 18.6; with rows of adapters to wait for it pays from four on: 32 tokens, 16
+// adapters, five to a thread, 24.3 and 22.3).
+template <int O, bool ADAPTERS>
+__device__ __forceinline__ void sum_and_finish(const FewParams& f, uint32_t smem_base, int first,
+                                               int step, int toks, int t0, int m0, int row, int S) {
+  if (m0 + row >= f.c) return;
+#pragma unroll 1
+  for (int t = first; t < toks; t += O * step) {
+    float v[O] = {};
+    int rows[O], at[O];
+    uint32_t from[O];
+#pragma unroll
+    for (int o = 0; o < O; ++o) {
+      const int mine = t + o * step, there = mine < toks ? mine : t;
+      at[o] = t0 + there;
+      rows[o] = mine < toks ? m0 + row : -1;
+      from[o] = smem_base + 4u * (uint32_t)(there * QM + row);
+    }
+#pragma unroll 4
+    for (int u = 0; u < S; ++u) {
+      float z[O];
+#pragma unroll
+      for (int o = 0; o < O; ++o)
+        asm volatile("ld.shared::cluster.f32 %0, [%1];"
+                     : "=f"(z[o])
+                     : "r"(map_to_cta(from[o], u))
+                     : "memory");
+#pragma unroll
+      for (int o = 0; o < O; ++o) v[o] += z[o];
+    }
+    finish<bf16, O, ADAPTERS>(f, rows, at, v);
+  }
+}
+
+// Eight fp32 values as pairs of bf16 in three planes (cut, not rounded: 24 bits in all).  The first plane
+// keeps an infinity or NaN and the others are zero beside it.
+__device__ __forceinline__ void planes_of(const float4& a, const float4& b, uint32_t (&o)[3][4]) {
+  float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+  for (int pl = 0; pl < 3; ++pl) {
+    uint32_t h[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const bool odd = pl == 0 && !isfinite(v[e]);
+      h[e] = odd && isnan(v[e]) ? 0x7FFF0000u : __float_as_uint(v[e]) & 0xFFFF0000u;
+      v[e] = odd ? 0.f : v[e] - __uint_as_float(h[e]);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[pl][j] = __byte_perm(h[2 * j], h[2 * j + 1], 0x7632);
+  }
+}
+
+// The same for adapters of more ranks: a warp's 32 rows and its tokens, up to eight of one adapter at a
+// time, as products on the tensor cores.  Which rank a lane holds at which place does not matter: a lane
+// reads eight consecutive ones of each of its rows of B and of its token of V.  (A row of B to a lane, token
+// by token, is 32 lines to a load of B and four passes to each of V: 128 tokens of 11008 x 4096 with four
+// adapters of rank 64 took 133 us; here 50.)
+__device__ __forceinline__ void finish_by_adapter(const FewParams& f, uint32_t smem_base, int first,
+                                                  int step, int toks, int t0, int m0, int row,
+                                                  int S) {
+  const int lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3, r0 = row & ~31;
+  // at most 32: 128 tokens and sixteen warps, or, where the rings of two CTAs fit, 64 and eight
+  const int count = first < toks ? (toks - first + step - 1) / step : 0;
+  int own = lane < count ? f.index[t0 + first + lane * step] : -1;
+  if (own < -1 || own >= f.n) {
+    if (m0 + r0 == 0) atomicCAS(f.status, 0, (int)THANOS_ERR_INVALID_ARG);
+    own = -1;
+  }
+  unsigned left = __ballot_sync(0xffffffffu, lane < count);
+  while (left) {
+    // the next token's adapter, and up to eight of its tokens: the g-th is this lane's of the operand, the
+    // 2 t4-th and the one after it are its results'
+    const int i = __shfl_sync(0xffffffffu, own, __ffs(left) - 1);
+    unsigned same = __ballot_sync(0xffffffffu, own == i) & left;
+    int in = -1, out[2] = {-1, -1};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int k = __ffs(same) - 1;  // -1: no more
+      if (e == g) in = k;
+      if (e == 2 * t4) out[0] = k;
+      if (e == 2 * t4 + 1) out[1] = k;
+      if (k >= 0) left &= ~(1u << k);
+      same &= same - 1;
+    }
+    float d[2][4] = {};
+    if (i >= 0) {
+      const float* vt = f.V + (int64_t)(t0 + first + (in < 0 ? 0 : in) * step) * f.r + 8 * t4;
+      const bf16* bw[2][2];
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          bw[m][h] = static_cast<const bf16*>(f.B) +
+                     ((int64_t)i * f.c + min(m0 + r0 + 16 * m + 8 * h + g, f.c - 1)) * f.r + 8 * t4;
+#pragma unroll 2
+      for (int j = 0; j < f.r; j += 32) {
+        const bool there = j + 8 * t4 < f.r;
+        uint4 w[2][2];
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            w[m][h] = there ? *reinterpret_cast<const uint4*>(bw[m][h] + j) : make_uint4(0u, 0u, 0u, 0u);
+        const float4 none = make_float4(0.f, 0.f, 0.f, 0.f);
+        const float4 va = there && in >= 0 ? *reinterpret_cast<const float4*>(vt + j) : none;
+        const float4 vb = there && in >= 0 ? *reinterpret_cast<const float4*>(vt + j + 4) : none;
+        uint32_t x[3][4];
+        planes_of(va, vb, x);
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          const uint32_t lo[4] = {w[m][0].x, w[m][1].x, w[m][0].y, w[m][1].y};
+          const uint32_t hi[4] = {w[m][0].z, w[m][1].z, w[m][0].w, w[m][1].w};
+#pragma unroll
+          for (int pl = 2; pl >= 0; --pl) {
+            mma_16816(d[m], lo, x[pl][0], x[pl][1], false);
+            mma_16816(d[m], hi, x[pl][2], x[pl][3], false);
+          }
+        }
+      }
+    }
+    const float scale = i >= 0 ? f.scale[i] : 0.f;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int t = first + (out[e] < 0 ? 0 : out[e]) * step;
+      float v[4] = {};
+#pragma unroll 2
+      for (int u = 0; u < S; ++u) {
+        float z[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          asm volatile("ld.shared::cluster.f32 %0, [%1];"
+                       : "=f"(z[q])
+                       : "r"(map_to_cta(smem_base + 4u * (uint32_t)(t * QM + r0 + 8 * q + g), u))
+                       : "memory");
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] += z[q];
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int at = m0 + r0 + 8 * q + g;
+        if (out[e] >= 0 && at < f.c)
+          static_cast<bf16*>(f.Y)[(int64_t)(t0 + t) * f.ldy + at] =
+              __float2bfloat16_rn(i >= 0 ? fmaf(scale, d[q >> 1][2 * (q & 1) + e], v[q]) : v[q]);
+      }
+    }
+  }
+}
+
+// What is added to the products.
+enum { NO_ADAPTERS, BY_TOKEN, BY_ADAPTER };
+
 // GROUPS of four warps that turn codes into weights, with two buffers each.
-template <int GROUPS>
+template <int GROUPS, int ADD>
 __global__ void __launch_bounds__(threads_of(GROUPS), GROUPS == 2 ? 2 : 1)
 tiles_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
-             const TilesParams p) {
+             const __grid_constant__ TilesParams p) {
   constexpr int QBUFS = 2 * GROUPS, PER = 4 / GROUPS;  // blocks of a stage that a group takes
   constexpr int PRODUCER = 4 * GROUPS, ISSUER = PRODUCER + 1;
   extern __shared__ unsigned char smem_raw[];
@@ -142,7 +298,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
   const int nblk = min(4 * st1, p.blocks) - 4 * st0;  // of this CTA, at least one
   const int stage_bytes = QCODES + N * QSTAGE * 2;
 
-  if (f.n == 0 && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *f.status = 0;
+  if (ADD == NO_ADAPTERS && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *f.status = 0;
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.stages; ++s) {
       mbar_init(full_bar(s), 1);
@@ -292,7 +448,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
     // ------------------------------------------------------------ sums
     ok = ok && mbar_wait_warp(done_bar, 0, abort_flag);
     tc_fence_after();
-    if (f.n > 0) grid_dependency_wait();
+    if (ADD != NO_ADAPTERS) grid_dependency_wait();
     if (ok) {
       float* part = reinterpret_cast<float*>(smem);  // the ring, whose operands are consumed
       const int toks = min(N, f.T - t0);
@@ -301,31 +457,43 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
         uint32_t v[8];
         tmem_ld8(tmem_base + lanes + j, v);
         tc_wait_ld();
+        if (S > 1 || ADD == BY_ADAPTER) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          if (S > 1) part[(j + e) * QM + row] = __uint_as_float(v[e]);
-          else if (j + e < toks && m0 + row < f.c)
-            finish<bf16>(f, m0 + row, t0 + j + e, __uint_as_float(v[e]));
+          for (int e = 0; e < 8; ++e) part[(j + e) * QM + row] = __uint_as_float(v[e]);
+        } else {
+#pragma unroll
+          for (int h = 0; h < 8; h += OUT) {
+            float y[OUT];
+            int rows[OUT], at[OUT];
+#pragma unroll
+            for (int e = 0; e < OUT; ++e) {
+              y[e] = __uint_as_float(v[h + e]);
+              at[e] = t0 + j + h + e;
+              rows[e] = j + h + e < toks && m0 + row < f.c ? m0 + row : -1;
+            }
+            finish<bf16, OUT, ADD != NO_ADAPTERS>(f, rows, at, y);
+          }
         }
       }
     }
   }
-  if (S > 1) {
+  if (S > 1 || ADD == BY_ADAPTER) {
     cluster_sync_all();
     if (warp < PRODUCER && ok) {
       const int row = threadIdx.x & (QM - 1), toks = min(N, f.T - t0);
-      for (int t = GROUPS * rank + (int)(threadIdx.x / QM); t < toks && m0 + row < f.c;
-           t += GROUPS * S) {
-        float v = 0.f;
-        for (int u = 0; u < S; ++u) {
-          float z;
-          asm volatile("ld.shared::cluster.f32 %0, [%1];"
-                       : "=f"(z)
-                       : "r"(map_to_cta(smem_base, u) + 4u * (uint32_t)(t * QM + row))
-                       : "memory");
-          v += z;
-        }
-        finish<bf16>(f, m0 + row, t0 + t, v);
+      const int step = GROUPS * S, first = GROUPS * rank + (int)(threadIdx.x / QM);
+      if constexpr (ADD == BY_ADAPTER) {
+        finish_by_adapter(f, smem_base, first, step, toks, t0, m0, row, S);
+      } else if constexpr (ADD == BY_TOKEN) {
+        if (toks < OUT * step || f.r > 16)
+          sum_and_finish<1, true>(f, smem_base, first, step, toks, t0, m0, row, S);
+        else
+          sum_and_finish<OUT, true>(f, smem_base, first, step, toks, t0, m0, row, S);
+      } else {
+        if (toks < 2 * OUT * step)
+          sum_and_finish<1, false>(f, smem_base, first, step, toks, t0, m0, row, S);
+        else
+          sum_and_finish<OUT, false>(f, smem_base, first, step, toks, t0, m0, row, S);
       }
     }
     __syncwarp();
@@ -356,11 +524,11 @@ bool make_map2(CUtensorMap* map, const void* base, CUtensorMapDataType type, int
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int GROUPS>
+template <int GROUPS, int ADD>
 thanos_status_t launch_tiles(const CUtensorMap& map_w, const CUtensorMap& map_x, const TilesParams& p,
                              int tiles_t, cudaStream_t stream) {
   static std::atomic<unsigned long long> done{0};
-  THANOS_CUDA(ensure_max_dyn_smem(tiles_kernel<GROUPS>, 227 * 1024, done));
+  THANOS_CUDA(ensure_max_dyn_smem(tiles_kernel<GROUPS, ADD>, 227 * 1024, done));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(ceil_div(p.f.c, QM) * p.split), (unsigned)tiles_t, 1);
   cfg.blockDim = dim3(threads_of(GROUPS), 1, 1);
@@ -374,9 +542,9 @@ thanos_status_t launch_tiles(const CUtensorMap& map_w, const CUtensorMap& map_x,
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = p.f.n > 0 ? 2 : 1;
+  cfg.numAttrs = ADD != NO_ADAPTERS ? 2 : 1;
   count_launch();
-  THANOS_CUDA(cudaLaunchKernelEx(&cfg, tiles_kernel<GROUPS>, map_w, map_x, p));
+  THANOS_CUDA(cudaLaunchKernelEx(&cfg, tiles_kernel<GROUPS, ADD>, map_w, map_x, p));
   return THANOS_OK;
 }
 
@@ -427,8 +595,19 @@ thanos_status_t packed_tiles(const FewParams& f, cudaStream_t stream) {
   p.ring_bytes = groups == 2 ? p.stages * stage_bytes : room;
   p.tmem_cols = 32;
   while (p.tmem_cols < p.N + 2 * groups * 32) p.tmem_cols *= 2;
-  return groups == 2 ? launch_tiles<2>(map_w, map_x, p, tiles_t, stream)
-                     : launch_tiles<4>(map_w, map_x, p, tiles_t, stream);
+  // By adapter from 17 ranks on: 16 adapters, 4096 x 4096, 128 tokens, rank 32 22.4 us (by token 29.1), rank
+  // 16 of 8 adapters 19.7 (20.3), but 32 tokens 15.8 (13.6), and 11008 x 4096, 16 of rank 16, 32.0 (22.1).
+  int add = f.n == 0 ? NO_ADAPTERS : BY_TOKEN;
+  if (f.n > 0 && f.r % 8 == 0 && f.r > 16 && p.N <= 32 * groups * p.split)
+    add = BY_ADAPTER;
+  auto launch = [&](auto add_) {
+    constexpr int ADD = decltype(add_)::value;
+    return groups == 2 ? launch_tiles<2, ADD>(map_w, map_x, p, tiles_t, stream)
+                       : launch_tiles<4, ADD>(map_w, map_x, p, tiles_t, stream);
+  };
+  return add == NO_ADAPTERS ? launch(std::integral_constant<int, NO_ADAPTERS>{})
+         : add == BY_TOKEN  ? launch(std::integral_constant<int, BY_TOKEN>{})
+                            : launch(std::integral_constant<int, BY_ADAPTER>{});
 }
 
 }  // namespace thanos

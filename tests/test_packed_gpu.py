@@ -503,3 +503,48 @@ def test_every_scale_and_every_code(T):
             assert torch.equal(P.scales.double(), scales)
             assert torch.equal(nibbles(P)[:, :Wk.shape[1]], codes)
             assert torch.equal(T.unpack_weights(P, F32).double(), values)
+
+
+# Rows of adapters held for several tokens, in one slice of k and in several, two CTAs to an SM and one;
+# tokens one by one beside them, of more and of fewer ranks; sixteen tokens of many rows.
+TOGETHER = [
+    (128, 12000, 264, 1, 64, "mixed"),
+    (97, 12000, 264, 2, 40, "mixed"),
+    (125, 8200, 136, 2, 56, "mixed"),
+    (64, 19200, 264, 1, 64, "mixed"),
+    (50, 19300, 72, 2, 24, "blocks"),
+    (128, 300, 4104, 1, 64, "mixed"),
+    (100, 1000, 2056, 2, 32, "blocks"),
+    (128, 12000, 264, 100, 64, "mixed"),
+    (128, 2100, 520, 2, 128, "mixed"),
+    (64, 2100, 520, 2, 20, "mixed"),
+    (128, 12000, 264, 40, 16, "mixed"),
+    (16, 5001, 264, 3, 16, "mixed"),
+    (11, 9001, 136, 2, 12, "mixed"),
+]
+
+
+@BOTH
+@pytest.mark.parametrize("shape", TOGETHER, ids=lambda s: "x".join(map(str, s)))
+def test_forward_of_tokens_that_share_adapters(T, shape, dtype):
+    """As test_forward; one index names no adapter, as if it were none."""
+    Tn, c, b, n, r, order = shape
+    X, P, W, A, B, index, scale, _ = operands(T, shape, dtype, 128, seed=Tn + r)
+    out = torch.full((Tn + 1, c + 5), math.nan, dtype=dtype, device=DEV)
+    Y, V = T.adapter_forward(X, P, A, B, index, scale, out=out[:Tn, :c], check=True)
+    Yr, Vr = ref_forward(X, W, A, B, index, scale)
+    assert rel(V, Vr) <= TOL[F32]
+    err = (Y.double() - Yr).norm(dim=1) / Yr.norm(dim=1)
+    assert err.max().item() <= 2 * TOL[dtype]
+    worst = (Y.double() - Yr).abs().max(0).values
+    assert bool((worst <= 0.05 * Yr.abs().max()).all())
+    assert bool(out[Tn:].isnan().all()) and bool(out[:, c:].isnan().all())
+    bad, none = index.clone(), index.clone()
+    bad[Tn // 2], none[Tn // 2] = n, -1
+    with pytest.raises(T.ThanosError):
+        T.adapter_forward(X, P, A, B, bad, scale, check=True)
+    Yb, _ = T.adapter_forward(X, P, A, B, bad, scale)
+    Yn, _ = T.adapter_forward(X, P, A, B, none, scale, check=True)
+    assert torch.equal(Yb, Yn)
+    keep = [t for t in range(Tn) if t != Tn // 2]
+    assert torch.equal(Yn[keep], Y[keep])
