@@ -334,14 +334,14 @@ thanos_status_t forward_few(const FewParams& p, cudaStream_t stream) {
 
 // Up to here the codes are turned into weights where they meet the activations; with more tokens they are
 // unpacked once and multiplied as they would be from memory.  Replayed, both ways:
-//   4096 x 4096     128 tokens   13.2 and 22.7 us    256 tokens   20.5 and 25.9 us
-//   4096 x 11008    128 tokens   22.0 and 53.9       256 tokens   37.2 and 63.8
-//   11008 x 4096    128 tokens   26.5 and 53.2       256 tokens   58.0 and 62.6
-//   the same, 16 adapters of rank 16   47.1 and 65.3;  192 tokens   97.8 and 75.2
+//   4096 x 4096     128 tokens   12.7 and 20.8 us    256 tokens   17.5 and 24.7 us
+//   4096 x 11008    128 tokens   21.6 and 54.9       256 tokens   34.5 and 62.7
+//   11008 x 4096    128 tokens   25.1 and 51.5       256 tokens   49.8 and 61.4    384 tokens  49.7 and 81.6
+//   256 tokens with adapters:    4096 x 4096, 8 of rank 16, 31.5 and 31.7; 2 of rank 64, 45 and 97; 4096 x
+//     11008, 16 of rank 16, 58 and 70; 11008 x 4096, 16 of rank 16, 82 and 78; 4 of rank 64, 90 and 82
+//   320 tokens:     4096 x 4096, 8 of rank 16, 44 and 39;  4096 x 11008, 16 of rank 16, 102 and 78
 //   fp32 2048 x 2048, 64 tokens   15.8 and 31.7;  768 x 768, 64 tokens   4.9 and 15.2
-bool packed_few_tokens(const AdapterArgs& a) {
-  return a.T <= (a.dtype == THANOS_F32 ? 64 : a.n > 0 ? 128 : 256);
-}
+bool packed_few_tokens(const AdapterArgs& a) { return a.T <= (a.dtype == THANOS_F32 ? 64 : 256); }
 
 size_t packed_few_workspace_bytes(int64_t T, int r) { return 256 + round_up((size_t)T * r * 4, 256); }
 

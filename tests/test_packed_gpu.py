@@ -521,6 +521,10 @@ TOGETHER = [
     (128, 12000, 264, 40, 16, "mixed"),
     (16, 5001, 264, 3, 16, "mixed"),
     (11, 9001, 136, 2, 12, "mixed"),
+    (200, 300, 1032, 3, 40, "mixed"),
+    (256, 12000, 136, 4, 64, "mixed"),
+    (177, 2000, 2056, 9, 16, "blocks"),
+    (257, 700, 264, 3, 24, "mixed"),
 ]
 
 
