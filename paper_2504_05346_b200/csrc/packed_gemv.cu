@@ -14,8 +14,8 @@
 //
 // mma.sync and not tcgen05: at this width the tensor cores are a fifth busy, and codes that go to tensor
 // memory need a permutation and a multiplication per pair more (packed_tc.cu).  What bounds it is turning
-// codes into numbers: of some 89 instructions for 16 x 64 weights 42 are integer and 32 bf16 ones, at half
-// rate both.  One token: 4096 x 4096 4.7 us, 11008 x 4096 9.6, 28672 x 8192 38 us (3.2 TB/s; without the
+// codes into numbers: of some 89 instructions for 16 x 64 weights half are integer and a third bf16 ones, at
+// half rate both.  One token: 4096 x 4096 4.7 us, 11008 x 4096 9.6, 28672 x 8192 38 us (3.2 TB/s; without the
 // arithmetic 24, with all loads from L1 35); 16 tokens: 6.8, 11.7 and 45 us.
 #include "packed_few.cuh"
 
@@ -319,11 +319,12 @@ thanos_status_t forward_few(const FewParams& p, cudaStream_t stream) {
   // Two tiles of rows share a warp's activations, where there are rows enough for every SM.  With 16 tokens
   // these are then four warps to a CTA, more and smaller pieces for two CTAs' worth of registers: 11008 x
   // 4096 11.7 and 12.9 us, 28672 x 8192 45.4 and 48.8; below, eight: 4096 x 4096 6.8 and 7.1, 4096 x 11008
-  // 13.7 and 15.2.
+  // 13.7 and 15.2.  fp32 keeps eight: 9 tokens, 11008 x 4096, 4 adapters 33.3 us, with four 42.2 (without
+  // adapters 30.7 and 31.0).
   const bool wide = p.c >= 32 * NUM_SMS;
   if (p.T <= 8) return wide ? launch<T, 2, 1>(p, stream) : launch<T, 1, 1>(p, stream);
   if constexpr (sizeof(T) == 4) {
-    return wide ? launch<T, 2, 2, 4>(p, stream) : launch<T, 2, 2>(p, stream);
+    return launch<T, 2, 2>(p, stream);
   } else {
     if (p.T <= 16) return wide ? launch<T, 2, 2, 4>(p, stream) : launch<T, 1, 2>(p, stream);
     return packed_tiles(p, stream);
