@@ -168,6 +168,17 @@ __device__ __forceinline__ void planes_of(const float4& a, const float4& b, uint
   }
 }
 
+// The adapter's part of one result as a sum of plain products.  In planes, an infinite weight would meet a
+// zero that is only a plane of its factor.
+__device__ __noinline__ float adapter_sum(const FewParams& f, int i, int t, int row) {
+  const bf16* b = static_cast<const bf16*>(f.B) + ((int64_t)i * f.c + row) * f.r;
+  const float* v = f.V + (int64_t)t * f.r;
+  float d = 0.f;
+#pragma unroll 1
+  for (int j = 0; j < f.r; ++j) d = fmaf(v[j], to_float(b[j]), d);
+  return d;
+}
+
 // The same for adapters of more ranks: a warp's 32 rows and its tokens, up to eight of one adapter at a
 // time, as products on the tensor cores.  Which rank a lane holds at which place does not matter: a lane
 // reads eight consecutive ones of each of its rows of B and of its token of V.  (A row of B to a lane, token
@@ -234,6 +245,17 @@ __device__ __forceinline__ void finish_by_adapter(const FewParams& f, uint32_t s
             mma_16816(d[m], hi, x[pl][2], x[pl][3], false);
           }
         }
+      }
+    }
+    float zero = 0.f;  // or NaN
+#pragma unroll
+    for (int e = 0; e < 8; ++e) zero = fmaf(d[e >> 2][e & 3], 0.f, zero);
+    if (zero != 0.f) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float& add = d[e >> 2][e & 3];
+        const int at = m0 + r0 + 8 * (e >> 1) + g, k = out[e & 1];
+        if (!isfinite(add) && k >= 0 && at < f.c) add = adapter_sum(f, i, t0 + first + k * step, at);
       }
     }
     const float scale = i >= 0 ? f.scale[i] : 0.f;
