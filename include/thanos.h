@@ -561,9 +561,8 @@ thanos_status_t thanos_unpack_activations(void* X, int64_t ldx, thanos_dtype_t d
 
 /*
  * thanos_adapter_forward with packed weights (w_codes, ldq, w_scales and group as above) in the place
- * of W, ldw.  The weights are w^, exactly: 32-bit results are those of 32-bit weights.  With few tokens
- * the scale is applied to sums over 64 columns: activations from 2^119 on may overflow there.  Everything
- * else as there; workspace: thanos_adapter_packed_workspace_bytes(0, 1, 0, ...) bytes.
+ * of W, ldw.  The weights are w^, exactly: 32-bit results are those of 32-bit weights.  Everything else as
+ * there; workspace: thanos_adapter_packed_workspace_bytes(0, 1, 0, ...) bytes.
  */
 thanos_status_t thanos_adapter_forward_packed(void* Y, int64_t ldy, float* V, const void* X,
                                               int64_t ldx, const uint8_t* w_codes, int64_t ldq,

@@ -28,11 +28,14 @@ struct PackedActivations {
 // eight bits, and is a bf16 number.
 constexpr uint32_t SCALE_BITS = 0xFFF8u;
 
-// The nibbles j and j + 4 of a word as the bf16 numbers 128 + nibble.  Both constants have to be in
-// registers (`Nibbles`): an instruction takes one of its own only, and the pair would take two.
+// The nibbles j and j + 4 of a word as the bf16 numbers whose low bits they are: 128 + nibble, or with
+// another base what that has.  Both constants have to be in registers (`Nibbles`): an instruction takes one
+// of its own only, and the pair would take two.
 struct Nibbles {
-  uint32_t mask = 0x000F000Fu, base = 0x43004300u;
-  __device__ __forceinline__ Nibbles() { asm volatile("" : "+r"(mask), "+r"(base)); }
+  uint32_t mask = 0x000F000Fu, base;
+  __device__ __forceinline__ explicit Nibbles(uint32_t base_ = 0x43004300u) : base(base_) {
+    asm volatile("" : "+r"(mask), "+r"(base));
+  }
   __device__ __forceinline__ uint32_t operator()(uint32_t w, int j) const {
     uint32_t v;
     asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(v) : "r"(w >> (4 * j)), "r"(mask), "r"(base));

@@ -6,10 +6,11 @@
 // In a block a lane reads eight bytes of each of its rows, which are 16 consecutive columns: which k a
 // lane holds at which place of the operand does not matter, as long as both operands agree, so the
 // activations are read the same way, straight from memory, once per warp.
-//   code   (nibble | 0x4300) is the bf16 number 128 + nibble; less 136 it is the code
+//   code   (nibble | 0x3E80) is the bf16 number 2^-2 + 2^-9 nibble; less 2^-2 + 2^-6 it is 2^-9 code
 //   scale  the block's products are summed apart and multiplied by the row's scale in fp32: four
-//          multiplications per 16 x 8 tile and block instead of one per weight (64 products of up to 8 x:
-//          no overflow that w^ would not have, as long as |x| < 2^119)
+//          multiplications per 16 x 8 tile and block instead of one per weight.  64 products of up to 8 x
+//          are 2^9 x, which is what the codes' 2^-9 is for: a sum does not leave fp32's range where w^
+//          would not, and the results take it back, exactly
 // fp32 activations go as three bf16 planes (cut, not rounded: 24 bits in all), three products.
 //
 // mma.sync and not tcgen05: at this width the tensor cores are a fifth busy, and codes that go to tensor
@@ -83,12 +84,13 @@ __global__ void __launch_bounds__(1024) shrink_kernel(const FewParams p) {
 }
 
 // --------------------------------------------------------------------------------------- products
-// Codes j and j + 4 of a word of eight as a pair of bf16.
+// Codes j and j + 4 of a word of eight, times 2^-9, as a pair of bf16.
+constexpr uint32_t CODE_BASE = 0x3E803E80u, CODE_ZERO = 0x3E883E88u;
+constexpr float CODE_UNIT = 512.f;
 __device__ __forceinline__ uint32_t codes_of(const Nibbles& nib, uint32_t w, int j) {
-  const uint32_t v = nib(w, j);
-  const uint32_t off = 0x43084308u;  // 136
+  const uint32_t v = nib(w, j), zero = CODE_ZERO;
   const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v),
-                                   *reinterpret_cast<const __nv_bfloat162*>(&off));
+                                   *reinterpret_cast<const __nv_bfloat162*>(&zero));
   return *reinterpret_cast<const uint32_t*>(&d);
 }
 // Eight activations, and as four pairs (x_j, x_j+4) in one plane or in three.
@@ -214,7 +216,7 @@ few_kernel(const FewParams p) {
     x[j] = static_cast<const T*>(p.X) + (int64_t)min(t0 + 8 * j + g, p.T - 1) * p.ldx + 16 * t4 +
            (int64_t)k0 * 128;
   const int64_t second = p.shift == 6 ? p.c : 0, step = p.shift == 6 ? 2 * (int64_t)p.c : p.c;
-  const Nibbles nib;
+  const Nibbles nib(CODE_BASE);
   float acc[MT][NT][4] = {};
 #pragma unroll 1
   for (int k = k0; k < k1; ++k) {
@@ -287,6 +289,7 @@ few_kernel(const FewParams p) {
     float v[1] = {};
 #pragma unroll
     for (int u = 0; u < GW; ++u) v[0] += part[u][t][m];
+    v[0] *= CODE_UNIT;
     const int row[1] = {m0 + m}, at[1] = {t0 + t};
     if (row[0] < p.c && at[0] < p.T) finish<T>(p, row, at, v);
   }

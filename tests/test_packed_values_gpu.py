@@ -1,5 +1,6 @@
 """The adapted projection on 4-bit weights at the ends of the types, against float64: infinite and NaN
-adapters, tokens that are not finite beside others of the same adapter.
+adapters, tokens that are not finite beside others of the same adapter, the largest activations and small
+ones.
 
 Tolerances as in test_packed_gpu.py (a rounding to bf16 3e-3 in the norm, sums in fp32 1e-5); what is not
 finite stands where the definition has it, with its sign.
@@ -84,3 +85,39 @@ def test_tokens_of_one_adapter_that_are_not_finite(T, shape, dtype):
     for kind in (torch.isnan, torch.isposinf, torch.isneginf):
         assert torch.equal(kind(Y.double()), kind(Yr))
     assert torch.equal(Y[3:], clean[3:])
+
+
+EVERY = pytest.mark.parametrize("Tn", [1, 3, 9, 16, 20, 50, 64, 200, 300])
+
+
+@BOTH
+@EVERY
+def test_the_largest_activations(T, Tn, dtype):
+    """Codes of -8 (and of 7 in every other row) with scales of 2^-14: 64 products of a code and an
+    activation are 2^9 times the activation, beyond the type's largest number, the result is not."""
+    c, b = 96, 328
+    codes = torch.zeros((c, 192), dtype=torch.uint8, device=DEV)
+    codes[1::2] = 0xFF
+    P = T.PackedWeights(codes, torch.full((6, c), 2.0 ** -14, dtype=BF16, device=DEV), 64, b)
+    W = T.unpack_weights(P, F32).double()
+    X = torch.full((Tn, b), torch.finfo(dtype).max, device=DEV).to(dtype)
+    X[1::2] = -X[1::2]
+    X[2::3, 1::2] *= 0.5
+    want = X.double() @ W.t()
+    assert float(want.abs().max()) < 0.2 * torch.finfo(dtype).max
+    Y, _ = T.adapter_forward(X, P)
+    assert bool(Y.isfinite().all())
+    assert rel(Y.double() * 2.0 ** -100, want * 2.0 ** -100) <= TOL[dtype]
+
+
+@BOTH
+@EVERY
+def test_small_activations(T, Tn, dtype):
+    """bf16 some 2^8 above its smallest normal number, fp32 as far down as three parts of eight bits are
+    bf16 numbers: products with codes are exact, and their sums keep more than the tolerances ask for."""
+    X, W, *_ = make(Tn, 96, 328, 1, 1, dtype, seed=Tn)
+    X = (X.float() * 2.0 ** (-118 if dtype == BF16 else -100)).to(dtype)
+    P = T.pack_weights(4 * W, 64)
+    want = X.double() @ T.unpack_weights(P, F32).double().t()
+    Y, _ = T.adapter_forward(X, P)
+    assert rel(Y.double() * 2.0 ** 100, want * 2.0 ** 100) <= TOL[dtype]
