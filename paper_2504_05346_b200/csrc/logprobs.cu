@@ -236,6 +236,7 @@ struct Shared {
   uint16_t who[LT * QUARTERS];
   uint64_t list[CANDIDATES];
   uint64_t best[MAX_TOP];
+  Sums total;  // for the cluster: the warps' may still be read when it is there
 };
 
 // Columns of this CTA's vectors [v0, v1) with a logit >= bound, at most CANDIDATES of them in list; the
@@ -474,10 +475,10 @@ __global__ void __launch_bounds__(LT, LT == 256 ? 5 : 8) logprobs_kernel(const F
 
   // ---- the row
   if (S > 1) {
-    if (tid == 0) sh.warp[0] = a;
+    if (tid == 0) sh.total = a;
     cluster_sync_all();
     if (rank == 0) {
-      const uint32_t sums = smem_u32(&sh.warp[0]), best = smem_u32(&sh.best[0]);
+      const uint32_t sums = smem_u32(&sh.total), best = smem_u32(&sh.best[0]);
       for (int w = 1; w < S; ++w) {
         const uint32_t at = map_to_cta(sums, w);
         float q[3];

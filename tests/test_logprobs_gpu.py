@@ -391,3 +391,17 @@ def test_offsets_beyond_32_bits(T):
     dl = torch.ones(2100, device=DEV)
     T.token_logprobs_backward(Z, f.stats, target, dl, out=Z)
     assert torch.equal(Z, T.token_logprobs_backward(Zs, f.stats, target, dl))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("Tn, V", [(1, 16384), (2, 40000), (37, 65536), (100, 300001), (147, 32768)])
+def test_rows_of_a_cluster_without_alternatives(T, Tn, V, dtype):
+    """With and without alternatives a row's sums are the same, added in the same order; where a cluster
+    shares a row there are barriers between them in one case only."""
+    Z, target = logits(Tn, V, dtype, seed=V)
+    want = T.token_logprobs(Z, target, 2)
+    check_forward(T, Z, target, 0)
+    for _ in range(50):
+        f = T.token_logprobs(Z, target, 0)
+        for x, y in zip(f[:3], want[:3]):
+            assert torch.equal(x, y)
