@@ -6,6 +6,7 @@ import contextlib
 import ctypes
 import functools
 import os
+import sys
 from dataclasses import dataclass
 from typing import NamedTuple, Optional, Tuple, Union
 
@@ -172,11 +173,14 @@ def load_library():
 
 def _bind_calls(lib):
     """Loads _calls.so beside the library.  It only makes calls shorter: without it, or with one that
-    was built for another torch, they go the long way."""
+    was built for another torch or Python, they go the long way."""
     global _calls
     try:
         from . import _calls as module
     except ImportError:
+        return
+    here = "torch %s, python %d.%d" % ((torch.__version__,) + sys.version_info[:2])
+    if getattr(module, "built_for", None) != here:
         return
     names = ["thanos_" + n for n in (
         "token_logprobs", "token_logprobs_backward", "pack_weights", "unpack_weights",

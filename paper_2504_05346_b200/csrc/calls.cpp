@@ -538,4 +538,9 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nul
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__calls() { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__calls() {
+  PyObject* m = PyModule_Create(&module);
+  // classes of another torch have other layouts, though their symbols may be found
+  if (m && PyModule_AddStringConstant(m, "built_for", THANOS_BUILT_FOR) != 0) Py_CLEAR(m);
+  return m;
+}
