@@ -562,7 +562,8 @@ thanos_status_t thanos_unpack_activations(void* X, int64_t ldx, thanos_dtype_t d
 /*
  * thanos_adapter_forward with packed weights (w_codes, ldq, w_scales and group as above) in the place
  * of W, ldw.  The weights are w^, exactly: 32-bit results are those of 32-bit weights.  Everything else as
- * there; workspace: thanos_adapter_packed_workspace_bytes(0, 1, 0, ...) bytes.
+ * there; workspace: thanos_adapter_packed_workspace_bytes(0, 1, 0, ...) bytes (with many tokens they hold
+ * the weights in bf16, 2 bytes each).
  */
 thanos_status_t thanos_adapter_forward_packed(void* Y, int64_t ldy, float* V, const void* X,
                                               int64_t ldx, const uint8_t* w_codes, int64_t ldq,
@@ -577,7 +578,9 @@ thanos_status_t thanos_adapter_forward_packed(void* Y, int64_t ldy, float* V, co
  * thanos_adapter_backward with packed weights, packed activations or both.  w_scales == NULL: W and ldw
  * as there (group is not read), else W are packed codes and ldw is their ldq.  x_exps == NULL: X and ldx
  * as there, else X are packed codes, ldx is their ldc, and x_exps and lde go with them.
- * workspace: thanos_adapter_packed_workspace_bytes(1, w_scales != NULL, x_exps != NULL, ...) bytes.
+ * workspace: thanos_adapter_packed_workspace_bytes(1, w_scales != NULL, x_exps != NULL, ...) bytes.  They
+ * hold the weights in bf16, 2 bytes each; without dX nothing is unpacked, and in bf16 the bytes for plain
+ * weights (packed_w == 0) are enough.
  */
 thanos_status_t thanos_adapter_backward_packed(void* dX, int64_t lddx, float* dA, float* dB,
                                                int32_t accumulate, const void* dY, int64_t lddy,

@@ -798,7 +798,8 @@ def adapter_backward(dY: torch.Tensor, X: Union[torch.Tensor, PackedActivations,
                 else:
                     _dense(dB, (n, c, r), torch.float32, dev, "dB")
             workspace = _scratch(workspace,
-                                 _packed_workspace(1, int(packed_w), int(packed_x), T, c, b, n, r, dt)
+                                 _packed_workspace(1, int(packed_w and (need_dx or dt == F32)),
+                                                   int(packed_x), T, c, b, n, r, dt)
                                  if packed_w or packed_x else _adapter_workspace(1, T, c, b, n, r, dt),
                                  dY)
         if need_dx:

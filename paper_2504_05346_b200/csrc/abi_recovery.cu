@@ -89,7 +89,7 @@ thanos_status_t packed_activations_ok(const PackedActivations& x, int64_t b) {
   return THANOS_OK;
 }
 
-// Room for packed weights in bf16, behind what the call needs itself (fp32 calls have room for planes).
+// Room for packed weights in bf16, behind what the call needs itself (fp32 calls have room for a plane).
 size_t packed_extra_bytes(int64_t c, int64_t b, thanos_dtype_t dtype) {
   return dtype == THANOS_BF16 ? round_up((size_t)c * round_up((size_t)b, PACKED_LINE) * 2, 256) : 0;
 }
@@ -191,7 +191,8 @@ thanos_status_t backward_call(void* dX, int64_t lddx, float* dA, float* dB, int3
     return THANOS_ERR_ALIGNMENT;
   const size_t need =
       w.is_packed
-          ? thanos_adapter_packed_workspace_bytes(1, 1, x_packed, n_tok, c, b, n_adapters, r, dtype)
+          ? thanos_adapter_packed_workspace_bytes(1, 1, x_packed, n_tok, c, b, n_adapters, r, dtype) -
+                (dX ? 0 : packed_extra_bytes(c, b, dtype))  // without dX nothing is unpacked
           : thanos_adapter_workspace_bytes(1, n_tok, c, b, n_adapters, r, dtype);
   if (!workspace || ws_bytes < need) return THANOS_ERR_WORKSPACE;
   if (n_tok == 0) {
@@ -234,8 +235,11 @@ thanos_status_t backward_call(void* dX, int64_t lddx, float* dA, float* dB, int3
   }
   if (w.is_packed) {
     a.packed = &w.packed;
-    ws_bytes = need - packed_extra_bytes(c, b, dtype);
-    a.unpacked = static_cast<char*>(workspace) + ws_bytes;
+    ws_bytes = need;
+    if (dX) {
+      ws_bytes -= packed_extra_bytes(c, b, dtype);
+      a.unpacked = static_cast<char*>(workspace) + ws_bytes;
+    }
     a.ldw = (int64_t)round_up((size_t)b, PACKED_LINE);
   }
   return adapter_backward_impl(a, workspace, ws_bytes, stream);
@@ -249,7 +253,7 @@ size_t thanos_adapter_workspace_bytes(int32_t backward, int64_t n_tok, int64_t c
                                       int64_t n_adapters, int32_t r, thanos_dtype_t dtype) {
   if (adapter_shape(n_tok, c, b, n_adapters, r, dtype) != THANOS_OK) return 0;
   return adapter_workspace_bytes(backward != 0, n_tok, c, b, n_adapters, n_adapters > 0 ? r : 1,
-                                 dtype);
+                                 dtype, false);
 }
 
 thanos_status_t thanos_adapter_forward(void* Y, int64_t ldy, float* V, const void* X, int64_t ldx,
@@ -288,7 +292,8 @@ size_t thanos_adapter_packed_workspace_bytes(int32_t backward, int32_t packed_w,
   a.r = n_adapters > 0 ? r : 1;
   a.dtype = dtype;
   if (!backward && packed_w && packed_few_tokens(a)) return packed_few_workspace_bytes(n_tok, a.r);
-  return round_up(thanos_adapter_workspace_bytes(backward, n_tok, c, b, n_adapters, r, dtype), 256) +
+  return round_up(adapter_workspace_bytes(backward != 0, n_tok, c, b, n_adapters, a.r, dtype, packed_w != 0),
+                  256) +
          (packed_w ? packed_extra_bytes(c, b, dtype) : 0);
 }
 

@@ -452,8 +452,8 @@ thanos_status_t backward16(const AdapterArgs& a, void* workspace, size_t ws_byte
 }  // namespace
 
 size_t adapter_workspace_bytes(bool backward, int64_t T, int64_t c, int64_t b, int64_t n, int r,
-                               thanos_dtype_t dtype) {
-  if (dtype == THANOS_F32) return adapter_f32_workspace_bytes(backward, T, c, b, n, r);
+                               thanos_dtype_t dtype, bool packed) {
+  if (dtype == THANOS_F32) return adapter_f32_workspace_bytes(backward, T, c, b, n, r, packed);
   size_t need = 256 + round_up((size_t)T * (size_t)r * 4, 256);
   const int64_t nt = proj_pair_tile(T, backward ? b : c), tiles = nt ? ceil_div(T, nt) : 0;
   need += round_up((size_t)tiles * 4, 256) + round_up((size_t)(tiles * nt) * 4, 256);

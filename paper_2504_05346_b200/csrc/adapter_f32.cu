@@ -368,7 +368,8 @@ bool shrink_on_tensor_cores(bool back, int64_t T, int64_t n, int r) {
 }
 
 template <typename Take>
-void layout32(Layout32& L, bool back, int64_t T, int64_t c, int64_t b, int64_t n, int r, Take take) {
+void layout32(Layout32& L, bool back, int64_t T, int64_t c, int64_t b, int64_t n, int r, bool packed,
+              Take take) {
   const int64_t K = back ? c : b;
   // Rows of whole 128-byte lines: TMA fetches a tile's row that straddles two lines twice (c = b =
   // 1000, 2000 tokens: the wide product takes 46 us instead of 78).
@@ -377,7 +378,8 @@ void layout32(Layout32& L, bool back, int64_t T, int64_t c, int64_t b, int64_t n
   L.status = static_cast<int32_t*>(take(256));
   L.R = static_cast<float*>(take((size_t)T * r * 4));
   L.in = static_cast<__nv_bfloat16*>(take((size_t)3 * T * L.k8 * 2));
-  L.w = static_cast<__nv_bfloat16*>(take((size_t)3 * c * L.w8 * 2));
+  // packed weights are bf16 numbers: one plane
+  L.w = static_cast<__nv_bfloat16*>(take((size_t)(packed ? 1 : 3) * c * L.w8 * 2));
   L.p = nullptr;
   if (shrink_on_tensor_cores(back, T, n, r))
     L.p = static_cast<__nv_bfloat16*>(take((size_t)3 * n * r * L.k8 * 2));
@@ -400,10 +402,11 @@ int split_blocks(int64_t rows) {
 
 }  // namespace
 
-size_t adapter_f32_workspace_bytes(bool back, int64_t T, int64_t c, int64_t b, int64_t n, int r) {
+size_t adapter_f32_workspace_bytes(bool back, int64_t T, int64_t c, int64_t b, int64_t n, int r,
+                                   bool packed) {
   size_t total = 0;
   Layout32 L;
-  layout32(L, back, T, c, b, n, r, [&](size_t bytes) -> void* {
+  layout32(L, back, T, c, b, n, r, packed, [&](size_t bytes) -> void* {
     total += round_up(bytes, 256);
     return nullptr;
   });
@@ -413,11 +416,12 @@ size_t adapter_f32_workspace_bytes(bool back, int64_t T, int64_t c, int64_t b, i
 // forward: in = X, out = Y; backward: in = dY, out = dX (may be null)
 thanos_status_t adapter_f32(bool back, const AdapterArgs& a, void* workspace, size_t ws_bytes,
                             cudaStream_t stream) {
-  if (ws_bytes < adapter_f32_workspace_bytes(back, a.T, a.c, a.b, a.n, a.r))
+  const bool packed = a.packed != nullptr;
+  if (ws_bytes < adapter_f32_workspace_bytes(back, a.T, a.c, a.b, a.n, a.r, packed))
     return THANOS_ERR_WORKSPACE;
   char* at = static_cast<char*>(workspace);
   Layout32 L;
-  layout32(L, back, a.T, a.c, a.b, a.n, a.r, [&](size_t bytes) -> void* {
+  layout32(L, back, a.T, a.c, a.b, a.n, a.r, packed, [&](size_t bytes) -> void* {
     void* q = at;
     at += round_up(bytes, 256);
     return q;
@@ -436,7 +440,7 @@ thanos_status_t adapter_f32(bool back, const AdapterArgs& a, void* workspace, si
     f.in.ldp = L.k8;
     f.in.blocks = split_blocks(a.T);
   }
-  if (a.out && !a.packed) {
+  if (a.out && !packed) {
     f.w.src = static_cast<const float*>(a.W);
     f.w.ld = a.ldw;
     f.w.rows = a.c;
@@ -477,8 +481,7 @@ thanos_status_t adapter_f32(bool back, const AdapterArgs& a, void* workspace, si
   if (blocks > 0) {
     front_f32_kernel<<<(unsigned)blocks, 256, 0, stream>>>(f);
     THANOS_CHECK_LAUNCH();
-    // packed weights are bf16 numbers: one plane
-    if (a.out && a.packed)
+    if (a.out && packed)
       THANOS_TRY(unpack_weights(L.w, L.w8, THANOS_BF16, *a.packed, a.c, a.b, stream, true));
     if (tc) {
       ProjArgs s;
@@ -513,7 +516,7 @@ thanos_status_t adapter_f32(bool back, const AdapterArgs& a, void* workspace, si
     g.A = L.w;
     g.lda = L.w8;
     g.a_batch = a.c * L.w8;
-    g.one_plane = a.packed ? 1 : 0;
+    g.one_plane = packed ? 1 : 0;
     g.a_mn = back ? 1 : 0;
     g.B = L.in;
     g.ldb = L.k8;

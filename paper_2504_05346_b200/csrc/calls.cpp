@@ -470,8 +470,8 @@ PyObject* adapter_backward(PyObject*, PyObject* const* a, Py_ssize_t given) {
   const thanos_dtype_t dt = (thanos_dtype_t)p.dt;
   const bool packed = p.is_packed || x_packed;
   const size_t need =
-      packed ? p_thanos_adapter_packed_workspace_bytes(1, p.is_packed, x_packed, p.T, p.c, p.b, p.n,
-                                                       (int32_t)p.r, dt)
+      packed ? p_thanos_adapter_packed_workspace_bytes(1, p.is_packed && (need_dx || dt == THANOS_F32),
+                                                       x_packed, p.T, p.c, p.b, p.n, (int32_t)p.r, dt)
              : p_thanos_adapter_workspace_bytes(1, p.T, p.c, p.b, p.n, (int32_t)p.r, dt);
   if (need == 0) LONG_WAY();
   Tensor dX, dA, dB;

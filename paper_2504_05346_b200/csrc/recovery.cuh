@@ -37,15 +37,17 @@ struct AdapterArgs {
   int r = 0;
 };
 
+// packed: of a call on packed weights, without room for them in bf16.
 size_t adapter_workspace_bytes(bool backward, int64_t T, int64_t c, int64_t b, int64_t n, int r,
-                               thanos_dtype_t dtype);
+                               thanos_dtype_t dtype, bool packed);
 thanos_status_t adapter_forward_impl(const AdapterArgs& a, void* workspace, size_t ws_bytes,
                                      cudaStream_t stream);
 thanos_status_t adapter_backward_impl(const AdapterArgs& a, void* workspace, size_t ws_bytes,
                                       cudaStream_t stream);
 
 // fp32 operands (adapter_f32.cu)
-size_t adapter_f32_workspace_bytes(bool back, int64_t T, int64_t c, int64_t b, int64_t n, int r);
+size_t adapter_f32_workspace_bytes(bool back, int64_t T, int64_t c, int64_t b, int64_t n, int r,
+                                   bool packed);
 thanos_status_t adapter_f32(bool back, const AdapterArgs& a, void* workspace, size_t ws_bytes,
                             cudaStream_t stream);
 

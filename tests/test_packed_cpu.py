@@ -136,3 +136,16 @@ def test_the_short_way_is_built(lib):
     assert binding._calls.adapter_forward(X, X, None, None, None, None) is None
     assert binding._calls.pack_activations(X) is None and binding._calls.token_logprobs(X, None, 1) is None
     assert binding._calls.pack_weights(None, 64) is None and binding._calls.pack_weights(X) is None
+
+
+@pytest.mark.parametrize("backward", [0, 1])
+def test_scratch_holds_the_weights_once(lib, backward):
+    """2 bytes a weight where they are unpacked, in either type, beside what plain operands need without
+    theirs; nothing where they are not."""
+    size, plain = lib.thanos_adapter_packed_workspace_bytes, lib.thanos_adapter_workspace_bytes
+    T, c, b, n, r = 2048, 11008, 4096, 4, 16
+    weights = c * b
+    # fp32: plain weights are three planes of 2 bytes, packed ones are one
+    assert plain(backward, T, c, b, n, r, F32) - size(backward, 1, 0, T, c, b, n, r, F32) >= 4 * weights - 512
+    assert size(backward, 1, 0, T, c, b, n, r, BF16) <= plain(backward, T, c, b, n, r, BF16) + 2 * weights + 512
+    assert size(backward, 0, 1, T, c, b, n, r, BF16) <= plain(backward, T, c, b, n, r, BF16) + 512

@@ -552,3 +552,51 @@ def test_forward_of_tokens_that_share_adapters(T, shape, dtype):
     assert torch.equal(Yb, Yn)
     keep = [t for t in range(Tn) if t != Tn // 2]
     assert torch.equal(Yn[keep], Y[keep])
+
+
+@BOTH
+@pytest.mark.parametrize("shape", [(100, 640, 1032, 3, 16, "mixed"), (300, 515, 520, 0, 0, "one"),
+                                   (1100, 264, 9000, 2, 8, "mixed"), (900, 9001, 136, 2, 12, "mixed")],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_no_more_scratch_than_is_asked_for(T, shape, dtype):
+    """A workspace of the stated size, memory behind it that stays as it is; gradients alone need no room
+    for unpacked weights."""
+    Tn, c, b, n, r, order = shape
+    X, P, W, A, B, index, scale, dY = operands(T, shape, dtype, 64, seed=c)
+    size, dt = T.load_library().thanos_adapter_packed_workspace_bytes, int(dtype == BF16)
+    args = (A, B, index, scale)
+
+    def room(nbytes):
+        buf = torch.full((nbytes + 4096,), 0xAB, dtype=torch.uint8, device=DEV)
+        return buf[:nbytes], buf[nbytes:]
+
+    want, V = T.adapter_forward(X, P, *args)
+    ws, behind = room(size(0, 1, 0, Tn, c, b, n, r, dt))
+    Y, _ = T.adapter_forward(X, P, *args, workspace=ws, check=True)
+    assert torch.equal(Y, want) and bool((behind == 0xAB).all())
+    with pytest.raises(T.ThanosError):
+        T.adapter_forward(X, P, *args, workspace=ws[:-1])
+    X8 = T.pack_activations(X)
+    full = T.adapter_backward(dY, X8, V, P, *args)
+    ws, behind = room(size(1, 1, 1, Tn, c, b, n, r, dt))
+    got = T.adapter_backward(dY, X8, V, P, *args, workspace=ws, check=True)
+    assert bool((behind == 0xAB).all())
+    for x, y in zip(got, full):
+        assert x is y is None or torch.equal(x, y)
+    with pytest.raises(T.ThanosError):
+        T.adapter_backward(dY, X8, V, P, *args, workspace=ws[:-1])
+    if n:
+        ws, behind = room(min(size(1, p, 1, Tn, c, b, n, r, dt) for p in (0, 1)))
+        none, dA, dB = T.adapter_backward(dY, X8, V, P, *args, need_dx=False, workspace=ws, check=True)
+        assert none is None and bool((behind == 0xAB).all())
+        assert torch.equal(dA, full[1]) and torch.equal(dB, full[2])
+        # and that is what a call without a workspace takes
+        del ws, behind
+        torch.cuda.synchronize()
+        torch.cuda.reset_peak_memory_stats()
+        before = torch.cuda.memory_allocated()
+        out = T.adapter_backward(dY, X8, V, P, *args, need_dx=False)
+        held = torch.cuda.memory_allocated() - before
+        assert len(out) == 3
+        assert torch.cuda.max_memory_allocated() - before - held <= min(
+            size(1, p, 1, Tn, c, b, n, r, dt) for p in (0, 1)) + 4096
