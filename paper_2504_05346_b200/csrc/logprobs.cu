@@ -30,8 +30,11 @@ using namespace tc;
 using bf16 = __nv_bfloat16;
 
 constexpr int BT = 256;               // threads of a CTA of the gradient
-constexpr int MAX_TOP = 64;
-constexpr int CANDIDATES = 512;       // >= 8 MAX_TOP: a cluster's lists
+constexpr int MAX_TOP = LOGPROBS_MAX_TOP;
+constexpr int MAX_SPLIT = 8;          // CTAs of a cluster that share a row
+constexpr int CANDIDATES = 512;
+static_assert(CANDIDATES >= MAX_SPLIT * MAX_TOP, "holds a cluster's lists");
+static_assert(2 * MAX_TOP <= 128 && MAX_TOP < BT, "bins of the fewest threads; a named column to a thread");
 constexpr int U = 4;                  // vectors of a thread's batch
 constexpr int QUARTERS = 4;           // a thread's batches in turn, each with a largest logit of its own
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
@@ -686,7 +689,7 @@ thanos_status_t forward(const LogprobsArgs& a, cudaStream_t stream) {
   p.k = a.k;
   // few rows: several CTAs share one, as long as each has some ten thousand bytes of it
   p.split = 1;
-  while (p.split < 8 && a.T * p.split < 2 * NUM_SMS &&
+  while (p.split < MAX_SPLIT && a.T * p.split < 2 * NUM_SMS &&
          a.V * (int64_t)sizeof(T) / p.split >= 16384)
     p.split *= 2;
   cudaLaunchConfig_t cfg = {};
