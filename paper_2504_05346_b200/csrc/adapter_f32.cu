@@ -273,13 +273,13 @@ __global__ void __launch_bounds__(256) grad_f32_kernel(const Grad32Params p) {
       for (int e = threadIdx.x; e < nq; e += 256) tok[e] = p.order[q0 + e];
       __syncthreads();
       // eight loads in flight (one at a time: 34 us for 1000 tokens, 768 + 768 features, three adapters)
-      const int j = threadIdx.x & (RANKS - 1);   // 256 is a multiple of RANKS
+      const int rank = threadIdx.x & (RANKS - 1);   // 256 is a multiple of RANKS
       for (int e0 = threadIdx.x; e0 < nq * RANKS; e0 += 256 * 8) {
         float v[8];
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
           const int e = e0 + 256 * u;
-          v[u] = e < nq * RANKS && j < nj ? sd.R[(int64_t)tok[e / RANKS] * p.r + j0 + j] : 0.f;
+          v[u] = e < nq * RANKS && rank < nj ? sd.R[(int64_t)tok[e / RANKS] * p.r + j0 + rank] : 0.f;
         }
 #pragma unroll
         for (int u = 0; u < 8; ++u)
@@ -294,7 +294,7 @@ __global__ void __launch_bounds__(256) grad_f32_kernel(const Grad32Params p) {
       if (f < sd.F) {
         // sixteen tokens of a warp in flight, added in their order
         constexpr int FLIGHT = 16;
-        for (int q0 = g; q0 < nq; q0 += 8 * FLIGHT) {
+        for (int first = g; first < nq; first += 8 * FLIGHT) {
           float z[FLIGHT];
           if (sd.Z8) {
             // a byte with its sign turned is code + 128, as the low bits of 2^23 a float; a conversion
@@ -302,22 +302,22 @@ __global__ void __launch_bounds__(256) grad_f32_kernel(const Grad32Params p) {
             uint32_t u[FLIGHT];
 #pragma unroll
             for (int k = 0; k < FLIGHT; ++k)
-              u[k] = q0 + 8 * k < nq ? (uint8_t)sd.Z8[(int64_t)tok[q0 + 8 * k] * sd.ldz + f] : 0x80u;
+              u[k] = first + 8 * k < nq ? (uint8_t)sd.Z8[(int64_t)tok[first + 8 * k] * sd.ldz + f] : 0x80u;
 #pragma unroll
             for (int k = 0; k < FLIGHT; ++k)
               z[k] = (__uint_as_float((u[k] ^ 0x80u) | 0x4B000000u) - 8388736.f) *
-                     (q0 + 8 * k < nq ? step[q0 + 8 * k] : 0.f);
+                     (first + 8 * k < nq ? step[first + 8 * k] : 0.f);
           } else {
 #pragma unroll
             for (int k = 0; k < FLIGHT; ++k)
-              z[k] = q0 + 8 * k < nq ? sd.Z[(int64_t)tok[q0 + 8 * k] * sd.ldz + f] : 0.f;
+              z[k] = first + 8 * k < nq ? sd.Z[(int64_t)tok[first + 8 * k] * sd.ldz + f] : 0.f;
           }
 #pragma unroll
           for (int k = 0; k < FLIGHT; ++k) {
-            if (q0 + 8 * k < nq) {
+            if (first + 8 * k < nq) {
 #pragma unroll
               for (int j = 0; j < RANKS; ++j)
-                s[j] = fmaf(fac[(q0 + 8 * k) * RANKS + j], z[k], s[j]);
+                s[j] = fmaf(fac[(first + 8 * k) * RANKS + j], z[k], s[j]);
             }
           }
         }
