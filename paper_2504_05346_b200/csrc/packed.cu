@@ -13,7 +13,7 @@
 // codes numbers by additions to 2^23 and byte permutations (a value at a time, with conversion instructions
 // and divisions, weights took 132 us both ways).  11008 x 4096 in bf16: weights packed in 26.5 us (4.3
 // TB/s) and unpacked in 26.2, activations in 26.4 (5.1 TB/s) and 24.6.  Packing weights issues in 82 % of
-// the cycles.
+// the cycles; unpacking them in 54 %, and half of its warps' time is waiting for loads.
 #include "packed.cuh"
 #include "proj_gemm.cuh"
 

@@ -14,10 +14,15 @@
 // fp32 activations go as three bf16 planes (cut, not rounded: 24 bits in all), three products.
 //
 // mma.sync and not tcgen05: at this width the tensor cores are a fifth busy, and codes that go to tensor
-// memory need a permutation and a multiplication per pair more (packed_tc.cu).  What bounds it is turning
-// codes into numbers: of some 89 instructions for 16 x 64 weights half are integer and a third bf16 ones, at
-// half rate both.  One token: 4096 x 4096 4.7 us, 11008 x 4096 9.6, 28672 x 8192 38 us (3.2 TB/s; without the
-// arithmetic 24, with all loads from L1 35); 16 tokens: 6.8, 11.7 and 45 us.
+// memory need a permutation and a multiplication per pair more (packed_tc.cu).  One token: 4096 x 4096 4.7
+// us, 11008 x 4096 9.6, 28672 x 8192 38 us (3.2 TB/s); 16 tokens: 6.8, 11.7 and 45 us.  The last of each comes
+// from memory, the others, replayed, from L2; over a set of layers larger than L2 they take up to 0.5 us
+// more.
+// What bounds it: loads and decoding, neither full, that overlap in part only.  28672 x 8192 takes 24 us
+// without the arithmetic and 35 with all loads from L1.  Of some 89 instructions for 16 x 64 weights half are
+// integer and a third bf16 ones, at half rate both; the issue slots are 56 % used, and of a warp's time 38 %
+// is waiting for loads: registers hold what is in flight, and 64 to 128 of them leave 16 to 32 warps on an
+// SM.  16 tokens with adapters: 30 % of the slots, 55 % of the time; latency.
 #include "packed_few.cuh"
 
 namespace thanos {
@@ -338,13 +343,26 @@ thanos_status_t forward_few(const FewParams& p, cudaStream_t stream) {
 
 // Up to here the codes are turned into weights where they meet the activations; with more tokens they are
 // unpacked once and multiplied as they would be from memory.  Replayed, both ways:
-//   4096 x 4096     128 tokens   12.7 and 20.8 us    256 tokens   17.5 and 24.7 us
-//   4096 x 11008    128 tokens   21.6 and 54.9       256 tokens   34.5 and 62.7
-//   11008 x 4096    128 tokens   25.1 and 51.5       256 tokens   49.8 and 61.4    384 tokens  49.7 and 81.6
-//   256 tokens with adapters:    4096 x 4096, 8 of rank 16, 31.5 and 31.7; 2 of rank 64, 45 and 97; 4096 x
-//     11008, 16 of rank 16, 58 and 70; 11008 x 4096, 16 of rank 16, 82 and 78; 4 of rank 64, 90 and 82
+//   4096 x 4096     128 tokens   12.7 and 20.8 us    256 tokens   17.4 and 24.8 us
+//   4096 x 11008    128 tokens   21.6 and 54.9       256 tokens   34.1 and 63.7
+//   11008 x 4096    128 tokens   25.1 and 51.5       256 tokens   49.7 and 63.0    384 tokens  49.7 and 81.6
+//   1024 x 4096                                      256 tokens   18.5 and 14.4
+//   with adapters, 256 tokens    16 of rank 16    4 of rank 64    8 of rank 12
+//     1024 x 4096                 29 and  23       66 and  46      31 and  22
+//     4096 x 4096                 32 and  34       49 and  74      36 and  31
+//     4096 x 11008                57 and  70       97 and 126      58 and  66
+//     8192 x 8192                 72 and 102      102 and 199      77 and  99
+//     11008 x 4096                81 and  79      111 and  83      95 and  73
+//     28672 x 8192               271 and 274      316 and 280     294 and 263
+//     12288 x 2048, three of rank 20: 88 and 44
 //   320 tokens:     4096 x 4096, 8 of rank 16, 44 and 39;  4096 x 11008, 16 of rank 16, 102 and 78
-//   fp32 2048 x 2048, 64 tokens   15.8 and 31.7;  768 x 768, 64 tokens   4.9 and 15.2
+//   fp32            2048 x 2048, 64 tokens   15.8 and 31.7;  768 x 768, 64 tokens   4.9 and 15.2;  11008 x
+//     4096, 16 tokens 32, 64 tokens 97, 65 (unpacked) 77
+// The number of tokens is all it looks at.  Over 288 sizes with adapters and 136 to 256 tokens 256 is the
+// better limit in the mean (6 % above the faster way for each size; 128: 19 %), but not for each: few rows,
+// ranks that are no multiple of 8, and tiles that fill little more than half of the SMs twice (11008 rows)
+// lose to unpacking, up to the half of their time.  Rules on rows, tokens and rank that fit one half of the
+// sizes did not fit the other: what decides is the shape of both launches.
 bool packed_few_tokens(const AdapterArgs& a) { return a.T <= (a.dtype == THANOS_F32 ? 64 : 256); }
 
 size_t packed_few_workspace_bytes(int64_t T, int r) { return 256 + round_up((size_t)T * r * 4, 256); }

@@ -16,8 +16,9 @@
 // What bounds it is turning codes into bf16: 19 instructions for eight weights (shift, mask, subtract,
 // multiply, and a permutation, because a word gives the columns j and j + 4 at once and an activation's
 // columns come as they are), most of them at half rate; 128 x 64 weights take an SM some 480 clocks, and
-// the tensor cores are a quarter busy.  64 tokens: 4096 x 4096 10.5 us, 11008 x 4096 17.6, 28672 x 8192
-// 60 us.
+// the tensor cores are a quarter busy.  The issue slots are 56 % used: with four warps to a scheduler, each
+// waiting for its own last result, a pipe or a load in turn, there is not always one that can go on.  64
+// tokens: 4096 x 4096 10.5 us, 11008 x 4096 17.6, 28672 x 8192 60 us.
 #include <type_traits>
 
 #include "packed_few.cuh"
