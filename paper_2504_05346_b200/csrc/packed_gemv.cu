@@ -10,7 +10,8 @@
 //   scale  the block's products are summed apart and multiplied by the row's scale in fp32: four
 //          multiplications per 16 x 8 tile and block instead of one per weight.  64 products of up to 8 x
 //          are 2^9 x, which is what the codes' 2^-9 is for: a sum does not leave fp32's range where w^
-//          would not, and the results take it back, exactly
+//          would not, and the results take it back, exactly (those below 2^-117 had fewer bits to be
+//          held in)
 // fp32 activations go as three bf16 planes (cut, not rounded: 24 bits in all), three products.
 //
 // mma.sync and not tcgen05: at this width the tensor cores are a fifth busy, and codes that go to tensor
