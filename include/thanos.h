@@ -562,8 +562,9 @@ thanos_status_t thanos_unpack_activations(void* X, int64_t ldx, thanos_dtype_t d
 /*
  * thanos_adapter_forward with packed weights (w_codes, ldq, w_scales and group as above) in the place
  * of W, ldw.  The weights are w^, exactly: 32-bit results are those of 32-bit weights (with few tokens a sum
- * is held as 2^-9 of itself: results below 2^-117 have fewer bits).  Everything else as there; workspace: thanos_adapter_packed_workspace_bytes(0, 1, 0, ...) bytes (with many tokens they hold
- * the weights in bf16, 2 bytes each).
+ * is held as 2^-9 of itself: results below 2^-117 have fewer bits).  Everything else as there; workspace:
+ * thanos_adapter_packed_workspace_bytes(0, 1, 0, ...) bytes (with many tokens they hold the weights in bf16,
+ * 2 bytes each).
  */
 thanos_status_t thanos_adapter_forward_packed(void* Y, int64_t ldy, float* V, const void* X,
                                               int64_t ldx, const uint8_t* w_codes, int64_t ldq,
